@@ -1,4 +1,4 @@
-"""ctypes binding of include/dmi.h: same names, argument marshalling only.
+"""ctypes binding of include/dmi.h and include/dmi_kv8.h: same names, argument marshalling only.
 
 Every step of the capture-and-stage path runs inside libdmi.so.  There is no
 fallback: if the library is missing or no GPU is present the calls raise.
@@ -190,6 +190,16 @@ def lib():
     L.dmi_observe_into.argtypes = [C.c_uint32, P(Tensor), P(Selection), P(Transform), C.c_uint64, C.c_uint64,
                                    C.c_uint32, C.c_void_p, C.c_uint64, P(C.c_uint64), C.c_void_p]
     L.dmi_observe_into.restype = C.c_int32
+    # (the structs of dmi_kv8.h go as bytes: see KV8)
+    S = C.c_char_p
+    L.dmi_kv8_append.argtypes = [S, S, S, S, C.c_void_p]
+    L.dmi_kv8_attend_workspace.argtypes = [S, S, C.c_uint32, C.c_int]
+    L.dmi_kv8_attend_workspace.restype = C.c_uint64
+    L.dmi_kv8_attend.argtypes = [S, S, S, C.c_uint32, C.c_float, S, C.c_void_p, S, S, C.c_float, C.c_void_p, C.c_uint64,
+                                 C.c_void_p]
+    L.dmi_kv8_evict.argtypes = [S, S, S, S, S, C.c_uint32, C.c_uint32, C.c_void_p, C.c_void_p, C.c_void_p]
+    for name in ("dmi_kv8_append", "dmi_kv8_attend", "dmi_kv8_evict"):
+        getattr(L, name).restype = C.c_int32
     L.dmi_drain.argtypes = [C.c_void_p, C.c_uint32, P(C.c_uint64)]
     L.dmi_poll_host.argtypes = [C.c_void_p, P(RecordViewC), C.c_uint32, P(C.c_uint32)]
     L.dmi_release_host.argtypes = [C.c_void_p, C.c_uint64]
@@ -733,3 +743,148 @@ class Ring:
         a, b = C.c_uint64(0), C.c_uint64(0)
         _check(lib().dmi_debug_exporter_allocs(self._h, C.byref(a), C.byref(b)))
         return a.value, b.value
+
+
+# ---------------------------------------------------------------- the 8-bit KV cache (include/dmi_kv8.h)
+# The structs as bytes, padding included, packed once for what stays and per call for what does not.
+_PACK_KV8 = struct.Struct("=QQQQqqqqqIIIIIIQq").pack
+_PACK_KV8_BATCH = struct.Struct("=IIIIQQQ").pack
+_PACK_KV8_HEADS = struct.Struct("=QI4xqq").pack
+_PACK_KV8_WEIGHT = struct.Struct("=Qqq").pack
+
+
+def _typed(t, what, dtype, dims):
+    import torch
+    if t.dtype != getattr(torch, dtype) or t.dim() != dims:
+        raise ValueError(f"{what} must be {dtype} with {dims} dimensions")
+    if t.stride(-1) != 1 and t.shape[-1] > 1:
+        raise ValueError(f"the last dimension of {what} must be contiguous")
+    return t
+
+
+class KV8:
+    """A paged cache in 8 bits (dmi_kv8_t) over the caller's tensors, which it keeps.
+
+    k, v: [blocks, slots, heads, dim], torch.uint8 or torch.float8_e4m3fn, any strides that dmi_kv8.h allows (the same for both);
+    k_scale, v_scale: fp32 [blocks, heads], the same strides; block_table: int32 [n_seqs, max_blocks]."""
+
+    def __init__(self, k, v, k_scale, v_scale, block_table):
+        import torch
+        for t, what in ((k, "k"), (v, "v")):
+            if t.dtype not in (torch.uint8, torch.float8_e4m3fn) or t.dim() != 4 or t.stride(3) != 1:
+                raise ValueError(f"{what} must be uint8 or float8_e4m3fn [blocks, slots, heads, dim] with contiguous rows")
+        for t, what in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+            if t.dtype != torch.float32 or t.dim() != 2:
+                raise ValueError(f"{what} must be float32 [blocks, heads]")
+        _typed(block_table, "block_table", "int32", 2)
+        if k.shape != v.shape or k.stride() != v.stride() or k_scale.stride() != v_scale.stride() \
+                or any(tuple(t.shape) != (k.shape[0], k.shape[2]) for t in (k_scale, v_scale)):
+            raise ValueError("k and v must share shape and strides, and so must their scales, [blocks, heads]")
+        self.k, self.v, self.k_scale, self.v_scale, self.block_table = k, v, k_scale, v_scale, block_table
+        self.n_heads, self.head_dim, self.block_size = k.shape[2], k.shape[3], k.shape[1]
+        self._raw = _PACK_KV8(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), k.stride(0), k.stride(1),
+                              k.stride(2), k_scale.stride(0), k_scale.stride(1), k.shape[1], k.shape[2], k.shape[3], k.shape[0],
+                              block_table.shape[0], block_table.shape[1], block_table.data_ptr(),
+                              max(block_table.stride(0), block_table.shape[1]))
+
+
+class KV8Batch:
+    """The requests of a call (dmi_kv8_batch_t): int32 device tensors lens [n_reqs], starts [n_reqs + 1] or None (one new token
+    each), rows [n_reqs] or None, and the host's bounds.  Their contents may change between calls, within the bounds."""
+
+    def __init__(self, lens, *, max_len: int, starts=None, rows=None, total_new: Optional[int] = None, max_new: int = 1):
+        n = lens.shape[0]
+        for t, what, size in ((lens, "lens", n), (starts, "starts", n + 1), (rows, "rows", n)):
+            if t is not None and _typed(t, what, "int32", 1).shape[0] != size:
+                raise ValueError(f"{what} must have {size} entries")
+        if total_new is None:
+            if starts is not None:
+                raise ValueError("starts without total_new")
+            total_new = n
+        self.lens, self.starts, self.rows = lens, starts, rows
+        self.n_reqs, self.total_new, self.max_new, self.max_len = n, total_new, max_new, max_len
+        self._raw = _PACK_KV8_BATCH(n, total_new, max_new, max_len, lens.data_ptr(), 0 if starts is None else starts.data_ptr(),
+                                    0 if rows is None else rows.data_ptr())
+
+
+def _kv8_heads(t, what, rows, heads, dim):
+    shape = t.shape
+    if len(shape) != 3 or shape[0] < rows or shape[1] != heads or shape[2] != dim:
+        raise ValueError(f"{what} must be [{rows}, {heads}, {dim}], not {list(shape)}")
+    stride = t.stride()
+    if stride[2] != 1:
+        raise ValueError(f"the last dimension of {what} must be contiguous")
+    return _PACK_KV8_HEADS(t.data_ptr(), _torch_dtype_code(t), stride[0], stride[1])
+
+
+def _kv8_weight(t, what, rows, heads, positions):
+    if t is None:
+        return None
+    _typed(t, what, "float32", 3)
+    shape, stride = t.shape, t.stride()
+    if shape[0] < rows or shape[1] != heads or shape[2] < positions:
+        raise ValueError(f"{what} must be [{rows}, {heads}, {positions}] or longer, not {list(shape)}")
+    return _PACK_KV8_WEIGHT(t.data_ptr(), stride[0], stride[1])
+
+
+def kv8_append(cache: KV8, batch: KV8Batch, key, value, *, stream: int = 0) -> None:
+    """dmi_kv8_append: key, value [total_new, heads, dim], bf16 / fp16 / fp32, into the cache."""
+    k = _kv8_heads(key, "key", batch.total_new, cache.n_heads, cache.head_dim)
+    v = _kv8_heads(value, "value", batch.total_new, cache.n_heads, cache.head_dim)
+    _check(lib().dmi_kv8_append(cache._raw, batch._raw, k, v, stream or None))
+
+
+def kv8_attend_workspace(cache: KV8, batch: KV8Batch, n_q_heads: int, with_weight: bool) -> int:
+    """Bytes of workspace that kv8_attend takes."""
+    return int(lib().dmi_kv8_attend_workspace(cache._raw, batch._raw, n_q_heads, int(with_weight)))
+
+
+def _scratch(n, like, stream):
+    """n bytes from torch's allocator, in the order of `stream`."""
+    import torch
+    if torch.cuda.current_stream(like.device).cuda_stream == stream:
+        return torch.empty(n, dtype=torch.uint8, device=like.device)
+    with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=like.device)):
+        return torch.empty(n, dtype=torch.uint8, device=like.device)
+
+
+def kv8_attend(cache: KV8, batch: KV8Batch, q, out, *, scale: Optional[float] = None, lse=None, weight=None, prior=None,
+               decay: float = 1.0, workspace=None, stream: int = 0) -> None:
+    """dmi_kv8_attend: q, out [total_new, query heads, dim], bf16 or fp16; lse fp32 [total_new, query heads]; weight, prior fp32
+    [n_seqs, heads, positions].  scale: dim ** -0.5 if not given.  workspace: uint8; without one it comes from torch's allocator."""
+    n, heads = batch.total_new, q.shape[1]
+    if weight is None and prior is not None:
+        raise ValueError("prior without weight")
+    if lse is not None and (tuple(lse.shape) != (n, heads) or not lse.is_contiguous()):
+        raise ValueError(f"lse must be contiguous [{n}, {heads}]")
+    if lse is not None and _torch_dtype_code(lse) != DT_FP32:
+        raise ValueError("lse must be float32")
+    raw_q = _kv8_heads(q, "q", n, heads, cache.head_dim)
+    raw_out = _kv8_heads(out, "out", n, heads, cache.head_dim)
+    rows = cache.block_table.shape[0]
+    raw_weight = _kv8_weight(weight, "weight", rows, cache.n_heads, batch.max_len)
+    raw_prior = _kv8_weight(prior, "prior", rows, cache.n_heads, batch.max_len)
+    if workspace is None:
+        need = lib().dmi_kv8_attend_workspace(cache._raw, batch._raw, heads, weight is not None)
+        if need:
+            workspace = _scratch(need, q, stream)
+    _check(lib().dmi_kv8_attend(cache._raw, batch._raw, raw_q, heads, cache.head_dim ** -0.5 if scale is None else scale, raw_out,
+                                None if lse is None else lse.data_ptr(), raw_weight, raw_prior, decay,
+                                None if workspace is None else workspace.data_ptr(),
+                                0 if workspace is None else workspace.numel() * workspace.element_size(), stream or None))
+
+
+def kv8_evict(cache: KV8, batch: KV8Batch, weight, to: KV8, to_weight, *, keep: int, recent: int, positions, lens,
+              stream: int = 0) -> None:
+    """dmi_kv8_evict: weight fp32 [n_seqs, heads, positions] of the cache's tokens; what is kept goes into `to`, to_weight (the
+    same layout, at least `keep` positions), positions int32 [n_reqs, heads, keep] and lens int32 [n_reqs]."""
+    rows = cache.block_table.shape[0]
+    raw_weight = _kv8_weight(weight, "weight", rows, cache.n_heads, batch.max_len)
+    raw_to_weight = _kv8_weight(to_weight, "to_weight", rows, cache.n_heads, min(keep, batch.max_len))
+    _typed(positions, "positions", "int32", 3)
+    _typed(lens, "lens", "int32", 1)
+    if tuple(positions.shape) != (batch.n_reqs, cache.n_heads, keep) or not positions.is_contiguous() \
+            or lens.shape[0] != batch.n_reqs:
+        raise ValueError(f"positions must be contiguous [{batch.n_reqs}, {cache.n_heads}, {keep}] and lens [{batch.n_reqs}]")
+    _check(lib().dmi_kv8_evict(cache._raw, batch._raw, raw_weight, to._raw, raw_to_weight, keep, recent, positions.data_ptr(),
+                               lens.data_ptr(), stream or None))

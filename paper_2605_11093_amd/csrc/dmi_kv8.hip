@@ -1,0 +1,168 @@
+// The C entry points of the operators on the 8-bit KV cache: arguments checked, kernels' arguments made.
+#include "dmi_ring.h"
+#include "dmi_kv8_internal.h"
+
+#include <cmath>
+
+using namespace dmi;
+using namespace dmi::host;
+using namespace dmi::kv8;
+
+namespace {
+
+// A stride that moves rows by whole 16-byte units
+bool whole(int64_t stride, uint32_t size) { return (stride * (int64_t)size) % 16 == 0; }
+
+dmi_status_t check_cache(const dmi_kv8_t *k, const char *what, Cache &c)
+{
+    if (!k) return fail(DMI_ERR_INVALID_ARG, "%s is NULL", what);
+    if (!k->k || !k->v || !k->k_scale || !k->v_scale || !k->block_table_dev)
+        return fail(DMI_ERR_INVALID_ARG, "%s: codes, scales or block table are NULL", what);
+    if ((uintptr_t)k->k % 16u || (uintptr_t)k->v % 16u || !whole(k->block_stride, 1) || !whole(k->slot_stride, 1) ||
+        !whole(k->head_stride, 1))
+        return fail(DMI_ERR_INVALID_ARG, "%s: codes must be 16-byte aligned with strides that are multiples of 16", what);
+    if ((uintptr_t)k->k_scale % 4u || (uintptr_t)k->v_scale % 4u || (uintptr_t)k->block_table_dev % 4u)
+        return fail(DMI_ERR_INVALID_ARG, "%s: scales and block table must be 4-byte aligned", what);
+    if (!k->block_size || k->block_size % 16u || k->block_size > kMaxBlock)
+        return fail(DMI_ERR_INVALID_ARG, "%s: block_size %u is not a multiple of 16 up to %u", what, k->block_size, kMaxBlock);
+    if (!k->head_dim || k->head_dim % 16u || k->head_dim > kMaxDim)
+        return fail(DMI_ERR_INVALID_ARG, "%s: head_dim %u is not a multiple of 16 up to %u", what, k->head_dim, kMaxDim);
+    if (!k->n_heads || k->n_heads > 1024u) return fail(DMI_ERR_INVALID_ARG, "%s: n_heads %u is not in 1..1024", what, k->n_heads);
+    if (!k->n_blocks || k->n_blocks > (1u << 30) || !k->n_seqs || k->n_seqs > (1u << 30) || !k->max_blocks ||
+        k->max_blocks > kMaxLen || k->block_table_stride < (int64_t)k->max_blocks)
+        return fail(DMI_ERR_INVALID_ARG, "%s: bad n_blocks, n_seqs, max_blocks or block_table_stride", what);
+    c = Cache{{static_cast<uint8_t *>(k->k), static_cast<uint8_t *>(k->v)}, {k->k_scale, k->v_scale}, k->block_table_dev,
+              k->block_stride, k->slot_stride, k->head_stride, k->scale_block_stride, k->scale_head_stride, k->block_table_stride,
+              k->block_size, k->n_heads, k->head_dim, k->n_blocks, k->n_seqs, k->max_blocks, 0u};
+    const uint32_t d = k->block_size / 16u;
+    c.per_block = ((1u << 31) + d - 1u) / d;
+    return DMI_OK;
+}
+
+dmi_status_t check_batch(const dmi_kv8_batch_t *k, const Cache &c, bool fresh, Batch &b)
+{
+    if (!k) return fail(DMI_ERR_INVALID_ARG, "batch is NULL");
+    if (k->n_reqs > kMaxReqs) return fail(DMI_ERR_INVALID_ARG, "n_reqs %u is more than %u", k->n_reqs, kMaxReqs);
+    if (k->n_reqs && !k->lens_dev) return fail(DMI_ERR_INVALID_ARG, "lens_dev is NULL");
+    if (((uintptr_t)k->lens_dev | (uintptr_t)k->starts_dev | (uintptr_t)k->rows_dev) % 4u)
+        return fail(DMI_ERR_INVALID_ARG, "lens_dev, starts_dev and rows_dev must be 4-byte aligned");
+    if (k->max_len > kMaxLen || (uint64_t)k->max_len > (uint64_t)c.max_blocks * c.bs)
+        return fail(DMI_ERR_INVALID_ARG, "max_len %u is more than the block table's %u blocks of %u tokens, or than %u", k->max_len,
+                    c.max_blocks, c.bs, kMaxLen);
+    if (!k->rows_dev && k->n_reqs > c.n_seqs)
+        return fail(DMI_ERR_INVALID_ARG, "n_reqs %u is more than the block table's %u rows", k->n_reqs, c.n_seqs);
+    if (fresh && (k->total_new > (1u << 30) || k->max_new > kMaxLen))
+        return fail(DMI_ERR_INVALID_ARG, "total_new %u or max_new %u is too large", k->total_new, k->max_new);
+    if (fresh && !k->starts_dev && (k->total_new != k->n_reqs || k->max_new != 1u))
+        return fail(DMI_ERR_INVALID_ARG, "without starts_dev there is one new token a request");
+    b = Batch{k->lens_dev, k->starts_dev, k->rows_dev, k->n_reqs, k->total_new, k->max_new, k->max_len};
+    return DMI_OK;
+}
+
+dmi_status_t check_rows(const dmi_kv8_heads_t *k, const char *what, const Batch &b, Rows &r)
+{
+    if (!k || (!k->data && b.total_new)) return fail(DMI_ERR_INVALID_ARG, "%s is NULL", what);
+    const uint32_t size = dtype_size(k->dtype);
+    if (size < 2u) return fail(DMI_ERR_INVALID_ARG, "%s: unsupported dtype %u", what, k->dtype);
+    if ((uintptr_t)k->data % 16u || !whole(k->row_stride, size) || !whole(k->head_stride, size))
+        return fail(DMI_ERR_INVALID_ARG, "%s must be 16-byte aligned with strides that are multiples of 16 bytes", what);
+    r = Rows{k->data, k->row_stride, k->head_stride};
+    return DMI_OK;
+}
+
+dmi_status_t check_weight(const dmi_kv8_weight_t *k, const char *what, Weight &w)
+{
+    w = Weight{nullptr, 0, 0};
+    if (!k) return DMI_OK;
+    if (!k->data || (uintptr_t)k->data % 4u) return fail(DMI_ERR_INVALID_ARG, "%s: data is NULL or not 4-byte aligned", what);
+    w = Weight{k->data, k->row_stride, k->head_stride};
+    return DMI_OK;
+}
+
+dmi_status_t launched(hipError_t e)
+{
+    return e == hipSuccess ? DMI_OK : fail(DMI_ERR_HIP, "launch failed: %s", hipGetErrorString(e));
+}
+
+}  // namespace
+
+extern "C" dmi_status_t dmi_kv8_append(const dmi_kv8_t *cache, const dmi_kv8_batch_t *batch, const dmi_kv8_heads_t *key,
+                                       const dmi_kv8_heads_t *value, void *hip_stream)
+{
+    AppendArgs a;
+    dmi_status_t st;
+    if ((st = check_cache(cache, "cache", a.c)) != DMI_OK || (st = check_batch(batch, a.c, true, a.b)) != DMI_OK ||
+        (st = check_rows(key, "key", a.b, a.x[0])) != DMI_OK || (st = check_rows(value, "value", a.b, a.x[1])) != DMI_OK)
+        return st;
+    if (key->dtype != value->dtype) return fail(DMI_ERR_INVALID_ARG, "key and value have different dtypes");
+    if (!a.b.n_reqs || !a.b.total_new || !a.b.max_new || !a.b.max_len) return DMI_OK;
+    a.touched = (a.b.max_new + a.c.bs - 2u) / a.c.bs + 1u;
+    return launched(launch_append(a, key->dtype, (hipStream_t)hip_stream));
+}
+
+extern "C" uint64_t dmi_kv8_attend_workspace(const dmi_kv8_t *cache, const dmi_kv8_batch_t *batch, uint32_t n_q_heads,
+                                             int with_weight)
+{
+    if (!cache || !batch) return 0;
+    return with_weight ? pad64((uint64_t)batch->total_new * n_q_heads * 4u) : 0u;
+}
+
+extern "C" dmi_status_t dmi_kv8_attend(const dmi_kv8_t *cache, const dmi_kv8_batch_t *batch, const dmi_kv8_heads_t *q,
+                                       uint32_t n_q_heads, float scale, const dmi_kv8_heads_t *out, float *lse_dev,
+                                       const dmi_kv8_weight_t *weight, const dmi_kv8_weight_t *prior, float decay,
+                                       void *workspace, uint64_t workspace_bytes, void *hip_stream)
+{
+    AttendArgs a;
+    dmi_status_t st;
+    if ((st = check_cache(cache, "cache", a.c)) != DMI_OK || (st = check_batch(batch, a.c, true, a.b)) != DMI_OK ||
+        (st = check_rows(q, "q", a.b, a.q)) != DMI_OK || (st = check_rows(out, "out", a.b, a.out)) != DMI_OK ||
+        (st = check_weight(weight, "weight", a.w)) != DMI_OK || (st = check_weight(prior, "prior", a.prior)) != DMI_OK)
+        return st;
+    if (q->dtype != out->dtype || (q->dtype != DMI_DTYPE_BF16 && q->dtype != DMI_DTYPE_FP16))
+        return fail(DMI_ERR_INVALID_ARG, "q and out must both be BF16 or both FP16");
+    if (!n_q_heads || n_q_heads % a.c.heads || n_q_heads > 65536u)
+        return fail(DMI_ERR_INVALID_ARG, "%u query heads do not share %u heads evenly", n_q_heads, a.c.heads);
+    if (!std::isfinite(scale)) return fail(DMI_ERR_INVALID_ARG, "scale is not finite");
+    if ((uintptr_t)lse_dev % 4u) return fail(DMI_ERR_INVALID_ARG, "lse_dev must be 4-byte aligned");
+    if (a.prior.data && !a.w.data) return fail(DMI_ERR_INVALID_ARG, "prior without weight");
+    if (a.prior.data && !std::isfinite(decay)) return fail(DMI_ERR_INVALID_ARG, "decay is not finite");
+    const uint64_t need = dmi_kv8_attend_workspace(cache, batch, n_q_heads, weight != nullptr);
+    if (need && (!workspace || (uintptr_t)workspace % 256u || workspace_bytes < need))
+        return fail(DMI_ERR_INVALID_ARG, "workspace must be 256-byte aligned and hold %llu bytes", (unsigned long long)need);
+    if (!a.b.n_reqs || !a.b.max_new || !a.b.total_new) return DMI_OK;
+    a.lse = lse_dev;
+    a.decay = a.prior.data ? decay : 0.0f;
+    a.scale_log2 = scale * 1.44269504088896340736f;
+    a.group = n_q_heads / a.c.heads;
+    a.q_heads = n_q_heads;
+    return launched(launch_attend(a, q->dtype, need ? static_cast<float *>(workspace) : nullptr, (hipStream_t)hip_stream));
+}
+
+extern "C" dmi_status_t dmi_kv8_evict(const dmi_kv8_t *cache, const dmi_kv8_batch_t *batch, const dmi_kv8_weight_t *weight,
+                                      const dmi_kv8_t *to, const dmi_kv8_weight_t *to_weight, uint32_t keep, uint32_t recent,
+                                      int32_t *positions_dev, int32_t *to_lens_dev, void *hip_stream)
+{
+    EvictArgs a;
+    dmi_status_t st;
+    if ((st = check_cache(cache, "cache", a.c)) != DMI_OK || (st = check_cache(to, "to", a.to)) != DMI_OK ||
+        (st = check_batch(batch, a.c, false, a.b)) != DMI_OK || (st = check_weight(weight, "weight", a.w)) != DMI_OK ||
+        (st = check_weight(to_weight, "to_weight", a.to_w)) != DMI_OK)
+        return st;
+    if (!a.w.data || !a.to_w.data) return fail(DMI_ERR_INVALID_ARG, "weight or to_weight is NULL");
+    if (a.to.heads != a.c.heads || a.to.dim != a.c.dim || a.to.bs != a.c.bs)
+        return fail(DMI_ERR_INVALID_ARG, "cache and to differ in n_heads, head_dim or block_size");
+    if (a.to.n_seqs < a.c.n_seqs) return fail(DMI_ERR_INVALID_ARG, "to's block table has fewer rows than the cache's");
+    if (!keep || recent > keep) return fail(DMI_ERR_INVALID_ARG, "keep %u must be positive and recent %u no more", keep, recent);
+    if (keep > kMaxLen || (uint64_t)keep > (uint64_t)a.to.max_blocks * a.to.bs)
+        return fail(DMI_ERR_INVALID_ARG, "keep %u is more than to's %u blocks of %u tokens, or than %u", keep, a.to.max_blocks, a.to.bs, kMaxLen);
+    if (!positions_dev || !to_lens_dev || (uintptr_t)positions_dev % 4u || (uintptr_t)to_lens_dev % 4u)
+        return fail(DMI_ERR_INVALID_ARG, "positions_dev or to_lens_dev is NULL or not 4-byte aligned");
+    if (to_lens_dev == batch->lens_dev) return fail(DMI_ERR_INVALID_ARG, "to_lens_dev is lens_dev");
+    if (!a.b.n_reqs) return DMI_OK;
+    a.b.starts = nullptr;
+    a.keep = keep;
+    a.recent = recent;
+    a.positions = positions_dev;
+    a.to_lens = to_lens_dev;
+    return launched(launch_evict(a, (hipStream_t)hip_stream));
+}
