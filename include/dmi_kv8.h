@@ -34,7 +34,7 @@ extern "C" {
 /* The cache.  Element (block b, slot s, head h, dim d) of K or V is the code at
  * base + b*block_stride + s*slot_stride + h*head_stride + d (strides in bytes, the same for K and V); it stands for
  * number(code) * scale, scale at scale_base + b*scale_block_stride + h*scale_head_stride (in floats), positive and finite.
- * k, v 16-byte aligned, strides multiples of 16 bytes.  block_size: a multiple of 16, at most 1024.  head_dim: a multiple of 16, at
+ * k, v 16-byte aligned, strides multiples of 16 bytes, slot_stride from 0 to 2^26.  block_size: a multiple of 16, at most 1024.  head_dim: a multiple of 16, at
  * most 256.  block_table_dev [device] int32 [n_seqs][block_table_stride], of which max_blocks columns are used: physical
  * block of logical block t / block_size of a sequence. */
 typedef struct {
@@ -93,7 +93,7 @@ dmi_status_t dmi_kv8_append(const dmi_kv8_t *cache /*[host]*/, const dmi_kv8_bat
  * Causal attention of the new tokens over the cache (which holds them: append first).  Query i of a request's n new tokens
  * sees positions t <= len - n + i.  Query heads h*g .. h*g+g-1 read head h of the cache, g = n_q_heads / n_heads.
  *     z_t = scale * q . k_t,   p = softmax(z),   out = sum_t p_t v_t,   lse = log sum_t exp(z_t)
- * A query that sees nothing gives out = 0 and lse = -inf.  A NaN in K makes the queries that see it NaN, a NaN in V that
+ * A query that sees nothing (or no score above -inf) gives out = 0 and lse = -inf.  A NaN in K makes the queries that see it NaN, a NaN in V that
  * element of theirs.
  *   q, out     BF16 or FP16, the same; total_new rows of n_q_heads heads
  *   lse_dev    [device, optional] fp32 [total_new][n_q_heads]

@@ -21,6 +21,8 @@ dmi_status_t check_cache(const dmi_kv8_t *k, const char *what, Cache &c)
     if ((uintptr_t)k->k % 16u || (uintptr_t)k->v % 16u || !whole(k->block_stride, 1) || !whole(k->slot_stride, 1) ||
         !whole(k->head_stride, 1))
         return fail(DMI_ERR_INVALID_ARG, "%s: codes must be 16-byte aligned with strides that are multiples of 16", what);
+    if (k->slot_stride < 0 || k->slot_stride > kMaxSlotStride)
+        return fail(DMI_ERR_INVALID_ARG, "%s: slot_stride is not in 0..%lld", what, (long long)kMaxSlotStride);
     if ((uintptr_t)k->k_scale % 4u || (uintptr_t)k->v_scale % 4u || (uintptr_t)k->block_table_dev % 4u)
         return fail(DMI_ERR_INVALID_ARG, "%s: scales and block table must be 4-byte aligned", what);
     if (!k->block_size || k->block_size % 16u || k->block_size > kMaxBlock)
@@ -100,11 +102,53 @@ extern "C" dmi_status_t dmi_kv8_append(const dmi_kv8_t *cache, const dmi_kv8_bat
     return launched(launch_append(a, key->dtype, (hipStream_t)hip_stream));
 }
 
+namespace {
+
+// Which kernels attend, and what lies where in their workspace.
+struct AttendPlan {
+    bool tokens;
+    TokensPlan t;
+    uint64_t totals, sums, parts, bytes;        // offsets (scores come first), the whole
+};
+
+// Wavefronts of tokens_kernel that are resident at once, two on each SIMD: a step of 128 contexts (512-8192 tokens x 8 heads x 128)
+// takes 190 us with them, 192 with one on each and 204 with three.
+constexpr uint32_t kResident = 2048;
+
+AttendPlan plan_attend(uint32_t block_heads, uint32_t dim, const dmi_kv8_batch_t &b, uint32_t q_heads, bool weight)
+{
+    AttendPlan p{};
+    const uint32_t group = q_heads / block_heads;
+    const uint64_t rows = (uint64_t)b.total_new * q_heads, shared = (uint64_t)b.max_new * group;
+    p.tokens = shared <= 32u;
+    if (!p.tokens) {
+        p.bytes = weight ? pad64(rows * 4u) : 0u;
+        return p;
+    }
+    TokensPlan &t = p.t;
+    t.tile_rows = shared <= 16u || dim > 128u ? 16u : 32u;     // (two tiles of 256 elements take more registers than there are)
+    t.row_tiles = shared ? ((uint32_t)shared + t.tile_rows - 1u) / t.tile_rows : 1u;
+    // As many wavefronts as are resident at once, if there is enough for them; a request's tiles apart from others' where there is not.
+    const uint32_t per = block_heads * t.row_tiles;
+    const uint64_t tiles = (uint64_t)b.n_reqs * std::max(1u, (b.max_len + 31u) / 32u);
+    t.ranges = (uint32_t)std::min<uint64_t>(std::max(kResident / per, 1u), std::max<uint64_t>(b.n_reqs, (tiles + 1u) / 2u));
+    t.join_blocks = t.ranges > 1u ? (uint32_t)(((uint64_t)b.max_new * q_heads + 3u) / 4u) : 0u;
+    t.score_stride = (b.max_len + 31u) & ~31u;
+    const uint64_t parts = t.join_blocks ? 2ull * t.ranges * per * t.tile_rows : 0u;
+    p.totals = weight ? pad64(rows * t.score_stride * 4u) : 0u;
+    p.sums = p.totals + (weight ? pad64(rows * 4u) : 0u);
+    p.parts = p.sums + pad64(parts * 8u);
+    p.bytes = p.parts + pad64(parts * dim * 4u);
+    return p;
+}
+
+}  // namespace
+
 extern "C" uint64_t dmi_kv8_attend_workspace(const dmi_kv8_t *cache, const dmi_kv8_batch_t *batch, uint32_t n_q_heads,
                                              int with_weight)
 {
-    if (!cache || !batch) return 0;
-    return with_weight ? pad64((uint64_t)batch->total_new * n_q_heads * 4u) : 0u;
+    if (!cache || !batch || !cache->n_heads || !n_q_heads || n_q_heads % cache->n_heads) return 0;
+    return plan_attend(cache->n_heads, cache->head_dim, *batch, n_q_heads, with_weight != 0).bytes;
 }
 
 extern "C" dmi_status_t dmi_kv8_attend(const dmi_kv8_t *cache, const dmi_kv8_batch_t *batch, const dmi_kv8_heads_t *q,
@@ -126,7 +170,8 @@ extern "C" dmi_status_t dmi_kv8_attend(const dmi_kv8_t *cache, const dmi_kv8_bat
     if ((uintptr_t)lse_dev % 4u) return fail(DMI_ERR_INVALID_ARG, "lse_dev must be 4-byte aligned");
     if (a.prior.data && !a.w.data) return fail(DMI_ERR_INVALID_ARG, "prior without weight");
     if (a.prior.data && !std::isfinite(decay)) return fail(DMI_ERR_INVALID_ARG, "decay is not finite");
-    const uint64_t need = dmi_kv8_attend_workspace(cache, batch, n_q_heads, weight != nullptr);
+    const AttendPlan plan = plan_attend(a.c.heads, a.c.dim, *batch, n_q_heads, weight != nullptr);
+    const uint64_t need = plan.bytes;
     if (need && (!workspace || (uintptr_t)workspace % 256u || workspace_bytes < need))
         return fail(DMI_ERR_INVALID_ARG, "workspace must be 256-byte aligned and hold %llu bytes", (unsigned long long)need);
     if (!a.b.n_reqs || !a.b.max_new || !a.b.total_new) return DMI_OK;
@@ -135,6 +180,15 @@ extern "C" dmi_status_t dmi_kv8_attend(const dmi_kv8_t *cache, const dmi_kv8_bat
     a.scale_log2 = scale * 1.44269504088896340736f;
     a.group = n_q_heads / a.c.heads;
     a.q_heads = n_q_heads;
+    if (plan.tokens) {
+        TokensPlan t = plan.t;
+        char *const at = static_cast<char *>(workspace);
+        t.scores = weight ? reinterpret_cast<float *>(at) : nullptr;
+        t.totals = weight ? reinterpret_cast<float *>(at + plan.totals) : nullptr;
+        t.sums = reinterpret_cast<f32x2 *>(at + plan.sums);
+        t.parts = reinterpret_cast<float *>(at + plan.parts);
+        return launched(launch_tokens(a, t, q->dtype, (hipStream_t)hip_stream));
+    }
     return launched(launch_attend(a, q->dtype, need ? static_cast<float *>(workspace) : nullptr, (hipStream_t)hip_stream));
 }
 

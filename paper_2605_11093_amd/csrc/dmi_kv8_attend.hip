@@ -7,10 +7,10 @@
 namespace dmi {
 namespace kv8 {
 
-struct Bf16 { uint16_t u; };
-__device__ __forceinline__ float number(Bf16 x) { return __uint_as_float((uint32_t)x.u << 16); }
+struct PlainBf16 { uint16_t u; };
+__device__ __forceinline__ float number(PlainBf16 x) { return __uint_as_float((uint32_t)x.u << 16); }
 __device__ __forceinline__ float number(_Float16 x) { return (float)x; }
-__device__ __forceinline__ void put(Bf16 *p, float x)
+__device__ __forceinline__ void put(PlainBf16 *p, float x)
 {
     const uint32_t u = __float_as_uint(x);
     p->u = x != x ? 0x7FC0u : (uint16_t)((u + 0x7FFFu + (u >> 16 & 1u)) >> 16);
@@ -114,7 +114,7 @@ template <typename T> hipError_t attend(const AttendArgs &a, float *lse2, hipStr
 
 hipError_t launch_attend(const AttendArgs &a, uint32_t dtype, float *lse2, hipStream_t s)
 {
-    return dtype == DMI_DTYPE_BF16 ? attend<Bf16>(a, lse2, s) : attend<_Float16>(a, lse2, s);
+    return dtype == DMI_DTYPE_BF16 ? attend<PlainBf16>(a, lse2, s) : attend<_Float16>(a, lse2, s);
 }
 
 }  // namespace kv8

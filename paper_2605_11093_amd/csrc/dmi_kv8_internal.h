@@ -10,6 +10,7 @@ namespace kv8 {
 constexpr uint32_t kMaxLen = 1u << 24;          // tokens of a request
 constexpr uint32_t kMaxBlock = 1024;            // tokens of a block
 constexpr uint32_t kMaxDim = 256;
+constexpr int64_t kMaxSlotStride = 1 << 26;     // sixteen tokens lie within 32-bit offsets of the first
 constexpr uint32_t kMaxReqs = 65535;            // requests of a call: what a launch's second dimension holds
 
 // A cache as the kernels see it; [0] is K, [1] is V.
@@ -62,9 +63,24 @@ struct AttendArgs {
     uint32_t group, q_heads;
 };
 
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+// How few query rows are attended to: see dmi_kv8_tokens.hip.
+struct TokensPlan {
+    uint32_t ranges;                            // equal parts of all contexts
+    uint32_t tile_rows, row_tiles;              // query rows of a wavefront; wavefronts for the rows that share a head
+    uint32_t join_blocks;                       // workgroups of the second launch that join parts, 0 if there can be none
+    uint32_t score_stride;
+    f32x2 *sums;                                // of parts: maximum, sum of 2^(score - maximum)
+    float *parts;                               // [part][dim]
+    float *totals;                              // [row of out]: log2 of the sum of 2^score of contexts whole in a range; NULL: no weights
+    float *scores;                              // [head][query row][score_stride]; NULL: no weights
+};
+
 hipError_t launch_append(const AppendArgs &a, uint32_t dtype, hipStream_t s);
 hipError_t launch_evict(const EvictArgs &a, hipStream_t s);
 hipError_t launch_attend(const AttendArgs &a, uint32_t dtype, float *lse2, hipStream_t s);
+hipError_t launch_tokens(const AttendArgs &a, const TokensPlan &p, uint32_t dtype, hipStream_t s);
 
 // ---------------------------------------------------------------- device side
 #ifdef __HIPCC__
@@ -121,7 +137,6 @@ __device__ __forceinline__ uint32_t to_codes(float a, float b, float c, float d)
     int w = __builtin_amdgcn_cvt_pk_fp8_f32(within(a), within(b), 0, false);
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(within(c), within(d), w, true);
 }
-typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));

@@ -1,0 +1,108 @@
+// What the attention kernels of the 8-bit KV cache share: the types that matrix instructions take, conversions into them.
+#pragma once
+#include "dmi_kv8_internal.h"
+
+#include <hip/hip_fp16.h>
+
+namespace dmi {
+namespace kv8 {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+// Matrix instructions take bf16 or f16 as q comes; an e4m3 number is one of either exactly.
+struct Bf16 {
+    static constexpr bool kNarrow = false;      // as wide a range of exponents as fp32
+    static constexpr uint32_t kOne = 0x3F80u, kInf = 0x7F80u;
+    // two neighbouring codes of a word
+    static __device__ __forceinline__ uint32_t two_codes(uint32_t w, bool hi)
+    {
+        return __builtin_bit_cast(uint32_t, hi ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true)
+                                               : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false));
+    }
+    static __device__ __forceinline__ uint32_t pack(float a, float b)
+    {
+        const f32x2 v = {a, b};
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
+    }
+    static __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c)
+    {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    }
+};
+
+struct Fp16 {
+    static constexpr bool kNarrow = true;
+    static constexpr uint32_t kOne = 0x3C00u, kInf = 0x7C00u;
+    static __device__ __forceinline__ uint32_t two_codes(uint32_t w, bool hi)
+    {
+        return __builtin_bit_cast(uint32_t, hi ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, true)
+                                               : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, false));
+    }
+    static __device__ __forceinline__ uint32_t pack(float a, float b)
+    {
+        const f32x2 v = {a, b};
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2));
+    }
+    static __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c)
+    {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    }
+};
+
+// Loads at 32-bit offsets from an address that is the same in every lane.  kOnce in the last argument: the line is not read
+// again soon.
+typedef __amdgpu_buffer_rsrc_t Buffer;
+constexpr int kOnce = 2;
+__device__ __forceinline__ Buffer buffer_at(const uint8_t *p)
+{
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p), 0, 0x7FFFFFFF, 0x00027000);
+}
+template <int AUX> __device__ __forceinline__ u32x4 load_b128(Buffer b, uint32_t at)
+{
+    return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(b, (int)at, 0, AUX));
+}
+template <int AUX> __device__ __forceinline__ u32x2 load_b64(Buffer b, uint32_t at)
+{
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(b, (int)at, 0, AUX));
+}
+template <int AUX> __device__ __forceinline__ uint32_t load_b32(Buffer b, uint32_t at)
+{
+    return __builtin_amdgcn_raw_buffer_load_b32(b, (int)at, 0, AUX);
+}
+
+__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float log2_of(float x) { return __builtin_amdgcn_logf(x); }
+constexpr float kLn2 = 0.693147180559945309417f;
+
+// Scores may rise this far (as powers of two) above the maximum that p is taken against before everything is taken against
+// a new one: p stays below 2^8, which costs no precision, and the rescaling becomes rare.
+constexpr float kSlack = 8.0f;
+
+// The top bit of every byte of w that is a NaN.
+__device__ __forceinline__ uint32_t nan_codes(uint32_t w) { return ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u; }
+
+// A query row among those that share a head of the cache: row = token * group + query head within the group.
+struct QueryRow {
+    int token;
+    uint32_t head;
+};
+__device__ __forceinline__ QueryRow query_row(const AttendArgs &a, uint32_t head, uint32_t row)
+{
+    const uint32_t i = row / a.group;
+    return {(int)i, head * a.group + (row - i * a.group)};
+}
+
+}  // namespace kv8
+}  // namespace dmi

@@ -1,0 +1,562 @@
+// Attention of few query rows over the 8-bit KV cache: single tokens, and a few of them.
+#include "dmi_internal.h"
+#include "dmi_kv8_mfma.h"
+
+namespace dmi {
+namespace kv8 {
+
+// ---------------------------------------------------------------- who does what
+// All contexts of a call, in tiles of 32 tokens one behind the other, are cut into p.ranges equal ranges; a wavefront takes a
+// range for one head (and one tile of query rows).  A context that lies within a range is finished there; of one that goes over
+// an end, every range leaves a part: in place 1 of its two where the context begins in it, in place 0 otherwise (a range holds at
+// most one of either), and a second launch puts them together.  Lengths are known on the device only, so every wavefront adds
+// them up for itself; equal ranges leave no wavefront idle at the end, and none starts for nothing.
+
+// Sums over the lanes up to each one
+__device__ __forceinline__ int lanes_scan(int v)
+{
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);     // within 16 lanes: shifts by 1, 2, 4, 8
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);     // the totals of 16 lanes carried on
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);
+    return v;
+}
+
+// A request with new tokens has a tile at least: an empty context's rows are written too.
+__device__ __forceinline__ int tiles_of(const Request &q) { return q.fresh > 0 ? max(1, (q.len + 31) >> 5) : 0; }
+
+// The tiles of requests n0 .. n0 + 63, one request a lane
+__device__ __forceinline__ int lane_tiles(const AttendArgs &a, uint32_t n0)
+{
+    const uint32_t r = n0 + (threadIdx.x & 63u);
+    return r < a.b.n_reqs ? tiles_of(request_of(a.b, a.c, (int)r)) : 0;
+}
+
+// Tiles of a range, given the tiles of all contexts
+__device__ __forceinline__ int range_tiles(const TokensPlan &p, int total) { return (total + (int)p.ranges - 1) / (int)p.ranges; }
+
+__device__ __forceinline__ int all_tiles(const AttendArgs &a)
+{
+    int total = 0;
+    for (uint32_t n0 = 0; n0 < a.b.n_reqs; n0 += 64u) total += __builtin_amdgcn_readlane(lanes_scan(lane_tiles(a, n0)), 63);
+    return total;
+}
+
+// Index of a query row's part
+__device__ __forceinline__ int64_t part_at(const AttendArgs &a, const TokensPlan &p, int range, int place, uint32_t head, uint32_t row)
+{
+    const uint32_t tile = row / p.tile_rows;
+    return (((int64_t)range * 2 + place) * p.row_tiles * a.c.heads + tile * a.c.heads + head) * p.tile_rows + (row - tile * p.tile_rows);
+}
+
+// ---------------------------------------------------------------- the sums
+// The transposed products, scores S^T = K Q^T and outputs O^T = V^T P^T, with 16x16x32 matrix instructions: tokens (then elements)
+// are rows, query rows are columns.  A lane's registers of S^T are then the P^T operand of the second product as they are: lane
+// (column c, group g) holds tokens 4g..4g+3 of each of two sixteens of tokens, and which token stands at which place of the
+// product's inner dimension is free as long as V agrees.  V is read with 8 tokens x 8 elements a lane (128 elements), its bytes
+// interleaved by twos and converted: column m of V^T is element 8m + j for instruction j.  Nothing passes through LDS.
+template <typename T, int DP, int NT>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP * NT <= 128 ? 2 : 1)))
+void tokens_kernel(AttendArgs a, TokensPlan p)
+{
+    constexpr int KL = DP / 64;                 // 16-byte loads of K a lane and sixteen
+    constexpr int KK = DP / 32;                 // instructions for a sixteen's scores
+    constexpr int VW = DP / 64;                 // words of V a lane and token
+    constexpr int NJ = DP / 16;                 // instructions for 16 query rows' outputs
+
+    const int lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
+    // Workgroups go to the eight XCDs in turn: the heads (and row tiles) of a range follow each other on one of them.
+    const uint32_t unit = (blockIdx.x >> 3) * 4u + (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), per = a.c.heads * p.row_tiles;
+    const int range = (int)(unit / per * 8u + (blockIdx.x & 7u));
+    const uint32_t head = unit % per % a.c.heads, row_tile = unit % per / a.c.heads;
+    const int row0 = (int)row_tile * 16 * NT;
+    if (range >= (int)p.ranges) return;
+
+    // the range's first tile, the request that it lies in
+    int total, of_range, r = 0, seg0 = 0;       // seg0: the request's first tile
+    if (a.b.n_reqs <= 64u) {
+        const int upto = lanes_scan(lane_tiles(a, 0));
+        total = __builtin_amdgcn_readlane(upto, 63);
+        of_range = range_tiles(p, total);
+        if (range * of_range >= total) return;
+        r = __ffsll((unsigned long long)__ballot(upto > range * of_range)) - 1;
+        seg0 = r ? __builtin_amdgcn_readlane(upto, r - 1) : 0;
+    } else {
+        total = all_tiles(a);
+        of_range = range_tiles(p, total);
+        if (range * of_range >= total) return;
+        for (;; r += 64) {
+            const int upto = lanes_scan(lane_tiles(a, (uint32_t)r)), sum = __builtin_amdgcn_readlane(upto, 63);
+            if (seg0 + sum <= range * of_range) {
+                seg0 += sum;
+                continue;
+            }
+            const int in = __ffsll((unsigned long long)__ballot(seg0 + upto > range * of_range)) - 1;
+            seg0 += in ? __builtin_amdgcn_readlane(upto, in - 1) : 0;
+            r += in;
+            break;
+        }
+    }
+    const int first = range * of_range, last = min(first + of_range, total);    // the range's tiles
+
+    // byte offsets of this lane within a sixteen; elements past the row's end are read from its start (q is 0 there, and
+    // V's columns there are not written)
+    uint32_t k_off[KL], v_off;
+#pragma unroll
+    for (int c = 0; c < KL; c++) {
+        const uint32_t d = (uint32_t)(g * (DP / 4) + 16 * c);
+        k_off[c] = (uint32_t)col * (uint32_t)a.c.slot_stride + (d < a.c.dim ? d : 0u);
+    }
+    v_off = (uint32_t)(4 * g) * (uint32_t)a.c.slot_stride + ((uint32_t)col * (DP / 16) < a.c.dim ? (uint32_t)col * (DP / 16) : 0u);
+
+    for (; r < (int)a.b.n_reqs && seg0 < last; r++) {
+        const Request q = request_of(a.b, a.c, r);
+        const int seg_tiles = tiles_of(q), seg_first = seg0;
+        seg0 += seg_tiles;
+        const int rows = q.fresh * (int)a.group;
+        if (!seg_tiles || row0 >= rows) continue;
+        // this context's tiles in this range
+        const int from = max(first, seg_first) - seg_first, to = min(last, seg_first + seg_tiles) - seg_first, tiles = to - from;
+        const int begin = 32 * from, end = min(q.len, 32 * to);
+
+        // entries and scales of the sixteens of 32 tiles, one a lane, and of the 32 tiles behind them
+        struct Look {
+            int entry;
+            float ks, vs;
+        };
+        auto look = [&](int tile) {
+            Look l{-1, 0.0f, 0.0f};
+            const int t = begin + 32 * tile + 16 * lane;
+            if (t < end) {
+                l.entry = entry_of(a.c, q.row, block_of(a.c, (uint32_t)t >> 4));
+                if (l.entry >= 0) {
+                    l.ks = *scale_at(a.c, 0, l.entry, head) * a.scale_log2;
+                    l.vs = *scale_at(a.c, 1, l.entry, head);
+                }
+            }
+            return l;
+        };
+        Look here = look(0), behind{-1, 0.0f, 0.0f};
+
+        u32x4 qf[NT][KK];
+        int lim[NT];                            // the last position a column's query sees
+#pragma unroll
+        for (int n = 0; n < NT; n++) {
+            const int row = row0 + 16 * n + col;
+            const QueryRow w = query_row(a, head, (uint32_t)row);
+            lim[n] = row < rows ? q.len - q.fresh + w.token : q.len;
+            const uint16_t *src = static_cast<const uint16_t *>(a.q.data) + (int64_t)(q.start + w.token) * a.q.row_stride + (int64_t)w.head * a.q.head_stride;
+#pragma unroll
+            for (int k = 0; k < KK; k++) {
+                const int d = g * (DP / 4) + 8 * k;
+                qf[n][k] = u32x4{0u, 0u, 0u, 0u};
+                if (row < rows && d < (int)a.c.dim) qf[n][k] = *reinterpret_cast<const u32x4 *>(src + d);
+            }
+        }
+        const int all_see = q.len - q.fresh + row0 / (int)a.group;      // what every row of the tile sees
+
+        // Where a sixteen's codes lie; one that is not there is read at the cache's first block and counts no token.
+        auto place = [&](int tile, int x) {
+            const int six = 2 * (tile & 31) + x, t = begin + 32 * tile + 16 * x, e = max(__builtin_amdgcn_readlane(here.entry, six), 0);
+            return (int64_t)e * a.c.block_stride + (int64_t)((uint32_t)t - block_of(a.c, (uint32_t)t >> 4) * a.c.bs) * a.c.slot_stride +
+                   (int64_t)head * a.c.head_stride;
+        };
+        u32x4 rk[2][KL];
+        uint32_t rv[8][VW];
+        auto fetch_k = [&](int tile) {
+#pragma unroll
+            for (int x = 0; x < 2; x++) {
+                const Buffer k = buffer_at(a.c.code[0] + place(tile, x));
+#pragma unroll
+                for (int c = 0; c < KL; c++) rk[x][c] = load_b128<0>(k, k_off[c]);
+            }
+        };
+        auto fetch_v = [&](int tile) {
+#pragma unroll
+            for (int x = 0; x < 2; x++) {
+                const Buffer v = buffer_at(a.c.code[1] + place(tile, x));
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    const uint32_t at = v_off + (uint32_t)i * (uint32_t)a.c.slot_stride;
+                    if constexpr (VW == 1) rv[4 * x + i][0] = load_b32<kOnce>(v, at);
+                    if constexpr (VW == 2) {
+                        const u32x2 w = load_b64<kOnce>(v, at);
+                        rv[4 * x + i][0] = w[0], rv[4 * x + i][1] = w[1];
+                    }
+                    if constexpr (VW == 4) {
+                        const u32x4 w = load_b128<kOnce>(v, at);
+#pragma unroll
+                        for (int y = 0; y < 4; y++) rv[4 * x + i][y] = w[y];
+                    }
+                }
+            }
+        };
+
+        float m[NT], base[NT], l[NT], v_ref = T::kNarrow ? 0.0f : 1.0f;
+        f32x4 o[NT][NJ];
+#pragma unroll
+        for (int n = 0; n < NT; n++) {
+            m[n] = -INFINITY, base[n] = 0.0f, l[n] = 0.0f;
+#pragma unroll
+            for (int j = 0; j < NJ; j++) o[n][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+
+        fetch_k(0);
+        fetch_v(0);
+        for (int tile = 0; tile < tiles; tile++) {
+            const int t0 = begin + 32 * tile, ahead = min(tile + 1, tiles - 1);
+            int count[2];
+            float ks[2], vs[2];
+#pragma unroll
+            for (int x = 0; x < 2; x++) {
+                const int six = 2 * (tile & 31) + x;
+                count[x] = __builtin_amdgcn_readlane(here.entry, six) < 0 ? 0 : min(16, end - t0 - 16 * x);
+                ks[x] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(here.ks), six));
+                vs[x] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(here.vs), six));
+            }
+            if ((tile & 31) == 0 && tile + 32 < tiles) behind = look(tile + 32);
+            if ((tile & 31) == 31) here = behind;
+            f32x4 z[NT][2];
+#pragma unroll
+            for (int x = 0; x < 2; x++) {
+#pragma unroll
+                for (int n = 0; n < NT; n++) z[n][x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int k = 0; k < KK; k++) {
+                    const uint32_t lo = rk[x][k / 2][2 * (k % 2)], hi = rk[x][k / 2][2 * (k % 2) + 1];
+                    const u32x4 f = {T::two_codes(lo, false), T::two_codes(lo, true), T::two_codes(hi, false), T::two_codes(hi, true)};
+#pragma unroll
+                    for (int n = 0; n < NT; n++) z[n][x] = T::mfma16(f, qf[n][k], z[n][x]);
+                }
+#pragma unroll
+                for (int n = 0; n < NT; n++) z[n][x] *= ks[x];
+            }
+            fetch_k(ahead);
+            const bool full = count[0] == 16 && count[1] == 16 && t0 + 31 <= all_see;
+            if (!full) {
+                // tokens that are not there, or not seen: no score, and no NaN out of V
+#pragma unroll
+                for (int x = 0; x < 2; x++)
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        const bool there = 4 * g + i < count[x];
+#pragma unroll
+                        for (int n = 0; n < NT; n++)
+                            z[n][x][i] = there && t0 + 16 * x + 4 * g + i <= lim[n] ? z[n][x][i] : -INFINITY;
+#pragma unroll
+                        for (int y = 0; y < VW; y++) rv[4 * x + i][y] = there ? rv[4 * x + i][y] : 0u;
+                    }
+            }
+            if (p.scores) {
+#pragma unroll
+                for (int n = 0; n < NT; n++) {
+                    const int row = row0 + 16 * n + col;
+                    if (row < rows) {
+                        float *s = p.scores + ((int64_t)head * a.b.total_new * a.group + (int64_t)q.start * a.group + row) * p.score_stride + t0 + 4 * g;
+#pragma unroll
+                        for (int x = 0; x < 2; x++)
+                            if (t0 + 16 * x < end) *reinterpret_cast<f32x4 *>(s + 16 * x) = z[n][x];
+                    }
+                }
+            }
+            bool rises = false;
+            float top[NT];
+#pragma unroll
+            for (int n = 0; n < NT; n++) {
+                top[n] = fmaxf(fmaxf(fmaxf(z[n][0][0], z[n][0][1]), fmaxf(z[n][0][2], z[n][0][3])),
+                               fmaxf(fmaxf(z[n][1][0], z[n][1][1]), fmaxf(z[n][1][2], z[n][1][3])));
+                rises |= top[n] > m[n] + kSlack;
+            }
+            if (__ballot(rises)) {
+#pragma unroll
+                for (int n = 0; n < NT; n++) {
+                    float t = top[n];
+                    t = fmaxf(t, __shfl_xor(t, 16));
+                    t = fmaxf(t, __shfl_xor(t, 32));
+                    const float now = fmaxf(m[n], t);
+                    const float f = now == -INFINITY ? 1.0f : exp2_of(m[n] - now);
+                    m[n] = now;
+                    base[n] = now == -INFINITY ? 0.0f : now;
+                    l[n] *= f;
+#pragma unroll
+                    for (int j = 0; j < NJ; j++) o[n][j] *= f;
+                }
+            }
+            // V's scale goes into P; in fp16 relative to the largest yet, to stay within its range
+            if constexpr (T::kNarrow) {
+                const float largest = fmaxf(vs[0], vs[1]);
+                if (largest > v_ref) {
+                    const float f = v_ref / largest;
+#pragma unroll
+                    for (int n = 0; n < NT; n++)
+#pragma unroll
+                        for (int j = 0; j < NJ; j++) o[n][j] *= f;
+                    v_ref = largest;
+                }
+                const float inv = v_ref > 0.0f ? 1.0f / v_ref : 0.0f;
+                vs[0] *= inv, vs[1] *= inv;
+            }
+            u32x4 pf[NT];
+#pragma unroll
+            for (int n = 0; n < NT; n++) {
+                float e[2][4];
+#pragma unroll
+                for (int x = 0; x < 2; x++) {
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        e[x][i] = exp2_of(z[n][x][i] - base[n]);
+                        l[n] += e[x][i];
+                        e[x][i] *= vs[x];
+                    }
+                    pf[n][2 * x] = T::pack(e[x][0], e[x][1]);
+                    pf[n][2 * x + 1] = T::pack(e[x][2], e[x][3]);
+                }
+            }
+            // A NaN in V of a token that some queries do not see: their p is 0, and 0 * NaN is not.  NaNs are taken out, and
+            // a product of their own counts how many of them each query sees.
+            if (!full) {
+                uint32_t any = 0;
+#pragma unroll
+                for (int i = 0; i < 8; i++)
+#pragma unroll
+                    for (int y = 0; y < VW; y++) any |= nan_codes(rv[i][y]);
+                if (__ballot(any != 0)) {
+#pragma unroll 1
+                    for (int j = 0; j < NJ; j++) {
+                        u32x4 bad;
+#pragma unroll
+                        for (int i = 0; i < 4; i++) {
+                            uint32_t w[2] = {0u, 0u};
+#pragma unroll
+                            for (int y = 0; y < VW; y++)
+#pragma unroll
+                                for (int e = 0; e < 2; e++)
+                                    if (y == j / 4) w[e] = nan_codes(rv[2 * i + e][y]) >> (8 * (j % 4)) & 0x80u;
+                            bad[i] = (w[0] ? T::kOne : 0u) | (w[1] ? T::kOne << 16 : 0u);
+                        }
+#pragma unroll
+                        for (int n = 0; n < NT; n++) {
+                            u32x4 seen;
+#pragma unroll
+                            for (int i = 0; i < 4; i++) {
+                                const int t = t0 + 16 * (i / 2) + 4 * g + 2 * (i % 2);
+                                seen[i] = (t <= lim[n] ? T::kOne : 0u) | (t + 1 <= lim[n] ? T::kOne << 16 : 0u);
+                            }
+                            const f32x4 nans = T::mfma16(bad, seen, f32x4{0.0f, 0.0f, 0.0f, 0.0f});
+#pragma unroll
+                            for (int k = 0; k < NJ; k++)
+#pragma unroll
+                                for (int i = 0; i < 4; i++) o[n][k][i] += k == j && nans[i] > 0.0f ? NAN : 0.0f;
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < 8; i++)
+#pragma unroll
+                        for (int y = 0; y < VW; y++) rv[i][y] &= ~(nan_codes(rv[i][y]) | (nan_codes(rv[i][y]) - (nan_codes(rv[i][y]) >> 7)));
+                }
+            }
+            uint32_t two[VW][2][4];                 // bytes of two tokens in turn: [word of a token][half][pair of tokens]
+#pragma unroll
+            for (int y = 0; y < VW; y++)
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    two[y][0][i] = __builtin_amdgcn_perm(rv[2 * i + 1][y], rv[2 * i][y], 0x05010400u);
+                    two[y][1][i] = __builtin_amdgcn_perm(rv[2 * i + 1][y], rv[2 * i][y], 0x07030602u);
+                }
+            fetch_v(ahead);
+#pragma unroll
+            for (int j = 0; j < NJ; j++) {
+                u32x4 vf;
+#pragma unroll
+                for (int i = 0; i < 4; i++) vf[i] = T::two_codes(two[j / 4][j / 2 % 2][i], j % 2);
+#pragma unroll
+                for (int n = 0; n < NT; n++) o[n][j] = T::mfma16(vf, pf[n], o[n][j]);
+            }
+        }
+
+#pragma unroll
+        for (int n = 0; n < NT; n++) {
+            l[n] += __shfl_xor(l[n], 16);
+            l[n] += __shfl_xor(l[n], 32);
+            const int row = row0 + 16 * n + col;
+            if (row >= rows) continue;
+            const QueryRow w = query_row(a, head, (uint32_t)row);
+            const int64_t at = (int64_t)(q.start + w.token) * a.q_heads + w.head;
+            const bool whole = tiles == seg_tiles;
+            const bool empty = m[n] == -INFINITY && l[n] == 0.0f;
+            const float f = (whole ? (empty ? 0.0f : 1.0f / l[n]) : 1.0f) * v_ref;
+            // a lane holds DP / 4 elements of its row that follow each other
+            if (whole) {
+                uint16_t *dst = static_cast<uint16_t *>(a.out.data) + (int64_t)(q.start + w.token) * a.out.row_stride + (int64_t)w.head * a.out.head_stride;
+#pragma unroll
+                for (int i = 0; i < 4; i++)
+#pragma unroll
+                    for (int j = 0; j < NJ; j += 4) {
+                        const int d = NJ * (4 * g + i) + j;
+                        if (d < (int)a.c.dim)
+                            *reinterpret_cast<u32x2 *>(dst + d) = u32x2{T::pack(o[n][j][i] * f, o[n][j + 1][i] * f), T::pack(o[n][j + 2][i] * f, o[n][j + 3][i] * f)};
+                    }
+                if (g == 0) {
+                    const float sum = empty ? -INFINITY : m[n] + log2_of(l[n]);
+                    if (a.lse) a.lse[at] = sum * kLn2;
+                    if (p.totals) p.totals[at] = sum;
+                }
+            } else {
+                const int64_t part = part_at(a, p, range, seg_first >= first, head, (uint32_t)row);
+                if (g == 0) p.sums[part] = f32x2{m[n], l[n]};
+                float *dst = p.parts + part * a.c.dim;
+#pragma unroll
+                for (int i = 0; i < 4; i++)
+#pragma unroll
+                    for (int j = 0; j < NJ; j += 4) {
+                        const int d = NJ * (4 * g + i) + j;
+                        if (d < (int)a.c.dim)
+                            *reinterpret_cast<f32x4 *>(dst + d) = f32x4{o[n][j][i], o[n][j + 1][i], o[n][j + 2][i], o[n][j + 3][i]} * f;
+                    }
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------- what ranges leave
+// A request's place among the ranges: whole in one, or parts from range `from` to `to`.
+struct Spread {
+    int from, to;
+};
+__device__ __forceinline__ Spread spread_of(const AttendArgs &a, const TokensPlan &p, uint32_t r)
+{
+    int total = 0, before = 0, own = 0;
+    for (uint32_t n0 = 0; n0 < a.b.n_reqs; n0 += 64u) {
+        const int tiles = lane_tiles(a, n0), upto = lanes_scan(tiles);
+        if (r >= n0 && r < n0 + 64u) {
+            own = __builtin_amdgcn_readlane(tiles, (int)(r - n0));
+            before = total + __builtin_amdgcn_readlane(upto, (int)(r - n0)) - own;
+        }
+        total += __builtin_amdgcn_readlane(upto, 63);
+    }
+    const int size = max(1, range_tiles(p, total));
+    return {before / size, (before + max(own, 1) - 1) / size};
+}
+
+// log2 of the sum of 2^score over all of a row's context; every lane of the wavefront gets it
+__device__ __forceinline__ float total_of(const AttendArgs &a, const TokensPlan &p, const Spread &s, uint32_t head, uint32_t row)
+{
+    const int lane = threadIdx.x & 63;
+    float m = -INFINITY, l = 0.0f;
+    for (int i = s.from + lane; i <= s.to; i += 64) {
+        const f32x2 x = p.sums[part_at(a, p, i, i == s.from, head, row)];
+        const float top = fmaxf(m, x[0]), to = top == -INFINITY ? 0.0f : top;
+        l = l * exp2_of(m - to) + x[1] * exp2_of(x[0] - to);
+        m = top;
+    }
+    float top = m;
+#pragma unroll
+    for (int k = 1; k < 64; k <<= 1) top = fmaxf(top, __shfl_xor(top, k));
+    const float to = top == -INFINITY ? 0.0f : top;
+    l *= exp2_of(m - to);
+#pragma unroll
+    for (int k = 1; k < 64; k <<= 1) l += __shfl_xor(l, k);
+    return top == -INFINITY && l == 0.0f ? -INFINITY : to + log2_of(l);
+}
+
+// The first p.join_blocks workgroups of a request: outputs out of parts, a wavefront a row.  The others: weights out of the
+// scores, four tokens a thread.
+template <typename T>
+__global__ __launch_bounds__(256) void finish_kernel(AttendArgs a, TokensPlan p)
+{
+    __shared__ float totals[256];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const Request q = request_of(a.b, a.c, (int)blockIdx.y);
+    const uint32_t rows = (uint32_t)q.fresh * a.group;
+    if (blockIdx.x < p.join_blocks) {
+        const uint32_t n = blockIdx.x * 4u + (uint32_t)wave;
+        if (n >= rows * a.c.heads) return;
+        const Spread s = spread_of(a, p, blockIdx.y);
+        if (s.from == s.to) return;
+        const uint32_t head = n / rows, row = n - head * rows;
+        const float total = total_of(a, p, s, head, row);
+        const QueryRow w = query_row(a, head, row);
+        // as many parts at a time as there are lanes for
+        const int wide = (int)a.c.dim / 4, teams = 64 / wide, team = lane / wide, d = 4 * (lane - team * wide);
+        f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (team < teams) {
+#pragma unroll 4
+            for (int i = s.from + team; i <= s.to; i += teams) {
+                const int64_t part = part_at(a, p, i, i == s.from, head, row);
+                const float f = total == -INFINITY ? 0.0f : exp2_of(p.sums[part][0] - total);
+                sum += *reinterpret_cast<const f32x4 *>(p.parts + part * a.c.dim + d) * f;
+            }
+        }
+        for (int k = 1; k < teams; k++)
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const float other = __shfl(sum[i], lane + k * wide);
+                if (team == 0) sum[i] += other;
+            }
+        if (team == 0) {
+            uint16_t *dst = static_cast<uint16_t *>(a.out.data) + (int64_t)(q.start + w.token) * a.out.row_stride + (int64_t)w.head * a.out.head_stride + d;
+            *reinterpret_cast<u32x2 *>(dst) = u32x2{T::pack(sum[0], sum[1]), T::pack(sum[2], sum[3])};
+        }
+        if (a.lse && !lane) a.lse[(int64_t)(q.start + w.token) * a.q_heads + w.head] = total * kLn2;
+        return;
+    }
+    const uint32_t rest = blockIdx.x - p.join_blocks, head = rest % a.c.heads;
+    const int t0 = 1024 * (int)(rest / a.c.heads), t = t0 + 4 * (int)threadIdx.x, older = q.len - q.fresh;
+    if (t0 >= q.len) return;
+    const Spread s = spread_of(a, p, blockIdx.y);
+    f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int r0 = 0; r0 < (int)rows; r0 += 256) {
+        const int r1 = min((int)rows, r0 + 256);
+        if (r0) __syncthreads();
+        for (int r = r0 + wave; r < r1; r += 4) {
+            const QueryRow w = query_row(a, head, (uint32_t)r);
+            const float total = s.from == s.to ? p.totals[(int64_t)(q.start + w.token) * a.q_heads + w.head] : total_of(a, p, s, head, (uint32_t)r);
+            if (!lane) totals[r - r0] = total;
+        }
+        __syncthreads();
+        if (t < q.len)
+            for (int r = r0; r < r1; r++) {
+                const float total = totals[r - r0];
+                if (total == -INFINITY) continue;
+                const f32x4 z = *reinterpret_cast<const f32x4 *>(
+                    p.scores + ((int64_t)head * a.b.total_new * a.group + (int64_t)q.start * a.group + r) * p.score_stride + t);
+#pragma unroll
+                for (int i = 0; i < 4; i++) sum[i] += exp2_of(z[i] - total);
+            }
+    }
+    const float *prior = a.prior.data + (int64_t)q.row * a.prior.row_stride + (int64_t)head * a.prior.head_stride;
+    float *to = a.w.data + (int64_t)q.row * a.w.row_stride + (int64_t)head * a.w.head_stride;
+#pragma unroll
+    for (int i = 0; i < 4; i++)
+        if (t + i < q.len) to[t + i] = a.prior.data && t + i < older ? a.decay * prior[t + i] + sum[i] : sum[i];
+}
+
+template <typename T> static hipError_t tokens(const AttendArgs &a, const TokensPlan &p, hipStream_t s)
+{
+    const uint32_t per = a.c.heads * p.row_tiles, units = (p.ranges + 7u) / 8u * per;      // on each XCD
+    const dim3 grid((units + 3u) / 4u * 8u);
+    const int dp = a.c.dim <= 64 ? 64 : a.c.dim <= 128 ? 128 : 256;
+    if (p.tile_rows == 16) {
+        if (dp == 64) tokens_kernel<T, 64, 1><<<grid, 256, 0, s>>>(a, p);
+        else if (dp == 128) tokens_kernel<T, 128, 1><<<grid, 256, 0, s>>>(a, p);
+        else tokens_kernel<T, 256, 1><<<grid, 256, 0, s>>>(a, p);
+    } else {
+        if (dp == 64) tokens_kernel<T, 64, 2><<<grid, 256, 0, s>>>(a, p);
+        else tokens_kernel<T, 128, 2><<<grid, 256, 0, s>>>(a, p);
+    }
+    hipError_t e = hipGetLastError();
+    const uint32_t weight_blocks = a.w.data ? (a.b.max_len + 1023u) / 1024u * a.c.heads : 0u;
+    if (e != hipSuccess || p.join_blocks + weight_blocks == 0) return e;
+    finish_kernel<T><<<dim3(p.join_blocks + weight_blocks, a.b.n_reqs), 256, 0, s>>>(a, p);
+    return hipGetLastError();
+}
+
+hipError_t launch_tokens(const AttendArgs &a, const TokensPlan &p, uint32_t dtype, hipStream_t s)
+{
+    return dtype == DMI_DTYPE_BF16 ? tokens<Bf16>(a, p, s) : tokens<Fp16>(a, p, s);
+}
+
+}  // namespace kv8
+}  // namespace dmi
