@@ -842,7 +842,7 @@ def kv8_attend_workspace(cache: KV8, batch: KV8Batch, n_q_heads: int, with_weigh
 def _scratch(n, like, stream):
     """n bytes from torch's allocator, in the order of `stream`."""
     import torch
-    if torch.cuda.current_stream(like.device).cuda_stream == stream:
+    if not like.is_cuda or torch.cuda.current_stream(like.device).cuda_stream == stream:
         return torch.empty(n, dtype=torch.uint8, device=like.device)
     with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=like.device)):
         return torch.empty(n, dtype=torch.uint8, device=like.device)

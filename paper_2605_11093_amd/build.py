@@ -11,7 +11,7 @@ ROOT = os.path.dirname(HERE)
 SO = os.path.join(HERE, "libdmi.so")
 SOURCES = [os.path.join(HERE, "csrc", f) for f in ("dmi_kernels.hip", "dmi_host.hip", "dmi_step.hip",
                                                      "dmi_exporter.hip", "dmi_noalloc.hip", "dmi_kv8.hip", "dmi_kv8_cache.hip",
-                                                     "dmi_kv8_attend.hip", "dmi_kv8_tokens.hip")]
+                                                     "dmi_kv8_tokens.hip", "dmi_kv8_parts.hip")]
 HEADERS = [os.path.join(HERE, "csrc", "dmi_internal.h"), os.path.join(HERE, "csrc", "dmi_ring.h"),
            os.path.join(HERE, "csrc", "dmi_kv8_internal.h"), os.path.join(HERE, "csrc", "dmi_kv8_mfma.h"), os.path.join(ROOT, "include", "dmi_kv8.h"),
            os.path.join(ROOT, "include", "dmi.h"), os.path.join(ROOT, "include", "dmi_debug.h")]

@@ -108,6 +108,7 @@ namespace {
 struct AttendPlan {
     bool tokens;
     TokensPlan t;
+    PartsPlan many;
     uint64_t totals, sums, parts, bytes;        // offsets (scores come first), the whole
 };
 
@@ -122,7 +123,17 @@ AttendPlan plan_attend(uint32_t block_heads, uint32_t dim, const dmi_kv8_batch_t
     const uint64_t rows = (uint64_t)b.total_new * q_heads, shared = (uint64_t)b.max_new * group;
     p.tokens = shared <= 32u;
     if (!p.tokens) {
-        p.bytes = weight ? pad64(rows * 4u) : 0u;
+        PartsPlan &m = p.many;
+        const uint32_t rows_each = dim <= 128u ? 256u : 128u;
+        m.row_tiles = (uint32_t)((shared + rows_each - 1u) / rows_each);
+        // two workgroups for each of the 256 compute units, but no less than 512 tokens for one
+        const uint64_t groups = (uint64_t)b.n_reqs * block_heads * m.row_tiles;
+        m.splits = (uint32_t)std::max<uint64_t>(1u, std::min<uint64_t>((512u + groups - 1u) / std::max<uint64_t>(groups, 1u), b.max_len / 512u));
+        m.chunk = std::max(64u, ((b.max_len + m.splits - 1u) / m.splits + 63u) & ~63u);
+        m.splits = std::max(1u, (b.max_len + m.chunk - 1u) / m.chunk);
+        p.sums = weight ? pad64(rows * 4u) : 0u;
+        p.parts = p.sums + (m.splits > 1u ? pad64(rows * m.splits * 8u) : 0u);
+        p.bytes = p.parts + (m.splits > 1u ? pad64(rows * m.splits * dim * 4u) : 0u);
         return p;
     }
     TokensPlan &t = p.t;
@@ -189,7 +200,12 @@ extern "C" dmi_status_t dmi_kv8_attend(const dmi_kv8_t *cache, const dmi_kv8_bat
         t.parts = reinterpret_cast<float *>(at + plan.parts);
         return launched(launch_tokens(a, t, q->dtype, (hipStream_t)hip_stream));
     }
-    return launched(launch_attend(a, q->dtype, need ? static_cast<float *>(workspace) : nullptr, (hipStream_t)hip_stream));
+    PartsPlan m = plan.many;
+    char *const at = static_cast<char *>(workspace);
+    m.totals = weight ? reinterpret_cast<float *>(at) : nullptr;
+    m.sums = reinterpret_cast<f32x2 *>(at + plan.sums);
+    m.parts = reinterpret_cast<float *>(at + plan.parts);
+    return launched(launch_parts(a, m, q->dtype, (hipStream_t)hip_stream));
 }
 
 extern "C" dmi_status_t dmi_kv8_evict(const dmi_kv8_t *cache, const dmi_kv8_batch_t *batch, const dmi_kv8_weight_t *weight,

@@ -77,9 +77,18 @@ struct TokensPlan {
     float *scores;                              // [head][query row][score_stride]; NULL: no weights
 };
 
+// How many query rows are attended to: see dmi_kv8_parts.hip.
+struct PartsPlan {
+    uint32_t row_tiles;                         // workgroups for the rows that share a head
+    uint32_t splits, chunk;                     // parts of the longest context, their tokens
+    f32x2 *sums;                                // [row of out][split]: maximum, sum of 2^(score - maximum); one split: unused
+    float *parts;                               // [row of out][split][dim]
+    float *totals;                              // [row of out]: log2 of the sum of 2^score; NULL: no weights
+};
+
 hipError_t launch_append(const AppendArgs &a, uint32_t dtype, hipStream_t s);
 hipError_t launch_evict(const EvictArgs &a, hipStream_t s);
-hipError_t launch_attend(const AttendArgs &a, uint32_t dtype, float *lse2, hipStream_t s);
+hipError_t launch_parts(const AttendArgs &a, const PartsPlan &p, uint32_t dtype, hipStream_t s);
 hipError_t launch_tokens(const AttendArgs &a, const TokensPlan &p, uint32_t dtype, hipStream_t s);
 
 // ---------------------------------------------------------------- device side
