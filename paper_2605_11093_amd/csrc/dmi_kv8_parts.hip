@@ -7,39 +7,45 @@ namespace kv8 {
 
 constexpr int kTile = 64;                       // tokens that a workgroup has in LDS at a time
 
-// What is looked up of sixteens of tokens, one a lane: entry of the block table, scales.
+// What is looked up of sixteens of tokens, one a lane: entry of the block table, K's scale, V's as a power of two and inverted.
 struct Look {
     int entry;
-    float ks, vs;
+    float ks, lift, inv;
 };
-__device__ __forceinline__ Look look_up(const AttendArgs &a, const Request &q, uint32_t head, int t, int end)
+__device__ __forceinline__ Look look_up(const AttendArgs &a, const Request &q, uint32_t head, int t, int end, float scale)
 {
-    Look l{-1, 0.0f, 0.0f};
+    Look l{-1, 1.0f, -INFINITY, 0.0f};          // (what is not there is masked, and weighs nothing)
     if (t < end) {
         l.entry = entry_of(a.c, q.row, block_of(a.c, (uint32_t)t >> 4));
         if (l.entry >= 0) {
-            l.ks = *scale_at(a.c, 0, l.entry, head);
-            l.vs = *scale_at(a.c, 1, l.entry, head);
+            const float vs = *scale_at(a.c, 1, l.entry, head);
+            l.ks = *scale_at(a.c, 0, l.entry, head) * scale;
+            l.lift = log2_of(vs);
+            l.inv = 1.0f / vs;
         }
     }
     return l;
 }
 __device__ __forceinline__ float lane_value(float v, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane)); }
 
-// As in tokens_kernel, S^T = K Q^T and O^T = V^T P^T with query rows as columns, here with 32x32x16 instructions, 32 * NQ query
-// rows a wavefront, four wavefronts on the same tokens.  K and V are converted once for the workgroup, on their way into LDS: K as
-// it lies, V transposed, the tokens of a sixteen in the order in which the lanes' registers of S^T hold them (0-3, 8-11 for
-// lanes 0-31, 4-7, 12-15 for lanes 32-63), so that an operand is 16 bytes in a row.
-template <typename T, int DP, int NQ>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1)))
+// As in tokens_kernel, S^T = K Q^T and O^T = V^T P^T with query rows as columns, here with 32x32x16 instructions, 32 query rows a
+// wavefront, NW wavefronts on the same tokens.  K and V are converted once for the workgroup, on their way into LDS: K as it
+// lies, V transposed, the tokens of a sixteen in the order in which the lanes' registers of S^T hold them (0-3, 8-11 for lanes
+// 0-31, 4-7, 12-15 for lanes 32-63), so that an operand is 16 bytes in a row.  With two wavefronts on a SIMD one's exponentials
+// run beside the other's products.
+template <typename T, int DP, int NW>
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW / 4)))
 void parts_kernel(AttendArgs a, PartsPlan p)
 {
     constexpr int KP = DP * 2 + 16, VP = kTile * 2 + 16;        // bytes of a row in LDS, padded so that rows start on other banks
     constexpr int KK = DP / 16, ND = DP / 32;
-    constexpr int KL = DP / 64;                                 // 16-byte loads of K a thread
-    constexpr int VU = (DP / 2 + 63) / 64;                      // units of 8 tokens x 4 elements a thread
+    constexpr int U = 8 / NW;                                   // eights of the tile's tokens that a wavefront stages
+    constexpr int KL = DP <= 128 ? 1 : 2;                       // 16-byte loads of K a lane and eight
+    constexpr int VL = DP <= 128 ? 1 : 2;                       // units of 4 tokens x 4 elements a lane and eight
     __shared__ __align__(16) uint8_t lds[2 * (kTile * KP + DP * VP)];
-    __shared__ int nan_tile[2];                                 // the last tile in either half with a NaN in V, counted from 1
+    // NaNs in V: the last tile, counted from 1, that had one in an eight; a bit for each of 4 tokens
+    __shared__ int nan_tile[2][8];
+    __shared__ __align__(4) uint8_t nan_bits[2][8][2][DP];
     auto lk = [&](int buf) { return lds + buf * kTile * KP; };
     auto lv = [&](int buf) { return lds + 2 * kTile * KP + buf * DP * VP; };
 
@@ -49,288 +55,286 @@ void parts_kernel(AttendArgs a, PartsPlan p)
     if (pair >= a.b.n_reqs * a.c.heads) return;
     const uint32_t head = pair % a.c.heads, split = in % p.splits, row_tile = p.row_tiles - 1u - in / p.splits;
     const Request q = request_of(a.b, a.c, (int)(pair / a.c.heads));
-    const int rows = q.fresh * (int)a.group, row0 = (int)row_tile * 128 * NQ;
+    const int rows = q.fresh * (int)a.group, row0 = (int)row_tile * 32 * NW;
     if (row0 >= rows) return;
-    const int older = q.len - q.fresh, last_row = min(row0 + 128 * NQ, rows) - 1;
+    const int older = q.len - q.fresh, last_row = min(row0 + 32 * NW, rows) - 1;
     const int seen = older + last_row / (int)a.group + 1;       // tokens that the workgroup's last row sees
     const int begin = (int)(split * p.chunk), end = min(seen, begin + (int)p.chunk), tiles = max(0, (end - begin + kTile - 1) / kTile);
     if (split && tiles == 0) return;                            // (what reads the parts counts the same way)
 
     // the wavefront's query rows; a negative scale goes into their sign
-    u32x4 qf[NQ][KK];
-    int lim[NQ];
     const uint32_t flip = a.scale_log2 < 0.0f ? 0x80008000u : 0u;
-    const float scale = fabsf(a.scale_log2);
-    const int wave_row = row0 + wave * 32 * NQ;
-#pragma unroll
-    for (int n = 0; n < NQ; n++) {
-        const int row = wave_row + 32 * n + col;
-        const QueryRow w = query_row(a, head, (uint32_t)row);
-        lim[n] = row < rows ? older + w.token : -1;
+    const float scale = fmaxf(fabsf(a.scale_log2), 1e-30f);     // (-inf times 0 would be no mask)
+    const int wave_row = row0 + wave * 32, row = wave_row + col;
+    const QueryRow w = query_row(a, head, (uint32_t)row);
+    const int lim = row < rows ? older + w.token : -1;          // the last position that the column's query sees
+    u32x4 qf[KK];
+    {
         const uint16_t *src = static_cast<const uint16_t *>(a.q.data) + (int64_t)(q.start + w.token) * a.q.row_stride + (int64_t)w.head * a.q.head_stride;
 #pragma unroll
         for (int k = 0; k < KK; k++) {
             const int d = 16 * k + 8 * half;
-            qf[n][k] = u32x4{0u, 0u, 0u, 0u};
+            qf[k] = u32x4{0u, 0u, 0u, 0u};
             if (row < rows && d < (int)a.c.dim) {
-                qf[n][k] = *reinterpret_cast<const u32x4 *>(src + d);
+                qf[k] = *reinterpret_cast<const u32x4 *>(src + d);
 #pragma unroll
-                for (int i = 0; i < 4; i++) qf[n][k][i] ^= flip;
+                for (int i = 0; i < 4; i++) qf[k][i] ^= flip;
             }
         }
     }
     // what the first and the last of them see
-    const int least = wave_row < rows ? older + wave_row / (int)a.group : -1;
-    const int most = wave_row < rows ? older + min(wave_row + 32 * NQ - 1, rows - 1) / (int)a.group : -1;
-    const bool ragged = wave_row + 32 * NQ > rows;              // (columns past the rows see nothing)
+    const int least = wave_row + 32 <= rows ? older + wave_row / (int)a.group : -1;
+    const int most = wave_row < rows ? older + min(wave_row + 31, rows - 1) / (int)a.group : -1;
 
-    // A wavefront stages a sixteen of the tile's four.
-    u32x4 rk[KL];
-    uint32_t rv[VU][8];
-    Look here{-1, 0.0f, 0.0f}, stage{-1, 0.0f, 0.0f};
-    auto fetch = [&](int tile) {
-        const int t = begin + kTile * tile + 16 * wave, six = (4 * tile + wave) & 63;
-        const int entry = __builtin_amdgcn_readlane(stage.entry, six);
-        const int64_t at = (int64_t)max(entry, 0) * a.c.block_stride +
-                           (int64_t)((uint32_t)t - block_of(a.c, (uint32_t)t >> 4) * a.c.bs) * a.c.slot_stride + (int64_t)head * a.c.head_stride;
-        const Buffer k = buffer_at(a.c.code[0] + at), v = buffer_at(a.c.code[1] + at);
-        const int there = entry < 0 ? 0 : min(16, end - t);
+    u32x4 rk[U][KL];
+    uint32_t rv[U][VL][4];
+    int there_v[U];
+    Look now{-1, 1.0f, -INFINITY, 0.0f}, next = now;            // of the 16 tiles that this one lies in, and the 16 behind them
+    auto fetch = [&](int tile, const Look &l) {
 #pragma unroll
-        for (int c = 0; c < KL; c++) {
-            const uint32_t d = 64u * c + 16u * (lane & 3);
-            rk[c] = load_b128<0>(k, (uint32_t)(lane >> 2) * (uint32_t)a.c.slot_stride + (d < a.c.dim ? d : 0u));
-        }
+        for (int u = 0; u < U; u++) {
+            const int eight = wave + NW * u, t = begin + kTile * tile + 16 * (eight >> 1);
+            const int entry = __builtin_amdgcn_readlane(l.entry, (4 * tile + (eight >> 1)) & 63);
+            const int64_t at = (int64_t)max(entry, 0) * a.c.block_stride +
+                               (int64_t)((uint32_t)t - block_of(a.c, (uint32_t)t >> 4) * a.c.bs) * a.c.slot_stride + (int64_t)head * a.c.head_stride;
+            const Buffer k = buffer_at(a.c.code[0] + at), v = buffer_at(a.c.code[1] + at);
+            there_v[u] = entry < 0 ? 0 : min(16, end - t);
 #pragma unroll
-        for (int u = 0; u < VU; u++) {
-            const int unit = lane + 64 * u, h = unit / (DP / 4) & 1, d = 4 * (unit % (DP / 4));
+            for (int c = 0; c < KL; c++) {      // 8 lanes a token (4 if it has 64 elements)
+                const uint32_t d = DP == 64 ? 16u * (lane & 3) : 128u * c + 16u * (lane & 7), token = 8u * (eight & 1) + (DP == 64 ? (lane >> 2 & 7) : lane >> 3);
+                rk[u][c] = load_b128<0>(k, token * (uint32_t)a.c.slot_stride + (d < a.c.dim ? d : 0u));
+            }
 #pragma unroll
-            for (int i = 0; i < 8; i++) {
-                const int token = 4 * h + (i & 3) + 8 * (i >> 2);
-                rv[u][i] = load_b32<0>(v, (uint32_t)token * (uint32_t)a.c.slot_stride + (d < (int)a.c.dim ? (uint32_t)d : 0u));
-                rv[u][i] = token < there ? rv[u][i] : 0u;
+            for (int c = 0; c < VL; c++) {
+                const int unit = lane + 64 * c, d = 4 * (unit % (DP / 4)), token = 4 * (eight & 1) + 8 * (unit / (DP / 4) & 1);
+#pragma unroll
+                for (int i = 0; i < 4; i++)
+                    rv[u][c][i] = load_b32<0>(v, (uint32_t)(token + i) * (uint32_t)a.c.slot_stride + (d < (int)a.c.dim ? (uint32_t)d : 0u));
             }
         }
     };
     auto place = [&](int tile) {
-        const int buf = tile & 1;
+        uint8_t *const to_k = lk(tile & 1), *const to_v = lv(tile & 1);
 #pragma unroll
-        for (int c = 0; c < KL; c++) {
-            uint8_t *to = lk(buf) + (16 * wave + (lane >> 2)) * KP + 2 * (64 * c + 16 * (lane & 3));
-            const u32x4 lo = {T::two_codes(rk[c][0], false), T::two_codes(rk[c][0], true), T::two_codes(rk[c][1], false), T::two_codes(rk[c][1], true)};
-            const u32x4 hi = {T::two_codes(rk[c][2], false), T::two_codes(rk[c][2], true), T::two_codes(rk[c][3], false), T::two_codes(rk[c][3], true)};
-            *reinterpret_cast<u32x4 *>(to) = lo;
-            *reinterpret_cast<u32x4 *>(to + 16) = hi;
-        }
-        uint32_t any = 0;
+        for (int u = 0; u < U; u++) {
+            const int eight = wave + NW * u;
 #pragma unroll
-        for (int u = 0; u < VU; u++) {
-            const int unit = lane + 64 * u, h = unit / (DP / 4) & 1, d = 4 * (unit % (DP / 4));
-            if (unit < DP / 2) {
-                u32x4 e[4];
+            for (int c = 0; c < KL; c++) {
+                const int d = DP == 64 ? 16 * (lane & 3) : 128 * c + 16 * (lane & 7), token = 8 * eight + (DP == 64 ? lane >> 2 : lane >> 3);
+                const u32x4 r = rk[u][c];
+                if (DP > 64 || lane < 32) {
+                    *reinterpret_cast<u32x4 *>(to_k + token * KP + 2 * d) = u32x4{T::two_codes(r[0], false), T::two_codes(r[0], true), T::two_codes(r[1], false), T::two_codes(r[1], true)};
+                    *reinterpret_cast<u32x4 *>(to_k + token * KP + 2 * d + 16) = u32x4{T::two_codes(r[2], false), T::two_codes(r[2], true), T::two_codes(r[3], false), T::two_codes(r[3], true)};
+                }
+            }
+            uint32_t any = 0;
+#pragma unroll
+            for (int c = 0; c < VL; c++)
 #pragma unroll
                 for (int i = 0; i < 4; i++) {
-                    any |= nan_codes(rv[u][2 * i]) | nan_codes(rv[u][2 * i + 1]);
-                    const uint32_t lo = __builtin_amdgcn_perm(rv[u][2 * i + 1], rv[u][2 * i], 0x05010400u);
-                    const uint32_t hi = __builtin_amdgcn_perm(rv[u][2 * i + 1], rv[u][2 * i], 0x07030602u);
+                    rv[u][c][i] = 4 * (eight & 1) + 8 * ((lane + 64 * c) / (DP / 4) & 1) + i < there_v[u] ? rv[u][c][i] : 0u;
+                    any |= nan_codes(rv[u][c][i]);
+                }
+            if (__ballot(any != 0)) {           // 0 takes a NaN's place, and the queries that see it are given it apart
+                if (lane == 0) nan_tile[tile & 1][eight] = tile + 1;
+#pragma unroll
+                for (int c = 0; c < VL; c++) {
+                    const int unit = lane + 64 * c, d = 4 * (unit % (DP / 4));
+                    uint32_t bits = 0;
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        const uint32_t top = nan_codes(rv[u][c][i]);
+                        bits |= top >> (7 - i);
+                        rv[u][c][i] &= ~(top | (top - (top >> 7)));
+                    }
+                    if (DP > 64 || lane < 32) *reinterpret_cast<uint32_t *>(&nan_bits[tile & 1][eight][unit / (DP / 4) & 1][d]) = bits;
+                }
+            }
+#pragma unroll
+            for (int c = 0; c < VL; c++) {
+                const int unit = lane + 64 * c, d = 4 * (unit % (DP / 4)), quad = unit / (DP / 4) & 1;
+                const uint32_t *r = rv[u][c];
+                u32x2 e[4];
+#pragma unroll
+                for (int i = 0; i < 2; i++) {
+                    const uint32_t lo = __builtin_amdgcn_perm(r[2 * i + 1], r[2 * i], 0x05010400u);
+                    const uint32_t hi = __builtin_amdgcn_perm(r[2 * i + 1], r[2 * i], 0x07030602u);
                     e[0][i] = T::two_codes(lo, false), e[1][i] = T::two_codes(lo, true);
                     e[2][i] = T::two_codes(hi, false), e[3][i] = T::two_codes(hi, true);
                 }
+                if (DP > 64 || lane < 32) {
 #pragma unroll
-                for (int i = 0; i < 4; i++) *reinterpret_cast<u32x4 *>(lv(buf) + (d + i) * VP + 32 * wave + 16 * h) = e[i];
+                    for (int i = 0; i < 4; i++) *reinterpret_cast<u32x2 *>(to_v + (d + i) * VP + 16 * eight + 8 * quad) = e[i];
+                }
             }
         }
-        if (__ballot(any != 0) && lane == 0) nan_tile[buf] = tile + 1;
     };
 
-    float m[NQ], base[NQ], l[NQ], v_ref = T::kNarrow ? 0.0f : 1.0f;
-    f32x16 o[NQ][ND];
+    float m = -INFINITY, base = 0.0f, l = 0.0f, lift_ref = T::kNarrow ? -INFINITY : 0.0f;
+    f32x16 o[ND];
 #pragma unroll
-    for (int n = 0; n < NQ; n++) {
-        m[n] = -INFINITY, base[n] = 0.0f, l[n] = 0.0f;
+    for (int d = 0; d < ND; d++)
 #pragma unroll
-        for (int d = 0; d < ND; d++)
-#pragma unroll
-            for (int i = 0; i < 16; i++) o[n][d][i] = 0.0f;
-    }
+        for (int i = 0; i < 16; i++) o[d][i] = 0.0f;
 
-    if (threadIdx.x < 2) nan_tile[threadIdx.x] = 0;
+    if (threadIdx.x < 16) nan_tile[threadIdx.x >> 3][threadIdx.x & 7] = 0;
     if (tiles) {
-        stage = look_up(a, q, head, begin + 16 * lane, end);
-        here = stage;
-        fetch(0);
+        now = look_up(a, q, head, begin + 16 * lane, end, scale);
+        fetch(0, now);
     }
-    __syncthreads();
+    __syncthreads();                            // (the NaN flags are cleared)
     if (tiles) place(0);
     for (int tile = 0; tile < tiles; tile++) {
         const int buf = tile & 1, t0 = begin + kTile * tile;
-        if (tile && (tile & 15) == 0) here = stage;
+        if (tile && (tile & 15) == 0) now = next;
         if (tile + 1 < tiles) {
-            if (((tile + 1) & 15) == 0) stage = look_up(a, q, head, begin + kTile * (tile + 1) + 16 * lane, end);
-            fetch(tile + 1);
+            if (((tile + 1) & 15) == 0) {
+                next = look_up(a, q, head, begin + kTile * (tile + 1) + 16 * lane, end, scale);
+                fetch(tile + 1, next);
+            } else {
+                fetch(tile + 1, now);
+            }
         }
         __syncthreads();                        // this tile is in LDS
         if (t0 <= most) {
+            f32x16 z[2];
 #pragma unroll
             for (int sub = 0; sub < 2; sub++) {
-                const int t = t0 + 32 * sub;
-                if (t > most) break;
-                float ks[2], vs[2];
-                bool there = true;
 #pragma unroll
-                for (int x = 0; x < 2; x++) {
-                    const int six = (4 * tile + 2 * sub + x) & 63;
-                    ks[x] = lane_value(here.ks, six) * scale;
-                    vs[x] = lane_value(here.vs, six);
-                    there = there && __builtin_amdgcn_readlane(here.entry, six) >= 0;
-                }
-                f32x16 z[NQ];
-#pragma unroll
-                for (int n = 0; n < NQ; n++)
-#pragma unroll
-                    for (int i = 0; i < 16; i++) z[n][i] = 0.0f;
+                for (int i = 0; i < 16; i++) z[sub][i] = 0.0f;
 #pragma unroll
                 for (int k = 0; k < KK; k++) {
                     const u32x4 f = *reinterpret_cast<const u32x4 *>(lk(buf) + (32 * sub + col) * KP + 32 * k + 16 * half);
-#pragma unroll
-                    for (int n = 0; n < NQ; n++) z[n] = T::mfma32(f, qf[n][k], z[n]);
+                    z[sub] = T::mfma32(f, qf[k], z[sub]);
                 }
-                const bool full = there && t + 31 <= least && !ragged;
-                if (!full) {
+            }
+            float ks[4], lift[4], inv[4];
+            bool there = true;
+#pragma unroll
+            for (int x = 0; x < 4; x++) {
+                const int six = (4 * tile + x) & 63;
+                ks[x] = lane_value(now.ks, six);
+                lift[x] = lane_value(now.lift, six);
+                inv[x] = lane_value(now.inv, six);
+                there = there && __builtin_amdgcn_readlane(now.entry, six) >= 0;
+            }
+            if (!there || t0 + kTile - 1 > least) {
+#pragma unroll
+                for (int sub = 0; sub < 2; sub++)
 #pragma unroll
                     for (int i = 0; i < 16; i++) {
-                        const int at = t + 8 * (i >> 2) + 4 * half + (i & 3);
-                        const bool is = __builtin_amdgcn_readlane(here.entry, (4 * tile + 2 * sub + (i >> 3)) & 63) >= 0;
-#pragma unroll
-                        for (int n = 0; n < NQ; n++) z[n][i] = is && at <= lim[n] ? z[n][i] : -INFINITY;
+                        const int at = t0 + 32 * sub + 8 * (i >> 2) + 4 * half + (i & 3);
+                        const bool is = __builtin_amdgcn_readlane(now.entry, (4 * tile + 2 * sub + (i >> 3)) & 63) >= 0;
+                        z[sub][i] = is && at <= lim ? z[sub][i] : -INFINITY;
                     }
+            }
+            float top = -INFINITY;
+#pragma unroll
+            for (int x = 0; x < 4; x++) {
+                const f32x16 &s = z[x >> 1];
+                const int i = 8 * (x & 1);
+                top = fmaxf(top, fmaxf(fmaxf(fmaxf(s[i], s[i + 1]), fmaxf(s[i + 2], s[i + 3])), fmaxf(fmaxf(s[i + 4], s[i + 5]), fmaxf(s[i + 6], s[i + 7]))) * ks[x]);
+            }
+            if (__ballot(top > m + kSlack)) {   // the sums against a higher maximum
+                const float to = fmaxf(m, fmaxf(top, __shfl_xor(top, 32)));
+                const float f = to == -INFINITY ? 1.0f : exp2_of(m - to);
+                m = to;
+                base = to == -INFINITY ? 0.0f : to;
+                l *= f;
+#pragma unroll
+                for (int d = 0; d < ND; d++) o[d] *= f;
+            }
+            if constexpr (T::kNarrow) {         // V's scale relative to the largest yet, to stay within fp16's range
+                const float largest = fmaxf(fmaxf(lift[0], lift[1]), fmaxf(lift[2], lift[3]));
+                if (largest > lift_ref) {
+                    const float f = exp2_of(lift_ref - largest);
+#pragma unroll
+                    for (int d = 0; d < ND; d++) o[d] *= f;
+                    lift_ref = largest;
                 }
-                bool rises = false;
-                float top[NQ];
+                const float ref = exp2_of(lift_ref);
 #pragma unroll
-                for (int n = 0; n < NQ; n++) {
-                    float x[2];
-#pragma unroll
-                    for (int y = 0; y < 2; y++)
-                        x[y] = fmaxf(fmaxf(fmaxf(z[n][8 * y], z[n][8 * y + 1]), fmaxf(z[n][8 * y + 2], z[n][8 * y + 3])),
-                                     fmaxf(fmaxf(z[n][8 * y + 4], z[n][8 * y + 5]), fmaxf(z[n][8 * y + 6], z[n][8 * y + 7])));
-                    // (-inf stays -inf, also where a scale is 0)
-                    top[n] = fmaxf(full || x[0] != -INFINITY ? x[0] * ks[0] : x[0], full || x[1] != -INFINITY ? x[1] * ks[1] : x[1]);
-                    rises |= top[n] > m[n] + kSlack;
+                for (int x = 0; x < 4; x++) {
+                    lift[x] = lift_ref == -INFINITY ? lift[x] : lift[x] - lift_ref;
+                    inv[x] *= ref;
                 }
-                if (__ballot(rises)) {
+            }
+            // p, times V's scale (in the exponent; what is summed is divided by it again)
+            u32x4 pf[4];
 #pragma unroll
-                    for (int n = 0; n < NQ; n++) {
-                        const float now = fmaxf(m[n], fmaxf(top[n], __shfl_xor(top[n], 32)));
-                        const float f = now == -INFINITY ? 1.0f : exp2_of(m[n] - now);
-                        m[n] = now;
-                        base[n] = now == -INFINITY ? 0.0f : now;
-                        l[n] *= f;
+            for (int x = 0; x < 4; x++) {
+                const float off = lift[x] - base;
+                float e[8], sum = 0.0f;
 #pragma unroll
-                        for (int d = 0; d < ND; d++) o[n][d] *= f;
-                    }
+                for (int i = 0; i < 8; i++) {
+                    e[i] = exp2_of(__builtin_fmaf(z[x >> 1][8 * (x & 1) + i], ks[x], off));
+                    sum += e[i];
                 }
-                if constexpr (T::kNarrow) {     // V's scale relative to the largest yet, to stay within fp16's range
-                    const float largest = fmaxf(vs[0], vs[1]);
-                    if (largest > v_ref) {
-                        const float f = v_ref / largest;
+                l = __builtin_fmaf(sum, inv[x], l);
 #pragma unroll
-                        for (int n = 0; n < NQ; n++)
+                for (int i = 0; i < 4; i++) pf[x][i] = T::pack(e[2 * i], e[2 * i + 1]);
+            }
 #pragma unroll
-                            for (int d = 0; d < ND; d++) o[n][d] *= f;
-                        v_ref = largest;
-                    }
-                    const float inv = v_ref > 0.0f ? 1.0f / v_ref : 0.0f;
-                    vs[0] *= inv, vs[1] *= inv;
+            for (int x = 0; x < 4; x++)
+#pragma unroll
+                for (int d = 0; d < ND; d++) {
+                    const u32x4 f = *reinterpret_cast<const u32x4 *>(lv(buf) + (32 * d + col) * VP + 32 * x + 16 * half);
+                    o[d] = T::mfma32(f, pf[x], o[d]);
                 }
-                u32x4 pf[NQ][2];
+            // a NaN in V reaches the queries that see it, and no others
+#pragma unroll 1
+            for (int e8 = 0; e8 < 8; e8++) {
+                if (nan_tile[buf][e8] != tile + 1) continue;
+                uint32_t sees[2] = {0u, 0u};
 #pragma unroll
-                for (int n = 0; n < NQ; n++)
-#pragma unroll
-                    for (int x = 0; x < 2; x++) {
-                        float e[8];
-#pragma unroll
-                        for (int i = 0; i < 8; i++) {
-                            const float s = z[n][8 * x + i];
-                            e[i] = exp2_of(full ? s * ks[x] - base[n] : s == -INFINITY ? s : s * ks[x] - base[n]);
-                            l[n] += e[i];
-                            e[i] *= vs[x];
-                        }
-#pragma unroll
-                        for (int i = 0; i < 4; i++) pf[n][x][i] = T::pack(e[2 * i], e[2 * i + 1]);
-                    }
-                const bool mixed = !full && nan_tile[buf] == tile + 1;
+                for (int i = 0; i < 8; i++)
+                    if (t0 + 16 * (e8 >> 1) + 4 * (e8 & 1) + (i & 3) + 8 * (i >> 2) <= lim) sees[i >> 2] |= 0x01010101u << (i & 3);
 #pragma unroll
                 for (int d = 0; d < ND; d++)
 #pragma unroll
-                    for (int x = 0; x < 2; x++) {
-                        u32x4 f = *reinterpret_cast<const u32x4 *>(lv(buf) + (32 * d + col) * VP + 64 * sub + 32 * x + 16 * half);
-                        if (mixed) {            // a NaN in V reaches the queries that see it, and 0 * NaN no other
-                            u32x4 bad;
+                    for (int y = 0; y < 4; y++) {
+                        const int e = 32 * d + 8 * y + 4 * half;
+                        const uint32_t bits = (*reinterpret_cast<const uint32_t *>(&nan_bits[buf][e8][0][e]) & sees[0]) |
+                                              (*reinterpret_cast<const uint32_t *>(&nan_bits[buf][e8][1][e]) & sees[1]);
 #pragma unroll
-                            for (int i = 0; i < 4; i++) {
-                                const bool lo = (f[i] & 0x7FFFu) > T::kInf, hi = (f[i] >> 16 & 0x7FFFu) > T::kInf;
-                                bad[i] = (lo ? T::kOne : 0u) | (hi ? T::kOne << 16 : 0u);
-                                f[i] &= (lo ? 0u : 0xFFFFu) | (hi ? 0u : 0xFFFF0000u);
-                            }
-#pragma unroll
-                            for (int n = 0; n < NQ; n++) {
-                                u32x4 sees;
-#pragma unroll
-                                for (int i = 0; i < 4; i++) {
-                                    const int at = t + 16 * x + 4 * half + 8 * (i >> 1) + 2 * (i & 1);
-                                    sees[i] = (at <= lim[n] ? T::kOne : 0u) | (at + 1 <= lim[n] ? T::kOne << 16 : 0u);
-                                }
-                                f32x16 nans;
-#pragma unroll
-                                for (int i = 0; i < 16; i++) nans[i] = 0.0f;
-                                nans = T::mfma32(bad, sees, nans);
-#pragma unroll
-                                for (int i = 0; i < 16; i++) o[n][d][i] += nans[i] > 0.0f ? NAN : 0.0f;
-                            }
-                        }
-#pragma unroll
-                        for (int n = 0; n < NQ; n++) o[n][d] = T::mfma32(f, pf[n][x], o[n][d]);
+                        for (int i = 0; i < 4; i++) o[d][4 * y + i] += bits >> (8 * i) & 0xFFu ? NAN : 0.0f;
                     }
             }
         }
         if (tile + 1 < tiles) place(tile + 1);
     }
 
+    const float v_ref = T::kNarrow ? exp2_of(lift_ref) : 1.0f;
+    l += __shfl_xor(l, 32);
+    if (row >= rows) return;
+    const int64_t at = (int64_t)(q.start + w.token) * a.q_heads + w.head;
+    const bool empty = m == -INFINITY && l == 0.0f;
+    if (p.splits == 1) {
+        const float f = (empty ? 0.0f : 1.0f / l) * v_ref;
+        uint16_t *dst = static_cast<uint16_t *>(a.out.data) + (int64_t)(q.start + w.token) * a.out.row_stride + (int64_t)w.head * a.out.head_stride;
 #pragma unroll
-    for (int n = 0; n < NQ; n++) {
-        l[n] += __shfl_xor(l[n], 32);
-        const int row = wave_row + 32 * n + col;
-        if (row >= rows) continue;
-        const QueryRow w = query_row(a, head, (uint32_t)row);
-        const int64_t at = (int64_t)(q.start + w.token) * a.q_heads + w.head;
-        const bool empty = m[n] == -INFINITY && l[n] == 0.0f;
-        if (p.splits == 1) {
-            const float f = (empty ? 0.0f : 1.0f / l[n]) * v_ref;
-            uint16_t *dst = static_cast<uint16_t *>(a.out.data) + (int64_t)(q.start + w.token) * a.out.row_stride + (int64_t)w.head * a.out.head_stride;
+        for (int d = 0; d < ND; d++)
 #pragma unroll
-            for (int d = 0; d < ND; d++)
-#pragma unroll
-                for (int i = 0; i < 16; i += 4) {
-                    const int e = 32 * d + 2 * i + 4 * half;
-                    if (e < (int)a.c.dim)
-                        *reinterpret_cast<u32x2 *>(dst + e) = u32x2{T::pack(o[n][d][i] * f, o[n][d][i + 1] * f), T::pack(o[n][d][i + 2] * f, o[n][d][i + 3] * f)};
-                }
-            if (half == 0) {
-                const float sum = empty ? -INFINITY : m[n] + log2_of(l[n]);
-                if (a.lse) a.lse[at] = sum * kLn2;
-                if (p.totals) p.totals[at] = sum;
+            for (int i = 0; i < 16; i += 4) {
+                const int e = 32 * d + 2 * i + 4 * half;
+                if (e < (int)a.c.dim)
+                    *reinterpret_cast<u32x2 *>(dst + e) = u32x2{T::pack(o[d][i] * f, o[d][i + 1] * f), T::pack(o[d][i + 2] * f, o[d][i + 3] * f)};
             }
-        } else {
-            if (half == 0) p.sums[at * p.splits + split] = f32x2{m[n], l[n]};
-            float *dst = p.parts + (at * p.splits + split) * a.c.dim;
-#pragma unroll
-            for (int d = 0; d < ND; d++)
-#pragma unroll
-                for (int i = 0; i < 16; i += 4) {
-                    const int e = 32 * d + 2 * i + 4 * half;
-                    if (e < (int)a.c.dim) *reinterpret_cast<f32x4 *>(dst + e) = f32x4{o[n][d][i], o[n][d][i + 1], o[n][d][i + 2], o[n][d][i + 3]} * v_ref;
-                }
+        if (half == 0) {
+            const float sum = empty ? -INFINITY : m + log2_of(l);
+            if (a.lse) a.lse[at] = sum * kLn2;
+            if (p.totals) p.totals[at] = sum;
         }
+    } else {
+        if (half == 0) p.sums[at * p.splits + split] = f32x2{m, l};
+        float *dst = p.parts + (at * p.splits + split) * a.c.dim;
+#pragma unroll
+        for (int d = 0; d < ND; d++)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const int e = 32 * d + 2 * i + 4 * half;
+                if (e < (int)a.c.dim) *reinterpret_cast<f32x4 *>(dst + e) = f32x4{o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]} * v_ref;
+            }
     }
 }
 
@@ -388,11 +392,11 @@ __global__ __launch_bounds__(256) void weights_kernel(AttendArgs a, PartsPlan p)
     const int first_row = max(0, block0 - older) * (int)a.group, tiles = (rows - first_row + 31) / 32;
 
     // K of the wavefront's tokens: two 32s, their sixteens' scales
-    const Look l = look_up(a, q, head, t0 + 16 * lane, lane < 4 ? q.len : 0);
+    const Look l = look_up(a, q, head, t0 + 16 * lane, lane < 4 ? q.len : 0, a.scale_log2);
     u32x4 kf[2][KK];
     float ks[4];
 #pragma unroll
-    for (int x = 0; x < 4; x++) ks[x] = lane_value(l.ks, x) * a.scale_log2;
+    for (int x = 0; x < 4; x++) ks[x] = lane_value(l.ks, x);
 #pragma unroll
     for (int s = 0; s < 2; s++) {
         const int t = t0 + 32 * s + col, e0 = __builtin_amdgcn_readlane(l.entry, 2 * s), e1 = __builtin_amdgcn_readlane(l.entry, 2 * s + 1);
@@ -488,13 +492,13 @@ __global__ __launch_bounds__(256) void weights_kernel(AttendArgs a, PartsPlan p)
         }
 }
 
-template <typename T, int DP, int NQ> static hipError_t parts(const AttendArgs &a, const PartsPlan &p, hipStream_t s)
+template <typename T, int DP, int NW> static hipError_t parts(const AttendArgs &a, const PartsPlan &p, hipStream_t s)
 {
     const uint32_t pairs = (a.b.n_reqs * a.c.heads + 7u) / 8u;
-    parts_kernel<T, DP, NQ><<<dim3(pairs * p.row_tiles * p.splits * 8u), 256, 0, s>>>(a, p);
+    parts_kernel<T, DP, NW><<<dim3(pairs * p.row_tiles * p.splits * 8u), 64 * NW, 0, s>>>(a, p);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && p.splits > 1u) {
-        join_parts_kernel<T><<<dim3((a.b.max_new * a.q_heads + 3u) / 4u, a.b.n_reqs), 256, 0, s>>>(a, p, 128u * NQ);
+        join_parts_kernel<T><<<dim3((a.b.max_new * a.q_heads + 3u) / 4u, a.b.n_reqs), 256, 0, s>>>(a, p, 32u * NW);
         e = hipGetLastError();
     }
     if (e == hipSuccess && a.w.data) {
@@ -506,7 +510,7 @@ template <typename T, int DP, int NQ> static hipError_t parts(const AttendArgs &
 
 template <typename T> static hipError_t parts_of(const AttendArgs &a, const PartsPlan &p, hipStream_t s)
 {
-    return a.c.dim <= 64 ? parts<T, 64, 2>(a, p, s) : a.c.dim <= 128 ? parts<T, 128, 2>(a, p, s) : parts<T, 256, 1>(a, p, s);
+    return a.c.dim <= 64 ? parts<T, 64, 8>(a, p, s) : a.c.dim <= 128 ? parts<T, 128, 8>(a, p, s) : parts<T, 256, 4>(a, p, s);
 }
 
 hipError_t launch_parts(const AttendArgs &a, const PartsPlan &p, uint32_t dtype, hipStream_t s)
