@@ -37,17 +37,21 @@ template <typename T, int DP, int NW>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW / 4)))
 void parts_kernel(AttendArgs a, PartsPlan p)
 {
-    constexpr int KP = DP * 2 + 16, VP = kTile * 2 + 16;        // bytes of a row in LDS, padded so that rows start on other banks
+    constexpr int KP = DP * 2 + 16, VP = kTile * 2;             // bytes of a row in LDS; K's are padded so that rows start on other banks
     constexpr int KK = DP / 16, ND = DP / 32;
     constexpr int U = 8 / NW;                                   // eights of the tile's tokens that a wavefront stages
     constexpr int KL = DP <= 128 ? 1 : 2;                       // 16-byte loads of K a lane and eight
     constexpr int VL = DP <= 128 ? 1 : 2;                       // units of 4 tokens x 4 elements a lane and eight
     __shared__ __align__(16) uint8_t lds[2 * (kTile * KP + DP * VP)];
     // NaNs in V: the last tile, counted from 1, that had one in an eight; a bit for each of 4 tokens
-    __shared__ int nan_tile[2][8];
+    __shared__ int nan_tile[2][8], nan_any[2];
     __shared__ __align__(4) uint8_t nan_bits[2][8][2][DP];
     auto lk = [&](int buf) { return lds + buf * kTile * KP; };
     auto lv = [&](int buf) { return lds + 2 * kTile * KP + buf * DP * VP; };
+
+    // V's 16-byte chunks are exchanged by row, so that neither the rows that lanes read nor those that they write (every fourth) meet
+    // on a bank
+    auto chunk_of = [](int row, int chunk) { return chunk ^ ((row >> 2 & 3) | ((row >> 1 ^ row >> 4) & 1) << 2); };
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
     // the row tiles of a request and head on one XCD, those that see most first
@@ -136,7 +140,7 @@ void parts_kernel(AttendArgs a, PartsPlan p)
                     any |= nan_codes(rv[u][c][i]);
                 }
             if (__ballot(any != 0)) {           // 0 takes a NaN's place, and the queries that see it are given it apart
-                if (lane == 0) nan_tile[tile & 1][eight] = tile + 1;
+                if (lane == 0) nan_tile[tile & 1][eight] = nan_any[tile & 1] = tile + 1;
 #pragma unroll
                 for (int c = 0; c < VL; c++) {
                     const int unit = lane + 64 * c, d = 4 * (unit % (DP / 4));
@@ -164,7 +168,7 @@ void parts_kernel(AttendArgs a, PartsPlan p)
                 }
                 if (DP > 64 || lane < 32) {
 #pragma unroll
-                    for (int i = 0; i < 4; i++) *reinterpret_cast<u32x2 *>(to_v + (d + i) * VP + 16 * eight + 8 * quad) = e[i];
+                    for (int i = 0; i < 4; i++) *reinterpret_cast<u32x2 *>(to_v + (d + i) * VP + 16 * chunk_of(d + i, eight) + 8 * quad) = e[i];
                 }
             }
         }
@@ -177,7 +181,7 @@ void parts_kernel(AttendArgs a, PartsPlan p)
 #pragma unroll
         for (int i = 0; i < 16; i++) o[d][i] = 0.0f;
 
-    if (threadIdx.x < 16) nan_tile[threadIdx.x >> 3][threadIdx.x & 7] = 0;
+    if (threadIdx.x < 16) nan_tile[threadIdx.x >> 3][threadIdx.x & 7] = nan_any[threadIdx.x & 1] = 0;
     if (tiles) {
         now = look_up(a, q, head, begin + 16 * lane, end, scale);
         fetch(0, now);
@@ -197,6 +201,7 @@ void parts_kernel(AttendArgs a, PartsPlan p)
         }
         __syncthreads();                        // this tile is in LDS
         if (t0 <= most) {
+            const bool nans = nan_any[buf] == tile + 1;
             f32x16 z[2];
 #pragma unroll
             for (int sub = 0; sub < 2; sub++) {
@@ -278,12 +283,12 @@ void parts_kernel(AttendArgs a, PartsPlan p)
             for (int x = 0; x < 4; x++)
 #pragma unroll
                 for (int d = 0; d < ND; d++) {
-                    const u32x4 f = *reinterpret_cast<const u32x4 *>(lv(buf) + (32 * d + col) * VP + 32 * x + 16 * half);
+                    const u32x4 f = *reinterpret_cast<const u32x4 *>(lv(buf) + (32 * d + col) * VP + 16 * chunk_of(col, 2 * x + half));
                     o[d] = T::mfma32(f, pf[x], o[d]);
                 }
             // a NaN in V reaches the queries that see it, and no others
 #pragma unroll 1
-            for (int e8 = 0; e8 < 8; e8++) {
+            for (int e8 = 0; nans && e8 < 8; e8++) {
                 if (nan_tile[buf][e8] != tile + 1) continue;
                 uint32_t sees[2] = {0u, 0u};
 #pragma unroll
