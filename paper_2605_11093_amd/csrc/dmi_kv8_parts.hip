@@ -174,6 +174,9 @@ void parts_kernel(AttendArgs a, PartsPlan p)
         }
     };
 
+    auto v_part = [&](int buf, int x, int d) {  // elements 32d.. of a sixteen's V
+        return *reinterpret_cast<const u32x4 *>(lv(buf) + (32 * d + col) * VP + 16 * chunk_of(col, 2 * x + half));
+    };
     float m = -INFINITY, base = 0.0f, l = 0.0f, lift_ref = T::kNarrow ? -INFINITY : 0.0f;
     f32x16 o[ND];
 #pragma unroll
@@ -202,16 +205,28 @@ void parts_kernel(AttendArgs a, PartsPlan p)
         __syncthreads();                        // this tile is in LDS
         if (t0 <= most) {
             const bool nans = nan_any[buf] == tile + 1;
+            // Operands are read from LDS eight ahead of the instructions that take them, V's first ones while K's last are used
+            // (left to itself the compiler reads one or two ahead, and every instruction waits for most of a trip to LDS).
             f32x16 z[2];
+            u32x4 kf[8], vf[8];
+            auto k_part = [&](int i) { return *reinterpret_cast<const u32x4 *>(lk(buf) + (32 * (i / KK) + col) * KP + 32 * (i % KK) + 16 * half); };
 #pragma unroll
-            for (int sub = 0; sub < 2; sub++) {
+            for (int i = 0; i < 8; i++) kf[i] = k_part(i);
+#pragma unroll
+            for (int sub = 0; sub < 2; sub++)
 #pragma unroll
                 for (int i = 0; i < 16; i++) z[sub][i] = 0.0f;
 #pragma unroll
-                for (int k = 0; k < KK; k++) {
-                    const u32x4 f = *reinterpret_cast<const u32x4 *>(lk(buf) + (32 * sub + col) * KP + 32 * k + 16 * half);
-                    z[sub] = T::mfma32(f, qf[k], z[sub]);
-                }
+            for (int i = 0; i < 2 * KK; i++) {
+                z[i / KK] = T::mfma32(kf[i % 8], qf[i % KK], z[i / KK]);
+                if (i + 8 < 2 * KK) kf[i % 8] = k_part(i + 8);
+                else vf[i + 8 - 2 * KK] = v_part(buf, (i + 8 - 2 * KK) / ND, (i + 8 - 2 * KK) % ND);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+#pragma unroll
+            for (int i = 0; i < 2 * KK; i++) {
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
             }
             float ks[4], lift[4], inv[4];
             bool there = true;
@@ -280,12 +295,10 @@ void parts_kernel(AttendArgs a, PartsPlan p)
                 for (int i = 0; i < 4; i++) pf[x][i] = T::pack(e[2 * i], e[2 * i + 1]);
             }
 #pragma unroll
-            for (int x = 0; x < 4; x++)
-#pragma unroll
-                for (int d = 0; d < ND; d++) {
-                    const u32x4 f = *reinterpret_cast<const u32x4 *>(lv(buf) + (32 * d + col) * VP + 16 * chunk_of(col, 2 * x + half));
-                    o[d] = T::mfma32(f, pf[x], o[d]);
-                }
+            for (int k = 0; k < 4 * ND; k++) {
+                o[k % ND] = T::mfma32(vf[k % 8], pf[k / ND], o[k % ND]);
+                if (k + 8 < 4 * ND) vf[k % 8] = v_part(buf, (k + 8) / ND, (k + 8) % ND);
+            }
             // a NaN in V reaches the queries that see it, and no others
 #pragma unroll 1
             for (int e8 = 0; nans && e8 < 8; e8++) {
