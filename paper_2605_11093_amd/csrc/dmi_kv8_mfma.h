@@ -28,6 +28,10 @@ struct Bf16 {
         const f32x2 v = {a, b};
         return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
     }
+    static __device__ __forceinline__ uint32_t scaled(uint32_t w, float f)
+    {
+        return pack(__uint_as_float(w << 16) * f, __uint_as_float(w & 0xFFFF0000u) * f);
+    }
     static __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c)
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
@@ -51,6 +55,11 @@ struct Fp16 {
         const f32x2 v = {a, b};
         return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2));
     }
+    static __device__ __forceinline__ uint32_t scaled(uint32_t w, float f)
+    {
+        const f16x2 h = __builtin_bit_cast(f16x2, w);
+        return pack((float)h[0] * f, (float)h[1] * f);
+    }
     static __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c)
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
@@ -67,7 +76,10 @@ typedef __amdgpu_buffer_rsrc_t Buffer;
 constexpr int kOnce = 2;
 __device__ __forceinline__ Buffer buffer_at(const uint8_t *p)
 {
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p), 0, 0x7FFFFFFF, 0x00027000);
+    // (said to be the same in every lane: a load from what may differ becomes a loop over the lanes' addresses)
+    const uint64_t at = (uint64_t)p;
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)at), hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(at >> 32));
+    return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>((uint64_t)hi << 32 | lo), 0, 0x7FFFFFFF, 0x00027000);
 }
 template <int AUX> __device__ __forceinline__ u32x4 load_b128(Buffer b, uint32_t at)
 {
@@ -80,6 +92,15 @@ template <int AUX> __device__ __forceinline__ u32x2 load_b64(Buffer b, uint32_t 
 template <int AUX> __device__ __forceinline__ uint32_t load_b32(Buffer b, uint32_t at)
 {
     return __builtin_amdgcn_raw_buffer_load_b32(b, (int)at, 0, AUX);
+}
+
+// A barrier for what passes through LDS: __syncthreads() waits for loads from memory as well, also for those that a loop has
+// just started for its next round.
+__device__ __forceinline__ void lds_barrier()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }

@@ -31,24 +31,26 @@ __device__ __forceinline__ float lane_value(float v, int lane) { return __int_as
 // As in tokens_kernel, S^T = K Q^T and O^T = V^T P^T with query rows as columns, here with 32x32x16 instructions, 32 query rows a
 // wavefront, NW wavefronts on the same tokens.  K and V are converted once for the workgroup, on their way into LDS: K as it
 // lies, V transposed, the tokens of a sixteen in the order in which the lanes' registers of S^T hold them (0-3, 8-11 for lanes
-// 0-31, 4-7, 12-15 for lanes 32-63), so that an operand is 16 bytes in a row.  With two wavefronts on a SIMD one's exponentials
-// run beside the other's products.
+// 0-31, 4-7, 12-15 for lanes 32-63), so that an operand is 16 bytes in a row.
+//
 template <typename T, int DP, int NW>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW / 4)))
 void parts_kernel(AttendArgs a, PartsPlan p)
 {
     constexpr int KP = DP * 2 + 16, VP = kTile * 2;             // bytes of a row in LDS; K's are padded so that rows start on other banks
     constexpr int KK = DP / 16, ND = DP / 32;
+    constexpr int A = DP <= 128 ? 8 : 4;                        // operands read ahead
     constexpr int U = 8 / NW;                                   // eights of the tile's tokens that a wavefront stages
     constexpr int KL = DP <= 128 ? 1 : 2;                       // 16-byte loads of K a lane and eight
     constexpr int VL = DP <= 128 ? 1 : 2;                       // units of 4 tokens x 4 elements a lane and eight
     __shared__ __align__(16) uint8_t lds[2 * (kTile * KP + DP * VP)];
-    // NaNs in V: the last tile, counted from 1, that had one in an eight; a bit for each of 4 tokens
-    __shared__ int nan_tile[2][8], nan_any[2];
+    // NaNs in V: the last tile, counted from 1, that had one (in an eight); a bit for each of 4 tokens
+    __shared__ int nan_any[2], nan_tile[2][8];
     __shared__ __align__(4) uint8_t nan_bits[2][8][2][DP];
-    auto lk = [&](int buf) { return lds + buf * kTile * KP; };
-    auto lv = [&](int buf) { return lds + 2 * kTile * KP + buf * DP * VP; };
-
+    // scales of sixteens: K's, V's as a power of two and inverted, of 16 tiles and the next 16
+    __shared__ __align__(16) float scales[2][3][64];
+    auto lk = [&](int tile) { return lds + (tile & 1) * (kTile * KP); };
+    auto lv = [&](int tile) { return lds + 2 * kTile * KP + (tile & 1) * (DP * VP); };
     // V's 16-byte chunks are exchanged by row, so that neither the rows that lanes read nor those that they write (every fourth) meet
     // on a bank
     auto chunk_of = [](int row, int chunk) { return chunk ^ ((row >> 2 & 3) | ((row >> 1 ^ row >> 4) & 1) << 2); };
@@ -74,95 +76,131 @@ void parts_kernel(AttendArgs a, PartsPlan p)
     const int lim = row < rows ? older + w.token : -1;          // the last position that the column's query sees
     u32x4 qf[KK];
     {
-        const uint16_t *src = static_cast<const uint16_t *>(a.q.data) + (int64_t)(q.start + w.token) * a.q.row_stride + (int64_t)w.head * a.q.head_stride;
+        // (loads that depend on nothing: each in a branch of its own would wait for itself)
+        const QueryRow v = query_row(a, head, (uint32_t)min(row, rows - 1));
+        const uint16_t *src = static_cast<const uint16_t *>(a.q.data) + (int64_t)(q.start + v.token) * a.q.row_stride + (int64_t)v.head * a.q.head_stride;
 #pragma unroll
-        for (int k = 0; k < KK; k++) {
-            const int d = 16 * k + 8 * half;
-            qf[k] = u32x4{0u, 0u, 0u, 0u};
-            if (row < rows && d < (int)a.c.dim) {
-                qf[k] = *reinterpret_cast<const u32x4 *>(src + d);
-#pragma unroll
-                for (int i = 0; i < 4; i++) qf[k][i] ^= flip;
-            }
-        }
+        for (int k = 0; k < KK; k++) qf[k] = *reinterpret_cast<const u32x4 *>(src + (16 * k + 8 * half < (int)a.c.dim ? 16 * k + 8 * half : 0));
     }
     // what the first and the last of them see
     const int least = wave_row + 32 <= rows ? older + wave_row / (int)a.group : -1;
     const int most = wave_row < rows ? older + min(wave_row + 31, rows - 1) / (int)a.group : -1;
 
-    u32x4 rk[U][KL];
-    uint32_t rv[U][VL][4];
-    int there_v[U];
-    Look now{-1, 1.0f, -INFINITY, 0.0f}, next = now;            // of the 16 tiles that this one lies in, and the 16 behind them
-    auto fetch = [&](int tile, const Look &l) {
-#pragma unroll
-        for (int u = 0; u < U; u++) {
-            const int eight = wave + NW * u, t = begin + kTile * tile + 16 * (eight >> 1);
-            const int entry = __builtin_amdgcn_readlane(l.entry, (4 * tile + (eight >> 1)) & 63);
-            const int64_t at = (int64_t)max(entry, 0) * a.c.block_stride +
-                               (int64_t)((uint32_t)t - block_of(a.c, (uint32_t)t >> 4) * a.c.bs) * a.c.slot_stride + (int64_t)head * a.c.head_stride;
-            const Buffer k = buffer_at(a.c.code[0] + at), v = buffer_at(a.c.code[1] + at);
-            there_v[u] = entry < 0 ? 0 : min(16, end - t);
-#pragma unroll
-            for (int c = 0; c < KL; c++) {      // 8 lanes a token (4 if it has 64 elements)
-                const uint32_t d = DP == 64 ? 16u * (lane & 3) : 128u * c + 16u * (lane & 7), token = 8u * (eight & 1) + (DP == 64 ? (lane >> 2 & 7) : lane >> 3);
-                rk[u][c] = load_b128<0>(k, token * (uint32_t)a.c.slot_stride + (d < a.c.dim ? d : 0u));
-            }
-#pragma unroll
-            for (int c = 0; c < VL; c++) {
-                const int unit = lane + 64 * c, d = 4 * (unit % (DP / 4)), token = 4 * (eight & 1) + 8 * (unit / (DP / 4) & 1);
-#pragma unroll
-                for (int i = 0; i < 4; i++)
-                    rv[u][c][i] = load_b32<0>(v, (uint32_t)(token + i) * (uint32_t)a.c.slot_stride + (d < (int)a.c.dim ? (uint32_t)d : 0u));
-            }
-        }
+    // ---- staging
+    struct KCodes {
+        u32x4 w[U][KL];
     };
-    auto place = [&](int tile) {
-        uint8_t *const to_k = lk(tile & 1), *const to_v = lv(tile & 1);
+    struct VCodes {
+        uint32_t w[U][VL][4];
+        int there[U];                           // tokens of the sixteen
+    };
+    uint32_t k_off[KL], v_off[VL];              // this lane's offsets in a sixteen: 8 lanes a token of K (4 if it has 64 elements)
+#pragma unroll
+    for (int c = 0; c < KL; c++) {
+        const uint32_t d = DP == 64 ? 16u * (lane & 3) : 128u * c + 16u * (lane & 7);
+        k_off[c] = (DP == 64 ? (lane >> 2 & 7) : lane >> 3) * (uint32_t)a.c.slot_stride + (d < a.c.dim ? d : 0u);
+    }
+#pragma unroll
+    for (int c = 0; c < VL; c++) {
+        const uint32_t unit = lane + 64 * c, d = 4 * (unit % (DP / 4));
+        v_off[c] = 8u * (unit / (DP / 4) & 1u) * (uint32_t)a.c.slot_stride + (d < a.c.dim ? d : 0u);
+    }
+    // Where sixteens lie, from the first code on: a batch's 64, one a lane (the cache's first, if there is no entry)
+    struct Places {
+        uint32_t lo, hi;
+        uint64_t there;                         // which of them the cache has
+    };
+    // a batch of 16 tiles is looked up, and its scales go into LDS (every wavefront writes the same)
+    auto look = [&](int batch) {
+        const int t = begin + 1024 * batch + 16 * lane;
+        const Look l = look_up(a, q, head, t, end, scale);
+        scales[batch & 1][0][lane] = l.ks;
+        scales[batch & 1][1][lane] = l.lift;
+        scales[batch & 1][2][lane] = l.inv;
+        const int64_t at = (int64_t)max(l.entry, 0) * a.c.block_stride +
+                           (int64_t)((uint32_t)t - block_of(a.c, (uint32_t)t >> 4) * a.c.bs) * a.c.slot_stride + (int64_t)head * a.c.head_stride;
+        return Places{(uint32_t)at, (uint32_t)(at >> 32), __ballot(l.entry >= 0)};
+    };
+    auto fetch = [&](int tile, const Places &p, KCodes &k, VCodes &v) {
 #pragma unroll
         for (int u = 0; u < U; u++) {
-            const int eight = wave + NW * u;
+            const int eight = wave + NW * u, six = (4 * tile + (eight >> 1)) & 63;
+            const uint64_t at = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)p.hi, six) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)p.lo, six);
+            const Buffer bk = buffer_at(a.c.code[0] + at), bv = buffer_at(a.c.code[1] + at);
+            v.there[u] = p.there >> six & 1u ? min(16, end - begin - kTile * tile - 16 * (eight >> 1)) : 0;
 #pragma unroll
-            for (int c = 0; c < KL; c++) {
-                const int d = DP == 64 ? 16 * (lane & 3) : 128 * c + 16 * (lane & 7), token = 8 * eight + (DP == 64 ? lane >> 2 : lane >> 3);
-                const u32x4 r = rk[u][c];
-                if (DP > 64 || lane < 32) {
-                    *reinterpret_cast<u32x4 *>(to_k + token * KP + 2 * d) = u32x4{T::two_codes(r[0], false), T::two_codes(r[0], true), T::two_codes(r[1], false), T::two_codes(r[1], true)};
-                    *reinterpret_cast<u32x4 *>(to_k + token * KP + 2 * d + 16) = u32x4{T::two_codes(r[2], false), T::two_codes(r[2], true), T::two_codes(r[3], false), T::two_codes(r[3], true)};
-                }
-            }
-            uint32_t any = 0;
+            for (int c = 0; c < KL; c++) k.w[u][c] = load_b128<0>(bk, k_off[c] + ((eight & 1) ? 8u * (uint32_t)a.c.slot_stride : 0u));
 #pragma unroll
             for (int c = 0; c < VL; c++)
 #pragma unroll
-                for (int i = 0; i < 4; i++) {
-                    rv[u][c][i] = 4 * (eight & 1) + 8 * ((lane + 64 * c) / (DP / 4) & 1) + i < there_v[u] ? rv[u][c][i] : 0u;
-                    any |= nan_codes(rv[u][c][i]);
+                for (int i = 0; i < 4; i++)
+                    v.w[u][c][i] = load_b32<0>(bv, v_off[c] + ((eight & 1) ? 4u * (uint32_t)a.c.slot_stride : 0u) + (uint32_t)i * (uint32_t)a.c.slot_stride);
+        }
+    };
+    auto place_k = [&](const KCodes &r, int tile) {
+#pragma unroll
+        for (int u = 0; u < U; u++)
+#pragma unroll
+            for (int c = 0; c < KL; c++) {
+                const int d = DP == 64 ? 16 * (lane & 3) : 128 * c + 16 * (lane & 7), token = 8 * (wave + NW * u) + (DP == 64 ? lane >> 2 : lane >> 3);
+                uint8_t *const to = lk(tile) + token * KP + 2 * d;
+                const u32x4 k = r.w[u][c];
+                if (DP > 64 || lane < 32) {
+                    *reinterpret_cast<u32x4 *>(to) = u32x4{T::two_codes(k[0], false), T::two_codes(k[0], true), T::two_codes(k[1], false), T::two_codes(k[1], true)};
+                    *reinterpret_cast<u32x4 *>(to + 16) = u32x4{T::two_codes(k[2], false), T::two_codes(k[2], true), T::two_codes(k[3], false), T::two_codes(k[3], true)};
                 }
-            if (__ballot(any != 0)) {           // 0 takes a NaN's place, and the queries that see it are given it apart
-                if (lane == 0) nan_tile[tile & 1][eight] = nan_any[tile & 1] = tile + 1;
+            }
+    };
+    // V's codes as they come: nothing where there is no token, and 0 in a NaN's place (the queries that see it are given it apart)
+    auto clean_v = [&](VCodes &r, int tile) {
+        const int buf = tile & 1;
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const int eight = wave + NW * u;
+            uint32_t any = 0;
+            if (r.there[u] < 16) {
+                asm volatile("");               // (a branch that most tiles skip)
+#pragma unroll
+                for (int c = 0; c < VL; c++)
+#pragma unroll
+                    for (int i = 0; i < 4; i++)
+                        r.w[u][c][i] = 4 * (eight & 1) + 8 * ((lane + 64 * c) / (DP / 4) & 1) + i < r.there[u] ? r.w[u][c][i] : 0u;
+            }
+#pragma unroll
+            for (int c = 0; c < VL; c++)
+#pragma unroll
+                for (int i = 0; i < 4; i++) any |= nan_codes(r.w[u][c][i]);
+            if (__ballot(any != 0)) {
+                if (lane == 0) nan_any[buf] = nan_tile[buf][eight] = tile + 1;
 #pragma unroll
                 for (int c = 0; c < VL; c++) {
                     const int unit = lane + 64 * c, d = 4 * (unit % (DP / 4));
                     uint32_t bits = 0;
 #pragma unroll
                     for (int i = 0; i < 4; i++) {
-                        const uint32_t top = nan_codes(rv[u][c][i]);
+                        const uint32_t top = nan_codes(r.w[u][c][i]);
                         bits |= top >> (7 - i);
-                        rv[u][c][i] &= ~(top | (top - (top >> 7)));
+                        r.w[u][c][i] &= ~(top | (top - (top >> 7)));
                     }
-                    if (DP > 64 || lane < 32) *reinterpret_cast<uint32_t *>(&nan_bits[tile & 1][eight][unit / (DP / 4) & 1][d]) = bits;
+                    if (DP > 64 || lane < 32) *reinterpret_cast<uint32_t *>(&nan_bits[buf][eight][unit / (DP / 4) & 1][d]) = bits;
                 }
             }
+        }
+    };
+    auto place_v = [&](const VCodes &r, int tile) {
+        uint8_t *const to_v = lv(tile);
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const int eight = wave + NW * u;
 #pragma unroll
             for (int c = 0; c < VL; c++) {
                 const int unit = lane + 64 * c, d = 4 * (unit % (DP / 4)), quad = unit / (DP / 4) & 1;
-                const uint32_t *r = rv[u][c];
+                const uint32_t *v = r.w[u][c];
                 u32x2 e[4];
 #pragma unroll
                 for (int i = 0; i < 2; i++) {
-                    const uint32_t lo = __builtin_amdgcn_perm(r[2 * i + 1], r[2 * i], 0x05010400u);
-                    const uint32_t hi = __builtin_amdgcn_perm(r[2 * i + 1], r[2 * i], 0x07030602u);
+                    const uint32_t lo = __builtin_amdgcn_perm(v[2 * i + 1], v[2 * i], 0x05010400u);
+                    const uint32_t hi = __builtin_amdgcn_perm(v[2 * i + 1], v[2 * i], 0x07030602u);
                     e[0][i] = T::two_codes(lo, false), e[1][i] = T::two_codes(lo, true);
                     e[2][i] = T::two_codes(hi, false), e[3][i] = T::two_codes(hi, true);
                 }
@@ -174,152 +212,155 @@ void parts_kernel(AttendArgs a, PartsPlan p)
         }
     };
 
-    auto v_part = [&](int buf, int x, int d) {  // elements 32d.. of a sixteen's V
-        return *reinterpret_cast<const u32x4 *>(lv(buf) + (32 * d + col) * VP + 16 * chunk_of(col, 2 * x + half));
+    // ---- operands out of LDS: two 32s' scores in turn (neither waits for itself); elements 32d.. of a sixteen's V
+    auto k_part = [&](int tile, int i) { return *reinterpret_cast<const u32x4 *>(lk(tile) + (32 * (i % 2) + col) * KP + 32 * (i / 2) + 16 * half); };
+    auto v_part = [&](int tile, int i) {
+        return *reinterpret_cast<const u32x4 *>(lv(tile) + (32 * (i % ND) + col) * VP + 16 * chunk_of(col, 2 * (i / ND) + half));
     };
+
     float m = -INFINITY, base = 0.0f, l = 0.0f, lift_ref = T::kNarrow ? -INFINITY : 0.0f;
     f32x16 o[ND];
 #pragma unroll
     for (int d = 0; d < ND; d++)
 #pragma unroll
         for (int i = 0; i < 16; i++) o[d][i] = 0.0f;
-
-    if (threadIdx.x < 16) nan_tile[threadIdx.x >> 3][threadIdx.x & 7] = nan_any[threadIdx.x & 1] = 0;
-    if (tiles) {
-        now = look_up(a, q, head, begin + 16 * lane, end, scale);
-        fetch(0, now);
-    }
-    __syncthreads();                            // (the NaN flags are cleared)
-    if (tiles) place(0);
-    for (int tile = 0; tile < tiles; tile++) {
-        const int buf = tile & 1, t0 = begin + kTile * tile;
-        if (tile && (tile & 15) == 0) now = next;
-        if (tile + 1 < tiles) {
-            if (((tile + 1) & 15) == 0) {
-                next = look_up(a, q, head, begin + kTile * (tile + 1) + 16 * lane, end, scale);
-                fetch(tile + 1, next);
-            } else {
-                fetch(tile + 1, now);
-            }
-        }
-        __syncthreads();                        // this tile is in LDS
-        if (t0 <= most) {
-            const bool nans = nan_any[buf] == tile + 1;
-            // Operands are read from LDS eight ahead of the instructions that take them, V's first ones while K's last are used
-            // (left to itself the compiler reads one or two ahead, and every instruction waits for most of a trip to LDS).
-            f32x16 z[2];
-            u32x4 kf[8], vf[8];
-            auto k_part = [&](int i) { return *reinterpret_cast<const u32x4 *>(lk(buf) + (32 * (i / KK) + col) * KP + 32 * (i % KK) + 16 * half); };
+    // a NaN in V reaches the queries that see it, and no others
+    auto give_nans = [&](int tile) {
+#pragma unroll 1
+        for (int e8 = 0; e8 < 8; e8++) {
+            if (nan_tile[tile & 1][e8] != tile + 1) continue;
+            uint32_t sees[2] = {0u, 0u};
 #pragma unroll
-            for (int i = 0; i < 8; i++) kf[i] = k_part(i);
+            for (int i = 0; i < 8; i++)
+                if (begin + kTile * tile + 16 * (e8 >> 1) + 4 * (e8 & 1) + (i & 3) + 8 * (i >> 2) <= lim) sees[i >> 2] |= 0x01010101u << (i & 3);
 #pragma unroll
-            for (int sub = 0; sub < 2; sub++)
+            for (int d = 0; d < ND; d++)
 #pragma unroll
-                for (int i = 0; i < 16; i++) z[sub][i] = 0.0f;
+                for (int y = 0; y < 4; y++) {
+                    const int e = 32 * d + 8 * y + 4 * half;
+                    const uint32_t bits = (*reinterpret_cast<const uint32_t *>(&nan_bits[tile & 1][e8][0][e]) & sees[0]) |
+                                          (*reinterpret_cast<const uint32_t *>(&nan_bits[tile & 1][e8][1][e]) & sees[1]);
 #pragma unroll
-            for (int i = 0; i < 2 * KK; i++) {
-                z[i / KK] = T::mfma32(kf[i % 8], qf[i % KK], z[i / KK]);
-                if (i + 8 < 2 * KK) kf[i % 8] = k_part(i + 8);
-                else vf[i + 8 - 2 * KK] = v_part(buf, (i + 8 - 2 * KK) / ND, (i + 8 - 2 * KK) % ND);
-            }
-            __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
-#pragma unroll
-            for (int i = 0; i < 2 * KK; i++) {
-                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-            }
-            float ks[4], lift[4], inv[4];
-            bool there = true;
-#pragma unroll
-            for (int x = 0; x < 4; x++) {
-                const int six = (4 * tile + x) & 63;
-                ks[x] = lane_value(now.ks, six);
-                lift[x] = lane_value(now.lift, six);
-                inv[x] = lane_value(now.inv, six);
-                there = there && __builtin_amdgcn_readlane(now.entry, six) >= 0;
-            }
-            if (!there || t0 + kTile - 1 > least) {
-#pragma unroll
-                for (int sub = 0; sub < 2; sub++)
-#pragma unroll
-                    for (int i = 0; i < 16; i++) {
-                        const int at = t0 + 32 * sub + 8 * (i >> 2) + 4 * half + (i & 3);
-                        const bool is = __builtin_amdgcn_readlane(now.entry, (4 * tile + 2 * sub + (i >> 3)) & 63) >= 0;
-                        z[sub][i] = is && at <= lim ? z[sub][i] : -INFINITY;
-                    }
-            }
-            float top = -INFINITY;
-#pragma unroll
-            for (int x = 0; x < 4; x++) {
-                const f32x16 &s = z[x >> 1];
-                const int i = 8 * (x & 1);
-                top = fmaxf(top, fmaxf(fmaxf(fmaxf(s[i], s[i + 1]), fmaxf(s[i + 2], s[i + 3])), fmaxf(fmaxf(s[i + 4], s[i + 5]), fmaxf(s[i + 6], s[i + 7]))) * ks[x]);
-            }
-            if (__ballot(top > m + kSlack)) {   // the sums against a higher maximum
-                const float to = fmaxf(m, fmaxf(top, __shfl_xor(top, 32)));
-                const float f = to == -INFINITY ? 1.0f : exp2_of(m - to);
-                m = to;
-                base = to == -INFINITY ? 0.0f : to;
-                l *= f;
-#pragma unroll
-                for (int d = 0; d < ND; d++) o[d] *= f;
-            }
-            if constexpr (T::kNarrow) {         // V's scale relative to the largest yet, to stay within fp16's range
-                const float largest = fmaxf(fmaxf(lift[0], lift[1]), fmaxf(lift[2], lift[3]));
-                if (largest > lift_ref) {
-                    const float f = exp2_of(lift_ref - largest);
-#pragma unroll
-                    for (int d = 0; d < ND; d++) o[d] *= f;
-                    lift_ref = largest;
+                    for (int i = 0; i < 4; i++) o[d][4 * y + i] += bits >> (8 * i) & 0xFFu ? NAN : 0.0f;
                 }
-                const float ref = exp2_of(lift_ref);
+        }
+    };
+    if (tiles) {
+        if (threadIdx.x < 16) nan_tile[threadIdx.x >> 3][threadIdx.x & 7] = nan_any[threadIdx.x & 1] = 0;
+        Places now = look(0), next = now;
+        KCodes kc;
+        VCodes vc;
+        fetch(0, now, kc, vc);
+        lds_barrier();                          // (the NaN flags are cleared)
+#pragma unroll
+        for (int k = 0; k < KK; k++)
+#pragma unroll
+            for (int i = 0; i < 4; i++) qf[k][i] = 16 * k + 8 * half < (int)a.c.dim ? qf[k][i] ^ flip : 0u;
+        clean_v(vc, 0);
+        place_v(vc, 0);
+        place_k(kc, 0);
+#pragma unroll 1
+        for (int tile = 0; tile < tiles; tile++) {
+            const int t0 = begin + kTile * tile;
+            if ((tile & 15) == 0 && tile) now = next;
+            if (((tile + 1) & 15) == 0) next = look((tile + 1) >> 4);
+            fetch(tile + 1, ((tile + 1) & 15) == 0 ? next : now, kc, vc);
+            lds_barrier();                      // the tile is in LDS
+            if (t0 <= most) {
+                const bool nans = nan_any[tile & 1] == tile + 1;
+                // Operands are read from LDS well ahead of the instructions that take them, V's first ones while K's last are
+                // used (left to itself the compiler reads one or two ahead, and every instruction waits for most of a trip to LDS).
+                f32x16 z[2];
+                u32x4 kf[A], vf[A];
+#pragma unroll
+                for (int i = 0; i < A; i++) kf[i] = k_part(tile, i);
+#pragma unroll
+                for (int s = 0; s < 2; s++)
+#pragma unroll
+                    for (int i = 0; i < 16; i++) z[s][i] = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 2 * KK; i++) {
+                    z[i % 2] = T::mfma32(kf[i % A], qf[i / 2], z[i % 2]);
+                    if (i + A < 2 * KK) kf[i % A] = k_part(tile, i + A);
+                    else vf[i + A - 2 * KK] = v_part(tile, i + A - 2 * KK);
+                }
+                f32x4 ks = *reinterpret_cast<const f32x4 *>(&scales[tile >> 4 & 1][0][4 * (tile & 15)]);
+                f32x4 lift = *reinterpret_cast<const f32x4 *>(&scales[tile >> 4 & 1][1][4 * (tile & 15)]);
+                f32x4 inv = *reinterpret_cast<const f32x4 *>(&scales[tile >> 4 & 1][2][4 * (tile & 15)]);
+                __builtin_amdgcn_sched_group_barrier(0x100, A, 0);
+#pragma unroll
+                for (int i = 0; i < 2 * KK; i++) {
+                    __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                }
+                const uint32_t there = (uint32_t)(now.there >> (4 * (tile & 15))) & 15u;
+                if (there != 15u || t0 + kTile - 1 > least) {
+                    asm volatile("");           // (a branch that most tiles skip, not selects in all of them)
+#pragma unroll
+                    for (int s = 0; s < 2; s++)
+#pragma unroll
+                        for (int i = 0; i < 16; i++)
+                            z[s][i] = (there >> (2 * s + (i >> 3)) & 1u) && t0 + 32 * s + 8 * (i >> 2) + 4 * half + (i & 3) <= lim ? z[s][i] : -INFINITY;
+                }
+                // (the middle of three with +inf is the larger of two, and takes products' results without a step to quiet NaNs first)
+                float top = -INFINITY;
 #pragma unroll
                 for (int x = 0; x < 4; x++) {
-                    lift[x] = lift_ref == -INFINITY ? lift[x] : lift[x] - lift_ref;
-                    inv[x] *= ref;
+                    float t = -INFINITY;
+#pragma unroll
+                    for (int i = 0; i < 8; i++) t = __builtin_amdgcn_fmed3f(t, z[x >> 1][8 * (x & 1) + i], INFINITY);
+                    top = fmaxf(top, t * ks[x]);
                 }
-            }
-            // p, times V's scale (in the exponent; what is summed is divided by it again)
-            u32x4 pf[4];
+                if (__ballot(top > m + kSlack)) {       // the sums against a higher maximum
+                    const float to = fmaxf(m, fmaxf(top, __shfl_xor(top, 32)));
+                    const float f = to == -INFINITY ? 1.0f : exp2_of(m - to);
+                    m = to;
+                    base = to == -INFINITY ? 0.0f : to;
+                    l *= f;
 #pragma unroll
-            for (int x = 0; x < 4; x++) {
-                const float off = lift[x] - base;
-                float e[8], sum = 0.0f;
-#pragma unroll
-                for (int i = 0; i < 8; i++) {
-                    e[i] = exp2_of(__builtin_fmaf(z[x >> 1][8 * (x & 1) + i], ks[x], off));
-                    sum += e[i];
+                    for (int d = 0; d < ND; d++) o[d] *= f;
                 }
-                l = __builtin_fmaf(sum, inv[x], l);
+                if constexpr (T::kNarrow) {     // V's scale relative to the largest yet, to stay within fp16's range
+                    const float largest = fmaxf(fmaxf(lift[0], lift[1]), fmaxf(lift[2], lift[3]));
+                    if (__ballot(largest > lift_ref)) {
+                        const float f = exp2_of(lift_ref - largest);
 #pragma unroll
-                for (int i = 0; i < 4; i++) pf[x][i] = T::pack(e[2 * i], e[2 * i + 1]);
-            }
-#pragma unroll
-            for (int k = 0; k < 4 * ND; k++) {
-                o[k % ND] = T::mfma32(vf[k % 8], pf[k / ND], o[k % ND]);
-                if (k + 8 < 4 * ND) vf[k % 8] = v_part(buf, (k + 8) / ND, (k + 8) % ND);
-            }
-            // a NaN in V reaches the queries that see it, and no others
-#pragma unroll 1
-            for (int e8 = 0; nans && e8 < 8; e8++) {
-                if (nan_tile[buf][e8] != tile + 1) continue;
-                uint32_t sees[2] = {0u, 0u};
-#pragma unroll
-                for (int i = 0; i < 8; i++)
-                    if (t0 + 16 * (e8 >> 1) + 4 * (e8 & 1) + (i & 3) + 8 * (i >> 2) <= lim) sees[i >> 2] |= 0x01010101u << (i & 3);
-#pragma unroll
-                for (int d = 0; d < ND; d++)
-#pragma unroll
-                    for (int y = 0; y < 4; y++) {
-                        const int e = 32 * d + 8 * y + 4 * half;
-                        const uint32_t bits = (*reinterpret_cast<const uint32_t *>(&nan_bits[buf][e8][0][e]) & sees[0]) |
-                                              (*reinterpret_cast<const uint32_t *>(&nan_bits[buf][e8][1][e]) & sees[1]);
-#pragma unroll
-                        for (int i = 0; i < 4; i++) o[d][4 * y + i] += bits >> (8 * i) & 0xFFu ? NAN : 0.0f;
+                        for (int d = 0; d < ND; d++) o[d] *= f;
+                        lift_ref = largest;
                     }
+                    const float ref = exp2_of(lift_ref);
+#pragma unroll
+                    for (int x = 0; x < 4; x++) {
+                        lift[x] = lift_ref == -INFINITY ? lift[x] : lift[x] - lift_ref;
+                        inv[x] *= ref;
+                    }
+                }
+                // p, times V's scale (in the exponent; what is summed is divided by it again)
+                u32x4 pf[4];
+#pragma unroll
+                for (int x = 0; x < 4; x++) {
+                    const float off = lift[x] - base;
+                    float e[8], sum[2] = {0.0f, 0.0f};
+#pragma unroll
+                    for (int i = 0; i < 8; i++) {
+                        e[i] = exp2_of(__builtin_fmaf(z[x >> 1][8 * (x & 1) + i], ks[x], off));
+                        sum[i & 1] += e[i];
+                    }
+                    l = __builtin_fmaf(sum[0] + sum[1], inv[x], l);
+#pragma unroll
+                    for (int i = 0; i < 4; i++) pf[x][i] = T::pack(e[2 * i], e[2 * i + 1]);
+                }
+#pragma unroll
+                for (int i = 0; i < 4 * ND; i++) {
+                    o[i % ND] = T::mfma32(vf[i % A], pf[i / ND], o[i % ND]);
+                    if (i + A < 4 * ND) vf[i % A] = v_part(tile, i + A);
+                }
+                if (nans) give_nans(tile);
             }
+            clean_v(vc, tile + 1);
+            place_v(vc, tile + 1);
+            place_k(kc, tile + 1);
         }
-        if (tile + 1 < tiles) place(tile + 1);
     }
 
     const float v_ref = T::kNarrow ? exp2_of(lift_ref) : 1.0f;
@@ -469,7 +510,7 @@ __global__ __launch_bounds__(256) void weights_kernel(AttendArgs a, PartsPlan p)
     for (int tile = 0; tile < tiles; tile++) {
         const int buf = tile & 1;
         if (tile + 1 < tiles) fetch(tile + 1);
-        __syncthreads();
+        lds_barrier();
         f32x16 z[2];
 #pragma unroll
         for (int s = 0; s < 2; s++)
