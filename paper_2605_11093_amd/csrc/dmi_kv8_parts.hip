@@ -397,58 +397,90 @@ void parts_kernel(AttendArgs a, PartsPlan p)
     }
 }
 
-// Outputs out of the parts that splits of the contexts left, a wavefront a row.
+// Outputs out of the parts that splits of the contexts left: a row by as many lanes as take four elements each of it.
 template <typename T>
 __global__ __launch_bounds__(256) void join_parts_kernel(AttendArgs a, PartsPlan p, uint32_t tile_rows)
 {
-    const int lane = threadIdx.x & 63;
     const Request q = request_of(a.b, a.c, (int)blockIdx.y);
-    const uint32_t n = blockIdx.x * 4u + (threadIdx.x >> 6), rows = (uint32_t)q.fresh * a.group;
-    if (n >= rows * a.c.heads) return;
-    const uint32_t head = n / rows, row = n - head * rows;
+    const uint32_t wide = a.c.dim / 4u, n = blockIdx.x * (256u / wide) + threadIdx.x / wide, rows = (uint32_t)q.fresh * a.group;
+    if (threadIdx.x >= 256u / wide * wide || n >= rows * a.c.heads) return;
+    const uint32_t head = n / rows, row = n - head * rows, lane = threadIdx.x % wide;
     const QueryRow w = query_row(a, head, row);
     const int64_t at = (int64_t)(q.start + w.token) * a.q_heads + w.head;
     // splits that the row's workgroup had work in
     const uint32_t last_row = min((row / tile_rows + 1u) * tile_rows, rows) - 1u;
     const int seen = q.len - q.fresh + (int)(last_row / a.group) + 1, splits = max(1, (seen + (int)p.chunk - 1) / (int)p.chunk);
     const f32x2 *sums = p.sums + at * p.splits;
-    float top = -INFINITY, sum = 0.0f;
-    for (int s = 0; s < splits; s++) top = fmaxf(top, sums[s][0]);
-    const float to = top == -INFINITY ? 0.0f : top;
-    for (int s = 0; s < splits; s++) sum += sums[s][1] * exp2_of(sums[s][0] - to);
-    const float total = top == -INFINITY && sum == 0.0f ? -INFINITY : to + log2_of(sum);
-    const int d = 4 * lane;
-    if (d < (int)a.c.dim) {
-        f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-        for (int s = 0; s < splits; s++) {
-            const float f = total == -INFINITY ? 0.0f : exp2_of(sums[s][0] - total);
-            o += *reinterpret_cast<const f32x4 *>(p.parts + (at * p.splits + s) * a.c.dim + d) * f;
-        }
-        uint16_t *dst = static_cast<uint16_t *>(a.out.data) + (int64_t)(q.start + w.token) * a.out.row_stride + (int64_t)w.head * a.out.head_stride + d;
-        *reinterpret_cast<u32x2 *>(dst) = u32x2{T::pack(o[0], o[1]), T::pack(o[2], o[3])};
+    const float *parts = p.parts + at * p.splits * a.c.dim + 4u * lane;
+    float m = -INFINITY, l = 0.0f;
+    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+    for (int s = 0; s < splits; s++) {
+        const f32x2 x = sums[s];
+        const f32x4 part = *reinterpret_cast<const f32x4 *>(parts + (int64_t)s * a.c.dim);
+        const float top = fmaxf(m, x[0]), to = top == -INFINITY ? 0.0f : top, f = exp2_of(m - to), g = exp2_of(x[0] - to);
+        l = l * f + x[1] * g;
+        o = o * f + part * g;
+        m = top;
     }
+    const bool empty = m == -INFINITY && l == 0.0f;
+    o *= empty ? 0.0f : 1.0f / l;
+    uint16_t *dst = static_cast<uint16_t *>(a.out.data) + (int64_t)(q.start + w.token) * a.out.row_stride + (int64_t)w.head * a.out.head_stride + 4u * lane;
+    *reinterpret_cast<u32x2 *>(dst) = u32x2{T::pack(o[0], o[1]), T::pack(o[2], o[3])};
     if (!lane) {
+        const float total = empty ? -INFINITY : m + log2_of(l);
         if (a.lse) a.lse[at] = total * kLn2;
         if (p.totals) p.totals[at] = total;
     }
 }
 
-// Weights: 256 tokens a workgroup, 64 a wavefront, whose K stays in registers; the query rows that see them pass through LDS 32 at
-// a time.  Scores once more (their rows' totals were not known before), p summed over the rows in fp32, in order.
+// Weights: 256 tokens a workgroup, 64 a wavefront, whose K stays in registers; the query rows that see them pass through LDS 64 at
+// a time (32 of 256 elements).  Scores once more (their rows' totals were not known before), p summed over the rows in fp32, in order.
 template <typename T, int DP>
-__global__ __launch_bounds__(256) void weights_kernel(AttendArgs a, PartsPlan p)
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ? 2 : 1))) void weights_kernel(AttendArgs a, PartsPlan p)
 {
-    constexpr int QP = DP * 2 + 16, KK = DP / 16;
-    __shared__ __align__(16) uint8_t lq[2][32 * QP];
-    __shared__ float lt[2][32];
-    __shared__ int ll[2][32];
+    constexpr int QP = DP * 2 + 16, KK = DP / 16, QT = DP <= 128 ? 64 : 32;
+    constexpr int TR = 256 / QT, QL = DP / (8 * TR);            // threads a query row, loads of 8 elements each of them
+    __shared__ __align__(16) uint8_t lq[2][QT * QP];
+    __shared__ float lt[2][QT];
+    __shared__ int ll[2][QT];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
     const uint32_t head = blockIdx.x % a.c.heads;
     const Request q = request_of(a.b, a.c, (int)blockIdx.y);
     const int block0 = (int)(blockIdx.x / a.c.heads) * 256, t0 = block0 + 64 * wave;
     if (block0 >= q.len) return;
     const int older = q.len - q.fresh, rows = q.fresh * (int)a.group;
-    const int first_row = max(0, block0 - older) * (int)a.group, tiles = (rows - first_row + 31) / 32;
+    const int first_row = max(0, block0 - older) * (int)a.group, tiles = (rows - first_row + QT - 1) / QT;
+
+    u32x4 rq[QL];
+    float rt = -INFINITY;
+    int rl = -1;
+    auto fetch = [&](int tile) {
+        const int row = first_row + QT * tile + (int)(threadIdx.x / TR);
+        const QueryRow w = query_row(a, head, (uint32_t)min(row, rows - 1));
+        const uint16_t *src = static_cast<const uint16_t *>(a.q.data) + (int64_t)(q.start + w.token) * a.q.row_stride + (int64_t)w.head * a.q.head_stride;
+#pragma unroll
+        for (int c = 0; c < QL; c++) {
+            const int d = 8 * TR * c + 8 * (int)(threadIdx.x % TR);
+            rq[c] = *reinterpret_cast<const u32x4 *>(src + (d < (int)a.c.dim ? d : 0));
+        }
+        rt = p.totals[(int64_t)(q.start + w.token) * a.q_heads + w.head];
+        rl = row < rows ? older + w.token : -1;
+    };
+    auto place = [&](int buf) {
+#pragma unroll
+        for (int c = 0; c < QL; c++) {
+            const int d = 8 * TR * c + 8 * (int)(threadIdx.x % TR);
+#pragma unroll
+            for (int i = 0; i < 4; i++) rq[c][i] = d < (int)a.c.dim ? rq[c][i] : 0u;
+            *reinterpret_cast<u32x4 *>(lq[buf] + (threadIdx.x / TR) * QP + 2 * d) = rq[c];
+        }
+        if ((threadIdx.x % TR) == 0) {
+            lt[buf][threadIdx.x / TR] = rt;
+            ll[buf][threadIdx.x / TR] = rt == -INFINITY ? -1 : rl;     // (a row that saw nothing weighs nothing)
+        }
+    };
+    if (tiles > 0) fetch(0);
 
     // K of the wavefront's tokens: two 32s, their sixteens' scales
     const Look l = look_up(a, q, head, t0 + 16 * lane, lane < 4 ? q.len : 0, a.scale_log2);
@@ -462,76 +494,60 @@ __global__ __launch_bounds__(256) void weights_kernel(AttendArgs a, PartsPlan p)
         const int e = col < 16 ? e0 : e1;
         const uint32_t b = block_of(a.c, (uint32_t)t >> 4);
         const uint8_t *k = code_at(a.c, 0, max(e, 0), (uint32_t)t - b * a.c.bs, head);
+        u32x2 w[KK];
 #pragma unroll
-        for (int i = 0; i < KK; i++) {
-            const int d = 16 * i + 8 * half;
-            u32x2 w = {0u, 0u};
-            if (d < (int)a.c.dim) w = *reinterpret_cast<const u32x2 *>(k + d);
-            kf[s][i] = u32x4{T::two_codes(w[0], false), T::two_codes(w[0], true), T::two_codes(w[1], false), T::two_codes(w[1], true)};
-        }
+        for (int i = 0; i < KK; i++) w[i] = *reinterpret_cast<const u32x2 *>(k + (16 * i + 8 * half < (int)a.c.dim ? 16 * i + 8 * half : 0));
+#pragma unroll
+        for (int i = 0; i < KK; i++) kf[s][i] = u32x4{T::two_codes(w[i][0], false), T::two_codes(w[i][0], true), T::two_codes(w[i][1], false), T::two_codes(w[i][1], true)};
     }
 
-    // 8 threads a query row
-    u32x4 rq[DP / 64];
-    float rt = -INFINITY;
-    int rl = -1;
-    auto fetch = [&](int tile) {
-        const int row = first_row + 32 * tile + (int)(threadIdx.x >> 3);
-        rt = -INFINITY, rl = -1;
-#pragma unroll
-        for (int c = 0; c < DP / 64; c++) rq[c] = u32x4{0u, 0u, 0u, 0u};
-        if (row < rows) {
-            const QueryRow w = query_row(a, head, (uint32_t)row);
-            const uint16_t *src = static_cast<const uint16_t *>(a.q.data) + (int64_t)(q.start + w.token) * a.q.row_stride + (int64_t)w.head * a.q.head_stride;
-#pragma unroll
-            for (int c = 0; c < DP / 64; c++) {
-                const int d = 64 * c + 8 * (int)(threadIdx.x & 7);
-                if (d < (int)a.c.dim) rq[c] = *reinterpret_cast<const u32x4 *>(src + d);
-            }
-            rt = p.totals[(int64_t)(q.start + w.token) * a.q_heads + w.head];
-            rl = rt == -INFINITY ? -1 : older + w.token;
-        }
-    };
-    auto place = [&](int buf) {
-#pragma unroll
-        for (int c = 0; c < DP / 64; c++)
-            *reinterpret_cast<u32x4 *>(lq[buf] + (threadIdx.x >> 3) * QP + 2 * (64 * c + 8 * (threadIdx.x & 7))) = rq[c];
-        if ((threadIdx.x & 7) == 0) lt[buf][threadIdx.x >> 3] = rt, ll[buf][threadIdx.x >> 3] = rl;
-    };
     float w[2][16];
 #pragma unroll
     for (int s = 0; s < 2; s++)
 #pragma unroll
         for (int i = 0; i < 16; i++) w[s][i] = 0.0f;
-    if (tiles > 0) {
-        fetch(0);
-        place(0);
-    }
+    if (tiles > 0) place(0);
+#pragma unroll 1
     for (int tile = 0; tile < tiles; tile++) {
         const int buf = tile & 1;
         if (tile + 1 < tiles) fetch(tile + 1);
         lds_barrier();
-        f32x16 z[2];
+#pragma unroll 1
+        for (int h = 0; h < QT / 32; h++) {
+            constexpr int A = DP <= 128 ? (KK < 8 ? KK : 8) : 4;      // operands read ahead
+            const uint8_t *const from = lq[buf] + (32 * h + col) * QP + 16 * half;
+            u32x4 f[A];
 #pragma unroll
-        for (int s = 0; s < 2; s++)
+            for (int k = 0; k < A; k++) f[k] = *reinterpret_cast<const u32x4 *>(from + 32 * k);
+            const float total = lt[buf][32 * h + col];
+            const int lim = ll[buf][32 * h + col];
+            f32x16 z[2];
 #pragma unroll
-            for (int i = 0; i < 16; i++) z[s][i] = 0.0f;
+            for (int s = 0; s < 2; s++)
 #pragma unroll
-        for (int k = 0; k < KK; k++) {
-            const u32x4 f = *reinterpret_cast<const u32x4 *>(lq[buf] + col * QP + 32 * k + 16 * half);
+                for (int i = 0; i < 16; i++) z[s][i] = 0.0f;
 #pragma unroll
-            for (int s = 0; s < 2; s++) z[s] = T::mfma32(kf[s][k], f, z[s]);
-        }
-        const float total = lt[buf][col];
-        const int lim = ll[buf][col];
-        const bool full = __ballot(lim < t0 + 63) == 0;
+            for (int k = 0; k < KK; k++) {
 #pragma unroll
-        for (int s = 0; s < 2; s++)
-#pragma unroll
-            for (int i = 0; i < 16; i++) {
-                const float e = exp2_of(z[s][i] * ks[2 * s + (i >> 3)] - total);
-                w[s][i] += full || t0 + 32 * s + 8 * (i >> 2) + 4 * half + (i & 3) <= lim ? e : 0.0f;
+                for (int s = 0; s < 2; s++) z[s] = T::mfma32(kf[s][k], f[k % A], z[s]);
+                if (k + A < KK) f[k % A] = *reinterpret_cast<const u32x4 *>(from + 32 * (k + A));
             }
+            if (__ballot(lim < t0 + 63)) {
+                asm volatile("");               // (a branch that most tiles skip, not selects in all of them)
+#pragma unroll
+                for (int s = 0; s < 2; s++)
+#pragma unroll
+                    for (int i = 0; i < 16; i++) {
+                        const float e = exp2_of(z[s][i] * ks[2 * s + (i >> 3)] - total);
+                        w[s][i] += t0 + 32 * s + 8 * (i >> 2) + 4 * half + (i & 3) <= lim ? e : 0.0f;
+                    }
+            } else {
+#pragma unroll
+                for (int s = 0; s < 2; s++)
+#pragma unroll
+                    for (int i = 0; i < 16; i++) w[s][i] += exp2_of(__builtin_fmaf(z[s][i], ks[2 * s + (i >> 3)], -total));
+            }
+        }
         if (tile + 1 < tiles) place(buf ^ 1);
     }
 #pragma unroll
@@ -557,7 +573,8 @@ template <typename T, int DP, int NW> static hipError_t parts(const AttendArgs &
     parts_kernel<T, DP, NW><<<dim3(pairs * p.row_tiles * p.splits * 8u), 64 * NW, 0, s>>>(a, p);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && p.splits > 1u) {
-        join_parts_kernel<T><<<dim3((a.b.max_new * a.q_heads + 3u) / 4u, a.b.n_reqs), 256, 0, s>>>(a, p, 32u * NW);
+        const uint32_t each = 256u / (a.c.dim / 4u);
+        join_parts_kernel<T><<<dim3((a.b.max_new * a.q_heads + each - 1u) / each, a.b.n_reqs), 256, 0, s>>>(a, p, 32u * NW);
         e = hipGetLastError();
     }
     if (e == hipSuccess && a.w.data) {
