@@ -164,13 +164,16 @@ __device__ __forceinline__ uint32_t order_of(float w)
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-constexpr uint32_t kSelectThreads = 512;
+constexpr uint32_t kSelectThreads = 512, kHeldKeys = 16;     // keys a thread keeps: 8192 tokens of a workgroup
+constexpr uint32_t kBins = 2048;                            // digits of 11, 11 and 10 bits
 
 // One workgroup per (request, head): the want-th largest weight among the older tokens, digit by digit, then the positions of
-// what is larger, and of as many that equal it as are still wanted, in order.
+// what is larger, and of as many that equal it as are still wanted, in order.  Weights are read once where a thread can keep its
+// own (up to 8192 tokens), and again for every digit behind that.  Weights of attention share few exponents: 11 bits spread them over
+// more counters than 8 do, and that lanes meet on one counter is what this kernel waits for.
 __global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictArgs a)
 {
-    __shared__ uint32_t hist[256], wave_n[kSelectThreads / 64][2], found[2];
+    __shared__ uint32_t hist[kBins], wave_n[kSelectThreads / 64][2], found[2];
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6, head = blockIdx.x, r = blockIdx.y;
     const Request q = request_of(a.b, a.c, (int)r);
     const uint32_t len = (uint32_t)q.len, left = min(len, a.keep);
@@ -192,49 +195,60 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictArgs a)
         to_w[want + i] = w[old + i];
     }
     if (!want) return;
+    float held[kHeldKeys];
+#pragma unroll
+    for (uint32_t k = 0; k < kHeldKeys; k++) held[k] = k * kSelectThreads + tid < old ? w[k * kSelectThreads + tid] : 0.0f;
     // the want-th largest: of the keys that begin with `prefix`, the rank-th
     uint32_t prefix = 0, rank = want;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        if (tid < 256u) hist[tid] = 0;
+    for (int digit = 0; digit < 3; digit++) {
+        const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0;
+        const uint32_t bins = digit == 2 ? 1024u : kBins, above = digit == 0 ? 0u : digit == 1 ? ~0u << 21 : ~0u << 10;
+        for (uint32_t i = tid; i < kBins; i += kSelectThreads) hist[i] = 0;
         __syncthreads();
-        for (uint32_t i = tid; i < old; i += kSelectThreads) {
-            const uint32_t k = order_of(w[i]);
-            if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255u], 1u);
+        auto count = [&](float x) {
+            const uint32_t k = order_of(x);
+            if ((k & above) == prefix) atomicAdd(&hist[(k >> shift) & (bins - 1u)], 1u);
+        };
+#pragma unroll
+        for (uint32_t k = 0; k < kHeldKeys; k++)
+            if (k * kSelectThreads + tid < old) count(held[k]);
+        for (uint32_t i = kHeldKeys * kSelectThreads + tid; i < old; i += kSelectThreads) count(w[i]);
+        __syncthreads();
+        // four bins a thread, from the largest down
+        uint32_t n[4], sum = 0;
+#pragma unroll
+        for (int i = 0; i < 4; i++) sum += n[i] = hist[kBins - 1u - 4u * tid - i];
+        uint32_t before = sum;
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) {
+            const uint32_t up = (uint32_t)__shfl_up((int)before, m);
+            if (lane >= (uint32_t)m) before += up;
         }
+        if (lane == 63u) wave_n[wave][0] = before;
         __syncthreads();
-        if (wave == 0) {                        // four bins a lane, from the largest down
-            uint32_t n[4], sum = 0;
+        before -= sum;
 #pragma unroll
-            for (int i = 0; i < 4; i++) sum += n[i] = hist[255u - 4u * lane - i];
-            uint32_t before = sum;
+        for (uint32_t v = 0; v < kSelectThreads / 64; v++)
+            if (v < wave) before += wave_n[v][0];
 #pragma unroll
-            for (int m = 1; m < 64; m <<= 1) {
-                const uint32_t up = (uint32_t)__shfl_up((int)before, m);
-                if (lane >= (uint32_t)m) before += up;
+        for (int i = 0; i < 4; i++) {
+            if (before < rank && rank <= before + n[i]) {
+                found[0] = kBins - 1u - 4u * tid - i;
+                found[1] = rank - before;
             }
-            before -= sum;
-#pragma unroll
-            for (int i = 0; i < 4; i++) {
-                if (before < rank && rank <= before + n[i]) {
-                    found[0] = 255u - 4u * lane - i;
-                    found[1] = rank - before;
-                }
-                before += n[i];
-            }
+            before += n[i];
         }
         __syncthreads();
         prefix |= found[0] << shift;
         rank = found[1];
-        __syncthreads();
     }
     // `rank` of the keys that equal `prefix` are taken, the lowest positions first
     uint32_t taken = 0, equal = 0;
-    for (uint32_t base = 0; base < old; base += kSelectThreads) {
-        const uint32_t i = base + tid;
-        const float x = i < old ? w[i] : 0.0f;
-        const uint32_t k = order_of(x);
+    auto take = [&](uint32_t base, float x) {
+        const uint32_t i = base + tid, k = order_of(x);
         const bool is_more = i < old && k > prefix, is_equal = i < old && k == prefix;
         const uint64_t more = __ballot(is_more), same = __ballot(is_equal);
+        __syncthreads();
         if (!lane) {
             wave_n[wave][0] = (uint32_t)__popcll(more);
             wave_n[wave][1] = (uint32_t)__popcll(same);
@@ -258,65 +272,102 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictArgs a)
         }
         taken += all_m + min(equal + all_e, rank) - min(equal, rank);
         equal += all_e;
-        __syncthreads();
-    }
+    };
+#pragma unroll
+    for (uint32_t k = 0; k < kHeldKeys; k++)
+        if (k * kSelectThreads < old) take(k * kSelectThreads, held[k]);
+    for (uint32_t base = kHeldKeys * kSelectThreads; base < old; base += kSelectThreads) take(base, base + tid < old ? w[base + tid] : 0.0f);
 }
 
-// One wavefront per (request, block of `to`, head, K or V): the largest scale among the tokens that meet in the block, then
-// their codes, 16 bytes a lane.
-__global__ __launch_bounds__(256) void move_kernel(EvictArgs a)
+constexpr uint32_t kMoveWaves = 4096;           // four on each SIMD
+
+// One wavefront per (request, head) and as many whole blocks of `to` as 64 tokens make, at least one (just one while that leaves
+// wavefronts to spare: four requests of 8 heads that keep 256 tokens take 6.4 us so and 10.6 with 64 tokens each): where its tokens lie, a token a
+// lane; the largest scales of K and V that meet in each block; then their codes, 16 bytes a lane, eight loads at a time.  The heads
+// of a span of tokens follow each other on one XCD: they read the same pages, and write one block.
+__global__ __launch_bounds__(256) void move_kernel(EvictArgs a, uint32_t blocks, uint32_t spans)
 {
-    const uint32_t lane = threadIdx.x & 63u;
-    const uint32_t item = blockIdx.x * 4u + (threadIdx.x >> 6);
-    const uint32_t kv = item & 1u, head = (item >> 1) % a.c.heads, nth = (item >> 1) / a.c.heads, r = blockIdx.y;
+    const uint32_t lane = threadIdx.x & 63u, span = blocks * a.c.bs;
+    const uint32_t unit = (blockIdx.x >> 3) * 4u + (threadIdx.x >> 6);
+    const uint32_t item = unit / a.c.heads * 8u + (blockIdx.x & 7u), head = unit % a.c.heads, r = item / spans, nth = item - r * spans;
+    if (r >= a.b.n_reqs) return;
     const Request q = request_of(a.b, a.c, (int)r);
-    const uint32_t left = min((uint32_t)q.len, a.keep), first = nth * a.c.bs;
+    const uint32_t left = min((uint32_t)q.len, a.keep), first = nth * span;
     if (first >= left) return;
-    const int to = entry_of(a.to, q.row, nth);
-    if (to < 0) return;
-    const uint32_t m = min(a.c.bs, left - first), per_row = a.c.dim >> 4;
+    const uint32_t m = min(span, left - first), per_row = a.c.dim >> 4;
     const int32_t *pos = a.positions + ((int64_t)r * a.c.heads + head) * a.keep + first;
-    // a token's block, or -1, its slot and its scale
-    auto source = [&](uint32_t t, int &b, uint32_t &slot, float &s) {
+    // a token's codes (-1: nowhere) and scales
+    auto source = [&](uint32_t t, int64_t &at, float &sk, float &sv) {
         const uint32_t p = (uint32_t)pos[t], lb = block_of(a.c, p >> 4);
-        b = entry_of(a.c, q.row, lb);
-        slot = p - lb * a.c.bs;
-        s = b < 0 ? 0.0f : *scale_at(a.c, (int)kv, b, head);
+        const int b = entry_of(a.c, q.row, lb);
+        at = b < 0 ? -1 : (int64_t)b * a.c.block_stride + (int64_t)(p - lb * a.c.bs) * a.c.slot_stride + (int64_t)head * a.c.head_stride;
+        sk = b < 0 ? 0.0f : *scale_at(a.c, 0, b, head);
+        sv = b < 0 ? 0.0f : *scale_at(a.c, 1, b, head);
     };
-    float largest = 0.0f, s = 0.0f;
-    int b = -1;
-    uint32_t slot = 0;
-    for (uint32_t t = lane; t < m; t += 64u) {
-        source(t, b, slot, s);
-        largest = fmaxf(largest, s);
+    int64_t at = -1;
+    float sk = 0.0f, sv = 0.0f, most_k = 0.0f, most_v = 0.0f;       // the largest: of the block that the lane's token joins
+    for (uint32_t t0 = 0; t0 < m; t0 += 64u) {      // (more than one round only for blocks of more than 64 tokens)
+        at = -1, sk = sv = 0.0f;
+        if (t0 + lane < m) source(t0 + lane, at, sk, sv);
+        most_k = fmaxf(most_k, sk);
+        most_v = fmaxf(most_v, sv);
     }
-    largest = __uint_as_float(wave_largest(__float_as_uint(largest)));
-    if (!(largest > 0.0f)) largest = __uint_as_float((127u - 100u) << 23);      // nothing but entries outside the cache
+    const int joined = blocks == 1u ? 64 : (int)a.c.bs;             // lanes
+    for (int x = 1; x < joined; x <<= 1) most_k = fmaxf(most_k, __shfl_xor(most_k, x)), most_v = fmaxf(most_v, __shfl_xor(most_v, x));
+    // nothing but entries outside the cache
+    if (!(most_k > 0.0f)) most_k = __uint_as_float((127u - 100u) << 23);
+    if (!(most_v > 0.0f)) most_v = __uint_as_float((127u - 100u) << 23);
+    const int to = lane < blocks ? entry_of(a.to, q.row, nth * blocks + lane) : -1;
     for (uint32_t t0 = 0; t0 < m; t0 += 64u) {
         if (m > 64u) {
-            b = -1;
-            if (t0 + lane < m) source(t0 + lane, b, slot, s);
+            at = -1, sk = sv = 0.0f;
+            if (t0 + lane < m) source(t0 + lane, at, sk, sv);
         }
-        const float f = s / largest;
+        const float fk = sk / most_k, fv = sv / most_v;
         const uint32_t units = min(64u, m - t0) * per_row;
-        for (uint32_t u0 = 0; u0 < units; u0 += 64u) {
-            const uint32_t u = u0 + lane, t = u / per_row, part = u % per_row * 16u;
-            const int b_t = __shfl(b, (int)(t & 63u));
-            const uint32_t slot_t = (uint32_t)__shfl((int)slot, (int)(t & 63u));
-            const float f_t = __shfl(f, (int)(t & 63u));
-            if (u >= units) continue;
-            u32x4 w = {0u, 0u, 0u, 0u};
-            if (b_t >= 0) {
-                w = *reinterpret_cast<const u32x4 *>(code_at(a.c, (int)kv, b_t, slot_t, head) + part);
-                if (f_t != 1.0f) {
+        for (uint32_t u0 = 0; u0 < units; u0 += 256u) {
+            u32x4 wk[4], wv[4];
+            float gk[4], gv[4];
+            int64_t dst[4];
 #pragma unroll
-                    for (int i = 0; i < 4; i++) w[i] = scaled_codes(w[i], f_t);
+            for (int j = 0; j < 4; j++) {
+                const uint32_t u = u0 + 64u * j + lane, t = u / per_row, part = (u - t * per_row) * 16u;
+                const int from = (int)(t & 63u);
+                const int64_t src = (int64_t)(uint32_t)__shfl((int)(uint32_t)at, from) | (int64_t)__shfl((int)(at >> 32), from) << 32;
+                gk[j] = __shfl(fk, from);
+                gv[j] = __shfl(fv, from);
+                const uint32_t slot = t0 + t, block = blocks == 1u ? 0u : slot / a.c.bs;
+                const int e = __shfl(to, (int)(block & 63u));
+                dst[j] = u < units && e >= 0 ? (int64_t)e * a.to.block_stride + (int64_t)(slot - block * a.c.bs) * a.to.slot_stride +
+                                                   (int64_t)head * a.to.head_stride + part : -1;
+                wk[j] = wv[j] = u32x4{0u, 0u, 0u, 0u};
+                if (dst[j] >= 0 && src >= 0) {
+                    wk[j] = *reinterpret_cast<const u32x4 *>(a.c.code[0] + src + part);
+                    wv[j] = *reinterpret_cast<const u32x4 *>(a.c.code[1] + src + part);
                 }
             }
-            *reinterpret_cast<u32x4 *>(code_at(a.to, (int)kv, to, t0 + t, head) + part) = w;
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                if (dst[j] < 0) continue;
+                if (gk[j] != 1.0f) {
+#pragma unroll
+                    for (int i = 0; i < 4; i++) wk[j][i] = scaled_codes(wk[j][i], gk[j]);
+                }
+                if (gv[j] != 1.0f) {
+#pragma unroll
+                    for (int i = 0; i < 4; i++) wv[j][i] = scaled_codes(wv[j][i], gv[j]);
+                }
+                *reinterpret_cast<u32x4 *>(a.to.code[0] + dst[j]) = wk[j];
+                *reinterpret_cast<u32x4 *>(a.to.code[1] + dst[j]) = wv[j];
+            }
         }
     }
-    if (!lane) *scale_at(a.to, (int)kv, to, head) = largest;
+    most_k = __shfl(most_k, (int)(lane * a.c.bs & 63u));
+    most_v = __shfl(most_v, (int)(lane * a.c.bs & 63u));
+    if (lane < blocks && lane * a.c.bs < m && to >= 0) {
+        *scale_at(a.to, 0, to, head) = most_k;
+        *scale_at(a.to, 1, to, head) = most_v;
+    }
 }
 
 hipError_t launch_evict(const EvictArgs &a, hipStream_t s)
@@ -324,8 +375,13 @@ hipError_t launch_evict(const EvictArgs &a, hipStream_t s)
     select_kernel<<<dim3(a.c.heads, a.b.n_reqs), kSelectThreads, 0, s>>>(a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    const uint32_t blocks = (min(a.keep, max(a.b.max_len, 1u)) + a.c.bs - 1u) / a.c.bs;
-    move_kernel<<<dim3((blocks * a.c.heads * 2u + 3u) / 4u, a.b.n_reqs), 256, 0, s>>>(a);
+    const uint32_t left = min(a.keep, max(a.b.max_len, 1u));
+    uint32_t blocks = max(1u, 64u / a.c.bs);
+    if ((uint64_t)left * a.b.n_reqs * a.c.heads < 64u * kMoveWaves) blocks = 1;
+    const uint32_t span = blocks * a.c.bs, spans = (left + span - 1u) / span;
+    const uint64_t units = ((uint64_t)spans * a.b.n_reqs + 7u) / 8u * a.c.heads, groups = (units + 3u) / 4u * 8u;    // units: on each XCD
+    if (groups > 0xffffffffu / 256u) return hipErrorInvalidConfiguration;
+    move_kernel<<<(uint32_t)groups, 256, 0, s>>>(a, blocks, spans);
     return hipGetLastError();
 }
 
