@@ -67,6 +67,7 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 // How few query rows are attended to: see dmi_kv8_tokens.hip.
 struct TokensPlan {
+    bool whole;                                 // a workgroup takes a request and head: no ranges
     uint32_t ranges;                            // equal parts of all contexts
     uint32_t tile_rows, row_tiles;              // query rows of a wavefront; wavefronts for the rows that share a head
     uint32_t join_blocks;                       // workgroups of the second launch that join parts, 0 if there can be none

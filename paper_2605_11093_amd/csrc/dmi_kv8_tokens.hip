@@ -27,6 +27,13 @@ __device__ __forceinline__ int lanes_scan(int v)
 // A request with new tokens has a tile at least: an empty context's rows are written too.
 __device__ __forceinline__ int tiles_of(const Request &q) { return q.fresh > 0 ? max(1, (q.len + 31) >> 5) : 0; }
 
+// A request that a lane has
+__device__ __forceinline__ Request request_in(const Request &q, int lane)
+{
+    return {__builtin_amdgcn_readlane(q.row, lane), __builtin_amdgcn_readlane(q.len, lane), __builtin_amdgcn_readlane(q.start, lane),
+            __builtin_amdgcn_readlane(q.fresh, lane)};
+}
+
 // The tiles of requests n0 .. n0 + 63, one request a lane
 __device__ __forceinline__ int lane_tiles(const AttendArgs &a, uint32_t n0)
 {
@@ -57,49 +64,70 @@ __device__ __forceinline__ int64_t part_at(const AttendArgs &a, const TokensPlan
 // (column c, group g) holds tokens 4g..4g+3 of each of two sixteens of tokens, and which token stands at which place of the
 // product's inner dimension is free as long as V agrees.  V is read with 8 tokens x 8 elements a lane (128 elements), its bytes
 // interleaved by twos and converted: column m of V^T is element 8m + j for instruction j.  Nothing passes through LDS.
-template <typename T, int DP, int NT>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP * NT <= 128 ? 2 : 1)))
+template <int N> struct Int {
+    static constexpr int value = N;
+};
+
+constexpr int waves_of(int dp, int nt, bool whole) { return !whole || dp * nt > 128 ? 4 : 8; }
+
+template <typename T, int DP, int NT, bool WHOLE>
+__global__ __launch_bounds__(64 * waves_of(DP, NT, WHOLE)) __attribute__((amdgpu_waves_per_eu(DP * NT <= 128 ? 2 : 1)))
 void tokens_kernel(AttendArgs a, TokensPlan p)
 {
     constexpr int KL = DP / 64;                 // 16-byte loads of K a lane and sixteen
     constexpr int KK = DP / 32;                 // instructions for a sixteen's scores
     constexpr int VW = DP / 64;                 // words of V a lane and token
     constexpr int NJ = DP / 16;                 // instructions for 16 query rows' outputs
+    [[maybe_unused]] constexpr int NW = waves_of(DP, NT, WHOLE);
 
     const int lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
-    // Workgroups go to the eight XCDs in turn: the heads (and row tiles) of a range follow each other on one of them.
-    const uint32_t unit = (blockIdx.x >> 3) * 4u + (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), per = a.c.heads * p.row_tiles;
-    const int range = (int)(unit / per * 8u + (blockIdx.x & 7u));
-    const uint32_t head = unit % per % a.c.heads, row_tile = unit % per / a.c.heads;
-    const int row0 = (int)row_tile * 16 * NT;
-    if (range >= (int)p.ranges) return;
-
-    // the range's first tile, the request that it lies in
-    int total, of_range, r = 0, seg0 = 0;       // seg0: the request's first tile
-    if (a.b.n_reqs <= 64u) {
-        const int upto = lanes_scan(lane_tiles(a, 0));
-        total = __builtin_amdgcn_readlane(upto, 63);
-        of_range = range_tiles(p, total);
-        if (range * of_range >= total) return;
-        r = __ffsll((unsigned long long)__ballot(upto > range * of_range)) - 1;
-        seg0 = r ? __builtin_amdgcn_readlane(upto, r - 1) : 0;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    uint32_t head, row_tile = 0;
+    int r = 0, seg0 = 0, range = 0, first, last;        // seg0: the request's first tile; first, last: the range's tiles
+    Request held{0, 0, 0, 0};                           // of this lane, where there are no more than lanes
+    if constexpr (WHOLE) {
+        r = (int)(blockIdx.x / a.c.heads);
+        head = blockIdx.x % a.c.heads;
+        const Request q = request_of(a.b, a.c, r);
+        const int tiles = q.fresh > 0 ? tiles_of(q) : a.w.data ? (q.len + 31) >> 5 : 0;
+        first = tiles * wave / NW;
+        last = tiles * (wave + 1) / NW;
     } else {
-        total = all_tiles(a);
-        of_range = range_tiles(p, total);
-        if (range * of_range >= total) return;
-        for (;; r += 64) {
-            const int upto = lanes_scan(lane_tiles(a, (uint32_t)r)), sum = __builtin_amdgcn_readlane(upto, 63);
-            if (seg0 + sum <= range * of_range) {
-                seg0 += sum;
-                continue;
+        // Workgroups go to the eight XCDs in turn: the heads (and row tiles) of a range follow each other on one of them.
+        const uint32_t unit = (blockIdx.x >> 3) * 4u + (uint32_t)wave, per = a.c.heads * p.row_tiles;
+        range = (int)(unit / per * 8u + (blockIdx.x & 7u));
+        head = unit % per % a.c.heads, row_tile = unit % per / a.c.heads;
+        if (range >= (int)p.ranges) return;
+        // the range's first tile, the request that it lies in
+        int total, of_range;
+        if (a.b.n_reqs <= 64u) {
+            if ((uint32_t)lane < a.b.n_reqs) held = request_of(a.b, a.c, lane);
+            const int upto = lanes_scan(tiles_of(held));
+            total = __builtin_amdgcn_readlane(upto, 63);
+            of_range = range_tiles(p, total);
+            if (range * of_range >= total) return;
+            r = __ffsll((unsigned long long)__ballot(upto > range * of_range)) - 1;
+            seg0 = r ? __builtin_amdgcn_readlane(upto, r - 1) : 0;
+        } else {
+            total = all_tiles(a);
+            of_range = range_tiles(p, total);
+            if (range * of_range >= total) return;
+            for (;; r += 64) {
+                const int upto = lanes_scan(lane_tiles(a, (uint32_t)r)), sum = __builtin_amdgcn_readlane(upto, 63);
+                if (seg0 + sum <= range * of_range) {
+                    seg0 += sum;
+                    continue;
+                }
+                const int in = __ffsll((unsigned long long)__ballot(seg0 + upto > range * of_range)) - 1;
+                seg0 += in ? __builtin_amdgcn_readlane(upto, in - 1) : 0;
+                r += in;
+                break;
             }
-            const int in = __ffsll((unsigned long long)__ballot(seg0 + upto > range * of_range)) - 1;
-            seg0 += in ? __builtin_amdgcn_readlane(upto, in - 1) : 0;
-            r += in;
-            break;
         }
+        first = range * of_range;
+        last = min(first + of_range, total);
     }
-    const int first = range * of_range, last = min(first + of_range, total);    // the range's tiles
+    const int row0 = (int)row_tile * 16 * NT;
 
     // byte offsets of this lane within a sixteen; elements past the row's end are read from its start (q is 0 there, and
     // V's columns there are not written)
@@ -111,12 +139,12 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
     }
     v_off = (uint32_t)(4 * g) * (uint32_t)a.c.slot_stride + ((uint32_t)col * (DP / 16) < a.c.dim ? (uint32_t)col * (DP / 16) : 0u);
 
-    for (; r < (int)a.b.n_reqs && seg0 < last; r++) {
-        const Request q = request_of(a.b, a.c, r);
-        const int seg_tiles = tiles_of(q), seg_first = seg0;
+    for (; r < (int)a.b.n_reqs && (WHOLE || seg0 < last); r++) {
+        const Request q = !WHOLE && a.b.n_reqs <= 64u ? request_in(held, r) : request_of(a.b, a.c, r);
+        const int seg_tiles = WHOLE ? last : tiles_of(q), seg_first = seg0;
         seg0 += seg_tiles;
         const int rows = q.fresh * (int)a.group;
-        if (!seg_tiles || row0 >= rows) continue;
+        if (!WHOLE && (!seg_tiles || row0 >= rows)) continue;
         // this context's tiles in this range
         const int from = max(first, seg_first) - seg_first, to = min(last, seg_first + seg_tiles) - seg_first, tiles = to - from;
         const int begin = 32 * from, end = min(q.len, 32 * to);
@@ -145,14 +173,14 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
 #pragma unroll
         for (int n = 0; n < NT; n++) {
             const int row = row0 + 16 * n + col;
-            const QueryRow w = query_row(a, head, (uint32_t)row);
+            const QueryRow w = query_row(a, head, (uint32_t)min(row, max(rows - 1, 0)));     // (columns behind the last row: not written)
             lim[n] = row < rows ? q.len - q.fresh + w.token : q.len;
-            const uint16_t *src = static_cast<const uint16_t *>(a.q.data) + (int64_t)(q.start + w.token) * a.q.row_stride + (int64_t)w.head * a.q.head_stride;
+            const uint16_t *src = static_cast<const uint16_t *>(a.q.data) + (int64_t)min(q.start + w.token, (int)a.b.total_new - 1) * a.q.row_stride +
+                                  (int64_t)w.head * a.q.head_stride;
 #pragma unroll
             for (int k = 0; k < KK; k++) {
                 const int d = g * (DP / 4) + 8 * k;
-                qf[n][k] = u32x4{0u, 0u, 0u, 0u};
-                if (row < rows && d < (int)a.c.dim) qf[n][k] = *reinterpret_cast<const u32x4 *>(src + d);
+                qf[n][k] = *reinterpret_cast<const u32x4 *>(src + (d < (int)a.c.dim ? d : 0));
             }
         }
         const int all_see = q.len - q.fresh + row0 / (int)a.group;      // what every row of the tile sees
@@ -203,9 +231,19 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
             for (int j = 0; j < NJ; j++) o[n][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         }
 
-        fetch_k(0);
-        fetch_v(0);
-        for (int tile = 0; tile < tiles; tile++) {
+        const bool any_tile = !WHOLE || (tiles > 0 && rows > 0);
+        if (any_tile) {
+            fetch_k(0);
+            fetch_v(0);
+        }
+        if ((int)a.c.dim < DP) {
+#pragma unroll
+            for (int n = 0; n < NT; n++)
+#pragma unroll
+                for (int k = 0; k < KK; k++)
+                    if (g * (DP / 4) + 8 * k >= (int)a.c.dim) qf[n][k] = u32x4{0u, 0u, 0u, 0u};
+        }
+        for (int tile = 0; any_tile && tile < tiles; tile++) {
             const int t0 = begin + 32 * tile, ahead = min(tile + 1, tiles - 1);
             int count[2];
             float ks[2], vs[2];
@@ -376,6 +414,116 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
             }
         }
 
+        if constexpr (WHOLE) {
+            // the wavefronts' sums, relative to the largest score of all; the later half of them hand theirs to the others
+            constexpr int kSlots = NW / 2;
+            __shared__ f32x4 joined[kSlots][NT * NJ * 64];
+            __shared__ float tops[NW][16 * NT], sums[NW][16 * NT];
+#pragma unroll
+            for (int n = 0; n < NT; n++) {
+                l[n] += __shfl_xor(l[n], 16);
+                l[n] += __shfl_xor(l[n], 32);
+                if (g == 0) tops[wave][16 * n + col] = m[n];
+            }
+            __syncthreads();
+            auto top_of = [&](int c) {
+                float t = -INFINITY;
+#pragma unroll
+                for (int v = 0; v < NW; v++) t = fmaxf(t, tops[v][c]);
+                return t;
+            };
+            auto total_of = [&](int c, float &sum) {    // log2 of the sum of 2^score
+                sum = 0.0f;
+#pragma unroll
+                for (int v = 0; v < NW; v++) sum += sums[v][c];
+                const float t = top_of(c);
+                return t == -INFINITY && sum == 0.0f ? -INFINITY : (t == -INFINITY ? 0.0f : t) + log2_of(sum);
+            };
+#pragma unroll
+            for (int n = 0; n < NT; n++) {
+                const float t = top_of(16 * n + col), f = exp2_of(m[n] - (t == -INFINITY ? 0.0f : t));
+                if (g == 0) sums[wave][16 * n + col] = l[n] * f;
+#pragma unroll
+                for (int j = 0; j < NJ; j++) {
+                    o[n][j] *= f * v_ref;
+                    if (wave >= kSlots) joined[wave - kSlots][(n * NJ + j) * 64 + lane] = o[n][j];
+                }
+            }
+            __syncthreads();
+            if (wave < kSlots) {
+#pragma unroll
+                for (int n = 0; n < NT; n++)
+#pragma unroll
+                    for (int j = 0; j < NJ; j++) joined[wave][(n * NJ + j) * 64 + lane] += o[n][j];
+            }
+            __syncthreads();
+            for (int u = (int)threadIdx.x; u < NT * NJ / 4 * 64; u += 64 * NW) {
+                const int n = (u >> 6) / (NJ / 4), j = (u >> 6) % (NJ / 4) * 4, row = 16 * n + col;
+                if (row >= rows) continue;
+                f32x4 sum[4] = {};
+#pragma unroll
+                for (int v = 0; v < kSlots; v++)
+#pragma unroll
+                    for (int k = 0; k < 4; k++) sum[k] += joined[v][(n * NJ + j + k) * 64 + lane];
+                float l_all;
+                const float total = total_of(row, l_all), f = total == -INFINITY && l_all == 0.0f ? 0.0f : 1.0f / l_all;
+                const QueryRow w = query_row(a, head, (uint32_t)row);
+                uint16_t *dst = static_cast<uint16_t *>(a.out.data) + (int64_t)(q.start + w.token) * a.out.row_stride + (int64_t)w.head * a.out.head_stride;
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    const int d = NJ * (4 * g + i) + j;
+                    if (d < (int)a.c.dim)
+                        *reinterpret_cast<u32x2 *>(dst + d) = u32x2{T::pack(sum[0][i] * f, sum[1][i] * f), T::pack(sum[2][i] * f, sum[3][i] * f)};
+                }
+                if (a.lse && g == 0 && j == 0) a.lse[(int64_t)(q.start + w.token) * a.q_heads + w.head] = total * kLn2;
+            }
+            if (!a.w.data) return;
+            // weights, out of the scores that the same lane wrote
+            float total[NT], unused;
+#pragma unroll
+            for (int n = 0; n < NT; n++) total[n] = total_of(16 * n + col, unused);
+            const float *prior = a.prior.data + (int64_t)q.row * a.prior.row_stride + (int64_t)head * a.prior.head_stride;
+            float *to_w = a.w.data + (int64_t)q.row * a.w.row_stride + (int64_t)head * a.w.head_stride;
+            const int older = q.len - q.fresh;
+            const int last_row = max(rows - 1, 0);
+            for (int t0 = begin; t0 < end; t0 += 128) {
+                f32x4 z[NT][8];
+                if (rows) {
+#pragma unroll
+                    for (int n = 0; n < NT; n++)
+#pragma unroll
+                        for (int x = 0; x < 8; x++)
+                            z[n][x] = *reinterpret_cast<const f32x4 *>(
+                                p.scores + ((int64_t)head * a.b.total_new * a.group + (int64_t)q.start * a.group + min(16 * n + col, last_row)) * p.score_stride +
+                                min(t0 + 16 * x, (end - 1) & ~15) + 4 * g);
+                }
+                float sum[32];
+#pragma unroll
+                for (int e = 0; e < 32; e++) {
+                    sum[e] = 0.0f;
+#pragma unroll
+                    for (int n = 0; n < NT; n++) sum[e] += 16 * n + col < rows && total[n] != -INFINITY ? exp2_of(z[n][e / 4][e % 4] - total[n]) : 0.0f;
+                }
+                // over the columns: of two lanes each goes on with half of the tokens
+                auto halve = [&](auto k_) {
+                    constexpr int k = decltype(k_)::value;
+#pragma unroll
+                    for (int e = 0; e < 2 * k; e++) {
+                        const float low = sum[e], high = sum[e + 2 * k], other = __shfl_xor(col & k ? low : high, k);
+                        sum[e] = (col & k ? high : low) + other;
+                    }
+                };
+                halve(Int<8>{});
+                halve(Int<4>{});
+                halve(Int<2>{});
+                halve(Int<1>{});
+                const int t = t0 + 8 * (col & ~1) + 4 * g + 2 * (col & 1);
+#pragma unroll
+                for (int i = 0; i < 2; i++)
+                    if (t + i < end) to_w[t + i] = a.prior.data && t + i < older ? a.decay * prior[t + i] + sum[i] : sum[i];
+            }
+            return;
+        }
 #pragma unroll
         for (int n = 0; n < NT; n++) {
             l[n] += __shfl_xor(l[n], 16);
@@ -472,21 +620,28 @@ __global__ __launch_bounds__(256) void finish_kernel(AttendArgs a, TokensPlan p)
     const uint32_t rows = (uint32_t)q.fresh * a.group;
     if (blockIdx.x < p.join_blocks) {
         const uint32_t n = blockIdx.x * 4u + (uint32_t)wave;
-        if (n >= rows * a.c.heads) return;
         const Spread s = spread_of(a, p, blockIdx.y);
-        if (s.from == s.to) return;
+        if (n >= rows * a.c.heads || s.from == s.to) return;
         const uint32_t head = n / rows, row = n - head * rows;
         const float total = total_of(a, p, s, head, row);
         const QueryRow w = query_row(a, head, row);
         // as many parts at a time as there are lanes for
         const int wide = (int)a.c.dim / 4, teams = 64 / wide, team = lane / wide, d = 4 * (lane - team * wide);
         f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (team < teams) {
-#pragma unroll 4
-            for (int i = s.from + team; i <= s.to; i += teams) {
-                const int64_t part = part_at(a, p, i, i == s.from, head, row);
-                const float f = total == -INFINITY ? 0.0f : exp2_of(p.sums[part][0] - total);
-                sum += *reinterpret_cast<const f32x4 *>(p.parts + part * a.c.dim + d) * f;
+        for (int i0 = s.from; i0 <= s.to && team < teams; i0 += 8 * teams) {
+            f32x4 x[8];
+            float f[8];
+#pragma unroll
+            for (int k = 0; k < 8; k++) {
+                const int i = i0 + k * teams + team;
+                const int64_t part = part_at(a, p, min(i, s.to), min(i, s.to) == s.from, head, row);
+                x[k] = *reinterpret_cast<const f32x4 *>(p.parts + part * a.c.dim + d);
+                f[k] = p.sums[part][0];
+            }
+#pragma unroll
+            for (int k = 0; k < 8; k++) {
+                if (i0 + k * teams > s.to) break;
+                if (i0 + k * teams + team <= s.to) sum += x[k] * (total == -INFINITY ? 0.0f : exp2_of(f[k] - total));
             }
         }
         for (int k = 1; k < teams; k++)
@@ -536,16 +691,21 @@ __global__ __launch_bounds__(256) void finish_kernel(AttendArgs a, TokensPlan p)
 template <typename T> static hipError_t tokens(const AttendArgs &a, const TokensPlan &p, hipStream_t s)
 {
     const uint32_t per = a.c.heads * p.row_tiles, units = (p.ranges + 7u) / 8u * per;      // on each XCD
-    const dim3 grid((units + 3u) / 4u * 8u);
     const int dp = a.c.dim <= 64 ? 64 : a.c.dim <= 128 ? 128 : 256;
+    auto launch = [&](auto dp_, auto nt_) {
+        constexpr int DP = decltype(dp_)::value, NT = decltype(nt_)::value;
+        if (p.whole) tokens_kernel<T, DP, NT, true><<<a.b.n_reqs * a.c.heads, 64 * waves_of(DP, NT, true), 0, s>>>(a, p);
+        else tokens_kernel<T, DP, NT, false><<<(units + 3u) / 4u * 8u, 256, 0, s>>>(a, p);
+    };
     if (p.tile_rows == 16) {
-        if (dp == 64) tokens_kernel<T, 64, 1><<<grid, 256, 0, s>>>(a, p);
-        else if (dp == 128) tokens_kernel<T, 128, 1><<<grid, 256, 0, s>>>(a, p);
-        else tokens_kernel<T, 256, 1><<<grid, 256, 0, s>>>(a, p);
+        if (dp == 64) launch(Int<64>{}, Int<1>{});
+        else if (dp == 128) launch(Int<128>{}, Int<1>{});
+        else launch(Int<256>{}, Int<1>{});
     } else {
-        if (dp == 64) tokens_kernel<T, 64, 2><<<grid, 256, 0, s>>>(a, p);
-        else tokens_kernel<T, 128, 2><<<grid, 256, 0, s>>>(a, p);
+        if (dp == 64) launch(Int<64>{}, Int<2>{});
+        else launch(Int<128>{}, Int<2>{});
     }
+    if (p.whole) return hipGetLastError();
     hipError_t e = hipGetLastError();
     const uint32_t weight_blocks = a.w.data ? (a.b.max_len + 1023u) / 1024u * a.c.heads : 0u;
     if (e != hipSuccess || p.join_blocks + weight_blocks == 0) return e;
