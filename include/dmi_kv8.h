@@ -120,7 +120,7 @@ dmi_status_t dmi_kv8_attend(const dmi_kv8_t *cache /*[host]*/, const dmi_kv8_bat
  * RN(code * scale / new scale)).  Shorter requests are copied whole.  `to` may lie in the same memory, but no block that it
  * lists may be listed by `cache` for a row of this call.  new_len = min(len, keep).
  *   batch         lens_dev, rows_dev, n_reqs and max_len are used
- *   to_weight     [host] the kept tokens' weights, in their new positions
+ *   to_weight     [host] the kept tokens' weights, in their new positions (not in weight's memory)
  *   positions_dev [device] int32 [n_reqs][n_heads][keep]: the kept tokens' old positions, -1 from new_len on
  *   to_lens_dev   [device] int32 [n_reqs]: the new lengths (not in lens_dev's memory)
  */

@@ -3,6 +3,6 @@
 The product is libdmi.so (HIP kernels + C ABI, see include/dmi.h); this package
 only marshals arguments for it.
 """
-from .binding import (DmiError, PreparedBatch, PreparedObserve, Ring, Step, Stats, RecordView, lib, library_path,  # noqa: F401
-                      record_bytes, version)
+from .binding import (DmiError, KV8, KV8Batch, PreparedBatch, PreparedObserve, Ring, Step, Stats, RecordView,  # noqa: F401
+                      kv8_append, kv8_attend, kv8_attend_workspace, kv8_evict, lib, library_path, record_bytes, version)
 from . import binding  # noqa: F401
