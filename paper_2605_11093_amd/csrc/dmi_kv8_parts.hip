@@ -436,6 +436,17 @@ __global__ __launch_bounds__(256) void join_parts_kernel(AttendArgs a, PartsPlan
 
 // Weights: 256 tokens a workgroup, 64 a wavefront, whose K stays in registers; the query rows that see them pass through LDS 64 at
 // a time (32 of 256 elements).  Scores once more (their rows' totals were not known before), p summed over the rows in fp32, in order.
+// A product's N matrix instructions and 48 vector ones in turn
+template <int N> __device__ __forceinline__ void interleave()
+{
+#pragma unroll
+    for (int k = 0; k < N; k++) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x402, 48 / N, 0);
+    }
+}
+
 template <typename T, int DP>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ? 2 : 1))) void weights_kernel(AttendArgs a, PartsPlan p)
 {
@@ -455,32 +466,38 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
     u32x4 rq[QL];
     float rt = -INFINITY;
     int rl = -1;
-    auto fetch = [&](int tile) {
-        const int row = first_row + QT * tile + (int)(threadIdx.x / TR);
-        const QueryRow w = query_row(a, head, (uint32_t)min(row, rows - 1));
-        const uint16_t *src = static_cast<const uint16_t *>(a.q.data) + (int64_t)(q.start + w.token) * a.q.row_stride + (int64_t)w.head * a.q.head_stride;
+    const int per_token = (int)a.group, step_token = QT / per_token, step_head = QT - step_token * per_token;
+    int next = first_row + (int)(threadIdx.x / TR), token = next / per_token, head_of = next - token * per_token;
+    auto fetch = [&]() {                        // of the rows that follow
+        const int at = min(token, q.fresh - 1);
+        const uint32_t q_head = head * a.group + (uint32_t)head_of;
+        const uint16_t *src = static_cast<const uint16_t *>(a.q.data) + (int64_t)(q.start + at) * a.q.row_stride + (int64_t)q_head * a.q.head_stride;
 #pragma unroll
         for (int c = 0; c < QL; c++) {
             const int d = 8 * TR * c + 8 * (int)(threadIdx.x % TR);
             rq[c] = *reinterpret_cast<const u32x4 *>(src + (d < (int)a.c.dim ? d : 0));
         }
-        rt = p.totals[(int64_t)(q.start + w.token) * a.q_heads + w.head];
-        rl = row < rows ? older + w.token : -1;
+        rt = p.totals[(int64_t)(q.start + at) * a.q_heads + q_head];
+        rl = token < q.fresh ? older + token : -1;
+        token += step_token, head_of += step_head;
+        if (head_of >= per_token) head_of -= per_token, token++;
     };
     auto place = [&](int buf) {
+        if ((int)a.c.dim < DP) {
 #pragma unroll
-        for (int c = 0; c < QL; c++) {
-            const int d = 8 * TR * c + 8 * (int)(threadIdx.x % TR);
+            for (int c = 0; c < QL; c++)
 #pragma unroll
-            for (int i = 0; i < 4; i++) rq[c][i] = d < (int)a.c.dim ? rq[c][i] : 0u;
-            *reinterpret_cast<u32x4 *>(lq[buf] + (threadIdx.x / TR) * QP + 2 * d) = rq[c];
+                for (int i = 0; i < 4; i++) rq[c][i] = 8 * TR * c + 8 * (int)(threadIdx.x % TR) < (int)a.c.dim ? rq[c][i] : 0u;
         }
-        if ((threadIdx.x % TR) == 0) {
-            lt[buf][threadIdx.x / TR] = rt;
-            ll[buf][threadIdx.x / TR] = rt == -INFINITY ? -1 : rl;     // (a row that saw nothing weighs nothing)
+#pragma unroll
+        for (int c = 0; c < QL; c++)
+            *reinterpret_cast<u32x4 *>(lq[buf] + (threadIdx.x / TR) * QP + 16 * TR * c + 16 * (threadIdx.x % TR)) = rq[c];
+        if ((threadIdx.x % TR) == 0) {          // a row that saw nothing, or is none, weighs nothing
+            lt[buf][threadIdx.x / TR] = rt == -INFINITY || rl < 0 ? INFINITY : rt;
+            ll[buf][threadIdx.x / TR] = rl;
         }
     };
-    if (tiles > 0) fetch(0);
+    if (tiles > 0) fetch();
 
     // K of the wavefront's tokens: two 32s, their sixteens' scales
     const Look l = look_up(a, q, head, t0 + 16 * lane, lane < 4 ? q.len : 0, a.scale_log2);
@@ -507,18 +524,21 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
 #pragma unroll
         for (int i = 0; i < 16; i++) w[s][i] = 0.0f;
     if (tiles > 0) place(0);
+    constexpr int A = DP <= 128 ? (KK < 8 ? KK : 8) : 4;          // operands read ahead
+    auto operand = [&](int buf, int h, int k) { return *reinterpret_cast<const u32x4 *>(lq[buf] + (32 * h + col) * QP + 16 * half + 32 * k); };
+    // rows that do not see all of the workgroup's tokens (those behind the context are not written)
+    const int seen = max(0, min(block0 + 255, q.len - 1) - older) * per_token - first_row;      // rows in front of the first that does
+    const int masked = min(tiles, (max(seen, 0) + QT - 1) / QT);
 #pragma unroll 1
-    for (int tile = 0; tile < tiles; tile++) {
+    for (int tile = 0; tile < masked; tile++) {
         const int buf = tile & 1;
-        if (tile + 1 < tiles) fetch(tile + 1);
+        if (tile + 1 < tiles) fetch();
         lds_barrier();
 #pragma unroll 1
         for (int h = 0; h < QT / 32; h++) {
-            constexpr int A = DP <= 128 ? (KK < 8 ? KK : 8) : 4;      // operands read ahead
-            const uint8_t *const from = lq[buf] + (32 * h + col) * QP + 16 * half;
             u32x4 f[A];
 #pragma unroll
-            for (int k = 0; k < A; k++) f[k] = *reinterpret_cast<const u32x4 *>(from + 32 * k);
+            for (int k = 0; k < A; k++) f[k] = operand(buf, h, k);
             const float total = lt[buf][32 * h + col];
             const int lim = ll[buf][32 * h + col];
             f32x16 z[2];
@@ -530,25 +550,70 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
             for (int k = 0; k < KK; k++) {
 #pragma unroll
                 for (int s = 0; s < 2; s++) z[s] = T::mfma32(kf[s][k], f[k % A], z[s]);
-                if (k + A < KK) f[k % A] = *reinterpret_cast<const u32x4 *>(from + 32 * (k + A));
+                if (k + A < KK) f[k % A] = operand(buf, h, k + A);
             }
-            if (__ballot(lim < t0 + 63)) {
-                asm volatile("");               // (a branch that most tiles skip, not selects in all of them)
 #pragma unroll
-                for (int s = 0; s < 2; s++)
+            for (int s = 0; s < 2; s++)
 #pragma unroll
-                    for (int i = 0; i < 16; i++) {
-                        const float e = exp2_of(z[s][i] * ks[2 * s + (i >> 3)] - total);
-                        w[s][i] += t0 + 32 * s + 8 * (i >> 2) + 4 * half + (i & 3) <= lim ? e : 0.0f;
-                    }
-            } else {
-#pragma unroll
-                for (int s = 0; s < 2; s++)
-#pragma unroll
-                    for (int i = 0; i < 16; i++) w[s][i] += exp2_of(__builtin_fmaf(z[s][i], ks[2 * s + (i >> 3)], -total));
-            }
+                for (int i = 0; i < 16; i++) {
+                    const float e = exp2_of(z[s][i] * ks[2 * s + (i >> 3)] - total);
+                    w[s][i] += t0 + 32 * s + 8 * (i >> 2) + 4 * half + (i & 3) <= lim ? e : 0.0f;
+                }
         }
         if (tile + 1 < tiles) place(buf ^ 1);
+    }
+    // The others: one 32 of tokens is weighed while the products of the other run.
+    if (masked < tiles) {
+        int buf = masked & 1, h = 0;
+        if (masked + 1 < tiles) fetch();
+        lds_barrier();
+        u32x4 f[KK];
+#pragma unroll
+        for (int k = 0; k < KK; k++) f[k] = operand(buf, 0, k);
+        float total = lt[buf][col];
+        f32x16 z0, z1;
+        auto zero = [](f32x16 &z) {
+#pragma unroll
+            for (int i = 0; i < 16; i++) z[i] = 0.0f;
+        };
+        zero(z0);
+#pragma unroll
+        for (int k = 0; k < KK; k++) z0 = T::mfma32(kf[0][k], f[k], z0);
+        int left = tiles - masked - 1;          // tiles behind this one
+#pragma unroll 1
+        for (int n = (left + 1) * (QT / 32) - 1; n > 0; n--) {
+            if (++h == QT / 32) {
+                place(buf ^ 1);
+                lds_barrier();
+                if (left > 1) fetch();
+                left--, buf ^= 1, h = 0;
+            }
+            const float next_total = lt[buf][32 * h + col];
+            zero(z1);
+#pragma unroll
+            for (int k = 0; k < KK; k++) {
+                z1 = T::mfma32(kf[1][k], f[k], z1);
+                f[k] = operand(buf, h, k);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; i++) w[0][i] += exp2_of(__builtin_fmaf(z0[i], ks[i >> 3], -total));
+            interleave<KK>();
+            zero(z0);
+#pragma unroll
+            for (int k = 0; k < KK; k++) z0 = T::mfma32(kf[0][k], f[k], z0);
+#pragma unroll
+            for (int i = 0; i < 16; i++) w[1][i] += exp2_of(__builtin_fmaf(z1[i], ks[2 + (i >> 3)], -total));
+            interleave<KK>();
+            total = next_total;
+        }
+        zero(z1);
+#pragma unroll
+        for (int k = 0; k < KK; k++) z1 = T::mfma32(kf[1][k], f[k], z1);
+#pragma unroll
+        for (int i = 0; i < 16; i++) {
+            w[0][i] += exp2_of(__builtin_fmaf(z0[i], ks[i >> 3], -total));
+            w[1][i] += exp2_of(__builtin_fmaf(z1[i], ks[2 + (i >> 3)], -total));
+        }
     }
 #pragma unroll
     for (int s = 0; s < 2; s++)
