@@ -107,6 +107,21 @@ __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2
 __device__ __forceinline__ float log2_of(float x) { return __builtin_amdgcn_logf(x); }
 constexpr float kLn2 = 0.693147180559945309417f;
 
+template <int N> struct Int {
+    static constexpr int value = N;
+};
+
+// Sums over lanes that differ in one bit of their number: of the 2 N values each lane goes on with the sums of N, the upper half of
+// them where its bit is set.
+template <int BIT, int N> __device__ __forceinline__ void halve(float *x, int lane)
+{
+#pragma unroll
+    for (int e = 0; e < N; e++) {
+        const float low = x[e], high = x[e + N], other = __shfl_xor(lane & BIT ? low : high, BIT);
+        x[e] = (lane & BIT ? high : low) + other;
+    }
+}
+
 // Scores may rise this far (as powers of two) above the maximum that p is taken against before everything is taken against
 // a new one: p stays below 2^8, which costs no precision, and the rescaling becomes rare.
 constexpr float kSlack = 8.0f;

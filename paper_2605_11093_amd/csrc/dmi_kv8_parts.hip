@@ -616,20 +616,21 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
         }
     }
 #pragma unroll
-    for (int s = 0; s < 2; s++)
-#pragma unroll
-        for (int i = 0; i < 16; i++) {
-            float x = w[s][i];
-#pragma unroll
-            for (int k = 1; k < 32; k <<= 1) x += __shfl_xor(x, k);
-            const int t = t0 + 32 * s + 8 * (i >> 2) + 4 * half + (i & 3);
-            if (__builtin_amdgcn_readlane(l.entry, 2 * s + (i >> 3)) < 0) x = 0.0f;
-            if (col == i && t < q.len) {
-                if (a.prior.data && t < older)
-                    x += a.decay * a.prior.data[(int64_t)q.row * a.prior.row_stride + (int64_t)head * a.prior.head_stride + t];
-                a.w.data[(int64_t)q.row * a.w.row_stride + (int64_t)head * a.w.head_stride + t] = x;
-            }
+    for (int s = 0; s < 2; s++) {
+        halve<16, 8>(w[s], col);
+        halve<8, 4>(w[s], col);
+        halve<4, 2>(w[s], col);
+        halve<2, 1>(w[s], col);
+        float x = w[s][0] + __shfl_xor(w[s][0], 1);
+        const int i = col >> 1, t = t0 + 32 * s + 8 * (i >> 2) + 4 * half + (i & 3);
+        const int e0 = __builtin_amdgcn_readlane(l.entry, 2 * s), e1 = __builtin_amdgcn_readlane(l.entry, 2 * s + 1);
+        if ((i >> 3 ? e1 : e0) < 0) x = 0.0f;
+        if (!(col & 1) && t < q.len) {
+            if (a.prior.data && t < older)
+                x += a.decay * a.prior.data[(int64_t)q.row * a.prior.row_stride + (int64_t)head * a.prior.head_stride + t];
+            a.w.data[(int64_t)q.row * a.w.row_stride + (int64_t)head * a.w.head_stride + t] = x;
         }
+    }
 }
 
 template <typename T, int DP, int NW> static hipError_t parts(const AttendArgs &a, const PartsPlan &p, hipStream_t s)

@@ -64,10 +64,6 @@ __device__ __forceinline__ int64_t part_at(const AttendArgs &a, const TokensPlan
 // (column c, group g) holds tokens 4g..4g+3 of each of two sixteens of tokens, and which token stands at which place of the
 // product's inner dimension is free as long as V agrees.  V is read with 8 tokens x 8 elements a lane (128 elements), its bytes
 // interleaved by twos and converted: column m of V^T is element 8m + j for instruction j.  Nothing passes through LDS.
-template <int N> struct Int {
-    static constexpr int value = N;
-};
-
 constexpr int waves_of(int dp, int nt, bool whole) { return !whole || dp * nt > 128 ? 4 : 8; }
 
 template <typename T, int DP, int NT, bool WHOLE>
@@ -505,18 +501,10 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
                     for (int n = 0; n < NT; n++) sum[e] += 16 * n + col < rows && total[n] != -INFINITY ? exp2_of(z[n][e / 4][e % 4] - total[n]) : 0.0f;
                 }
                 // over the columns: of two lanes each goes on with half of the tokens
-                auto halve = [&](auto k_) {
-                    constexpr int k = decltype(k_)::value;
-#pragma unroll
-                    for (int e = 0; e < 2 * k; e++) {
-                        const float low = sum[e], high = sum[e + 2 * k], other = __shfl_xor(col & k ? low : high, k);
-                        sum[e] = (col & k ? high : low) + other;
-                    }
-                };
-                halve(Int<8>{});
-                halve(Int<4>{});
-                halve(Int<2>{});
-                halve(Int<1>{});
+                halve<8, 16>(sum, col);
+                halve<4, 8>(sum, col);
+                halve<2, 4>(sum, col);
+                halve<1, 2>(sum, col);
                 const int t = t0 + 8 * (col & ~1) + 4 * g + 2 * (col & 1);
 #pragma unroll
                 for (int i = 0; i < 2; i++)
