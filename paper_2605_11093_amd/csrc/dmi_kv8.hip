@@ -150,13 +150,20 @@ AttendPlan plan_attend(uint32_t block_heads, uint32_t dim, const dmi_kv8_batch_t
     const uint32_t per = block_heads * t.row_tiles;
     const uint64_t tiles = (uint64_t)b.n_reqs * std::max(1u, (b.max_len + 31u) / 32u);
     t.ranges = (uint32_t)std::min<uint64_t>(std::max(kResident / per, 1u), std::max<uint64_t>(b.n_reqs, (tiles + 1u) / 2u));
-    // Short contexts: one workgroup each and head, joined in LDS, and no second launch.  Measured (us, ranges / whole): one request
-    // of 1024 tokens 17 / 12.5, of 2048 17 / 20; 32 requests of 512-1024 24 / 17; 128 of them 49 / 55, of 128-256 28 / 29; with
-    // 32 rows a head instead of 4, 8 requests of 1024-2048 38 / 25.
-    t.whole = t.row_tiles == 1u && b.max_len <= (shared > 16u ? 2048u : (uint64_t)b.n_reqs * block_heads <= 512u ? 1024u : 256u);
-    t.join_blocks = t.ranges > 1u && !t.whole ? (uint32_t)(((uint64_t)b.max_new * q_heads + 3u) / 4u) : 0u;
+    // Few or short contexts: one workgroup each and head, joined in LDS, and no second launch; longer ones in equal splits, of 512 tokens
+    // while there are compute units for them.  Measured (us, ranges / whole): one request of 1024 tokens 17 / 12.5 (in two splits 17), of
+    // 8000 34 / 17, of 32000 65 / 28; 8 of 2000-4000 28 / 23, of 4000-8000 36 / 34; 32 of 512-1024 24 / 17; 128 of them 49 / 55, of 128-256
+    // 28 / 29; with 32 rows a head instead of 4, one of 8000 49 / 21, 128 of 768-1536 132 / 90.
+    const uint64_t units = (uint64_t)b.n_reqs * block_heads;
+    const uint32_t reach = shared > 16u ? 2048u : 1024u;       // tokens of a workgroup
+    t.splits = 1;
+    if (b.max_len > 1024u) t.splits = std::max(1u, (uint32_t)std::min<uint64_t>(256u / std::max<uint64_t>(units, 1u), (b.max_len + 511u) / 512u));
+    if (b.max_len > reach * t.splits) t.splits = (b.max_len + reach - 1u) / reach;
+    t.whole = t.row_tiles == 1u && (units * t.splits <= 512u || (t.splits == 1u && (shared > 16u || b.max_len <= 256u)));
+    t.join_blocks = t.whole ? t.splits > 1u : t.ranges > 1u;
+    if (t.join_blocks) t.join_blocks = (uint32_t)(((uint64_t)b.max_new * q_heads + 3u) / 4u);
     t.score_stride = (b.max_len + 31u) & ~31u;
-    const uint64_t parts = t.join_blocks ? 2ull * t.ranges * per * t.tile_rows : 0u;
+    const uint64_t parts = !t.join_blocks ? 0u : t.whole ? rows * t.splits : 2ull * t.ranges * per * t.tile_rows;
     p.totals = weight ? pad64(rows * t.score_stride * 4u) : 0u;
     p.sums = p.totals + (weight && !t.whole ? pad64(rows * 4u) : 0u);
     p.parts = p.sums + pad64(parts * 8u);

@@ -67,7 +67,8 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 // How few query rows are attended to: see dmi_kv8_tokens.hip.
 struct TokensPlan {
-    bool whole;                                 // a workgroup takes a request and head: no ranges
+    bool whole;                                 // a workgroup takes a request and head, or one of its equal splits: no ranges
+    uint32_t splits;
     uint32_t ranges;                            // equal parts of all contexts
     uint32_t tile_rows, row_tiles;              // query rows of a wavefront; wavefronts for the rows that share a head
     uint32_t join_blocks;                       // workgroups of the second launch that join parts, 0 if there can be none

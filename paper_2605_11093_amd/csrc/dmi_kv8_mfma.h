@@ -28,10 +28,6 @@ struct Bf16 {
         const f32x2 v = {a, b};
         return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
     }
-    static __device__ __forceinline__ uint32_t scaled(uint32_t w, float f)
-    {
-        return pack(__uint_as_float(w << 16) * f, __uint_as_float(w & 0xFFFF0000u) * f);
-    }
     static __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c)
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
@@ -54,11 +50,6 @@ struct Fp16 {
     {
         const f32x2 v = {a, b};
         return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2));
-    }
-    static __device__ __forceinline__ uint32_t scaled(uint32_t w, float f)
-    {
-        const f16x2 h = __builtin_bit_cast(f16x2, w);
-        return pack((float)h[0] * f, (float)h[1] * f);
     }
     static __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c)
     {

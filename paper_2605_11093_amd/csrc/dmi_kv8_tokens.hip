@@ -51,9 +51,10 @@ __device__ __forceinline__ int all_tiles(const AttendArgs &a)
     return total;
 }
 
-// Index of a query row's part
-__device__ __forceinline__ int64_t part_at(const AttendArgs &a, const TokensPlan &p, int range, int place, uint32_t head, uint32_t row)
+// Index of a query row's part; `at`: the row of out, where contexts are split evenly
+__device__ __forceinline__ int64_t part_at(const AttendArgs &a, const TokensPlan &p, int range, int place, uint32_t head, uint32_t row, int64_t at)
 {
+    if (p.whole) return at * p.splits + range;
     const uint32_t tile = row / p.tile_rows;
     return (((int64_t)range * 2 + place) * p.row_tiles * a.c.heads + tile * a.c.heads + head) * p.tile_rows + (row - tile * p.tile_rows);
 }
@@ -82,12 +83,15 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
     int r = 0, seg0 = 0, range = 0, first, last;        // seg0: the request's first tile; first, last: the range's tiles
     Request held{0, 0, 0, 0};                           // of this lane, where there are no more than lanes
     if constexpr (WHOLE) {
-        r = (int)(blockIdx.x / a.c.heads);
-        head = blockIdx.x % a.c.heads;
+        const uint32_t pair = blockIdx.x / p.splits;
+        range = (int)(blockIdx.x - pair * p.splits);
+        r = (int)(pair / a.c.heads);
+        head = pair % a.c.heads;
         const Request q = request_of(a.b, a.c, r);
         const int tiles = q.fresh > 0 ? tiles_of(q) : a.w.data ? (q.len + 31) >> 5 : 0;
-        first = tiles * wave / NW;
-        last = tiles * (wave + 1) / NW;
+        const int nth = range * NW + wave, of = (int)p.splits * NW;
+        first = (int)((int64_t)tiles * nth / of);
+        last = (int)((int64_t)tiles * (nth + 1) / of);
     } else {
         // Workgroups go to the eight XCDs in turn: the heads (and row tiles) of a range follow each other on one of them.
         const uint32_t unit = (blockIdx.x >> 3) * 4u + (uint32_t)wave, per = a.c.heads * p.row_tiles;
@@ -464,6 +468,17 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
                 float l_all;
                 const float total = total_of(row, l_all), f = total == -INFINITY && l_all == 0.0f ? 0.0f : 1.0f / l_all;
                 const QueryRow w = query_row(a, head, (uint32_t)row);
+                if (p.splits > 1u) {
+                    const int64_t part = ((int64_t)(q.start + w.token) * a.q_heads + w.head) * p.splits + range;
+                    if (g == 0 && j == 0) p.sums[part] = f32x2{top_of(row), l_all};
+                    float *dst = p.parts + part * a.c.dim;
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        const int d = NJ * (4 * g + i) + j;
+                        if (d < (int)a.c.dim) *reinterpret_cast<f32x4 *>(dst + d) = f32x4{sum[0][i], sum[1][i], sum[2][i], sum[3][i]};
+                    }
+                    continue;
+                }
                 uint16_t *dst = static_cast<uint16_t *>(a.out.data) + (int64_t)(q.start + w.token) * a.out.row_stride + (int64_t)w.head * a.out.head_stride;
 #pragma unroll
                 for (int i = 0; i < 4; i++) {
@@ -473,7 +488,7 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
                 }
                 if (a.lse && g == 0 && j == 0) a.lse[(int64_t)(q.start + w.token) * a.q_heads + w.head] = total * kLn2;
             }
-            if (!a.w.data) return;
+            if (!a.w.data || p.splits > 1u) return;
             // weights, out of the scores that the same lane wrote
             float total[NT], unused;
 #pragma unroll
@@ -540,7 +555,7 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
                     if (p.totals) p.totals[at] = sum;
                 }
             } else {
-                const int64_t part = part_at(a, p, range, seg_first >= first, head, (uint32_t)row);
+                const int64_t part = part_at(a, p, range, seg_first >= first, head, (uint32_t)row, at);
                 if (g == 0) p.sums[part] = f32x2{m[n], l[n]};
                 float *dst = p.parts + part * a.c.dim;
 #pragma unroll
@@ -563,6 +578,7 @@ struct Spread {
 };
 __device__ __forceinline__ Spread spread_of(const AttendArgs &a, const TokensPlan &p, uint32_t r)
 {
+    if (p.whole) return {0, (int)p.splits - 1};
     int total = 0, before = 0, own = 0;
     for (uint32_t n0 = 0; n0 < a.b.n_reqs; n0 += 64u) {
         const int tiles = lane_tiles(a, n0), upto = lanes_scan(tiles);
@@ -577,12 +593,12 @@ __device__ __forceinline__ Spread spread_of(const AttendArgs &a, const TokensPla
 }
 
 // log2 of the sum of 2^score over all of a row's context; every lane of the wavefront gets it
-__device__ __forceinline__ float total_of(const AttendArgs &a, const TokensPlan &p, const Spread &s, uint32_t head, uint32_t row)
+__device__ __forceinline__ float total_of(const AttendArgs &a, const TokensPlan &p, const Spread &s, uint32_t head, uint32_t row, int64_t at)
 {
     const int lane = threadIdx.x & 63;
     float m = -INFINITY, l = 0.0f;
     for (int i = s.from + lane; i <= s.to; i += 64) {
-        const f32x2 x = p.sums[part_at(a, p, i, i == s.from, head, row)];
+        const f32x2 x = p.sums[part_at(a, p, i, i == s.from, head, row, at)];
         const float top = fmaxf(m, x[0]), to = top == -INFINITY ? 0.0f : top;
         l = l * exp2_of(m - to) + x[1] * exp2_of(x[0] - to);
         m = top;
@@ -611,8 +627,9 @@ __global__ __launch_bounds__(256) void finish_kernel(AttendArgs a, TokensPlan p)
         const Spread s = spread_of(a, p, blockIdx.y);
         if (n >= rows * a.c.heads || s.from == s.to) return;
         const uint32_t head = n / rows, row = n - head * rows;
-        const float total = total_of(a, p, s, head, row);
         const QueryRow w = query_row(a, head, row);
+        const int64_t at = (int64_t)(q.start + w.token) * a.q_heads + w.head;
+        const float total = total_of(a, p, s, head, row, at);
         // as many parts at a time as there are lanes for
         const int wide = (int)a.c.dim / 4, teams = 64 / wide, team = lane / wide, d = 4 * (lane - team * wide);
         f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -622,7 +639,7 @@ __global__ __launch_bounds__(256) void finish_kernel(AttendArgs a, TokensPlan p)
 #pragma unroll
             for (int k = 0; k < 8; k++) {
                 const int i = i0 + k * teams + team;
-                const int64_t part = part_at(a, p, min(i, s.to), min(i, s.to) == s.from, head, row);
+                const int64_t part = part_at(a, p, min(i, s.to), min(i, s.to) == s.from, head, row, at);
                 x[k] = *reinterpret_cast<const f32x4 *>(p.parts + part * a.c.dim + d);
                 f[k] = p.sums[part][0];
             }
@@ -642,7 +659,7 @@ __global__ __launch_bounds__(256) void finish_kernel(AttendArgs a, TokensPlan p)
             uint16_t *dst = static_cast<uint16_t *>(a.out.data) + (int64_t)(q.start + w.token) * a.out.row_stride + (int64_t)w.head * a.out.head_stride + d;
             *reinterpret_cast<u32x2 *>(dst) = u32x2{T::pack(sum[0], sum[1]), T::pack(sum[2], sum[3])};
         }
-        if (a.lse && !lane) a.lse[(int64_t)(q.start + w.token) * a.q_heads + w.head] = total * kLn2;
+        if (a.lse && !lane) a.lse[at] = total * kLn2;
         return;
     }
     const uint32_t rest = blockIdx.x - p.join_blocks, head = rest % a.c.heads;
@@ -655,7 +672,8 @@ __global__ __launch_bounds__(256) void finish_kernel(AttendArgs a, TokensPlan p)
         if (r0) __syncthreads();
         for (int r = r0 + wave; r < r1; r += 4) {
             const QueryRow w = query_row(a, head, (uint32_t)r);
-            const float total = s.from == s.to ? p.totals[(int64_t)(q.start + w.token) * a.q_heads + w.head] : total_of(a, p, s, head, (uint32_t)r);
+            const int64_t at = (int64_t)(q.start + w.token) * a.q_heads + w.head;
+            const float total = s.from == s.to ? p.totals[at] : total_of(a, p, s, head, (uint32_t)r, at);
             if (!lane) totals[r - r0] = total;
         }
         __syncthreads();
@@ -682,7 +700,7 @@ template <typename T> static hipError_t tokens(const AttendArgs &a, const Tokens
     const int dp = a.c.dim <= 64 ? 64 : a.c.dim <= 128 ? 128 : 256;
     auto launch = [&](auto dp_, auto nt_) {
         constexpr int DP = decltype(dp_)::value, NT = decltype(nt_)::value;
-        if (p.whole) tokens_kernel<T, DP, NT, true><<<a.b.n_reqs * a.c.heads, 64 * waves_of(DP, NT, true), 0, s>>>(a, p);
+        if (p.whole) tokens_kernel<T, DP, NT, true><<<a.b.n_reqs * a.c.heads * p.splits, 64 * waves_of(DP, NT, true), 0, s>>>(a, p);
         else tokens_kernel<T, DP, NT, false><<<(units + 3u) / 4u * 8u, 256, 0, s>>>(a, p);
     };
     if (p.tile_rows == 16) {
@@ -693,7 +711,7 @@ template <typename T> static hipError_t tokens(const AttendArgs &a, const Tokens
         if (dp == 64) launch(Int<64>{}, Int<2>{});
         else launch(Int<128>{}, Int<2>{});
     }
-    if (p.whole) return hipGetLastError();
+    if (p.whole && p.splits == 1u) return hipGetLastError();
     hipError_t e = hipGetLastError();
     const uint32_t weight_blocks = a.w.data ? (a.b.max_len + 1023u) / 1024u * a.c.heads : 0u;
     if (e != hipSuccess || p.join_blocks + weight_blocks == 0) return e;
