@@ -342,8 +342,8 @@ __global__ __launch_bounds__(256) void move_kernel(EvictArgs a, uint32_t blocks,
                                                    (int64_t)head * a.to.head_stride + part : -1;
                 wk[j] = wv[j] = u32x4{0u, 0u, 0u, 0u};
                 if (dst[j] >= 0 && src >= 0) {
-                    wk[j] = *reinterpret_cast<const u32x4 *>(a.c.code[0] + src + part);
-                    wv[j] = *reinterpret_cast<const u32x4 *>(a.c.code[1] + src + part);
+                    wk[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(a.c.code[0] + src + part));
+                    wv[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(a.c.code[1] + src + part));
                 }
             }
 #pragma unroll
@@ -357,8 +357,8 @@ __global__ __launch_bounds__(256) void move_kernel(EvictArgs a, uint32_t blocks,
 #pragma unroll
                     for (int i = 0; i < 4; i++) wv[j][i] = scaled_codes(wv[j][i], gv[j]);
                 }
-                *reinterpret_cast<u32x4 *>(a.to.code[0] + dst[j]) = wk[j];
-                *reinterpret_cast<u32x4 *>(a.to.code[1] + dst[j]) = wv[j];
+                __builtin_nontemporal_store(wk[j], reinterpret_cast<u32x4 *>(a.to.code[0] + dst[j]));
+                __builtin_nontemporal_store(wv[j], reinterpret_cast<u32x4 *>(a.to.code[1] + dst[j]));
             }
         }
     }
