@@ -16,7 +16,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 // Matrix instructions take bf16 or f16 as q comes; an e4m3 number is one of either exactly.
 struct Bf16 {
     static constexpr bool kNarrow = false;      // as wide a range of exponents as fp32
-    static constexpr uint32_t kOne = 0x3F80u, kInf = 0x7F80u;
+    static constexpr uint32_t kOne = 0x3F80u;
     // two neighbouring codes of a word
     static __device__ __forceinline__ uint32_t two_codes(uint32_t w, bool hi)
     {
@@ -40,7 +40,7 @@ struct Bf16 {
 
 struct Fp16 {
     static constexpr bool kNarrow = true;
-    static constexpr uint32_t kOne = 0x3C00u, kInf = 0x7C00u;
+    static constexpr uint32_t kOne = 0x3C00u;
     static __device__ __forceinline__ uint32_t two_codes(uint32_t w, bool hi)
     {
         return __builtin_bit_cast(uint32_t, hi ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, true)

@@ -31,8 +31,15 @@ __device__ __forceinline__ float lane_value(float v, int lane) { return __int_as
 // As in tokens_kernel, S^T = K Q^T and O^T = V^T P^T with query rows as columns, here with 32x32x16 instructions, 32 query rows a
 // wavefront, NW wavefronts on the same tokens.  K and V are converted once for the workgroup, on their way into LDS: K as it
 // lies, V transposed, the tokens of a sixteen in the order in which the lanes' registers of S^T hold them (0-3, 8-11 for lanes
-// 0-31, 4-7, 12-15 for lanes 32-63), so that an operand is 16 bytes in a row.
+// 0-31, 4-7, 12-15 for lanes 32-63), so that an operand is 16 bytes in a row.  Both have two places in LDS: one tile is staged while
+// the other is used, with one barrier a tile.
 //
+// Bound by neither pipe alone: a tile takes a wavefront 32 matrix instructions (1280 cycles) and some 280 vector ones (1500), 112 of
+// them to stage, and the two wavefronts of a SIMD together 6000 cycles: they leave the barrier together and so want the same pipe
+// at the same time.  32 ragged prompts of 128-2048 tokens, 32 query heads over 8: 620 us, 725 TFLOP/s (a large product of the library:
+// 1250); parts of four long prompts 229 us, 770 TFLOP/s.  Measured and not better: one wavefront of 64 rows a SIMD (spills), the second
+// four wavefronts half a tile behind the first (658 us), staging between the instructions of a product (627-671), two workgroups
+// of four wavefronts (634), priorities (624-639), a maximum looked for only where sums grow (637-700).
 template <typename T, int DP, int NW>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW / 4)))
 void parts_kernel(AttendArgs a, PartsPlan p)
@@ -397,7 +404,8 @@ void parts_kernel(AttendArgs a, PartsPlan p)
     }
 }
 
-// Outputs out of the parts that splits of the contexts left: a row by as many lanes as take four elements each of it.
+// Outputs out of the parts that splits of the contexts left: a row by as many lanes as take four elements each of it, in one pass with
+// the running maximum.  Bound by memory and its latency: 48000 rows of 128 elements out of three parts, 86 MB, 24 us.
 template <typename T>
 __global__ __launch_bounds__(256) void join_parts_kernel(AttendArgs a, PartsPlan p, uint32_t tile_rows)
 {
@@ -434,8 +442,6 @@ __global__ __launch_bounds__(256) void join_parts_kernel(AttendArgs a, PartsPlan
     }
 }
 
-// Weights: 256 tokens a workgroup, 64 a wavefront, whose K stays in registers; the query rows that see them pass through LDS 64 at
-// a time (32 of 256 elements).  Scores once more (their rows' totals were not known before), p summed over the rows in fp32, in order.
 // A product's N matrix instructions and 48 vector ones in turn
 template <int N> __device__ __forceinline__ void interleave()
 {
@@ -447,6 +453,12 @@ template <int N> __device__ __forceinline__ void interleave()
     }
 }
 
+// Weights: 256 tokens a workgroup, 64 a wavefront, whose K stays in registers; the query rows that see them pass through LDS 64 at
+// a time (32 of 256 elements).  Scores once more (their rows' totals were not known before), p summed over the rows in fp32, in an
+// order that timing does not change.  A row of queries is a column of the product: a lane adds up its column's rows in turn, and lanes
+// are joined once at the end.  Half of attention's operations, and an exp2 for each score: bound by the vector instructions (three a
+// score, exp2 at half rate) that run between the matrix ones: four long prompts' parts, 343 million scores, 88 GFLOP in 106 us (172 us
+// with 32 rows a step and nothing read ahead, 130 with the two one after the other, 121 with 160 lane exchanges at the end).
 template <typename T, int DP>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ? 2 : 1))) void weights_kernel(AttendArgs a, PartsPlan p)
 {
