@@ -57,9 +57,9 @@ __device__ __forceinline__ int all_tiles(const AttendArgs &a)
 }
 
 // Index of a query row's part; `at`: the row of out, where contexts are split evenly
-__device__ __forceinline__ int64_t part_at(const AttendArgs &a, const TokensPlan &p, int range, int place, uint32_t head, uint32_t row, int64_t at)
+template <bool WHOLE> __device__ __forceinline__ int64_t part_at(const AttendArgs &a, const TokensPlan &p, int range, int place, uint32_t head, uint32_t row, int64_t at)
 {
-    if (p.whole) return at * p.splits + range;
+    if constexpr (WHOLE) return at * p.splits + range;
     const uint32_t tile = row / p.tile_rows;
     return (((int64_t)range * 2 + place) * p.row_tiles * a.c.heads + tile * a.c.heads + head) * p.tile_rows + (row - tile * p.tile_rows);
 }
@@ -566,7 +566,7 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
                     if (p.totals) p.totals[at] = sum;
                 }
             } else {
-                const int64_t part = part_at(a, p, range, seg_first >= first, head, (uint32_t)row, at);
+                const int64_t part = part_at<WHOLE>(a, p, range, seg_first >= first, head, (uint32_t)row, at);
                 if (g == 0) p.sums[part] = f32x2{m[n], l[n]};
                 float *dst = p.parts + part * a.c.dim;
 #pragma unroll
@@ -587,9 +587,9 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
 struct Spread {
     int from, to;
 };
-__device__ __forceinline__ Spread spread_of(const AttendArgs &a, const TokensPlan &p, uint32_t r)
+template <bool WHOLE> __device__ __forceinline__ Spread spread_of(const AttendArgs &a, const TokensPlan &p, uint32_t r)
 {
-    if (p.whole) return {0, (int)p.splits - 1};
+    if constexpr (WHOLE) return {0, (int)p.splits - 1};
     int total = 0, before = 0, own = 0;
     for (uint32_t n0 = 0; n0 < a.b.n_reqs; n0 += 64u) {
         const int tiles = lane_tiles(a, n0), upto = lanes_scan(tiles);
@@ -604,12 +604,12 @@ __device__ __forceinline__ Spread spread_of(const AttendArgs &a, const TokensPla
 }
 
 // log2 of the sum of 2^score over all of a row's context; every lane of the wavefront gets it
-__device__ __forceinline__ float total_of(const AttendArgs &a, const TokensPlan &p, const Spread &s, uint32_t head, uint32_t row, int64_t at)
+template <bool WHOLE> __device__ __forceinline__ float total_of(const AttendArgs &a, const TokensPlan &p, const Spread &s, uint32_t head, uint32_t row, int64_t at)
 {
     const int lane = threadIdx.x & 63;
     float m = -INFINITY, l = 0.0f;
     for (int i = s.from + lane; i <= s.to; i += 64) {
-        const f32x2 x = p.sums[part_at(a, p, i, i == s.from, head, row, at)];
+        const f32x2 x = p.sums[part_at<WHOLE>(a, p, i, i == s.from, head, row, at)];
         const float top = fmaxf(m, x[0]), to = top == -INFINITY ? 0.0f : top;
         l = l * exp2_of(m - to) + x[1] * exp2_of(x[0] - to);
         m = top;
@@ -626,8 +626,9 @@ __device__ __forceinline__ float total_of(const AttendArgs &a, const TokensPlan 
 
 // The first p.join_blocks workgroups of a request: outputs out of parts, a wavefront a row, eight parts a team of lanes at once.  The
 // others: weights out of the scores, four tokens a thread; query rows are added in order, so no result depends on timing.  Bound by
-// loads that wait for each other: 8 us behind the 181 above; 16 contexts of up to 8192 tokens with weights 8 to 10 us behind 32.
-template <typename T>
+// loads that wait for each other: 8 us behind the 181 above; 16 contexts of up to 8192 tokens with weights 8 us
+// behind 32 (what waits for no total is read first; 10 with one variant for both layouts of parts).
+template <typename T, bool WHOLE>
 __global__ __launch_bounds__(256) void finish_kernel(AttendArgs a, TokensPlan p)
 {
     __shared__ float totals[256];
@@ -636,12 +637,12 @@ __global__ __launch_bounds__(256) void finish_kernel(AttendArgs a, TokensPlan p)
     const uint32_t rows = (uint32_t)q.fresh * a.group;
     if (blockIdx.x < p.join_blocks) {
         const uint32_t n = blockIdx.x * 4u + (uint32_t)wave;
-        const Spread s = spread_of(a, p, blockIdx.y);
+        const Spread s = spread_of<WHOLE>(a, p, blockIdx.y);
         if (n >= rows * a.c.heads || s.from == s.to) return;
         const uint32_t head = n / rows, row = n - head * rows;
         const QueryRow w = query_row(a, head, row);
         const int64_t at = (int64_t)(q.start + w.token) * a.q_heads + w.head;
-        const float total = total_of(a, p, s, head, row, at);
+        const float total = total_of<WHOLE>(a, p, s, head, row, at);
         // as many parts at a time as there are lanes for
         const int wide = (int)a.c.dim / 4, teams = 64 / wide, team = lane / wide, d = 4 * (lane - team * wide);
         f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -651,7 +652,7 @@ __global__ __launch_bounds__(256) void finish_kernel(AttendArgs a, TokensPlan p)
 #pragma unroll
             for (int k = 0; k < 8; k++) {
                 const int i = i0 + k * teams + team;
-                const int64_t part = part_at(a, p, min(i, s.to), min(i, s.to) == s.from, head, row, at);
+                const int64_t part = part_at<WHOLE>(a, p, min(i, s.to), min(i, s.to) == s.from, head, row, at);
                 x[k] = *reinterpret_cast<const f32x4 *>(p.parts + part * a.c.dim + d);
                 f[k] = p.sums[part][0];
             }
@@ -677,7 +678,20 @@ __global__ __launch_bounds__(256) void finish_kernel(AttendArgs a, TokensPlan p)
     const uint32_t rest = blockIdx.x - p.join_blocks, head = rest % a.c.heads;
     const int t0 = 1024 * (int)(rest / a.c.heads), t = t0 + 4 * (int)threadIdx.x, older = q.len - q.fresh;
     if (t0 >= q.len) return;
-    const Spread s = spread_of(a, p, blockIdx.y);
+    // what waits for no total: prior weights, and the first rows' scores
+    constexpr int kFirst = 4;
+    const float *scores = p.scores + ((int64_t)head * a.b.total_new * a.group + (int64_t)q.start * a.group) * p.score_stride + (t < q.len ? t : 0);
+    const float *prior = a.prior.data + (int64_t)q.row * a.prior.row_stride + (int64_t)head * a.prior.head_stride;
+    f32x4 z[kFirst], before = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (rows) {
+#pragma unroll
+        for (int r = 0; r < kFirst; r++) z[r] = *reinterpret_cast<const f32x4 *>(scores + (int64_t)min(r, (int)rows - 1) * p.score_stride);
+    }
+    if (a.prior.data) {
+#pragma unroll
+        for (int i = 0; i < 4; i++) before[i] = prior[max(min(t + i, older - 1), 0)];
+    }
+    const Spread s = spread_of<WHOLE>(a, p, blockIdx.y);
     f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int r0 = 0; r0 < (int)rows; r0 += 256) {
         const int r1 = min((int)rows, r0 + 256);
@@ -685,25 +699,29 @@ __global__ __launch_bounds__(256) void finish_kernel(AttendArgs a, TokensPlan p)
         for (int r = r0 + wave; r < r1; r += 4) {
             const QueryRow w = query_row(a, head, (uint32_t)r);
             const int64_t at = (int64_t)(q.start + w.token) * a.q_heads + w.head;
-            const float total = s.from == s.to ? p.totals[at] : total_of(a, p, s, head, (uint32_t)r, at);
+            const float total = s.from == s.to ? p.totals[at] : total_of<WHOLE>(a, p, s, head, (uint32_t)r, at);
             if (!lane) totals[r - r0] = total;
         }
         __syncthreads();
-        if (t < q.len)
-            for (int r = r0; r < r1; r++) {
-                const float total = totals[r - r0];
-                if (total == -INFINITY) continue;
-                const f32x4 z = *reinterpret_cast<const f32x4 *>(
-                    p.scores + ((int64_t)head * a.b.total_new * a.group + (int64_t)q.start * a.group + r) * p.score_stride + t);
+        auto add = [&](int r, const f32x4 &x) {
+            const float total = totals[r - r0];
 #pragma unroll
-                for (int i = 0; i < 4; i++) sum[i] += exp2_of(z[i] - total);
-            }
+            for (int i = 0; i < 4; i++) sum[i] += total == -INFINITY ? 0.0f : exp2_of(x[i] - total);
+        };
+        if (!r0) {
+#pragma unroll
+            for (int r = 0; r < kFirst; r++)
+                if (r < r1) add(r, z[r]);
+        }
+        if (t < q.len) {
+#pragma unroll 4
+            for (int r = r0 ? r0 : kFirst; r < r1; r++) add(r, *reinterpret_cast<const f32x4 *>(scores + (int64_t)r * p.score_stride));
+        }
     }
-    const float *prior = a.prior.data + (int64_t)q.row * a.prior.row_stride + (int64_t)head * a.prior.head_stride;
     float *to = a.w.data + (int64_t)q.row * a.w.row_stride + (int64_t)head * a.w.head_stride;
 #pragma unroll
     for (int i = 0; i < 4; i++)
-        if (t + i < q.len) to[t + i] = a.prior.data && t + i < older ? a.decay * prior[t + i] + sum[i] : sum[i];
+        if (t + i < q.len) to[t + i] = a.prior.data && t + i < older ? a.decay * before[i] + sum[i] : sum[i];
 }
 
 template <typename T> static hipError_t tokens(const AttendArgs &a, const TokensPlan &p, hipStream_t s)
@@ -727,7 +745,9 @@ template <typename T> static hipError_t tokens(const AttendArgs &a, const Tokens
     hipError_t e = hipGetLastError();
     const uint32_t weight_blocks = a.w.data ? (a.b.max_len + 1023u) / 1024u * a.c.heads : 0u;
     if (e != hipSuccess || p.join_blocks + weight_blocks == 0) return e;
-    finish_kernel<T><<<dim3(p.join_blocks + weight_blocks, a.b.n_reqs), 256, 0, s>>>(a, p);
+    const dim3 finish(p.join_blocks + weight_blocks, a.b.n_reqs);
+    if (p.whole) finish_kernel<T, true><<<finish, 256, 0, s>>>(a, p);
+    else finish_kernel<T, false><<<finish, 256, 0, s>>>(a, p);
     return hipGetLastError();
 }
 
