@@ -117,16 +117,22 @@ void parts_kernel(AttendArgs a, PartsPlan p)
         uint32_t lo, hi;
         uint64_t there;                         // which of them the cache has
     };
-    // a batch of 16 tiles is looked up, and its scales go into LDS (every wavefront writes the same)
-    auto look = [&](int batch) {
+    // a batch of 16 tiles is looked up, and its scales go into LDS (every wavefront writes the same; what is not there is masked, and
+    // weighs nothing); what is done in between does not wait for the scales
+    auto look = [&](int batch, auto between) {
         const int t = begin + 1024 * batch + 16 * lane;
-        const Look l = look_up(a, q, head, t, end, scale);
-        scales[batch & 1][0][lane] = l.ks;
-        scales[batch & 1][1][lane] = l.lift;
-        scales[batch & 1][2][lane] = l.inv;
-        const int64_t at = (int64_t)max(l.entry, 0) * a.c.block_stride +
-                           (int64_t)((uint32_t)t - block_of(a.c, (uint32_t)t >> 4) * a.c.bs) * a.c.slot_stride + (int64_t)head * a.c.head_stride;
-        return Places{(uint32_t)at, (uint32_t)(at >> 32), __ballot(l.entry >= 0)};
+        const uint32_t block = block_of(a.c, (uint32_t)t >> 4);
+        const int raw = a.c.table[(int64_t)q.row * a.c.table_stride + min(block, a.c.max_blocks - 1u)];
+        const bool there = t < end && block < a.c.max_blocks && (uint32_t)raw < a.c.n_blocks;
+        const int entry = there ? raw : 0;
+        const int64_t at = (int64_t)entry * a.c.block_stride + (int64_t)((uint32_t)t - block * a.c.bs) * a.c.slot_stride + (int64_t)head * a.c.head_stride;
+        const Places l{(uint32_t)at, (uint32_t)(at >> 32), __ballot(there)};
+        const float ks = *scale_at(a.c, 0, entry, head), vs = *scale_at(a.c, 1, entry, head);
+        between(l);
+        scales[batch & 1][0][lane] = there ? ks * scale : 1.0f;
+        scales[batch & 1][1][lane] = there ? log2_of(vs) : -INFINITY;
+        scales[batch & 1][2][lane] = there ? 1.0f / vs : 0.0f;
+        return l;
     };
     auto fetch = [&](int tile, const Places &p, KCodes &k, VCodes &v) {
 #pragma unroll
@@ -254,10 +260,9 @@ void parts_kernel(AttendArgs a, PartsPlan p)
     };
     if (tiles) {
         if (threadIdx.x < 16) nan_tile[threadIdx.x >> 3][threadIdx.x & 7] = nan_any[threadIdx.x & 1] = 0;
-        Places now = look(0), next = now;
         KCodes kc;
         VCodes vc;
-        fetch(0, now, kc, vc);
+        Places now = look(0, [&](const Places &l) { fetch(0, l, kc, vc); }), next = now;
         lds_barrier();                          // (the NaN flags are cleared)
 #pragma unroll
         for (int k = 0; k < KK; k++)
@@ -270,7 +275,7 @@ void parts_kernel(AttendArgs a, PartsPlan p)
         for (int tile = 0; tile < tiles; tile++) {
             const int t0 = begin + kTile * tile;
             if ((tile & 15) == 0 && tile) now = next;
-            if (((tile + 1) & 15) == 0) next = look((tile + 1) >> 4);
+            if (((tile + 1) & 15) == 0) next = look((tile + 1) >> 4, [](const Places &) {});
             fetch(tile + 1, ((tile + 1) & 15) == 0 ? next : now, kc, vc);
             lds_barrier();                      // the tile is in LDS
             if (t0 <= most) {
@@ -372,26 +377,36 @@ void parts_kernel(AttendArgs a, PartsPlan p)
 
     const float v_ref = T::kNarrow ? exp2_of(lift_ref) : 1.0f;
     l += __shfl_xor(l, 32);
-    if (row >= rows) return;
     const int64_t at = (int64_t)(q.start + w.token) * a.q_heads + w.head;
     const bool empty = m == -INFINITY && l == 0.0f;
     if (p.splits == 1) {
+        // Rows are put together in LDS, so that a store writes whole ones: as the lanes hold them it would write 16 bytes here and there.
+        constexpr int kRow = 2 * DP, kChunks = DP / 8, kRows = 64 / kChunks;       // bytes; 16s of them; rows of a store
+        static_assert(NW * 32 * kRow <= 2 * (kTile * KP + DP * VP));
+        uint8_t *const own = lds + wave * 32 * kRow;
         const float f = (empty ? 0.0f : 1.0f / l) * v_ref;
-        uint16_t *dst = static_cast<uint16_t *>(a.out.data) + (int64_t)(q.start + w.token) * a.out.row_stride + (int64_t)w.head * a.out.head_stride;
+        const int64_t dst = (int64_t)(q.start + w.token) * a.out.row_stride + (int64_t)w.head * a.out.head_stride;
+        lds_barrier();                          // (the tiles are done with)
 #pragma unroll
         for (int d = 0; d < ND; d++)
 #pragma unroll
-            for (int i = 0; i < 16; i += 4) {
-                const int e = 32 * d + 2 * i + 4 * half;
-                if (e < (int)a.c.dim)
-                    *reinterpret_cast<u32x2 *>(dst + e) = u32x2{T::pack(o[d][i] * f, o[d][i + 1] * f), T::pack(o[d][i + 2] * f, o[d][i + 3] * f)};
-            }
-        if (half == 0) {
+            for (int i = 0; i < 16; i += 4)
+                *reinterpret_cast<u32x2 *>(own + col * kRow + 16 * ((4 * d + i / 4) ^ (col & (kChunks - 1))) + 8 * half) =
+                    u32x2{T::pack(o[d][i] * f, o[d][i + 1] * f), T::pack(o[d][i + 2] * f, o[d][i + 3] * f)};
+#pragma unroll
+        for (int j = 0; j < 32; j += kRows) {
+            const int r = j + lane / kChunks, chunk = lane % kChunks;
+            const u32x4 x = *reinterpret_cast<const u32x4 *>(own + r * kRow + 16 * (chunk ^ (r & (kChunks - 1))));
+            const int64_t to = (int64_t)(uint32_t)__shfl((int)(uint32_t)dst, r) | (int64_t)__shfl((int)(dst >> 32), r) << 32;
+            if (wave_row + r < rows && 8 * chunk < (int)a.c.dim)
+                *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(a.out.data) + to + 8 * chunk) = x;
+        }
+        if (row < rows && half == 0) {
             const float sum = empty ? -INFINITY : m + log2_of(l);
             if (a.lse) a.lse[at] = sum * kLn2;
             if (p.totals) p.totals[at] = sum;
         }
-    } else {
+    } else if (row < rows) {
         if (half == 0) p.sums[at * p.splits + split] = f32x2{m, l};
         float *dst = p.parts + (at * p.splits + split) * a.c.dim;
 #pragma unroll

@@ -39,3 +39,16 @@ def test_ranges(B, dtype, reqs, heads, group, dim, new, longest, weights):      
 @pytest.mark.parametrize("weights", [True, False])
 def test_splits(B, dtype, spans, heads, group, dim, weights):                       # noqa: F811
     _check_attend(B, Setup(B, 22, spans, heads, dim, 32), dtype, group, weights=weights)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("reqs,heads,dim,new,longest", [
+    (33, 16, 64, 40, 200),              # more tiles of query rows than workgroups, which take them in turn
+    (70, 8, 80, 34, 150),               # more requests than lanes
+    (33, 8, 128, 40, 1100),             # contexts in two splits as well
+], ids=["rows", "many", "splits"])
+def test_tiles_in_turn(B, dtype, reqs, heads, dim, new, longest):                   # noqa: F811
+    r = np.random.default_rng(reqs)
+    spans = [(int(new if i % 7 else 0), int(n)) for i, n in enumerate(r.integers(new, new + 50, reqs), 1)]
+    spans[reqs // 2] = (300, longest + 300)
+    _check_attend(B, Setup(B, 23, spans, heads, dim, 16), dtype, 1)
