@@ -36,10 +36,12 @@ __device__ __forceinline__ float lane_value(float v, int lane) { return __int_as
 //
 // Bound by neither pipe alone: a tile takes a wavefront 32 matrix instructions (1280 cycles) and some 280 vector ones (1500), 112 of
 // them to stage, and the two wavefronts of a SIMD together 6000 cycles: they leave the barrier together and so want the same pipe
-// at the same time.  32 ragged prompts of 128-2048 tokens, 32 query heads over 8: 620 us, 725 TFLOP/s (a large product of the library:
-// 1250); parts of four long prompts 229 us, 770 TFLOP/s.  Measured and not better: one wavefront of 64 rows a SIMD (spills), the second
-// four wavefronts half a tile behind the first (658 us), staging between the instructions of a product (627-671), two workgroups
-// of four wavefronts (634), priorities (624-639), a maximum looked for only where sums grow (637-700).
+// at the same time; a workgroup's start and end cost as much as four tiles of its dozen.  32 ragged prompts of 128-2048 tokens, 32 query
+// heads over 8: 585 us, 766 TFLOP/s (a large product of the library: 1250); parts of four long prompts 222 us, 790 TFLOP/s.  Queries and
+// outputs that went between memory and the lanes without LDS cost 33 us of it.  Measured and not better (before that, at 620): one
+// wavefront of 64 rows a SIMD (spills), the second four wavefronts half a tile behind the first (658), staging between the
+// instructions of a product (627-671), two workgroups of four wavefronts (634), priorities (624-639), a maximum looked for only where
+// sums grow (637-700), two to eight row tiles a workgroup in turn (670-818), workgroups that stay and draw row tiles (642).
 template <typename T, int DP, int NW>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW / 4)))
 void parts_kernel(AttendArgs a, PartsPlan p)
@@ -81,13 +83,23 @@ void parts_kernel(AttendArgs a, PartsPlan p)
     const int wave_row = row0 + wave * 32, row = wave_row + col;
     const QueryRow w = query_row(a, head, (uint32_t)row);
     const int lim = row < rows ? older + w.token : -1;          // the last position that the column's query sees
+    // Read by whole rows, and given to the lanes that take them through LDS (rows of its own for each wavefront; outputs go the same way)
+    constexpr int kRow = 2 * DP, kChunks = DP / 8, kRows = 64 / kChunks;       // bytes; 16s of them; rows of a load
+    static_assert(NW * 32 * kRow <= 2 * (kTile * KP + DP * VP));
+    uint8_t *const own = lds + wave * 32 * kRow;
+    auto in_row = [&](int r, int chunk) { return own + r * kRow + 16 * (chunk ^ (r & (kChunks - 1))); };
     u32x4 qf[KK];
     {
         // (loads that depend on nothing: each in a branch of its own would wait for itself)
         const QueryRow v = query_row(a, head, (uint32_t)min(row, rows - 1));
-        const uint16_t *src = static_cast<const uint16_t *>(a.q.data) + (int64_t)(q.start + v.token) * a.q.row_stride + (int64_t)v.head * a.q.head_stride;
+        const int64_t src = (int64_t)(q.start + v.token) * a.q.row_stride + (int64_t)v.head * a.q.head_stride;
+        const int chunk = lane % kChunks;
 #pragma unroll
-        for (int k = 0; k < KK; k++) qf[k] = *reinterpret_cast<const u32x4 *>(src + (16 * k + 8 * half < (int)a.c.dim ? 16 * k + 8 * half : 0));
+        for (int k = 0; k < KK; k++) {
+            const int r = k * kRows + lane / kChunks;
+            const int64_t from = (int64_t)(uint32_t)__shfl((int)(uint32_t)src, r) | (int64_t)__shfl((int)(src >> 32), r) << 32;
+            qf[k] = *reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(a.q.data) + from + (8 * chunk < (int)a.c.dim ? 8 * chunk : 0));
+        }
     }
     // what the first and the last of them see
     const int least = wave_row + 32 <= rows ? older + wave_row / (int)a.group : -1;
@@ -263,7 +275,11 @@ void parts_kernel(AttendArgs a, PartsPlan p)
         KCodes kc;
         VCodes vc;
         Places now = look(0, [&](const Places &l) { fetch(0, l, kc, vc); }), next = now;
-        lds_barrier();                          // (the NaN flags are cleared)
+#pragma unroll
+        for (int k = 0; k < KK; k++) *reinterpret_cast<u32x4 *>(in_row(k * kRows + lane / kChunks, lane % kChunks)) = qf[k];
+#pragma unroll
+        for (int k = 0; k < KK; k++) qf[k] = *reinterpret_cast<const u32x4 *>(in_row(col, 2 * k + half));
+        lds_barrier();                          // (the NaN flags are cleared, and the rows read)
 #pragma unroll
         for (int k = 0; k < KK; k++)
 #pragma unroll
@@ -381,9 +397,6 @@ void parts_kernel(AttendArgs a, PartsPlan p)
     const bool empty = m == -INFINITY && l == 0.0f;
     if (p.splits == 1) {
         // Rows are put together in LDS, so that a store writes whole ones: as the lanes hold them it would write 16 bytes here and there.
-        constexpr int kRow = 2 * DP, kChunks = DP / 8, kRows = 64 / kChunks;       // bytes; 16s of them; rows of a store
-        static_assert(NW * 32 * kRow <= 2 * (kTile * KP + DP * VP));
-        uint8_t *const own = lds + wave * 32 * kRow;
         const float f = (empty ? 0.0f : 1.0f / l) * v_ref;
         const int64_t dst = (int64_t)(q.start + w.token) * a.out.row_stride + (int64_t)w.head * a.out.head_stride;
         lds_barrier();                          // (the tiles are done with)
@@ -391,12 +404,12 @@ void parts_kernel(AttendArgs a, PartsPlan p)
         for (int d = 0; d < ND; d++)
 #pragma unroll
             for (int i = 0; i < 16; i += 4)
-                *reinterpret_cast<u32x2 *>(own + col * kRow + 16 * ((4 * d + i / 4) ^ (col & (kChunks - 1))) + 8 * half) =
+                *reinterpret_cast<u32x2 *>(in_row(col, 4 * d + i / 4) + 8 * half) =
                     u32x2{T::pack(o[d][i] * f, o[d][i + 1] * f), T::pack(o[d][i + 2] * f, o[d][i + 3] * f)};
 #pragma unroll
         for (int j = 0; j < 32; j += kRows) {
             const int r = j + lane / kChunks, chunk = lane % kChunks;
-            const u32x4 x = *reinterpret_cast<const u32x4 *>(own + r * kRow + 16 * (chunk ^ (r & (kChunks - 1))));
+            const u32x4 x = *reinterpret_cast<const u32x4 *>(in_row(r, chunk));
             const int64_t to = (int64_t)(uint32_t)__shfl((int)(uint32_t)dst, r) | (int64_t)__shfl((int)(dst >> 32), r) << 32;
             if (wave_row + r < rows && 8 * chunk < (int)a.c.dim)
                 *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(a.out.data) + to + 8 * chunk) = x;
@@ -406,16 +419,27 @@ void parts_kernel(AttendArgs a, PartsPlan p)
             if (a.lse) a.lse[at] = sum * kLn2;
             if (p.totals) p.totals[at] = sum;
         }
-    } else if (row < rows) {
-        if (half == 0) p.sums[at * p.splits + split] = f32x2{m, l};
-        float *dst = p.parts + (at * p.splits + split) * a.c.dim;
+    } else {
+        if (row < rows && half == 0) p.sums[at * p.splits + split] = f32x2{m, l};
+        const int64_t part = at * p.splits + split;
+        lds_barrier();                          // (the tiles are done with)
 #pragma unroll
-        for (int d = 0; d < ND; d++)
+        for (int h = 0; h < 2; h++) {           // halves of a row in fp32
 #pragma unroll
-            for (int i = 0; i < 16; i += 4) {
-                const int e = 32 * d + 2 * i + 4 * half;
-                if (e < (int)a.c.dim) *reinterpret_cast<f32x4 *>(dst + e) = f32x4{o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]} * v_ref;
+            for (int d = 0; d < ND / 2; d++)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) {
+                    const f32x16 &x = o[h * (ND / 2) + d];
+                    *reinterpret_cast<f32x4 *>(in_row(col, 8 * d + i / 2 + half)) = f32x4{x[i], x[i + 1], x[i + 2], x[i + 3]} * v_ref;
+                }
+#pragma unroll
+            for (int j = 0; j < 32; j += kRows) {
+                const int r = j + lane / kChunks, e = h * (DP / 2) + 4 * (lane % kChunks);
+                const f32x4 x = *reinterpret_cast<const f32x4 *>(in_row(r, lane % kChunks));
+                const int64_t to = (int64_t)(uint32_t)__shfl((int)(uint32_t)part, r) | (int64_t)__shfl((int)(part >> 32), r) << 32;
+                if (wave_row + r < rows && e < (int)a.c.dim) *reinterpret_cast<f32x4 *>(p.parts + to * a.c.dim + e) = x;
             }
+        }
     }
 }
 

@@ -43,11 +43,11 @@ def test_splits(B, dtype, spans, heads, group, dim, weights):                   
 
 @pytest.mark.parametrize("dtype", [BF16, FP16])
 @pytest.mark.parametrize("reqs,heads,dim,new,longest", [
-    (33, 16, 64, 40, 200),              # more tiles of query rows than workgroups, which take them in turn
+    (33, 16, 64, 40, 200),              # many more workgroups than compute units
     (70, 8, 80, 34, 150),               # more requests than lanes
     (33, 8, 128, 40, 1100),             # contexts in two splits as well
 ], ids=["rows", "many", "splits"])
-def test_tiles_in_turn(B, dtype, reqs, heads, dim, new, longest):                   # noqa: F811
+def test_many_rows(B, dtype, reqs, heads, dim, new, longest):                   # noqa: F811
     r = np.random.default_rng(reqs)
     spans = [(int(new if i % 7 else 0), int(n)) for i, n in enumerate(r.integers(new, new + 50, reqs), 1)]
     spans[reqs // 2] = (300, longest + 300)
