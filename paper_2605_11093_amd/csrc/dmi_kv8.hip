@@ -161,7 +161,7 @@ AttendPlan plan_attend(uint32_t block_heads, uint32_t dim, const dmi_kv8_batch_t
     t.splits = 1;
     if (b.max_len > 1024u) t.splits = std::max(1u, (uint32_t)std::min<uint64_t>(256u / std::max<uint64_t>(units, 1u), (b.max_len + 511u) / 512u));
     if (b.max_len > reach * t.splits) t.splits = (b.max_len + reach - 1u) / reach;
-    t.whole = t.row_tiles == 1u && (units * t.splits <= 512u || (t.splits == 1u && (shared > 16u || b.max_len <= 256u)));
+    t.whole = t.row_tiles == 1u && (units * t.splits <= 512u || (t.splits == 1u && units <= 1u << 22 && (shared > 16u || b.max_len <= 256u)));
     t.join_blocks = t.whole ? t.splits > 1u : t.ranges > 1u;
     if (t.join_blocks) t.join_blocks = (uint32_t)(((uint64_t)b.max_new * q_heads + 3u) / 4u);
     t.score_stride = (b.max_len + 31u) & ~31u;

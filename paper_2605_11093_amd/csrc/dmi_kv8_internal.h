@@ -82,6 +82,7 @@ struct TokensPlan {
 // How many query rows are attended to: see dmi_kv8_parts.hip.
 struct PartsPlan {
     uint32_t row_tiles;                         // workgroups for the rows that share a head
+    bool counted;                               // requests' rows differ much: see parts_kernel
     uint32_t splits, chunk;                     // parts of the longest context, their tokens
     f32x2 *sums;                                // [row of out][split]: maximum, sum of 2^(score - maximum); one split: unused
     float *parts;                               // [row of out][split][dim]

@@ -65,13 +65,45 @@ void parts_kernel(AttendArgs a, PartsPlan p)
     auto chunk_of = [](int row, int chunk) { return chunk ^ ((row >> 2 & 3) | ((row >> 1 ^ row >> 4) & 1) << 2); };
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
-    // the row tiles of a request and head on one XCD, those that see most first
-    const uint32_t seq = blockIdx.x >> 3, pair = seq / (p.row_tiles * p.splits) * 8u + (blockIdx.x & 7u), in = seq % (p.row_tiles * p.splits);
-    if (pair >= a.b.n_reqs * a.c.heads) return;
-    const uint32_t head = pair % a.c.heads, split = in % p.splits, row_tile = p.row_tiles - 1u - in / p.splits;
-    const Request q = request_of(a.b, a.c, (int)(pair / a.c.heads));
-    const int rows = q.fresh * (int)a.group, row0 = (int)row_tile * 32 * NW;
-    if (row0 >= rows) return;
+    // The row tiles of a request and head on one XCD, those that see most first: workgroups go to the eight XCDs in turn, and every eighth
+    // pair of request and head belongs to each.
+    const uint32_t xcd = blockIdx.x & 7u, item = (blockIdx.x >> 3) / p.splits, split = (blockIdx.x >> 3) - item * p.splits;
+    Request q{0, 0, 0, 0};
+    uint32_t head = 0;
+    int row0 = -1;
+    if (p.counted) {
+        // as many workgroups as all requests' rows make: their tiles are counted here
+        for (uint32_t n0 = 0, before = 0; n0 < a.b.n_reqs; n0 += 64u) {
+            const uint32_t r = n0 + (uint32_t)lane;
+            Request own{0, 0, 0, 0};
+            if (r < a.b.n_reqs) own = request_of(a.b, a.c, (int)r);
+            const int row_tiles = (own.fresh * (int)a.group + 32 * NW - 1) / (32 * NW);
+            const uint32_t pairs = ((r + 1u) * a.c.heads + 7u - xcd) / 8u - (r * a.c.heads + 7u - xcd) / 8u;
+            const int upto = lanes_scan(row_tiles * (int)pairs), place = (int)(item - before);
+            const uint64_t behind = __ballot(upto > place);
+            if (!behind) {
+                before += (uint32_t)__builtin_amdgcn_readlane(upto, 63);
+                continue;
+            }
+            const int in = __ffsll((unsigned long long)behind) - 1, of = __builtin_amdgcn_readlane(row_tiles, in);
+            const int nth = place - (in ? __builtin_amdgcn_readlane(upto, in - 1) : 0), which = nth / of;
+            const uint32_t first = (n0 + (uint32_t)in) * a.c.heads;
+            q = request_in(own, in);
+            head = ((xcd - first) & 7u) + 8u * (uint32_t)which;
+            row0 = (of - 1 - (nth - which * of)) * 32 * NW;
+            break;
+        }
+    } else {
+        // as many for every request as the one with most rows has
+        const uint32_t pair = item / p.row_tiles * 8u + xcd, r = pair / a.c.heads;
+        if (r >= a.b.n_reqs) return;
+        head = pair - r * a.c.heads;
+        q = request_of(a.b, a.c, (int)r);
+        row0 = (int)(p.row_tiles - 1u - item % p.row_tiles) * 32 * NW;
+        if (row0 >= q.fresh * (int)a.group) return;
+    }
+    if (row0 < 0) return;
+    const int rows = q.fresh * (int)a.group;
     const int older = q.len - q.fresh, last_row = min(row0 + 32 * NW, rows) - 1;
     const int seen = older + last_row / (int)a.group + 1;       // tokens that the workgroup's last row sees
     const int begin = (int)(split * p.chunk), end = min(seen, begin + (int)p.chunk), tiles = max(0, (end - begin + kTile - 1) / kTile);
@@ -684,10 +716,18 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
     }
 }
 
-template <typename T, int DP, int NW> static hipError_t parts(const AttendArgs &a, const PartsPlan &p, hipStream_t s)
+template <typename T, int DP, int NW> static hipError_t parts(const AttendArgs &a, PartsPlan p, hipStream_t s)
 {
-    const uint32_t pairs = (a.b.n_reqs * a.c.heads + 7u) / 8u;
-    parts_kernel<T, DP, NW><<<dim3(pairs * p.row_tiles * p.splits * 8u), 64 * NW, 0, s>>>(a, p);
+    // Row tiles of an XCD at most: as many as the longest request makes, for each pair; as many as all rows make, and one for each request.
+    // Where the second is less the kernel counts for itself: a workgroup that finds nothing to do has waited for a compute unit of its own.
+    // Measured (us, first / second): one prompt of 8192 tokens among 63 single ones 2163 / 1387, one of 512 among 255 1031 / 284, 32 ragged
+    // prompts 609 / 603; where all requests are alike counting costs some 0.7 us for every 64 of them, and is not done.
+    const uint64_t by_pairs = ((uint64_t)a.b.n_reqs * a.c.heads + 7u) / 8u * p.row_tiles;
+    const uint64_t by_rows = ((uint64_t)a.b.total_new * a.group / (32u * NW) + a.b.n_reqs) * ((a.c.heads + 7u) / 8u);
+    p.counted = by_pairs > by_rows;
+    const uint64_t groups = (p.counted ? by_rows : by_pairs) * p.splits * 8u;
+    if (groups > 0xffffffffu / (64u * NW)) return hipErrorInvalidConfiguration;
+    parts_kernel<T, DP, NW><<<(uint32_t)groups, 64 * NW, 0, s>>>(a, p);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && p.splits > 1u) {
         const uint32_t each = 256u / (a.c.dim / 4u);

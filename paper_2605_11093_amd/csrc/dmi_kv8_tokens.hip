@@ -17,27 +17,8 @@ namespace kv8 {
 // wavefronts equal ranges of the context; their sums meet in LDS, and nothing is left for a second launch.  p.splits workgroups share a
 // longer context and leave a part each.
 
-// Sums over the lanes up to each one
-__device__ __forceinline__ int lanes_scan(int v)
-{
-    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);     // within 16 lanes: shifts by 1, 2, 4, 8
-    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);     // the totals of 16 lanes carried on
-    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);
-    return v;
-}
-
 // A request with new tokens has a tile at least: an empty context's rows are written too.
 __device__ __forceinline__ int tiles_of(const Request &q) { return q.fresh > 0 ? max(1, (q.len + 31) >> 5) : 0; }
-
-// A request that a lane has
-__device__ __forceinline__ Request request_in(const Request &q, int lane)
-{
-    return {__builtin_amdgcn_readlane(q.row, lane), __builtin_amdgcn_readlane(q.len, lane), __builtin_amdgcn_readlane(q.start, lane),
-            __builtin_amdgcn_readlane(q.fresh, lane)};
-}
 
 // The tiles of requests n0 .. n0 + 63, one request a lane
 __device__ __forceinline__ int lane_tiles(const AttendArgs &a, uint32_t n0)

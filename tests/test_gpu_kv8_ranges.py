@@ -50,5 +50,5 @@ def test_splits(B, dtype, spans, heads, group, dim, weights):                   
 def test_many_rows(B, dtype, reqs, heads, dim, new, longest):                   # noqa: F811
     r = np.random.default_rng(reqs)
     spans = [(int(new if i % 7 else 0), int(n)) for i, n in enumerate(r.integers(new, new + 50, reqs), 1)]
-    spans[reqs // 2] = (300, longest + 300)
+    spans[reqs // 2] = (300, longest + 300)        # a prompt among short ones
     _check_attend(B, Setup(B, 23, spans, heads, dim, 16), dtype, 1)
