@@ -55,18 +55,41 @@ template <> __device__ __forceinline__ void Eight<float>::numbers(float x[8]) co
 // One wavefront per (request, block that it reaches, head, K or V): the largest magnitude of the new tokens' elements, the scale
 // from its exponent, then the codes.  What a block of 16 tokens and 128 elements holds stays in registers between the two, so x is
 // read once; a scale is one block's and head's alone, so wavefronts share nothing.  Bound by memory where there is much to write: 32
-// prompts, 38600 tokens of 8 heads x 128 in bf16, 237 MB in 57 us (4.2 TB/s; a copy reaches 5.0 on this card); elsewhere by a chain of
-// four loads that wait for each other (length, table, scale, rows): 128 single tokens 4.6 us.  Non-temporal loads and stores gain
-// 4 us with the prompts and lose 3 to 4 where the caller has just written x (16 requests of some 30 tokens, fp32: 8.5 us).
+// prompts, 38600 tokens of 8 heads x 128 in bf16, 237 MB in 52 us (4.6 TB/s; a copy reaches 5.0 on this card); elsewhere by a chain of
+// four loads that wait for each other (length, table, scale, rows): 128 single tokens 4.6 us.  Non-temporal loads and stores gained
+// 4 us with the prompts and lost 3 to 4 where the caller has just written x (16 requests of some 30 tokens, fp32: 8.5 us).
 template <typename T>
 __global__ __launch_bounds__(256) void append_kernel(AppendArgs a)
 {
     constexpr int kHeld = 4;                    // units of 8 elements a lane keeps
     const uint32_t lane = threadIdx.x & 63u;
-    const uint32_t item = blockIdx.x * 4u + (threadIdx.x >> 6);
-    const uint32_t kv = item & 1u, head = (item >> 1) % a.c.heads, nth = (item >> 1) / a.c.heads;
-    if (nth >= a.touched) return;
-    const Request q = request_of(a.b, a.c, (int)blockIdx.y);
+    const uint32_t item = blockIdx.x * 4u + (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t kv = item & 1u, head = (item >> 1) % a.c.heads;
+    uint32_t nth = (item >> 1) / a.c.heads;
+    Request q{0, 0, 0, 0};
+    if (a.counted) {
+        // as many wavefronts as all requests' new tokens make: the blocks that they reach are counted here
+        for (uint32_t n0 = 0;; n0 += 64u) {
+            if (n0 >= a.b.n_reqs) return;
+            Request own{0, 0, 0, 0};
+            if (n0 + lane < a.b.n_reqs) own = request_of(a.b, a.c, (int)(n0 + lane));
+            const int begin = max(own.len - own.fresh, 0);
+            const int reached = own.len > begin ? (int)(block_of(a.c, (uint32_t)(own.len - 1) >> 4) - block_of(a.c, (uint32_t)begin >> 4)) + 1 : 0;
+            const int upto = lanes_scan(reached);
+            const uint64_t behind = __ballot(upto > (int)nth);
+            if (!behind) {
+                nth -= (uint32_t)__builtin_amdgcn_readlane(upto, 63);
+                continue;
+            }
+            const int in = __ffsll((unsigned long long)behind) - 1;
+            if (in) nth -= (uint32_t)__builtin_amdgcn_readlane(upto, in - 1);
+            q = request_in(own, in);
+            break;
+        }
+    } else {
+        if (nth >= a.touched) return;
+        q = request_of(a.b, a.c, (int)blockIdx.y);
+    }
     const int first = q.len - q.fresh;          // the first new token's position; below 0: that token has none
     const int from = max(first, 0);
     const uint32_t block = block_of(a.c, (uint32_t)from >> 4) + nth;
@@ -148,9 +171,16 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a)
     if (!lane) *scale_p = s;
 }
 
-hipError_t launch_append(const AppendArgs &a, uint32_t dtype, hipStream_t s)
+hipError_t launch_append(AppendArgs a, uint32_t dtype, hipStream_t s)
 {
-    const dim3 grid((a.touched * a.c.heads * 2u + 3u) / 4u, a.b.n_reqs);
+    // Blocks that all new tokens reach at most: as many as they fill, and a part of one at either end of a request.  Where the most that one
+    // request may reach, for every request, is more than twice that, the kernel counts for itself (us, without / with): a prompt of
+    // 8192 tokens among 63 single ones 74 / 15, one of 2048 among 255 70 / 10, 32 ragged prompts 52 either way.
+    const uint64_t reached = (uint64_t)a.b.total_new / a.c.bs + 2u * (uint64_t)a.b.n_reqs;
+    a.counted = (uint64_t)a.touched * a.b.n_reqs > 2u * reached;
+    const uint64_t groups = ((a.counted ? reached : a.touched) * a.c.heads * 2u + 3u) / 4u;
+    if (groups > 0xffffffffu / 256u) return hipErrorInvalidConfiguration;
+    const dim3 grid((uint32_t)groups, a.counted ? 1u : a.b.n_reqs);
     switch (dtype) {
     case DMI_DTYPE_BF16: append_kernel<Bf16><<<grid, 256, 0, s>>>(a); break;
     case DMI_DTYPE_FP16: append_kernel<_Float16><<<grid, 256, 0, s>>>(a); break;

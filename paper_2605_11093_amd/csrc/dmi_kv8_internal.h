@@ -43,6 +43,7 @@ struct AppendArgs {
     Batch b;
     Rows x[2];
     uint32_t touched;                           // blocks that a request's new tokens may reach
+    bool counted;                               // requests' new tokens differ much: see append_kernel
 };
 
 struct EvictArgs {
@@ -89,7 +90,7 @@ struct PartsPlan {
     float *totals;                              // [row of out]: log2 of the sum of 2^score; NULL: no weights
 };
 
-hipError_t launch_append(const AppendArgs &a, uint32_t dtype, hipStream_t s);
+hipError_t launch_append(AppendArgs a, uint32_t dtype, hipStream_t s);
 hipError_t launch_evict(const EvictArgs &a, hipStream_t s);
 hipError_t launch_parts(const AttendArgs &a, const PartsPlan &p, uint32_t dtype, hipStream_t s);
 hipError_t launch_tokens(const AttendArgs &a, const TokensPlan &p, uint32_t dtype, hipStream_t s);
@@ -115,6 +116,25 @@ __device__ __forceinline__ Request request_of(const Batch &b, const Cache &c, in
         q.fresh = 1;
     }
     return q;
+}
+
+// Sums over the lanes up to each one
+__device__ __forceinline__ int lanes_scan(int v)
+{
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);     // within 16 lanes: shifts by 1, 2, 4, 8
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);     // the totals of 16 lanes carried on
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);
+    return v;
+}
+
+// A request that a lane has
+__device__ __forceinline__ Request request_in(const Request &q, int lane)
+{
+    return {__builtin_amdgcn_readlane(q.row, lane), __builtin_amdgcn_readlane(q.len, lane), __builtin_amdgcn_readlane(q.start, lane),
+            __builtin_amdgcn_readlane(q.fresh, lane)};
 }
 
 // Logical block of the 16 tokens from 16 * sixteen on.  bs / 16 is at most 64 and sixteen below 2^20: with the reciprocal

@@ -98,25 +98,6 @@ __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2
 __device__ __forceinline__ float log2_of(float x) { return __builtin_amdgcn_logf(x); }
 constexpr float kLn2 = 0.693147180559945309417f;
 
-// Sums over the lanes up to each one
-__device__ __forceinline__ int lanes_scan(int v)
-{
-    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);     // within 16 lanes: shifts by 1, 2, 4, 8
-    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);     // the totals of 16 lanes carried on
-    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);
-    return v;
-}
-
-// A request that a lane has
-__device__ __forceinline__ Request request_in(const Request &q, int lane)
-{
-    return {__builtin_amdgcn_readlane(q.row, lane), __builtin_amdgcn_readlane(q.len, lane), __builtin_amdgcn_readlane(q.start, lane),
-            __builtin_amdgcn_readlane(q.fresh, lane)};
-}
-
 template <int N> struct Int {
     static constexpr int value = N;
 };

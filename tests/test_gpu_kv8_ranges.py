@@ -1,9 +1,11 @@
 """Attention of few query rows over many contexts, cut into equal ranges that pass the ends of requests, and over single long ones in
-equal splits: against the definition in 64 bits, as in test_gpu_kv8.py."""
+equal splits; batches whose requests differ much, whose work is counted on the device: against the definitions in 64 bits, as in
+test_gpu_kv8.py."""
 import numpy as np
 import pytest
 import torch
 
+import _kv8 as K
 from test_gpu_kv8 import B, Setup, _check_attend        # noqa: F401
 
 pytestmark = pytest.mark.gpu
@@ -52,3 +54,21 @@ def test_many_rows(B, dtype, reqs, heads, dim, new, longest):                   
     spans = [(int(new if i % 7 else 0), int(n)) for i, n in enumerate(r.integers(new, new + 50, reqs), 1)]
     spans[reqs // 2] = (300, longest + 300)        # a prompt among short ones
     _check_attend(B, Setup(B, 23, spans, heads, dim, 16), dtype, 1)
+
+
+@pytest.mark.parametrize("dtype", [BF16, torch.float32])
+@pytest.mark.parametrize("reqs,heads,dim,block,new", [(70, 3, 80, 16, 200), (9, 2, 128, 32, 700), (130, 1, 64, 16, 400)], ids=["many", "few", "more"])
+def test_append_a_prompt_among_short_ones(B, dtype, reqs, heads, dim, block, new):  # noqa: F811
+    r = np.random.default_rng(reqs)
+    spans = [(int(i % 3 > 0), int(n)) for i, n in enumerate(r.integers(1, 50, reqs))]
+    spans[reqs // 3] = (new, new + 21)
+    s = Setup(B, 24, spans, heads, dim, block, fill=False)
+    key, kn = s.values(heads, dtype, 3.0)
+    value, vn = s.values(heads, dtype, 0.2)
+    cpu = s.cpu()
+    B.kv8_append(s.cache, s.batch, key, value, stream=torch.cuda.current_stream().cuda_stream)
+    K.append(cpu, s.spans, kn, vn)
+    for got, want in ((s.k, cpu.code[0]), (s.v, cpu.code[1])):
+        K.equal_codes(got.cpu().contiguous().numpy(), want)
+    for got, want in ((s.k_scale, cpu.scale[0]), (s.v_scale, cpu.scale[1])):
+        assert np.array_equal(got.cpu().numpy().astype(np.float64), want, equal_nan=True)
