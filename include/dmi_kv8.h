@@ -35,8 +35,8 @@ extern "C" {
  * base + b*block_stride + s*slot_stride + h*head_stride + d (strides in bytes, the same for K and V); it stands for
  * number(code) * scale, scale at scale_base + b*scale_block_stride + h*scale_head_stride (in floats), positive and finite.
  * k, v 16-byte aligned, strides multiples of 16 bytes, slot_stride from 0 to 2^26.  block_size: a multiple of 16, at most 1024.  head_dim: a multiple of 16, at
- * most 256.  block_table_dev [device] int32 [n_seqs][block_table_stride], of which max_blocks columns are used: physical
- * block of logical block t / block_size of a sequence. */
+ * most 256.  block_table_dev [device] int32 [n_seqs][block_table_stride], of which max_blocks columns are used (rows do not
+ * overlap: block_table_stride >= max_blocks): physical block of logical block t / block_size of a sequence. */
 typedef struct {
     void *k, *v;                /* [device] e4m3 codes */
     float *k_scale, *v_scale;   /* [device] */

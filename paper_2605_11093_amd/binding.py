@@ -785,7 +785,7 @@ class KV8:
         self._raw = _PACK_KV8(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), k.stride(0), k.stride(1),
                               k.stride(2), k_scale.stride(0), k_scale.stride(1), k.shape[1], k.shape[2], k.shape[3], k.shape[0],
                               block_table.shape[0], block_table.shape[1], block_table.data_ptr(),
-                              max(block_table.stride(0), block_table.shape[1]))
+                              block_table.stride(0) if block_table.shape[0] > 1 else block_table.shape[1])
 
 
 class KV8Batch:
