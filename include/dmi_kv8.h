@@ -100,7 +100,8 @@ dmi_status_t dmi_kv8_append(const dmi_kv8_t *cache /*[host]*/, const dmi_kv8_bat
  *   weight     [host, optional] for every request, head of the cache and position t < len:
  *              weight = decay * prior + sum of p_t over the call's new tokens and the g query heads.
  *              prior [host, optional]: the same layout, may be the same memory; positions of new tokens count as 0 in it.
- *   workspace  [device] 256-byte aligned, at least dmi_kv8_attend_workspace(...) bytes; contents need not be kept.
+ *   workspace  [device] 256-byte aligned, at least dmi_kv8_attend_workspace(...) bytes; contents need not be kept.  (That function
+ *              looks at sizes alone, and gives 0 for those that this call refuses.)
  * Scores, softmax, sums and weights are fp32; products are of q as it is and the codes' exact values; p is rounded to q's type
  * for its product with V.
  */

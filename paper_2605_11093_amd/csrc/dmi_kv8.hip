@@ -13,6 +13,33 @@ namespace {
 // A stride that moves rows by whole 16-byte units
 bool whole(int64_t stride, uint32_t size) { return (stride * (int64_t)size) % 16 == 0; }
 
+// Sizes that plans are made of
+dmi_status_t check_shape(const dmi_kv8_t *k, const char *what)
+{
+    if (!k->block_size || k->block_size % 16u || k->block_size > kMaxBlock)
+        return fail(DMI_ERR_INVALID_ARG, "%s: block_size %u is not a multiple of 16 up to %u", what, k->block_size, kMaxBlock);
+    if (!k->head_dim || k->head_dim % 16u || k->head_dim > kMaxDim)
+        return fail(DMI_ERR_INVALID_ARG, "%s: head_dim %u is not a multiple of 16 up to %u", what, k->head_dim, kMaxDim);
+    if (!k->n_heads || k->n_heads > 1024u) return fail(DMI_ERR_INVALID_ARG, "%s: n_heads %u is not in 1..1024", what, k->n_heads);
+    return DMI_OK;
+}
+
+dmi_status_t check_counts(const dmi_kv8_batch_t *k, bool fresh)
+{
+    if (k->n_reqs > kMaxReqs) return fail(DMI_ERR_INVALID_ARG, "n_reqs %u is more than %u", k->n_reqs, kMaxReqs);
+    if (k->max_len > kMaxLen) return fail(DMI_ERR_INVALID_ARG, "max_len %u is more than %u", k->max_len, kMaxLen);
+    if (fresh && (k->total_new > (1u << 30) || k->max_new > kMaxLen))
+        return fail(DMI_ERR_INVALID_ARG, "total_new %u or max_new %u is too large", k->total_new, k->max_new);
+    return DMI_OK;
+}
+
+dmi_status_t check_q_heads(uint32_t n_q_heads, uint32_t heads)
+{
+    if (!n_q_heads || n_q_heads % heads || n_q_heads > 65536u)
+        return fail(DMI_ERR_INVALID_ARG, "%u query heads do not share %u heads evenly", n_q_heads, heads);
+    return DMI_OK;
+}
+
 dmi_status_t check_cache(const dmi_kv8_t *k, const char *what, Cache &c)
 {
     if (!k) return fail(DMI_ERR_INVALID_ARG, "%s is NULL", what);
@@ -25,11 +52,8 @@ dmi_status_t check_cache(const dmi_kv8_t *k, const char *what, Cache &c)
         return fail(DMI_ERR_INVALID_ARG, "%s: slot_stride is not in 0..%lld", what, (long long)kMaxSlotStride);
     if ((uintptr_t)k->k_scale % 4u || (uintptr_t)k->v_scale % 4u || (uintptr_t)k->block_table_dev % 4u)
         return fail(DMI_ERR_INVALID_ARG, "%s: scales and block table must be 4-byte aligned", what);
-    if (!k->block_size || k->block_size % 16u || k->block_size > kMaxBlock)
-        return fail(DMI_ERR_INVALID_ARG, "%s: block_size %u is not a multiple of 16 up to %u", what, k->block_size, kMaxBlock);
-    if (!k->head_dim || k->head_dim % 16u || k->head_dim > kMaxDim)
-        return fail(DMI_ERR_INVALID_ARG, "%s: head_dim %u is not a multiple of 16 up to %u", what, k->head_dim, kMaxDim);
-    if (!k->n_heads || k->n_heads > 1024u) return fail(DMI_ERR_INVALID_ARG, "%s: n_heads %u is not in 1..1024", what, k->n_heads);
+    const dmi_status_t st = check_shape(k, what);
+    if (st != DMI_OK) return st;
     if (!k->n_blocks || k->n_blocks > (1u << 30) || !k->n_seqs || k->n_seqs > (1u << 30) || !k->max_blocks ||
         k->max_blocks > kMaxLen || k->block_table_stride < (int64_t)k->max_blocks)
         return fail(DMI_ERR_INVALID_ARG, "%s: bad n_blocks, n_seqs, max_blocks or block_table_stride", what);
@@ -44,17 +68,15 @@ dmi_status_t check_cache(const dmi_kv8_t *k, const char *what, Cache &c)
 dmi_status_t check_batch(const dmi_kv8_batch_t *k, const Cache &c, bool fresh, Batch &b)
 {
     if (!k) return fail(DMI_ERR_INVALID_ARG, "batch is NULL");
-    if (k->n_reqs > kMaxReqs) return fail(DMI_ERR_INVALID_ARG, "n_reqs %u is more than %u", k->n_reqs, kMaxReqs);
+    const dmi_status_t st = check_counts(k, fresh);
+    if (st != DMI_OK) return st;
     if (k->n_reqs && !k->lens_dev) return fail(DMI_ERR_INVALID_ARG, "lens_dev is NULL");
     if (((uintptr_t)k->lens_dev | (uintptr_t)k->starts_dev | (uintptr_t)k->rows_dev) % 4u)
         return fail(DMI_ERR_INVALID_ARG, "lens_dev, starts_dev and rows_dev must be 4-byte aligned");
-    if (k->max_len > kMaxLen || (uint64_t)k->max_len > (uint64_t)c.max_blocks * c.bs)
-        return fail(DMI_ERR_INVALID_ARG, "max_len %u is more than the block table's %u blocks of %u tokens, or than %u", k->max_len,
-                    c.max_blocks, c.bs, kMaxLen);
+    if ((uint64_t)k->max_len > (uint64_t)c.max_blocks * c.bs)
+        return fail(DMI_ERR_INVALID_ARG, "max_len %u is more than the block table's %u blocks of %u tokens", k->max_len, c.max_blocks, c.bs);
     if (!k->rows_dev && k->n_reqs > c.n_seqs)
         return fail(DMI_ERR_INVALID_ARG, "n_reqs %u is more than the block table's %u rows", k->n_reqs, c.n_seqs);
-    if (fresh && (k->total_new > (1u << 30) || k->max_new > kMaxLen))
-        return fail(DMI_ERR_INVALID_ARG, "total_new %u or max_new %u is too large", k->total_new, k->max_new);
     if (fresh && !k->starts_dev && (k->total_new != k->n_reqs || k->max_new != 1u))
         return fail(DMI_ERR_INVALID_ARG, "without starts_dev there is one new token a request");
     b = Batch{k->lens_dev, k->starts_dev, k->rows_dev, k->n_reqs, k->total_new, k->max_new, k->max_len};
@@ -178,7 +200,9 @@ AttendPlan plan_attend(uint32_t block_heads, uint32_t dim, const dmi_kv8_batch_t
 extern "C" uint64_t dmi_kv8_attend_workspace(const dmi_kv8_t *cache, const dmi_kv8_batch_t *batch, uint32_t n_q_heads,
                                              int with_weight)
 {
-    if (!cache || !batch || !cache->n_heads || !n_q_heads || n_q_heads % cache->n_heads) return 0;
+    if (!cache || !batch || check_shape(cache, "cache") != DMI_OK || check_counts(batch, true) != DMI_OK ||
+        check_q_heads(n_q_heads, cache->n_heads) != DMI_OK)
+        return 0;
     return plan_attend(cache->n_heads, cache->head_dim, *batch, n_q_heads, with_weight != 0).bytes;
 }
 
@@ -195,8 +219,7 @@ extern "C" dmi_status_t dmi_kv8_attend(const dmi_kv8_t *cache, const dmi_kv8_bat
         return st;
     if (q->dtype != out->dtype || (q->dtype != DMI_DTYPE_BF16 && q->dtype != DMI_DTYPE_FP16))
         return fail(DMI_ERR_INVALID_ARG, "q and out must both be BF16 or both FP16");
-    if (!n_q_heads || n_q_heads % a.c.heads || n_q_heads > 65536u)
-        return fail(DMI_ERR_INVALID_ARG, "%u query heads do not share %u heads evenly", n_q_heads, a.c.heads);
+    if ((st = check_q_heads(n_q_heads, a.c.heads)) != DMI_OK) return st;
     if (!std::isfinite(scale)) return fail(DMI_ERR_INVALID_ARG, "scale is not finite");
     if ((uintptr_t)lse_dev % 4u) return fail(DMI_ERR_INVALID_ARG, "lse_dev must be 4-byte aligned");
     if (a.prior.data && !a.w.data) return fail(DMI_ERR_INVALID_ARG, "prior without weight");

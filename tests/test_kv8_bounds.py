@@ -1,8 +1,14 @@
 """Arguments of the 8-bit KV cache's calls that would lead a kernel outside its tensors, or a launch past its limits: refused on the host."""
+import os
+import subprocess
+import sys
+
 import pytest
 import torch
 
 from paper_2605_11093_amd import binding as B
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 def _cache(table, blocks=8, block=16, heads=2, dim=64):
@@ -26,3 +32,33 @@ def test_a_table_of_one_row_may_have_any_stride():
     c = _cache(torch.zeros(4, dtype=torch.int32).as_strided((1, 4), (0, 1)))
     x = torch.zeros(0, 2, 64)
     B.kv8_append(c, B.KV8Batch(torch.ones(0, dtype=torch.int32), max_len=32), x, x)
+
+
+_WORKSPACE = """
+import sys
+from paper_2605_11093_amd import binding as B
+heads, dim, q_heads, reqs, total, new, length = map(int, sys.argv[1:])
+cache = B._PACK_KV8(0, 0, 0, 0, 0, 0, 0, 0, 0, 16, heads, dim, 1, 1, 1, 0, 1)
+print(B.lib().dmi_kv8_attend_workspace(cache, B._PACK_KV8_BATCH(reqs, total, new, length, 0, 0, 0), q_heads, 1))
+"""
+
+
+def _workspace(*numbers):
+    p = subprocess.run([sys.executable, "-c", _WORKSPACE, *map(str, numbers)], capture_output=True, text=True, cwd=ROOT)
+    assert p.returncode == 0, f"ended by {p.returncode}: {p.stderr}"
+    return int(p.stdout)
+
+
+@pytest.mark.parametrize("numbers", [
+    (1 << 31, 256, 1 << 31, 1, 32, 32, 100),        # heads whose tiles of query rows are more than 32 bits count
+    (2048, 64, 2048, 1, 1, 1, 100), (2, 512, 4, 1, 1, 1, 100), (2, 0, 4, 1, 1, 1, 100), (2, 64, 3, 1, 1, 1, 100),
+    (1, 64, 1 << 17, 1, 1, 1, 100), (2, 64, 4, 1 << 17, 1 << 17, 1, 100), (2, 64, 4, 1, 1, 1, 1 << 25),
+    (2, 64, 4, 1, 1 << 31, 1, 100), (2, 64, 4, 1, 1 << 20, 1 << 25, 100)],
+    ids=["tiles", "heads", "dim", "no dim", "uneven", "q heads", "requests", "length", "rows", "new"])
+def test_workspace_of_sizes_that_attend_refuses(numbers):
+    """In a process of its own: a division by zero would end it."""
+    assert _workspace(*numbers) == 0
+
+
+def test_workspace_of_sizes_that_attend_takes():
+    assert _workspace(8, 128, 32, 16, 16, 1, 8192) >= 16 * 32 * 8192 * 4
