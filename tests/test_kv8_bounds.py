@@ -62,3 +62,24 @@ def test_workspace_of_sizes_that_attend_refuses(numbers):
 
 def test_workspace_of_sizes_that_attend_takes():
     assert _workspace(8, 128, 32, 16, 16, 1, 8192) >= 16 * 32 * 8192 * 4
+
+
+@pytest.mark.parametrize("numbers", [
+    (1, 64, 2, 1, 1 << 30, 16, 1 << 24),            # scores of more bytes than 64 bits count
+    (1024, 64, 1 << 15, 1, 1 << 30, 1, 1 << 24),
+    (1, 64, 65536, 1, 1 << 30, 1 << 24, 100),       # query rows of one request past 32 bits
+], ids=["scores", "heads", "rows"])
+def test_more_query_rows_than_31_bits_count(numbers):
+    """Sizes in bytes would wrap, and rows of a request: refused by the workspace's function and by the call."""
+    heads, dim, q_heads, reqs, total, new, length = numbers
+    assert _workspace(*numbers) == 0
+    blocks = -(-length // 16)
+    word = torch.zeros(4, dtype=torch.int32)
+    code = (16 - word.data_ptr() % 16) % 16 + word.data_ptr()
+    # (pointers are only looked at: it is refused before anything is launched)
+    cache = B._PACK_KV8(code, code, code, code, 16 * heads * 64, heads * 64, 64, heads, 1, 16, heads, dim, 1, 1, blocks, code, blocks)
+    batch = B._PACK_KV8_BATCH(reqs, total, new, length, code, code, 0)
+    rows = B._PACK_KV8_HEADS(code, B.DT_BF16, q_heads * dim, dim)
+    weight = B._PACK_KV8_WEIGHT(code, heads * length, length)
+    assert B.lib().dmi_kv8_attend(cache, batch, rows, q_heads, 1.0, rows, None, weight, None, 0.0, 256, 1 << 62, None) == B.ERR_INVALID_ARG
+    assert b"total_new" in B.lib().dmi_last_error()
