@@ -2,6 +2,7 @@
 #include "dmi_ring.h"
 #include "dmi_kv8_internal.h"
 
+#include <algorithm>
 #include <cmath>
 
 using namespace dmi;
@@ -82,7 +83,7 @@ dmi_status_t check_batch(const dmi_kv8_batch_t *k, const Cache &c, bool fresh, B
         return fail(DMI_ERR_INVALID_ARG, "n_reqs %u is more than the block table's %u rows", k->n_reqs, c.n_seqs);
     if (fresh && !k->starts_dev && (k->total_new != k->n_reqs || k->max_new != 1u))
         return fail(DMI_ERR_INVALID_ARG, "without starts_dev there is one new token a request");
-    b = Batch{k->lens_dev, k->starts_dev, k->rows_dev, k->n_reqs, k->total_new, k->max_new, k->max_len};
+    b = Batch{k->lens_dev, k->starts_dev, k->rows_dev, k->n_reqs, k->total_new, std::min(k->max_new, k->total_new), k->max_len};
     return DMI_OK;
 }
 
@@ -144,8 +145,8 @@ constexpr uint32_t kResident = 2048;
 AttendPlan plan_attend(uint32_t block_heads, uint32_t dim, const dmi_kv8_batch_t &b, uint32_t q_heads, bool weight)
 {
     AttendPlan p{};
-    const uint32_t group = q_heads / block_heads;
-    const uint64_t rows = (uint64_t)b.total_new * q_heads, shared = (uint64_t)b.max_new * group;
+    const uint32_t group = q_heads / block_heads, max_new = std::min(b.max_new, b.total_new);
+    const uint64_t rows = (uint64_t)b.total_new * q_heads, shared = (uint64_t)max_new * group;
     // Up to 32 rows of queries share a head: tokens_kernel.  Measured (us, tokens / parts; 8 requests of 4000-8000 tokens and 64 of 2000-
     // 4000, 8 heads x 128): 16 rows 38 / 80 and 98 / 253, 32 rows 34 / 44 and 124 / 177, 64 rows 67 / 53 and 182 / 181.
     p.tokens = shared <= 32u;
@@ -188,7 +189,7 @@ AttendPlan plan_attend(uint32_t block_heads, uint32_t dim, const dmi_kv8_batch_t
     if (b.max_len > reach * t.splits) t.splits = (b.max_len + reach - 1u) / reach;
     t.whole = t.row_tiles == 1u && (units * t.splits <= 512u || (t.splits == 1u && units <= 1u << 22 && (shared > 16u || b.max_len <= 256u)));
     t.join_blocks = t.whole ? t.splits > 1u : t.ranges > 1u;
-    if (t.join_blocks) t.join_blocks = (uint32_t)(((uint64_t)b.max_new * q_heads + 3u) / 4u);
+    if (t.join_blocks) t.join_blocks = (uint32_t)(((uint64_t)max_new * q_heads + 3u) / 4u);
     t.score_stride = (b.max_len + 31u) & ~31u;
     const uint64_t parts = !t.join_blocks ? 0u : t.whole ? rows * t.splits : 2ull * t.ranges * per * t.tile_rows;
     p.totals = weight ? pad64(rows * t.score_stride * 4u) : 0u;

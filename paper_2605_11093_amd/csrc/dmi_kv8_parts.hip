@@ -2,6 +2,8 @@
 #include "dmi_internal.h"
 #include "dmi_kv8_mfma.h"
 
+#include <algorithm>
+
 namespace dmi {
 namespace kv8 {
 
@@ -476,40 +478,43 @@ void parts_kernel(AttendArgs a, PartsPlan p)
 }
 
 // Outputs out of the parts that splits of the contexts left: a row by as many lanes as take four elements each of it, in one pass with
-// the running maximum.  Bound by memory and its latency: 48000 rows of 128 elements out of three parts, 86 MB, 24 us.
+// the running maximum (and then another row, where a request has more than a launch has workgroups for).  Bound by memory and its
+// latency: 48000 rows of 128 elements out of three parts, 86 MB, 24 us.
 template <typename T>
 __global__ __launch_bounds__(256) void join_parts_kernel(AttendArgs a, PartsPlan p, uint32_t tile_rows)
 {
     const Request q = request_of(a.b, a.c, (int)blockIdx.y);
-    const uint32_t wide = a.c.dim / 4u, n = blockIdx.x * (256u / wide) + threadIdx.x / wide, rows = (uint32_t)q.fresh * a.group;
-    if (threadIdx.x >= 256u / wide * wide || n >= rows * a.c.heads) return;
-    const uint32_t head = n / rows, row = n - head * rows, lane = threadIdx.x % wide;
-    const QueryRow w = query_row(a, head, row);
-    const int64_t at = (int64_t)(q.start + w.token) * a.q_heads + w.head;
-    // splits that the row's workgroup had work in
-    const uint32_t last_row = min((row / tile_rows + 1u) * tile_rows, rows) - 1u;
-    const int seen = q.len - q.fresh + (int)(last_row / a.group) + 1, splits = max(1, (seen + (int)p.chunk - 1) / (int)p.chunk);
-    const f32x2 *sums = p.sums + at * p.splits;
-    const float *parts = p.parts + at * p.splits * a.c.dim + 4u * lane;
-    float m = -INFINITY, l = 0.0f;
-    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+    const uint32_t wide = a.c.dim / 4u, each = 256u / wide, rows = (uint32_t)q.fresh * a.group, lane = threadIdx.x % wide;
+    if (threadIdx.x >= each * wide) return;
+    for (uint32_t n = blockIdx.x * each + threadIdx.x / wide; n < rows * a.c.heads; n += gridDim.x * each) {
+        const uint32_t head = n / rows, row = n - head * rows;
+        const QueryRow w = query_row(a, head, row);
+        const int64_t at = (int64_t)(q.start + w.token) * a.q_heads + w.head;
+        // splits that the row's workgroup had work in
+        const uint32_t last_row = min((row / tile_rows + 1u) * tile_rows, rows) - 1u;
+        const int seen = q.len - q.fresh + (int)(last_row / a.group) + 1, splits = max(1, (seen + (int)p.chunk - 1) / (int)p.chunk);
+        const f32x2 *sums = p.sums + at * p.splits;
+        const float *parts = p.parts + at * p.splits * a.c.dim + 4u * lane;
+        float m = -INFINITY, l = 0.0f;
+        f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 4
-    for (int s = 0; s < splits; s++) {
-        const f32x2 x = sums[s];
-        const f32x4 part = *reinterpret_cast<const f32x4 *>(parts + (int64_t)s * a.c.dim);
-        const float top = fmaxf(m, x[0]), to = top == -INFINITY ? 0.0f : top, f = exp2_of(m - to), g = exp2_of(x[0] - to);
-        l = l * f + x[1] * g;
-        o = o * f + part * g;
-        m = top;
-    }
-    const bool empty = m == -INFINITY && l == 0.0f;
-    o *= empty ? 0.0f : 1.0f / l;
-    uint16_t *dst = static_cast<uint16_t *>(a.out.data) + (int64_t)(q.start + w.token) * a.out.row_stride + (int64_t)w.head * a.out.head_stride + 4u * lane;
-    *reinterpret_cast<u32x2 *>(dst) = u32x2{T::pack(o[0], o[1]), T::pack(o[2], o[3])};
-    if (!lane) {
-        const float total = empty ? -INFINITY : m + log2_of(l);
-        if (a.lse) a.lse[at] = total * kLn2;
-        if (p.totals) p.totals[at] = total;
+        for (int s = 0; s < splits; s++) {
+            const f32x2 x = sums[s];
+            const f32x4 part = *reinterpret_cast<const f32x4 *>(parts + (int64_t)s * a.c.dim);
+            const float top = fmaxf(m, x[0]), to = top == -INFINITY ? 0.0f : top, f = exp2_of(m - to), g = exp2_of(x[0] - to);
+            l = l * f + x[1] * g;
+            o = o * f + part * g;
+            m = top;
+        }
+        const bool empty = m == -INFINITY && l == 0.0f;
+        o *= empty ? 0.0f : 1.0f / l;
+        uint16_t *dst = static_cast<uint16_t *>(a.out.data) + (int64_t)(q.start + w.token) * a.out.row_stride + (int64_t)w.head * a.out.head_stride + 4u * lane;
+        *reinterpret_cast<u32x2 *>(dst) = u32x2{T::pack(o[0], o[1]), T::pack(o[2], o[3])};
+        if (!lane) {
+            const float total = empty ? -INFINITY : m + log2_of(l);
+            if (a.lse) a.lse[at] = total * kLn2;
+            if (p.totals) p.totals[at] = total;
+        }
     }
 }
 
@@ -731,7 +736,7 @@ template <typename T, int DP, int NW> static hipError_t parts(const AttendArgs &
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && p.splits > 1u) {
         const uint32_t each = 256u / (a.c.dim / 4u);
-        join_parts_kernel<T><<<dim3((a.b.max_new * a.q_heads + each - 1u) / each, a.b.n_reqs), 256, 0, s>>>(a, p, 32u * NW);
+        join_parts_kernel<T><<<dim3(std::min((a.b.max_new * a.q_heads + each - 1u) / each, 1u << 20), a.b.n_reqs), 256, 0, s>>>(a, p, 32u * NW);
         e = hipGetLastError();
     }
     if (e == hipSuccess && a.w.data) {

@@ -1,0 +1,28 @@
+"""The operators on the 8-bit KV cache at the edges of what they accept: loose bounds, calls without new tokens, scales far from each other,
+queries that are no numbers; against the definitions in 64 bits."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import _kv8 as K
+from test_gpu_kv8 import B, BF16, DEV, FP16, Setup, _check_attend, _stream        # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def test_bounds_far_above_the_new_tokens(B):        # noqa: F811
+    """max_new far above any request's new tokens."""
+    s = Setup(B, 36, [(20, 1500), (3, 60), (0, 10)], 8, 64, 16)
+    group = 32
+    q, _ = s.values(8 * group, BF16)
+    got = []
+    for most in (20, 1 << 10, 1 << 20, 1 << 24):
+        batch = B.KV8Batch(s.lens, starts=s.starts_dev, total_new=s.total, max_new=most, max_len=s.max_len)
+        out, lse, w = torch.full_like(q, 7.0), torch.full(q.shape[:2], 7.0, device=DEV), torch.zeros(3, 8, s.max_len, device=DEV)
+        B.kv8_attend(s.cache, batch, q, out, lse=lse, weight=w, stream=_stream())
+        got.append((out, lse, w))
+    for other in got[1:]:
+        for x, y in zip(got[0], other):
+            assert (x.float() - y.float()).abs().max() <= 1e-2
