@@ -739,7 +739,7 @@ template <typename T, int DP, int NW> static hipError_t parts(const AttendArgs &
         join_parts_kernel<T><<<dim3(std::min((a.b.max_new * a.q_heads + each - 1u) / each, 1u << 20), a.b.n_reqs), 256, 0, s>>>(a, p, 32u * NW);
         e = hipGetLastError();
     }
-    if (e == hipSuccess && a.w.data) {
+    if (e == hipSuccess && a.w.data && a.b.max_len) {
         weights_kernel<T, DP><<<dim3((a.b.max_len + 255u) / 256u * a.c.heads, a.b.n_reqs), 256, 0, s>>>(a, p);
         e = hipGetLastError();
     }

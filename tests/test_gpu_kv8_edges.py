@@ -26,3 +26,13 @@ def test_bounds_far_above_the_new_tokens(B):        # noqa: F811
     for other in got[1:]:
         for x, y in zip(got[0], other):
             assert (x.float() - y.float()).abs().max() <= 1e-2
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_lengths_bounded_by_zero(B, new):        # noqa: F811
+    s = Setup(B, 37, [(new, 40), (new, 50)], 2, 64, 16)
+    batch = B.KV8Batch(s.lens, starts=s.starts_dev, total_new=s.total, max_new=new, max_len=0)
+    q, _ = s.values(4, BF16)
+    out, lse, w = torch.full_like(q, 7.0), torch.full(q.shape[:2], 7.0, device=DEV), torch.full((2, 2, 64), 5.0, device=DEV)
+    B.kv8_attend(s.cache, batch, q, out, lse=lse, weight=w, stream=_stream())
+    assert (out == 0).all() and (lse == -math.inf).all() and (w == 5.0).all()
