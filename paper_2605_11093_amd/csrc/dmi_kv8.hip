@@ -109,6 +109,7 @@ dmi_status_t check_weight(const dmi_kv8_weight_t *k, const char *what, Weight &w
 
 dmi_status_t launched(hipError_t e)
 {
+    if (e == hipErrorInvalidConfiguration) return fail(DMI_ERR_INVALID_ARG, "more work than a launch has workgroups for");
     return e == hipSuccess ? DMI_OK : fail(DMI_ERR_HIP, "launch failed: %s", hipGetErrorString(e));
 }
 

@@ -179,7 +179,7 @@ hipError_t launch_append(AppendArgs a, uint32_t dtype, hipStream_t s)
     const uint64_t reached = (uint64_t)a.b.total_new / a.c.bs + 2u * (uint64_t)a.b.n_reqs;
     a.counted = (uint64_t)a.touched * a.b.n_reqs > 2u * reached;
     const uint64_t groups = ((a.counted ? reached : a.touched) * a.c.heads * 2u + 3u) / 4u;
-    if (groups > 0xffffffffu / 256u) return hipErrorInvalidConfiguration;
+    if (!launchable(groups, 256)) return hipErrorInvalidConfiguration;
     const dim3 grid((uint32_t)groups, a.counted ? 1u : a.b.n_reqs);
     switch (dtype) {
     case DMI_DTYPE_BF16: append_kernel<Bf16><<<grid, 256, 0, s>>>(a); break;
@@ -409,15 +409,15 @@ __global__ __launch_bounds__(256) void move_kernel(EvictArgs a, uint32_t blocks,
 
 hipError_t launch_evict(const EvictArgs &a, hipStream_t s)
 {
-    select_kernel<<<dim3(a.c.heads, a.b.n_reqs), kSelectThreads, 0, s>>>(a);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
     const uint32_t left = min(a.keep, max(a.b.max_len, 1u));
     uint32_t blocks = max(1u, 64u / a.c.bs);
     if ((uint64_t)left * a.b.n_reqs * a.c.heads < 64u * kMoveWaves) blocks = 1;
     const uint32_t span = blocks * a.c.bs, spans = (left + span - 1u) / span;
     const uint64_t units = ((uint64_t)spans * a.b.n_reqs + 7u) / 8u * a.c.heads, groups = (units + 3u) / 4u * 8u;    // units: on each XCD
-    if (groups > 0xffffffffu / 256u) return hipErrorInvalidConfiguration;
+    if (!launchable(groups, 256)) return hipErrorInvalidConfiguration;
+    select_kernel<<<dim3(a.c.heads, a.b.n_reqs), kSelectThreads, 0, s>>>(a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
     move_kernel<<<(uint32_t)groups, 256, 0, s>>>(a, blocks, spans);
     return hipGetLastError();
 }

@@ -90,6 +90,10 @@ struct PartsPlan {
     float *totals;                              // [row of out]: log2 of the sum of 2^score; NULL: no weights
 };
 
+// What a launch may have in its first dimension: threads are counted in 32 bits.  A call whose launches need more is refused before
+// the first of them (hipErrorInvalidConfiguration).
+inline bool launchable(uint64_t groups, uint32_t threads) { return groups <= 0xffffffffu / threads; }
+
 hipError_t launch_append(AppendArgs a, uint32_t dtype, hipStream_t s);
 hipError_t launch_evict(const EvictArgs &a, hipStream_t s);
 hipError_t launch_parts(const AttendArgs &a, const PartsPlan &p, uint32_t dtype, hipStream_t s);

@@ -731,7 +731,8 @@ template <typename T, int DP, int NW> static hipError_t parts(const AttendArgs &
     const uint64_t by_rows = ((uint64_t)a.b.total_new * a.group / (32u * NW) + a.b.n_reqs) * ((a.c.heads + 7u) / 8u);
     p.counted = by_pairs > by_rows;
     const uint64_t groups = (p.counted ? by_rows : by_pairs) * p.splits * 8u;
-    if (groups > 0xffffffffu / (64u * NW)) return hipErrorInvalidConfiguration;
+    const uint64_t weight_groups = a.w.data ? (a.b.max_len + 255ull) / 256u * a.c.heads : 0u;
+    if (!launchable(groups, 64u * NW) || !launchable(weight_groups, 256)) return hipErrorInvalidConfiguration;
     parts_kernel<T, DP, NW><<<(uint32_t)groups, 64 * NW, 0, s>>>(a, p);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && p.splits > 1u) {
@@ -739,8 +740,8 @@ template <typename T, int DP, int NW> static hipError_t parts(const AttendArgs &
         join_parts_kernel<T><<<dim3(std::min((a.b.max_new * a.q_heads + each - 1u) / each, 1u << 20), a.b.n_reqs), 256, 0, s>>>(a, p, 32u * NW);
         e = hipGetLastError();
     }
-    if (e == hipSuccess && a.w.data && a.b.max_len) {
-        weights_kernel<T, DP><<<dim3((a.b.max_len + 255u) / 256u * a.c.heads, a.b.n_reqs), 256, 0, s>>>(a, p);
+    if (e == hipSuccess && weight_groups) {
+        weights_kernel<T, DP><<<dim3((uint32_t)weight_groups, a.b.n_reqs), 256, 0, s>>>(a, p);
         e = hipGetLastError();
     }
     return e;

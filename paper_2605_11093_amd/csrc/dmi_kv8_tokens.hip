@@ -708,6 +708,8 @@ __global__ __launch_bounds__(256) void finish_kernel(AttendArgs a, TokensPlan p)
 template <typename T> static hipError_t tokens(const AttendArgs &a, const TokensPlan &p, hipStream_t s)
 {
     const uint32_t per = a.c.heads * p.row_tiles, units = (p.ranges + 7u) / 8u * per;      // on each XCD
+    const uint64_t finish_groups = p.whole && p.splits == 1u ? 0u : p.join_blocks + (a.w.data ? (a.b.max_len + 1023ull) / 1024u * a.c.heads : 0u);
+    if (!launchable(finish_groups, 256)) return hipErrorInvalidConfiguration;
     const int dp = a.c.dim <= 64 ? 64 : a.c.dim <= 128 ? 128 : 256;
     auto launch = [&](auto dp_, auto nt_) {
         constexpr int DP = decltype(dp_)::value, NT = decltype(nt_)::value;
@@ -722,11 +724,9 @@ template <typename T> static hipError_t tokens(const AttendArgs &a, const Tokens
         if (dp == 64) launch(Int<64>{}, Int<2>{});
         else launch(Int<128>{}, Int<2>{});
     }
-    if (p.whole && p.splits == 1u) return hipGetLastError();
-    hipError_t e = hipGetLastError();
-    const uint32_t weight_blocks = a.w.data ? (a.b.max_len + 1023u) / 1024u * a.c.heads : 0u;
-    if (e != hipSuccess || p.join_blocks + weight_blocks == 0) return e;
-    const dim3 finish(p.join_blocks + weight_blocks, a.b.n_reqs);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !finish_groups) return e;
+    const dim3 finish((uint32_t)finish_groups, a.b.n_reqs);
     if (p.whole) finish_kernel<T, true><<<finish, 256, 0, s>>>(a, p);
     else finish_kernel<T, false><<<finish, 256, 0, s>>>(a, p);
     return hipGetLastError();

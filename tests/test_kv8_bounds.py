@@ -83,3 +83,38 @@ def test_more_query_rows_than_31_bits_count(numbers):
     weight = B._PACK_KV8_WEIGHT(code, heads * length, length)
     assert B.lib().dmi_kv8_attend(cache, batch, rows, q_heads, 1.0, rows, None, weight, None, 0.0, 256, 1 << 62, None) == B.ERR_INVALID_ARG
     assert b"total_new" in B.lib().dmi_last_error()
+
+
+def _pointer():
+    word = torch.zeros(64, dtype=torch.int32)
+    return (256 - word.data_ptr() % 256) % 256 + word.data_ptr()
+
+
+@pytest.mark.parametrize("group,new", [(1, 1), (1, 64)], ids=["few", "many"])
+def test_attend_past_the_workgroups_of_a_launch(group, new):
+    """Weights of 2^24 positions of 1024 heads: more workgroups than a launch has, found before the first of its launches."""
+    heads, length, at = 1024, 1 << 24, _pointer()
+    cache = B._PACK_KV8(at, at, at, at, 16 * heads * 64, heads * 64, 64, heads, 1, 16, heads, 64, 1, 1, length // 16, at, length // 16)
+    batch = B._PACK_KV8_BATCH(1, new, new, length, at, at, 0)
+    q, out = (B._PACK_KV8_HEADS(at + x, B.DT_BF16, heads * 64, 64) for x in (0, 1 << 40))
+    weight = B._PACK_KV8_WEIGHT(at, heads * length, length)
+    assert B.lib().dmi_kv8_attend(cache, batch, q, heads * group, 1.0, out, None, weight, None, 0.0, 256, 1 << 62, None) == B.ERR_INVALID_ARG
+    assert b"launch" in B.lib().dmi_last_error()
+
+
+def test_evict_past_the_workgroups_of_a_launch():
+    heads, keep, at = 1024, 1 << 24, _pointer()
+    cache = B._PACK_KV8(at, at, at, at, 16 * heads * 64, heads * 64, 64, heads, 1, 16, heads, 64, 1, 64, keep // 16, at, keep // 16)
+    batch = B._PACK_KV8_BATCH(64, 0, 0, keep, at, 0, 0)
+    w, to_w = (B._PACK_KV8_WEIGHT(x, heads * keep, keep) for x in (at, at + 64))
+    assert B.lib().dmi_kv8_evict(cache, batch, w, cache, to_w, keep, 1, at, at + 128, None) == B.ERR_INVALID_ARG
+    assert b"launch" in B.lib().dmi_last_error()
+
+
+def test_append_past_the_workgroups_of_a_launch():
+    heads, new, at = 1024, 1 << 24, _pointer()
+    cache = B._PACK_KV8(at, at, at, at, 16 * heads * 64, heads * 64, 64, heads, 1, 16, heads, 64, 1, 1, new // 16, at, new // 16)
+    batch = B._PACK_KV8_BATCH(1, new, new, new, at, at, 0)
+    x = B._PACK_KV8_HEADS(at, B.DT_BF16, heads * 64, 64)
+    assert B.lib().dmi_kv8_append(cache, batch, x, x, None) == B.ERR_INVALID_ARG
+    assert b"launch" in B.lib().dmi_last_error()
