@@ -98,7 +98,7 @@ dmi_status_t dmi_kv8_append(const dmi_kv8_t *cache /*[host]*/, const dmi_kv8_bat
  *   q, out     BF16 or FP16, the same; total_new rows of n_q_heads heads (fewer than 2^31 of them in all)
  *   lse_dev    [device, optional] fp32 [total_new][n_q_heads]
  *   weight     [host, optional] for every request, head of the cache and position t < len:
- *              weight = decay * prior + sum of p_t over the call's new tokens and the g query heads.
+ *              weight = decay * prior + sum of p_t over the call's new tokens and the g query heads (without new tokens: decay * prior).
  *              prior [host, optional]: the same layout, may be the same memory; positions of new tokens count as 0 in it.
  *   workspace  [device] 256-byte aligned, at least dmi_kv8_attend_workspace(...) bytes; contents need not be kept.  (That function
  *              looks at sizes alone, and gives 0 for those that this call refuses.)

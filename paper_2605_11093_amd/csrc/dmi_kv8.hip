@@ -148,6 +148,12 @@ AttendPlan plan_attend(uint32_t block_heads, uint32_t dim, const dmi_kv8_batch_t
     AttendPlan p{};
     const uint32_t group = q_heads / block_heads, max_new = std::min(b.max_new, b.total_new);
     const uint64_t rows = (uint64_t)b.total_new * q_heads, shared = (uint64_t)max_new * group;
+    if (!shared) {                              // no request has a query: weights lose their share, nothing else is there to do
+        p.tokens = true;
+        p.t.splits = p.t.ranges = p.t.row_tiles = 1u;
+        p.t.tile_rows = 16u;
+        return p;
+    }
     // Up to 32 rows of queries share a head: tokens_kernel.  Measured (us, tokens / parts; 8 requests of 4000-8000 tokens and 64 of 2000-
     // 4000, 8 heads x 128): 16 rows 38 / 80 and 98 / 253, 32 rows 34 / 44 and 124 / 177, 64 rows 67 / 53 and 182 / 181.
     p.tokens = shared <= 32u;
@@ -174,7 +180,7 @@ AttendPlan plan_attend(uint32_t block_heads, uint32_t dim, const dmi_kv8_batch_t
     }
     TokensPlan &t = p.t;
     t.tile_rows = shared <= 16u || dim > 128u ? 16u : 32u;     // (two tiles of 256 elements take more registers than there are)
-    t.row_tiles = shared ? ((uint32_t)shared + t.tile_rows - 1u) / t.tile_rows : 1u;
+    t.row_tiles = ((uint32_t)shared + t.tile_rows - 1u) / t.tile_rows;
     // As many wavefronts as are resident at once, if there is enough for them; a request's tiles apart from others' where there is not.
     const uint32_t per = block_heads * t.row_tiles;
     const uint64_t tiles = (uint64_t)b.n_reqs * std::max(1u, (b.max_len + 31u) / 32u);
@@ -233,7 +239,7 @@ extern "C" dmi_status_t dmi_kv8_attend(const dmi_kv8_t *cache, const dmi_kv8_bat
     const uint64_t need = plan.bytes;
     if (need && (!workspace || (uintptr_t)workspace % 256u || workspace_bytes < need))
         return fail(DMI_ERR_INVALID_ARG, "workspace must be 256-byte aligned and hold %llu bytes", (unsigned long long)need);
-    if (!a.b.n_reqs || !a.b.max_new || !a.b.total_new) return DMI_OK;
+    if (!a.b.n_reqs || (!a.b.max_new && !a.w.data)) return DMI_OK;
     a.lse = lse_dev;
     a.decay = a.prior.data ? decay : 0.0f;
     a.scale_log2 = scale * 1.44269504088896340736f;

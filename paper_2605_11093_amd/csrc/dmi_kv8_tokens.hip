@@ -712,6 +712,7 @@ template <typename T> static hipError_t tokens(const AttendArgs &a, const Tokens
     if (!launchable(finish_groups, 256)) return hipErrorInvalidConfiguration;
     const int dp = a.c.dim <= 64 ? 64 : a.c.dim <= 128 ? 128 : 256;
     auto launch = [&](auto dp_, auto nt_) {
+        if (!a.b.max_new) return;               // (no queries: what they would read is not there)
         constexpr int DP = decltype(dp_)::value, NT = decltype(nt_)::value;
         if (p.whole) tokens_kernel<T, DP, NT, true><<<a.b.n_reqs * a.c.heads * p.splits, 64 * waves_of(DP, NT, true), 0, s>>>(a, p);
         else tokens_kernel<T, DP, NT, false><<<(units + 3u) / 4u * 8u, 256, 0, s>>>(a, p);

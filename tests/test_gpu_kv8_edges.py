@@ -36,3 +36,18 @@ def test_lengths_bounded_by_zero(B, new):        # noqa: F811
     out, lse, w = torch.full_like(q, 7.0), torch.full(q.shape[:2], 7.0, device=DEV), torch.full((2, 2, 64), 5.0, device=DEV)
     B.kv8_attend(s.cache, batch, q, out, lse=lse, weight=w, stream=_stream())
     assert (out == 0).all() and (lse == -math.inf).all() and (w == 5.0).all()
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("max_new,max_len", [(0, 90), (1, 90), (64, 90), (64, 2000)])
+def test_weights_where_no_request_has_new_tokens(B, in_place, max_new, max_len):        # noqa: F811
+    s = Setup(B, 34, [(0, 90), (0, 17), (0, 0)], 2, 64, 16, seqs=5, room=130)
+    batch = B.KV8Batch(s.lens, starts=torch.zeros(4, dtype=torch.int32, device=DEV), rows=s.rows_dev, total_new=0, max_new=max_new, max_len=max_len)
+    prior = torch.rand(5, 2, max_len, device=DEV)
+    w = prior.clone() if in_place else torch.full_like(prior, 5.0)
+    want = w.clone()
+    for row, _, _, t in s.spans:
+        want[row, :, :t] = 0.75 * prior[row, :, :t]
+    q = torch.empty(0, 4, 64, dtype=BF16, device=DEV)
+    B.kv8_attend(s.cache, batch, q, q, weight=w, prior=w if in_place else prior, decay=0.75, stream=_stream())
+    assert torch.equal(w, want)
