@@ -95,7 +95,8 @@ dmi_status_t dmi_kv8_append(const dmi_kv8_t *cache /*[host]*/, const dmi_kv8_bat
  *     z_t = scale * q . k_t,   p = softmax(z),   out = sum_t p_t v_t,   lse = log sum_t exp(z_t)
  * A query that sees nothing (or no score above -inf) gives out = 0 and lse = -inf.  A NaN in K makes the queries that see it NaN, a NaN in V that
  * element of theirs.
- *   q, out     BF16 or FP16, the same; total_new rows of n_q_heads heads (fewer than 2^31 of them in all)
+ *   q, out     BF16 or FP16, the same; total_new rows of n_q_heads heads (fewer than 2^31 of them in all).  out may be q, or share no
+ *              element with it; where weights are asked for it shares none
  *   lse_dev    [device, optional] fp32 [total_new][n_q_heads]
  *   weight     [host, optional] for every request, head of the cache and position t < len:
  *              weight = decay * prior + sum of p_t over the call's new tokens and the g query heads (without new tokens: decay * prior).

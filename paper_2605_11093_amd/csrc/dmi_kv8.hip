@@ -98,6 +98,36 @@ dmi_status_t check_rows(const dmi_kv8_heads_t *k, const char *what, const Batch 
     return DMI_OK;
 }
 
+// Whether two tensors of n rows of heads, `size` bytes an element, may share an element: exactly where their strides are the same, by
+// the memory that they reach over where they are not.
+bool share(const Rows &x, const Rows &y, uint32_t n, uint32_t heads, uint32_t dim, uint32_t size)
+{
+    typedef __int128 wide;
+    struct Reach {
+        wide lo, hi;
+    };
+    auto reach = [&](const Rows &r) {
+        const wide row = (wide)r.row_stride * size * (n - 1), head = (wide)r.head_stride * size * (heads - 1), at = (wide)(uintptr_t)r.data;
+        return Reach{at + std::min<wide>(row, 0) + std::min<wide>(head, 0), at + std::max<wide>(row, 0) + std::max<wide>(head, 0) + (wide)dim * size};
+    };
+    if (!n) return false;
+    const Reach a = reach(x), b = reach(y);
+    if (a.hi <= b.lo || b.hi <= a.lo) return false;
+    if ((n > 1 && x.row_stride != y.row_stride) || (heads > 1 && x.head_stride != y.head_stride)) return true;
+    const wide apart = (wide)(uintptr_t)y.data - (wide)(uintptr_t)x.data, length = (wide)dim * size;
+    const wide row = n > 1 ? (wide)x.row_stride * size : 0;
+    for (int64_t h = -(int64_t)heads + 1; h < (int64_t)heads; h++) {
+        const wide d = apart + h * (wide)x.head_stride * size;      // one's element to the other's, of one row
+        wide i = row ? -d / row : 0;                                // rows between them that come nearest: this many, or one more or less
+        for (i--; ; i++) {
+            const wide to = d + i * row;
+            if (i > -(wide)n && i < (wide)n && to < length && -to < length) return true;
+            if (i > (row ? -d / row : 0)) break;
+        }
+    }
+    return false;
+}
+
 dmi_status_t check_weight(const dmi_kv8_weight_t *k, const char *what, Weight &w)
 {
     w = Weight{nullptr, 0, 0};
@@ -231,6 +261,8 @@ extern "C" dmi_status_t dmi_kv8_attend(const dmi_kv8_t *cache, const dmi_kv8_bat
     if (q->dtype != out->dtype || (q->dtype != DMI_DTYPE_BF16 && q->dtype != DMI_DTYPE_FP16))
         return fail(DMI_ERR_INVALID_ARG, "q and out must both be BF16 or both FP16");
     if ((st = check_q_heads(n_q_heads, a.c.heads, a.b.total_new)) != DMI_OK) return st;
+    if (a.w.data && share(a.q, a.out, a.b.total_new, n_q_heads, a.c.dim, 2u))
+        return fail(DMI_ERR_INVALID_ARG, "out and q lie in the same memory, and weights are asked for");
     if (!std::isfinite(scale)) return fail(DMI_ERR_INVALID_ARG, "scale is not finite");
     if ((uintptr_t)lse_dev % 4u) return fail(DMI_ERR_INVALID_ARG, "lse_dev must be 4-byte aligned");
     if (a.prior.data && !a.w.data) return fail(DMI_ERR_INVALID_ARG, "prior without weight");

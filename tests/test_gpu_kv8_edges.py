@@ -51,3 +51,13 @@ def test_weights_where_no_request_has_new_tokens(B, in_place, max_new, max_len):
     q = torch.empty(0, 4, 64, dtype=BF16, device=DEV)
     B.kv8_attend(s.cache, batch, q, q, weight=w, prior=w if in_place else prior, decay=0.75, stream=_stream())
     assert torch.equal(w, want)
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_queries_in_the_outputs_memory(B, new):        # noqa: F811
+    s = Setup(B, 38, [(new, 300), (new, 41)], 2, 64, 16)
+    q, _ = s.values(8, BF16)
+    out = torch.empty_like(q)
+    B.kv8_attend(s.cache, s.batch, q, out, stream=_stream())
+    B.kv8_attend(s.cache, s.batch, q, q, stream=_stream())
+    assert torch.equal(q, out)

@@ -118,3 +118,27 @@ def test_append_past_the_workgroups_of_a_launch():
     x = B._PACK_KV8_HEADS(at, B.DT_BF16, heads * 64, 64)
     assert B.lib().dmi_kv8_append(cache, batch, x, x, None) == B.ERR_INVALID_ARG
     assert b"launch" in B.lib().dmi_last_error()
+
+
+@pytest.mark.parametrize("rows", [1, 40], ids=["few", "many"])
+def test_weights_with_outputs_in_the_queries_memory(rows):
+    """Weights of many query rows are computed behind the outputs, out of the queries: both in one memory are refused, whatever the rows;
+    slices of one tensor that share no element are not."""
+    k = torch.zeros(8, 16, 2, 64, dtype=torch.uint8)
+    c = B.KV8(k, k.clone(), torch.ones(8, 2), torch.ones(8, 2), torch.zeros(1, 4, dtype=torch.int32))
+    batch = B.KV8Batch(torch.ones(1, dtype=torch.int32), max_len=64, starts=torch.zeros(2, dtype=torch.int32), total_new=rows, max_new=rows)
+    w, both = torch.zeros(1, 2, 64), torch.zeros(rows, 8, 144, dtype=torch.bfloat16)
+
+    def call(q, out, weight):
+        with pytest.raises(B.DmiError) as e:    # (refused, or no device to launch on)
+            B.kv8_attend(c, batch, q, out, weight=weight)
+        return "same memory" in str(e.value)
+    q = both[:, :4, :64]
+    assert call(q, q, w) and not call(q, q, None)
+    assert call(q, both[:, 2:6, :64], w) and call(q, both[:, 3:7, :64], w)
+    assert call(both[:, :, :64][:, ::2], both[:, :4, 48:112], w) and call(both[:, 1:5, :64], both[:, :4, :64], w)
+    assert not call(q, both[:, 4:, :64], w) and not call(q, both[:, :4, 80:], w) and not call(both[:, ::2, :64], both[:, 1::2, :64], w)
+    assert not call(q, torch.zeros(rows, 4, 64, dtype=torch.bfloat16), w)
+    if rows > 1:
+        wide = torch.zeros(rows + 1, 4, 64, dtype=torch.bfloat16)
+        assert call(wide[1:], wide[:-1], w)
