@@ -2,6 +2,8 @@
 #include "dmi_internal.h"
 #include "dmi_kv8_mfma.h"
 
+#include <cfloat>
+
 namespace dmi {
 namespace kv8 {
 
@@ -280,14 +282,20 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
                     }
             }
             if (p.scores) {
+                // (-inf says that a query does not see a token: its weight is 0 then whatever the row's total, a NaN too)
 #pragma unroll
                 for (int n = 0; n < NT; n++) {
                     const int row = row0 + 16 * n + col;
                     if (row < rows) {
                         float *s = p.scores + ((int64_t)head * a.b.total_new * a.group + (int64_t)q.start * a.group + row) * p.score_stride + t0 + 4 * g;
 #pragma unroll
-                        for (int x = 0; x < 2; x++)
-                            if (t0 + 16 * x < end) *reinterpret_cast<f32x4 *>(s + 16 * x) = z[n][x];
+                        for (int x = 0; x < 2; x++) {
+                            f32x4 kept;
+#pragma unroll
+                            for (int i = 0; i < 4; i++)
+                                kept[i] = full || (4 * g + i < count[x] && t0 + 16 * x + 4 * g + i <= lim[n]) ? fmaxf(z[n][x][i], -FLT_MAX) : -INFINITY;
+                            if (t0 + 16 * x < end) *reinterpret_cast<f32x4 *>(s + 16 * x) = kept;
+                        }
                     }
                 }
             }
@@ -484,7 +492,10 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
             // weights, out of the scores that the same lane wrote
             float total[NT], unused;
 #pragma unroll
-            for (int n = 0; n < NT; n++) total[n] = total_of(16 * n + col, unused);
+            for (int n = 0; n < NT; n++) {
+                total[n] = total_of(16 * n + col, unused);
+                if (total[n] == -INFINITY) total[n] = INFINITY;         // a row that saw nothing weighs nothing
+            }
             const float *prior = a.prior.data + (int64_t)q.row * a.prior.row_stride + (int64_t)head * a.prior.head_stride;
             float *to_w = a.w.data + (int64_t)q.row * a.w.row_stride + (int64_t)head * a.w.head_stride;
             const int older = q.len - q.fresh;
@@ -505,7 +516,7 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
                 for (int e = 0; e < 32; e++) {
                     sum[e] = 0.0f;
 #pragma unroll
-                    for (int n = 0; n < NT; n++) sum[e] += 16 * n + col < rows && total[n] != -INFINITY ? exp2_of(z[n][e / 4][e % 4] - total[n]) : 0.0f;
+                    for (int n = 0; n < NT; n++) sum[e] += 16 * n + col < rows && z[n][e / 4][e % 4] != -INFINITY ? exp2_of(z[n][e / 4][e % 4] - total[n]) : 0.0f;
                 }
                 // over the columns: of two lanes each goes on with half of the tokens
                 halve<8, 16>(sum, col);
@@ -681,13 +692,13 @@ __global__ __launch_bounds__(256) void finish_kernel(AttendArgs a, TokensPlan p)
             const QueryRow w = query_row(a, head, (uint32_t)r);
             const int64_t at = (int64_t)(q.start + w.token) * a.q_heads + w.head;
             const float total = s.from == s.to ? p.totals[at] : total_of<WHOLE>(a, p, s, head, (uint32_t)r, at);
-            if (!lane) totals[r - r0] = total;
+            if (!lane) totals[r - r0] = total == -INFINITY ? INFINITY : total;       // (a row that saw nothing weighs nothing)
         }
         __syncthreads();
         auto add = [&](int r, const f32x4 &x) {
             const float total = totals[r - r0];
 #pragma unroll
-            for (int i = 0; i < 4; i++) sum[i] += total == -INFINITY ? 0.0f : exp2_of(x[i] - total);
+            for (int i = 0; i < 4; i++) sum[i] += x[i] == -INFINITY ? 0.0f : exp2_of(x[i] - total);
         };
         if (!r0) {
 #pragma unroll

@@ -61,3 +61,14 @@ def test_queries_in_the_outputs_memory(B, new):        # noqa: F811
     B.kv8_attend(s.cache, s.batch, q, out, stream=_stream())
     B.kv8_attend(s.cache, s.batch, q, q, stream=_stream())
     assert torch.equal(q, out)
+
+
+@pytest.mark.parametrize("spans", [[(3, 90), (2, 20)], [(3, 3000), (2, 70)], [(3, 90 + i) for i in range(40)], [(30, 90), (20, 50)], [(40, 1400)]],
+                         ids=["whole", "splits", "ranges", "parts", "partsplits"])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_weights_of_tokens_that_a_spoiled_query_does_not_see(B, spans, bad):        # noqa: F811
+    s = Setup(B, 35, spans, 2, 64, 16)
+    q = s.values(8, BF16)
+    for _, start, _, _ in s.spans:
+        q[0][start, 3, 5], q[1][start, 3, 5] = bad, bad
+    _check_attend(B, s, BF16, 4, q=q)
