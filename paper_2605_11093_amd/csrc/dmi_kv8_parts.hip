@@ -3,6 +3,7 @@
 #include "dmi_kv8_mfma.h"
 
 #include <algorithm>
+#include <cfloat>
 
 namespace dmi {
 namespace kv8 {
@@ -113,7 +114,7 @@ void parts_kernel(AttendArgs a, PartsPlan p)
 
     // the wavefront's query rows; a negative scale goes into their sign
     const uint32_t flip = a.scale_log2 < 0.0f ? 0x80008000u : 0u;
-    const float scale = fmaxf(fabsf(a.scale_log2), 1e-30f);     // (-inf times 0 would be no mask)
+    const float scale = fabsf(a.scale_log2);
     const int wave_row = row0 + wave * 32, row = wave_row + col;
     const QueryRow w = query_row(a, head, (uint32_t)row);
     const int lim = row < rows ? older + w.token : -1;          // the last position that the column's query sees
@@ -175,7 +176,7 @@ void parts_kernel(AttendArgs a, PartsPlan p)
         const Places l{(uint32_t)at, (uint32_t)(at >> 32), __ballot(there)};
         const float ks = *scale_at(a.c, 0, entry, head), vs = *scale_at(a.c, 1, entry, head);
         between(l);
-        scales[batch & 1][0][lane] = there ? ks * scale : 1.0f;
+        scales[batch & 1][0][lane] = there ? fmaxf(ks * scale, FLT_MIN) : 1.0f;     // (-inf times 0 would be no mask)
         scales[batch & 1][1][lane] = there ? log2_of(vs) : -INFINITY;
         scales[batch & 1][2][lane] = there ? 1.0f / vs : 0.0f;
         return l;

@@ -72,3 +72,15 @@ def test_weights_of_tokens_that_a_spoiled_query_does_not_see(B, spans, bad):    
     for _, start, _, _ in s.spans:
         q[0][start, 3, 5], q[1][start, 3, 5] = bad, bad
     _check_attend(B, s, BF16, 4, q=q)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("new", [1, 40])
+def test_scale_zero_over_a_block_of_zeros(B, dtype, new):        # noqa: F811
+    s = Setup(B, 33, [(new, 100), (new, 45)], 2, 64, 16)
+    for row in s.rows:
+        for block in range(3):
+            e = int(s.table[row, block])
+            s.k[e] = 0
+            s.k_scale[e] = 2.0 ** -100
+    _check_attend(B, s, dtype, 2, scale=0.0, prior=False)
