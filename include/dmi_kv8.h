@@ -33,7 +33,7 @@ extern "C" {
 
 /* The cache.  Element (block b, slot s, head h, dim d) of K or V is the code at
  * base + b*block_stride + s*slot_stride + h*head_stride + d (strides in bytes, the same for K and V); it stands for
- * number(code) * scale, scale at scale_base + b*scale_block_stride + h*scale_head_stride (in floats), positive and finite.
+ * number(code) * scale, scale at scale_base + b*scale_block_stride + h*scale_head_stride (in floats), a positive normal number.
  * k, v 16-byte aligned, strides multiples of 16 bytes, slot_stride from 0 to 2^26.  block_size: a multiple of 16, at most 1024.  head_dim: a multiple of 16, at
  * most 256.  block_table_dev [device] int32 [n_seqs][block_table_stride], of which max_blocks columns are used (rows do not
  * overlap: block_table_stride >= max_blocks): physical block of logical block t / block_size of a sequence. */
@@ -103,8 +103,9 @@ dmi_status_t dmi_kv8_append(const dmi_kv8_t *cache /*[host]*/, const dmi_kv8_bat
  *              prior [host, optional]: the same layout, may be the same memory; positions of new tokens count as 0 in it.
  *   workspace  [device] 256-byte aligned, at least dmi_kv8_attend_workspace(...) bytes; contents need not be kept.  (That function
  *              looks at sizes alone, and gives 0 for those that this call refuses.)
- * Scores, softmax, sums and weights are fp32; products are of q as it is and the codes' exact values; p is rounded to q's type
- * for its product with V.
+ * Scores, softmax, sums and weights are fp32; products are of q as it is and the codes' exact values; p (with what V's scale is between
+ * powers of two) is rounded to q's type for its product with V.  In fp16 the scales that V has within 64 tokens may lie 2^22 apart; what
+ * lies below that is rounded to 2^-32 of the largest.
  */
 uint64_t dmi_kv8_attend_workspace(const dmi_kv8_t *cache /*[host]*/, const dmi_kv8_batch_t *batch /*[host]*/,
                                   uint32_t n_q_heads, int with_weight);

@@ -17,11 +17,11 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 struct Bf16 {
     static constexpr bool kNarrow = false;      // as wide a range of exponents as fp32
     static constexpr uint32_t kOne = 0x3F80u;
-    // two neighbouring codes of a word
-    static __device__ __forceinline__ uint32_t two_codes(uint32_t w, bool hi)
+    // two neighbouring codes of a word, times a power of two
+    static __device__ __forceinline__ uint32_t two_codes(uint32_t w, bool hi, float power = 1.0f)
     {
-        return __builtin_bit_cast(uint32_t, hi ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true)
-                                               : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false));
+        return __builtin_bit_cast(uint32_t, hi ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, power, true)
+                                               : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, power, false));
     }
     static __device__ __forceinline__ uint32_t pack(float a, float b)
     {
@@ -41,10 +41,10 @@ struct Bf16 {
 struct Fp16 {
     static constexpr bool kNarrow = true;
     static constexpr uint32_t kOne = 0x3C00u;
-    static __device__ __forceinline__ uint32_t two_codes(uint32_t w, bool hi)
+    static __device__ __forceinline__ uint32_t two_codes(uint32_t w, bool hi, float power = 1.0f)
     {
-        return __builtin_bit_cast(uint32_t, hi ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, true)
-                                               : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, false));
+        return __builtin_bit_cast(uint32_t, hi ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, power, true)
+                                               : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, power, false));
     }
     static __device__ __forceinline__ uint32_t pack(float a, float b)
     {
@@ -116,6 +116,26 @@ template <int BIT, int N> __device__ __forceinline__ void halve(float *x, int la
 // Scores may rise this far (as powers of two) above the maximum that p is taken against before everything is taken against
 // a new one: p stays below 2^8, which costs no precision, and the rescaling becomes rare.
 constexpr float kSlack = 8.0f;
+
+// V's scale is m 2^e, 1 <= m < 2.  m goes into p, in fp32 and before p's one rounding; 2^e goes into the codes as they are converted,
+// without one: bf16 holds every code times 2^-117 to 2^119.  fp16 holds them times 2^-15 to 2^7.  There outputs are summed in units of
+// 2^unit and codes converted times 2^(e - unit); a tile some of whose scales lie outside of that takes another unit, to which the sums are
+// brought first (in fp32, by a power of two: nothing is rounded).  Where a tile's own scales are further apart than 2^22 the largest
+// ones are held exactly and the others to 2^-32 of them: less than half of fp16's smallest number, as long as V's own numbers
+// are none that fp16 cannot hold.  So is what a scale below 2^-40 stands for, which therefore moves no unit.
+__device__ __forceinline__ int exponent_of(uint32_t bits) { return max((int)(bits >> 23), 1) - 127; }
+__device__ __forceinline__ float mantissa_of(uint32_t bits) { return bits >> 23 ? __uint_as_float((bits & 0x7FFFFFu) | 0x3F800000u) : 1.0f; }
+__device__ __forceinline__ float power_of(int e) { return __uint_as_float((uint32_t)(max(e, -126) + 127) << 23); }
+constexpr int kLeast = -15, kMost = 7, kFaint = -40;
+__device__ __forceinline__ bool outside(int e, int unit) { return e >= kFaint && (e < unit + kLeast || e > unit + kMost); }
+template <int N> __device__ __forceinline__ int unit_for(int unit, const int (&e)[N])
+{
+    int hi = kFaint, lo = 127;                  // of the scales that count
+#pragma unroll
+    for (int x = 0; x < N; x++) hi = max(hi, e[x]), lo = min(lo, e[x] < kFaint ? 127 : e[x]);
+    if (lo == 127 || (hi <= unit + kMost && lo >= unit + kLeast)) return unit;
+    return max(hi - kMost, min(hi, lo - kLeast));
+}
 
 // The top bit of every byte of w that is a NaN.
 __device__ __forceinline__ uint32_t nan_codes(uint32_t w) { return ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u; }

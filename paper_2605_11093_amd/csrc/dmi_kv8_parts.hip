@@ -59,7 +59,7 @@ void parts_kernel(AttendArgs a, PartsPlan p)
     // NaNs in V: the last tile, counted from 1, that had one (in an eight); a bit for each of 4 tokens
     __shared__ int nan_any[2], nan_tile[2][8];
     __shared__ __align__(4) uint8_t nan_bits[2][8][2][DP];
-    // scales of sixteens: K's, V's as a power of two and inverted, of 16 tiles and the next 16
+    // scales of sixteens: K's, log2 and inverse of what V's is between 1 and 2, of 16 tiles and the next 16
     __shared__ __align__(16) float scales[2][3][64];
     auto lk = [&](int tile) { return lds + (tile & 1) * (kTile * KP); };
     auto lv = [&](int tile) { return lds + 2 * kTile * KP + (tile & 1) * (DP * VP); };
@@ -147,6 +147,7 @@ void parts_kernel(AttendArgs a, PartsPlan p)
     struct VCodes {
         uint32_t w[U][VL][4];
         int there[U];                           // tokens of the sixteen
+        float power[U];                         // what codes are converted times
     };
     uint32_t k_off[KL], v_off[VL];              // this lane's offsets in a sixteen: 8 lanes a token of K (4 if it has 64 elements)
 #pragma unroll
@@ -162,8 +163,11 @@ void parts_kernel(AttendArgs a, PartsPlan p)
     // Where sixteens lie, from the first code on: a batch's 64, one a lane (the cache's first, if there is no entry)
     struct Places {
         uint32_t lo, hi;
+        int e;                                  // exponent of V's scale
         uint64_t there;                         // which of them the cache has
+        uint64_t far;                           // fp16: whose scale lies outside of the unit's reach
     };
+    int unit = 0;                               // of the sums over V: see unit_for
     // a batch of 16 tiles is looked up, and its scales go into LDS (every wavefront writes the same; what is not there is masked, and
     // weighs nothing); what is done in between does not wait for the scales
     auto look = [&](int batch, auto between) {
@@ -173,12 +177,15 @@ void parts_kernel(AttendArgs a, PartsPlan p)
         const bool there = t < end && block < a.c.max_blocks && (uint32_t)raw < a.c.n_blocks;
         const int entry = there ? raw : 0;
         const int64_t at = (int64_t)entry * a.c.block_stride + (int64_t)((uint32_t)t - block * a.c.bs) * a.c.slot_stride + (int64_t)head * a.c.head_stride;
-        const Places l{(uint32_t)at, (uint32_t)(at >> 32), __ballot(there)};
+        Places l{(uint32_t)at, (uint32_t)(at >> 32), 0, __ballot(there), 0};
         const float ks = *scale_at(a.c, 0, entry, head), vs = *scale_at(a.c, 1, entry, head);
         between(l);
+        l.e = there ? exponent_of(__float_as_uint(vs)) : -126;
+        if constexpr (T::kNarrow) l.far = __ballot(outside(l.e, unit));
+        const float m = mantissa_of(__float_as_uint(vs));
         scales[batch & 1][0][lane] = there ? fmaxf(ks * scale, FLT_MIN) : 1.0f;     // (-inf times 0 would be no mask)
-        scales[batch & 1][1][lane] = there ? log2_of(vs) : -INFINITY;
-        scales[batch & 1][2][lane] = there ? 1.0f / vs : 0.0f;
+        scales[batch & 1][1][lane] = there ? log2_of(m) : -INFINITY;
+        scales[batch & 1][2][lane] = there ? 1.0f / m : 0.0f;
         return l;
     };
     auto fetch = [&](int tile, const Places &p, KCodes &k, VCodes &v) {
@@ -210,6 +217,19 @@ void parts_kernel(AttendArgs a, PartsPlan p)
                     *reinterpret_cast<u32x4 *>(to + 16) = u32x4{T::two_codes(k[2], false), T::two_codes(k[2], true), T::two_codes(k[3], false), T::two_codes(k[3], true)};
                 }
             }
+    };
+    // What V's codes are converted times, in the unit of the tile; which of the batch's scales lie outside of its reach
+    auto powers = [&](int tile, int exponents, uint64_t far, VCodes &v) {
+        auto exponent_in = [&](int x) { return __builtin_amdgcn_readlane(exponents, (4 * tile + x) & 63); };
+        if constexpr (T::kNarrow) {
+            if (far >> (4 * tile & 63) & 15u) {
+                unit = unit_for(unit, {exponent_in(0), exponent_in(1), exponent_in(2), exponent_in(3)});
+                far = __ballot(outside(exponents, unit));
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; u++) v.power[u] = power_of(exponent_in((wave + NW * u) >> 1) - unit);
+        return far;
     };
     // V's codes as they come: nothing where there is no token, and 0 in a NaN's place (the queries that see it are given it apart)
     auto clean_v = [&](VCodes &r, int tile) {
@@ -261,8 +281,8 @@ void parts_kernel(AttendArgs a, PartsPlan p)
                 for (int i = 0; i < 2; i++) {
                     const uint32_t lo = __builtin_amdgcn_perm(v[2 * i + 1], v[2 * i], 0x05010400u);
                     const uint32_t hi = __builtin_amdgcn_perm(v[2 * i + 1], v[2 * i], 0x07030602u);
-                    e[0][i] = T::two_codes(lo, false), e[1][i] = T::two_codes(lo, true);
-                    e[2][i] = T::two_codes(hi, false), e[3][i] = T::two_codes(hi, true);
+                    e[0][i] = T::two_codes(lo, false, r.power[u]), e[1][i] = T::two_codes(lo, true, r.power[u]);
+                    e[2][i] = T::two_codes(hi, false, r.power[u]), e[3][i] = T::two_codes(hi, true, r.power[u]);
                 }
                 if (DP > 64 || lane < 32) {
 #pragma unroll
@@ -278,7 +298,8 @@ void parts_kernel(AttendArgs a, PartsPlan p)
         return *reinterpret_cast<const u32x4 *>(lv(tile) + (32 * (i % ND) + col) * VP + 16 * chunk_of(col, 2 * (i / ND) + half));
     };
 
-    float m = -INFINITY, base = 0.0f, l = 0.0f, lift_ref = T::kNarrow ? -INFINITY : 0.0f;
+    float m = -INFINITY, base = 0.0f, l = 0.0f;
+    int ref = 0;                                // outputs are sums in units of 2^ref
     f32x16 o[ND];
 #pragma unroll
     for (int d = 0; d < ND; d++)
@@ -319,6 +340,7 @@ void parts_kernel(AttendArgs a, PartsPlan p)
         for (int k = 0; k < KK; k++)
 #pragma unroll
             for (int i = 0; i < 4; i++) qf[k][i] = 16 * k + 8 * half < (int)a.c.dim ? qf[k][i] ^ flip : 0u;
+        now.far = powers(0, now.e, now.far, vc);
         clean_v(vc, 0);
         place_v(vc, 0);
         place_k(kc, 0);
@@ -374,6 +396,15 @@ void parts_kernel(AttendArgs a, PartsPlan p)
                     for (int i = 0; i < 8; i++) t = __builtin_amdgcn_fmed3f(t, z[x >> 1][8 * (x & 1) + i], INFINITY);
                     top = fmaxf(top, t * ks[x]);
                 }
+                if constexpr (T::kNarrow) {
+                    if (unit != ref) {          // the sums in the tile's unit
+#pragma unroll
+                        for (int d = 0; d < ND; d++)
+#pragma unroll
+                            for (int i = 0; i < 16; i++) o[d][i] = __builtin_ldexpf(o[d][i], ref - unit);
+                        ref = unit;
+                    }
+                }
                 if (__ballot(top > m + kSlack)) {       // the sums against a higher maximum
                     const float to = fmaxf(m, fmaxf(top, __shfl_xor(top, 32)));
                     const float f = to == -INFINITY ? 1.0f : exp2_of(m - to);
@@ -383,22 +414,7 @@ void parts_kernel(AttendArgs a, PartsPlan p)
 #pragma unroll
                     for (int d = 0; d < ND; d++) o[d] *= f;
                 }
-                if constexpr (T::kNarrow) {     // V's scale relative to the largest yet, to stay within fp16's range
-                    const float largest = fmaxf(fmaxf(lift[0], lift[1]), fmaxf(lift[2], lift[3]));
-                    if (__ballot(largest > lift_ref)) {
-                        const float f = exp2_of(lift_ref - largest);
-#pragma unroll
-                        for (int d = 0; d < ND; d++) o[d] *= f;
-                        lift_ref = largest;
-                    }
-                    const float ref = exp2_of(lift_ref);
-#pragma unroll
-                    for (int x = 0; x < 4; x++) {
-                        lift[x] = lift_ref == -INFINITY ? lift[x] : lift[x] - lift_ref;
-                        inv[x] *= ref;
-                    }
-                }
-                // p, times V's scale (in the exponent; what is summed is divided by it again)
+                // p, times V's scale between 1 and 2 (in the exponent; what is summed is divided by it again)
                 u32x4 pf[4];
 #pragma unroll
                 for (int x = 0; x < 4; x++) {
@@ -420,19 +436,21 @@ void parts_kernel(AttendArgs a, PartsPlan p)
                 }
                 if (nans) give_nans(tile);
             }
+            const bool other = ((tile + 1) & 15) == 0;          // (a batch is not looked at again behind its last tile)
+            now.far = powers(tile + 1, other ? next.e : now.e, other ? next.far : now.far, vc);
+            if (other) next.far = now.far;
             clean_v(vc, tile + 1);
             place_v(vc, tile + 1);
             place_k(kc, tile + 1);
         }
     }
 
-    const float v_ref = T::kNarrow ? exp2_of(lift_ref) : 1.0f;
     l += __shfl_xor(l, 32);
     const int64_t at = (int64_t)(q.start + w.token) * a.q_heads + w.head;
     const bool empty = m == -INFINITY && l == 0.0f;
     if (p.splits == 1) {
         // Rows are put together in LDS, so that a store writes whole ones: as the lanes hold them it would write 16 bytes here and there.
-        const float f = (empty ? 0.0f : 1.0f / l) * v_ref;
+        const float f = __builtin_ldexpf(empty ? 0.0f : 1.0f / l, ref);
         const int64_t dst = (int64_t)(q.start + w.token) * a.out.row_stride + (int64_t)w.head * a.out.head_stride;
         lds_barrier();                          // (the tiles are done with)
 #pragma unroll
@@ -455,6 +473,7 @@ void parts_kernel(AttendArgs a, PartsPlan p)
             if (p.totals) p.totals[at] = sum;
         }
     } else {
+        const float unit = power_of(ref);
         if (row < rows && half == 0) p.sums[at * p.splits + split] = f32x2{m, l};
         const int64_t part = at * p.splits + split;
         lds_barrier();                          // (the tiles are done with)
@@ -465,7 +484,7 @@ void parts_kernel(AttendArgs a, PartsPlan p)
 #pragma unroll
                 for (int i = 0; i < 16; i += 4) {
                     const f32x16 &x = o[h * (ND / 2) + d];
-                    *reinterpret_cast<f32x4 *>(in_row(col, 8 * d + i / 2 + half)) = f32x4{x[i], x[i + 1], x[i + 2], x[i + 3]} * v_ref;
+                    *reinterpret_cast<f32x4 *>(in_row(col, 8 * d + i / 2 + half)) = f32x4{x[i], x[i + 1], x[i + 2], x[i + 3]} * unit;
                 }
 #pragma unroll
             for (int j = 0; j < 32; j += kRows) {

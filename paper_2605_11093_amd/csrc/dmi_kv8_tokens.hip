@@ -216,7 +216,8 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
             }
         };
 
-        float m[NT], base[NT], l[NT], v_ref = T::kNarrow ? 0.0f : 1.0f;
+        float m[NT], base[NT], l[NT];
+        int unit = 0;                           // outputs are sums in units of 2^unit
         f32x4 o[NT][NJ];
 #pragma unroll
         for (int n = 0; n < NT; n++) {
@@ -240,13 +241,15 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
         for (int tile = 0; any_tile && tile < tiles; tile++) {
             const int t0 = begin + 32 * tile, ahead = min(tile + 1, tiles - 1);
             int count[2];
-            float ks[2], vs[2];
+            float ks[2], vs[2];                 // vs: V's scale between 1 and 2, times 2^ve
+            int ve[2];
 #pragma unroll
             for (int x = 0; x < 2; x++) {
                 const int six = 2 * (tile & 31) + x;
                 count[x] = __builtin_amdgcn_readlane(here.entry, six) < 0 ? 0 : min(16, end - t0 - 16 * x);
                 ks[x] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(here.ks), six));
-                vs[x] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(here.vs), six));
+                const uint32_t scale = (uint32_t)__builtin_amdgcn_readlane(__float_as_int(here.vs), six);
+                vs[x] = mantissa_of(scale), ve[x] = exponent_of(scale);
             }
             if ((tile & 31) == 0 && tile + 32 < tiles) behind = look(tile + 32);
             if ((tile & 31) == 31) here = behind;
@@ -307,7 +310,13 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
                                fmaxf(fmaxf(z[n][1][0], z[n][1][1]), fmaxf(z[n][1][2], z[n][1][3])));
                 rises |= top[n] > m[n] + kSlack;
             }
-            if (__ballot(rises)) {
+            int moves = 0;                          // the sums' unit, by so many powers of two
+            if constexpr (T::kNarrow) {
+                const int to = unit_for(unit, ve);
+                moves = unit - to;
+                unit = to;
+            }
+            if (moves || __ballot(rises)) {
 #pragma unroll
                 for (int n = 0; n < NT; n++) {
                     float t = top[n];
@@ -318,23 +327,10 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
                     m[n] = now;
                     base[n] = now == -INFINITY ? 0.0f : now;
                     l[n] *= f;
+                    const float g = T::kNarrow ? __builtin_ldexpf(f, moves) : f;
 #pragma unroll
-                    for (int j = 0; j < NJ; j++) o[n][j] *= f;
+                    for (int j = 0; j < NJ; j++) o[n][j] *= g;
                 }
-            }
-            // V's scale goes into P; in fp16 relative to the largest yet, to stay within its range
-            if constexpr (T::kNarrow) {
-                const float largest = fmaxf(vs[0], vs[1]);
-                if (largest > v_ref) {
-                    const float f = v_ref / largest;
-#pragma unroll
-                    for (int n = 0; n < NT; n++)
-#pragma unroll
-                        for (int j = 0; j < NJ; j++) o[n][j] *= f;
-                    v_ref = largest;
-                }
-                const float inv = v_ref > 0.0f ? 1.0f / v_ref : 0.0f;
-                vs[0] *= inv, vs[1] *= inv;
             }
             u32x4 pf[NT];
 #pragma unroll
@@ -404,11 +400,12 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
                     two[y][1][i] = __builtin_amdgcn_perm(rv[2 * i + 1][y], rv[2 * i][y], 0x07030602u);
                 }
             fetch_v(ahead);
+            const float power[2] = {power_of(ve[0] - unit), power_of(ve[1] - unit)};
 #pragma unroll
             for (int j = 0; j < NJ; j++) {
                 u32x4 vf;
 #pragma unroll
-                for (int i = 0; i < 4; i++) vf[i] = T::two_codes(two[j / 4][j / 2 % 2][i], j % 2);
+                for (int i = 0; i < 4; i++) vf[i] = T::two_codes(two[j / 4][j / 2 % 2][i], j % 2, power[i / 2]);
 #pragma unroll
                 for (int n = 0; n < NT; n++) o[n][j] = T::mfma16(vf, pf[n], o[n][j]);
             }
@@ -445,7 +442,7 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
                 if (g == 0) sums[wave][16 * n + col] = l[n] * f;
 #pragma unroll
                 for (int j = 0; j < NJ; j++) {
-                    o[n][j] *= f * v_ref;
+                    o[n][j] *= __builtin_ldexpf(f, unit);
                     if (wave >= kSlots) joined[wave - kSlots][(n * NJ + j) * 64 + lane] = o[n][j];
                 }
             }
@@ -540,7 +537,7 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
             const int64_t at = (int64_t)(q.start + w.token) * a.q_heads + w.head;
             const bool whole = tiles == seg_tiles;
             const bool empty = m[n] == -INFINITY && l[n] == 0.0f;
-            const float f = (whole ? (empty ? 0.0f : 1.0f / l[n]) : 1.0f) * v_ref;
+            const float f = __builtin_ldexpf(whole ? (empty ? 0.0f : 1.0f / l[n]) : 1.0f, unit);
             // a lane holds DP / 4 elements of its row that follow each other
             if (whole) {
                 uint16_t *dst = static_cast<uint16_t *>(a.out.data) + (int64_t)(q.start + w.token) * a.out.row_stride + (int64_t)w.head * a.out.head_stride;

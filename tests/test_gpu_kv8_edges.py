@@ -84,3 +84,104 @@ def test_scale_zero_over_a_block_of_zeros(B, dtype, new):        # noqa: F811
             s.k[e] = 0
             s.k_scale[e] = 2.0 ** -100
     _check_attend(B, s, dtype, 2, scale=0.0, prior=False)
+
+
+def _bounds(s, q, scale, group, dtype):
+    """What _kv8.attend gives, but fp16's own bound token by token: a p below fp16's normal numbers is off by 2^-25 at most, and by no more
+    than itself, times that token's V; an output below them by 2^-25."""
+    (o, l, w), (do, dl, dw) = K.attend(s.cpu(), s.spans, q, scale, group, BF16)
+    if dtype == BF16:
+        return (o, l, w), (do, dl, dw)
+    cpu, do = s.cpu(), np.zeros_like(do)
+    for row, start, new, length in s.spans:
+        if length <= 0:
+            continue
+        (k, there), (v, _) = cpu.tokens(0, row, length), cpu.tokens(1, row, length)
+        for i in range(new):
+            seen = (np.arange(length) <= length - new + i) & there
+            if not seen.any():
+                continue
+            for g in range(q.shape[1]):
+                ks, vs = k[seen][:, g // group], np.abs(v[seen][:, g // group])
+                z = ks @ q[start + i, g] * scale
+                p = np.exp(z - z.max())
+                p /= p.sum()
+                dz = (s.dim + 8) * K.F * float(np.max(np.abs(ks) @ np.abs(q[start + i, g]))) * abs(scale) + 4 * K.F * float(np.abs(z).max())
+                rel = 2 * dz + (len(z) / 4 + 64) * K.F
+                u = K.U[FP16]
+                do[start + i, g] = u * np.abs(o[start + i, g]) + (u + rel) * (p @ vs) + np.minimum(p, 2.0 ** -25) @ vs + 2.0 ** -25
+    return (o, l, w), (do, dl, dw)
+
+
+def _scales(s, kind, rng):
+    blocks = s.v_scale.shape
+    if kind == "spread":
+        e = rng.integers(-14, 3, blocks)
+    elif kind == "far":
+        e = np.where(rng.random(blocks) < 0.5, -26, 1)
+    elif kind == "tiny":
+        e = rng.integers(-118, -100, blocks)
+    elif kind == "wide":
+        e = rng.integers(-70, 30, blocks)
+    else:
+        e = rng.integers(-7, -4, blocks)
+    x = 2.0 ** e
+    if kind == "odd":
+        x = x * rng.uniform(1, 2, blocks)
+    return torch.from_numpy(x.astype(np.float32)).to(DEV)
+
+
+@pytest.mark.parametrize("spans,group,dim", [
+    ([(1, 300), (1, 40)], 4, 128), ([(3, 200), (3, 33)], 2, 64), ([(1, 3000)], 4, 64), ([(4, 150), (2, 70)], 7, 80), ([(1, 200), (1, 17)], 4, 256),
+    ([(40, 150), (33, 70)], 2, 64), ([(50, 300), (5, 120)], 2, 128), ([(20, 90), (60, 60)], 2, 240), ([(40, 1300)], 2, 128)],
+    ids=["token", "some", "splits", "wide", "256", "parts64", "parts128", "parts240", "partsplits"])
+@pytest.mark.parametrize("dtype,kind", [(FP16, "spread"), (FP16, "far"), (FP16, "odd"), (BF16, "spread"), (BF16, "odd"), (BF16, "tiny"), (BF16, "wide")])
+def test_scales_of_v(B, spans, group, dim, dtype, kind):        # noqa: F811
+    s = Setup(B, 31, spans, 2, dim, 16)
+    s.v_scale.copy_(_scales(s, kind, s.rng))
+    if kind == "odd":
+        s.k_scale.copy_(_scales(s, kind, s.rng))
+    qd, qn = s.values(2 * group, dtype, 1.3)
+    out, lse = torch.empty_like(qd), torch.empty(qd.shape[:2], device=DEV)
+    w = torch.zeros(s.seqs, 2, s.max_len, device=DEV)
+    B.kv8_attend(s.cache, s.batch, qd, out, lse=lse, weight=w, stream=_stream())
+    (o, l, ww), (do, dl, dw) = _bounds(s, qn, dim ** -0.5, group, dtype)
+    K.near(lse.cpu().numpy(), l, dl, "lse")
+    K.near(out.float().cpu().numpy(), o, do, "out")
+    for row, _, _, t in s.spans:
+        K.near(w[row, :, :t].cpu().numpy(), ww[row], dw[row], "weight")
+
+
+@pytest.mark.parametrize("new", [1, 3, 50])
+@pytest.mark.parametrize("dtype", [FP16, BF16])
+def test_a_loud_block_of_no_weight(B, new, dtype):        # noqa: F811
+    s = Setup(B, 32, [(new, 400), (new, 100)], 2, 128, 16)
+    s.v_scale.copy_(_scales(s, "", s.rng))
+    for r, block in ((0, 3), (0, 20), (1, 5)):
+        e = int(s.table[s.rows[r], block])
+        s.k[e] = int(K.nearest_code(-200.0))
+        s.v_scale[e] = 2.0 ** 8
+    qd, qn = s.values(8, dtype, 1.3)
+    qd, qn = qd.abs(), np.abs(qn)
+    out = torch.empty_like(qd)
+    B.kv8_attend(s.cache, s.batch, qd, out, stream=_stream())
+    (o, _, _), (do, _, _) = _bounds(s, qn, 128 ** -0.5, 4, dtype)
+    K.near(out.float().cpu().numpy(), o, do, "out")
+
+
+@pytest.mark.parametrize("dtype", [FP16, BF16])
+@pytest.mark.parametrize("spans,heads", [([(33, 1090 + 7 * i) for i in range(16)], 16), ([(1, 9000)], 2), ([(2, 2000 + i) for i in range(20)], 8)],
+                         ids=["parts", "splits", "ranges"])
+def test_scales_of_v_that_drift(B, dtype, spans, heads):        # noqa: F811
+    """From 2^-30 to 2^4 and back over a long context."""
+    s = Setup(B, 41, spans, heads, 64, 16)
+    for row, _, _, length in s.spans:
+        blocks = -(-length // 16)
+        e = np.round(-13 + 17 * np.sin(np.arange(blocks) / 6.0)).astype(int)
+        s.v_scale[s.table[row, :blocks].long()] = torch.from_numpy(2.0 ** e).float().to(DEV)[:, None].expand(blocks, heads)
+    qd, qn = s.values(heads, dtype, 1.3)
+    out, lse = torch.empty_like(qd), torch.empty(qd.shape[:2], device=DEV)
+    B.kv8_attend(s.cache, s.batch, qd, out, lse=lse, stream=_stream())
+    (o, l, _), (do, dl, _) = _bounds(s, qn, 64 ** -0.5, 1, dtype)
+    K.near(lse.cpu().numpy(), l, dl, "lse")
+    K.near(out.float().cpu().numpy(), o, do, "out")
