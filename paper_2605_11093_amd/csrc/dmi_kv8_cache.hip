@@ -315,6 +315,7 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictArgs a)
 }
 
 constexpr uint32_t kMoveWaves = 4096;           // four on each SIMD
+constexpr int64_t kNowhere = INT64_MIN;         // an offset of codes that are not there (any other may lie on either side of 0)
 
 // One wavefront per (request, head) and as many whole blocks of `to` as 64 tokens make, at least one (just one while that leaves
 // wavefronts to spare: four requests of 8 heads that keep 256 tokens take 6.4 us so and 10.6 with 64 tokens each): where its tokens lie, a token a
@@ -333,18 +334,18 @@ __global__ __launch_bounds__(256) void move_kernel(EvictArgs a, uint32_t blocks,
     if (first >= left) return;
     const uint32_t m = min(span, left - first), per_row = a.c.dim >> 4;
     const int32_t *pos = a.positions + ((int64_t)r * a.c.heads + head) * a.keep + first;
-    // a token's codes (-1: nowhere) and scales
+    // a token's codes and scales
     auto source = [&](uint32_t t, int64_t &at, float &sk, float &sv) {
         const uint32_t p = (uint32_t)pos[t], lb = block_of(a.c, p >> 4);
         const int b = entry_of(a.c, q.row, lb);
-        at = b < 0 ? -1 : (int64_t)b * a.c.block_stride + (int64_t)(p - lb * a.c.bs) * a.c.slot_stride + (int64_t)head * a.c.head_stride;
+        at = b < 0 ? kNowhere : (int64_t)b * a.c.block_stride + (int64_t)(p - lb * a.c.bs) * a.c.slot_stride + (int64_t)head * a.c.head_stride;
         sk = b < 0 ? 0.0f : *scale_at(a.c, 0, b, head);
         sv = b < 0 ? 0.0f : *scale_at(a.c, 1, b, head);
     };
-    int64_t at = -1;
+    int64_t at = kNowhere;
     float sk = 0.0f, sv = 0.0f, most_k = 0.0f, most_v = 0.0f;       // the largest: of the block that the lane's token joins
     for (uint32_t t0 = 0; t0 < m; t0 += 64u) {      // (more than one round only for blocks of more than 64 tokens)
-        at = -1, sk = sv = 0.0f;
+        at = kNowhere, sk = sv = 0.0f;
         if (t0 + lane < m) source(t0 + lane, at, sk, sv);
         most_k = fmaxf(most_k, sk);
         most_v = fmaxf(most_v, sv);
@@ -357,7 +358,7 @@ __global__ __launch_bounds__(256) void move_kernel(EvictArgs a, uint32_t blocks,
     const int to = lane < blocks ? entry_of(a.to, q.row, nth * blocks + lane) : -1;
     for (uint32_t t0 = 0; t0 < m; t0 += 64u) {
         if (m > 64u) {
-            at = -1, sk = sv = 0.0f;
+            at = kNowhere, sk = sv = 0.0f;
             if (t0 + lane < m) source(t0 + lane, at, sk, sv);
         }
         const float fk = sk / most_k, fv = sv / most_v;
@@ -376,16 +377,16 @@ __global__ __launch_bounds__(256) void move_kernel(EvictArgs a, uint32_t blocks,
                 const uint32_t slot = t0 + t, block = blocks == 1u ? 0u : slot / a.c.bs;
                 const int e = __shfl(to, (int)(block & 63u));
                 dst[j] = u < units && e >= 0 ? (int64_t)e * a.to.block_stride + (int64_t)(slot - block * a.c.bs) * a.to.slot_stride +
-                                                   (int64_t)head * a.to.head_stride + part : -1;
+                                                   (int64_t)head * a.to.head_stride + part : kNowhere;
                 wk[j] = wv[j] = u32x4{0u, 0u, 0u, 0u};
-                if (dst[j] >= 0 && src >= 0) {
+                if (dst[j] != kNowhere && src != kNowhere) {
                     wk[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(a.c.code[0] + src + part));
                     wv[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(a.c.code[1] + src + part));
                 }
             }
 #pragma unroll
             for (int j = 0; j < 4; j++) {
-                if (dst[j] < 0) continue;
+                if (dst[j] == kNowhere) continue;
                 if (gk[j] != 1.0f) {
 #pragma unroll
                     for (int i = 0; i < 4; i++) wk[j][i] = scaled_codes(wk[j][i], gk[j]);

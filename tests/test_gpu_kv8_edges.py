@@ -185,3 +185,35 @@ def test_scales_of_v_that_drift(B, dtype, spans, heads):        # noqa: F811
     (o, l, _), (do, dl, _) = _bounds(s, qn, 64 ** -0.5, 1, dtype)
     K.near(lse.cpu().numpy(), l, dl, "lse")
     K.near(out.float().cpu().numpy(), o, do, "out")
+
+
+def test_evict_with_blocks_that_lie_backwards(B):        # noqa: F811
+    """block_stride and head_stride below zero, in both caches."""
+    s, to = Setup(B, 39, [(0, 200), (0, 30)], 2, 64, 16), Setup(B, 40, [(0, 64)] * 2, 2, 64, 16)
+    weight = torch.rand(2, 2, 200, device=DEV)
+
+    def call(cache, dst):
+        positions, lens = torch.empty(2, 2, 64, dtype=torch.int32, device=DEV), torch.empty(2, dtype=torch.int32, device=DEV)
+        to_w = torch.zeros(2, 2, 64, device=DEV)
+        B.kv8_evict(cache, s.batch, weight, dst, to_w, keep=64, recent=9, positions=positions, lens=lens, stream=_stream())
+        return positions, lens, to_w
+
+    def backwards(x):
+        """The same blocks and heads in memory in the other order; element (0, 0, 0, 0) is the last block's last head."""
+        k, v = (y.flip(0, 2).contiguous() for y in (x.k, x.v))
+        c = B.KV8(k, v, x.k_scale, x.v_scale, x.table)
+        at = (k.shape[0] - 1) * k.stride(0) + (k.shape[2] - 1) * k.stride(2)
+        c._raw = B._PACK_KV8(k.data_ptr() + at, v.data_ptr() + at, x.k_scale.data_ptr(), x.v_scale.data_ptr(), -k.stride(0), k.stride(1), -k.stride(2),
+                             x.k_scale.stride(0), x.k_scale.stride(1), k.shape[1], k.shape[2], k.shape[3], k.shape[0], x.table.shape[0],
+                             x.table.shape[1], x.table.data_ptr(), x.table.stride(0))
+        return c, k, v
+    c, _, _ = backwards(s)
+    t, tk, tv = backwards(to)
+    scales = to.k_scale.clone(), to.v_scale.clone()
+    got = call(c, t)
+    got_scales = to.k_scale.clone(), to.v_scale.clone()
+    to.k_scale.copy_(scales[0]), to.v_scale.copy_(scales[1])
+    want = call(s.cache, to.cache)
+    for x, y in zip((*got, *got_scales), (*want, to.k_scale, to.v_scale)):
+        assert torch.equal(x.nan_to_num(-1), y.nan_to_num(-1))
+    assert torch.equal(tk.flip(0, 2), to.k) and torch.equal(tv.flip(0, 2), to.v)
