@@ -26,8 +26,8 @@ template <typename T> struct Eight {
     }
     __device__ __forceinline__ void numbers(float x[8]) const;
 };
-struct Bf16 { uint16_t u; };
-template <> __device__ __forceinline__ void Eight<Bf16>::numbers(float x[8]) const
+struct Bf16Bits { uint16_t u; };
+template <> __device__ __forceinline__ void Eight<Bf16Bits>::numbers(float x[8]) const
 {
 #pragma unroll
     for (int i = 0; i < 4; i++) {
@@ -182,7 +182,7 @@ hipError_t launch_append(AppendArgs a, uint32_t dtype, hipStream_t s)
     if (!launchable(groups, 256)) return hipErrorInvalidConfiguration;
     const dim3 grid((uint32_t)groups, a.counted ? 1u : a.b.n_reqs);
     switch (dtype) {
-    case DMI_DTYPE_BF16: append_kernel<Bf16><<<grid, 256, 0, s>>>(a); break;
+    case DMI_DTYPE_BF16: append_kernel<Bf16Bits><<<grid, 256, 0, s>>>(a); break;
     case DMI_DTYPE_FP16: append_kernel<_Float16><<<grid, 256, 0, s>>>(a); break;
     default: append_kernel<float><<<grid, 256, 0, s>>>(a); break;
     }
