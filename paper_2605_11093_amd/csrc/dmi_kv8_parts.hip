@@ -10,22 +10,17 @@ namespace kv8 {
 
 constexpr int kTile = 64;                       // tokens that a workgroup has in LDS at a time
 
-// What is looked up of sixteens of tokens, one a lane: entry of the block table, K's scale, V's as a power of two and inverted.
+// What is looked up of sixteens of tokens, one a lane: entry of the block table, K's scale.
 struct Look {
     int entry;
-    float ks, lift, inv;
+    float ks;
 };
 __device__ __forceinline__ Look look_up(const AttendArgs &a, const Request &q, uint32_t head, int t, int end, float scale)
 {
-    Look l{-1, 1.0f, -INFINITY, 0.0f};          // (what is not there is masked, and weighs nothing)
+    Look l{-1, 1.0f};
     if (t < end) {
         l.entry = entry_of(a.c, q.row, block_of(a.c, (uint32_t)t >> 4));
-        if (l.entry >= 0) {
-            const float vs = *scale_at(a.c, 1, l.entry, head);
-            l.ks = *scale_at(a.c, 0, l.entry, head) * scale;
-            l.lift = log2_of(vs);
-            l.inv = 1.0f / vs;
-        }
+        if (l.entry >= 0) l.ks = *scale_at(a.c, 0, l.entry, head) * scale;
     }
     return l;
 }
