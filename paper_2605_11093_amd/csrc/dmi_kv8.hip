@@ -186,7 +186,7 @@ AttendPlan plan_attend(uint32_t block_heads, uint32_t dim, const dmi_kv8_batch_t
     }
     // Up to 32 rows of queries share a head: tokens_kernel.  Measured (us, tokens / parts; 8 requests of 4000-8000 tokens and 64 of 2000-
     // 4000, 8 heads x 128): 16 rows 38 / 80 and 98 / 253, 32 rows 34 / 44 and 124 / 177, 64 rows 67 / 53 and 182 / 181.
-    p.tokens = shared <= 32u;
+    p.tokens = shared <= kFewRows;
     if (!p.tokens) {
         PartsPlan &m = p.many;
         const uint32_t rows_each = dim <= 128u ? 256u : 128u;

@@ -66,6 +66,8 @@ struct AttendArgs {
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
+constexpr uint32_t kFewRows = 32;               // query rows that share a head: up to here by tokens_kernel
+
 // How few query rows are attended to: see dmi_kv8_tokens.hip.
 struct TokensPlan {
     bool whole;                                 // a workgroup takes a request and head, or one of its equal splits: no ranges

@@ -620,7 +620,7 @@ template <bool WHOLE> __device__ __forceinline__ float total_of(const AttendArgs
 template <typename T, bool WHOLE>
 __global__ __launch_bounds__(256) void finish_kernel(AttendArgs a, TokensPlan p)
 {
-    __shared__ float totals[256];
+    __shared__ float totals[kFewRows];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const Request q = request_of(a.b, a.c, (int)blockIdx.y);
     const uint32_t rows = (uint32_t)q.fresh * a.group;
@@ -681,31 +681,25 @@ __global__ __launch_bounds__(256) void finish_kernel(AttendArgs a, TokensPlan p)
         for (int i = 0; i < 4; i++) before[i] = prior[max(min(t + i, older - 1), 0)];
     }
     const Spread s = spread_of<WHOLE>(a, p, blockIdx.y);
+    for (int r = wave; r < (int)rows; r += 4) {
+        const QueryRow w = query_row(a, head, (uint32_t)r);
+        const int64_t at = (int64_t)(q.start + w.token) * a.q_heads + w.head;
+        const float total = s.from == s.to ? p.totals[at] : total_of<WHOLE>(a, p, s, head, (uint32_t)r, at);
+        if (!lane) totals[r] = total == -INFINITY ? INFINITY : total;       // (a row that saw nothing weighs nothing)
+    }
+    __syncthreads();
     f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int r0 = 0; r0 < (int)rows; r0 += 256) {
-        const int r1 = min((int)rows, r0 + 256);
-        if (r0) __syncthreads();
-        for (int r = r0 + wave; r < r1; r += 4) {
-            const QueryRow w = query_row(a, head, (uint32_t)r);
-            const int64_t at = (int64_t)(q.start + w.token) * a.q_heads + w.head;
-            const float total = s.from == s.to ? p.totals[at] : total_of<WHOLE>(a, p, s, head, (uint32_t)r, at);
-            if (!lane) totals[r - r0] = total == -INFINITY ? INFINITY : total;       // (a row that saw nothing weighs nothing)
-        }
-        __syncthreads();
-        auto add = [&](int r, const f32x4 &x) {
-            const float total = totals[r - r0];
+    auto add = [&](int r, const f32x4 &x) {
+        const float total = totals[r];
 #pragma unroll
-            for (int i = 0; i < 4; i++) sum[i] += x[i] == -INFINITY ? 0.0f : exp2_of(x[i] - total);
-        };
-        if (!r0) {
+        for (int i = 0; i < 4; i++) sum[i] += x[i] == -INFINITY ? 0.0f : exp2_of(x[i] - total);
+    };
 #pragma unroll
-            for (int r = 0; r < kFirst; r++)
-                if (r < r1) add(r, z[r]);
-        }
-        if (t < q.len) {
+    for (int r = 0; r < kFirst; r++)
+        if (r < (int)rows) add(r, z[r]);
+    if (t < q.len) {
 #pragma unroll 4
-            for (int r = r0 ? r0 : kFirst; r < r1; r++) add(r, *reinterpret_cast<const f32x4 *>(scores + (int64_t)r * p.score_stride));
-        }
+        for (int r = kFirst; r < (int)rows; r++) add(r, *reinterpret_cast<const f32x4 *>(scores + (int64_t)r * p.score_stride));
     }
     float *to = a.w.data + (int64_t)q.row * a.w.row_stride + (int64_t)head * a.w.head_stride;
 #pragma unroll
