@@ -94,6 +94,14 @@ __device__ __forceinline__ void lds_barrier()
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
+// The same among the lanes of one wavefront, whose accesses to LDS are carried out in order: only the compiler has to keep it.
+__device__ __forceinline__ void lds_handover()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float log2_of(float x) { return __builtin_amdgcn_logf(x); }
 constexpr float kLn2 = 0.693147180559945309417f;

@@ -328,6 +328,7 @@ void parts_kernel(AttendArgs a, PartsPlan p)
         Places now = look(0, [&](const Places &l) { fetch(0, l, kc, vc); }), next = now;
 #pragma unroll
         for (int k = 0; k < KK; k++) *reinterpret_cast<u32x4 *>(in_row(k * kRows + lane / kChunks, lane % kChunks)) = qf[k];
+        lds_handover();
 #pragma unroll
         for (int k = 0; k < KK; k++) qf[k] = *reinterpret_cast<const u32x4 *>(in_row(col, 2 * k + half));
         lds_barrier();                          // (the NaN flags are cleared, and the rows read)
@@ -454,6 +455,7 @@ void parts_kernel(AttendArgs a, PartsPlan p)
             for (int i = 0; i < 16; i += 4)
                 *reinterpret_cast<u32x2 *>(in_row(col, 4 * d + i / 4) + 8 * half) =
                     u32x2{T::pack(o[d][i] * f, o[d][i + 1] * f), T::pack(o[d][i + 2] * f, o[d][i + 3] * f)};
+        lds_handover();
 #pragma unroll
         for (int j = 0; j < 32; j += kRows) {
             const int r = j + lane / kChunks, chunk = lane % kChunks;
@@ -481,6 +483,7 @@ void parts_kernel(AttendArgs a, PartsPlan p)
                     const f32x16 &x = o[h * (ND / 2) + d];
                     *reinterpret_cast<f32x4 *>(in_row(col, 8 * d + i / 2 + half)) = f32x4{x[i], x[i + 1], x[i + 2], x[i + 3]} * unit;
                 }
+            lds_handover();
 #pragma unroll
             for (int j = 0; j < 32; j += kRows) {
                 const int r = j + lane / kChunks, e = h * (DP / 2) + 4 * (lane % kChunks);
@@ -488,6 +491,7 @@ void parts_kernel(AttendArgs a, PartsPlan p)
                 const int64_t to = (int64_t)(uint32_t)__shfl((int)(uint32_t)part, r) | (int64_t)__shfl((int)(part >> 32), r) << 32;
                 if (wave_row + r < rows && e < (int)a.c.dim) *reinterpret_cast<f32x4 *>(p.parts + to * a.c.dim + e) = x;
             }
+            lds_handover();
         }
     }
 }
