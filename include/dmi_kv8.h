@@ -56,7 +56,7 @@ typedef struct {
  *              (total_new = n_reqs, max_new = 1).
  *   rows_dev   [device, optional] n_reqs different rows of the block table (and of weights); NULL: request r has row r.
  * total_new, max_new, max_len are upper bounds of the rows, of one request's new tokens and of the lengths: launches
- * are sized by them. */
+ * are sized by them (n_reqs * max_len at most 2^35 for dmi_kv8_attend). */
 typedef struct {
     uint32_t n_reqs, total_new, max_new, max_len;
     const int32_t *lens_dev, *starts_dev, *rows_dev;
@@ -95,7 +95,7 @@ dmi_status_t dmi_kv8_append(const dmi_kv8_t *cache /*[host]*/, const dmi_kv8_bat
  *     z_t = scale * q . k_t,   p = softmax(z),   out = sum_t p_t v_t,   lse = log sum_t exp(z_t)
  * A query that sees nothing (or no score above -inf) gives out = 0 and lse = -inf.  A NaN in K makes the queries that see it NaN, a NaN in V that
  * element of theirs.
- *   q, out     BF16 or FP16, the same; total_new rows of n_q_heads heads (fewer than 2^31 of them in all).  out may be q, or share no
+ *   q, out     BF16 or FP16, the same; total_new rows of n_q_heads heads (at most 2^30 of them in all).  out may be q, or share no
  *              element with it; where weights are asked for it shares none
  *   lse_dev    [device, optional] fp32 [total_new][n_q_heads]
  *   weight     [host, optional] for every request, head of the cache and position t < len:

@@ -34,13 +34,18 @@ dmi_status_t check_counts(const dmi_kv8_batch_t *k, bool fresh)
     return DMI_OK;
 }
 
-// Query rows are counted in 31 bits (and the bytes of a float for each of them and of 2^24 tokens in 64).
-dmi_status_t check_q_heads(uint32_t n_q_heads, uint32_t heads, uint32_t total_new)
+// Kernels count query rows, and the tiles of 32 tokens of all contexts, in 31 bits; both with room to round up (and the bytes of a float
+// for each row and 2^24 tokens are counted in 64).
+constexpr uint64_t kMostRows = 1u << 30, kMostTiles = 1u << 30;
+
+dmi_status_t check_attend(uint32_t n_q_heads, uint32_t heads, const dmi_kv8_batch_t &b)
 {
     if (!n_q_heads || n_q_heads % heads || n_q_heads > 65536u)
         return fail(DMI_ERR_INVALID_ARG, "%u query heads do not share %u heads evenly", n_q_heads, heads);
-    if ((uint64_t)total_new * n_q_heads > 0x7FFFFFFFu)
-        return fail(DMI_ERR_INVALID_ARG, "total_new %u rows of %u query heads are more than 2^31 - 1", total_new, n_q_heads);
+    if ((uint64_t)b.total_new * n_q_heads > kMostRows)
+        return fail(DMI_ERR_INVALID_ARG, "total_new %u rows of %u query heads are more than 2^30", b.total_new, n_q_heads);
+    if (b.n_reqs * ((b.max_len + 31ull) / 32u) > kMostTiles)
+        return fail(DMI_ERR_INVALID_ARG, "%u requests of max_len %u are more than 2^35 tokens", b.n_reqs, b.max_len);
     return DMI_OK;
 }
 
@@ -242,7 +247,7 @@ extern "C" uint64_t dmi_kv8_attend_workspace(const dmi_kv8_t *cache, const dmi_k
                                              int with_weight)
 {
     if (!cache || !batch || check_shape(cache, "cache") != DMI_OK || check_counts(batch, true) != DMI_OK ||
-        check_q_heads(n_q_heads, cache->n_heads, batch->total_new) != DMI_OK)
+        check_attend(n_q_heads, cache->n_heads, *batch) != DMI_OK)
         return 0;
     return plan_attend(cache->n_heads, cache->head_dim, *batch, n_q_heads, with_weight != 0).bytes;
 }
@@ -260,7 +265,7 @@ extern "C" dmi_status_t dmi_kv8_attend(const dmi_kv8_t *cache, const dmi_kv8_bat
         return st;
     if (q->dtype != out->dtype || (q->dtype != DMI_DTYPE_BF16 && q->dtype != DMI_DTYPE_FP16))
         return fail(DMI_ERR_INVALID_ARG, "q and out must both be BF16 or both FP16");
-    if ((st = check_q_heads(n_q_heads, a.c.heads, a.b.total_new)) != DMI_OK) return st;
+    if ((st = check_attend(n_q_heads, a.c.heads, *batch)) != DMI_OK) return st;
     if (a.w.data && share(a.q, a.out, a.b.total_new, n_q_heads, a.c.dim, 2u))
         return fail(DMI_ERR_INVALID_ARG, "out and q lie in the same memory, and weights are asked for");
     if (!std::isfinite(scale)) return fail(DMI_ERR_INVALID_ARG, "scale is not finite");

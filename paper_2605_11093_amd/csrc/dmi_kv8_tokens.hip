@@ -107,6 +107,7 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
             of_range = range_tiles(p, total);
             if (range * of_range >= total) return;
             for (;; r += 64) {
+                if (r >= (int)a.b.n_reqs) return;
                 const int upto = lanes_scan(lane_tiles(a, (uint32_t)r)), sum = __builtin_amdgcn_readlane(upto, 63);
                 if (seg0 + sum <= range * of_range) {
                     seg0 += sum;

@@ -142,3 +142,14 @@ def test_weights_with_outputs_in_the_queries_memory(rows):
     if rows > 1:
         wide = torch.zeros(rows + 1, 4, 64, dtype=torch.bfloat16)
         assert call(wide[1:], wide[:-1], w)
+
+
+def test_more_tokens_than_tiles_are_counted():
+    """Tiles of 32 tokens of all contexts are added up in 31 bits: lengths that a sum would wrap for are refused by their bound."""
+    reqs, length, at = 65535, 1 << 24, _pointer()
+    assert _workspace(1, 64, 1, reqs, reqs, 1, length) == 0 and _workspace(1, 64, 1, 1024, 1024, 1, length) > 0
+    cache = B._PACK_KV8(at, at, at, at, 16 * 64, 64, 64, 1, 1, 16, 1, 64, 1, reqs, length // 16, at, length // 16)
+    batch = B._PACK_KV8_BATCH(reqs, reqs, 1, length, at, 0, 0)
+    q, out = (B._PACK_KV8_HEADS(at + x, B.DT_BF16, 64, 64) for x in (0, 1 << 40))
+    assert B.lib().dmi_kv8_attend(cache, batch, q, 1, 1.0, out, None, None, None, 0.0, 256, 1 << 62, None) == B.ERR_INVALID_ARG
+    assert b"2^35" in B.lib().dmi_last_error()
