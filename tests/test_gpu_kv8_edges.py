@@ -217,3 +217,19 @@ def test_evict_with_blocks_that_lie_backwards(B):        # noqa: F811
     for x, y in zip((*got, *got_scales), (*want, to.k_scale, to.v_scale)):
         assert torch.equal(x.nan_to_num(-1), y.nan_to_num(-1))
     assert torch.equal(tk.flip(0, 2), to.k) and torch.equal(tv.flip(0, 2), to.v)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("spans,group", [([(5, 3), (4, 0), (3, 40)], 4), ([(60, 30), (40, 0), (50, 50), (33, 1)], 2), ([(64, 1400), (80, 20)], 2)],
+                         ids=["few", "many", "splits"])
+def test_more_new_tokens_than_the_length(B, dtype, spans, group):        # noqa: F811
+    """The first of them have no position: they see nothing, and are not stored."""
+    s = Setup(B, 42, spans, 2, 64, 16)
+    _check_attend(B, s, dtype, group)
+    s = Setup(B, 43, spans, 2, 64, 16, fill=False)
+    (key, kn), (value, vn) = s.values(2, dtype, 3.0), s.values(2, dtype, 0.2)
+    cpu = s.cpu()
+    B.kv8_append(s.cache, s.batch, key, value, stream=_stream())
+    K.append(cpu, s.spans, kn, vn)
+    for got, want in ((s.k, cpu.code[0]), (s.v, cpu.code[1])):
+        K.equal_codes(got.cpu().numpy(), want)
