@@ -318,7 +318,9 @@ extern "C" dmi_status_t dmi_kv8_evict(const dmi_kv8_t *cache, const dmi_kv8_batc
         return fail(DMI_ERR_INVALID_ARG, "keep %u is more than to's %u blocks of %u tokens, or than %u", keep, a.to.max_blocks, a.to.bs, kMaxLen);
     if (!positions_dev || !to_lens_dev || (uintptr_t)positions_dev % 4u || (uintptr_t)to_lens_dev % 4u)
         return fail(DMI_ERR_INVALID_ARG, "positions_dev or to_lens_dev is NULL or not 4-byte aligned");
-    if (to_lens_dev == batch->lens_dev) return fail(DMI_ERR_INVALID_ARG, "to_lens_dev is lens_dev");
+    const int64_t apart = (int64_t)((uintptr_t)to_lens_dev - (uintptr_t)batch->lens_dev), length = 4ll * a.b.n_reqs;
+    if (to_lens_dev == batch->lens_dev || (apart < length && -apart < length))
+        return fail(DMI_ERR_INVALID_ARG, "to_lens_dev lies in lens_dev's memory");
     if (a.w.data == a.to_w.data) return fail(DMI_ERR_INVALID_ARG, "to_weight is weight");
     if (!a.b.n_reqs) return DMI_OK;
     a.b.starts = nullptr;

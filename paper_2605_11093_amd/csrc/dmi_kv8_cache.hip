@@ -337,7 +337,7 @@ __global__ __launch_bounds__(256) void move_kernel(EvictArgs a, uint32_t blocks,
     // a token's codes and scales
     auto source = [&](uint32_t t, int64_t &at, float &sk, float &sv) {
         const uint32_t p = (uint32_t)pos[t], lb = block_of(a.c, p >> 4);
-        const int b = entry_of(a.c, q.row, lb);
+        const int b = p < (uint32_t)q.len ? entry_of(a.c, q.row, lb) : -1;     // (a length that is another than select_kernel saw)
         at = b < 0 ? kNowhere : (int64_t)b * a.c.block_stride + (int64_t)(p - lb * a.c.bs) * a.c.slot_stride + (int64_t)head * a.c.head_stride;
         sk = b < 0 ? 0.0f : *scale_at(a.c, 0, b, head);
         sv = b < 0 ? 0.0f : *scale_at(a.c, 1, b, head);

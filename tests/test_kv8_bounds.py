@@ -107,7 +107,7 @@ def test_evict_past_the_workgroups_of_a_launch():
     cache = B._PACK_KV8(at, at, at, at, 16 * heads * 64, heads * 64, 64, heads, 1, 16, heads, 64, 1, 64, keep // 16, at, keep // 16)
     batch = B._PACK_KV8_BATCH(64, 0, 0, keep, at, 0, 0)
     w, to_w = (B._PACK_KV8_WEIGHT(x, heads * keep, keep) for x in (at, at + 64))
-    assert B.lib().dmi_kv8_evict(cache, batch, w, cache, to_w, keep, 1, at, at + 128, None) == B.ERR_INVALID_ARG
+    assert B.lib().dmi_kv8_evict(cache, batch, w, cache, to_w, keep, 1, at, at + 4096, None) == B.ERR_INVALID_ARG
     assert b"launch" in B.lib().dmi_last_error()
 
 
@@ -153,3 +153,14 @@ def test_more_tokens_than_tiles_are_counted():
     q, out = (B._PACK_KV8_HEADS(at + x, B.DT_BF16, 64, 64) for x in (0, 1 << 40))
     assert B.lib().dmi_kv8_attend(cache, batch, q, 1, 1.0, out, None, None, None, 0.0, 256, 1 << 62, None) == B.ERR_INVALID_ARG
     assert b"2^35" in B.lib().dmi_last_error()
+
+
+def test_new_lengths_inside_the_lengths():
+    """to_lens_dev anywhere in lens_dev's memory: the move would take other requests' new lengths for their lengths."""
+    both, w = torch.ones(5, dtype=torch.int32), torch.zeros(2, 3, 2, 64)
+    c, to = (_cache(torch.zeros(3, 4, dtype=torch.int32)) for _ in range(2))
+    positions = torch.zeros(3, 2, 16, dtype=torch.int32)
+    for lens, new in ((both[:3], both[2:]), (both[1:4], both[:3]), (both[:3], both[:3])):
+        with pytest.raises(B.DmiError, match="lens_dev") as e:
+            B.kv8_evict(c, B.KV8Batch(lens, max_len=64), w[0], to, w[1], keep=16, recent=4, positions=positions, lens=new)
+        assert e.value.code == B.ERR_INVALID_ARG
