@@ -197,8 +197,9 @@ AttendPlan plan_attend(uint32_t block_heads, uint32_t dim, const dmi_kv8_batch_t
         const uint32_t rows_each = dim <= 128u ? 256u : 128u;
         m.row_tiles = (uint32_t)((shared + rows_each - 1u) / rows_each);
         // Workgroups run one on each of the 256 compute units: as many splits of the contexts as give the shortest sum of rounds, a
-        // workgroup's start and end counted as three tiles of 64 tokens (parts of four long prompts, 166 groups of rows: two splits
-        // 243 us, three 229, before their parts were stored by whole rows).
+        // workgroup's start and end counted as three tiles of 64 tokens.  What splits write and the join reads is not counted: parts of
+        // four long prompts behind up to 7600 tokens, 8 heads x 128, get six splits (150 MB of parts), and measure, weights included,
+        // 371 us with six, 342 with one, 373 with two, 372 with three, 387 with four.
         const uint64_t bound = (uint64_t)b.n_reqs * m.row_tiles, likely = (uint64_t)b.total_new * group / rows_each + b.n_reqs / 2u + 1u;
         const uint64_t groups = std::min(bound, likely) * block_heads, len_tiles = (b.max_len + 63u) / 64u;
         uint64_t best = ~0ull;

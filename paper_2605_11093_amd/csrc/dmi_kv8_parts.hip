@@ -35,7 +35,8 @@ __device__ __forceinline__ float lane_value(float v, int lane) { return __int_as
 // Bound by neither pipe alone: a tile takes a wavefront 32 matrix instructions (1280 cycles) and some 280 vector ones (1500), 112 of
 // them to stage, and the two wavefronts of a SIMD together 6000 cycles: they leave the barrier together and so want the same pipe
 // at the same time; a workgroup's start and end cost as much as four tiles of its dozen.  32 ragged prompts of 128-2048 tokens, 32 query
-// heads over 8: 585 us, 766 TFLOP/s (a large product of the library: 1250); parts of four long prompts 222 us, 790 TFLOP/s.  Queries and
+// heads over 8: 585 to 603 us by card, 746 to 768 TFLOP/s (a large product of the library: 1250); parts of four long prompts, six splits,
+// 222 to 232 us, 755 to 790 TFLOP/s.  In fp16 and with 256 elements 2 to 3 % more.  Queries and
 // outputs that went between memory and the lanes without LDS cost 33 us of it.  Measured and not better (before that, at 620): one
 // wavefront of 64 rows a SIMD (spills), the second four wavefronts half a tile behind the first (658), staging between the
 // instructions of a product (627-671), two workgroups of four wavefronts (634), priorities (624-639), a maximum looked for only where
@@ -498,7 +499,7 @@ void parts_kernel(AttendArgs a, PartsPlan p)
 
 // Outputs out of the parts that splits of the contexts left: a row by as many lanes as take four elements each of it, in one pass with
 // the running maximum (and then another row, where a request has more than a launch has workgroups for).  Bound by memory and its
-// latency: 48000 rows of 128 elements out of three parts, 86 MB, 24 us.
+// latency: 48000 rows of 128 elements out of six parts, 150 MB, 25 us.
 template <typename T>
 __global__ __launch_bounds__(256) void join_parts_kernel(AttendArgs a, PartsPlan p, uint32_t tile_rows)
 {
@@ -552,7 +553,7 @@ template <int N> __device__ __forceinline__ void interleave()
 // a time (32 of 256 elements).  Scores once more (their rows' totals were not known before), p summed over the rows in fp32, in an
 // order that timing does not change.  A row of queries is a column of the product: a lane adds up its column's rows in turn, and lanes
 // are joined once at the end.  Half of attention's operations, and an exp2 for each score: bound by the vector instructions (three a
-// score, exp2 at half rate) that run between the matrix ones: four long prompts' parts, 343 million scores, 88 GFLOP in 106 us (172 us
+// score, exp2 at half rate) that run between the matrix ones: four long prompts' parts, 343 million scores, 88 GFLOP in 104 to 110 us by card (172 us
 // with 32 rows a step and nothing read ahead, 130 with the two one after the other, 121 with 160 lane exchanges at the end).
 template <typename T, int DP>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ? 2 : 1))) void weights_kernel(AttendArgs a, PartsPlan p)
