@@ -125,14 +125,14 @@ template <int BIT, int N> __device__ __forceinline__ void halve(float *x, int la
 // a new one: p stays below 2^8, which costs no precision, and the rescaling becomes rare.
 constexpr float kSlack = 8.0f;
 
-// V's scale is m 2^e, 1 <= m < 2.  m goes into p, in fp32 and before p's one rounding; 2^e goes into the codes as they are converted,
+// V's scale is m 2^e, 1 <= m < 2 (more where e would pass 119).  m goes into p, in fp32 and before p's one rounding; 2^e goes into the codes as they are converted,
 // without one: bf16 holds every code times 2^-117 to 2^119.  fp16 holds them times 2^-15 to 2^7.  There outputs are summed in units of
 // 2^unit and codes converted times 2^(e - unit); a tile some of whose scales lie outside of that takes another unit, to which the sums are
 // brought first (in fp32, by a power of two: nothing is rounded).  Where a tile's own scales are further apart than 2^22 the largest
 // ones are held exactly and the others to 2^-32 of them: less than half of fp16's smallest number, as long as V's own numbers
 // are none that fp16 cannot hold.  So is what a scale below 2^-40 stands for, which therefore moves no unit.
-__device__ __forceinline__ int exponent_of(uint32_t bits) { return max((int)(bits >> 23), 1) - 127; }
-__device__ __forceinline__ float mantissa_of(uint32_t bits) { return bits >> 23 ? __uint_as_float((bits & 0x7FFFFFu) | 0x3F800000u) : 1.0f; }
+__device__ __forceinline__ int exponent_of(uint32_t bits) { return min(max((int)(bits >> 23), 1) - 127, 119); }
+__device__ __forceinline__ float mantissa_of(uint32_t bits) { return __uint_as_float(bits - ((uint32_t)exponent_of(bits) << 23)); }
 __device__ __forceinline__ float power_of(int e) { return __uint_as_float((uint32_t)(max(e, -126) + 127) << 23); }
 constexpr int kLeast = -15, kMost = 7, kFaint = -40;
 __device__ __forceinline__ bool outside(int e, int unit) { return e >= kFaint && (e < unit + kLeast || e > unit + kMost); }

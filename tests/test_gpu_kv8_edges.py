@@ -233,3 +233,22 @@ def test_more_new_tokens_than_the_length(B, dtype, spans, group):        # noqa:
     K.append(cpu, s.spans, kn, vn)
     for got, want in ((s.k, cpu.code[0]), (s.v, cpu.code[1])):
         K.equal_codes(got.cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("new", [3, 40])
+def test_a_scale_that_takes_a_hidden_code_past_the_largest_number(B, new):        # noqa: F811
+    """bf16 holds no 448 * 2^120; a query that does not see it is none the worse, and one that sees smaller codes there has them."""
+    s = Setup(B, 44, [(new, 200), (new, 80)], 2, 64, 16)
+    for r, length in ((0, 200), (1, 80)):
+        e = int(s.table[s.rows[r], (length - 1) // 16])
+        s.v_scale[s.table[s.rows[r]].long()] = 2.0 ** 100
+        s.v_scale[e] = 2.0 ** 120
+        s.v[e] = int(K.nearest_code(2.0 ** -6))
+        s.v[e, (length - 1) % 16, 1] = 0x7E
+    qd, qn = s.values(4, BF16)
+    out = torch.empty_like(qd)
+    B.kv8_attend(s.cache, s.batch, qd, out, stream=_stream())
+    (o, _, _), (do, _, _) = K.attend(s.cpu(), s.spans, qn, 0.125, 2, BF16)
+    for row, start, _, _ in s.spans:
+        K.near(out[start:start + new - 1].float().cpu().numpy(), o[start:start + new - 1], do[start:start + new - 1], "out")
+        K.near(out[start:start + new, :2].float().cpu().numpy(), o[start:start + new, :2], do[start:start + new, :2], "out")
