@@ -35,7 +35,7 @@ __device__ __forceinline__ float lane_value(float v, int lane) { return __int_as
 // Bound by neither pipe alone: a tile takes a wavefront 32 matrix instructions (1280 cycles) and some 280 vector ones (1500), 112 of
 // them to stage, and the two wavefronts of a SIMD together 6000 cycles: they leave the barrier together and so want the same pipe
 // at the same time; a workgroup's start and end cost as much as four tiles of its dozen.  32 ragged prompts of 128-2048 tokens, 32 query
-// heads over 8: 585 to 603 us by card, 746 to 768 TFLOP/s (a large product of the library: 1250); parts of four long prompts, six splits,
+// heads over 8: 581 to 638 us by card, 706 to 773 TFLOP/s (a large product of the library: 1250); parts of four long prompts, six splits,
 // 222 to 232 us, 755 to 790 TFLOP/s.  In fp16 and with 256 elements 2 to 3 % more.  Queries and
 // outputs that went between memory and the lanes without LDS cost 33 us of it.  Measured and not better (before that, at 620): one
 // wavefront of 64 rows a SIMD (spills), the second four wavefronts half a tile behind the first (658), staging between the
