@@ -1,4 +1,4 @@
-"""ctypes binding of include/dmi.h and include/dmi_kv8.h: same names, argument marshalling only.
+"""ctypes binding of include/dmi.h, include/dmi_kv8.h and include/dmi_kv8_long.h: same names, argument marshalling only.
 
 Every step of the capture-and-stage path runs inside libdmi.so.  There is no
 fallback: if the library is missing or no GPU is present the calls raise.
@@ -198,7 +198,19 @@ def lib():
     L.dmi_kv8_attend.argtypes = [S, S, S, C.c_uint32, C.c_float, S, C.c_void_p, S, S, C.c_float, C.c_void_p, C.c_uint64,
                                  C.c_void_p]
     L.dmi_kv8_evict.argtypes = [S, S, S, S, S, C.c_uint32, C.c_uint32, C.c_void_p, C.c_void_p, C.c_void_p]
-    for name in ("dmi_kv8_append", "dmi_kv8_attend", "dmi_kv8_evict"):
+    L.dmi_kv8_append_rotated.argtypes = [S, S, S, S, S, S, C.c_uint32, S, C.c_void_p]
+    L.dmi_kv8_bound.argtypes = [S, S, S, C.c_void_p]
+    L.dmi_kv8_select_workspace.argtypes = [S, S, C.c_uint32]
+    L.dmi_kv8_select.argtypes = [S, S, S, S, C.c_uint32, C.c_uint32, C.c_uint32, C.c_uint32, C.c_void_p, C.c_void_p, C.c_uint64, C.c_void_p]
+    L.dmi_kv8_attend_blocks_workspace.argtypes = [S, S, C.c_uint32, C.c_uint32]
+    L.dmi_kv8_attend_blocks.argtypes = [S, S, C.c_void_p, C.c_uint32, S, C.c_uint32, C.c_float, S, C.c_void_p, C.c_void_p, C.c_uint64,
+                                        C.c_void_p]
+    L.dmi_kv8_attend_shared_workspace.argtypes = [S, S, S, C.c_uint32]
+    L.dmi_kv8_attend_shared.argtypes = [S, S, S, S, C.c_uint32, C.c_float, S, C.c_void_p, C.c_void_p, C.c_uint64, C.c_void_p]
+    for name in ("select", "attend_blocks", "attend_shared"):
+        getattr(L, f"dmi_kv8_{name}_workspace").restype = C.c_uint64
+    for name in ("dmi_kv8_append", "dmi_kv8_attend", "dmi_kv8_evict", "dmi_kv8_append_rotated", "dmi_kv8_bound", "dmi_kv8_select",
+                 "dmi_kv8_attend_blocks", "dmi_kv8_attend_shared"):
         getattr(L, name).restype = C.c_int32
     L.dmi_drain.argtypes = [C.c_void_p, C.c_uint32, P(C.c_uint64)]
     L.dmi_poll_host.argtypes = [C.c_void_p, P(RecordViewC), C.c_uint32, P(C.c_uint32)]
@@ -888,3 +900,137 @@ def kv8_evict(cache: KV8, batch: KV8Batch, weight, to: KV8, to_weight, *, keep: 
         raise ValueError(f"positions must be contiguous [{batch.n_reqs}, {cache.n_heads}, {keep}] and lens [{batch.n_reqs}]")
     _check(lib().dmi_kv8_evict(cache._raw, batch._raw, raw_weight, to._raw, raw_to_weight, keep, recent, positions.data_ptr(),
                                lens.data_ptr(), stream or None))
+
+
+# ---------------------------------------------------------------- the 8-bit KV cache: long contexts (include/dmi_kv8_long.h)
+_PACK_KV8_ROTARY = struct.Struct("=QQII").pack
+_PACK_KV8_BOUNDS = struct.Struct("=Qqq").pack
+_PACK_KV8_PREFIX = struct.Struct("=IIQQ").pack
+
+
+class KV8Rotary:
+    """How positions rotate rows of heads (dmi_kv8_rotary_t): freq fp32 [pairs], radians a position; positions int32 [total_new] or None
+    (a token's place in the cache); pairs: neighbouring elements are a pair, not elements half of the rotated ones apart."""
+
+    def __init__(self, freq, *, positions=None, pairs: bool = False):
+        if not _typed(freq, "freq", "float32", 1).numel():
+            raise ValueError("freq is empty")
+        if positions is not None:
+            _typed(positions, "positions", "int32", 1)
+        self.freq, self.positions, self.rotary_dim, self.pairs = freq, positions, 2 * freq.shape[0], bool(pairs)
+        self._raw = _PACK_KV8_ROTARY(freq.data_ptr(), 0 if positions is None else positions.data_ptr(), self.rotary_dim, int(self.pairs))
+
+
+class KV8Prefix:
+    """Groups of requests whose contexts begin alike (dmi_kv8_prefix_t): int32 device tensors group_starts [n_groups + 1] (requests)
+    and prefix [n_groups] (tokens), of at most max_prefix.  Their contents may change between calls."""
+
+    def __init__(self, group_starts, prefix, *, max_prefix: int):
+        _typed(group_starts, "group_starts", "int32", 1)
+        if _typed(prefix, "prefix", "int32", 1).shape[0] + 1 != group_starts.shape[0]:
+            raise ValueError("group_starts must have one entry more than prefix")
+        self.group_starts, self.prefix, self.n_groups, self.max_prefix = group_starts, prefix, prefix.shape[0], max_prefix
+        self._raw = _PACK_KV8_PREFIX(self.n_groups, max_prefix, group_starts.data_ptr(), prefix.data_ptr())
+
+
+def kv8_append_rotated(cache: KV8, batch: KV8Batch, key, value, rotary: KV8Rotary, *, q=None, q_out=None, stream: int = 0) -> None:
+    """dmi_kv8_append_rotated: key (rotated) and value [total_new, heads, dim] into the cache; q [total_new, query heads, dim] rotated into
+    q_out, which may be q.  bf16 / fp16 / fp32, all the same."""
+    n, dim = batch.total_new, cache.head_dim
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out go together")
+    if rotary.positions is not None and rotary.positions.shape[0] < n:
+        raise ValueError(f"positions must have {n} entries")
+    heads = 0 if q is None else q.shape[1]
+    k = _kv8_heads(key, "key", n, cache.n_heads, dim)
+    v = _kv8_heads(value, "value", n, cache.n_heads, dim)
+    _check(lib().dmi_kv8_append_rotated(cache._raw, batch._raw, k, v, rotary._raw, None if q is None else _kv8_heads(q, "q", n, heads, dim),
+                                        heads, None if q is None else _kv8_heads(q_out, "q_out", n, heads, dim), stream or None))
+
+
+def _kv8_bounds(t, cache):
+    import torch
+    shape, stride = t.shape, t.stride()
+    if t.dtype not in (torch.uint8, torch.float8_e4m3fn) or tuple(shape) != (cache.k.shape[0], cache.n_heads, 2, cache.head_dim) \
+            or stride[3] != 1 or stride[2] != cache.head_dim:
+        raise ValueError(f"bounds must be uint8 or float8_e4m3fn [{cache.k.shape[0]}, {cache.n_heads}, 2, {cache.head_dim}], the last two contiguous")
+    return _PACK_KV8_BOUNDS(t.data_ptr(), stride[0], stride[1])
+
+
+def kv8_bound(cache: KV8, batch: KV8Batch, bounds, *, stream: int = 0) -> None:
+    """dmi_kv8_bound: bounds [blocks, heads, 2, dim] (the least, the largest) of the blocks that the call's new tokens reach."""
+    _check(lib().dmi_kv8_bound(cache._raw, batch._raw, _kv8_bounds(bounds, cache), stream or None))
+
+
+def _kv8_blocks(t, batch, cache):
+    _typed(t, "blocks", "int32", 3)
+    if t.shape[0] < batch.total_new or t.shape[1] != cache.n_heads or not t.is_contiguous():
+        raise ValueError(f"blocks must be contiguous [{batch.total_new}, {cache.n_heads}, blocks of a token], not {list(t.shape)}")
+    return t.data_ptr()
+
+
+def _kv8_workspace(workspace, need, like, stream):
+    """(the workspace, which the caller holds until its call has returned, its address, its bytes)."""
+    if workspace is None and need:
+        workspace = _scratch(need, like, stream)
+    return (None, None, 0) if workspace is None else (workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size())
+
+
+def kv8_select_workspace(cache: KV8, batch: KV8Batch, n_select: int) -> int:
+    """Bytes of workspace that kv8_select takes."""
+    return int(lib().dmi_kv8_select_workspace(cache._raw, batch._raw, n_select))
+
+
+def kv8_select(cache: KV8, batch: KV8Batch, bounds, q, blocks, *, first: int = 1, recent: int = 2, workspace=None, stream: int = 0) -> None:
+    """dmi_kv8_select: for each new token and head of the cache, blocks.shape[2] blocks, into blocks int32 [total_new, heads, n_select]: the
+    first and the most recent ones, and those whose bounds allow q [total_new, query heads, dim] (bf16 or fp16) the largest scores."""
+    n, n_select = batch.total_new, blocks.shape[-1]
+    to = _kv8_blocks(blocks, batch, cache)
+    raw_q, raw_bounds = _kv8_heads(q, "q", n, q.shape[1], cache.head_dim), _kv8_bounds(bounds, cache)
+    need = 0 if workspace is not None else lib().dmi_kv8_select_workspace(cache._raw, batch._raw, n_select)
+    held, at, size = _kv8_workspace(workspace, need, q, stream)
+    _check(lib().dmi_kv8_select(cache._raw, batch._raw, raw_bounds, raw_q, q.shape[1], n_select, first, recent, to, at, size, stream or None))
+
+
+def _kv8_lse(lse, n, heads):
+    if lse is None:
+        return None
+    if tuple(lse.shape) != (n, heads) or not lse.is_contiguous():
+        raise ValueError(f"lse must be contiguous [{n}, {heads}]")
+    if _torch_dtype_code(lse) != DT_FP32:
+        raise ValueError("lse must be float32")
+    return lse.data_ptr()
+
+
+def kv8_attend_blocks_workspace(cache: KV8, batch: KV8Batch, n_q_heads: int, n_select: int) -> int:
+    """Bytes of workspace that kv8_attend_blocks takes."""
+    return int(lib().dmi_kv8_attend_blocks_workspace(cache._raw, batch._raw, n_q_heads, n_select))
+
+
+def kv8_attend_blocks(cache: KV8, batch: KV8Batch, blocks, q, out, *, scale: Optional[float] = None, lse=None, workspace=None,
+                      stream: int = 0) -> None:
+    """dmi_kv8_attend_blocks: attention of each new token over the blocks listed for it, int32 [total_new, heads, n_select] as kv8_select
+    writes them; q, out, scale, lse and workspace as in kv8_attend."""
+    n, heads, n_select = batch.total_new, q.shape[1], blocks.shape[-1]
+    of = _kv8_blocks(blocks, batch, cache)
+    raw_q, raw_out = _kv8_heads(q, "q", n, heads, cache.head_dim), _kv8_heads(out, "out", n, heads, cache.head_dim)
+    need = 0 if workspace is not None else lib().dmi_kv8_attend_blocks_workspace(cache._raw, batch._raw, heads, n_select)
+    held, at, size = _kv8_workspace(workspace, need, q, stream)
+    _check(lib().dmi_kv8_attend_blocks(cache._raw, batch._raw, of, n_select, raw_q, heads, cache.head_dim ** -0.5 if scale is None else scale,
+                                       raw_out, _kv8_lse(lse, n, heads), at, size, stream or None))
+
+
+def kv8_attend_shared_workspace(cache: KV8, batch: KV8Batch, prefix: KV8Prefix, n_q_heads: int) -> int:
+    """Bytes of workspace that kv8_attend_shared takes."""
+    return int(lib().dmi_kv8_attend_shared_workspace(cache._raw, batch._raw, prefix._raw, n_q_heads))
+
+
+def kv8_attend_shared(cache: KV8, batch: KV8Batch, prefix: KV8Prefix, q, out, *, scale: Optional[float] = None, lse=None, workspace=None,
+                      stream: int = 0) -> None:
+    """dmi_kv8_attend_shared: kv8_attend, without weights, of requests in groups that share the beginning of their contexts."""
+    n, heads = batch.total_new, q.shape[1]
+    raw_q, raw_out = _kv8_heads(q, "q", n, heads, cache.head_dim), _kv8_heads(out, "out", n, heads, cache.head_dim)
+    need = 0 if workspace is not None else lib().dmi_kv8_attend_shared_workspace(cache._raw, batch._raw, prefix._raw, heads)
+    held, at, size = _kv8_workspace(workspace, need, q, stream)
+    _check(lib().dmi_kv8_attend_shared(cache._raw, batch._raw, prefix._raw, raw_q, heads, cache.head_dim ** -0.5 if scale is None else scale,
+                                       raw_out, _kv8_lse(lse, n, heads), at, size, stream or None))

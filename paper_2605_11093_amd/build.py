@@ -11,9 +11,11 @@ ROOT = os.path.dirname(HERE)
 SO = os.path.join(HERE, "libdmi.so")
 SOURCES = [os.path.join(HERE, "csrc", f) for f in ("dmi_kernels.hip", "dmi_host.hip", "dmi_step.hip",
                                                      "dmi_exporter.hip", "dmi_noalloc.hip", "dmi_kv8.hip", "dmi_kv8_cache.hip",
-                                                     "dmi_kv8_tokens.hip", "dmi_kv8_parts.hip")]
+                                                     "dmi_kv8_tokens.hip", "dmi_kv8_parts.hip", "dmi_kv8_long.hip",
+                                                     "dmi_kv8_rotate.hip", "dmi_kv8_select.hip")]
 HEADERS = [os.path.join(HERE, "csrc", "dmi_internal.h"), os.path.join(HERE, "csrc", "dmi_ring.h"),
-           os.path.join(HERE, "csrc", "dmi_kv8_internal.h"), os.path.join(HERE, "csrc", "dmi_kv8_mfma.h"), os.path.join(ROOT, "include", "dmi_kv8.h"),
+           os.path.join(HERE, "csrc", "dmi_kv8_internal.h"), os.path.join(HERE, "csrc", "dmi_kv8_mfma.h"), os.path.join(HERE, "csrc", "dmi_kv8_rows.h"),
+           os.path.join(HERE, "csrc", "dmi_kv8_checks.h"), os.path.join(ROOT, "include", "dmi_kv8.h"), os.path.join(ROOT, "include", "dmi_kv8_long.h"),
            os.path.join(ROOT, "include", "dmi.h"), os.path.join(ROOT, "include", "dmi_debug.h")]
 
 

@@ -54,6 +54,40 @@ struct EvictArgs {
     int32_t *positions, *to_lens;
 };
 
+struct RotateArgs {
+    Cache c;
+    Batch b;
+    Rows x[2], q, q_out;
+    const float *freq;
+    const int32_t *positions;                   // NULL: a token's place
+    uint32_t rotary, q_heads;                   // q_heads 0: no queries
+    bool neighbours;                            // what makes a pair: see dmi_kv8_rotary_t
+    bool counted;                               // as in AppendArgs
+    uint32_t tokens;                            // whose cosines are in LDS at a time
+    uint32_t each, groups;                      // items of a workgroup, workgroups of a block
+};
+
+struct BoundArgs {
+    Cache c;
+    Batch b;
+    uint8_t *bounds;
+    int64_t bounds_block_stride, bounds_head_stride;
+    uint32_t touched;
+    bool counted;
+};
+
+struct SelectArgs {
+    Cache c;
+    Batch b;
+    Rows q;
+    const uint8_t *bounds;
+    int64_t bounds_block_stride, bounds_head_stride;
+    uint32_t group, n_select, n_first, n_recent;
+    uint32_t stride;                            // blocks of the longest request
+    uint64_t *keys;                             // [new token][head][stride], scores in an order of unsigned numbers
+    int32_t *blocks;
+};
+
 struct AttendArgs {
     Cache c;
     Batch b;
@@ -62,7 +96,13 @@ struct AttendArgs {
     Weight w, prior;                            // data NULL: none
     float decay, scale_log2;                    // scale * log2(e): scores are kept as powers of two
     uint32_t group, q_heads;
+    const int32_t *blocks;                      // kListed: those attended to, [new token][head][n_select]
+    uint32_t n_select;
 };
+
+// What the attention kernels do: a whole context; the rest of one behind a shared prefix, whose sums are left as parts whatever their
+// number; such a prefix, for all rows of a group of requests; listed blocks, for each new token by itself.
+enum Kind { kWhole, kRest, kPrefix, kListed };
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
@@ -92,13 +132,34 @@ struct PartsPlan {
     float *totals;                              // [row of out]: log2 of the sum of 2^score; NULL: no weights
 };
 
+// How contexts behind shared prefixes are attended to: see dmi_kv8_parts.hip.
+struct SharedPlan {
+    PartsPlan prefix;                           // splits 0: there is none
+    bool tokens;                                // few rows a head behind it: by tokens_kernel
+    TokensPlan few;
+    PartsPlan many;
+    uint32_t splits;                            // of what is behind the prefix
+    f32x2 *sums;                                // [row of out][split]
+    float *parts;
+    uint32_t n_groups, max_prefix;
+    const int32_t *group_starts, *prefix_tokens;
+    int32_t *shared, *lens, *seqs;              // for each request: tokens read for its group, its others, its place in the block table
+    int32_t *group_lens, *group_seqs, *group_rows;      // for each group: tokens read for all, row of the block table, first row of q
+};
+
 // What a launch may have in its first dimension: threads are counted in 32 bits.  A call whose launches need more is refused before
 // the first of them (hipErrorInvalidConfiguration).
 inline bool launchable(uint64_t groups, uint32_t threads) { return groups <= 0xffffffffu / threads; }
 
 hipError_t launch_append(AppendArgs a, uint32_t dtype, hipStream_t s);
+hipError_t launch_rotate(RotateArgs a, uint32_t dtype, hipStream_t s);
+hipError_t launch_bound(BoundArgs a, hipStream_t s);
+hipError_t launch_select(const SelectArgs &a, uint32_t dtype, hipStream_t s);
 hipError_t launch_evict(const EvictArgs &a, hipStream_t s);
 hipError_t launch_parts(const AttendArgs &a, const PartsPlan &p, uint32_t dtype, hipStream_t s);
+hipError_t launch_parts_apart(const AttendArgs &a, const PartsPlan &p, Kind kind, uint32_t dtype, hipStream_t s);
+hipError_t launch_shared(const AttendArgs &a, const SharedPlan &p, uint32_t dtype, hipStream_t s);
+hipError_t launch_tokens_apart(const AttendArgs &a, const TokensPlan &p, Kind kind, uint32_t dtype, hipStream_t s);
 hipError_t launch_tokens(const AttendArgs &a, const TokensPlan &p, uint32_t dtype, hipStream_t s);
 
 // ---------------------------------------------------------------- device side
@@ -122,6 +183,26 @@ __device__ __forceinline__ Request request_of(const Batch &b, const Cache &c, in
         q.fresh = 1;
     }
     return q;
+}
+
+// A new token as a request of its own, with a length of what it sees: the last request whose rows begin at or in front of it, if the
+// token is one of that request's.  64 places at a time are looked at, so 65535 requests take three trips to memory.
+__device__ __forceinline__ Request token_of(const Batch &b, const Cache &c, int token)
+{
+    int r = token;
+    if (b.starts) {
+        int n = (int)b.n_reqs;
+        r = 0;
+        while (n > 1) {
+            const int step = (n + 63) >> 6, at = (int)(threadIdx.x & 63u) * step;
+            const int k = max(1, __popcll(__ballot(at < n && b.starts[r + min(at, n - 1)] <= token)));
+            r += (k - 1) * step;
+            n = min(step, n - (k - 1) * step);
+        }
+    }
+    const Request q = request_of(b, c, min(r, (int)b.n_reqs - 1));
+    const int nth = token - q.start;
+    return {q.row, min(q.len, max(0, q.len - q.fresh + nth + 1)), token, nth >= 0 && nth < q.fresh ? 1 : 0};
 }
 
 // Sums over the lanes up to each one

@@ -17,6 +17,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 struct Bf16 {
     static constexpr bool kNarrow = false;      // as wide a range of exponents as fp32
     static constexpr uint32_t kOne = 0x3F80u;
+    static __device__ __forceinline__ float number(uint16_t w) { return __uint_as_float((uint32_t)w << 16); }
     // two neighbouring codes of a word, times a power of two
     static __device__ __forceinline__ uint32_t two_codes(uint32_t w, bool hi, float power = 1.0f)
     {
@@ -41,6 +42,7 @@ struct Bf16 {
 struct Fp16 {
     static constexpr bool kNarrow = true;
     static constexpr uint32_t kOne = 0x3C00u;
+    static __device__ __forceinline__ float number(uint16_t w) { return (float)__builtin_bit_cast(_Float16, w); }
     static __device__ __forceinline__ uint32_t two_codes(uint32_t w, bool hi, float power = 1.0f)
     {
         return __builtin_bit_cast(uint32_t, hi ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, power, true)

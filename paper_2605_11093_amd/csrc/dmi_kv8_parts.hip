@@ -41,7 +41,7 @@ __device__ __forceinline__ float lane_value(float v, int lane) { return __int_as
 // wavefront of 64 rows a SIMD (spills), the second four wavefronts half a tile behind the first (658), staging between the
 // instructions of a product (627-671), two workgroups of four wavefronts (634), priorities (624-639), a maximum looked for only where
 // sums grow (637-700), two to eight row tiles a workgroup in turn (670-818), workgroups that stay and draw row tiles (642).
-template <typename T, int DP, int NW>
+template <typename T, int DP, int NW, Kind KIND = kWhole>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW / 4)))
 void parts_kernel(AttendArgs a, PartsPlan p)
 {
@@ -103,8 +103,9 @@ void parts_kernel(AttendArgs a, PartsPlan p)
     }
     if (row0 < 0) return;
     const int rows = q.fresh * (int)a.group;
-    const int older = q.len - q.fresh, last_row = min(row0 + 32 * NW, rows) - 1;
-    const int seen = older + last_row / (int)a.group + 1;       // tokens that the workgroup's last row sees
+    const int older = KIND == kPrefix ? q.len - 1 : q.len - q.fresh, last_row = min(row0 + 32 * NW, rows) - 1;
+    // tokens that the workgroup's last row sees (of a prefix all rows see all)
+    const int seen = KIND == kPrefix ? q.len : older + last_row / (int)a.group + 1;
     const int begin = (int)(split * p.chunk), end = min(seen, begin + (int)p.chunk), tiles = max(0, (end - begin + kTile - 1) / kTile);
     if (split && tiles == 0) return;                            // (what reads the parts counts the same way)
 
@@ -113,7 +114,7 @@ void parts_kernel(AttendArgs a, PartsPlan p)
     const float scale = fabsf(a.scale_log2);
     const int wave_row = row0 + wave * 32, row = wave_row + col;
     const QueryRow w = query_row(a, head, (uint32_t)row);
-    const int lim = row < rows ? older + w.token : -1;          // the last position that the column's query sees
+    const int lim = row < rows ? older + (KIND == kPrefix ? 0 : w.token) : -1;      // the last position that the column's query sees
     // Read by whole rows, and given to the lanes that take them through LDS (rows of its own for each wavefront; outputs go the same way)
     constexpr int kRow = 2 * DP, kChunks = DP / 8, kRows = 64 / kChunks;       // bytes; 16s of them; rows of a load
     static_assert(NW * 32 * kRow <= 2 * (kTile * KP + DP * VP));
@@ -133,8 +134,8 @@ void parts_kernel(AttendArgs a, PartsPlan p)
         }
     }
     // what the first and the last of them see
-    const int least = wave_row + 32 <= rows ? older + wave_row / (int)a.group : -1;
-    const int most = wave_row < rows ? older + min(wave_row + 31, rows - 1) / (int)a.group : -1;
+    const int least = wave_row + 32 <= rows ? older + (KIND == kPrefix ? 0 : wave_row / (int)a.group) : -1;
+    const int most = wave_row < rows ? older + (KIND == kPrefix ? 0 : min(wave_row + 31, rows - 1) / (int)a.group) : -1;
 
     // ---- staging
     struct KCodes {
@@ -169,7 +170,9 @@ void parts_kernel(AttendArgs a, PartsPlan p)
     auto look = [&](int batch, auto between) {
         const int t = begin + 1024 * batch + 16 * lane;
         const uint32_t block = block_of(a.c, (uint32_t)t >> 4);
-        const int raw = a.c.table[(int64_t)q.row * a.c.table_stride + min(block, a.c.max_blocks - 1u)];
+        // (a rest's row begins inside of a table's: columns behind its last token may be none of the table)
+        const uint32_t last = KIND == kRest ? block_of(a.c, (uint32_t)(q.len - 1) >> 4) : a.c.max_blocks - 1u;
+        const int raw = a.c.table[(int64_t)q.row * a.c.table_stride + min(block, last)];
         const bool there = t < end && block < a.c.max_blocks && (uint32_t)raw < a.c.n_blocks;
         const int entry = there ? raw : 0;
         const int64_t at = (int64_t)entry * a.c.block_stride + (int64_t)((uint32_t)t - block * a.c.bs) * a.c.slot_stride + (int64_t)head * a.c.head_stride;
@@ -445,7 +448,7 @@ void parts_kernel(AttendArgs a, PartsPlan p)
     l += __shfl_xor(l, 32);
     const int64_t at = (int64_t)(q.start + w.token) * a.q_heads + w.head;
     const bool empty = m == -INFINITY && l == 0.0f;
-    if (p.splits == 1) {
+    if (KIND == kWhole && p.splits == 1) {
         // Rows are put together in LDS, so that a store writes whole ones: as the lanes hold them it would write 16 bytes here and there.
         const float f = __builtin_ldexpf(empty ? 0.0f : 1.0f / l, ref);
         const int64_t dst = (int64_t)(q.start + w.token) * a.out.row_stride + (int64_t)w.head * a.out.head_stride;
@@ -741,7 +744,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
     }
 }
 
-template <typename T, int DP, int NW> static hipError_t parts(const AttendArgs &a, PartsPlan p, hipStream_t s)
+template <typename T, int DP, int NW, Kind KIND> static hipError_t parts(const AttendArgs &a, PartsPlan p, hipStream_t s)
 {
     // Row tiles of an XCD at most: as many as the longest request makes, for each pair; as many as all rows make, and one for each request.
     // Where the second is less the kernel counts for itself: a workgroup that finds nothing to do has waited for a compute unit of its own.
@@ -753,8 +756,9 @@ template <typename T, int DP, int NW> static hipError_t parts(const AttendArgs &
     const uint64_t groups = (p.counted ? by_rows : by_pairs) * p.splits * 8u;
     const uint64_t weight_groups = a.w.data ? (a.b.max_len + 255ull) / 256u * a.c.heads : 0u;
     if (!launchable(groups, 64u * NW) || !launchable(weight_groups, 256)) return hipErrorInvalidConfiguration;
-    parts_kernel<T, DP, NW><<<(uint32_t)groups, 64 * NW, 0, s>>>(a, p);
+    parts_kernel<T, DP, NW, KIND><<<(uint32_t)groups, 64 * NW, 0, s>>>(a, p);
     hipError_t e = hipGetLastError();
+    if constexpr (KIND != kWhole) return e;
     if (e == hipSuccess && p.splits > 1u) {
         const uint32_t each = 256u / (a.c.dim / 4u);
         join_parts_kernel<T><<<dim3(std::min((a.b.max_new * a.q_heads + each - 1u) / each, 1u << 20), a.b.n_reqs), 256, 0, s>>>(a, p, 32u * NW);
@@ -767,14 +771,133 @@ template <typename T, int DP, int NW> static hipError_t parts(const AttendArgs &
     return e;
 }
 
-template <typename T> static hipError_t parts_of(const AttendArgs &a, const PartsPlan &p, hipStream_t s)
+template <typename T, Kind KIND> static hipError_t parts_of(const AttendArgs &a, const PartsPlan &p, hipStream_t s)
 {
-    return a.c.dim <= 64 ? parts<T, 64, 8>(a, p, s) : a.c.dim <= 128 ? parts<T, 128, 8>(a, p, s) : parts<T, 256, 4>(a, p, s);
+    return a.c.dim <= 64 ? parts<T, 64, 8, KIND>(a, p, s) : a.c.dim <= 128 ? parts<T, 128, 8, KIND>(a, p, s) : parts<T, 256, 4, KIND>(a, p, s);
 }
 
 hipError_t launch_parts(const AttendArgs &a, const PartsPlan &p, uint32_t dtype, hipStream_t s)
 {
-    return dtype == DMI_DTYPE_BF16 ? parts_of<Bf16>(a, p, s) : parts_of<Fp16>(a, p, s);
+    return dtype == DMI_DTYPE_BF16 ? parts_of<Bf16, kWhole>(a, p, s) : parts_of<Fp16, kWhole>(a, p, s);
+}
+
+hipError_t launch_parts_apart(const AttendArgs &a, const PartsPlan &p, Kind kind, uint32_t dtype, hipStream_t s)
+{
+    if (kind == kPrefix) return dtype == DMI_DTYPE_BF16 ? parts_of<Bf16, kPrefix>(a, p, s) : parts_of<Fp16, kPrefix>(a, p, s);
+    return dtype == DMI_DTYPE_BF16 ? parts_of<Bf16, kRest>(a, p, s) : parts_of<Fp16, kRest>(a, p, s);
+}
+
+// ---------------------------------------------------------------- contexts behind shared prefixes
+// Tokens of group g's prefix that are read for all: whole blocks, in front of all new tokens, of requests that have some.  All lanes of a
+// wavefront have to come here, and all get it.
+__device__ __forceinline__ int prefix_of(const AttendArgs &a, const SharedPlan &p, int g)
+{
+    const int n = (int)a.b.n_reqs, first = min(max(p.group_starts[g], 0), n), last = min(max(p.group_starts[g + 1], first), n);
+    int least = first < last ? min(max(p.prefix_tokens[g], 0), (int)p.max_prefix) : 0;
+    for (int r = first + (int)(threadIdx.x & 63u); r < last; r += 64) {
+        const Request q = request_of(a.b, a.c, r);
+        if (q.fresh > 0 || r == first) least = min(least, max(q.len - q.fresh, 0));
+    }
+#pragma unroll
+    for (int m = 32; m; m >>= 1) least = min(least, __shfl_xor(least, m));
+    return (int)(block_of(a.c, (uint32_t)least >> 4) * a.c.bs);
+}
+
+// The prefixes as a batch, one request for each group, and what each request has behind its group's, over a table of one column: its place
+// in the block table, its length.  A wavefront for each; a request that no group has shares nothing.
+__global__ __launch_bounds__(256) void shared_kernel(AttendArgs a, SharedPlan p)
+{
+    const int lane = threadIdx.x & 63;
+    int r = (int)(blockIdx.x * 4u + (threadIdx.x >> 6));
+    if (r >= (int)a.b.n_reqs) {
+        r -= (int)a.b.n_reqs;
+        if (r > (int)p.n_groups || !p.n_groups) return;
+        // rows of a group begin where its first request's do, and the last one's end where the next group's begin
+        const int first = min(max(p.group_starts[r], 0), (int)a.b.n_reqs);
+        const int tokens = r < (int)p.n_groups ? prefix_of(a, p, r) : 0;
+        if (lane) return;
+        p.group_rows[r] = a.b.starts ? a.b.starts[first] : first;
+        if (r < (int)p.n_groups) {
+            p.group_lens[r] = tokens;
+            p.group_seqs[r] = first < (int)a.b.n_reqs ? request_of(a.b, a.c, first).row : 0;
+        }
+        return;
+    }
+    // the last group that begins at or in front of the request
+    int g = 0, n = (int)p.n_groups;
+    while (n > 1) {
+        const int step = (n + 63) >> 6, at = lane * step;
+        const int k = max(1, __popcll(__ballot(at < n && p.group_starts[g + min(at, n - 1)] <= r)));
+        g += (k - 1) * step;
+        n = min(step, n - (k - 1) * step);
+    }
+    const Request q = request_of(a.b, a.c, r);
+    int shared = 0;
+    if (n && p.group_starts[g] <= r && r < p.group_starts[g + 1]) shared = min(prefix_of(a, p, g), max(q.len - q.fresh, 0));
+    if (lane) return;
+    p.shared[r] = shared;
+    p.lens[r] = q.len - shared;
+    p.seqs[r] = (int32_t)((int64_t)q.row * a.c.table_stride + (int64_t)block_of(a.c, (uint32_t)shared >> 4));
+}
+
+// Outputs out of the parts of prefixes and of what is behind them: see join_parts_kernel.
+template <typename T>
+__global__ __launch_bounds__(256) void join_shared_kernel(AttendArgs a, SharedPlan p)
+{
+    const Request q = request_of(a.b, a.c, (int)blockIdx.y);
+    const uint32_t wide = a.c.dim / 4u, each = 256u / wide, rows = (uint32_t)q.fresh * a.group, lane = threadIdx.x % wide;
+    if (threadIdx.x >= each * wide) return;
+    const int shared = p.shared[blockIdx.y];
+    const int before = p.prefix.chunk ? min((shared + (int)p.prefix.chunk - 1) / (int)p.prefix.chunk, (int)p.prefix.splits) : 0;
+    for (uint32_t n = blockIdx.x * each + threadIdx.x / wide; n < rows * a.c.heads; n += gridDim.x * each) {
+        const uint32_t head = n / rows, row = n - head * rows;
+        const QueryRow w = query_row(a, head, row);
+        const int64_t at = (int64_t)(q.start + w.token) * a.q_heads + w.head;
+        float m = -INFINITY, l = 0.0f;
+        f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+        auto add = [&](const f32x2 *sums, const float *parts, int count) {
+            parts += 4u * lane;
+#pragma unroll 4
+            for (int s = 0; s < count; s++) {
+                const f32x2 x = sums[s];
+                const f32x4 part = *reinterpret_cast<const f32x4 *>(parts + (int64_t)s * a.c.dim);
+                const float top = fmaxf(m, x[0]), to = top == -INFINITY ? 0.0f : top, f = exp2_of(m - to), g = exp2_of(x[0] - to);
+                l = l * f + x[1] * g;
+                o = o * f + part * g;
+                m = top;
+            }
+        };
+        add(p.prefix.sums + at * p.prefix.splits, p.prefix.parts + at * p.prefix.splits * a.c.dim, before);
+        add(p.sums + at * p.splits, p.parts + at * p.splits * a.c.dim, (int)p.splits);
+        const bool empty = m == -INFINITY && l == 0.0f;
+        o *= empty ? 0.0f : 1.0f / l;
+        uint16_t *dst = static_cast<uint16_t *>(a.out.data) + (int64_t)(q.start + w.token) * a.out.row_stride + (int64_t)w.head * a.out.head_stride + 4u * lane;
+        *reinterpret_cast<u32x2 *>(dst) = u32x2{T::pack(o[0], o[1]), T::pack(o[2], o[3])};
+        if (!lane && a.lse) a.lse[at] = empty ? -INFINITY : (m + log2_of(l)) * kLn2;
+    }
+}
+
+hipError_t launch_shared(const AttendArgs &a, const SharedPlan &p, uint32_t dtype, hipStream_t s)
+{
+    shared_kernel<<<(a.b.n_reqs + p.n_groups + 4u) / 4u, 256, 0, s>>>(a, p);
+    hipError_t e = hipGetLastError();
+    if (e == hipSuccess && p.prefix.splits) {
+        AttendArgs group = a;
+        group.b = Batch{p.group_lens, p.group_rows, p.group_seqs, p.n_groups, a.b.total_new, a.b.total_new, p.max_prefix};
+        e = launch_parts_apart(group, p.prefix, kPrefix, dtype, s);
+    }
+    if (e != hipSuccess) return e;
+    // a table of one column, of which each request has those from its place in the real one on
+    AttendArgs rest = a;
+    rest.c.n_seqs = 1u << 31, rest.c.table_stride = 1;
+    rest.b.rows = p.seqs, rest.b.lens = p.lens;
+    e = p.tokens ? launch_tokens_apart(rest, p.few, kRest, dtype, s) : launch_parts_apart(rest, p.many, kRest, dtype, s);
+    if (e != hipSuccess) return e;
+    const uint32_t each = 256u / (a.c.dim / 4u);
+    const dim3 grid(std::min((a.b.max_new * a.q_heads + each - 1u) / each, 1u << 20), a.b.n_reqs);
+    if (dtype == DMI_DTYPE_BF16) join_shared_kernel<Bf16><<<grid, 256, 0, s>>>(a, p);
+    else join_shared_kernel<Fp16><<<grid, 256, 0, s>>>(a, p);
+    return hipGetLastError();
 }
 
 }  // namespace kv8

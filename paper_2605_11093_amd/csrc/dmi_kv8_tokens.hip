@@ -3,6 +3,7 @@
 #include "dmi_kv8_mfma.h"
 
 #include <cfloat>
+#include <climits>
 
 namespace dmi {
 namespace kv8 {
@@ -21,6 +22,12 @@ namespace kv8 {
 
 // A request with new tokens has a tile at least: an empty context's rows are written too.
 __device__ __forceinline__ int tiles_of(const Request &q) { return q.fresh > 0 ? max(1, (q.len + 31) >> 5) : 0; }
+
+// How many places of a token's list count: of whole blocks
+__device__ __forceinline__ int listed_tokens(const AttendArgs &a, const Request &q)
+{
+    return q.len > 0 && q.fresh > 0 ? (int)(min(a.n_select, (uint32_t)(q.len - 1) / a.c.bs + 1u) * a.c.bs) : 0;
+}
 
 // The tiles of requests n0 .. n0 + 63, one request a lane
 __device__ __forceinline__ int lane_tiles(const AttendArgs &a, uint32_t n0)
@@ -61,7 +68,7 @@ template <bool WHOLE> __device__ __forceinline__ int64_t part_at(const AttendArg
 // instead of 238 at that time).
 constexpr int waves_of(int dp, int nt, bool whole) { return !whole || dp * nt > 128 ? 4 : 8; }
 
-template <typename T, int DP, int NT, bool WHOLE>
+template <typename T, int DP, int NT, bool WHOLE, Kind KIND = kWhole>
 __global__ __launch_bounds__(64 * waves_of(DP, NT, WHOLE)) __attribute__((amdgpu_waves_per_eu(DP * NT <= 128 ? 2 : 1)))
 void tokens_kernel(AttendArgs a, TokensPlan p)
 {
@@ -81,8 +88,9 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
         range = (int)(blockIdx.x - pair * p.splits);
         r = (int)(pair / a.c.heads);
         head = pair % a.c.heads;
-        const Request q = request_of(a.b, a.c, r);
-        const int tiles = q.fresh > 0 ? tiles_of(q) : a.w.data ? (q.len + 31) >> 5 : 0;
+        const Request q = KIND == kListed ? token_of(a.b, a.c, r) : request_of(a.b, a.c, r);
+        const int tiles = KIND == kListed ? (listed_tokens(a, q) + 31) >> 5 : q.fresh > 0 ? tiles_of(q) : a.w.data ? (q.len + 31) >> 5 : 0;
+        if constexpr (KIND == kListed) held = q;
         const int nth = range * NW + wave, of = (int)p.splits * NW;
         first = (int)((int64_t)tiles * nth / of);
         last = (int)((int64_t)tiles * (nth + 1) / of);
@@ -134,26 +142,35 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
     }
     v_off = (uint32_t)(4 * g) * (uint32_t)a.c.slot_stride + ((uint32_t)col * (DP / 16) < a.c.dim ? (uint32_t)col * (DP / 16) : 0u);
 
-    for (; r < (int)a.b.n_reqs && (WHOLE || seg0 < last); r++) {
-        const Request q = !WHOLE && a.b.n_reqs <= 64u ? request_in(held, r) : request_of(a.b, a.c, r);
+    for (; KIND == kListed || (r < (int)a.b.n_reqs && (WHOLE || seg0 < last)); r++) {
+        const Request q = KIND == kListed ? held : !WHOLE && a.b.n_reqs <= 64u ? request_in(held, r) : request_of(a.b, a.c, r);
         const int seg_tiles = WHOLE ? last : tiles_of(q), seg_first = seg0;
         seg0 += seg_tiles;
         const int rows = q.fresh * (int)a.group;
         if (!WHOLE && (!seg_tiles || row0 >= rows)) continue;
         // this context's tiles in this range
         const int from = max(first, seg_first) - seg_first, to = min(last, seg_first + seg_tiles) - seg_first, tiles = to - from;
-        const int begin = 32 * from, end = min(q.len, 32 * to);
+        const int begin = 32 * from, end = min(KIND == kListed ? listed_tokens(a, q) : q.len, 32 * to);
 
         // entries and scales of the sixteens of 32 tiles, one a lane, and of the 32 tiles behind them
+        // (where blocks are listed, places count in the list's order, and `left` is what the query sees of a sixteen)
         struct Look {
             int entry;
             float ks, vs;
+            int left;
         };
         auto look = [&](int tile) {
-            Look l{-1, 0.0f, 0.0f};
+            Look l{-1, 0.0f, 0.0f, 0};
             const int t = begin + 32 * tile + 16 * lane;
             if (t < end) {
-                l.entry = entry_of(a.c, q.row, block_of(a.c, (uint32_t)t >> 4));
+                uint32_t block = block_of(a.c, (uint32_t)t >> 4);
+                if constexpr (KIND == kListed) {
+                    const uint32_t slot = (uint32_t)t - block * a.c.bs;
+                    block = (uint32_t)a.blocks[((int64_t)q.start * a.c.heads + head) * a.n_select + block];
+                    l.left = block <= (uint32_t)(q.len - 1) / a.c.bs ? min(16, q.len - (int)(block * a.c.bs + slot)) : 0;
+                    if (l.left <= 0) block = a.c.max_blocks;
+                }
+                l.entry = entry_of(a.c, q.row, block);
                 if (l.entry >= 0) {
                     l.ks = *scale_at(a.c, 0, l.entry, head) * a.scale_log2;
                     l.vs = *scale_at(a.c, 1, l.entry, head);
@@ -161,7 +178,7 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
             }
             return l;
         };
-        Look here = look(0), behind{-1, 0.0f, 0.0f};
+        Look here = look(0), behind{-1, 0.0f, 0.0f, 0};
 
         u32x4 qf[NT][KK];
         int lim[NT];                            // the last position a column's query sees
@@ -169,7 +186,7 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
         for (int n = 0; n < NT; n++) {
             const int row = row0 + 16 * n + col;
             const QueryRow w = query_row(a, head, (uint32_t)min(row, max(rows - 1, 0)));     // (columns behind the last row: not written)
-            lim[n] = row < rows ? q.len - q.fresh + w.token : q.len;
+            lim[n] = KIND == kListed ? INT_MAX : row < rows ? q.len - q.fresh + w.token : q.len;
             const uint16_t *src = static_cast<const uint16_t *>(a.q.data) + (int64_t)min(q.start + w.token, (int)a.b.total_new - 1) * a.q.row_stride +
                                   (int64_t)w.head * a.q.head_stride;
 #pragma unroll
@@ -178,7 +195,7 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
                 qf[n][k] = *reinterpret_cast<const u32x4 *>(src + (d < (int)a.c.dim ? d : 0));
             }
         }
-        const int all_see = q.len - q.fresh + row0 / (int)a.group;      // what every row of the tile sees
+        const int all_see = KIND == kListed ? INT_MAX : q.len - q.fresh + row0 / (int)a.group;      // what every row of the tile sees
 
         // Where a sixteen's codes lie; one that is not there is read at the cache's first block and counts no token.
         auto place = [&](int tile, int x) {
@@ -247,7 +264,8 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
 #pragma unroll
             for (int x = 0; x < 2; x++) {
                 const int six = 2 * (tile & 31) + x;
-                count[x] = __builtin_amdgcn_readlane(here.entry, six) < 0 ? 0 : min(16, end - t0 - 16 * x);
+                if constexpr (KIND == kListed) count[x] = __builtin_amdgcn_readlane(here.entry, six) < 0 ? 0 : __builtin_amdgcn_readlane(here.left, six);
+                else count[x] = __builtin_amdgcn_readlane(here.entry, six) < 0 ? 0 : min(16, end - t0 - 16 * x);
                 ks[x] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(here.ks), six));
                 const uint32_t scale = (uint32_t)__builtin_amdgcn_readlane(__float_as_int(here.vs), six);
                 vs[x] = mantissa_of(scale), ve[x] = exponent_of(scale);
@@ -285,7 +303,7 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
                         for (int y = 0; y < VW; y++) rv[4 * x + i][y] = there ? rv[4 * x + i][y] : 0u;
                     }
             }
-            if (p.scores) {
+            if (KIND == kWhole && p.scores) {
                 // (-inf says that a query does not see a token: its weight is 0 then whatever the row's total, a NaN too)
 #pragma unroll
                 for (int n = 0; n < NT; n++) {
@@ -466,7 +484,7 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
                 float l_all;
                 const float total = total_of(row, l_all), f = total == -INFINITY && l_all == 0.0f ? 0.0f : 1.0f / l_all;
                 const QueryRow w = query_row(a, head, (uint32_t)row);
-                if (p.splits > 1u) {
+                if (KIND == kRest || p.splits > 1u) {
                     const int64_t part = ((int64_t)(q.start + w.token) * a.q_heads + w.head) * p.splits + range;
                     if (g == 0 && j == 0) p.sums[part] = f32x2{top_of(row), l_all};
                     float *dst = p.parts + part * a.c.dim;
@@ -486,7 +504,7 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
                 }
                 if (a.lse && g == 0 && j == 0) a.lse[(int64_t)(q.start + w.token) * a.q_heads + w.head] = total * kLn2;
             }
-            if (!a.w.data || p.splits > 1u) return;
+            if (KIND != kWhole || !a.w.data || p.splits > 1u) return;
             // weights, out of the scores that the same lane wrote
             float total[NT], unused;
 #pragma unroll
@@ -618,12 +636,12 @@ template <bool WHOLE> __device__ __forceinline__ float total_of(const AttendArgs
 // others: weights out of the scores, four tokens a thread; query rows are added in order, so no result depends on timing.  Bound by
 // loads that wait for each other: 8 us behind the 181 above; 16 contexts of up to 8192 tokens with weights 8 us
 // behind 32 (what waits for no total is read first; 10 with one variant for both layouts of parts).
-template <typename T, bool WHOLE>
+template <typename T, bool WHOLE, Kind KIND = kWhole>
 __global__ __launch_bounds__(256) void finish_kernel(AttendArgs a, TokensPlan p)
 {
     __shared__ float totals[kFewRows];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const Request q = request_of(a.b, a.c, (int)blockIdx.y);
+    const Request q = KIND == kListed ? token_of(a.b, a.c, (int)blockIdx.y) : request_of(a.b, a.c, (int)blockIdx.y);
     const uint32_t rows = (uint32_t)q.fresh * a.group;
     if (blockIdx.x < p.join_blocks) {
         const uint32_t n = blockIdx.x * 4u + (uint32_t)wave;
@@ -665,6 +683,7 @@ __global__ __launch_bounds__(256) void finish_kernel(AttendArgs a, TokensPlan p)
         if (a.lse && !lane) a.lse[at] = total * kLn2;
         return;
     }
+    if constexpr (KIND != kWhole) return;       // (no weights)
     const uint32_t rest = blockIdx.x - p.join_blocks, head = rest % a.c.heads;
     const int t0 = 1024 * (int)(rest / a.c.heads), t = t0 + 4 * (int)threadIdx.x, older = q.len - q.fresh;
     if (t0 >= q.len) return;
@@ -734,6 +753,33 @@ template <typename T> static hipError_t tokens(const AttendArgs &a, const Tokens
     if (p.whole) finish_kernel<T, true><<<finish, 256, 0, s>>>(a, p);
     else finish_kernel<T, false><<<finish, 256, 0, s>>>(a, p);
     return hipGetLastError();
+}
+
+// A workgroup (or p.splits of them) for each request or new token and head: the rest of contexts behind a prefix, whose parts another
+// kernel joins, or listed blocks.
+template <typename T, Kind KIND> static hipError_t tokens_apart(const AttendArgs &a, const TokensPlan &p, hipStream_t s)
+{
+    const uint32_t units = KIND == kListed ? a.b.total_new : a.b.n_reqs;
+    auto launch = [&](auto dp_, auto nt_) {
+        constexpr int DP = decltype(dp_)::value, NT = decltype(nt_)::value, threads = 64 * waves_of(DP, NT, true);
+        const uint64_t groups = (uint64_t)units * a.c.heads * p.splits;
+        if (!launchable(groups, threads)) return hipErrorInvalidConfiguration;
+        tokens_kernel<T, DP, NT, true, KIND><<<(uint32_t)groups, threads, 0, s>>>(a, p);
+        return hipGetLastError();
+    };
+    const int dp = a.c.dim <= 64 ? 64 : a.c.dim <= 128 ? 128 : 256;
+    hipError_t e;
+    if (p.tile_rows == 16) e = dp == 64 ? launch(Int<64>{}, Int<1>{}) : dp == 128 ? launch(Int<128>{}, Int<1>{}) : launch(Int<256>{}, Int<1>{});
+    else e = dp == 64 ? launch(Int<64>{}, Int<2>{}) : launch(Int<128>{}, Int<2>{});
+    if (KIND != kListed || e != hipSuccess || p.splits == 1u) return e;
+    finish_kernel<T, true, KIND><<<dim3(p.join_blocks, units), 256, 0, s>>>(a, p);
+    return hipGetLastError();
+}
+
+hipError_t launch_tokens_apart(const AttendArgs &a, const TokensPlan &p, Kind kind, uint32_t dtype, hipStream_t s)
+{
+    if (kind == kListed) return dtype == DMI_DTYPE_BF16 ? tokens_apart<Bf16, kListed>(a, p, s) : tokens_apart<Fp16, kListed>(a, p, s);
+    return dtype == DMI_DTYPE_BF16 ? tokens_apart<Bf16, kRest>(a, p, s) : tokens_apart<Fp16, kRest>(a, p, s);
 }
 
 hipError_t launch_tokens(const AttendArgs &a, const TokensPlan &p, uint32_t dtype, hipStream_t s)
