@@ -13,6 +13,8 @@ constexpr uint32_t kMaxDim = 256;
 constexpr int64_t kMaxSlotStride = 1 << 26;     // sixteen tokens lie within 32-bit offsets of the first
 constexpr uint32_t kMaxReqs = 65535;            // requests of a call: what a launch's second dimension holds
 
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
 // A cache as the kernels see it; [0] is K, [1] is V.
 struct Cache {
     uint8_t *code[2];
@@ -84,7 +86,8 @@ struct SelectArgs {
     int64_t bounds_block_stride, bounds_head_stride;
     uint32_t group, n_select, n_first, n_recent;
     uint32_t stride;                            // blocks of the longest request
-    uint64_t *keys;                             // [new token][head][stride], scores in an order of unsigned numbers
+    f32x2 *scores;                              // [new token][head][stride]: a score, how far it may be off
+    uint64_t *keys;                             // the same places: scores in 64 bits, as unsigned numbers in their order
     int32_t *blocks;
 };
 
@@ -103,8 +106,6 @@ struct AttendArgs {
 // What the attention kernels do: a whole context; the rest of one behind a shared prefix, whose sums are left as parts whatever their
 // number; such a prefix, for all rows of a group of requests; listed blocks, for each new token by itself.
 enum Kind { kWhole, kRest, kPrefix, kListed };
-
-typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 constexpr uint32_t kFewRows = 32;               // query rows that share a head: up to here by tokens_kernel
 

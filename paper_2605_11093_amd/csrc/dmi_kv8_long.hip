@@ -126,7 +126,7 @@ dmi_status_t check_select(const dmi_kv8_t &cache, const dmi_kv8_batch_t &b, uint
 uint64_t select_bytes(const dmi_kv8_t &cache, const dmi_kv8_batch_t &b, uint32_t n_select)
 {
     const uint32_t stride = score_stride(cache, b);
-    return stride > n_select ? (uint64_t)b.total_new * cache.n_heads * stride * 8u : 0u;
+    return stride > n_select ? 2u * pad64((uint64_t)b.total_new * cache.n_heads * stride * 8u) : 0u;
 }
 
 }  // namespace
@@ -161,7 +161,8 @@ extern "C" dmi_status_t dmi_kv8_select(const dmi_kv8_t *cache, const dmi_kv8_bat
     a.group = n_q_heads / a.c.heads;
     a.n_select = n_select, a.n_first = n_first, a.n_recent = n_recent;
     a.stride = score_stride(*cache, *batch);
-    a.keys = static_cast<uint64_t *>(workspace);
+    a.scores = static_cast<f32x2 *>(workspace);
+    a.keys = reinterpret_cast<uint64_t *>(static_cast<char *>(workspace) + select_bytes(*cache, *batch, n_select) / 2u);
     a.blocks = blocks_dev;
     return launched(launch_select(a, q->dtype, (hipStream_t)hip_stream));
 }

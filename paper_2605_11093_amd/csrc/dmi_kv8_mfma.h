@@ -16,7 +16,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 // Matrix instructions take bf16 or f16 as q comes; an e4m3 number is one of either exactly.
 struct Bf16 {
     static constexpr bool kNarrow = false;      // as wide a range of exponents as fp32
-    static constexpr uint32_t kOne = 0x3F80u;
+    static constexpr uint32_t kOne = 0x3F80u, kExponent = 0x7F80u;
     static __device__ __forceinline__ float number(uint16_t w) { return __uint_as_float((uint32_t)w << 16); }
     // two neighbouring codes of a word, times a power of two
     static __device__ __forceinline__ uint32_t two_codes(uint32_t w, bool hi, float power = 1.0f)
@@ -41,7 +41,7 @@ struct Bf16 {
 
 struct Fp16 {
     static constexpr bool kNarrow = true;
-    static constexpr uint32_t kOne = 0x3C00u;
+    static constexpr uint32_t kOne = 0x3C00u, kExponent = 0x7C00u;
     static __device__ __forceinline__ float number(uint16_t w) { return (float)__builtin_bit_cast(_Float16, w); }
     static __device__ __forceinline__ uint32_t two_codes(uint32_t w, bool hi, float power = 1.0f)
     {

@@ -26,193 +26,440 @@ __device__ __forceinline__ uint64_t order_of(double x)
     const uint64_t u = __builtin_bit_cast(uint64_t, x + 0.0);
     return u >> 63 ? ~u : u | 1ull << 63;
 }
-constexpr uint32_t kRowsAtOnce = 4;             // query rows whose scores a lane sums at a time
-
-// A workgroup per new token, head and 256 blocks, a lane per block: the larger of q x least and q x largest is one product with the
-// one or the other, by q's sign, so that a score is the sum of two products' and every term but rounding in 64 bits is exact.  The
-// order in which it is summed moves a score by some 2^-50 of its terms, and which blocks are taken hangs on no order.
-template <typename T, int DP>
-__global__ __launch_bounds__(256) void score_kernel(SelectArgs a)
+__device__ __forceinline__ uint32_t order_of(float x)
 {
-    __shared__ __align__(16) double lq[DP][kRowsAtOnce][2];
-    const uint32_t per = (a.stride + 255u) / 256u, item = blockIdx.x / per, chunk = blockIdx.x - item * per;
-    const uint32_t token = item / a.c.heads, head = item - token * a.c.heads;
-    const Request q = token_of(a.b, a.c, (int)token);
-    const Choice x = choice_of(a, q);
-    const uint32_t block = x.lo + 256u * chunk + threadIdx.x;
-    if (q.fresh <= 0 || x.lo + 256u * chunk >= x.hi) return;
+    const uint32_t u = __float_as_uint(x);
+    return u >> 31 ? ~u : u | 1u << 31;
+}
+__device__ __forceinline__ float float_of(uint32_t order) { return __uint_as_float(order >> 31 ? order & 0x7FFFFFFFu : ~order); }
 
-    const int entry = block < x.hi ? entry_of(a.c, q.row, block) : -1;
-    u32x4 low[DP / 16], high[DP / 16];
-    const uint8_t *const at = a.bounds + (int64_t)max(entry, 0) * a.bounds_block_stride + (int64_t)head * a.bounds_head_stride;
-#pragma unroll
-    for (int i = 0; i < DP / 16; i++) low[i] = *reinterpret_cast<const u32x4 *>(at + (16u * i < a.c.dim ? 16u * i : 0u));
-#pragma unroll
-    for (int i = 0; i < DP / 16; i++) high[i] = *reinterpret_cast<const u32x4 *>(at + a.c.dim + (16u * i < a.c.dim ? 16u * i : 0u));
-    const double scale = entry >= 0 ? (double)*scale_at(a.c, 0, entry, head) : 0.0;
+// Largest of what 16 lanes have
+__device__ __forceinline__ float largest_of_16(float x)
+{
+    auto turned = [](float v, auto n) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x120 + decltype(n)::value, 0xF, 0xF, false)); };
+    x = fmaxf(x, turned(x, Int<8>{}));
+    x = fmaxf(x, turned(x, Int<4>{}));
+    x = fmaxf(x, turned(x, Int<2>{}));
+    return fmaxf(x, turned(x, Int<1>{}));
+}
 
-    double best = -INFINITY;
-    bool bad = false;
-    for (uint32_t row0 = 0; row0 < a.group; row0 += kRowsAtOnce) {
-        const uint32_t rows = min(kRowsAtOnce, a.group - row0);
-        if (row0) __syncthreads();
-        for (uint32_t u = threadIdx.x; u < DP * kRowsAtOnce; u += 256u) {
-            const uint32_t r = u / DP, d = u - r * DP;
-            double v = 0.0;
-            if (r < rows && d < a.c.dim)
-                v = T::number(static_cast<const uint16_t *>(a.q.data)[(int64_t)token * a.q.row_stride + (int64_t)(head * a.group + row0 + r) * a.q.head_stride + d]);
-            lq[d][r][0] = v > 0.0 ? 0.0 : v;
-            lq[d][r][1] = v > 0.0 ? v : 0.0;
-        }
-        __syncthreads();
-        double sum[kRowsAtOnce] = {};
+// ---------------------------------------------------------------- scores, nearly
+// The larger of q x least and q x largest is one product with the one or the other, by q's sign: a score is the product of a row (q where
+// it is negative; q where it is positive) with a column (least; largest), and matrix instructions take it, 16 blocks x 16 query rows at a
+// time.  Every product is exact in fp32; their sum is off by no more than 2 dim + 16 roundings (of one unit in the last place, whatever
+// the instruction's order and rounding) of 448 sum |q|, the most that the terms' magnitudes add up to, and by what numbers of q below
+// the normal ones make, should they count as 0.  What lies nearer than twice that to the score at which the selection ends is looked at
+// again in 64 bits.
+//
+// 32 blocks a wavefront at a time, all of whose bounds are asked for before any is used.
+template <typename T, int DP> struct Scorer {
+    static constexpr int KL = DP / 64, KK = DP / 32;
+    const SelectArgs &a;
+    const Request &q;
+    uint32_t token, head;
+    int lane, col, g;
+    u32x4 below[KK], above[KK];                 // q where it is negative, positive
+    float off;                                  // how far a score may be off, before K's scale
+
+    __device__ __forceinline__ Scorer(const SelectArgs &a_, const Request &q_, uint32_t token_, uint32_t head_)
+        : a(a_), q(q_), token(token_), head(head_), lane(threadIdx.x & 63), col(lane & 15), g(lane >> 4), off(0.0f) {}
+
+    __device__ __forceinline__ void rows(uint32_t row0)
+    {
+        const uint32_t row = min(row0 + (uint32_t)col, a.group - 1u);
+        const uint16_t *const src = static_cast<const uint16_t *>(a.q.data) + (int64_t)token * a.q.row_stride + (int64_t)(head * a.group + row) * a.q.head_stride;
+        float sum = 0.0f, faint = 0.0f;
 #pragma unroll
-        for (int i = 0; i < DP / 16; i++) {
-            if (16u * i >= a.c.dim) break;
+        for (int k = 0; k < KK; k++) {
+            const uint32_t d = (uint32_t)(g * (DP / 4) + 8 * k);
+            const u32x4 w = *reinterpret_cast<const u32x4 *>(src + (d < a.c.dim ? d : 0u));
 #pragma unroll
-            for (int w = 0; w < 4; w++) {
-                const f32x2 l[2] = {__builtin_amdgcn_cvt_pk_f32_fp8((int)low[i][w], false), __builtin_amdgcn_cvt_pk_f32_fp8((int)low[i][w], true)};
-                const f32x2 h[2] = {__builtin_amdgcn_cvt_pk_f32_fp8((int)high[i][w], false), __builtin_amdgcn_cvt_pk_f32_fp8((int)high[i][w], true)};
+            for (int i = 0; i < 4; i++) {
+                const uint32_t v = d < a.c.dim ? w[i] : 0u, sign = (v >> 15 & 0x00010001u) * 0xFFFFu;
+                below[k][i] = v & sign, above[k][i] = v & ~sign;
 #pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    const double least = l[e >> 1][e & 1], largest = h[e >> 1][e & 1];
-#pragma unroll
-                    for (uint32_t r = 0; r < kRowsAtOnce; r++) {
-                        sum[r] = __builtin_fma(lq[16 * i + 4 * w + e][r][0], least, sum[r]);
-                        sum[r] = __builtin_fma(lq[16 * i + 4 * w + e][r][1], largest, sum[r]);
-                    }
+                for (int y = 0; y < 2; y++) {
+                    const float size = fabsf(T::number((uint16_t)(v >> 16 * y)));
+                    sum += size;
+                    if (!(v >> 16 * y & T::kExponent)) faint += size;
                 }
             }
         }
-#pragma unroll
-        for (uint32_t r = 0; r < kRowsAtOnce; r++)
-            if (r < rows) {
-                bad |= sum[r] != sum[r];
-                best = sum[r] > best ? sum[r] : best;
-            }
+        sum += __shfl_xor(sum, 16), faint += __shfl_xor(faint, 16);
+        sum += __shfl_xor(sum, 32), faint += __shfl_xor(faint, 32);
+        // (of nothing but zeros every score is 0 or no number, and that is exact)
+        const float most = sum == 0.0f ? 0.0f : sum > 0x1p-90f && sum < 0x1p+100f ? 448.0f * ((float)(2 * DP + 16) * 0x1p-23f * sum + 1.001f * faint) : INFINITY;
+        off = fmaxf(off, largest_of_16(most));
     }
-    if (block < x.hi) a.keys[(int64_t)item * a.stride + block] = order_of(entry < 0 || bad ? -INFINITY : best * scale);
+    // Scores of blocks block0 .. block0 + 31 by these rows, one in each of lanes 0-31, and K's scale of it (where `end` or the cache ends
+    // before: 0).  INFINITY says that one of them is no number.
+    __device__ __forceinline__ float of(uint32_t row0, uint32_t block0, uint32_t end, float &scale)
+    {
+        const uint32_t block = block0 + (uint32_t)(lane & 31);
+        const int entry = block < end ? entry_of(a.c, q.row, block) : -1;
+        scale = entry >= 0 ? *scale_at(a.c, 0, entry, head) : 0.0f;
+        u32x4 low[2][KL], high[2][KL];
+#pragma unroll
+        for (int x = 0; x < 2; x++) {
+            const uint8_t *const at = a.bounds + (int64_t)max(__shfl(entry, 16 * x + col), 0) * a.bounds_block_stride + (int64_t)head * a.bounds_head_stride;
+#pragma unroll
+            for (int c = 0; c < KL; c++) {
+                const uint32_t d = (uint32_t)(g * (DP / 4) + 16 * c), from = d < a.c.dim ? d : 0u;
+                low[x][c] = *reinterpret_cast<const u32x4 *>(at + from);
+                high[x][c] = *reinterpret_cast<const u32x4 *>(at + a.c.dim + from);
+            }
+        }
+        f32x4 z[2];
+#pragma unroll
+        for (int x = 0; x < 2; x++) {
+            z[x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int k = 0; k < KK; k++) {
+                const u32x4 &l = low[x][k / 2], &h = high[x][k / 2];
+                const uint32_t l0 = l[2 * (k % 2)], l1 = l[2 * (k % 2) + 1], h0 = h[2 * (k % 2)], h1 = h[2 * (k % 2) + 1];
+                z[x] = T::mfma16(u32x4{T::two_codes(l0, false), T::two_codes(l0, true), T::two_codes(l1, false), T::two_codes(l1, true)}, below[k], z[x]);
+                z[x] = T::mfma16(u32x4{T::two_codes(h0, false), T::two_codes(h0, true), T::two_codes(h1, false), T::two_codes(h1, true)}, above[k], z[x]);
+            }
+        }
+        const bool real = row0 + (uint32_t)col < a.group;
+#pragma unroll
+        for (int x = 0; x < 2; x++)
+#pragma unroll
+            for (int i = 0; i < 4; i++) z[x][i] = largest_of_16(real ? (z[x][i] == z[x][i] ? z[x][i] : INFINITY) : -INFINITY);
+        // block 16 x + 4 g + i to its lane
+        const int from = (lane >> 2 & 3) * 16;
+        float best = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const float v0 = __shfl(z[0][i], from), v1 = __shfl(z[1][i], from);
+            if ((lane & 3) == i) best = lane & 16 ? v1 : v0;
+        }
+        return best;
+    }
+};
+// A block's score as it counts: none where there is no block (scale 0), or no number
+__device__ __forceinline__ float counted(float best, float scale)
+{
+    const float v = best * scale;
+    return scale != 0.0f && fabsf(v) < INFINITY ? v + 0.0f : -INFINITY;
 }
 
-constexpr uint32_t kChooseThreads = 256, kChooseHeld = 16;      // keys a thread keeps: 4096 blocks
-constexpr uint32_t kChooseBins = 2048;
-
-// A workgroup per new token and head: the want-th largest score digit by digit, from the top and only as far as it takes to tell
-// it from the others, then the blocks in order.
-__global__ __launch_bounds__(kChooseThreads) void choose_kernel(SelectArgs a)
+// A score in 64 bits, as an unsigned number in their order: a wavefront's work.
+template <typename T> __device__ __forceinline__ uint64_t exact_order(const SelectArgs &a, const Request &q, uint32_t token, uint32_t head, uint32_t block)
 {
-    constexpr uint32_t kWaves = kChooseThreads / 64;
-    __shared__ uint32_t hist[kChooseBins], wave_n[kWaves][2], found[3];
-    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6, item = blockIdx.x, token = item / a.c.heads;
-    const Request q = token_of(a.b, a.c, (int)token);
-    if (q.fresh <= 0) return;                   // no request's
-    const Choice x = choice_of(a, q);
-    int32_t *const to = a.blocks + (int64_t)item * a.n_select;
-    if (x.seen <= a.n_select) {
-        for (uint32_t i = tid; i < a.n_select; i += kChooseThreads) to[i] = i < x.seen ? (int32_t)i : -1;
-        return;
-    }
-    const uint32_t want = a.n_select - a.n_first - a.n_recent, count = x.hi - x.lo;
-    for (uint32_t i = tid; i < a.n_first; i += kChooseThreads) to[i] = (int32_t)i;
-    for (uint32_t i = tid; i < a.n_recent; i += kChooseThreads) to[a.n_first + want + i] = (int32_t)(x.hi + i);
-    if (!want) return;
-    const uint64_t *const keys = a.keys + (int64_t)item * a.stride + x.lo;
-    uint64_t held[kChooseHeld];
-#pragma unroll
-    for (uint32_t k = 0; k < kChooseHeld; k++) held[k] = k * kChooseThreads + tid < count ? keys[k * kChooseThreads + tid] : 0ull;
-    // of the keys that begin with `prefix` the rank-th is looked for; all of those that begin with a larger one are taken
-    uint64_t prefix = 0;
-    uint32_t rank = want;
-    int shift = 64;
-    while (shift > 0) {
-        const int bits = min(11, shift);
-        const uint32_t bins = 1u << bits;
-        const int above = shift;
-        shift -= bits;
-        for (uint32_t i = tid; i < kChooseBins; i += kChooseThreads) hist[i] = 0;
-        __syncthreads();
-        auto add = [&](uint64_t k) {
-            if (above == 64 || k >> above == prefix) atomicAdd(&hist[(uint32_t)(k >> shift) & (bins - 1u)], 1u);
-        };
-#pragma unroll
-        for (uint32_t k = 0; k < kChooseHeld; k++)
-            if (k * kChooseThreads + tid < count) add(held[k]);
-        for (uint32_t i = kChooseHeld * kChooseThreads + tid; i < count; i += kChooseThreads) add(keys[i]);
-        __syncthreads();
-        // eight bins a thread, from the largest down
-        uint32_t n[8], sum = 0;
-#pragma unroll
-        for (int i = 0; i < 8; i++) sum += n[i] = hist[kChooseBins - 1u - 8u * tid - i];
-        uint32_t before = (uint32_t)lanes_scan((int)sum);
-        if (lane == 63u) wave_n[wave][0] = before;
-        __syncthreads();
-        before -= sum;
-#pragma unroll
-        for (uint32_t v = 0; v < kWaves; v++)
-            if (v < wave) before += wave_n[v][0];
-#pragma unroll
-        for (int i = 0; i < 8; i++) {
-            if (before < rank && rank <= before + n[i]) {
-                found[0] = kChooseBins - 1u - 8u * tid - i;
-                found[1] = rank - before;
-                found[2] = n[i];
-            }
-            before += n[i];
+    const uint32_t lane = threadIdx.x & 63u;
+    const int entry = entry_of(a.c, q.row, block);
+    if (entry < 0) return order_of((double)-INFINITY);
+    const uint8_t *const at = a.bounds + (int64_t)entry * a.bounds_block_stride + (int64_t)head * a.bounds_head_stride;
+    double best = -INFINITY;
+    bool bad = false;
+    for (uint32_t r = 0; r < a.group; r++) {
+        const uint16_t *const src = static_cast<const uint16_t *>(a.q.data) + (int64_t)token * a.q.row_stride + (int64_t)(head * a.group + r) * a.q.head_stride;
+        double sum = 0.0;
+        for (uint32_t d = lane; d < a.c.dim; d += 64u) {
+            const double v = T::number(src[d]);
+            const double least = v * __builtin_amdgcn_cvt_f32_fp8((int)at[d], 0), most = v * __builtin_amdgcn_cvt_f32_fp8((int)at[a.c.dim + d], 0);
+            sum += least != least || most != most ? NAN : fmax(least, most);
         }
-        __syncthreads();
-        prefix = prefix << bits | found[0];
-        rank = found[1];
-        if (found[2] == rank) break;            // all of these are taken
+#pragma unroll
+        for (int m = 32; m; m >>= 1) sum += __shfl_xor(sum, m);
+        bad |= sum != sum;
+        best = sum > best ? sum : best;
     }
-    // `rank` of the keys that begin with `prefix` are taken, the lowest blocks first
+    return order_of(bad ? (double)-INFINITY : best * (double)*scale_at(a.c, 0, entry, head));
+}
+
+// ---------------------------------------------------------------- which blocks
+constexpr uint32_t kScoreThreads = 256, kBlocksAtOnce = kScoreThreads / 2;      // blocks of a workgroup
+constexpr uint32_t kMostInLds = 8192;                           // blocks whose scores a workgroup keeps
+constexpr uint32_t kPickBins = 2048;
+constexpr uint32_t kClose = 256;                                // blocks near the border that are ranked in LDS
+
+struct PickShared {
+    uint32_t hist[kPickBins];
+    uint32_t wave_n[16][2], found[3], count[3];
+    float wave_x[16][3];
+    uint32_t close[kClose];
+    uint64_t order[kClose];
+};
+
+// The bin that holds the rank-th of those counted, from the largest bin down: found = bin, rank in it, how many it has.
+template <uint32_t N> __device__ __forceinline__ void find_bin(PickShared &s, uint32_t rank)
+{
+    constexpr uint32_t kEach = kPickBins / N;
+    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6;
+    __syncthreads();
+    uint32_t n[kEach], sum = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < kEach; i++) sum += n[i] = s.hist[kPickBins - 1u - kEach * tid - i];
+    uint32_t before = (uint32_t)lanes_scan((int)sum);
+    if (lane == 63u) s.wave_n[wave][0] = before;
+    __syncthreads();
+    before -= sum;
+#pragma unroll
+    for (uint32_t v = 0; v < N / 64u; v++)
+        if (v < wave) before += s.wave_n[v][0];
+#pragma unroll
+    for (uint32_t i = 0; i < kEach; i++) {
+        if (before < rank && rank <= before + n[i]) {
+            s.found[0] = kPickBins - 1u - kEach * tid - i;
+            s.found[1] = rank - before;
+            s.found[2] = n[i];
+        }
+        before += n[i];
+    }
+    __syncthreads();
+}
+
+// Of `count` unsigned numbers that key(i) gives, those that begin with `prefix` (their bits from `shift` on) hold the want-th largest: `rank`-th
+// of them, `same` in all.  Digit by digit, from the top and, unless all bits are asked for, only as far as it takes to tell it from the others.
+template <uint32_t N, typename U, typename Key>
+__device__ __forceinline__ void find_rank(PickShared &s, uint32_t count, uint32_t want, bool all_bits, const Key &key, U &prefix, int &shift, uint32_t &rank)
+{
+    const uint32_t tid = threadIdx.x;
+    prefix = 0;
+    rank = want;
+    shift = 8 * (int)sizeof(U);
+    while (shift > 0) {
+        const int bits = min(11, shift), above = shift;
+        shift -= bits;
+        for (uint32_t i = tid; i < kPickBins; i += N) s.hist[i] = 0;
+        __syncthreads();
+        for (uint32_t i = tid; i < count; i += N) {
+            const U k = key(i);
+            if (above == 8 * (int)sizeof(U) || k >> above == prefix) atomicAdd(&s.hist[(uint32_t)(k >> shift) & ((1u << bits) - 1u)], 1u);
+        }
+        find_bin<N>(s, rank);
+        prefix = prefix << bits | s.found[0];
+        rank = s.found[1];
+        if (!all_bits && s.found[2] == rank) break;
+    }
+}
+
+// Numbers lo + i of those i < count that are more than, or among the first `rank` that are equal, in order.
+template <uint32_t N, typename Which> __device__ __forceinline__ void write_in_order(PickShared &s, uint32_t count, uint32_t lo, uint32_t rank, const Which &which, int32_t *to)
+{
+    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6;
     uint32_t taken = 0, equal = 0;
-    for (uint32_t base = 0; base < count; base += kChooseThreads) {
+    for (uint32_t base = 0; base < count; base += N) {
         const uint32_t i = base + tid;
-        const uint64_t k = i < count ? keys[i] >> shift : 0ull;
-        const bool is_more = i < count && k > prefix, is_equal = i < count && k == prefix;
-        const uint64_t more = __ballot(is_more), same = __ballot(is_equal);
+        const int w = i < count ? which(i) : -1;        // 1: more, 0: equal
+        const uint64_t more = __ballot(w > 0), same = __ballot(w == 0);
         __syncthreads();
         if (!lane) {
-            wave_n[wave][0] = (uint32_t)__popcll(more);
-            wave_n[wave][1] = (uint32_t)__popcll(same);
+            s.wave_n[wave][0] = (uint32_t)__popcll(more);
+            s.wave_n[wave][1] = (uint32_t)__popcll(same);
         }
         __syncthreads();
         uint32_t m = 0, e = 0, all_m = 0, all_e = 0;
 #pragma unroll
-        for (uint32_t v = 0; v < kWaves; v++) {
-            if (v < wave) m += wave_n[v][0], e += wave_n[v][1];
-            all_m += wave_n[v][0];
-            all_e += wave_n[v][1];
+        for (uint32_t v = 0; v < N / 64u; v++) {
+            if (v < wave) m += s.wave_n[v][0], e += s.wave_n[v][1];
+            all_m += s.wave_n[v][0];
+            all_e += s.wave_n[v][1];
         }
         const uint64_t below = (1ull << lane) - 1ull;
         m += (uint32_t)__popcll(more & below);
         e += (uint32_t)__popcll(same & below);
         const uint32_t at = taken + m + min(equal + e, rank) - min(equal, rank);
-        if (is_more || (is_equal && equal + e < rank)) to[a.n_first + at] = (int32_t)(x.lo + i);
+        if (w > 0 || (w == 0 && equal + e < rank)) to[at] = (int32_t)(lo + i);
         taken += all_m + min(equal + all_e, rank) - min(equal, rank);
         equal += all_e;
     }
 }
 
-template <typename T> static void scores(const SelectArgs &a, uint32_t groups, hipStream_t s)
+// (two wavefronts a SIMD with 256 elements, four with fewer)
+template <typename T, int DP> __global__ __launch_bounds__(kScoreThreads) __attribute__((amdgpu_waves_per_eu(DP <= 128 ? 4 : 2))) void score_kernel(SelectArgs a)
 {
-    if (a.c.dim <= 64) score_kernel<T, 64><<<groups, 256, 0, s>>>(a);
-    else if (a.c.dim <= 128) score_kernel<T, 128><<<groups, 256, 0, s>>>(a);
-    else score_kernel<T, 256><<<groups, 256, 0, s>>>(a);
+    const uint32_t per = (a.stride + kBlocksAtOnce - 1u) / kBlocksAtOnce, item = blockIdx.x / per, chunk = blockIdx.x - item * per;
+    const uint32_t token = item / a.c.heads, head = item - token * a.c.heads, lane = threadIdx.x & 63u;
+    const Request q = token_of(a.b, a.c, (int)token);
+    const Choice x = choice_of(a, q);
+    const uint32_t block0 = x.lo + kBlocksAtOnce * chunk + 32u * (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (q.fresh <= 0 || block0 >= x.hi) return;
+    Scorer<T, DP> scorer(a, q, token, head);
+    float scale = 0.0f, s = -INFINITY;
+    for (uint32_t row0 = 0; row0 < a.group; row0 += 16u) {
+        scorer.rows(row0);
+        s = fmaxf(s, scorer.of(row0, block0, x.hi, scale));
+    }
+    if (lane < 32u && block0 + lane < x.hi) a.scores[(int64_t)item * a.stride + block0 + lane] = f32x2{counted(s, scale), scorer.off * scale};
+}
+
+// N threads per new token and head.  Scores in fp32 (made here, FUSED; else score_kernel has left them in memory), of which LDS holds as many
+// as it has room for; which of 2048 even steps between the least and the largest the want-th largest lies in, and which it is of those;
+// what lies nearer to it than the scores' error once more in 64 bits; then the blocks in order.  Which blocks are taken hangs on no rounding but of
+// the 64 bits, and on no order of sums.
+template <typename T, int DP, bool FUSED, uint32_t N>
+__global__ __launch_bounds__(N) __attribute__((amdgpu_waves_per_eu(DP <= 128 ? 4 : 2))) void pick_kernel(SelectArgs a)
+{
+    __shared__ PickShared s;
+    extern __shared__ float own[];              // scores
+    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = (uint32_t)__builtin_amdgcn_readfirstlane(tid >> 6);
+    const uint32_t item = blockIdx.x, token = item / a.c.heads, head = item - token * a.c.heads;
+    const Request q = token_of(a.b, a.c, (int)token);
+    if (q.fresh <= 0) return;                   // no request's
+    const Choice x = choice_of(a, q);
+    int32_t *const to = a.blocks + (int64_t)item * a.n_select;
+    if (x.seen <= a.n_select) {
+        for (uint32_t i = tid; i < a.n_select; i += N) to[i] = i < x.seen ? (int32_t)i : -1;
+        return;
+    }
+    const uint32_t want = a.n_select - a.n_first - a.n_recent, count = x.hi - x.lo;
+    for (uint32_t i = tid; i < a.n_first; i += N) to[i] = (int32_t)i;
+    for (uint32_t i = tid; i < a.n_recent; i += N) to[a.n_first + want + i] = (int32_t)(x.hi + i);
+    if (!want) return;
+    f32x2 *const left = a.scores + (int64_t)item * a.stride + x.lo;
+    const bool in_lds = FUSED || a.stride <= kMostInLds;
+    for (uint32_t i = tid; i < kPickBins; i += N) s.hist[i] = 0;
+    if (tid < 3u) s.count[tid] = 0;
+    // how far the scores may be off, the least and the largest of them
+    float off = 0.0f, least = INFINITY, most = -INFINITY;
+    auto look = [&](float v) { most = fmaxf(most, v), least = fminf(least, v == -INFINITY ? INFINITY : v); };
+    if constexpr (FUSED) {
+        Scorer<T, DP> scorer(a, q, token, head);
+        for (uint32_t row0 = 0; row0 < a.group; row0 += 16u) {
+            scorer.rows(row0);
+            for (uint32_t base = 32u * wave; base < count; base += N / 2u) {
+                float scale, v = scorer.of(row0, x.lo + base, x.hi, scale);
+                off = fmaxf(off, scorer.off * scale);   // (no number where there is no block and no bound: left out)
+                if (lane < 32u && base + lane < count) {
+                    if (row0) v = fmaxf(v, own[base + lane]);
+                    if (row0 + 16u >= a.group) v = counted(v, scale), look(v);
+                    own[base + lane] = v;
+                }
+            }
+        }
+    } else {
+        for (uint32_t i = tid; i < count; i += N) {
+            const f32x2 v = left[i];
+            off = fmaxf(off, v[1]);
+            look(v[0]);
+            if (in_lds) own[i] = v[0];
+        }
+    }
+#pragma unroll
+    for (int m = 32; m; m >>= 1) off = fmaxf(off, __shfl_xor(off, m)), most = fmaxf(most, __shfl_xor(most, m)), least = fminf(least, __shfl_xor(least, m));
+    if (!lane) s.wave_x[wave][0] = off, s.wave_x[wave][1] = most, s.wave_x[wave][2] = least;
+    __syncthreads();
+#pragma unroll
+    for (uint32_t v = 0; v < N / 64u; v++) off = fmaxf(off, s.wave_x[v][0]), most = fmaxf(most, s.wave_x[v][1]), least = fminf(least, s.wave_x[v][2]);
+    auto score = [&](uint32_t i) { return in_lds ? own[i] : left[i][0]; };
+    // A step of the range: equal numbers share one, larger ones have none that is lower
+    const float steps = (float)(kPickBins - 1u) / fmaxf(most - least, 0x1p-100f);
+    auto step_of = [&](float v) { return (uint32_t)fminf(fmaxf((v - least) * steps, 0.0f), (float)(kPickBins - 1u)); };
+    for (uint32_t i = tid; i < count; i += N) atomicAdd(&s.hist[step_of(score(i))], 1u);
+    find_bin<N>(s, want);
+    const uint32_t bin = s.found[0], in_bin = s.found[2];
+    uint32_t rank = s.found[1];
+    if (in_bin <= kClose) {
+        for (uint32_t i = tid; i < count; i += N) {
+            const float v = score(i);
+            if (step_of(v) == bin) s.close[atomicAdd(&s.count[2], 1u)] = order_of(v);
+        }
+        __syncthreads();
+        if (tid < in_bin) {
+            uint32_t more = 0, same = 0;
+            for (uint32_t i = 0; i < in_bin; i++) more += s.close[i] > s.close[tid], same += s.close[i] == s.close[tid];
+            if (more < rank && rank <= more + same) s.found[0] = s.close[tid];
+        }
+        __syncthreads();
+    } else {
+        uint32_t border;
+        int shift;
+        __syncthreads();
+        find_rank<N, uint32_t>(s, count, want, true, [&](uint32_t i) { return order_of(score(i)); }, border, shift, rank);
+        __syncthreads();
+        if (!tid) s.found[0] = border;
+        __syncthreads();
+    }
+    const float t = float_of(s.found[0]);       // the want-th largest
+    // what is nearer to the want-th than both may be off together (and numbers so small that fp32 runs out below them are all near)
+    const float off2 = off > 0.0f && off < 0x1p-80f ? INFINITY : 2.001f * off;
+    auto side = [&](float v) { return v == t ? 0 : v > t ? (v - t > off2 ? 1 : 0) : (t - v > off2 ? -1 : 0); };      // 0: near
+    for (uint32_t i0 = 0; i0 < count; i0 += N) {
+        const uint32_t i = i0 + tid;
+        const int w = i < count ? side(score(i)) : -1;
+        const uint64_t more = __ballot(w > 0), near = __ballot(w == 0);
+        uint32_t at = 0;
+        if (!lane) {
+            if (more) atomicAdd(&s.count[0], (uint32_t)__popcll(more));
+            if (near) at = atomicAdd(&s.count[1], (uint32_t)__popcll(near));
+        }
+        at = (uint32_t)__builtin_amdgcn_readfirstlane((int)at) + (uint32_t)__popcll(near & ((1ull << lane) - 1ull));
+        if (w == 0 && at < kClose) s.close[at] = i;
+    }
+    __syncthreads();
+    const uint32_t close = s.count[1], need = want - s.count[0];
+    if (close == need || (t == -INFINITY && off2 < INFINITY)) {
+        // all of those (where the want-th has no score: as many as are wanted, the lowest first)
+        write_in_order<N>(s, count, x.lo, need, [&](uint32_t i) { return side(score(i)); }, to + a.n_first);
+        return;
+    }
+    if (close <= kClose) {
+        // ranked in 64 bits, equal ones by their number
+        for (uint32_t i = wave; i < close; i += N / 64u) {
+            const uint64_t o = exact_order<T>(a, q, token, head, x.lo + s.close[i]);
+            if (!lane) s.order[i] = o;
+        }
+        __syncthreads();
+        if (tid < close) {
+            const uint64_t o = s.order[tid];
+            const uint32_t mine = s.close[tid];
+            uint32_t before = 0;
+            for (uint32_t i = 0; i < close; i++) before += s.order[i] > o || (s.order[i] == o && s.close[i] < mine);
+            const float v = before < need ? INFINITY : -INFINITY;
+            if (in_lds) own[mine] = v;
+            else left[mine][0] = v;
+        }
+        __threadfence_block();
+        __syncthreads();
+        write_in_order<N>(s, count, x.lo, 0u, [&](uint32_t i) { const float v = score(i); return v == INFINITY ? 1 : v == -INFINITY ? -1 : side(v) > 0 ? 1 : -1; }, to + a.n_first);
+        return;
+    }
+    // more than there is room for: those near in 64 bits through memory, what is sure at either end
+    uint64_t *const keys = a.keys + (int64_t)item * a.stride + x.lo;
+    for (uint32_t i = wave; i < count; i += N / 64u) {
+        const int w = side(score(i));
+        const uint64_t o = w > 0 ? ~0ull : w < 0 ? 0ull : exact_order<T>(a, q, token, head, x.lo + i);
+        if (!lane) keys[i] = o;
+    }
+    __threadfence_block();
+    __syncthreads();
+    uint64_t prefix;
+    int shift;
+    find_rank<N, uint64_t>(s, count, want, false, [&](uint32_t i) { return keys[i]; }, prefix, shift, rank);
+    write_in_order<N>(s, count, x.lo, rank, [&](uint32_t i) { const uint64_t k = keys[i] >> shift; return k > prefix ? 1 : k == prefix ? 0 : -1; }, to + a.n_first);
+}
+
+template <typename T, int DP> static hipError_t select(const SelectArgs &a, hipStream_t s)
+{
+    constexpr uint32_t kFew = 256, kMany = DP <= 128 ? 1024 : 512;
+    const uint64_t items = (uint64_t)a.b.total_new * a.c.heads, per = (a.stride + kBlocksAtOnce - 1u) / kBlocksAtOnce;
+    // One launch where tokens and heads give every compute unit a workgroup, or there are few blocks; scores over more workgroups otherwise.
+    const bool fused = a.stride <= kMostInLds && (items >= 256u || a.stride <= 4u * kBlocksAtOnce);
+    if (!launchable(items, kMany) || !launchable(items * per, kScoreThreads)) return hipErrorInvalidConfiguration;
+    const uint32_t lds = a.stride > a.n_select && a.stride <= kMostInLds ? a.stride * 4u : 0u;
+    if (fused) {
+        pick_kernel<T, DP, true, kFew><<<(uint32_t)items, kFew, lds, s>>>(a);
+        return hipGetLastError();
+    }
+    if (a.stride > a.n_select) {
+        score_kernel<T, DP><<<(uint32_t)(items * per), kScoreThreads, 0, s>>>(a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    pick_kernel<T, DP, false, kMany><<<(uint32_t)items, kMany, lds, s>>>(a);
+    return hipGetLastError();
 }
 
 hipError_t launch_select(const SelectArgs &a, uint32_t dtype, hipStream_t s)
 {
-    const uint64_t items = (uint64_t)a.b.total_new * a.c.heads, groups = items * ((a.stride + 255u) / 256u);
-    if (!launchable(items, kChooseThreads) || !launchable(groups, 256)) return hipErrorInvalidConfiguration;
-    if (a.stride > a.n_select) {
-        if (dtype == DMI_DTYPE_BF16) scores<Bf16>(a, (uint32_t)groups, s);
-        else scores<Fp16>(a, (uint32_t)groups, s);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
-    choose_kernel<<<(uint32_t)items, kChooseThreads, 0, s>>>(a);
-    return hipGetLastError();
+    auto by_dim = [&](auto type) {
+        typedef decltype(type) T;
+        return a.c.dim <= 64 ? select<T, 64>(a, s) : a.c.dim <= 128 ? select<T, 128>(a, s) : select<T, 256>(a, s);
+    };
+    return dtype == DMI_DTYPE_BF16 ? by_dim(Bf16{}) : by_dim(Fp16{});
 }
 
 }  // namespace kv8

@@ -203,6 +203,35 @@ def test_selections_with_what_is_no_number(B):        # noqa: F811
     _check_select(B, s, BF16, 2, 30, 1, 1, bounds=x, q=(q, q.double().cpu().numpy()))
 
 
+@pytest.mark.parametrize("length", [16 * 300, 16 * 1500])
+def test_selections_of_scores_that_lie_close(B, length):        # noqa: F811
+    """What fp32 cannot tell apart is told apart: scores that differ in the last of some forty bits, and not at all; few of them and
+    more than there is room for."""
+    s = Setup(B, 37, [(1, length)], 2, 64, 16)
+    s.k_scale.fill_(0.25)
+    s.cache = B.KV8(s.k, s.v, s.k_scale, s.v_scale, s.table)
+    bounds = np.full((s.k.shape[0], 2, 2, 64), 0x7E, dtype=np.uint8)                  # 448
+    bounds[:, :, :, -1] = s.rng.integers(0, 4, size=bounds.shape[:3])                 # 0 to 3 * 2^-9
+    q = torch.ones((1, 4, 64), dtype=BF16, device=DEV)
+    q[..., -1] = 2.0 ** -12
+    for _ in range(2):
+        _check_select(B, s, BF16, 2, 40, 1, 1, bounds=np.sort(bounds, axis=2), q=(q, q.double().cpu().numpy()))
+        some = s.rng.random(len(bounds)) < 0.97
+        bounds[some, :, :, 0] = 0x70
+    bounds[:] = 0x38
+    _check_select(B, s, BF16, 2, 40, 1, 1, bounds=bounds, q=(q, q.double().cpu().numpy()))
+
+
+@pytest.mark.parametrize("dtype,size", [(FP16, 2.0 ** -22), (FP16, 2.0 ** -14), (BF16, 2.0 ** -120), (BF16, 2.0 ** -132), (BF16, 2.0 ** 118), (BF16, 0.0)])
+def test_selections_by_queries_of_any_size(B, dtype, size):        # noqa: F811
+    s = Setup(B, 38, [(1, 16 * 90), (1, 16 * 40)], 2, 80, 16)
+    q = (torch.from_numpy(s.rng.normal(size=(2, 6, 80))) * size).to(dtype)
+    _check_select(B, s, dtype, 3, 20, 1, 1, q=(q.to(DEV), q.double().numpy()))
+    if size == 2.0 ** 118:
+        q[0, 0, 0], q[1, 3, 3] = float("inf"), -float("inf")
+        _check_select(B, s, dtype, 3, 20, 1, 1, q=(q.to(DEV), q.double().numpy()))
+
+
 def test_no_block_left_out_has_a_larger_score(B):        # noqa: F811
     """Bounds of the codes themselves, and a selection by them: no score of a token in a block is above the block's."""
     s = Setup(B, 36, [(1, 16 * 50)], 1, 64, 16)

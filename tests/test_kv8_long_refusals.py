@@ -120,7 +120,7 @@ def test_selections_tensors():
                 torch.zeros(3, 2, 3, dtype=torch.int64)):
         with pytest.raises(ValueError, match="blocks"):
             B.kv8_select(c, b, bounds, _x(4), bad)
-    assert B.kv8_select_workspace(c, b, 3) == 3 * 2 * 4 * 8 and B.kv8_select_workspace(c, b, 4) == 0
+    assert B.kv8_select_workspace(c, b, 3) >= 3 * 2 * 4 * 8 and B.kv8_select_workspace(c, b, 4) == 0
 
 
 def test_sizes_that_are_refused_have_no_workspace():
