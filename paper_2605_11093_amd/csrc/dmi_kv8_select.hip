@@ -51,7 +51,7 @@ __device__ __forceinline__ float largest_of_16(float x)
 // the normal ones make, should they count as 0.  What lies nearer than twice that to the score at which the selection ends is looked at
 // again in 64 bits.
 //
-// 32 blocks a wavefront at a time, all of whose bounds are asked for before any is used.
+// A wavefront asks for the bounds of its next 16 blocks before it uses those of the last.
 template <typename T, int DP> struct Scorer {
     static constexpr int KL = DP / 64, KK = DP / 32;
     const SelectArgs &a;
@@ -91,48 +91,43 @@ template <typename T, int DP> struct Scorer {
         const float most = sum == 0.0f ? 0.0f : sum > 0x1p-90f && sum < 0x1p+100f ? 448.0f * ((float)(2 * DP + 16) * 0x1p-23f * sum + 1.001f * faint) : INFINITY;
         off = fmaxf(off, largest_of_16(most));
     }
-    // Scores of blocks block0 .. block0 + 31 by these rows, one in each of lanes 0-31, and K's scale of it (where `end` or the cache ends
-    // before: 0).  INFINITY says that one of them is no number.
-    __device__ __forceinline__ float of(uint32_t row0, uint32_t block0, uint32_t end, float &scale)
+    struct Tile {
+        u32x4 low[KL], high[KL];
+        float scale;
+    };
+    // 16 blocks' bounds, and for the lanes with col < 4 K's scale of block 4 g + col (0 where there is none).  entry(i): where block i lies
+    template <typename Entry> __device__ __forceinline__ Tile fetch(const Entry &entry) const
     {
-        const uint32_t block = block0 + (uint32_t)(lane & 31);
-        const int entry = block < end ? entry_of(a.c, q.row, block) : -1;
-        scale = entry >= 0 ? *scale_at(a.c, 0, entry, head) : 0.0f;
-        u32x4 low[2][KL], high[2][KL];
+        Tile x;
+        const int mine = entry((uint32_t)(4 * g + (col & 3)));
+        x.scale = *scale_at(a.c, 0, max(mine, 0), head);
+        const uint8_t *const at = a.bounds + (int64_t)max(entry((uint32_t)col), 0) * a.bounds_block_stride + (int64_t)head * a.bounds_head_stride;
 #pragma unroll
-        for (int x = 0; x < 2; x++) {
-            const uint8_t *const at = a.bounds + (int64_t)max(__shfl(entry, 16 * x + col), 0) * a.bounds_block_stride + (int64_t)head * a.bounds_head_stride;
-#pragma unroll
-            for (int c = 0; c < KL; c++) {
-                const uint32_t d = (uint32_t)(g * (DP / 4) + 16 * c), from = d < a.c.dim ? d : 0u;
-                low[x][c] = *reinterpret_cast<const u32x4 *>(at + from);
-                high[x][c] = *reinterpret_cast<const u32x4 *>(at + a.c.dim + from);
-            }
+        for (int c = 0; c < KL; c++) {
+            const uint32_t d = (uint32_t)(g * (DP / 4) + 16 * c), from = d < a.c.dim ? d : 0u;
+            x.low[c] = *reinterpret_cast<const u32x4 *>(at + from);
+            x.high[c] = *reinterpret_cast<const u32x4 *>(at + a.c.dim + from);
         }
-        f32x4 z[2];
+        if (mine < 0) x.scale = 0.0f;
+        return x;
+    }
+    // The largest score of block 4 g + (col & 3) by these rows (rows behind the group's last are that one again).  INFINITY says that one is
+    // no number.
+    __device__ __forceinline__ float of(const Tile &x) const
+    {
+        f32x4 z = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int x = 0; x < 2; x++) {
-            z[x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int k = 0; k < KK; k++) {
-                const u32x4 &l = low[x][k / 2], &h = high[x][k / 2];
-                const uint32_t l0 = l[2 * (k % 2)], l1 = l[2 * (k % 2) + 1], h0 = h[2 * (k % 2)], h1 = h[2 * (k % 2) + 1];
-                z[x] = T::mfma16(u32x4{T::two_codes(l0, false), T::two_codes(l0, true), T::two_codes(l1, false), T::two_codes(l1, true)}, below[k], z[x]);
-                z[x] = T::mfma16(u32x4{T::two_codes(h0, false), T::two_codes(h0, true), T::two_codes(h1, false), T::two_codes(h1, true)}, above[k], z[x]);
-            }
+        for (int k = 0; k < KK; k++) {
+            const u32x4 &l = x.low[k / 2], &h = x.high[k / 2];
+            const uint32_t l0 = l[2 * (k % 2)], l1 = l[2 * (k % 2) + 1], h0 = h[2 * (k % 2)], h1 = h[2 * (k % 2) + 1];
+            z = T::mfma16(u32x4{T::two_codes(l0, false), T::two_codes(l0, true), T::two_codes(l1, false), T::two_codes(l1, true)}, below[k], z);
+            z = T::mfma16(u32x4{T::two_codes(h0, false), T::two_codes(h0, true), T::two_codes(h1, false), T::two_codes(h1, true)}, above[k], z);
         }
-        const bool real = row0 + (uint32_t)col < a.group;
-#pragma unroll
-        for (int x = 0; x < 2; x++)
-#pragma unroll
-            for (int i = 0; i < 4; i++) z[x][i] = largest_of_16(real ? (z[x][i] == z[x][i] ? z[x][i] : INFINITY) : -INFINITY);
-        // block 16 x + 4 g + i to its lane
-        const int from = (lane >> 2 & 3) * 16;
         float best = 0.0f;
 #pragma unroll
         for (int i = 0; i < 4; i++) {
-            const float v0 = __shfl(z[0][i], from), v1 = __shfl(z[1][i], from);
-            if ((lane & 3) == i) best = lane & 16 ? v1 : v0;
+            const float v = largest_of_16(z[i] == z[i] ? z[i] : INFINITY);
+            if ((col & 3) == i) best = v;
         }
         return best;
     }
@@ -144,29 +139,51 @@ __device__ __forceinline__ float counted(float best, float scale)
     return scale != 0.0f && fabsf(v) < INFINITY ? v + 0.0f : -INFINITY;
 }
 
-// A score in 64 bits, as an unsigned number in their order: a wavefront's work.
+// A score in 64 bits, as an unsigned number in their order: a wavefront's work, 16 lanes a query row.
 template <typename T> __device__ __forceinline__ uint64_t exact_order(const SelectArgs &a, const Request &q, uint32_t token, uint32_t head, uint32_t block)
 {
     const uint32_t lane = threadIdx.x & 63u;
     const int entry = entry_of(a.c, q.row, block);
     if (entry < 0) return order_of((double)-INFINITY);
     const uint8_t *const at = a.bounds + (int64_t)entry * a.bounds_block_stride + (int64_t)head * a.bounds_head_stride;
+    const double scale = *scale_at(a.c, 0, entry, head);
     double best = -INFINITY;
     bool bad = false;
-    for (uint32_t r = 0; r < a.group; r++) {
+    for (uint32_t r0 = 0; r0 < a.group; r0 += 4u) {
+        const uint32_t r = min(r0 + (lane >> 4), a.group - 1u);
         const uint16_t *const src = static_cast<const uint16_t *>(a.q.data) + (int64_t)token * a.q.row_stride + (int64_t)(head * a.group + r) * a.q.head_stride;
         double sum = 0.0;
-        for (uint32_t d = lane; d < a.c.dim; d += 64u) {
-            const double v = T::number(src[d]);
-            const double least = v * __builtin_amdgcn_cvt_f32_fp8((int)at[d], 0), most = v * __builtin_amdgcn_cvt_f32_fp8((int)at[a.c.dim + d], 0);
-            sum += least != least || most != most ? NAN : fmax(least, most);
-        }
+        for (uint32_t d = 8u * (lane & 15u); d < a.c.dim; d += 128u) {
+            const u32x4 v = *reinterpret_cast<const u32x4 *>(src + d);
+            const u32x2 l = *reinterpret_cast<const u32x2 *>(at + d), h = *reinterpret_cast<const u32x2 *>(at + a.c.dim + d);
 #pragma unroll
-        for (int m = 32; m; m >>= 1) sum += __shfl_xor(sum, m);
+            for (int i = 0; i < 8; i++) {
+                const double x = T::number((uint16_t)(v[i / 2] >> 16 * (i % 2)));
+                const f32x2 l2 = i & 2 ? __builtin_amdgcn_cvt_pk_f32_fp8((int)l[i / 4], true) : __builtin_amdgcn_cvt_pk_f32_fp8((int)l[i / 4], false);
+                const f32x2 h2 = i & 2 ? __builtin_amdgcn_cvt_pk_f32_fp8((int)h[i / 4], true) : __builtin_amdgcn_cvt_pk_f32_fp8((int)h[i / 4], false);
+                const double least = x * (double)l2[i & 1], most = x * (double)h2[i & 1];
+                sum += least != least || most != most ? NAN : fmax(least, most);
+            }
+        }
+        auto turned = [](double v, auto n) {
+            const uint64_t w = __builtin_bit_cast(uint64_t, v);
+            const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)w, 0x120 + decltype(n)::value, 0xF, 0xF, false);
+            const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(w >> 32), 0x120 + decltype(n)::value, 0xF, 0xF, false);
+            return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+        };
+        sum += turned(sum, Int<8>{});
+        sum += turned(sum, Int<4>{});
+        sum += turned(sum, Int<2>{});
+        sum += turned(sum, Int<1>{});
         bad |= sum != sum;
         best = sum > best ? sum : best;
     }
-    return order_of(bad ? (double)-INFINITY : best * (double)*scale_at(a.c, 0, entry, head));
+#pragma unroll
+    for (int m = 16; m < 64; m <<= 1) {
+        const double other = __shfl_xor(best, m);
+        best = other > best ? other : best;
+    }
+    return order_of(__ballot(bad) ? (double)-INFINITY : best * scale);
 }
 
 // ---------------------------------------------------------------- which blocks
@@ -236,35 +253,29 @@ __device__ __forceinline__ void find_rank(PickShared &s, uint32_t count, uint32_
     }
 }
 
-// Numbers lo + i of those i < count that are more than, or among the first `rank` that are equal, in order.
+// Numbers lo + i of those i < count that are more (which(i) > 0), or among the first `rank` that are equal (0), in order.  A thread has
+// neighbours, so that one look over all threads' counts is enough.
 template <uint32_t N, typename Which> __device__ __forceinline__ void write_in_order(PickShared &s, uint32_t count, uint32_t lo, uint32_t rank, const Which &which, int32_t *to)
 {
-    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6;
-    uint32_t taken = 0, equal = 0;
-    for (uint32_t base = 0; base < count; base += N) {
-        const uint32_t i = base + tid;
-        const int w = i < count ? which(i) : -1;        // 1: more, 0: equal
-        const uint64_t more = __ballot(w > 0), same = __ballot(w == 0);
-        __syncthreads();
-        if (!lane) {
-            s.wave_n[wave][0] = (uint32_t)__popcll(more);
-            s.wave_n[wave][1] = (uint32_t)__popcll(same);
-        }
-        __syncthreads();
-        uint32_t m = 0, e = 0, all_m = 0, all_e = 0;
+    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6, each = (count + N - 1u) / N;
+    const uint32_t from = min(tid * each, count), end = min(from + each, count);
+    uint32_t more = 0, same = 0;
+    for (uint32_t i = from; i < end; i++) {
+        const int w = which(i);
+        more += w > 0, same += w == 0;
+    }
+    uint32_t m = (uint32_t)lanes_scan((int)more), e = (uint32_t)lanes_scan((int)same);
+    __syncthreads();
+    if (lane == 63u) s.wave_n[wave][0] = m, s.wave_n[wave][1] = e;
+    __syncthreads();
+    m -= more, e -= same;
 #pragma unroll
-        for (uint32_t v = 0; v < N / 64u; v++) {
-            if (v < wave) m += s.wave_n[v][0], e += s.wave_n[v][1];
-            all_m += s.wave_n[v][0];
-            all_e += s.wave_n[v][1];
-        }
-        const uint64_t below = (1ull << lane) - 1ull;
-        m += (uint32_t)__popcll(more & below);
-        e += (uint32_t)__popcll(same & below);
-        const uint32_t at = taken + m + min(equal + e, rank) - min(equal, rank);
-        if (w > 0 || (w == 0 && equal + e < rank)) to[at] = (int32_t)(lo + i);
-        taken += all_m + min(equal + all_e, rank) - min(equal, rank);
-        equal += all_e;
+    for (uint32_t v = 0; v < N / 64u; v++)
+        if (v < wave) m += s.wave_n[v][0], e += s.wave_n[v][1];
+    for (uint32_t i = from; i < end; i++) {
+        const int w = which(i);
+        if (w > 0 || (w == 0 && e < rank)) to[m + min(e, rank)] = (int32_t)(lo + i);
+        m += w > 0, e += w == 0;
     }
 }
 
@@ -278,12 +289,21 @@ template <typename T, int DP> __global__ __launch_bounds__(kScoreThreads) __attr
     const uint32_t block0 = x.lo + kBlocksAtOnce * chunk + 32u * (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (q.fresh <= 0 || block0 >= x.hi) return;
     Scorer<T, DP> scorer(a, q, token, head);
-    float scale = 0.0f, s = -INFINITY;
+    const int own = block0 + (lane & 31u) < x.hi ? entry_of(a.c, q.row, block0 + (lane & 31u)) : -1;
+    typename Scorer<T, DP>::Tile tile[2];
+#pragma unroll
+    for (uint32_t y = 0; y < 2u; y++) tile[y] = scorer.fetch([&](uint32_t i) { return __shfl(own, (int)(16u * y + i)); });
+    float s[2] = {-INFINITY, -INFINITY};
     for (uint32_t row0 = 0; row0 < a.group; row0 += 16u) {
         scorer.rows(row0);
-        s = fmaxf(s, scorer.of(row0, block0, x.hi, scale));
+#pragma unroll
+        for (int y = 0; y < 2; y++) s[y] = fmaxf(s[y], scorer.of(tile[y]));
     }
-    if (lane < 32u && block0 + lane < x.hi) a.scores[(int64_t)item * a.stride + block0 + lane] = f32x2{counted(s, scale), scorer.off * scale};
+#pragma unroll
+    for (uint32_t y = 0; y < 2u; y++) {
+        const uint32_t block = block0 + 16u * y + 4u * (uint32_t)scorer.g + (uint32_t)scorer.col;
+        if (scorer.col < 4 && block < x.hi) a.scores[(int64_t)item * a.stride + block] = f32x2{counted(s[y], tile[y].scale), scorer.off * tile[y].scale};
+    }
 }
 
 // N threads per new token and head.  Scores in fp32 (made here, FUSED; else score_kernel has left them in memory), of which LDS holds as many
@@ -296,7 +316,18 @@ __global__ __launch_bounds__(N) __attribute__((amdgpu_waves_per_eu(DP <= 128 ? 4
     __shared__ PickShared s;
     extern __shared__ float own[];              // scores
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = (uint32_t)__builtin_amdgcn_readfirstlane(tid >> 6);
-    const uint32_t item = blockIdx.x, token = item / a.c.heads, head = item - token * a.c.heads;
+    // Workgroups go to the eight XCDs in turn: with FUSED the heads of a token follow each other on one of them, whose scales of a block
+    // lie in one line.
+    uint32_t token, head;
+    if constexpr (FUSED) {
+        const uint32_t nth = blockIdx.x >> 3;
+        token = nth / a.c.heads, head = nth - token * a.c.heads;
+        token = 8u * token + (blockIdx.x & 7u);
+        if (token >= a.b.total_new) return;
+    } else {
+        token = blockIdx.x / a.c.heads, head = blockIdx.x - token * a.c.heads;
+    }
+    const uint32_t item = token * a.c.heads + head;
     const Request q = token_of(a.b, a.c, (int)token);
     if (q.fresh <= 0) return;                   // no request's
     const Choice x = choice_of(a, q);
@@ -318,24 +349,48 @@ __global__ __launch_bounds__(N) __attribute__((amdgpu_waves_per_eu(DP <= 128 ? 4
     auto look = [&](float v) { most = fmaxf(most, v), least = fminf(least, v == -INFINITY ? INFINITY : v); };
     if constexpr (FUSED) {
         Scorer<T, DP> scorer(a, q, token, head);
+        // where all blocks lie first, in the scores' places
+        for (uint32_t i = tid; i < count; i += N) own[i] = __int_as_float(entry_of(a.c, q.row, x.lo + i));
         for (uint32_t row0 = 0; row0 < a.group; row0 += 16u) {
             scorer.rows(row0);
-            for (uint32_t base = 32u * wave; base < count; base += N / 2u) {
-                float scale, v = scorer.of(row0, x.lo + base, x.hi, scale);
-                off = fmaxf(off, scorer.off * scale);   // (no number where there is no block and no bound: left out)
-                if (lane < 32u && base + lane < count) {
-                    if (row0) v = fmaxf(v, own[base + lane]);
-                    if (row0 + 16u >= a.group) v = counted(v, scale), look(v);
-                    own[base + lane] = v;
+            if (!row0) __syncthreads();
+            uint32_t base = 16u * wave;
+            if (base >= count) break;
+            auto entries = [&](uint32_t from) {
+                return [&, from](uint32_t i) {
+                    i += from;
+                    return i >= count ? -1 : row0 ? entry_of(a.c, q.row, x.lo + i) : __float_as_int(own[i]);
+                };
+            };
+            auto tile = scorer.fetch(entries(base));
+            for (;;) {
+                const auto here = tile;
+                const uint32_t next = base + N / 4u;
+                if (next < count) tile = scorer.fetch(entries(next));
+                float v = scorer.of(here);
+                off = fmaxf(off, scorer.off * here.scale);      // (no number where there is no block and no bound: left out)
+                const uint32_t i = base + 4u * (uint32_t)scorer.g + (uint32_t)scorer.col;
+                if (scorer.col < 4 && i < count) {
+                    if (row0) v = fmaxf(v, own[i]);
+                    if (row0 + 16u >= a.group) v = counted(v, here.scale), look(v);
+                    own[i] = v;
                 }
+                if (next >= count) break;
+                base = next;
             }
         }
     } else {
-        for (uint32_t i = tid; i < count; i += N) {
-            const f32x2 v = left[i];
-            off = fmaxf(off, v[1]);
-            look(v[0]);
-            if (in_lds) own[i] = v[0];
+        constexpr uint32_t kAhead = 8;
+        for (uint32_t i0 = tid; i0 < count; i0 += kAhead * N) {
+            f32x2 v[kAhead];
+#pragma unroll
+            for (uint32_t k = 0; k < kAhead; k++) v[k] = left[min(i0 + k * N, count - 1u)];
+#pragma unroll
+            for (uint32_t k = 0; k < kAhead; k++) {
+                off = fmaxf(off, v[k][1]);
+                look(v[k][0]);
+                if (in_lds && i0 + k * N < count) own[i0 + k * N] = v[k][0];
+            }
         }
     }
 #pragma unroll
@@ -377,18 +432,18 @@ __global__ __launch_bounds__(N) __attribute__((amdgpu_waves_per_eu(DP <= 128 ? 4
     // what is nearer to the want-th than both may be off together (and numbers so small that fp32 runs out below them are all near)
     const float off2 = off > 0.0f && off < 0x1p-80f ? INFINITY : 2.001f * off;
     auto side = [&](float v) { return v == t ? 0 : v > t ? (v - t > off2 ? 1 : 0) : (t - v > off2 ? -1 : 0); };      // 0: near
-    for (uint32_t i0 = 0; i0 < count; i0 += N) {
-        const uint32_t i = i0 + tid;
-        const int w = i < count ? side(score(i)) : -1;
-        const uint64_t more = __ballot(w > 0), near = __ballot(w == 0);
-        uint32_t at = 0;
-        if (!lane) {
-            if (more) atomicAdd(&s.count[0], (uint32_t)__popcll(more));
-            if (near) at = atomicAdd(&s.count[1], (uint32_t)__popcll(near));
+    uint32_t surely = 0;
+    for (uint32_t i = tid; i < count; i += N) {
+        const int w = side(score(i));
+        surely += w > 0;
+        if (w == 0) {
+            const uint32_t at = atomicAdd(&s.count[1], 1u);
+            if (at < kClose) s.close[at] = i;
         }
-        at = (uint32_t)__builtin_amdgcn_readfirstlane((int)at) + (uint32_t)__popcll(near & ((1ull << lane) - 1ull));
-        if (w == 0 && at < kClose) s.close[at] = i;
     }
+#pragma unroll
+    for (int m = 32; m; m >>= 1) surely += (uint32_t)__shfl_xor((int)surely, m);
+    if (!lane) atomicAdd(&s.count[0], surely);
     __syncthreads();
     const uint32_t close = s.count[1], need = want - s.count[0];
     if (close == need || (t == -INFINITY && off2 < INFINITY)) {
@@ -438,10 +493,10 @@ template <typename T, int DP> static hipError_t select(const SelectArgs &a, hipS
     const uint64_t items = (uint64_t)a.b.total_new * a.c.heads, per = (a.stride + kBlocksAtOnce - 1u) / kBlocksAtOnce;
     // One launch where tokens and heads give every compute unit a workgroup, or there are few blocks; scores over more workgroups otherwise.
     const bool fused = a.stride <= kMostInLds && (items >= 256u || a.stride <= 4u * kBlocksAtOnce);
-    if (!launchable(items, kMany) || !launchable(items * per, kScoreThreads)) return hipErrorInvalidConfiguration;
+    if (!launchable(items + 8u * a.c.heads, kMany) || !launchable(items * per, kScoreThreads)) return hipErrorInvalidConfiguration;
     const uint32_t lds = a.stride > a.n_select && a.stride <= kMostInLds ? a.stride * 4u : 0u;
     if (fused) {
-        pick_kernel<T, DP, true, kFew><<<(uint32_t)items, kFew, lds, s>>>(a);
+        pick_kernel<T, DP, true, kFew><<<(a.b.total_new + 7u) / 8u * 8u * a.c.heads, kFew, lds, s>>>(a);
         return hipGetLastError();
     }
     if (a.stride > a.n_select) {
