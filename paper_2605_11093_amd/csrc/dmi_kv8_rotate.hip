@@ -76,25 +76,18 @@ __device__ __forceinline__ Place place_of(uint32_t sixteen, uint32_t rotary, boo
 }
 
 // Eight pairs turned, in F: fp64 for K, whose scale and codes then hang on no order of operations, and fp32 for queries of 16 bits.
-template <typename F> __device__ __forceinline__ void turn(float (&x)[16], const float *cos, const float *sin, bool neighbours)
+template <typename F, bool NEIGHBOURS> __device__ __forceinline__ void turn(float (&x)[16], const float *cos, const float *sin)
 {
-    float c[8], s[8];
 #pragma unroll
     for (int i = 0; i < 8; i += 4) {
-        *reinterpret_cast<f32x4 *>(c + i) = *reinterpret_cast<const f32x4 *>(cos + i);
-        *reinterpret_cast<f32x4 *>(s + i) = *reinterpret_cast<const f32x4 *>(sin + i);
-    }
-    float y[16];
+        const f32x4 c = *reinterpret_cast<const f32x4 *>(cos + i), s = *reinterpret_cast<const f32x4 *>(sin + i);
 #pragma unroll
-    for (int i = 0; i < 8; i++) {
-        const F u = neighbours ? x[2 * i] : x[i], v = neighbours ? x[2 * i + 1] : x[8 + i];
-        const float a = (float)(u * (F)c[i] - v * (F)s[i]), b = (float)(u * (F)s[i] + v * (F)c[i]);
-        y[i] = a, y[8 + i] = b;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; i++) {
-        x[neighbours ? 2 * i : i] = y[i];
-        x[neighbours ? 2 * i + 1 : 8 + i] = y[8 + i];
+        for (int k = 0; k < 4; k++) {
+            float &p = NEIGHBOURS ? x[2 * (i + k)] : x[i + k], &r = NEIGHBOURS ? x[2 * (i + k) + 1] : x[8 + i + k];
+            const F u = p, v = r;
+            p = (float)(u * (F)c[k] - v * (F)s[k]), r = (float)(u * (F)s[k] + v * (F)c[k]);
+            if constexpr (sizeof(F) == 8) __builtin_amdgcn_sched_barrier(0);       // (all pairs at once would take all registers)
+        }
     }
 }
 
@@ -121,34 +114,47 @@ template <> __device__ __forceinline__ void store8<float>(float *p, const float 
     *reinterpret_cast<f32x4 *>(p + 4) = f32x4{x[4], x[5], x[6], x[7]};
 }
 
-constexpr uint32_t kQueryHeads = 4;             // query heads that a wavefront takes at a time
+constexpr uint32_t kMostHeads = 8;              // query heads that a wavefront takes at a time
+template <typename T> constexpr uint32_t kAheadOf = sizeof(T) == 4 ? 2 : 4;     // sixteens of queries that are asked for before the first is used
 constexpr uint32_t kTableBytes = 32768;         // cosines and sines in LDS: as many tokens as they are room for
 
-// A workgroup per block that new tokens reach and a.each of its items: K of a head, V of a head, four heads of queries.  Cosines and sines
+// A workgroup per block that new tokens reach and a.each of its items: K of a head, V of a head, queries of a.q_each heads.  Cosines and sines
 // of the block's tokens are computed once into LDS, in 64 bits (angles of far positions have no others), and every item takes them from
-// there; a wavefront has an item at a time.  As in append_kernel the scale of K and V wants the largest of all the block's new elements
-// first; what a lane can hold of them it does.
-template <typename T>
-__global__ __launch_bounds__(256) void rotate_kernel(RotateArgs a)
+// there; a wavefront has an item at a time, a lane the same sixteen of every few rows.  As in append_kernel the scale of K and V wants the
+// largest of all the block's new elements first; what a lane can hold of them it does.
+template <typename T, bool NEIGHBOURS>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void rotate_kernel(RotateArgs a)
 {
     extern __shared__ __align__(16) float table[];
-    constexpr int kHeld = 2;                    // sixteens a lane keeps
+    constexpr int kHeld = 2;                    // sixteens of K or V a lane keeps
+    constexpr uint32_t kAhead = kAheadOf<T>;
     const uint32_t lane = threadIdx.x & 63u, wave = (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Reached x = reached_by(a.b, a.c, a.counted ? -1 : (int)blockIdx.y, blockIdx.x / a.groups);
     if (x.lo >= x.hi) return;
     const uint32_t half = a.rotary / 2u, per_row = a.c.dim / 16u, stored = 2u * a.c.heads;
-    const uint32_t items = stored + (a.q_heads + kQueryHeads - 1u) / kQueryHeads;
+    const uint32_t items = stored + (a.q_heads + a.q_each - 1u) / a.q_each;
     const uint32_t first_item = blockIdx.x % a.groups * a.each, last_item = min(first_item + a.each, items);
     const int first = x.q.len - x.q.fresh;      // the first new token's place
     const int entry = entry_of(a.c, x.q.row, (uint32_t)x.block);
     const uint32_t slot0 = (uint32_t)x.lo - (uint32_t)x.block * a.c.bs;
     float *const cosines = table, *const sines = table + a.tokens * half;
-    const bool neighbours = a.neighbours;
+    // this lane's row among those of a step, its sixteen of it
+    const uint32_t of_step = 64u / per_row, row = lane / per_row, sixteen = lane - row * per_row;
+    const Place rotated = place_of(sixteen, a.rotary, NEIGHBOURS), as_is = place_of(sixteen, 0u, NEIGHBOURS);
 
+    struct Raw {
+        Eight<T> a, b;
+        __device__ __forceinline__ void load(const T *row, const Place &p) { a.load(row + p.a), b.load(row + p.b); }
+        __device__ __forceinline__ void numbers(float (&v)[16]) const
+        {
+            a.numbers(*reinterpret_cast<float(*)[8]>(&v[0]));
+            b.numbers(*reinterpret_cast<float(*)[8]>(&v[8]));
+        }
+    };
     auto fill = [&](int lo, int tokens) {
         for (uint32_t u = threadIdx.x; u < (uint32_t)tokens * half; u += 256u) {
             const uint32_t t = u / half, i = u - t * half;
-            const int row = x.q.start + lo - first + (int)t, at = a.positions ? a.positions[row] : lo + (int)t;
+            const int nth = x.q.start + lo - first + (int)t, at = a.positions ? a.positions[nth] : lo + (int)t;
             const double angle = (double)at * (double)a.freq[i];
             // less whole turns, whose length in two parts
             const double turns = __builtin_rint(angle * 0.15915494309189533577);
@@ -158,14 +164,6 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs a)
             cosines[t * half + i] = (float)c;
             sines[t * half + i] = (float)s;
         }
-    };
-    // a lane's sixteen of a row as numbers, rotated where it is
-    auto numbers = [&](const T *row, const Place &p, float (&v)[16]) {
-        Eight<T> e, f;
-        e.load(row + p.a);
-        f.load(row + p.b);
-        e.numbers(*reinterpret_cast<float(*)[8]>(&v[0]));
-        f.numbers(*reinterpret_cast<float(*)[8]>(&v[8]));
     };
 
     const int tokens = x.hi - x.lo, chunk = (int)a.tokens;
@@ -181,6 +179,7 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs a)
         const T *const src = static_cast<const T *>(a.x[kv].data) + (int64_t)(x.q.start + x.lo - first) * a.x[kv].row_stride + (int64_t)head * a.x[kv].head_stride;
         float *const scale_p = scale_at(a.c, (int)kv, max(entry, 0), head);
         const float had = store && slot0 ? *scale_p : 0.0f;
+        const Place p = kv ? as_is : rotated;
         float held[kHeld][16];
         uint32_t largest = 0;
         float s = 0.0f, inv = 0.0f;
@@ -188,22 +187,16 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs a)
         // twice over the tokens for K and V, the second time with their scale
         for (int pass = 0; pass < (one && !store ? 1 : 2); pass++) {
             for (int lo = 0; lo < tokens; lo += chunk) {
-                const int here = min(chunk, tokens - lo);
+                const uint32_t here = (uint32_t)min(chunk, tokens - lo);
                 if (!one) {
                     __syncthreads();            // (the cosines of the last chunk have been used)
-                    fill(x.lo + lo, here);
+                    fill(x.lo + lo, (int)here);
                     __syncthreads();
                 }
-                const uint32_t units = (uint32_t)here * per_row;
-                auto get = [&](uint32_t u, float (&v)[16]) {
-                    const uint32_t t = u / per_row;
-                    const Place p = place_of(u - t * per_row, kv ? 0u : a.rotary, neighbours);
-                    numbers(src + (int64_t)(lo + (int)t) * a.x[kv].row_stride, p, v);
-                    if (p.pair >= 0) {
-                        const uint32_t at = t * half + (uint32_t)p.pair;
-                        if (neighbours) turn<double>(v, cosines + at, sines + at, true);
-                        else turn<double>(v, cosines + at, sines + at, false);
-                    }
+                auto ask = [&](uint32_t t, Raw &r) { r.load(src + (int64_t)(lo + (int)t) * a.x[kv].row_stride, p); };
+                auto have = [&](uint32_t t, const Raw &r, float (&v)[16]) {
+                    r.numbers(v);
+                    if (!kv && p.pair >= 0) turn<double, NEIGHBOURS>(v, cosines + t * half + (uint32_t)p.pair, sines + t * half + (uint32_t)p.pair);
                 };
                 auto look = [&](const float (&v)[16]) {
 #pragma unroll
@@ -212,55 +205,73 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs a)
                         largest = max(largest, m < 0x7F800000u ? m : 0u);
                     }
                 };
-                auto put = [&](uint32_t u, const float (&v)[16]) {
-                    const uint32_t t = u / per_row;
-                    const Place p = place_of(u - t * per_row, kv ? 0u : a.rotary, neighbours);
+                auto put = [&](uint32_t t, const float (&v)[16]) {
                     float y[16];
 #pragma unroll
-                    for (int i = 0; i < 16; i++) y[i] = exact ? v[i] * inv : v[i] / s;
+                    for (int i = 0; i < 16; i++) y[i] = v[i] * inv;
+                    if (!exact) {
+#pragma unroll
+                            for (int i = 0; i < 16; i++) {
+                            y[i] = v[i] / s;
+                            __builtin_amdgcn_sched_barrier(0);
+                        }
+                    }
                     uint8_t *const to = code_at(a.c, (int)kv, entry, slot0 + (uint32_t)lo + t, head);
                     *reinterpret_cast<u32x2 *>(to + p.a) = u32x2{to_codes(y[0], y[1], y[2], y[3]), to_codes(y[4], y[5], y[6], y[7])};
                     *reinterpret_cast<u32x2 *>(to + p.b) = u32x2{to_codes(y[8], y[9], y[10], y[11]), to_codes(y[12], y[13], y[14], y[15])};
                 };
-                if (store && pass == 0) {
-                    if (one) {
+                if (store && row < of_step) {
+                    if (one && pass == 0) {
+                        Raw raw[kHeld];
 #pragma unroll
-                        for (int i = 0; i < kHeld; i++)
-                            if (lane + 64u * i < units) get(lane + 64u * i, held[i]), look(held[i]);
-                    }
-                    for (uint32_t u = lane + (one ? 64u * kHeld : 0u); u < units; u += 64u) {
-                        float v[16];
-                        get(u, v);
-                        look(v);
-                    }
-                } else if (store) {
-                    if (one) {
+                        for (uint32_t i = 0; i < kHeld; i++) ask(min(row + i * of_step, here - 1u), raw[i]);
 #pragma unroll
-                        for (int i = 0; i < kHeld; i++)
-                            if (lane + 64u * i < units) put(lane + 64u * i, held[i]);
-                    }
-                    for (uint32_t u = lane + (one ? 64u * kHeld : 0u); u < units; u += 64u) {
-                        float v[16];
-                        get(u, v);
-                        put(u, v);
-                    }
-                } else if (turns_q && pass == 0) {
-                    const uint32_t head0 = (item - stored) * kQueryHeads, heads = min(kQueryHeads, a.q_heads - head0);
-                    for (uint32_t u = lane; u < units * heads; u += 64u) {
-                        const uint32_t t = u / (per_row * heads), w = u - t * per_row * heads, h = w / per_row;
-                        const Place p = place_of(w - h * per_row, a.rotary, neighbours);
-                        const int64_t row = x.q.start + x.lo - first + lo + (int)t;
-                        float v[16];
-                        numbers(static_cast<const T *>(a.q.data) + row * a.q.row_stride + (int64_t)(head0 + h) * a.q.head_stride, p, v);
-                        if (p.pair >= 0) {
-                            typedef std::conditional_t<sizeof(T) == 4, double, float> F;
-                            const uint32_t at = t * half + (uint32_t)p.pair;
-                            if (neighbours) turn<F>(v, cosines + at, sines + at, true);
-                            else turn<F>(v, cosines + at, sines + at, false);
+                        for (uint32_t i = 0; i < kHeld; i++) {
+                            have(min(row + i * of_step, here - 1u), raw[i], held[i]);
+                            look(held[i]);      // (behind the last token that one again)
                         }
-                        T *const to = static_cast<T *>(a.q_out.data) + row * a.q_out.row_stride + (int64_t)(head0 + h) * a.q_out.head_stride;
-                        store8<T>(to + p.a, v);
-                        store8<T>(to + p.b, v + 8);
+                    } else if (one) {
+#pragma unroll
+                        for (uint32_t i = 0; i < kHeld; i++)
+                            if (row + i * of_step < here) put(row + i * of_step, held[i]);
+                    }
+                    for (uint32_t t = row + (one ? of_step * kHeld : 0u); t < here; t += of_step) {
+                        Raw r;
+                        float v[16];
+                        ask(t, r);
+                        have(t, r, v);
+                        if (pass == 0) look(v);
+                        else put(t, v);
+                    }
+                } else if (turns_q && pass == 0 && row < of_step) {
+                    const uint32_t head0 = (item - stored) * a.q_each, heads = min(a.q_each, a.q_heads - head0), rows = here * heads;
+                    const uint32_t share = (65536u + heads - 1u) / heads;       // (rows are few: a quotient by a product)
+                    const int64_t at0 = x.q.start + x.lo - first + lo;
+                    auto locate = [&](uint32_t r, uint32_t &t, uint32_t &h) {
+                        t = r * share >> 16;
+                        h = head0 + r - t * heads;
+                    };
+                    for (uint32_t r0 = row; r0 < rows; r0 += kAhead * of_step) {
+                        Raw raw[kAhead];
+#pragma unroll
+                        for (uint32_t i = 0; i < kAhead; i++) {
+                            uint32_t t, h;
+                            locate(min(r0 + i * of_step, rows - 1u), t, h);
+                            raw[i].load(static_cast<const T *>(a.q.data) + (at0 + t) * a.q.row_stride + (int64_t)h * a.q.head_stride, rotated);
+                        }
+#pragma unroll
+                        for (uint32_t i = 0; i < kAhead; i++) {
+                            if (r0 + i * of_step >= rows) break;
+                            uint32_t t, h;
+                            locate(r0 + i * of_step, t, h);
+                            float v[16];
+                            raw[i].numbers(v);
+                            typedef std::conditional_t<sizeof(T) == 4, double, float> F;
+                            if (rotated.pair >= 0) turn<F, NEIGHBOURS>(v, cosines + t * half + (uint32_t)rotated.pair, sines + t * half + (uint32_t)rotated.pair);
+                            T *const to = static_cast<T *>(a.q_out.data) + (at0 + t) * a.q_out.row_stride + (int64_t)h * a.q_out.head_stride;
+                            store8<T>(to + rotated.a, v);
+                            store8<T>(to + rotated.b, v + 8);
+                        }
                     }
                 }
             }
@@ -277,11 +288,11 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs a)
                     const float f = had / s;
                     const uint32_t eights = a.c.dim / 8u;
                     for (uint32_t u = lane; u < slot0 * eights; u += 64u) {
-                        u32x2 *p = reinterpret_cast<u32x2 *>(code_at(a.c, (int)kv, entry, u / eights, head) + (u % eights) * 8u);
-                        u32x2 w = *p;
+                        u32x2 *at = reinterpret_cast<u32x2 *>(code_at(a.c, (int)kv, entry, u / eights, head) + (u % eights) * 8u);
+                        u32x2 w = *at;
                         w[0] = scaled_codes(w[0], f);
                         w[1] = scaled_codes(w[1], f);
-                        *p = w;
+                        *at = w;
                     }
                 }
             }
@@ -297,7 +308,9 @@ hipError_t launch_rotate(RotateArgs a, uint32_t dtype, hipStream_t s)
     const uint32_t half = a.rotary / 2u;
     a.tokens = std::max(1u, std::min({a.c.bs, a.b.max_new, kTableBytes / (8u * half)}));
     // Few blocks: their items over more workgroups, each of which computes the block's cosines for itself.
-    const uint32_t items = 2u * a.c.heads + (a.q_heads + kQueryHeads - 1u) / kQueryHeads;
+    const uint32_t ahead = (dtype == DMI_DTYPE_FP32 ? kAheadOf<float> : kAheadOf<_Float16>) * (64u / (a.c.dim / 16u));
+    a.q_each = std::max(1u, std::min(kMostHeads, 2u * ahead / a.tokens));
+    const uint32_t items = 2u * a.c.heads + (a.q_heads + a.q_each - 1u) / a.q_each;
     const uint64_t blocks = reach.blocks * reach.reqs;
     a.each = (uint32_t)std::min<uint64_t>((items + 3u) & ~3u, std::max<uint64_t>(4u, (blocks * items / 2048u + 3u) & ~3ull));
     a.groups = (items + a.each - 1u) / a.each;
@@ -305,12 +318,13 @@ hipError_t launch_rotate(RotateArgs a, uint32_t dtype, hipStream_t s)
     if (!launchable(groups, 256)) return hipErrorInvalidConfiguration;
     const dim3 grid((uint32_t)groups, reach.reqs);
     const uint32_t lds = a.tokens * half * 8u;
-    switch (dtype) {
-    case DMI_DTYPE_BF16: rotate_kernel<Bf16Bits><<<grid, 256, lds, s>>>(a); break;
-    case DMI_DTYPE_FP16: rotate_kernel<_Float16><<<grid, 256, lds, s>>>(a); break;
-    default: rotate_kernel<float><<<grid, 256, lds, s>>>(a); break;
-    }
-    return hipGetLastError();
+    auto launch = [&](auto type) {
+        typedef decltype(type) T;
+        if (a.neighbours) rotate_kernel<T, true><<<grid, 256, lds, s>>>(a);
+        else rotate_kernel<T, false><<<grid, 256, lds, s>>>(a);
+        return hipGetLastError();
+    };
+    return dtype == DMI_DTYPE_BF16 ? launch(Bf16Bits{}) : dtype == DMI_DTYPE_FP16 ? launch((_Float16)0) : launch(0.0f);
 }
 
 // ---------------------------------------------------------------- bounds
