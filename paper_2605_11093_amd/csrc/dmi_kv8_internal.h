@@ -105,8 +105,9 @@ struct AttendArgs {
 };
 
 // What the attention kernels do: a whole context; the rest of one behind a shared prefix, whose sums are left as parts whatever their
-// number; such a prefix, for all rows of a group of requests; listed blocks, for each new token by itself.
-enum Kind { kWhole, kRest, kPrefix, kListed };
+// number; such a prefix, for all rows of a group of requests, whose sums are left as parts, or which goes on from the rests' sums to outputs;
+// listed blocks, for each new token by itself.
+enum Kind { kWhole, kRest, kPrefix, kLast, kListed };
 
 constexpr uint32_t kFewRows = 32;               // query rows that share a head: up to here by tokens_kernel
 
@@ -115,6 +116,8 @@ struct TokensPlan {
     bool whole;                                 // a workgroup takes a request and head, or one of its equal splits: no ranges
     uint32_t splits;
     uint32_t ranges;                            // equal parts of all contexts
+    uint32_t waves;                             // of a workgroup, not kWhole: 4 or 8
+    bool by_xcd;                                // the heads of a request on one XCD, not kWhole
     uint32_t tile_rows, row_tiles;              // query rows of a wavefront; wavefronts for the rows that share a head
     uint32_t join_blocks;                       // workgroups of the second launch that join parts, 0 if there can be none
     uint32_t score_stride;
@@ -137,6 +140,7 @@ struct PartsPlan {
 // How contexts behind shared prefixes are attended to: see dmi_kv8_parts.hip.
 struct SharedPlan {
     PartsPlan prefix;                           // splits 0: there is none
+    bool last;                                  // the prefix goes on from the rests' sums: nothing is split
     bool tokens;                                // few rows a head behind it: by tokens_kernel
     TokensPlan few;
     PartsPlan many;

@@ -54,6 +54,14 @@ uint32_t splits_of(uint64_t units, uint64_t tokens, uint32_t rows)
     return (uint32_t)std::min<uint64_t>(s, 64u);
 }
 
+// How workgroups of `units` requests (or tokens) are made: of four wavefronts where there is one for every compute unit with them, of eight
+// where not; a request's heads on one XCD where that leaves none of them idle.
+void workgroups_of(TokensPlan &t, uint64_t units, uint32_t heads)
+{
+    t.waves = units * heads * t.splits > 256u ? 4u : 8u;
+    t.by_xcd = units >= 64u;
+}
+
 }  // namespace
 
 extern "C" dmi_status_t dmi_kv8_append_rotated(const dmi_kv8_t *cache, const dmi_kv8_batch_t *batch, const dmi_kv8_heads_t *key,
@@ -184,6 +192,7 @@ BlocksPlan plan_blocks(uint32_t heads, uint32_t dim, uint32_t block_size, const 
     t.row_tiles = 1u;
     // (the launch that joins parts has a token in each of its rows)
     t.splits = b.total_new > 65535u ? 1u : splits_of((uint64_t)b.total_new * heads, blocks * block_size, group);
+    workgroups_of(t, b.total_new, heads);
     t.join_blocks = t.splits > 1u ? (q_heads + 3u) / 4u : 0u;
     const uint64_t parts = t.splits > 1u ? (uint64_t)b.total_new * q_heads * t.splits : 0u;
     p.parts = pad64(parts * 8u);
@@ -250,7 +259,7 @@ SharedSizes plan_shared(uint32_t heads, uint32_t dim, uint32_t block_size, const
         m.row_tiles = (uint32_t)((all + rows_each - 1u) / rows_each);
         // As many splits as make the sum of two least: rounds of 256 workgroups, with three tiles of 64 tokens for each one's start and
         // end, 2.5 us a tile; and a part of every row written and read again, at 4 TB/s.
-        const uint64_t groups = (all / rows_each + x.n_groups / 2u + 1u) * heads, tiles = (prefix + 63u) / 64u;
+        const uint64_t groups = std::max<uint64_t>(x.n_groups, (all + (uint64_t)x.n_groups * rows_each / 2u) / rows_each) * heads, tiles = (prefix + 63u) / 64u;
         double best = INFINITY;
         for (uint32_t s = 1; s <= 64u && (s == 1u || s * 128u <= prefix); s++) {
             const double cost = (double)((groups * s + 255u) / 256u) * (double)((tiles + s - 1u) / s + 3u) * 2.5 + (double)rows * s * dim * 8.0 / 4e6;
@@ -268,15 +277,20 @@ SharedSizes plan_shared(uint32_t heads, uint32_t dim, uint32_t block_size, const
         t.tile_rows = shared <= 16u ? 16u : 32u;
         t.row_tiles = 1u;
         t.splits = p.splits = splits_of((uint64_t)b.n_reqs * heads, behind, (uint32_t)shared);
+        workgroups_of(t, b.n_reqs, heads);
     } else {
         PartsPlan &m = p.many;
         m.row_tiles = (uint32_t)((shared + rows_each - 1u) / rows_each);
         m.splits = 1u;
         m.chunk = std::max(64u, (b.max_len + 63u) & ~63u);
     }
+    // Nothing split: the sums of what is behind the prefix are where the prefix begins, and its end writes outputs (32 prompts behind 4000
+    // tokens: a part of every row less to write, two less to read).
+    p.last = p.prefix.splits == 1u && p.splits == 1u;
     z.prefix_sums = 3u * (pad64(b.n_reqs * 4ull) + pad64((x.n_groups + 1u) * 4ull));
-    z.prefix_parts = z.prefix_sums + pad64(rows * p.prefix.splits * 8u);
-    z.sums = z.prefix_parts + pad64(rows * p.prefix.splits * dim * 4u);
+    const uint64_t parts = p.last ? 0u : rows * p.prefix.splits;
+    z.prefix_parts = z.prefix_sums + pad64(parts * 8u);
+    z.sums = z.prefix_parts + pad64(parts * dim * 4u);
     z.parts = z.sums + pad64(rows * p.splits * 8u);
     z.bytes = rows && b.n_reqs ? z.parts + pad64(rows * p.splits * dim * 4u) : 0u;
     return z;

@@ -45,6 +45,7 @@ template <typename T, int DP, int NW, Kind KIND = kWhole>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW / 4)))
 void parts_kernel(AttendArgs a, PartsPlan p)
 {
+    constexpr bool PREFIX = KIND == kPrefix || KIND == kLast;
     constexpr int KP = DP * 2 + 16, VP = kTile * 2;             // bytes of a row in LDS; K's are padded so that rows start on other banks
     constexpr int KK = DP / 16, ND = DP / 32;
     constexpr int A = DP <= 128 ? 8 : 3;                        // operands read ahead (four, with 256 elements: 433 us for 424)
@@ -103,9 +104,9 @@ void parts_kernel(AttendArgs a, PartsPlan p)
     }
     if (row0 < 0) return;
     const int rows = q.fresh * (int)a.group;
-    const int older = KIND == kPrefix ? q.len - 1 : q.len - q.fresh, last_row = min(row0 + 32 * NW, rows) - 1;
+    const int older = PREFIX ? q.len - 1 : q.len - q.fresh, last_row = min(row0 + 32 * NW, rows) - 1;
     // tokens that the workgroup's last row sees (of a prefix all rows see all)
-    const int seen = KIND == kPrefix ? q.len : older + last_row / (int)a.group + 1;
+    const int seen = PREFIX ? q.len : older + last_row / (int)a.group + 1;
     const int begin = (int)(split * p.chunk), end = min(seen, begin + (int)p.chunk), tiles = max(0, (end - begin + kTile - 1) / kTile);
     if (split && tiles == 0) return;                            // (what reads the parts counts the same way)
 
@@ -114,7 +115,7 @@ void parts_kernel(AttendArgs a, PartsPlan p)
     const float scale = fabsf(a.scale_log2);
     const int wave_row = row0 + wave * 32, row = wave_row + col;
     const QueryRow w = query_row(a, head, (uint32_t)row);
-    const int lim = row < rows ? older + (KIND == kPrefix ? 0 : w.token) : -1;      // the last position that the column's query sees
+    const int lim = row < rows ? older + (PREFIX ? 0 : w.token) : -1;      // the last position that the column's query sees
     // Read by whole rows, and given to the lanes that take them through LDS (rows of its own for each wavefront; outputs go the same way)
     constexpr int kRow = 2 * DP, kChunks = DP / 8, kRows = 64 / kChunks;       // bytes; 16s of them; rows of a load
     static_assert(NW * 32 * kRow <= 2 * (kTile * KP + DP * VP));
@@ -134,8 +135,8 @@ void parts_kernel(AttendArgs a, PartsPlan p)
         }
     }
     // what the first and the last of them see
-    const int least = wave_row + 32 <= rows ? older + (KIND == kPrefix ? 0 : wave_row / (int)a.group) : -1;
-    const int most = wave_row < rows ? older + (KIND == kPrefix ? 0 : min(wave_row + 31, rows - 1) / (int)a.group) : -1;
+    const int least = wave_row + 32 <= rows ? older + (PREFIX ? 0 : wave_row / (int)a.group) : -1;
+    const int most = wave_row < rows ? older + (PREFIX ? 0 : min(wave_row + 31, rows - 1) / (int)a.group) : -1;
 
     // ---- staging
     struct KCodes {
@@ -344,6 +345,23 @@ void parts_kernel(AttendArgs a, PartsPlan p)
         clean_v(vc, 0);
         place_v(vc, 0);
         place_k(kc, 0);
+        if constexpr (KIND == kLast) {              // goes on from the sums of what is behind the prefix
+            const int64_t part = (int64_t)(q.start + min(w.token, q.fresh - 1)) * a.q_heads + w.head;
+            const f32x2 x = p.sums[part];
+            const float *const from = p.parts + part * a.c.dim;
+            m = row < rows ? x[0] : -INFINITY;
+            base = m == -INFINITY ? 0.0f : m;
+            l = row < rows && !half ? x[1] : 0.0f;
+#pragma unroll
+            for (int d = 0; d < ND; d++)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) {
+                    const int e = 32 * d + 2 * i + 4 * half;
+                    const f32x4 y = *reinterpret_cast<const f32x4 *>(from + (e < (int)a.c.dim ? e : 0));
+#pragma unroll
+                    for (int k = 0; k < 4; k++) o[d][i + k] = row < rows ? y[k] : 0.0f;
+                }
+        }
 #pragma unroll 1
         for (int tile = 0; tile < tiles; tile++) {
             const int t0 = begin + kTile * tile;
@@ -445,10 +463,12 @@ void parts_kernel(AttendArgs a, PartsPlan p)
         }
     }
 
+    // (rows that share nothing are joined elsewhere.  No return for them: without a way around the loop the compiler runs out of registers)
+    const int written = KIND == kLast && !tiles ? 0 : rows;
     l += __shfl_xor(l, 32);
     const int64_t at = (int64_t)(q.start + w.token) * a.q_heads + w.head;
     const bool empty = m == -INFINITY && l == 0.0f;
-    if (KIND == kWhole && p.splits == 1) {
+    if (KIND == kLast || (KIND == kWhole && p.splits == 1)) {
         // Rows are put together in LDS, so that a store writes whole ones: as the lanes hold them it would write 16 bytes here and there.
         const float f = __builtin_ldexpf(empty ? 0.0f : 1.0f / l, ref);
         const int64_t dst = (int64_t)(q.start + w.token) * a.out.row_stride + (int64_t)w.head * a.out.head_stride;
@@ -465,10 +485,10 @@ void parts_kernel(AttendArgs a, PartsPlan p)
             const int r = j + lane / kChunks, chunk = lane % kChunks;
             const u32x4 x = *reinterpret_cast<const u32x4 *>(in_row(r, chunk));
             const int64_t to = (int64_t)(uint32_t)__shfl((int)(uint32_t)dst, r) | (int64_t)__shfl((int)(dst >> 32), r) << 32;
-            if (wave_row + r < rows && 8 * chunk < (int)a.c.dim)
+            if (wave_row + r < written && 8 * chunk < (int)a.c.dim)
                 *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(a.out.data) + to + 8 * chunk) = x;
         }
-        if (row < rows && half == 0) {
+        if (row < written && half == 0) {
             const float sum = empty ? -INFINITY : m + log2_of(l);
             if (a.lse) a.lse[at] = sum * kLn2;
             if (p.totals) p.totals[at] = sum;
@@ -783,23 +803,27 @@ hipError_t launch_parts(const AttendArgs &a, const PartsPlan &p, uint32_t dtype,
 
 hipError_t launch_parts_apart(const AttendArgs &a, const PartsPlan &p, Kind kind, uint32_t dtype, hipStream_t s)
 {
+    if (kind == kLast) return dtype == DMI_DTYPE_BF16 ? parts_of<Bf16, kLast>(a, p, s) : parts_of<Fp16, kLast>(a, p, s);
     if (kind == kPrefix) return dtype == DMI_DTYPE_BF16 ? parts_of<Bf16, kPrefix>(a, p, s) : parts_of<Fp16, kPrefix>(a, p, s);
     return dtype == DMI_DTYPE_BF16 ? parts_of<Bf16, kRest>(a, p, s) : parts_of<Fp16, kRest>(a, p, s);
 }
 
 // ---------------------------------------------------------------- contexts behind shared prefixes
-// Tokens of group g's prefix that are read for all: whole blocks, in front of all new tokens, of requests that have some.  All lanes of a
-// wavefront have to come here, and all get it.
+// Tokens of group g's prefix that are read for all: whole blocks, in front of all new tokens, of requests that have some; none where the
+// rows from its first request's to the next group's first are others than those requests' new tokens.  All lanes of a wavefront have to come
+// here, and all get it.
 __device__ __forceinline__ int prefix_of(const AttendArgs &a, const SharedPlan &p, int g)
 {
     const int n = (int)a.b.n_reqs, first = min(max(p.group_starts[g], 0), n), last = min(max(p.group_starts[g + 1], first), n);
-    int least = first < last ? min(max(p.prefix_tokens[g], 0), (int)p.max_prefix) : 0;
+    int least = first < last ? min(max(p.prefix_tokens[g], 0), (int)p.max_prefix) : 0, rows = 0;
     for (int r = first + (int)(threadIdx.x & 63u); r < last; r += 64) {
         const Request q = request_of(a.b, a.c, r);
         if (q.fresh > 0 || r == first) least = min(least, max(q.len - q.fresh, 0));
+        rows += q.fresh;
     }
 #pragma unroll
-    for (int m = 32; m; m >>= 1) least = min(least, __shfl_xor(least, m));
+    for (int m = 32; m; m >>= 1) least = min(least, __shfl_xor(least, m)), rows += __shfl_xor(rows, m);
+    if (a.b.starts && rows != a.b.starts[last] - a.b.starts[first]) least = 0;
     return (int)(block_of(a.c, (uint32_t)least >> 4) * a.c.bs);
 }
 
@@ -840,7 +864,8 @@ __global__ __launch_bounds__(256) void shared_kernel(AttendArgs a, SharedPlan p)
     p.seqs[r] = (int32_t)((int64_t)q.row * a.c.table_stride + (int64_t)block_of(a.c, (uint32_t)shared >> 4));
 }
 
-// Outputs out of the parts of prefixes and of what is behind them: see join_parts_kernel.
+// Outputs out of the parts of prefixes and of what is behind them (p.last: of requests that share nothing, the others' are written already):
+// see join_parts_kernel.
 template <typename T>
 __global__ __launch_bounds__(256) void join_shared_kernel(AttendArgs a, SharedPlan p)
 {
@@ -848,6 +873,7 @@ __global__ __launch_bounds__(256) void join_shared_kernel(AttendArgs a, SharedPl
     const uint32_t wide = a.c.dim / 4u, each = 256u / wide, rows = (uint32_t)q.fresh * a.group, lane = threadIdx.x % wide;
     if (threadIdx.x >= each * wide) return;
     const int shared = p.shared[blockIdx.y];
+    if (p.last && shared) return;
     const int before = p.prefix.chunk ? min((shared + (int)p.prefix.chunk - 1) / (int)p.prefix.chunk, (int)p.prefix.splits) : 0;
     for (uint32_t n = blockIdx.x * each + threadIdx.x / wide; n < rows * a.c.heads; n += gridDim.x * each) {
         const uint32_t head = n / rows, row = n - head * rows;
@@ -881,20 +907,23 @@ hipError_t launch_shared(const AttendArgs &a, const SharedPlan &p, uint32_t dtyp
 {
     shared_kernel<<<(a.b.n_reqs + p.n_groups + 4u) / 4u, 256, 0, s>>>(a, p);
     hipError_t e = hipGetLastError();
-    if (e == hipSuccess && p.prefix.splits) {
-        AttendArgs group = a;
-        group.b = Batch{p.group_lens, p.group_rows, p.group_seqs, p.n_groups, a.b.total_new, a.b.total_new, p.max_prefix};
-        e = launch_parts_apart(group, p.prefix, kPrefix, dtype, s);
-    }
     if (e != hipSuccess) return e;
+    AttendArgs group = a;
+    group.b = Batch{p.group_lens, p.group_rows, p.group_seqs, p.n_groups, a.b.total_new, a.b.total_new, p.max_prefix};
+    if (p.n_groups && !p.last && (e = launch_parts_apart(group, p.prefix, kPrefix, dtype, s)) != hipSuccess) return e;
     // a table of one column, of which each request has those from its place in the real one on
     AttendArgs rest = a;
     rest.c.n_seqs = 1u << 31, rest.c.table_stride = 1;
     rest.b.rows = p.seqs, rest.b.lens = p.lens;
     e = p.tokens ? launch_tokens_apart(rest, p.few, kRest, dtype, s) : launch_parts_apart(rest, p.many, kRest, dtype, s);
     if (e != hipSuccess) return e;
+    if (p.last) {
+        PartsPlan prefix = p.prefix;
+        prefix.sums = p.sums, prefix.parts = p.parts;
+        if ((e = launch_parts_apart(group, prefix, kLast, dtype, s)) != hipSuccess) return e;
+    }
     const uint32_t each = 256u / (a.c.dim / 4u);
-    const dim3 grid(std::min((a.b.max_new * a.q_heads + each - 1u) / each, 1u << 20), a.b.n_reqs);
+    const dim3 grid(std::min((a.b.max_new * a.q_heads + each - 1u) / each, p.last ? 64u : 1u << 20), a.b.n_reqs);
     if (dtype == DMI_DTYPE_BF16) join_shared_kernel<Bf16><<<grid, 256, 0, s>>>(a, p);
     else join_shared_kernel<Fp16><<<grid, 256, 0, s>>>(a, p);
     return hipGetLastError();

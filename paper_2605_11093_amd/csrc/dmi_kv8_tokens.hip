@@ -68,15 +68,14 @@ template <bool WHOLE> __device__ __forceinline__ int64_t part_at(const AttendArg
 // instead of 238 at that time).
 constexpr int waves_of(int dp, int nt, bool whole) { return !whole || dp * nt > 128 ? 4 : 8; }
 
-template <typename T, int DP, int NT, bool WHOLE, Kind KIND = kWhole>
-__global__ __launch_bounds__(64 * waves_of(DP, NT, WHOLE)) __attribute__((amdgpu_waves_per_eu(DP * NT <= 128 ? 2 : 1)))
+template <typename T, int DP, int NT, bool WHOLE, Kind KIND = kWhole, int NW = waves_of(DP, NT, WHOLE)>
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DP * NT <= 128 ? 2 : 1)))
 void tokens_kernel(AttendArgs a, TokensPlan p)
 {
     constexpr int KL = DP / 64;                 // 16-byte loads of K a lane and sixteen
     constexpr int KK = DP / 32;                 // instructions for a sixteen's scores
     constexpr int VW = DP / 64;                 // words of V a lane and token
     constexpr int NJ = DP / 16;                 // instructions for 16 query rows' outputs
-    [[maybe_unused]] constexpr int NW = waves_of(DP, NT, WHOLE);
 
     const int lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -84,8 +83,16 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
     int r = 0, seg0 = 0, range = 0, first, last;        // seg0: the request's first tile; first, last: the range's tiles
     Request held{0, 0, 0, 0};                           // of this lane, where there are no more than lanes
     if constexpr (WHOLE) {
-        const uint32_t pair = blockIdx.x / p.splits;
+        uint32_t pair = blockIdx.x / p.splits;
         range = (int)(blockIdx.x - pair * p.splits);
+        if (KIND != kWhole && p.by_xcd) {
+            // workgroups go to the eight XCDs in turn: the heads of a request on one of them, whose scales of a block lie in one line
+            const uint32_t nth = blockIdx.x >> 3, each = a.c.heads * p.splits, eighth = nth / each;
+            pair = (nth - eighth * each) / p.splits;
+            range = (int)(nth - eighth * each - pair * p.splits);
+            pair += (8u * eighth + (blockIdx.x & 7u)) * a.c.heads;
+            if (pair >= (KIND == kListed ? a.b.total_new : a.b.n_reqs) * a.c.heads) return;
+        }
         r = (int)(pair / a.c.heads);
         head = pair % a.c.heads;
         const Request q = KIND == kListed ? token_of(a.b, a.c, r) : request_of(a.b, a.c, r);
@@ -760,11 +767,12 @@ template <typename T> static hipError_t tokens(const AttendArgs &a, const Tokens
 template <typename T, Kind KIND> static hipError_t tokens_apart(const AttendArgs &a, const TokensPlan &p, hipStream_t s)
 {
     const uint32_t units = KIND == kListed ? a.b.total_new : a.b.n_reqs;
+    const uint64_t groups = (uint64_t)(p.by_xcd ? (units + 7u) / 8u * 8u : units) * a.c.heads * p.splits;
+    if (!launchable(groups, 512) || (uint64_t)units * a.c.heads > UINT32_MAX) return hipErrorInvalidConfiguration;
     auto launch = [&](auto dp_, auto nt_) {
-        constexpr int DP = decltype(dp_)::value, NT = decltype(nt_)::value, threads = 64 * waves_of(DP, NT, true);
-        const uint64_t groups = (uint64_t)units * a.c.heads * p.splits;
-        if (!launchable(groups, threads)) return hipErrorInvalidConfiguration;
-        tokens_kernel<T, DP, NT, true, KIND><<<(uint32_t)groups, threads, 0, s>>>(a, p);
+        constexpr int DP = decltype(dp_)::value, NT = decltype(nt_)::value, many = waves_of(DP, NT, true);
+        if (p.waves == 4u || many == 4) tokens_kernel<T, DP, NT, true, KIND, 4><<<(uint32_t)groups, 256, 0, s>>>(a, p);
+        else tokens_kernel<T, DP, NT, true, KIND, many><<<(uint32_t)groups, 64 * many, 0, s>>>(a, p);
         return hipGetLastError();
     };
     const int dp = a.c.dim <= 64 ? 64 : a.c.dim <= 128 ? 128 : 256;
