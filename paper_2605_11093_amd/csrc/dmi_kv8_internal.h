@@ -140,6 +140,8 @@ struct PartsPlan {
 // How contexts behind shared prefixes are attended to: see dmi_kv8_parts.hip.
 struct SharedPlan {
     PartsPlan prefix;                           // splits 0: there is none
+    bool few_rows;                              // few rows for it: by tokens_kernel, whose splits are all there
+    TokensPlan prefix_few;
     bool last;                                  // the prefix goes on from the rests' sums: nothing is split
     bool tokens;                                // few rows a head behind it: by tokens_kernel
     TokensPlan few;

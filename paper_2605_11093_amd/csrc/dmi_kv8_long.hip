@@ -254,19 +254,38 @@ SharedSizes plan_shared(uint32_t heads, uint32_t dim, uint32_t block_size, const
     const uint64_t rows = (uint64_t)b.total_new * q_heads, shared = (uint64_t)max_new * group;
     const uint32_t prefix = std::min(x.max_prefix, b.max_len) / block_size * block_size;
     if (x.n_groups && prefix) {
-        PartsPlan &m = p.prefix;
         const uint64_t all = (uint64_t)b.total_new * group;
-        m.row_tiles = (uint32_t)((all + rows_each - 1u) / rows_each);
-        // As many splits as make the sum of two least: rounds of 256 workgroups, with three tiles of 64 tokens for each one's start and
-        // end, 2.5 us a tile; and a part of every row written and read again, at 4 TB/s.
-        const uint64_t groups = std::max<uint64_t>(x.n_groups, (all + (uint64_t)x.n_groups * rows_each / 2u) / rows_each) * heads, tiles = (prefix + 63u) / 64u;
-        double best = INFINITY;
-        for (uint32_t s = 1; s <= 64u && (s == 1u || s * 128u <= prefix); s++) {
-            const double cost = (double)((groups * s + 255u) / 256u) * (double)((tiles + s - 1u) / s + 3u) * 2.5 + (double)rows * s * dim * 8.0 / 4e6;
-            if (cost < best) best = cost, m.splits = s;
+        auto tiles_of = [&](uint32_t rows) { return std::max<uint64_t>(x.n_groups, (all + (uint64_t)x.n_groups * rows / 2u) / rows); };
+        TokensPlan &t = p.prefix_few;
+        t.tile_rows = all <= 16u || dim > 128u ? 16u : 32u;
+        t.row_tiles = (uint32_t)((all + t.tile_rows - 1u) / t.tile_rows);
+        const uint64_t few = tiles_of(t.tile_rows) * heads;
+        // Few rows by tokens_kernel, many by parts_kernel.  Measured (us, the whole call, tokens / parts; 300 tokens behind the prefix; 8 heads x
+        // 128, or 4 x 64 or 256): one prefix of 8000 tokens with 32 rows a head 32.6 / 33.8, with 64 33.5 / 35.4, with 128 37.4 / 38.7, with 256
+        // 47.4 / 46.6, of 30000 tokens with 64 45 / 49, with 128 61 / 54; four of 2000 with 32 in all 40 / 35; 64 elements, 8000 tokens, with 128
+        // 27 / 39, with 256 29 / 43; 256 elements with 64 37 / 61, with 128 40 / 52.
+        p.few_rows = few <= 256u && (uint64_t)t.row_tiles * x.n_groups <= 8u * tiles_of(t.tile_rows) &&
+                     (dim <= 64u || dim > 128u || (x.n_groups == 1u && all <= 64u));
+        if (p.few_rows) {
+            // four wavefronts with 256 tokens at least, on every compute unit
+            t.whole = true;
+            t.waves = 4u;
+            t.by_xcd = x.n_groups * heads >= 8u;
+            t.splits = p.prefix.splits = (uint32_t)std::max<uint64_t>(1u, std::min<uint64_t>(256u / few, prefix / 256u));
+        } else {
+            PartsPlan &m = p.prefix;
+            m.row_tiles = (uint32_t)((all + rows_each - 1u) / rows_each);
+            // As many splits as make the sum of two least: rounds of 256 workgroups, with three tiles of 64 tokens for each one's start and
+            // end, 2.5 us a tile; and a part of every row written and read again, at 4 TB/s.
+            const uint64_t groups = tiles_of(rows_each) * heads, tiles = (prefix + 63u) / 64u;
+            double best = INFINITY;
+            for (uint32_t s = 1; s <= 64u && (s == 1u || s * 128u <= prefix); s++) {
+                const double cost = (double)((groups * s + 255u) / 256u) * (double)((tiles + s - 1u) / s + 3u) * 2.5 + (double)rows * s * dim * 8.0 / 4e6;
+                if (cost < best) best = cost, m.splits = s;
+            }
+            m.chunk = std::max(64u, ((prefix + m.splits - 1u) / m.splits + 63u) & ~63u);
+            m.splits = (prefix + m.chunk - 1u) / m.chunk;
         }
-        m.chunk = std::max(64u, ((prefix + m.splits - 1u) / m.splits + 63u) & ~63u);
-        m.splits = (prefix + m.chunk - 1u) / m.chunk;
     }
     p.tokens = shared <= most_rows(dim);
     p.splits = 1u;
@@ -286,7 +305,7 @@ SharedSizes plan_shared(uint32_t heads, uint32_t dim, uint32_t block_size, const
     }
     // Nothing split: the sums of what is behind the prefix are where the prefix begins, and its end writes outputs (32 prompts behind 4000
     // tokens: a part of every row less to write, two less to read).
-    p.last = p.prefix.splits == 1u && p.splits == 1u;
+    p.last = !p.few_rows && p.prefix.splits == 1u && p.splits == 1u;
     z.prefix_sums = 3u * (pad64(b.n_reqs * 4ull) + pad64((x.n_groups + 1u) * 4ull));
     const uint64_t parts = p.last ? 0u : rows * p.prefix.splits;
     z.prefix_parts = z.prefix_sums + pad64(parts * 8u);
@@ -342,6 +361,8 @@ extern "C" dmi_status_t dmi_kv8_attend_shared(const dmi_kv8_t *cache, const dmi_
     for (uint64_t i = 0; i < 6u; i++) *lists[i] = reinterpret_cast<int32_t *>(at + std::min<uint64_t>(i, 3u) * reqs + (i > 3u ? i - 3u : 0u) * groups);
     p.prefix.sums = reinterpret_cast<f32x2 *>(at + z.prefix_sums);
     p.prefix.parts = reinterpret_cast<float *>(at + z.prefix_parts);
+    p.prefix_few.sums = p.prefix.sums;
+    p.prefix_few.parts = p.prefix.parts;
     p.few.sums = p.many.sums = p.sums = reinterpret_cast<f32x2 *>(at + z.sums);
     p.few.parts = p.many.parts = p.parts = reinterpret_cast<float *>(at + z.parts);
     return launched(launch_shared(a, p, q->dtype, (hipStream_t)hip_stream));

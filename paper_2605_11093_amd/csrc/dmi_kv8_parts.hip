@@ -874,7 +874,7 @@ __global__ __launch_bounds__(256) void join_shared_kernel(AttendArgs a, SharedPl
     if (threadIdx.x >= each * wide) return;
     const int shared = p.shared[blockIdx.y];
     if (p.last && shared) return;
-    const int before = p.prefix.chunk ? min((shared + (int)p.prefix.chunk - 1) / (int)p.prefix.chunk, (int)p.prefix.splits) : 0;
+    const int before = p.few_rows ? (shared ? (int)p.prefix.splits : 0) : p.prefix.chunk ? min((shared + (int)p.prefix.chunk - 1) / (int)p.prefix.chunk, (int)p.prefix.splits) : 0;
     for (uint32_t n = blockIdx.x * each + threadIdx.x / wide; n < rows * a.c.heads; n += gridDim.x * each) {
         const uint32_t head = n / rows, row = n - head * rows;
         const QueryRow w = query_row(a, head, row);
@@ -910,7 +910,10 @@ hipError_t launch_shared(const AttendArgs &a, const SharedPlan &p, uint32_t dtyp
     if (e != hipSuccess) return e;
     AttendArgs group = a;
     group.b = Batch{p.group_lens, p.group_rows, p.group_seqs, p.n_groups, a.b.total_new, a.b.total_new, p.max_prefix};
-    if (p.n_groups && !p.last && (e = launch_parts_apart(group, p.prefix, kPrefix, dtype, s)) != hipSuccess) return e;
+    if (p.n_groups && !p.last) {
+        e = p.few_rows ? launch_tokens_apart(group, p.prefix_few, kPrefix, dtype, s) : launch_parts_apart(group, p.prefix, kPrefix, dtype, s);
+        if (e != hipSuccess) return e;
+    }
     // a table of one column, of which each request has those from its place in the real one on
     AttendArgs rest = a;
     rest.c.n_seqs = 1u << 31, rest.c.table_stride = 1;

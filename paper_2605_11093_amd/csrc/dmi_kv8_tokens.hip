@@ -76,6 +76,7 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
     constexpr int KK = DP / 32;                 // instructions for a sixteen's scores
     constexpr int VW = DP / 64;                 // words of V a lane and token
     constexpr int NJ = DP / 16;                 // instructions for 16 query rows' outputs
+    constexpr int kV = KIND == kPrefix ? 0 : kOnce;     // (a prefix is read by every row tile)
 
     const int lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -85,7 +86,14 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
     if constexpr (WHOLE) {
         uint32_t pair = blockIdx.x / p.splits;
         range = (int)(blockIdx.x - pair * p.splits);
-        if (KIND != kWhole && p.by_xcd) {
+        if constexpr (KIND == kPrefix) {
+            // all row tiles and splits of a group and head on one XCD, whose cache its codes go through once
+            const uint32_t each = p.row_tiles * p.splits, nth = p.by_xcd ? blockIdx.x >> 3 : blockIdx.x, which = nth / each, inner = nth - which * each;
+            pair = p.by_xcd ? 8u * which + (blockIdx.x & 7u) : which;
+            row_tile = inner / p.splits;
+            range = (int)(inner - row_tile * p.splits);
+            if (pair >= a.b.n_reqs * a.c.heads) return;
+        } else if (KIND != kWhole && p.by_xcd) {
             // workgroups go to the eight XCDs in turn: the heads of a request on one of them, whose scales of a block lie in one line
             const uint32_t nth = blockIdx.x >> 3, each = a.c.heads * p.splits, eighth = nth / each;
             pair = (nth - eighth * each) / p.splits;
@@ -96,7 +104,8 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
         r = (int)(pair / a.c.heads);
         head = pair % a.c.heads;
         const Request q = KIND == kListed ? token_of(a.b, a.c, r) : request_of(a.b, a.c, r);
-        const int tiles = KIND == kListed ? (listed_tokens(a, q) + 31) >> 5 : q.fresh > 0 ? tiles_of(q) : a.w.data ? (q.len + 31) >> 5 : 0;
+        if (KIND == kPrefix && (int)row_tile * 16 * NT >= q.fresh * (int)a.group) return;
+        const int tiles = KIND == kListed ? (listed_tokens(a, q) + 31) >> 5 : KIND == kPrefix ? (q.len + 31) >> 5 : q.fresh > 0 ? tiles_of(q) : a.w.data ? (q.len + 31) >> 5 : 0;
         if constexpr (KIND == kListed) held = q;
         const int nth = range * NW + wave, of = (int)p.splits * NW;
         first = (int)((int64_t)tiles * nth / of);
@@ -193,7 +202,7 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
         for (int n = 0; n < NT; n++) {
             const int row = row0 + 16 * n + col;
             const QueryRow w = query_row(a, head, (uint32_t)min(row, max(rows - 1, 0)));     // (columns behind the last row: not written)
-            lim[n] = KIND == kListed ? INT_MAX : row < rows ? q.len - q.fresh + w.token : q.len;
+            lim[n] = KIND == kListed || KIND == kPrefix ? INT_MAX : row < rows ? q.len - q.fresh + w.token : q.len;
             const uint16_t *src = static_cast<const uint16_t *>(a.q.data) + (int64_t)min(q.start + w.token, (int)a.b.total_new - 1) * a.q.row_stride +
                                   (int64_t)w.head * a.q.head_stride;
 #pragma unroll
@@ -202,7 +211,7 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
                 qf[n][k] = *reinterpret_cast<const u32x4 *>(src + (d < (int)a.c.dim ? d : 0));
             }
         }
-        const int all_see = KIND == kListed ? INT_MAX : q.len - q.fresh + row0 / (int)a.group;      // what every row of the tile sees
+        const int all_see = KIND == kListed || KIND == kPrefix ? INT_MAX : q.len - q.fresh + row0 / (int)a.group;      // what every row of the tile sees
 
         // Where a sixteen's codes lie; one that is not there is read at the cache's first block and counts no token.
         auto place = [&](int tile, int x) {
@@ -227,13 +236,13 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
 #pragma unroll
                 for (int i = 0; i < 4; i++) {
                     const uint32_t at = v_off + (uint32_t)i * (uint32_t)a.c.slot_stride;
-                    if constexpr (VW == 1) rv[4 * x + i][0] = load_b32<kOnce>(v, at);
+                    if constexpr (VW == 1) rv[4 * x + i][0] = load_b32<kV>(v, at);
                     if constexpr (VW == 2) {
-                        const u32x2 w = load_b64<kOnce>(v, at);
+                        const u32x2 w = load_b64<kV>(v, at);
                         rv[4 * x + i][0] = w[0], rv[4 * x + i][1] = w[1];
                     }
                     if constexpr (VW == 4) {
-                        const u32x4 w = load_b128<kOnce>(v, at);
+                        const u32x4 w = load_b128<kV>(v, at);
 #pragma unroll
                         for (int y = 0; y < 4; y++) rv[4 * x + i][y] = w[y];
                     }
@@ -481,7 +490,7 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
             }
             __syncthreads();
             for (int u = (int)threadIdx.x; u < NT * NJ / 4 * 64; u += 64 * NW) {
-                const int n = (u >> 6) / (NJ / 4), j = (u >> 6) % (NJ / 4) * 4, row = 16 * n + col;
+                const int n = (u >> 6) / (NJ / 4), j = (u >> 6) % (NJ / 4) * 4, nth = 16 * n + col, row = row0 + nth;
                 if (row >= rows) continue;
                 f32x4 sum[4] = {};
 #pragma unroll
@@ -489,11 +498,11 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
 #pragma unroll
                     for (int k = 0; k < 4; k++) sum[k] += joined[v][(n * NJ + j + k) * 64 + lane];
                 float l_all;
-                const float total = total_of(row, l_all), f = total == -INFINITY && l_all == 0.0f ? 0.0f : 1.0f / l_all;
+                const float total = total_of(nth, l_all), f = total == -INFINITY && l_all == 0.0f ? 0.0f : 1.0f / l_all;
                 const QueryRow w = query_row(a, head, (uint32_t)row);
-                if (KIND == kRest || p.splits > 1u) {
+                if (KIND == kRest || KIND == kPrefix || p.splits > 1u) {
                     const int64_t part = ((int64_t)(q.start + w.token) * a.q_heads + w.head) * p.splits + range;
-                    if (g == 0 && j == 0) p.sums[part] = f32x2{top_of(row), l_all};
+                    if (g == 0 && j == 0) p.sums[part] = f32x2{top_of(nth), l_all};
                     float *dst = p.parts + part * a.c.dim;
 #pragma unroll
                     for (int i = 0; i < 4; i++) {
@@ -762,13 +771,15 @@ template <typename T> static hipError_t tokens(const AttendArgs &a, const Tokens
     return hipGetLastError();
 }
 
-// A workgroup (or p.splits of them) for each request or new token and head: the rest of contexts behind a prefix, whose parts another
-// kernel joins, or listed blocks.
+// A workgroup (or p.splits of them) for each request or new token and head: the rest of contexts behind a prefix, or a prefix and one of its
+// group's row tiles, whose parts another kernel joins, or listed blocks.
 template <typename T, Kind KIND> static hipError_t tokens_apart(const AttendArgs &a, const TokensPlan &p, hipStream_t s)
 {
     const uint32_t units = KIND == kListed ? a.b.total_new : a.b.n_reqs;
-    const uint64_t groups = (uint64_t)(p.by_xcd ? (units + 7u) / 8u * 8u : units) * a.c.heads * p.splits;
-    if (!launchable(groups, 512) || (uint64_t)units * a.c.heads > UINT32_MAX) return hipErrorInvalidConfiguration;
+    const uint64_t pairs = (uint64_t)units * a.c.heads;
+    const uint64_t groups = KIND == kPrefix ? (p.by_xcd ? (pairs + 7u) / 8u * 8u : pairs) * p.row_tiles * p.splits
+                                            : (uint64_t)(p.by_xcd ? (units + 7u) / 8u * 8u : units) * a.c.heads * p.splits;
+    if (!launchable(groups, 512) || pairs > UINT32_MAX) return hipErrorInvalidConfiguration;
     auto launch = [&](auto dp_, auto nt_) {
         constexpr int DP = decltype(dp_)::value, NT = decltype(nt_)::value, many = waves_of(DP, NT, true);
         if (p.waves == 4u || many == 4) tokens_kernel<T, DP, NT, true, KIND, 4><<<(uint32_t)groups, 256, 0, s>>>(a, p);
@@ -786,6 +797,7 @@ template <typename T, Kind KIND> static hipError_t tokens_apart(const AttendArgs
 
 hipError_t launch_tokens_apart(const AttendArgs &a, const TokensPlan &p, Kind kind, uint32_t dtype, hipStream_t s)
 {
+    if (kind == kPrefix) return dtype == DMI_DTYPE_BF16 ? tokens_apart<Bf16, kPrefix>(a, p, s) : tokens_apart<Fp16, kPrefix>(a, p, s);
     if (kind == kListed) return dtype == DMI_DTYPE_BF16 ? tokens_apart<Bf16, kListed>(a, p, s) : tokens_apart<Fp16, kListed>(a, p, s);
     return dtype == DMI_DTYPE_BF16 ? tokens_apart<Bf16, kRest>(a, p, s) : tokens_apart<Fp16, kRest>(a, p, s);
 }
