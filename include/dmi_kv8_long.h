@@ -102,9 +102,9 @@ typedef struct {
 } dmi_kv8_prefix_t;
 
 /*
- * dmi_kv8_attend (without weights) for such groups.  Of a prefix, the whole blocks that all new tokens of the group see are read once
- * for the group, through the row of its first request (which must list them; the other requests' rows need not), and all other tokens of a request through its own.
- * starts_dev, where given, must be contiguous within a group (starts[r+1] is where request r+1's rows begin, as always).
+ * dmi_kv8_attend (without weights) for such groups.  The whole blocks of a prefix that lie in front of the first request's new tokens are
+ * read once for the group, through that request's row of the block table (the others' rows need not list them), by every request that has as
+ * many tokens in front of its new ones.  All other tokens, and all tokens of a request that has not, are read through its own row.
  */
 uint64_t dmi_kv8_attend_shared_workspace(const dmi_kv8_t *cache /*[host]*/, const dmi_kv8_batch_t *batch /*[host]*/,
                                          const dmi_kv8_prefix_t *prefix /*[host]*/, uint32_t n_q_heads);

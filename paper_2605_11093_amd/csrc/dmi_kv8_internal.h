@@ -102,6 +102,8 @@ struct AttendArgs {
     uint32_t group, q_heads;
     const int32_t *blocks;                      // kListed: those attended to, [new token][head][n_select]
     uint32_t n_select;
+    uint32_t n_groups, max_prefix;              // kPrefix, kLast, kRest: see dmi_kv8_prefix_t
+    const int32_t *group_starts, *prefix;
 };
 
 // What the attention kernels do: a whole context; the rest of one behind a shared prefix, whose sums are left as parts whatever their
@@ -149,10 +151,6 @@ struct SharedPlan {
     uint32_t splits;                            // of what is behind the prefix
     f32x2 *sums;                                // [row of out][split]
     float *parts;
-    uint32_t n_groups, max_prefix;
-    const int32_t *group_starts, *prefix_tokens;
-    int32_t *shared, *lens, *seqs;              // for each request: tokens read for its group, its others, its place in the block table
-    int32_t *group_lens, *group_seqs, *group_rows;      // for each group: tokens read for all, row of the block table, first row of q
 };
 
 // What a launch may have in its first dimension: threads are counted in 32 bits.  A call whose launches need more is refused before
@@ -211,6 +209,45 @@ __device__ __forceinline__ Request token_of(const Batch &b, const Cache &c, int 
     const Request q = request_of(b, c, min(r, (int)b.n_reqs - 1));
     const int nth = token - q.start;
     return {q.row, min(q.len, max(0, q.len - q.fresh + nth + 1)), token, nth >= 0 && nth < q.fresh ? 1 : 0};
+}
+
+// Groups of requests that share the beginning of their contexts.  What a group shares hangs on its first request alone, and whether
+// another request takes part on that request alone, so that nothing has to be counted before a launch.
+// A group as a request: the rows of all its requests' new tokens; `row` is its first request here.
+__device__ __forceinline__ Request group_rows(const AttendArgs &a, int g)
+{
+    const int n = (int)a.b.n_reqs, first = min(max(a.group_starts[g], 0), n), last = min(max(a.group_starts[g + 1], first), n);
+    const int start = a.b.starts ? min(max(a.b.starts[first], 0), (int)a.b.total_new) : first;
+    const int end = a.b.starts ? min(max(a.b.starts[last], start), (int)a.b.total_new) : last;
+    return {first, 0, start, first < last ? end - start : 0};
+}
+// Tokens that are read once for group g: whole blocks of its prefix, in front of its first request's new tokens.  `row`: that one's in the table.
+__device__ __forceinline__ int group_tokens(const AttendArgs &a, int g, int &row)
+{
+    const int first = min(max(a.group_starts[g], 0), (int)a.b.n_reqs);
+    row = 0;
+    if (first >= min(a.group_starts[g + 1], (int)a.b.n_reqs)) return 0;
+    const Request q = request_of(a.b, a.c, first);
+    row = q.row;
+    const int tokens = min(min(max(a.prefix[g], 0), (int)a.max_prefix), max(q.len - q.fresh, 0));
+    return (int)(((uint32_t)(((uint64_t)((uint32_t)tokens >> 4) * a.c.per_block) >> 31)) * a.c.bs);
+}
+// How many of them a request takes: all, where it has as many in front of its new tokens, or none.  All lanes of a wavefront look for its
+// group, the last one that begins at or in front of it, 64 places at a time.
+__device__ __forceinline__ int shared_tokens(const AttendArgs &a, int r, const Request &q)
+{
+    int g = 0, n = (int)a.n_groups;
+    if (!n) return 0;
+    while (n > 1) {
+        const int step = (n + 63) >> 6, at = (int)(threadIdx.x & 63u) * step;
+        const int k = max(1, __popcll(__ballot(at < n && a.group_starts[g + min(at, n - 1)] <= r)));
+        g += (k - 1) * step;
+        n = min(step, n - (k - 1) * step);
+    }
+    if (r < a.group_starts[g] || r >= a.group_starts[g + 1]) return 0;
+    int row;
+    const int tokens = group_tokens(a, g, row);
+    return q.len - q.fresh >= tokens ? tokens : 0;
 }
 
 // Sums over the lanes up to each one

@@ -244,7 +244,7 @@ namespace {
 
 struct SharedSizes {
     SharedPlan p;
-    uint64_t prefix_sums, prefix_parts, sums, parts, bytes;     // (what is counted for each request comes first)
+    uint64_t prefix_parts, sums, parts, bytes;  // (the prefixes' sums come first)
 };
 SharedSizes plan_shared(uint32_t heads, uint32_t dim, uint32_t block_size, const dmi_kv8_batch_t &b, const dmi_kv8_prefix_t &x, uint32_t q_heads)
 {
@@ -306,9 +306,8 @@ SharedSizes plan_shared(uint32_t heads, uint32_t dim, uint32_t block_size, const
     // Nothing split: the sums of what is behind the prefix are where the prefix begins, and its end writes outputs (32 prompts behind 4000
     // tokens: a part of every row less to write, two less to read).
     p.last = !p.few_rows && p.prefix.splits == 1u && p.splits == 1u;
-    z.prefix_sums = 3u * (pad64(b.n_reqs * 4ull) + pad64((x.n_groups + 1u) * 4ull));
     const uint64_t parts = p.last ? 0u : rows * p.prefix.splits;
-    z.prefix_parts = z.prefix_sums + pad64(parts * 8u);
+    z.prefix_parts = pad64(parts * 8u);
     z.sums = z.prefix_parts + pad64(parts * dim * 4u);
     z.parts = z.sums + pad64(rows * p.splits * 8u);
     z.bytes = rows && b.n_reqs ? z.parts + pad64(rows * p.splits * dim * 4u) : 0u;
@@ -345,21 +344,16 @@ extern "C" dmi_status_t dmi_kv8_attend_shared(const dmi_kv8_t *cache, const dmi_
         return fail(DMI_ERR_INVALID_ARG, "group_starts_dev or prefix_dev is NULL");
     if (((uintptr_t)prefix->group_starts_dev | (uintptr_t)prefix->prefix_dev) % 4u)
         return fail(DMI_ERR_INVALID_ARG, "group_starts_dev and prefix_dev must be 4-byte aligned");
-    // (a request's place in the block table goes through 31 bits)
-    if ((__int128)a.c.n_seqs * a.c.table_stride > INT32_MAX) return fail(DMI_ERR_INVALID_ARG, "the block table has more than 2^31 - 1 places");
     const SharedSizes z = plan_shared(a.c.heads, a.c.dim, a.c.bs, *batch, *prefix, n_q_heads);
     if ((st = check_workspace(z.bytes, workspace, workspace_bytes)) != DMI_OK) return st;
     if (!a.b.n_reqs || !a.b.total_new || !a.b.max_new) return DMI_OK;
     SharedPlan p = z.p;
-    p.n_groups = p.prefix.splits ? prefix->n_groups : 0u;
-    p.max_prefix = std::min(prefix->max_prefix, a.b.max_len);
-    p.group_starts = prefix->group_starts_dev;
-    p.prefix_tokens = prefix->prefix_dev;
+    a.n_groups = p.prefix.splits ? prefix->n_groups : 0u;
+    a.max_prefix = std::min(prefix->max_prefix, a.b.max_len);
+    a.group_starts = prefix->group_starts_dev;
+    a.prefix = prefix->prefix_dev;
     char *const at = static_cast<char *>(workspace);
-    const uint64_t reqs = pad64(a.b.n_reqs * 4ull), groups = pad64((prefix->n_groups + 1u) * 4ull);
-    int32_t **const lists[] = {&p.shared, &p.lens, &p.seqs, &p.group_lens, &p.group_seqs, &p.group_rows};
-    for (uint64_t i = 0; i < 6u; i++) *lists[i] = reinterpret_cast<int32_t *>(at + std::min<uint64_t>(i, 3u) * reqs + (i > 3u ? i - 3u : 0u) * groups);
-    p.prefix.sums = reinterpret_cast<f32x2 *>(at + z.prefix_sums);
+    p.prefix.sums = reinterpret_cast<f32x2 *>(at);
     p.prefix.parts = reinterpret_cast<float *>(at + z.prefix_parts);
     p.prefix_few.sums = p.prefix.sums;
     p.prefix_few.parts = p.prefix.parts;

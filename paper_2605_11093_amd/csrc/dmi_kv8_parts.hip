@@ -70,13 +70,16 @@ void parts_kernel(AttendArgs a, PartsPlan p)
     const uint32_t xcd = blockIdx.x & 7u, item = (blockIdx.x >> 3) / p.splits, split = (blockIdx.x >> 3) - item * p.splits;
     Request q{0, 0, 0, 0};
     uint32_t head = 0;
+    [[maybe_unused]] int unit_at = 0;           // the request, or group
+    [[maybe_unused]] uint32_t skipped = 0;      // kRest: blocks in front
     int row0 = -1;
+    const uint32_t units = PREFIX ? a.n_groups : a.b.n_reqs;
     if (p.counted) {
         // as many workgroups as all requests' rows make: their tiles are counted here
-        for (uint32_t n0 = 0, before = 0; n0 < a.b.n_reqs; n0 += 64u) {
+        for (uint32_t n0 = 0, before = 0; n0 < units; n0 += 64u) {
             const uint32_t r = n0 + (uint32_t)lane;
             Request own{0, 0, 0, 0};
-            if (r < a.b.n_reqs) own = request_of(a.b, a.c, (int)r);
+            if (r < units) own = PREFIX ? group_rows(a, (int)r) : request_of(a.b, a.c, (int)r);
             const int row_tiles = (own.fresh * (int)a.group + 32 * NW - 1) / (32 * NW);
             const uint32_t pairs = ((r + 1u) * a.c.heads + 7u - xcd) / 8u - (r * a.c.heads + 7u - xcd) / 8u;
             const int upto = lanes_scan(row_tiles * (int)pairs), place = (int)(item - before);
@@ -89,6 +92,7 @@ void parts_kernel(AttendArgs a, PartsPlan p)
             const int nth = place - (in ? __builtin_amdgcn_readlane(upto, in - 1) : 0), which = nth / of;
             const uint32_t first = (n0 + (uint32_t)in) * a.c.heads;
             q = request_in(own, in);
+            unit_at = (int)n0 + in;
             head = ((xcd - first) & 7u) + 8u * (uint32_t)which;
             row0 = (of - 1 - (nth - which * of)) * 32 * NW;
             break;
@@ -96,14 +100,21 @@ void parts_kernel(AttendArgs a, PartsPlan p)
     } else {
         // as many for every request as the one with most rows has
         const uint32_t pair = item / p.row_tiles * 8u + xcd, r = pair / a.c.heads;
-        if (r >= a.b.n_reqs) return;
+        if (r >= units) return;
         head = pair - r * a.c.heads;
-        q = request_of(a.b, a.c, (int)r);
+        q = PREFIX ? group_rows(a, (int)r) : request_of(a.b, a.c, (int)r);
+        unit_at = (int)r;
         row0 = (int)(p.row_tiles - 1u - item % p.row_tiles) * 32 * NW;
         if (row0 >= q.fresh * (int)a.group) return;
     }
     if (row0 < 0) return;
     const int rows = q.fresh * (int)a.group;
+    if constexpr (PREFIX) q.len = group_tokens(a, unit_at, q.row);
+    if constexpr (KIND == kRest) {
+        const int shared = shared_tokens(a, unit_at, q);
+        q.len -= shared;
+        skipped = block_of(a.c, (uint32_t)shared >> 4);
+    }
     const int older = PREFIX ? q.len - 1 : q.len - q.fresh, last_row = min(row0 + 32 * NW, rows) - 1;
     // tokens that the workgroup's last row sees (of a prefix all rows see all)
     const int seen = PREFIX ? q.len : older + last_row / (int)a.group + 1;
@@ -171,10 +182,9 @@ void parts_kernel(AttendArgs a, PartsPlan p)
     auto look = [&](int batch, auto between) {
         const int t = begin + 1024 * batch + 16 * lane;
         const uint32_t block = block_of(a.c, (uint32_t)t >> 4);
-        // (a rest's row begins inside of a table's: columns behind its last token may be none of the table)
-        const uint32_t last = KIND == kRest ? block_of(a.c, (uint32_t)(q.len - 1) >> 4) : a.c.max_blocks - 1u;
-        const int raw = a.c.table[(int64_t)q.row * a.c.table_stride + min(block, last)];
-        const bool there = t < end && block < a.c.max_blocks && (uint32_t)raw < a.c.n_blocks;
+        const uint32_t column = KIND == kRest ? block + skipped : block;
+        const int raw = a.c.table[(int64_t)q.row * a.c.table_stride + min(column, a.c.max_blocks - 1u)];
+        const bool there = t < end && column < a.c.max_blocks && (uint32_t)raw < a.c.n_blocks;
         const int entry = there ? raw : 0;
         const int64_t at = (int64_t)entry * a.c.block_stride + (int64_t)((uint32_t)t - block * a.c.bs) * a.c.slot_stride + (int64_t)head * a.c.head_stride;
         Places l{(uint32_t)at, (uint32_t)(at >> 32), 0, __ballot(there), 0};
@@ -463,8 +473,27 @@ void parts_kernel(AttendArgs a, PartsPlan p)
         }
     }
 
-    // (rows that share nothing are joined elsewhere.  No return for them: without a way around the loop the compiler runs out of registers)
-    const int written = KIND == kLast && !tiles ? 0 : rows;
+    // Rows of requests that share nothing are joined elsewhere, and rows of no request are none.  (No return for them: without a way around
+    // the loop the compiler runs out of registers.)
+    [[maybe_unused]] uint32_t written_rows = 0;
+    if constexpr (KIND == kLast) {
+        bool shares = tiles > 0 && row < rows;
+        if (shares) {
+            const int token = q.start + w.token;
+            int r = token;
+            if (a.b.starts) {                   // the last request whose rows begin at or in front of it
+                r = 0;
+                for (int n = (int)a.b.n_reqs; n > 1;) {
+                    const int step = n >> 1;
+                    if (a.b.starts[r + step] <= token) r += step, n -= step;
+                    else n = step;
+                }
+            }
+            const Request of = request_of(a.b, a.c, r);
+            shares = token >= of.start && token < of.start + of.fresh && of.len - of.fresh >= q.len;
+        }
+        written_rows = (uint32_t)__ballot(shares);
+    }
     l += __shfl_xor(l, 32);
     const int64_t at = (int64_t)(q.start + w.token) * a.q_heads + w.head;
     const bool empty = m == -INFINITY && l == 0.0f;
@@ -485,10 +514,10 @@ void parts_kernel(AttendArgs a, PartsPlan p)
             const int r = j + lane / kChunks, chunk = lane % kChunks;
             const u32x4 x = *reinterpret_cast<const u32x4 *>(in_row(r, chunk));
             const int64_t to = (int64_t)(uint32_t)__shfl((int)(uint32_t)dst, r) | (int64_t)__shfl((int)(dst >> 32), r) << 32;
-            if (wave_row + r < written && 8 * chunk < (int)a.c.dim)
+            if ((KIND == kLast ? (bool)(written_rows >> r & 1u) : wave_row + r < rows) && 8 * chunk < (int)a.c.dim)
                 *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(a.out.data) + to + 8 * chunk) = x;
         }
-        if (row < written && half == 0) {
+        if ((KIND == kLast ? (bool)(written_rows >> col & 1u) : row < rows) && half == 0) {
             const float sum = empty ? -INFINITY : m + log2_of(l);
             if (a.lse) a.lse[at] = sum * kLn2;
             if (p.totals) p.totals[at] = sum;
@@ -770,8 +799,9 @@ template <typename T, int DP, int NW, Kind KIND> static hipError_t parts(const A
     // Where the second is less the kernel counts for itself: a workgroup that finds nothing to do has waited for a compute unit of its own.
     // Measured (us, first / second): one prompt of 8192 tokens among 63 single ones 2163 / 1387, one of 512 among 255 1031 / 284, 32 ragged
     // prompts 609 / 603; where all requests are alike counting costs some 0.7 us for every 64 of them, and is not done.
-    const uint64_t by_pairs = ((uint64_t)a.b.n_reqs * a.c.heads + 7u) / 8u * p.row_tiles;
-    const uint64_t by_rows = ((uint64_t)a.b.total_new * a.group / (32u * NW) + a.b.n_reqs) * ((a.c.heads + 7u) / 8u);
+    const uint64_t units = KIND == kPrefix || KIND == kLast ? a.n_groups : a.b.n_reqs;
+    const uint64_t by_pairs = (units * a.c.heads + 7u) / 8u * p.row_tiles;
+    const uint64_t by_rows = ((uint64_t)a.b.total_new * a.group / (32u * NW) + units) * ((a.c.heads + 7u) / 8u);
     p.counted = by_pairs > by_rows;
     const uint64_t groups = (p.counted ? by_rows : by_pairs) * p.splits * 8u;
     const uint64_t weight_groups = a.w.data ? (a.b.max_len + 255ull) / 256u * a.c.heads : 0u;
@@ -809,61 +839,6 @@ hipError_t launch_parts_apart(const AttendArgs &a, const PartsPlan &p, Kind kind
 }
 
 // ---------------------------------------------------------------- contexts behind shared prefixes
-// Tokens of group g's prefix that are read for all: whole blocks, in front of all new tokens, of requests that have some; none where the
-// rows from its first request's to the next group's first are others than those requests' new tokens.  All lanes of a wavefront have to come
-// here, and all get it.
-__device__ __forceinline__ int prefix_of(const AttendArgs &a, const SharedPlan &p, int g)
-{
-    const int n = (int)a.b.n_reqs, first = min(max(p.group_starts[g], 0), n), last = min(max(p.group_starts[g + 1], first), n);
-    int least = first < last ? min(max(p.prefix_tokens[g], 0), (int)p.max_prefix) : 0, rows = 0;
-    for (int r = first + (int)(threadIdx.x & 63u); r < last; r += 64) {
-        const Request q = request_of(a.b, a.c, r);
-        if (q.fresh > 0 || r == first) least = min(least, max(q.len - q.fresh, 0));
-        rows += q.fresh;
-    }
-#pragma unroll
-    for (int m = 32; m; m >>= 1) least = min(least, __shfl_xor(least, m)), rows += __shfl_xor(rows, m);
-    if (a.b.starts && rows != a.b.starts[last] - a.b.starts[first]) least = 0;
-    return (int)(block_of(a.c, (uint32_t)least >> 4) * a.c.bs);
-}
-
-// The prefixes as a batch, one request for each group, and what each request has behind its group's, over a table of one column: its place
-// in the block table, its length.  A wavefront for each; a request that no group has shares nothing.
-__global__ __launch_bounds__(256) void shared_kernel(AttendArgs a, SharedPlan p)
-{
-    const int lane = threadIdx.x & 63;
-    int r = (int)(blockIdx.x * 4u + (threadIdx.x >> 6));
-    if (r >= (int)a.b.n_reqs) {
-        r -= (int)a.b.n_reqs;
-        if (r > (int)p.n_groups || !p.n_groups) return;
-        // rows of a group begin where its first request's do, and the last one's end where the next group's begin
-        const int first = min(max(p.group_starts[r], 0), (int)a.b.n_reqs);
-        const int tokens = r < (int)p.n_groups ? prefix_of(a, p, r) : 0;
-        if (lane) return;
-        p.group_rows[r] = a.b.starts ? a.b.starts[first] : first;
-        if (r < (int)p.n_groups) {
-            p.group_lens[r] = tokens;
-            p.group_seqs[r] = first < (int)a.b.n_reqs ? request_of(a.b, a.c, first).row : 0;
-        }
-        return;
-    }
-    // the last group that begins at or in front of the request
-    int g = 0, n = (int)p.n_groups;
-    while (n > 1) {
-        const int step = (n + 63) >> 6, at = lane * step;
-        const int k = max(1, __popcll(__ballot(at < n && p.group_starts[g + min(at, n - 1)] <= r)));
-        g += (k - 1) * step;
-        n = min(step, n - (k - 1) * step);
-    }
-    const Request q = request_of(a.b, a.c, r);
-    int shared = 0;
-    if (n && p.group_starts[g] <= r && r < p.group_starts[g + 1]) shared = min(prefix_of(a, p, g), max(q.len - q.fresh, 0));
-    if (lane) return;
-    p.shared[r] = shared;
-    p.lens[r] = q.len - shared;
-    p.seqs[r] = (int32_t)((int64_t)q.row * a.c.table_stride + (int64_t)block_of(a.c, (uint32_t)shared >> 4));
-}
-
 // Outputs out of the parts of prefixes and of what is behind them (p.last: of requests that share nothing, the others' are written already):
 // see join_parts_kernel.
 template <typename T>
@@ -871,9 +846,9 @@ __global__ __launch_bounds__(256) void join_shared_kernel(AttendArgs a, SharedPl
 {
     const Request q = request_of(a.b, a.c, (int)blockIdx.y);
     const uint32_t wide = a.c.dim / 4u, each = 256u / wide, rows = (uint32_t)q.fresh * a.group, lane = threadIdx.x % wide;
-    if (threadIdx.x >= each * wide) return;
-    const int shared = p.shared[blockIdx.y];
+    const int shared = shared_tokens(a, (int)blockIdx.y, q);
     if (p.last && shared) return;
+    if (threadIdx.x >= each * wide) return;
     const int before = p.few_rows ? (shared ? (int)p.prefix.splits : 0) : p.prefix.chunk ? min((shared + (int)p.prefix.chunk - 1) / (int)p.prefix.chunk, (int)p.prefix.splits) : 0;
     for (uint32_t n = blockIdx.x * each + threadIdx.x / wide; n < rows * a.c.heads; n += gridDim.x * each) {
         const uint32_t head = n / rows, row = n - head * rows;
@@ -905,25 +880,17 @@ __global__ __launch_bounds__(256) void join_shared_kernel(AttendArgs a, SharedPl
 
 hipError_t launch_shared(const AttendArgs &a, const SharedPlan &p, uint32_t dtype, hipStream_t s)
 {
-    shared_kernel<<<(a.b.n_reqs + p.n_groups + 4u) / 4u, 256, 0, s>>>(a, p);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    AttendArgs group = a;
-    group.b = Batch{p.group_lens, p.group_rows, p.group_seqs, p.n_groups, a.b.total_new, a.b.total_new, p.max_prefix};
-    if (p.n_groups && !p.last) {
-        e = p.few_rows ? launch_tokens_apart(group, p.prefix_few, kPrefix, dtype, s) : launch_parts_apart(group, p.prefix, kPrefix, dtype, s);
+    hipError_t e = hipSuccess;
+    if (a.n_groups && !p.last) {
+        e = p.few_rows ? launch_tokens_apart(a, p.prefix_few, kPrefix, dtype, s) : launch_parts_apart(a, p.prefix, kPrefix, dtype, s);
         if (e != hipSuccess) return e;
     }
-    // a table of one column, of which each request has those from its place in the real one on
-    AttendArgs rest = a;
-    rest.c.n_seqs = 1u << 31, rest.c.table_stride = 1;
-    rest.b.rows = p.seqs, rest.b.lens = p.lens;
-    e = p.tokens ? launch_tokens_apart(rest, p.few, kRest, dtype, s) : launch_parts_apart(rest, p.many, kRest, dtype, s);
+    e = p.tokens ? launch_tokens_apart(a, p.few, kRest, dtype, s) : launch_parts_apart(a, p.many, kRest, dtype, s);
     if (e != hipSuccess) return e;
     if (p.last) {
         PartsPlan prefix = p.prefix;
         prefix.sums = p.sums, prefix.parts = p.parts;
-        if ((e = launch_parts_apart(group, prefix, kLast, dtype, s)) != hipSuccess) return e;
+        if ((e = launch_parts_apart(a, prefix, kLast, dtype, s)) != hipSuccess) return e;
     }
     const uint32_t each = 256u / (a.c.dim / 4u);
     const dim3 grid(std::min((a.b.max_new * a.q_heads + each - 1u) / each, p.last ? 64u : 1u << 20), a.b.n_reqs);

@@ -83,6 +83,7 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
     uint32_t head, row_tile = 0;
     int r = 0, seg0 = 0, range = 0, first, last;        // seg0: the request's first tile; first, last: the range's tiles
     Request held{0, 0, 0, 0};                           // of this lane, where there are no more than lanes
+    [[maybe_unused]] uint32_t skipped = 0;              // kRest: blocks in front
     if constexpr (WHOLE) {
         uint32_t pair = blockIdx.x / p.splits;
         range = (int)(blockIdx.x - pair * p.splits);
@@ -92,7 +93,7 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
             pair = p.by_xcd ? 8u * which + (blockIdx.x & 7u) : which;
             row_tile = inner / p.splits;
             range = (int)(inner - row_tile * p.splits);
-            if (pair >= a.b.n_reqs * a.c.heads) return;
+            if (pair >= a.n_groups * a.c.heads) return;
         } else if (KIND != kWhole && p.by_xcd) {
             // workgroups go to the eight XCDs in turn: the heads of a request on one of them, whose scales of a block lie in one line
             const uint32_t nth = blockIdx.x >> 3, each = a.c.heads * p.splits, eighth = nth / each;
@@ -103,10 +104,16 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
         }
         r = (int)(pair / a.c.heads);
         head = pair % a.c.heads;
-        const Request q = KIND == kListed ? token_of(a.b, a.c, r) : request_of(a.b, a.c, r);
+        Request q = KIND == kListed ? token_of(a.b, a.c, r) : KIND == kPrefix ? group_rows(a, r) : request_of(a.b, a.c, r);
+        if constexpr (KIND == kPrefix) q.len = group_tokens(a, r, q.row);
+        if constexpr (KIND == kRest) {
+            const int shared = shared_tokens(a, r, q);
+            q.len -= shared;
+            skipped = block_of(a.c, (uint32_t)shared >> 4);
+        }
         if (KIND == kPrefix && (int)row_tile * 16 * NT >= q.fresh * (int)a.group) return;
         const int tiles = KIND == kListed ? (listed_tokens(a, q) + 31) >> 5 : KIND == kPrefix ? (q.len + 31) >> 5 : q.fresh > 0 ? tiles_of(q) : a.w.data ? (q.len + 31) >> 5 : 0;
-        if constexpr (KIND == kListed) held = q;
+        if constexpr (KIND != kWhole) held = q;
         const int nth = range * NW + wave, of = (int)p.splits * NW;
         first = (int)((int64_t)tiles * nth / of);
         last = (int)((int64_t)tiles * (nth + 1) / of);
@@ -158,8 +165,8 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
     }
     v_off = (uint32_t)(4 * g) * (uint32_t)a.c.slot_stride + ((uint32_t)col * (DP / 16) < a.c.dim ? (uint32_t)col * (DP / 16) : 0u);
 
-    for (; KIND == kListed || (r < (int)a.b.n_reqs && (WHOLE || seg0 < last)); r++) {
-        const Request q = KIND == kListed ? held : !WHOLE && a.b.n_reqs <= 64u ? request_in(held, r) : request_of(a.b, a.c, r);
+    for (; KIND != kWhole || (r < (int)a.b.n_reqs && (WHOLE || seg0 < last)); r++) {
+        const Request q = KIND != kWhole ? held : !WHOLE && a.b.n_reqs <= 64u ? request_in(held, r) : request_of(a.b, a.c, r);
         const int seg_tiles = WHOLE ? last : tiles_of(q), seg_first = seg0;
         seg0 += seg_tiles;
         const int rows = q.fresh * (int)a.group;
@@ -186,6 +193,7 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
                     l.left = block <= (uint32_t)(q.len - 1) / a.c.bs ? min(16, q.len - (int)(block * a.c.bs + slot)) : 0;
                     if (l.left <= 0) block = a.c.max_blocks;
                 }
+                if constexpr (KIND == kRest) block += skipped;
                 l.entry = entry_of(a.c, q.row, block);
                 if (l.entry >= 0) {
                     l.ks = *scale_at(a.c, 0, l.entry, head) * a.scale_log2;
@@ -775,7 +783,7 @@ template <typename T> static hipError_t tokens(const AttendArgs &a, const Tokens
 // group's row tiles, whose parts another kernel joins, or listed blocks.
 template <typename T, Kind KIND> static hipError_t tokens_apart(const AttendArgs &a, const TokensPlan &p, hipStream_t s)
 {
-    const uint32_t units = KIND == kListed ? a.b.total_new : a.b.n_reqs;
+    const uint32_t units = KIND == kListed ? a.b.total_new : KIND == kPrefix ? a.n_groups : a.b.n_reqs;
     const uint64_t pairs = (uint64_t)units * a.c.heads;
     const uint64_t groups = KIND == kPrefix ? (p.by_xcd ? (pairs + 7u) / 8u * 8u : pairs) * p.row_tiles * p.splits
                                             : (uint64_t)(p.by_xcd ? (units + 7u) / 8u * 8u : units) * a.c.heads * p.splits;

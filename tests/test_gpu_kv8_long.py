@@ -422,6 +422,39 @@ def test_shared_in_place(B):        # noqa: F811
     _check_shared(B, s, BF16, 4, in_place=True)
 
 
+@pytest.mark.parametrize("dtype,dim,group", [(BF16, 128, 4), (FP16, 128, 8), (BF16, 96, 4)])
+def test_shared_and_never_split(B, dtype, dim, group):        # noqa: F811
+    """Short prefixes under many rows, single tokens and prompts: what is behind them is where their sums begin.  Some requests share
+    nothing: of no group, too short for the prefix, without tokens, of a group whose first is too short."""
+    s = Shared(B, 62, [(200, [(1, 230 + 7 * i) for i in range(40)] + [(1, 120), (0, 300), (1, 1)])], 2, dim, 16, alone=(3, 2))
+    _check_shared(B, s, dtype, group)
+    s = Shared(B, 63, [(200, [(40, 300), (3, 210), (50, 120), (90, 400)]), (64, [(3, 40), (64, 128)]), (100, [(20, 200)] * 3)], 2, dim, 16, alone=(1, 1))
+    _check_shared(B, s, dtype, group)
+
+
+def test_rows_behind_max_new_are_left(B):        # noqa: F811
+    """A request with more rows than max_new has as many new tokens as that, and the others are no request's."""
+    s = Shared(B, 64, [(200, [(40, 300), (30, 290), (40, 280)])], 2, 128, 16)
+    batch = B.KV8Batch(s.lens, starts=s.starts_dev, total_new=s.total, max_new=30, max_len=s.max_len)
+    q, qn = s.values(8, BF16)
+    out, lse = torch.full((s.total, 8, 128), 7.0, dtype=BF16, device=DEV), torch.full((s.total, 8), 7.0, device=DEV)
+    B.kv8_attend_shared(s.cache, batch, s.prefix, q, out, lse=lse, stream=_stream())
+    spans = [(row, start, 30, length) for row, start, _, length in s.spans]
+    (o, l, _), (do, dl, _) = K.attend(s.cpu(), spans, qn, 128 ** -0.5, 4, BF16)
+    for start, end in ((30, 40), (100, 110)):
+        o[start:end], l[start:end] = 7.0, 7.0
+    K.near(out.float().cpu().numpy(), o, do, "out")
+    K.near(lse.cpu().numpy(), l, dl, "lse")
+
+
+def test_shared_by_many_requests_and_groups(B):        # noqa: F811
+    """More groups and requests than a wavefront looks at at once."""
+    s = Shared(B, 65, [(20 + i % 30, [(1, 52 + (i * k) % 40) for k in range(1 + i % 3)]) for i in range(70)], 1, 64, 16, alone=(2, 5))
+    _check_shared(B, s, BF16, 2)
+    s = Shared(B, 66, [(40, [(1, 44 + i % 60) for i in range(150)]), (60, [(2, 64 + i) for i in range(5)])], 1, 64, 16)
+    _check_shared(B, s, FP16, 4)
+
+
 @pytest.mark.parametrize("starts", [[3, 1, 0], [0, 100, 200], [-5, 2, 1 << 30], [2, 2, 2]])
 def test_shared_by_groups_that_are_none(B, starts):        # noqa: F811
     """Contents that describe no groups lead nowhere: nothing outside of the outputs is written, nothing outside of the tensors read."""

@@ -161,14 +161,6 @@ def test_attention_behind_shared_prefixes():
     _refused("n_groups", B.kv8_attend_shared, c, b, p, _x(4), _x(4), workspace=torch.zeros(1 << 20, dtype=torch.uint8))
     with pytest.raises(ValueError, match="one entry more"):
         B.KV8Prefix(torch.zeros(1, dtype=I32), torch.zeros(1, dtype=I32), max_prefix=32)
-    # a place in the block table has to fit 31 bits
-    far = torch.zeros(4, dtype=I32).as_strided((1, 4), (4, 1))
-    c = _cache()
-    raw = B._PACK_KV8(c.k.data_ptr(), c.v.data_ptr(), c.k_scale.data_ptr(), c.v_scale.data_ptr(), *c.k.stride()[:3], *c.k_scale.stride(), 16, 2, 64, 8, 1 << 16, 4,
-                      far.data_ptr(), 1 << 16)
-    c._raw = raw
-    p = B.KV8Prefix(torch.zeros(2, dtype=I32), torch.zeros(1, dtype=I32), max_prefix=32)
-    _refused("2\\^31", B.kv8_attend_shared, c, b, p, _x(4), _x(4), workspace=torch.zeros(1 << 20, dtype=torch.uint8))
 
 
 def test_no_rows_are_no_work():
