@@ -342,64 +342,77 @@ __device__ __forceinline__ uint32_t unordered(uint32_t w)
 }
 // The top bit of every byte that is 255
 __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) { return (w & 0x7F7F7F7Fu) + 0x01010101u & w & 0x80808080u; }
-typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-// The larger of two words' bytes, each
-__device__ __forceinline__ uint32_t larger(uint32_t x, uint32_t y)
-{
-    const u16x2 a = __builtin_bit_cast(u16x2, x & 0x00FF00FFu), b = __builtin_bit_cast(u16x2, y & 0x00FF00FFu);
-    const u16x2 c = __builtin_bit_cast(u16x2, x & 0xFF00FF00u), d = __builtin_bit_cast(u16x2, y & 0xFF00FF00u);
-    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(a, b)) | __builtin_bit_cast(uint32_t, __builtin_elementwise_max(c, d));
-}
 
-// A wavefront per block that new tokens reach and head: a lane has 16 elements of every few tokens, as words whose bytes compare like the
-// numbers (the least as the largest of what is left to 255).
+// The largest and the least of bytes, of each of a word's four: as the upper bytes of 16-bit numbers, whose order they decide, the second and
+// fourth where they are, the first and third shifted there.
+struct Extremes {
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    u16x2 most[2] = {{0, 0}, {0, 0}}, least[2] = {{0xFFFF, 0xFFFF}, {0xFFFF, 0xFFFF}};
+    __device__ __forceinline__ void take(uint32_t for_most, uint32_t for_least)
+    {
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            most[i] = __builtin_elementwise_max(most[i], __builtin_bit_cast(u16x2, i ? for_most << 8 : for_most));
+            least[i] = __builtin_elementwise_min(least[i], __builtin_bit_cast(u16x2, i ? for_least << 8 : for_least));
+        }
+    }
+    static __device__ __forceinline__ uint32_t bytes(const u16x2 (&x)[2])
+    {
+        return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, x[0]), __builtin_bit_cast(uint32_t, x[1]), 0x07030501u);
+    }
+};
+
+// A wavefront per block that new tokens reach and 64 places of its heads' rows, a lane 16 elements of every token (of every few, where the
+// heads have fewer places): what the wavefront reads of a token lies in one piece where heads follow each other.
 __global__ __launch_bounds__(256) void bound_kernel(BoundArgs a)
 {
     const uint32_t lane = threadIdx.x & 63u, item = blockIdx.x * 4u + (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t head = item % a.c.heads;
-    if (!a.counted && item / a.c.heads >= a.touched) return;
-    const Reached x = reached_by(a.b, a.c, a.counted ? -1 : (int)blockIdx.y, item / a.c.heads);
+    const uint32_t wide = a.c.dim / 16u, places = a.c.heads * wide, parts = (places + 63u) / 64u, nth = item / parts;
+    if (!a.counted && nth >= a.touched) return;
+    const Reached x = reached_by(a.b, a.c, a.counted ? -1 : (int)blockIdx.y, nth);
     if (x.lo >= x.hi) return;
     const int entry = entry_of(a.c, x.q.row, (uint32_t)x.block);
     if (entry < 0) return;
-    const uint32_t tokens = (uint32_t)x.hi - (uint32_t)x.block * a.c.bs, wide = a.c.dim / 16u, teams = 64u / wide;
-    const uint32_t team = lane / wide, d = 16u * (lane - team * wide);
-    u32x4 low = {0u, 0u, 0u, 0u}, high = low;
-    auto take = [&](const u32x4 &w) {
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-            const uint32_t o = ordered(w[i]);
-            high[i] = larger(high[i], o);
-            low[i] = larger(low[i], ~o);
-        }
-    };
-    if (team < teams) {
-        constexpr uint32_t kAhead = 4;
+    const uint32_t tokens = (uint32_t)x.hi - (uint32_t)x.block * a.c.bs, each = min(places, 64u), teams = 64u / each, team = lane / each;
+    const uint32_t place = (item - nth * parts) * 64u + lane - team * each, head = place / wide, d = 16u * (place - head * wide);
+    const bool there = team < teams && place < places;
+    Extremes e[4];
+    if (there) {
+        constexpr uint32_t kAhead = 8;
+        const uint8_t *const from = code_at(a.c, 0, entry, 0, head) + d;
         for (uint32_t t = team; t < tokens; t += kAhead * teams) {
             u32x4 w[kAhead];
 #pragma unroll
-            for (uint32_t i = 0; i < kAhead; i++) w[i] = *reinterpret_cast<const u32x4 *>(code_at(a.c, 0, entry, min(t + i * teams, tokens - 1u), head) + d);
+            for (uint32_t i = 0; i < kAhead; i++) w[i] = *reinterpret_cast<const u32x4 *>(from + (int64_t)min(t + i * teams, tokens - 1u) * a.c.slot_stride);
 #pragma unroll
-            for (uint32_t i = 0; i < kAhead; i++) take(w[i]);
+            for (uint32_t i = 0; i < kAhead; i++)
+#pragma unroll
+                for (int k = 0; k < 4; k++) {
+                    const uint32_t o = ordered(w[i][k]);
+                    e[k].take(o, o);
+                }
         }
     }
     // over the teams: those behind hand theirs to those in front (a last one that has no partner keeps its own)
     for (uint32_t n = teams; n > 1u;) {
         const uint32_t half = (n + 1u) / 2u;
 #pragma unroll
-        for (int i = 0; i < 4; i++) {
-            const uint32_t h = (uint32_t)__shfl((int)high[i], (int)(lane + half * wide)), l = (uint32_t)__shfl((int)low[i], (int)(lane + half * wide));
-            if (team + half < n) high[i] = larger(high[i], h), low[i] = larger(low[i], l);
+        for (int k = 0; k < 4; k++) {
+            const uint32_t most = (uint32_t)__shfl((int)Extremes::bytes(e[k].most), (int)(lane + half * each));
+            const uint32_t least = (uint32_t)__shfl((int)Extremes::bytes(e[k].least), (int)(lane + half * each));
+            if (team + half < n) e[k].take(most, least);
         }
         n = half;
     }
-    if (team) return;
+    if (team || !there) return;
     uint8_t *const to = a.bounds + (int64_t)entry * a.bounds_block_stride + (int64_t)head * a.bounds_head_stride + d;
+    u32x4 low, high;
 #pragma unroll
-    for (int i = 0; i < 4; i++) {
-        const uint32_t nan = (nan_bytes(high[i]) | nan_bytes(low[i])) >> 7, all = nan * 0xFFu;
-        high[i] = (unordered(high[i]) & ~all) | (0x7F7F7F7Fu & all);
-        low[i] = (unordered(~low[i]) & ~all) | (0x7F7F7F7Fu & all);
+    for (int k = 0; k < 4; k++) {
+        high[k] = Extremes::bytes(e[k].most), low[k] = Extremes::bytes(e[k].least);
+        const uint32_t all = ((nan_bytes(high[k]) | nan_bytes(~low[k])) >> 7) * 0xFFu;
+        high[k] = (unordered(high[k]) & ~all) | (0x7F7F7F7Fu & all);
+        low[k] = (unordered(low[k]) & ~all) | (0x7F7F7F7Fu & all);
     }
     *reinterpret_cast<u32x4 *>(to) = low;
     *reinterpret_cast<u32x4 *>(to + a.c.dim) = high;
@@ -410,7 +423,7 @@ hipError_t launch_bound(BoundArgs a, hipStream_t s)
     const Reach reach = reach_of(a.c, a.b);
     a.counted = reach.counted;
     a.touched = (uint32_t)std::min<uint64_t>(reach.blocks, 0xffffffffu);
-    const uint64_t groups = (reach.blocks * a.c.heads + 3u) / 4u;
+    const uint64_t groups = (reach.blocks * ((a.c.heads * (a.c.dim / 16u) + 63u) / 64u) + 3u) / 4u;
     if (!launchable(groups, 256)) return hipErrorInvalidConfiguration;
     bound_kernel<<<dim3((uint32_t)groups, reach.reqs), 256, 0, s>>>(a);
     return hipGetLastError();
