@@ -113,6 +113,13 @@ enum Kind { kWhole, kRest, kPrefix, kLast, kListed };
 
 constexpr uint32_t kFewRows = 32;               // query rows that share a head: up to here by tokens_kernel
 
+// What a prefix has left: of every row of out, splits parts, those behind a row's prefix not written where `chunk` tokens make one.
+struct PrefixParts {
+    uint32_t splits, chunk;                     // chunk 0: all are there
+    const f32x2 *sums;                          // [row of out][split]
+    const float *parts;                         // [row of out][split][dim]
+};
+
 // How few query rows are attended to: see dmi_kv8_tokens.hip.
 struct TokensPlan {
     bool whole;                                 // a workgroup takes a request and head, or one of its equal splits: no ranges
@@ -127,6 +134,8 @@ struct TokensPlan {
     float *parts;                               // [part][dim]
     float *totals;                              // [row of out]: log2 of the sum of 2^score of contexts whole in a range; NULL: no weights
     float *scores;                              // [head][query row][score_stride]; NULL: no weights
+    bool before;                                // kRest, one split: joined with the parts of prefixes, to outputs
+    PrefixParts prefix;
 };
 
 // How many query rows are attended to: see dmi_kv8_parts.hip.

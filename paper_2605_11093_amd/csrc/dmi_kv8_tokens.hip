@@ -497,6 +497,78 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
                     for (int j = 0; j < NJ; j++) joined[wave][(n * NJ + j) * 64 + lane] += o[n][j];
             }
             __syncthreads();
+            if constexpr (KIND == kRest) {
+                if (p.before) {
+                    // outputs, out of these sums and of the parts of the prefix in front: four elements a thread, the threads that a
+                    // workgroup has more than its rows have elements share the parts
+                    __shared__ f32x4 sub_o[64 * NW];
+                    __shared__ f32x2 sub_l[64 * NW];
+                    const PrefixParts &x = p.prefix;
+                    const int wide = (int)a.c.dim / 4, teams = 64 * NW / wide, team = (int)threadIdx.x / wide, d = 4 * ((int)threadIdx.x - team * wide);
+                    const int parts = !skipped ? 0 : x.chunk ? min(((int)(skipped * a.c.bs) + (int)x.chunk - 1) / (int)x.chunk, (int)x.splits) : (int)x.splits;
+                    for (int r0 = 0; r0 < rows; r0 += teams) {
+                        const int here = min(rows - r0, teams), share = teams / here, sub = team / here, nth = r0 + team - sub * here;
+                        f32x4 o4 = {0.0f, 0.0f, 0.0f, 0.0f};
+                        float m4 = -INFINITY, l4 = 0.0f;
+                        const QueryRow w = query_row(a, head, (uint32_t)min(nth, rows - 1));
+                        const int64_t at = (int64_t)(q.start + w.token) * a.q_heads + w.head;
+                        if (sub < share) {
+                            auto add = [&](float top, float sum, const f32x4 &o) {
+                                const float to = fmaxf(m4, top), base = to == -INFINITY ? 0.0f : to, f = exp2_of(m4 - base), g = exp2_of(top - base);
+                                l4 = l4 * f + sum * g;
+                                o4 = o4 * f + o * g;
+                                m4 = to;
+                            };
+                            const f32x2 *const sums_of = x.sums + at * x.splits;
+                            const float *const parts_of = x.parts + at * x.splits * a.c.dim + d;
+                            constexpr int kAhead = 8;
+                            for (int s0 = sub; s0 < parts; s0 += kAhead * share) {
+                                f32x2 s[kAhead];
+                                f32x4 o[kAhead];
+#pragma unroll
+                                for (int k = 0; k < kAhead; k++) {
+                                    const int i = min(s0 + k * share, parts - 1);
+                                    s[k] = sums_of[i];
+                                    o[k] = *reinterpret_cast<const f32x4 *>(parts_of + (int64_t)i * a.c.dim);
+                                }
+#pragma unroll
+                                for (int k = 0; k < kAhead; k++)
+                                    if (s0 + k * share < parts) add(s[k][0], s[k][1], o[k]);
+                            }
+                            if (!sub) {         // this workgroup's own
+                                const int n = nth >> 4, c = nth & 15, j = d % NJ, at4 = d / NJ;
+                                f32x4 own = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                                for (int v = 0; v < kSlots; v++)
+#pragma unroll
+                                    for (int k = 0; k < 4; k++) own[k] += reinterpret_cast<const float *>(&joined[v][(n * NJ + j + k) * 64 + 16 * (at4 >> 2) + c])[at4 & 3];
+                                float sum;
+                                total_of(nth, sum);
+                                add(top_of(nth), sum, own);
+                            }
+                        }
+                        __syncthreads();        // (the last rows' have been read)
+                        sub_o[threadIdx.x] = o4;
+                        sub_l[threadIdx.x] = f32x2{m4, l4};
+                        __syncthreads();
+                        if (sub) continue;
+                        for (int k = 1; k < share; k++) {
+                            const int from = (int)threadIdx.x + k * here * wide;
+                            const f32x2 s = sub_l[from];
+                            const float to = fmaxf(m4, s[0]), base = to == -INFINITY ? 0.0f : to, f = exp2_of(m4 - base), g = exp2_of(s[0] - base);
+                            l4 = l4 * f + s[1] * g;
+                            o4 = o4 * f + sub_o[from] * g;
+                            m4 = to;
+                        }
+                        const bool empty = m4 == -INFINITY && l4 == 0.0f;
+                        o4 *= empty ? 0.0f : 1.0f / l4;
+                        uint16_t *dst = static_cast<uint16_t *>(a.out.data) + (int64_t)(q.start + w.token) * a.out.row_stride + (int64_t)w.head * a.out.head_stride + d;
+                        *reinterpret_cast<u32x2 *>(dst) = u32x2{T::pack(o4[0], o4[1]), T::pack(o4[2], o4[3])};
+                        if (!d && a.lse) a.lse[at] = empty ? -INFINITY : (m4 + log2_of(l4)) * kLn2;
+                    }
+                    return;
+                }
+            }
             for (int u = (int)threadIdx.x; u < NT * NJ / 4 * 64; u += 64 * NW) {
                 const int n = (u >> 6) / (NJ / 4), j = (u >> 6) % (NJ / 4) * 4, nth = 16 * n + col, row = row0 + nth;
                 if (row >= rows) continue;

@@ -558,3 +558,70 @@ def test_repeated_calls_are_bit_equal(B):        # noqa: F811
         got.append((out, other))
     for x in got[1:]:
         assert torch.equal(x[0], got[0][0]) and torch.equal(x[1], got[0][1])
+
+
+def test_strided_tensors_and_rows_of_no_request(B):        # noqa: F811
+    """Queries, outputs and bounds that lie among others, heads before blocks; total_new past the last request's rows, which stay as they are."""
+    s = Shared(B, 74, [(64, [(3, 100 + 40 * i) for i in range(4)])], 2, 80, 16)
+    total = s.total + 5
+    batch = B.KV8Batch(s.lens, starts=s.starts_dev, total_new=total, max_new=3, max_len=s.max_len)
+    wide = torch.from_numpy(s.rng.normal(size=(total, 14, 96))).to(BF16).to(DEV)
+    q = wide[:, 3:9, 16:]
+    bounds = torch.full((2, s.k.shape[0], 3, 80), 0x55, dtype=torch.uint8, device=DEV).transpose(0, 1)[:, :, :2]
+    s2 = s.cpu()
+    want = bounds.cpu().numpy().copy()
+    B.kv8_bound(s.cache, batch, bounds, stream=_stream())
+    L.bound(s2, s.spans, want)
+    np.testing.assert_array_equal(K.CODES[bounds.cpu().numpy()], K.CODES[want])
+    x = K.nearest_code(np.sort(s.rng.normal(size=want.shape) * 60, axis=2))
+    bounds.copy_(torch.from_numpy(x))
+    blocks = torch.full((total, 2, 5), 77, dtype=torch.int32, device=DEV)
+    lists = np.full((total, 2, 5), 77, dtype=np.int32)
+    B.kv8_select(s.cache, batch, bounds, q, blocks, first=1, recent=1, stream=_stream())
+    qn = q.double().cpu().numpy()
+    L.select(s2, s.spans, x, qn, 3, 5, 1, 1, lists)
+    np.testing.assert_array_equal(blocks.cpu().numpy(), lists)
+    for call, (o, do) in ((lambda out, lse: B.kv8_attend_blocks(s.cache, batch, blocks, q, out, lse=lse, stream=_stream()),
+                           [x[0] for x in L.attend_blocks(s2, s.spans, lists, qn, 80 ** -0.5, 3, BF16)]),
+                          (lambda out, lse: B.kv8_attend_shared(s.cache, batch, s.prefix, q, out, lse=lse, stream=_stream()),
+                           [x[0] for x in K.attend(s2, s.spans, qn, 80 ** -0.5, 3, BF16)])):
+        room = torch.full((total, 14, 96), 7.0, dtype=BF16, device=DEV)
+        lse = torch.full((total, 6), 7.0, device=DEV)
+        call(room[:, 3:9, 16:], lse)
+        got = room.float().cpu().numpy()
+        K.near(got[:s.total, 3:9, 16:], o[:s.total], do[:s.total], "out")
+        got[:s.total, 3:9, 16:] = 7.0
+        assert (got == 7.0).all() and (lse[s.total:] == 7.0).all()
+
+
+def test_a_cache_past_32_bits(B):        # noqa: F811
+    """Blocks that lie more than 2^32 bytes from the first."""
+    blocks, heads, dim = (1 << 32) // (16 * 2 * 64) + 40, 2, 64
+    k, v = (torch.zeros((blocks, 16, heads, dim), dtype=torch.uint8, device=DEV) for _ in range(2))
+    k_scale, v_scale = (torch.ones((blocks, heads), device=DEV) for _ in range(2))
+    table = torch.tensor([[blocks - 1 - 3 * i for i in range(12)]], dtype=torch.int32, device=DEV)
+    rng = np.random.default_rng(75)
+    for c, scale in ((k, k_scale), (v, v_scale)):
+        c[table[0].long()] = torch.from_numpy(K.nearest_code(rng.normal(size=(12, 16, heads, dim)) * 60)).to(DEV)
+        scale[table[0].long()] = 2.0 ** -6
+    cache = B.KV8(k, v, k_scale, v_scale, table)
+    batch = B.KV8Batch(torch.tensor([185], dtype=torch.int32, device=DEV), max_len=192)
+    few = torch.arange(12, dtype=torch.int32, device=DEV)[None]                       # the same in a cache of its own
+    small = B.KV8(*(x[table[0].long()].contiguous() for x in (k, v, k_scale, v_scale)), few)
+    x = torch.from_numpy(rng.normal(size=(1, 12, dim))).to(BF16).to(DEV)
+    rot = B.KV8Rotary(_freq(dim).to(DEV))
+    prefix = B.KV8Prefix(torch.tensor([0, 1], dtype=torch.int32, device=DEV), torch.tensor([100], dtype=torch.int32, device=DEV), max_prefix=100)
+    got = []
+    for c in (cache, small):
+        q, blocks_dev, out, dense = torch.empty_like(x[:, :8]), torch.empty((1, heads, 5), dtype=torch.int32, device=DEV), torch.empty_like(x[:, :8]), torch.empty_like(x[:, :8])
+        bounds = torch.zeros((c.k.shape[0], heads, 2, dim), dtype=torch.uint8, device=DEV)
+        every = B.KV8Batch(batch.lens, starts=torch.tensor([0, 185], dtype=torch.int32, device=DEV), total_new=185, max_new=185, max_len=192)
+        B.kv8_append_rotated(c, batch, x[:, 8:10], x[:, 10:], rot, q=x[:, :8], q_out=q, stream=_stream())
+        B.kv8_bound(c, every, bounds, stream=_stream())
+        B.kv8_select(c, batch, bounds, q, blocks_dev, first=1, recent=1, stream=_stream())
+        B.kv8_attend_blocks(c, batch, blocks_dev, q, out, stream=_stream())
+        B.kv8_attend_shared(c, batch, prefix, q, dense, stream=_stream())
+        at = c.block_table[0].long()
+        got.append([q, blocks_dev, out, dense, c.k[at], c.v[at], c.k_scale[at], c.v_scale[at], bounds[at]])
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
