@@ -44,11 +44,14 @@ dmi_status_t check_attention(const dmi_kv8_t *cache, const dmi_kv8_batch_t *batc
 uint32_t most_rows(uint32_t dim) { return dim > 128u ? 16u : kFewRows; }
 
 // Splits of `tokens` for `units` pairs of request and head, by dmi_kv8_attend's rule: of 512 tokens while there are compute units for
-// them, of 1024 (2048 for many rows) in any case.
-uint32_t splits_of(uint64_t units, uint64_t tokens, uint32_t rows)
+// them, of 1024 (2048 for many rows) in any case.  None where a workgroup goes through them all in the time that a second launch takes to join
+// parts.  Measured over listed blocks (us, one / split): 4 pairs x 2048 tokens x 64 elements 13.7 / 18.9, 96 of them 17.3 / 19.6, 128 17.6 /
+// 22.6, 16 x 1536 x 128 15.4 / 18.8; 8 x 2048 x 128 17.8 / 19.1, 64 of them 23.3 / 19.5, 16 x 1536 x 256 23.4 / 19.0.
+uint32_t splits_of(uint64_t units, uint64_t tokens, uint32_t rows, uint32_t dim)
 {
     const uint64_t reach = rows > 16u ? 2048u : 1024u;
     uint64_t s = 1;
+    if (rows <= 16u && tokens * dim <= 3u << 16) return 1u;
     if (tokens > 1024u) s = std::max<uint64_t>(1u, std::min(256u / std::max<uint64_t>(units, 1u), (tokens + 511u) / 512u));
     if (tokens > reach * s) s = (tokens + reach - 1u) / reach;
     return (uint32_t)std::min<uint64_t>(s, 64u);
@@ -191,7 +194,7 @@ BlocksPlan plan_blocks(uint32_t heads, uint32_t dim, uint32_t block_size, const 
     t.tile_rows = group <= 16u ? 16u : 32u;
     t.row_tiles = 1u;
     // (the launch that joins parts has a token in each of its rows)
-    t.splits = b.total_new > 65535u ? 1u : splits_of((uint64_t)b.total_new * heads, blocks * block_size, group);
+    t.splits = b.total_new > 65535u ? 1u : splits_of((uint64_t)b.total_new * heads, blocks * block_size, group, dim);
     workgroups_of(t, b.total_new, heads);
     t.join_blocks = t.splits > 1u ? (q_heads + 3u) / 4u : 0u;
     const uint64_t parts = t.splits > 1u ? (uint64_t)b.total_new * q_heads * t.splits : 0u;
@@ -295,7 +298,7 @@ SharedSizes plan_shared(uint32_t heads, uint32_t dim, uint32_t block_size, const
         t.whole = true;
         t.tile_rows = shared <= 16u ? 16u : 32u;
         t.row_tiles = 1u;
-        t.splits = p.splits = splits_of((uint64_t)b.n_reqs * heads, behind, (uint32_t)shared);
+        t.splits = p.splits = splits_of((uint64_t)b.n_reqs * heads, behind, (uint32_t)shared, dim);
         workgroups_of(t, b.n_reqs, heads);
     } else {
         PartsPlan &m = p.many;
