@@ -67,7 +67,7 @@ struct RotateArgs {
     bool counted;                               // as in AppendArgs
     uint32_t tokens;                            // whose cosines are in LDS at a time
     uint32_t each, groups;                      // items of a workgroup, workgroups of a block
-    uint32_t q_each;                            // query heads of an item: about twice the rows that a wavefront asks for at once
+    uint32_t q_each, q_part;                    // tokens whose queries an item has; 2^32 / q_heads, rounded up
 };
 
 struct BoundArgs {

@@ -114,11 +114,11 @@ template <> __device__ __forceinline__ void store8<float>(float *p, const float 
     *reinterpret_cast<f32x4 *>(p + 4) = f32x4{x[4], x[5], x[6], x[7]};
 }
 
-constexpr uint32_t kMostHeads = 8;              // query heads that a wavefront takes at a time
 template <typename T> constexpr uint32_t kAheadOf = sizeof(T) == 4 ? 2 : 4;     // sixteens of queries that are asked for before the first is used
 constexpr uint32_t kTableBytes = 32768;         // cosines and sines in LDS: as many tokens as they are room for
 
-// A workgroup per block that new tokens reach and a.each of its items: K of a head, V of a head, queries of a.q_each heads.  Cosines and sines
+// A workgroup per block that new tokens reach and a.each of its items: K of a head, V of a head, queries of a.q_each tokens
+// (which lie in one piece).  Cosines and sines
 // of the block's tokens are computed once into LDS, in 64 bits (angles of far positions have no others), and every item takes them from
 // there; a wavefront has an item at a time, a lane the same sixteen of every few rows.  As in append_kernel the scale of K and V wants the
 // largest of all the block's new elements first; what a lane can hold of them it does.
@@ -132,7 +132,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void r
     const Reached x = reached_by(a.b, a.c, a.counted ? -1 : (int)blockIdx.y, blockIdx.x / a.groups);
     if (x.lo >= x.hi) return;
     const uint32_t half = a.rotary / 2u, per_row = a.c.dim / 16u, stored = 2u * a.c.heads;
-    const uint32_t items = stored + (a.q_heads + a.q_each - 1u) / a.q_each;
+    const uint32_t items = stored + (a.q_heads ? (a.tokens + a.q_each - 1u) / a.q_each : 0u);
     const uint32_t first_item = blockIdx.x % a.groups * a.each, last_item = min(first_item + a.each, items);
     const int first = x.q.len - x.q.fresh;      // the first new token's place
     const int entry = entry_of(a.c, x.q.row, (uint32_t)x.block);
@@ -244,12 +244,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void r
                         else put(t, v);
                     }
                 } else if (turns_q && pass == 0 && row < of_step) {
-                    const uint32_t head0 = (item - stored) * a.q_each, heads = min(a.q_each, a.q_heads - head0), rows = here * heads;
-                    const uint32_t share = (65536u + heads - 1u) / heads;       // (rows are few: a quotient by a product)
+                    const uint32_t token0 = (item - stored) * a.q_each, rows = token0 < here ? min(a.q_each, here - token0) * a.q_heads : 0u;
                     const int64_t at0 = x.q.start + x.lo - first + lo;
                     auto locate = [&](uint32_t r, uint32_t &t, uint32_t &h) {
-                        t = r * share >> 16;
-                        h = head0 + r - t * heads;
+                        t = a.q_heads == 1u ? r : __umulhi(r, a.q_part);
+                        h = r - t * a.q_heads;
+                        t += token0;
                     };
                     for (uint32_t r0 = row; r0 < rows; r0 += kAhead * of_step) {
                         Raw raw[kAhead];
@@ -309,8 +309,9 @@ hipError_t launch_rotate(RotateArgs a, uint32_t dtype, hipStream_t s)
     a.tokens = std::max(1u, std::min({a.c.bs, a.b.max_new, kTableBytes / (8u * half)}));
     // Few blocks: their items over more workgroups, each of which computes the block's cosines for itself.
     const uint32_t ahead = (dtype == DMI_DTYPE_FP32 ? kAheadOf<float> : kAheadOf<_Float16>) * (64u / (a.c.dim / 16u));
-    a.q_each = std::max(1u, std::min(kMostHeads, 2u * ahead / a.tokens));
-    const uint32_t items = 2u * a.c.heads + (a.q_heads + a.q_each - 1u) / a.q_each;
+    a.q_each = std::max(1u, 2u * ahead / std::max(1u, a.q_heads));
+    a.q_part = a.q_heads > 1u ? (uint32_t)(((1ull << 32) + a.q_heads - 1u) / a.q_heads) : 0u;
+    const uint32_t items = 2u * a.c.heads + (a.q_heads ? (a.tokens + a.q_each - 1u) / a.q_each : 0u);
     const uint64_t blocks = reach.blocks * reach.reqs;
     a.each = (uint32_t)std::min<uint64_t>((items + 3u) & ~3u, std::max<uint64_t>(4u, (blocks * items / 2048u + 3u) & ~3ull));
     a.groups = (items + a.each - 1u) / a.each;
