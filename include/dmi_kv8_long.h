@@ -38,7 +38,8 @@ typedef struct {
  * Writes the new tokens' K, rotated, and V into their places as dmi_kv8_append does (a rotated element is rounded to fp32, and from
  * there on is dmi_kv8_append's x).  With q, the new tokens' queries are rotated into q_out, rounded once to their type.
  *   q, q_out  [host, optional, both or neither] total_new rows of n_q_heads heads, of key's dtype.  q_out may be q, or share no element
- *             with q, key or value.  Rows of tokens that no request has are left as they were.  n_q_heads need not be a multiple of n_heads.
+ *             with q, key or value.  Rows of tokens that no request has, or whose place lies below 0, are left as they were.  n_q_heads need
+ *             not be a multiple of n_heads.
  */
 dmi_status_t dmi_kv8_append_rotated(const dmi_kv8_t *cache /*[host]*/, const dmi_kv8_batch_t *batch /*[host]*/,
                                     const dmi_kv8_heads_t *key /*[host]*/, const dmi_kv8_heads_t *value /*[host]*/,

@@ -116,7 +116,7 @@ extern "C" dmi_status_t dmi_kv8_attend(const dmi_kv8_t *cache, const dmi_kv8_bat
                                        const dmi_kv8_weight_t *weight, const dmi_kv8_weight_t *prior, float decay,
                                        void *workspace, uint64_t workspace_bytes, void *hip_stream)
 {
-    AttendArgs a;
+    AttendArgs a{};
     dmi_status_t st;
     if ((st = check_cache(cache, "cache", a.c)) != DMI_OK || (st = check_batch(batch, a.c, true, a.b)) != DMI_OK ||
         (st = check_rows(q, "q", a.b, a.q)) != DMI_OK || (st = check_rows(out, "out", a.b, a.out)) != DMI_OK ||

@@ -446,8 +446,8 @@ __global__ __launch_bounds__(N) __attribute__((amdgpu_waves_per_eu(DP <= 128 ? 4
     if (!lane) atomicAdd(&s.count[0], surely);
     __syncthreads();
     const uint32_t close = s.count[1], need = want - s.count[0];
-    if (close == need || (t == -INFINITY && off2 < INFINITY)) {
-        // all of those (where the want-th has no score: as many as are wanted, the lowest first)
+    if (close == need || off2 == 0.0f || (t == -INFINITY && off2 < INFINITY)) {
+        // all of those (where scores are exact, or the want-th has none: as many as are wanted, the lowest first)
         write_in_order<N>(s, count, x.lo, need, [&](uint32_t i) { return side(score(i)); }, to + a.n_first);
         return;
     }
