@@ -75,7 +75,8 @@ __device__ __forceinline__ Place place_of(uint32_t sixteen, uint32_t rotary, boo
     return {8u * sixteen, 8u * sixteen + rotary / 2u, (int)(8u * sixteen)};
 }
 
-// Eight pairs turned, in F: fp64 for K, whose scale and codes then hang on no order of operations, and fp32 for queries of 16 bits.
+// Eight pairs turned, in F: fp64 for K and for queries in fp32, whose codes and elements then hang on no order of operations, fp32 for
+// queries of 16 bits.
 template <typename F, bool NEIGHBOURS> __device__ __forceinline__ void turn(float (&x)[16], const float *cos, const float *sin)
 {
 #pragma unroll
@@ -117,11 +118,14 @@ template <> __device__ __forceinline__ void store8<float>(float *p, const float 
 template <typename T> constexpr uint32_t kAheadOf = sizeof(T) == 4 ? 2 : 4;     // sixteens of queries that are asked for before the first is used
 constexpr uint32_t kTableBytes = 32768;         // cosines and sines in LDS: as many tokens as they are room for
 
-// A workgroup per block that new tokens reach and a.each of its items: K of a head, V of a head, queries of a.q_each tokens
-// (which lie in one piece).  Cosines and sines
-// of the block's tokens are computed once into LDS, in 64 bits (angles of far positions have no others), and every item takes them from
-// there; a wavefront has an item at a time, a lane the same sixteen of every few rows.  As in append_kernel the scale of K and V wants the
-// largest of all the block's new elements first; what a lane can hold of them it does.
+// A workgroup per block that new tokens reach and a.each of its items: K of a head, V of a head, queries of a.q_each tokens (which lie in one
+// piece).  Cosines and sines of the block's tokens are computed once into LDS, in 64 bits (angles of far positions have no others), and every
+// item takes them from there; a wavefront has an item at a time, a lane the same sixteen of every few rows.  As in append_kernel the scale of K
+// and V wants the largest of all the block's new elements first; what a lane can hold of them it does.
+//
+// Bound by memory where there is much: 32 prompts, 38600 tokens, K and V of 8 heads x 128 and queries of 32 in bf16, 857 MB in 180 us (4.8 TB/s;
+// a copy reaches 5.2); single tokens by the chain of lengths, table, cosines, rows: 7.3 us.  Measured and not better for the prompts: one
+// sixteen of queries under way at a time 268, four wavefronts a SIMD (spills) 362, three sixteens of K or V held 205, queries by head 186.
 template <typename T, bool NEIGHBOURS>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void rotate_kernel(RotateArgs a)
 {
@@ -364,7 +368,9 @@ struct Extremes {
 };
 
 // A wavefront per block that new tokens reach and 64 places of its heads' rows, a lane 16 elements of every token (of every few, where the
-// heads have fewer places): what the wavefront reads of a token lies in one piece where heads follow each other.
+// heads have fewer places): what the wavefront reads of a token lies in one piece where heads follow each other, and no extreme has to cross
+// lanes.  Bound by memory where there is much: 32 prompts, 2400 blocks of 16 x 8 x 128, 40 MB in 10.5 us (3.8 TB/s; 21 us with a wavefront a
+// head, whose lanes shared a token's elements: vector instructions); single tokens of 128 requests 4.2 us, loads that wait for each other.
 __global__ __launch_bounds__(256) void bound_kernel(BoundArgs a)
 {
     const uint32_t lane = threadIdx.x & 63u, item = blockIdx.x * 4u + (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
