@@ -81,8 +81,9 @@ dmi_status_t dmi_kv8_select(const dmi_kv8_t *cache /*[host]*/, const dmi_kv8_bat
                             void *workspace, uint64_t workspace_bytes, void *hip_stream);
 
 /*
- * As dmi_kv8_attend, every new token by itself, over those tokens that it sees and that lie in the blocks listed for it and the head.  A
- * row of blocks_dev ends with its first entry below 0 and counts no more entries than the token sees blocks; blocks that are listed twice count twice.
+ * As dmi_kv8_attend, every new token by itself, over those tokens that it sees and that lie in the blocks listed for it and the head.  Of
+ * a row of blocks_dev as many entries are looked at as the token sees blocks; those below 0, and those behind the token's own block, stand for
+ * nothing, and a block that is listed twice counts twice.
  *   blocks_dev  [device] int32 [total_new][n_heads][n_select], as dmi_kv8_select writes it
  *   n_q_heads   up to 32 query heads read a head of the cache
  */

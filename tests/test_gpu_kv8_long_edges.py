@@ -1,0 +1,147 @@
+"""The operators for long contexts on the 8-bit KV cache at the edges of what they accept: scales far from each other, scales that are no
+powers of two, queries that are no numbers, no rows, the longest lists; against the definitions in 64 bits."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import _kv8 as K
+import _kv8_long as L
+from test_gpu_kv8 import B, BF16, DEV, FP16, FP32, Setup, _stream        # noqa: F401
+from test_gpu_kv8_edges import _bounds, _scales
+from test_gpu_kv8_long import Shared, _check_blocks, _check_rotated, _check_select, _check_shared, _lists
+
+pytestmark = pytest.mark.gpu
+
+
+def _same_prefixes(s):
+    """Requests' tables begin alike, so their scales do."""
+    assert (s.table[s.rows[0], 0] == s.table[s.rows[1], 0]).all()
+
+
+@pytest.mark.parametrize("groups,group,dim", [
+    ([(300, [(1, 310 + i) for i in range(5)])], 4, 64),                         # few rows, the prefix by tokens
+    ([(400, [(1, 405 + 9 * i) for i in range(30)])], 4, 128),                   # many rows, the prefix in parts
+    ([(190, [(1, 205 + 9 * i) for i in range(30)])], 4, 128),                   # and unsplit
+    ([(190, [(40, 250), (33, 300)])], 2, 128),                                  # unsplit under prompts
+    ([(100, [(2, 120), (1, 130)])], 4, 256), ([(300, [(50, 350), (3, 320)])], 2, 240)],
+    ids=["tokens", "parts", "unsplit", "prompts", "256", "parts240"])
+@pytest.mark.parametrize("dtype,kind", [(FP16, "spread"), (FP16, "far"), (FP16, "odd"), (BF16, "odd"), (BF16, "tiny"), (BF16, "wide")])
+def test_scales_of_v_behind_prefixes(B, groups, group, dim, dtype, kind):        # noqa: F811
+    s = Shared(B, 81, groups, 2, dim, 16)
+    _same_prefixes(s)
+    s.v_scale.copy_(_scales(s, kind, s.rng))
+    if kind == "odd":
+        s.k_scale.copy_(_scales(s, kind, s.rng))
+    qd, qn = s.values(2 * group, dtype, 1.3)
+    out, lse = torch.empty_like(qd), torch.empty(qd.shape[:2], device=DEV)
+    B.kv8_attend_shared(s.cache, s.batch, s.prefix, qd, out, lse=lse, stream=_stream())
+    (o, l, _), (do, dl, _) = _bounds(s, qn, dim ** -0.5, group, dtype)
+    K.near(lse.cpu().numpy(), l, dl, "lse")
+    K.near(out.float().cpu().numpy(), o, do, "out")
+
+
+@pytest.mark.parametrize("dim,length", [(64, 300), (128, 200), (256, 170), (64, 5000)])
+@pytest.mark.parametrize("dtype,kind", [(FP16, "spread"), (FP16, "far"), (FP16, "odd"), (BF16, "odd"), (BF16, "tiny"), (BF16, "wide")])
+def test_scales_of_v_in_listed_blocks(B, dim, length, dtype, kind):        # noqa: F811
+    """Lists of all blocks, the last ones first."""
+    s = Setup(B, 82, [(1, length), (1, 40)], 2, dim, 16)
+    s.v_scale.copy_(_scales(s, kind, s.rng))
+    if kind == "odd":
+        s.k_scale.copy_(_scales(s, kind, s.rng))
+    n = -(-length // 16)
+    lists = np.full((2, 2, n), -1, dtype=np.int32)
+    for r, (_, _, _, t) in enumerate(s.spans):
+        lists[r, :, :-(-t // 16)] = np.arange(-(-t // 16))[::-1]
+    qd, qn = s.values(8, dtype, 1.3)
+    out, lse = torch.empty_like(qd), torch.empty(qd.shape[:2], device=DEV)
+    B.kv8_attend_blocks(s.cache, s.batch, torch.from_numpy(lists).to(DEV), qd, out, lse=lse, stream=_stream())
+    (o, l, _), (do, dl, _) = _bounds(s, qn, dim ** -0.5, 4, dtype)
+    K.near(lse.cpu().numpy(), l, dl, "lse")
+    K.near(out.float().cpu().numpy(), o, do, "out")
+
+
+@pytest.mark.parametrize("kind", ["odd", "wide", "tiny"])
+def test_selections_by_scales_of_any_size(B, kind):        # noqa: F811
+    s = Setup(B, 83, [(1, 16 * 70), (2, 16 * 33)], 2, 64, 16)
+    s.k_scale.copy_(_scales(s, kind, s.rng))
+    _check_select(B, s, BF16, 3, 20, 1, 1)
+    _check_select(B, s, FP16, 3, 20, 1, 1)
+
+
+def test_rotated_into_blocks_whose_scale_is_no_power_of_two(B):        # noqa: F811
+    """Codes are nearest to quotients by the scale that a block has; none of those here lies within fp32's rounding of a border."""
+    s = Setup(B, 84, [(5, 21), (1, 4), (20, 45)], 2, 64, 16, fill=False)
+    held = s.rng.uniform(1, 2, s.k_scale.shape) * 2.0 ** s.rng.integers(-8, 2, s.k_scale.shape)
+    s.k_scale.copy_(torch.from_numpy(held.astype(np.float32)))
+    s.v_scale.copy_(torch.from_numpy(held[::-1].astype(np.float32).copy()))
+    _check_rotated(B, s, BF16, 4, 64, False)
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+@pytest.mark.parametrize("many", [False, True])
+def test_queries_that_are_no_numbers_spoil_no_others(B, bad, many):        # noqa: F811
+    """A query that is no number makes its own output none, and leaves those of other heads and requests alone."""
+    s = Shared(B, 85, [(190, [(1, 205 + 9 * i) for i in range(30 if many else 4)])], 2, 128, 16)
+    q, qn = s.values(8, BF16)
+    clean, spoiled = torch.empty_like(q), torch.empty_like(q)
+    B.kv8_attend_shared(s.cache, s.batch, s.prefix, q, clean, stream=_stream())
+    q[1, 3, 5] = bad
+    B.kv8_attend_shared(s.cache, s.batch, s.prefix, q, spoiled, stream=_stream())
+    assert spoiled[1, 3].isnan().any()
+    spoiled[1, 3] = clean[1, 3]
+    (o, _, _), (do, _, _) = K.attend(s.cpu(), s.spans, qn, 128 ** -0.5, 4, BF16)
+    K.near(spoiled.float().cpu().numpy(), o, do, "others")
+    blocks = torch.from_numpy(_lists(s, 8)).to(DEV)
+    B.kv8_attend_blocks(s.cache, s.batch, blocks, q, spoiled, stream=_stream())
+    assert spoiled[1, 3].isnan().any() and spoiled[0].isfinite().all() and spoiled[1, :3].isfinite().all() and spoiled[1, 4:].isfinite().all()
+
+
+def test_calls_without_rows(B):        # noqa: F811
+    """Requests none of which has a new token; a longest length of zero."""
+    s = Shared(B, 86, [(32, [(0, 50), (0, 60)])], 2, 64, 16)
+    q = torch.empty((0, 8, 64), dtype=BF16, device=DEV)
+    for total, most in ((0, 0), (0, 4)):
+        batch = B.KV8Batch(s.lens, starts=s.starts_dev, total_new=total, max_new=most, max_len=s.max_len)
+        B.kv8_attend_shared(s.cache, batch, s.prefix, q, q, stream=_stream())
+        B.kv8_attend_blocks(s.cache, batch, torch.empty((0, 2, 3), dtype=torch.int32, device=DEV), q, q, stream=_stream())
+    one = B.KV8Batch(s.lens, max_len=0)
+    q, out, lse = torch.ones((2, 8, 64), dtype=BF16, device=DEV), torch.full((2, 8, 64), 7.0, dtype=BF16, device=DEV), torch.zeros(2, 8, device=DEV)
+    bounds, blocks = torch.zeros((s.k.shape[0], 2, 2, 64), dtype=torch.uint8, device=DEV), torch.zeros((2, 2, 3), dtype=torch.int32, device=DEV)
+    before = s.k.clone()
+    B.kv8_append_rotated(s.cache, one, q[:, :2], q[:, :2], B.KV8Rotary(torch.ones(32, device=DEV)), q=q, q_out=out, stream=_stream())
+    assert (out == 7.0).all() and torch.equal(before, s.k)
+    B.kv8_bound(s.cache, one, bounds, stream=_stream())
+    B.kv8_select(s.cache, one, bounds, q, blocks, stream=_stream())
+    assert (bounds == 0).all() and (blocks == -1).all()
+    for call in (lambda: B.kv8_attend_blocks(s.cache, one, blocks, q, out, lse=lse, stream=_stream()),
+                 lambda: B.kv8_attend_shared(s.cache, one, s.prefix, q, out, lse=lse, stream=_stream())):
+        out.fill_(7.0)
+        call()
+        assert (out == 0.0).all() and (lse == -math.inf).all()
+
+
+def test_one_block_of_everything(B):        # noqa: F811
+    """A context of one token and one block, lists and prefixes of one."""
+    s = Shared(B, 87, [(1, [(1, 2), (1, 2)])], 1, 16, 16)
+    _check_shared(B, s, BF16, 1)
+    _check_blocks(B, s, BF16, 1, np.zeros((2, 1, 1), dtype=np.int32))
+    _check_select(B, s, BF16, 1, 1, 0, 1)
+    s = Setup(B, 88, [(1, 1)], 1, 16, 16, fill=False)
+    _check_rotated(B, s, FP32, 1, 16, True)
+
+
+def test_more_query_heads_than_a_tile(B):        # noqa: F811
+    """37 query heads share one: several tiles of rows in prefixes and rests, several sets of rows in selections."""
+    s = Shared(B, 89, [(100, [(1, 110 + i) for i in range(4)])], 2, 64, 16)
+    _check_shared(B, s, BF16, 37)
+    s = Setup(B, 90, [(1, 16 * 40), (2, 16 * 21)], 2, 64, 16)
+    _check_select(B, s, BF16, 37, 12, 1, 1)
+
+
+def test_positions_behind_an_eviction(B):        # noqa: F811
+    """Places behind positions, as dmi_kv8_evict leaves them."""
+    s = Setup(B, 91, [(1, 120), (1, 90)], 2, 64, 16, fill=False)
+    at = [5000, 70000]
+    _check_rotated(B, s, BF16, 4, 64, False, positions=at)
