@@ -494,14 +494,20 @@ __global__ __launch_bounds__(N) __attribute__((amdgpu_waves_per_eu(DP <= 128 ? 4
 
 template <typename T, int DP> static hipError_t select(const SelectArgs &a, hipStream_t s)
 {
-    constexpr uint32_t kFew = 256, kMany = DP <= 128 ? 1024 : 512;
+    constexpr uint32_t kMany = DP <= 128 ? 1024 : 512;
     const uint64_t items = (uint64_t)a.b.total_new * a.c.heads, per = (a.stride + kBlocksAtOnce - 1u) / kBlocksAtOnce;
-    // One launch where tokens and heads give every compute unit a workgroup, or there are few blocks; scores over more workgroups otherwise.
-    const bool fused = a.stride <= kMostInLds && (items >= 256u || a.stride <= 4u * kBlocksAtOnce);
+    // One launch where a workgroup goes through a head's blocks in the time that a second one takes, or there are workgroups enough; scores
+    // over more workgroups otherwise.  Measured (us, one launch / two; tokens x heads, blocks): 8, 500 15 / 19, 128, 500 15 / 20, 8, 2000 27 / 20,
+    // 128, 2000 29 / 31, 256, 2000 34 / 47, 512, 2000 73 / 95, 8, 7000 72 / 23, 128, 7000 98 / 81.
+    const bool fused = a.stride <= kMostInLds && (a.stride <= 1024u || items >= a.stride / 16u);
     if (!launchable(items + 8u * a.c.heads, kMany) || !launchable(items * per, kScoreThreads)) return hipErrorInvalidConfiguration;
     const uint32_t lds = a.stride > a.n_select && a.stride <= kMostInLds ? a.stride * 4u : 0u;
     if (fused) {
-        pick_kernel<T, DP, true, kFew><<<(a.b.total_new + 7u) / 8u * 8u * a.c.heads, kFew, lds, s>>>(a);
+        // Workgroups of eight wavefronts while all of them are resident, of four beyond (us, four / eight: 256, 500 18 / 16, 512, 500 22 / 22, 1024 of
+        // up to 512 27 / 32).
+        const uint32_t groups = (a.b.total_new + 7u) / 8u * 8u * a.c.heads;
+        if (items <= 512u) pick_kernel<T, DP, true, 512><<<groups, 512, lds, s>>>(a);
+        else pick_kernel<T, DP, true, 256><<<groups, 256, lds, s>>>(a);
         return hipGetLastError();
     }
     if (a.stride > a.n_select) {
