@@ -126,7 +126,7 @@ struct TokensPlan {
     uint32_t splits;
     uint32_t ranges;                            // equal parts of all contexts
     uint32_t waves;                             // of a workgroup, not kWhole: 4 or 8
-    bool by_xcd;                                // the heads of a request on one XCD, not kWhole
+    bool by_xcd;                                // kPrefix: what reads the same codes on one XCD
     uint32_t tile_rows, row_tiles;              // query rows of a wavefront; wavefronts for the rows that share a head
     uint32_t join_blocks;                       // workgroups of the second launch that join parts, 0 if there can be none
     uint32_t score_stride;

@@ -46,7 +46,8 @@ __device__ __forceinline__ Reached reached_by(const Batch &b, const Cache &c, in
     return x;
 }
 
-// How many of them a launch is made for, for every request or for all; the rule is launch_append's.
+// How many of them a launch is made for, for every request or for all; the rule is launch_append's (a prompt of 8192 tokens among 63 single
+// ones, for every request / counted: rotated 62.9 / 48.1 us, bounds 9.0 / 8.6).
 struct Reach {
     uint64_t blocks;
     uint32_t reqs;

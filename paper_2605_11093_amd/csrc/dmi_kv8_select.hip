@@ -322,7 +322,7 @@ __global__ __launch_bounds__(N) __attribute__((amdgpu_waves_per_eu(DP <= 128 ? 4
     extern __shared__ float own[];              // scores
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = (uint32_t)__builtin_amdgcn_readfirstlane(tid >> 6);
     // Workgroups go to the eight XCDs in turn: with FUSED the heads of a token follow each other on one of them, whose scales of a block
-    // lie in one line.
+    // lie in one line (128 tokens 27.8 us, 29.2 without).
     uint32_t token, head;
     if constexpr (FUSED) {
         const uint32_t nth = blockIdx.x >> 3;

@@ -88,19 +88,13 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
         uint32_t pair = blockIdx.x / p.splits;
         range = (int)(blockIdx.x - pair * p.splits);
         if constexpr (KIND == kPrefix) {
-            // all row tiles and splits of a group and head on one XCD, whose cache its codes go through once
+            // all row tiles and splits of a group and head on one XCD, whose cache its codes go through once (workgroups go to the eight in turn;
+            // 24 requests in four groups 20.9 us, 21.9 without)
             const uint32_t each = p.row_tiles * p.splits, nth = p.by_xcd ? blockIdx.x >> 3 : blockIdx.x, which = nth / each, inner = nth - which * each;
             pair = p.by_xcd ? 8u * which + (blockIdx.x & 7u) : which;
             row_tile = inner / p.splits;
             range = (int)(inner - row_tile * p.splits);
             if (pair >= a.n_groups * a.c.heads) return;
-        } else if (KIND != kWhole && p.by_xcd) {
-            // workgroups go to the eight XCDs in turn: the heads of a request on one of them, whose scales of a block lie in one line
-            const uint32_t nth = blockIdx.x >> 3, each = a.c.heads * p.splits, eighth = nth / each;
-            pair = (nth - eighth * each) / p.splits;
-            range = (int)(nth - eighth * each - pair * p.splits);
-            pair += (8u * eighth + (blockIdx.x & 7u)) * a.c.heads;
-            if (pair >= (KIND == kListed ? a.b.total_new : a.b.n_reqs) * a.c.heads) return;
         }
         r = (int)(pair / a.c.heads);
         head = pair % a.c.heads;
@@ -859,8 +853,7 @@ template <typename T, Kind KIND> static hipError_t tokens_apart(const AttendArgs
 {
     const uint32_t units = KIND == kListed ? a.b.total_new : KIND == kPrefix ? a.n_groups : a.b.n_reqs;
     const uint64_t pairs = (uint64_t)units * a.c.heads;
-    const uint64_t groups = KIND == kPrefix ? (p.by_xcd ? (pairs + 7u) / 8u * 8u : pairs) * p.row_tiles * p.splits
-                                            : (uint64_t)(p.by_xcd ? (units + 7u) / 8u * 8u : units) * a.c.heads * p.splits;
+    const uint64_t groups = (KIND != kPrefix ? pairs : (p.by_xcd ? (pairs + 7u) / 8u * 8u : pairs) * p.row_tiles) * p.splits;
     if (!launchable(groups, 512) || pairs > UINT32_MAX) return hipErrorInvalidConfiguration;
     auto launch = [&](auto dp_, auto nt_) {
         constexpr int DP = decltype(dp_)::value, NT = decltype(nt_)::value, many = waves_of(DP, NT, true);
