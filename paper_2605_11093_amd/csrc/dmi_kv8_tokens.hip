@@ -450,7 +450,7 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
 
         if constexpr (WHOLE) {
             // the wavefronts' sums, relative to the largest score of all; the later half of them hand theirs to the others
-            constexpr int kSlots = NW / 2;
+            constexpr int kSlots = (NW + 1) / 2;
             __shared__ f32x4 joined[kSlots][NT * NJ * 64];
             __shared__ float tops[NW][16 * NT], sums[NW][16 * NT];
 #pragma unroll
@@ -488,7 +488,10 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
 #pragma unroll
                 for (int n = 0; n < NT; n++)
 #pragma unroll
-                    for (int j = 0; j < NJ; j++) joined[wave][(n * NJ + j) * 64 + lane] += o[n][j];
+                    for (int j = 0; j < NJ; j++) {
+                        f32x4 &to = joined[wave][(n * NJ + j) * 64 + lane];
+                        to = NW == 1 ? o[n][j] : to + o[n][j];
+                    }
             }
             __syncthreads();
             if constexpr (KIND == kRest) {
@@ -857,9 +860,14 @@ template <typename T, Kind KIND> static hipError_t tokens_apart(const AttendArgs
     if (!launchable(groups, 512) || pairs > UINT32_MAX) return hipErrorInvalidConfiguration;
     auto launch = [&](auto dp_, auto nt_) {
         constexpr int DP = decltype(dp_)::value, NT = decltype(nt_)::value, many = waves_of(DP, NT, true);
-        if (p.waves == 4u || many == 4) tokens_kernel<T, DP, NT, true, KIND, 4><<<(uint32_t)groups, 256, 0, s>>>(a, p);
-        else tokens_kernel<T, DP, NT, true, KIND, many><<<(uint32_t)groups, 64 * many, 0, s>>>(a, p);
-        return hipGetLastError();
+        auto with = [&](auto waves) {
+            constexpr int NW = decltype(waves)::value;
+            tokens_kernel<T, DP, NT, true, KIND, NW><<<(uint32_t)groups, 64 * NW, 0, s>>>(a, p);
+            return hipGetLastError();
+        };
+        if constexpr (KIND == kListed)
+            if (p.waves == 1u) return with(Int<1>{});
+        return p.waves == 4u || many == 4 ? with(Int<4>{}) : with(Int<many>{});
     };
     const int dp = a.c.dim <= 64 ? 64 : a.c.dim <= 128 ? 128 : 256;
     hipError_t e;

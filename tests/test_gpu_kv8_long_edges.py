@@ -145,3 +145,14 @@ def test_positions_behind_an_eviction(B):        # noqa: F811
     s = Setup(B, 91, [(1, 120), (1, 90)], 2, 64, 16, fill=False)
     at = [5000, 70000]
     _check_rotated(B, s, BF16, 4, 64, False, positions=at)
+
+
+@pytest.mark.parametrize("dtype,heads,group,dim,new,kind", [
+    (BF16, 16, 4, 128, 1, "spread"), (FP16, 16, 16, 64, 1, "far"), (BF16, 16, 20, 128, 50, "spread"), (FP16, 13, 1, 256, 60, "odd"), (BF16, 16, 32, 80, 50, "tiny")])
+def test_lists_of_a_wavefront_each(B, dtype, heads, group, dim, new, kind):        # noqa: F811
+    """Many short lists, of one block to all, each gone through by one wavefront."""
+    spans = [(1, 17 + 3 * i % 150) for i in range(60)] if new == 1 else [(new, new + 40), (2, 7)]
+    s = Setup(B, 92, spans, heads, dim, 16)
+    s.v_scale.copy_(_scales(s, kind, s.rng))
+    assert s.total * heads >= 768
+    _check_blocks(B, s, dtype, group, _lists(s, 5))
