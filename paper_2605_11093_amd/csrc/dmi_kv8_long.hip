@@ -297,9 +297,9 @@ SharedSizes plan_shared(uint32_t heads, uint32_t dim, uint32_t block_size, const
     }
     p.tokens = shared <= most_rows(dim);
     p.splits = 1u;
+    const uint32_t behind = b.max_len - std::min(b.max_len, p.prefix.splits ? prefix : 0u);
     if (p.tokens) {
         TokensPlan &t = p.few;
-        const uint32_t behind = b.max_len - std::min(b.max_len, p.prefix.splits ? prefix : 0u);
         t.whole = true;
         t.tile_rows = shared <= 16u ? 16u : 32u;
         t.row_tiles = 1u;
@@ -308,8 +308,22 @@ SharedSizes plan_shared(uint32_t heads, uint32_t dim, uint32_t block_size, const
     } else {
         PartsPlan &m = p.many;
         m.row_tiles = (uint32_t)((shared + rows_each - 1u) / rows_each);
-        m.splits = 1u;
-        m.chunk = std::max(64u, (b.max_len + 63u) & ~63u);
+        // Splits as for prefixes; without any, and with an unsplit prefix, no part is written.  (Requests that share less have more behind it than
+        // is counted for here, and more splits of the same length.)  Measured (us, the whole call,
+        // unsplit / so; 8 heads x 128, 32 query heads): 8 requests of 16 new tokens, 4000 behind prefixes of 2000, 116 / 58, 8000 behind 175 / 78; two of 64 and
+        // 8000 257 / 57; one of 40 and 20000, 2 heads, 566 / 66; one head of 256 and 7 query heads, 4 x 6 and 1400 99 / 34; 4 x 256 and 2000 168 / 172.
+        const uint64_t groups = std::min((uint64_t)b.n_reqs * m.row_tiles, (uint64_t)b.total_new * group / rows_each + b.n_reqs / 2u + 1u) * heads;
+        const uint64_t tiles = (behind + 63u) / 64u;
+        const bool last = !p.few_rows && p.prefix.splits == 1u;
+        double best = INFINITY;
+        for (uint32_t s = 1; s <= 16u && (s == 1u || s * 128u <= behind); s++) {
+            const double parts = last && s == 1u ? 0.0 : (double)rows * (s + (last ? 1u : 0u)) * dim * 8.0 / 4e6;
+            const double cost = (double)((groups * s + 255u) / 256u) * (double)((tiles + s - 1u) / s + 3u) * 2.5 + parts;
+            if (cost < best) best = cost, m.splits = s;
+        }
+        const uint32_t length = m.splits > 1u ? std::max((behind + m.splits - 1u) / m.splits, b.max_len / 16u) : b.max_len;
+        m.chunk = std::max(64u, (length + 63u) & ~63u);
+        m.splits = p.splits = std::max(1u, (b.max_len + m.chunk - 1u) / m.chunk);
     }
     // Nothing split: the sums of what is behind the prefix are where the prefix begins, and its end writes outputs (32 prompts behind 4000
     // tokens 753 us; 810 with a part of every row more to write, and two to read).

@@ -873,7 +873,12 @@ __global__ __launch_bounds__(256) void join_shared_kernel(AttendArgs a, SharedPl
             }
         };
         add(p.prefix.sums + at * p.prefix.splits, p.prefix.parts + at * p.prefix.splits * a.c.dim, before);
-        add(p.sums + at * p.splits, p.parts + at * p.splits * a.c.dim, (int)p.splits);
+        int behind = (int)p.splits;
+        if (!p.tokens) {                        // splits that the row's workgroup had work in, as in join_parts_kernel
+            const uint32_t tile_rows = a.c.dim <= 128u ? 256u : 128u, last_row = min((row / tile_rows + 1u) * tile_rows, rows) - 1u;
+            behind = max(1, (q.len - shared - q.fresh + (int)(last_row / a.group) + (int)p.many.chunk) / (int)p.many.chunk);
+        }
+        add(p.sums + at * p.splits, p.parts + at * p.splits * a.c.dim, behind);
         const bool empty = m == -INFINITY && l == 0.0f;
         o *= empty ? 0.0f : 1.0f / l;
         uint16_t *dst = static_cast<uint16_t *>(a.out.data) + (int64_t)(q.start + w.token) * a.out.row_stride + (int64_t)w.head * a.out.head_stride + 4u * lane;

@@ -156,3 +156,11 @@ def test_lists_of_a_wavefront_each(B, dtype, heads, group, dim, new, kind):     
     s.v_scale.copy_(_scales(s, kind, s.rng))
     assert s.total * heads >= 768
     _check_blocks(B, s, dtype, group, _lists(s, 5))
+
+
+@pytest.mark.parametrize("dtype,heads,group,dim", [(BF16, 1, 7, 256), (FP16, 2, 4, 128), (BF16, 1, 24, 64), (FP16, 1, 5, 80)])
+@pytest.mark.parametrize("shared,lens", [(50, (900, 1471, 300)), (0, (2000, 64, 1)), (1000, (1010, 2900, 1700))])
+def test_many_rows_in_front_of_long_rests_of_unequal_length(B, dtype, heads, group, dim, shared, lens):        # noqa: F811
+    """More rows than a tile a head, contexts behind the prefixes (and those of requests without one) in splits that not every request reaches."""
+    s = Shared(B, 93, [(shared, [(12, n + 12) for n in lens]), (48, [(1, 60), (9, 700)])], heads, dim, 16, alone=(1, 1))
+    _check_shared(B, s, dtype, group)
