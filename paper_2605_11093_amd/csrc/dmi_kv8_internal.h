@@ -90,6 +90,7 @@ struct SelectArgs {
     f32x2 *scores;                              // [new token][head][stride]: a score, how far it may be off
     uint64_t *keys;                             // the same places: scores in 64 bits, as unsigned numbers in their order
     int32_t *blocks;
+    uint32_t several;                           // tokens that a pass over the bounds is for
 };
 
 struct AttendArgs {
@@ -200,9 +201,9 @@ __device__ __forceinline__ Request request_of(const Batch &b, const Cache &c, in
     return q;
 }
 
-// A new token as a request of its own, with a length of what it sees: the last request whose rows begin at or in front of it, if the
-// token is one of that request's.  64 places at a time are looked at, so 65535 requests take three trips to memory.
-__device__ __forceinline__ Request token_of(const Batch &b, const Cache &c, int token)
+// The last request whose rows begin at a token or in front of it.  64 places at a time are looked at, so 65535 requests take three trips to
+// memory.
+__device__ __forceinline__ Request request_with(const Batch &b, const Cache &c, int token)
 {
     int r = token;
     if (b.starts) {
@@ -215,7 +216,12 @@ __device__ __forceinline__ Request token_of(const Batch &b, const Cache &c, int 
             n = min(step, n - (k - 1) * step);
         }
     }
-    const Request q = request_of(b, c, min(r, (int)b.n_reqs - 1));
+    return request_of(b, c, min(r, (int)b.n_reqs - 1));
+}
+// A new token as a request of its own, with a length of what it sees, if it is one of that request's
+__device__ __forceinline__ Request token_of(const Batch &b, const Cache &c, int token)
+{
+    const Request q = request_with(b, c, token);
     const int nth = token - q.start;
     return {q.row, min(q.len, max(0, q.len - q.fresh + nth + 1)), token, nth >= 0 && nth < q.fresh ? 1 : 0};
 }

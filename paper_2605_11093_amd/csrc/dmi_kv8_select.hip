@@ -43,6 +43,17 @@ __device__ __forceinline__ float largest_of_16(float x)
     return fmaxf(x, turned(x, Int<1>{}));
 }
 
+// Largest of what `each` neighbours have, 1 to 16 (a power of two)
+__device__ __forceinline__ float largest_of(float x, uint32_t each)
+{
+    auto other = [](float v, auto how) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(how)::value, 0xF, 0xF, false)); };
+    if (each > 1u) x = fmaxf(x, other(x, Int<0xB1>{}));         // the one beside it
+    if (each > 2u) x = fmaxf(x, other(x, Int<0x4E>{}));         // two further
+    if (each > 4u) x = fmaxf(x, other(x, Int<0x141>{}));        // eight, mirrored
+    if (each > 8u) x = fmaxf(x, other(x, Int<0x140>{}));        // sixteen
+    return x;
+}
+
 // ---------------------------------------------------------------- scores, nearly
 // The larger of q x least and q x largest is one product with the one or the other, by q's sign: a score is the product of a row (q where
 // it is negative; q where it is positive) with a column (least; largest), and matrix instructions take it, 16 blocks x 16 query rows at a
@@ -64,10 +75,10 @@ template <typename T, int DP> struct Scorer {
     __device__ __forceinline__ Scorer(const SelectArgs &a_, const Request &q_, uint32_t token_, uint32_t head_)
         : a(a_), q(q_), token(token_), head(head_), lane(threadIdx.x & 63), col(lane & 15), g(lane >> 4), off(0.0f) {}
 
-    __device__ __forceinline__ void rows(uint32_t row0)
+    // A column's query row, of token t; how far its scores may be off
+    __device__ __forceinline__ float column(uint32_t t, uint32_t row)
     {
-        const uint32_t row = min(row0 + (uint32_t)col, a.group - 1u);
-        const uint16_t *const src = static_cast<const uint16_t *>(a.q.data) + (int64_t)token * a.q.row_stride + (int64_t)(head * a.group + row) * a.q.head_stride;
+        const uint16_t *const src = static_cast<const uint16_t *>(a.q.data) + (int64_t)t * a.q.row_stride + (int64_t)(head * a.group + row) * a.q.head_stride;
         float sum = 0.0f, faint = 0.0f;
 #pragma unroll
         for (int k = 0; k < KK; k++) {
@@ -88,9 +99,9 @@ template <typename T, int DP> struct Scorer {
         sum += __shfl_xor(sum, 16), faint += __shfl_xor(faint, 16);
         sum += __shfl_xor(sum, 32), faint += __shfl_xor(faint, 32);
         // (of nothing but zeros every score is 0 or no number, and that is exact)
-        const float most = sum == 0.0f ? 0.0f : sum > 0x1p-90f && sum < 0x1p+100f ? 448.0f * ((float)(2 * DP + 16) * 0x1p-23f * sum + 1.001f * faint) : INFINITY;
-        off = fmaxf(off, largest_of_16(most));
+        return sum == 0.0f ? 0.0f : sum > 0x1p-90f && sum < 0x1p+100f ? 448.0f * ((float)(2 * DP + 16) * 0x1p-23f * sum + 1.001f * faint) : INFINITY;
     }
+    __device__ __forceinline__ void rows(uint32_t row0) { off = fmaxf(off, largest_of_16(column(token, min(row0 + (uint32_t)col, a.group - 1u)))); }
     struct Tile {
         u32x4 low[KL], high[KL];
         float scale;
@@ -111,9 +122,8 @@ template <typename T, int DP> struct Scorer {
         if (mine < 0) x.scale = 0.0f;
         return x;
     }
-    // The largest score of block 4 g + (col & 3) by these rows (rows behind the group's last are that one again).  INFINITY says that one is
-    // no number.
-    __device__ __forceinline__ float of(const Tile &x) const
+    // Scores of blocks 4 g + 0..3 by the column's row
+    __device__ __forceinline__ f32x4 products(const Tile &x) const
     {
         f32x4 z = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
@@ -123,6 +133,13 @@ template <typename T, int DP> struct Scorer {
             z = T::mfma16(u32x4{T::two_codes(l0, false), T::two_codes(l0, true), T::two_codes(l1, false), T::two_codes(l1, true)}, below[k], z);
             z = T::mfma16(u32x4{T::two_codes(h0, false), T::two_codes(h0, true), T::two_codes(h1, false), T::two_codes(h1, true)}, above[k], z);
         }
+        return z;
+    }
+    // The largest score of block 4 g + (col & 3) by these rows (rows behind the group's last are that one again).  INFINITY says that one is
+    // no number.
+    __device__ __forceinline__ float of(const Tile &x) const
+    {
+        const f32x4 z = products(x);
         float best = 0.0f;
 #pragma unroll
         for (int i = 0; i < 4; i++) {
@@ -198,6 +215,7 @@ struct PickShared {
     float wave_x[16][3];
     uint32_t close[kClose];
     uint64_t order[kClose];
+    uint32_t off[16];                           // several tokens: how far their scores may be off, as numbers of fp32
 };
 
 // The bin that holds the rank-th of those counted, from the largest bin down: found = bin, rank in it, how many it has.
@@ -306,98 +324,15 @@ template <typename T, int DP> __global__ __launch_bounds__(kScoreThreads) __attr
     }
 }
 
-// N threads per new token and head.  Scores in fp32 (made here, FUSED; else score_kernel has left them in memory), of which LDS holds as many
-// as it has room for; which of 2048 even steps between the least and the largest the want-th largest lies in, and which it is of those;
-// what lies nearer to it than the scores' error once more in 64 bits; then the blocks in order.  Which blocks are taken hangs on no rounding
-// but of the 64 bits, and on no order of sums.
-//
-// 128 tokens over 512-8192 tokens in blocks of 16, 8 heads x 128: 74 MB of bounds in 27 us.  4.5 go by until the lengths are there, 18 to the
-// last score (4.1 TB/s, in pieces of 256 bytes from all over; the arithmetic takes 5 beside that), 5 from there on.  Scores in 64 bits throughout
-// took 47 us and 8 for the choice (the queries came out of LDS), digits of 11 bits for the choice 8 us more than even steps do, 512 threads 32.
-// Four contexts of 60000-120000 tokens, 4 heads x 64: scores 6.8 us, choice 14.5, of which 64 bits 4 (three loads that wait for each other).
-template <typename T, int DP, bool FUSED, uint32_t N>
-__global__ __launch_bounds__(N) __attribute__((amdgpu_waves_per_eu(DP <= 128 ? 4 : 2))) void pick_kernel(SelectArgs a)
+// The choice out of scores, in LDS or in memory; off, most and least as the thread has seen them
+template <typename T, uint32_t N>
+__device__ __forceinline__ void choose(PickShared &s, const SelectArgs &a, const Request &q, uint32_t token, uint32_t head, const Choice &x, float *own,
+                                       bool in_lds, float off, float most, float least)
 {
-    __shared__ PickShared s;
-    extern __shared__ float own[];              // scores
-    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = (uint32_t)__builtin_amdgcn_readfirstlane(tid >> 6);
-    // Workgroups go to the eight XCDs in turn: with FUSED the heads of a token follow each other on one of them, whose scales of a block
-    // lie in one line (128 tokens 27.8 us, 29.2 without).
-    uint32_t token, head;
-    if constexpr (FUSED) {
-        const uint32_t nth = blockIdx.x >> 3;
-        token = nth / a.c.heads, head = nth - token * a.c.heads;
-        token = 8u * token + (blockIdx.x & 7u);
-        if (token >= a.b.total_new) return;
-    } else {
-        token = blockIdx.x / a.c.heads, head = blockIdx.x - token * a.c.heads;
-    }
-    const uint32_t item = token * a.c.heads + head;
-    const Request q = token_of(a.b, a.c, (int)token);
-    if (q.fresh <= 0) return;                   // no request's
-    const Choice x = choice_of(a, q);
-    int32_t *const to = a.blocks + (int64_t)item * a.n_select;
-    if (x.seen <= a.n_select) {
-        for (uint32_t i = tid; i < a.n_select; i += N) to[i] = i < x.seen ? (int32_t)i : -1;
-        return;
-    }
+    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = (uint32_t)__builtin_amdgcn_readfirstlane(tid >> 6), item = token * a.c.heads + head;
     const uint32_t want = a.n_select - a.n_first - a.n_recent, count = x.hi - x.lo;
-    for (uint32_t i = tid; i < a.n_first; i += N) to[i] = (int32_t)i;
-    for (uint32_t i = tid; i < a.n_recent; i += N) to[a.n_first + want + i] = (int32_t)(x.hi + i);
-    if (!want) return;
+    int32_t *const to = a.blocks + (int64_t)item * a.n_select;
     f32x2 *const left = a.scores + (int64_t)item * a.stride + x.lo;
-    const bool in_lds = FUSED || a.stride <= kMostInLds;
-    for (uint32_t i = tid; i < kPickBins; i += N) s.hist[i] = 0;
-    if (tid < 3u) s.count[tid] = 0;
-    // how far the scores may be off, the least and the largest of them
-    float off = 0.0f, least = INFINITY, most = -INFINITY;
-    auto look = [&](float v) { most = fmaxf(most, v), least = fminf(least, v == -INFINITY ? INFINITY : v); };
-    if constexpr (FUSED) {
-        Scorer<T, DP> scorer(a, q, token, head);
-        // where all blocks lie first, in the scores' places
-        for (uint32_t i = tid; i < count; i += N) own[i] = __int_as_float(entry_of(a.c, q.row, x.lo + i));
-        for (uint32_t row0 = 0; row0 < a.group; row0 += 16u) {
-            scorer.rows(row0);
-            if (!row0) __syncthreads();
-            uint32_t base = 16u * wave;
-            if (base >= count) break;
-            auto entries = [&](uint32_t from) {
-                return [&, from](uint32_t i) {
-                    i += from;
-                    return i >= count ? -1 : row0 ? entry_of(a.c, q.row, x.lo + i) : __float_as_int(own[i]);
-                };
-            };
-            auto tile = scorer.fetch(entries(base));
-            for (;;) {
-                const auto here = tile;
-                const uint32_t next = base + N / 4u;
-                if (next < count) tile = scorer.fetch(entries(next));
-                float v = scorer.of(here);
-                off = fmaxf(off, scorer.off * here.scale);      // (no number where there is no block and no bound: left out)
-                const uint32_t i = base + 4u * (uint32_t)scorer.g + (uint32_t)scorer.col;
-                if (scorer.col < 4 && i < count) {
-                    if (row0) v = fmaxf(v, own[i]);
-                    if (row0 + 16u >= a.group) v = counted(v, here.scale), look(v);
-                    own[i] = v;
-                }
-                if (next >= count) break;
-                base = next;
-            }
-        }
-    } else {
-        constexpr uint32_t kAhead = 8;
-        for (uint32_t i0 = tid; i0 < count; i0 += kAhead * N) {
-            f32x2 v[kAhead];
-#pragma unroll
-            for (uint32_t k = 0; k < kAhead; k++) v[k] = left[min(i0 + k * N, count - 1u)];
-#pragma unroll
-            for (uint32_t k = 0; k < kAhead; k++) {
-                off = fmaxf(off, v[k][1]);
-                look(v[k][0]);
-                if (in_lds && i0 + k * N < count) own[i0 + k * N] = v[k][0];
-            }
-        }
-    }
 #pragma unroll
     for (int m = 32; m; m >>= 1) off = fmaxf(off, __shfl_xor(off, m)), most = fmaxf(most, __shfl_xor(most, m)), least = fminf(least, __shfl_xor(least, m));
     if (!lane) s.wave_x[wave][0] = off, s.wave_x[wave][1] = most, s.wave_x[wave][2] = least;
@@ -492,7 +427,198 @@ __global__ __launch_bounds__(N) __attribute__((amdgpu_waves_per_eu(DP <= 128 ? 4
     write_in_order<N>(s, count, x.lo, rank, [&](uint32_t i) { const uint64_t k = keys[i] >> shift; return k > prefix ? 1 : k == prefix ? 0 : -1; }, to + a.n_first);
 }
 
-template <typename T, int DP> static hipError_t select(const SelectArgs &a, hipStream_t s)
+// N threads per new token and head.  Scores in fp32 (made here, FUSED; else score_kernel has left them in memory), of which LDS holds as many
+// as it has room for; which of 2048 even steps between the least and the largest the want-th largest lies in, and which it is of those;
+// what lies nearer to it than the scores' error once more in 64 bits; then the blocks in order.  Which blocks are taken hangs on no rounding
+// but of the 64 bits, and on no order of sums.
+//
+// 128 tokens over 512-8192 tokens in blocks of 16, 8 heads x 128: 74 MB of bounds in 27 us.  4.5 go by until the lengths are there, 18 to the
+// last score (4.1 TB/s, in pieces of 256 bytes from all over; the arithmetic takes 5 beside that), 5 from there on.  Scores in 64 bits throughout
+// took 47 us and 8 for the choice (the queries came out of LDS), digits of 11 bits for the choice 8 us more than even steps do, 512 threads 32.
+// Four contexts of 60000-120000 tokens, 4 heads x 64: scores 6.8 us, choice 14.5, of which 64 bits 4 (three loads that wait for each other).
+template <typename T, int DP, bool FUSED, uint32_t N>
+__global__ __launch_bounds__(N) __attribute__((amdgpu_waves_per_eu(DP <= 128 ? 4 : 2))) void pick_kernel(SelectArgs a)
+{
+    __shared__ PickShared s;
+    extern __shared__ float own[];              // scores
+    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = (uint32_t)__builtin_amdgcn_readfirstlane(tid >> 6);
+    // Workgroups go to the eight XCDs in turn: with FUSED the heads of a token follow each other on one of them, whose scales of a block
+    // lie in one line (128 tokens 27.8 us, 29.2 without).
+    uint32_t token, head;
+    if constexpr (FUSED) {
+        const uint32_t nth = blockIdx.x >> 3;
+        token = nth / a.c.heads, head = nth - token * a.c.heads;
+        token = 8u * token + (blockIdx.x & 7u);
+        if (token >= a.b.total_new) return;
+    } else {
+        token = blockIdx.x / a.c.heads, head = blockIdx.x - token * a.c.heads;
+    }
+    const uint32_t item = token * a.c.heads + head;
+    const Request q = token_of(a.b, a.c, (int)token);
+    if (q.fresh <= 0) return;                   // no request's
+    const Choice x = choice_of(a, q);
+    int32_t *const to = a.blocks + (int64_t)item * a.n_select;
+    if (x.seen <= a.n_select) {
+        for (uint32_t i = tid; i < a.n_select; i += N) to[i] = i < x.seen ? (int32_t)i : -1;
+        return;
+    }
+    const uint32_t want = a.n_select - a.n_first - a.n_recent, count = x.hi - x.lo;
+    for (uint32_t i = tid; i < a.n_first; i += N) to[i] = (int32_t)i;
+    for (uint32_t i = tid; i < a.n_recent; i += N) to[a.n_first + want + i] = (int32_t)(x.hi + i);
+    if (!want) return;
+    f32x2 *const left = a.scores + (int64_t)item * a.stride + x.lo;
+    const bool in_lds = FUSED || a.stride <= kMostInLds;
+    for (uint32_t i = tid; i < kPickBins; i += N) s.hist[i] = 0;
+    if (tid < 3u) s.count[tid] = 0;
+    // how far the scores may be off, the least and the largest of them
+    float off = 0.0f, least = INFINITY, most = -INFINITY;
+    auto look = [&](float v) { most = fmaxf(most, v), least = fminf(least, v == -INFINITY ? INFINITY : v); };
+    if constexpr (FUSED) {
+        Scorer<T, DP> scorer(a, q, token, head);
+        // where all blocks lie first, in the scores' places
+        for (uint32_t i = tid; i < count; i += N) own[i] = __int_as_float(entry_of(a.c, q.row, x.lo + i));
+        for (uint32_t row0 = 0; row0 < a.group; row0 += 16u) {
+            scorer.rows(row0);
+            if (!row0) __syncthreads();
+            uint32_t base = 16u * wave;
+            if (base >= count) break;
+            auto entries = [&](uint32_t from) {
+                return [&, from](uint32_t i) {
+                    i += from;
+                    return i >= count ? -1 : row0 ? entry_of(a.c, q.row, x.lo + i) : __float_as_int(own[i]);
+                };
+            };
+            auto tile = scorer.fetch(entries(base));
+            for (;;) {
+                const auto here = tile;
+                const uint32_t next = base + N / 4u;
+                if (next < count) tile = scorer.fetch(entries(next));
+                float v = scorer.of(here);
+                off = fmaxf(off, scorer.off * here.scale);      // (no number where there is no block and no bound: left out)
+                const uint32_t i = base + 4u * (uint32_t)scorer.g + (uint32_t)scorer.col;
+                if (scorer.col < 4 && i < count) {
+                    if (row0) v = fmaxf(v, own[i]);
+                    if (row0 + 16u >= a.group) v = counted(v, here.scale), look(v);
+                    own[i] = v;
+                }
+                if (next >= count) break;
+                base = next;
+            }
+        }
+    } else {
+        constexpr uint32_t kAhead = 8;
+        for (uint32_t i0 = tid; i0 < count; i0 += kAhead * N) {
+            f32x2 v[kAhead];
+#pragma unroll
+            for (uint32_t k = 0; k < kAhead; k++) v[k] = left[min(i0 + k * N, count - 1u)];
+#pragma unroll
+            for (uint32_t k = 0; k < kAhead; k++) {
+                off = fmaxf(off, v[k][1]);
+                look(v[k][0]);
+                if (in_lds && i0 + k * N < count) own[i0 + k * N] = v[k][0];
+            }
+        }
+    }
+    choose<T, N>(s, a, q, token, head, x, own, in_lds, off, most, least);
+}
+
+// Several tokens of a request at a time, one pass over the bounds for all of them: the columns of the products are rows of 16 / each tokens, their
+// scores lie in LDS one token's behind the other's, and the choices follow each other.
+template <typename T, int DP, uint32_t N>
+__global__ __launch_bounds__(N) __attribute__((amdgpu_waves_per_eu(DP <= 64 ? 4 : DP <= 128 ? 3 : 2))) void pick_several_kernel(SelectArgs a)
+{
+    __shared__ PickShared s;
+    extern __shared__ float scores[];
+    const uint32_t tid = threadIdx.x, wave = (uint32_t)__builtin_amdgcn_readfirstlane(tid >> 6);
+    const uint32_t nth = blockIdx.x / a.c.heads, head = blockIdx.x - nth * a.c.heads, first = nth * a.several;
+    const uint32_t last = min(first + a.several, a.b.total_new), want = a.n_select - a.n_first - a.n_recent, lo = a.n_first;
+    const uint32_t each = a.group <= 1u ? 1u : 2u << (31 - __builtin_clz(a.group - 1u));
+    for (uint32_t t0 = first; t0 < last;) {
+        const Request r = request_with(a.b, a.c, (int)t0);
+        const int before = (int)t0 - r.start;
+        if (before < 0 || before >= r.fresh) {                  // no request's
+            t0++;
+            continue;
+        }
+        const uint32_t n = min(last - t0, (uint32_t)(r.fresh - before));
+        auto nth_of = [&](uint32_t y) { return Request{r.row, min(r.len, max(0, r.len - r.fresh + before + (int)y + 1)), (int)(t0 + y), 1}; };
+        auto count_of = [&](uint32_t y) {
+            const Choice x = choice_of(a, nth_of(y));
+            return x.hi - x.lo;
+        };
+        __syncthreads();
+        if (tid < 16u) s.off[tid] = 0;
+        const uint32_t most_blocks = want ? count_of(n - 1u) : 0u;
+        if (most_blocks) {
+            Scorer<T, DP> scorer(a, r, t0, head);
+            for (uint32_t i = tid; i < most_blocks; i += N) scores[i] = __int_as_float(entry_of(a.c, r.row, lo + i));
+            const uint32_t own = (uint32_t)scorer.col / each, row = (uint32_t)scorer.col & (each - 1u);
+            const float wide = largest_of(scorer.column(t0 + min(own, n - 1u), min(row, a.group - 1u)), each);
+            const uint32_t count = own < n ? count_of(min(own, n - 1u)) : 0u;
+            float *const to = scores + own * a.stride;
+            __syncthreads();
+            uint32_t base = 16u * wave;
+            auto entries = [&](uint32_t from) {
+                return [&, from](uint32_t i) { return i + from >= most_blocks ? -1 : __float_as_int(scores[i + from]); };
+            };
+            if (base < most_blocks) {
+                auto tile = scorer.fetch(entries(base));
+                float off = 0.0f;
+                for (;;) {
+                    const auto here = tile;
+                    const uint32_t next = base + N / 4u;
+                    if (next < most_blocks) tile = scorer.fetch(entries(next));
+                    const f32x4 z = scorer.products(here);
+                    float v[4];
+#pragma unroll
+                    for (int i = 0; i < 4; i++) v[i] = largest_of(z[i] == z[i] ? z[i] : INFINITY, each);
+                    const uint32_t block = base + 4u * (uint32_t)scorer.g;
+                    if (each >= 4u) {           // one of four lanes' blocks
+                        const float w = row & 2u ? row & 1u ? v[3] : v[2] : row & 1u ? v[1] : v[0];
+                        if (row < 4u && block + row < count) to[block + row] = counted(w, here.scale), off = fmaxf(off, wide * here.scale);
+                    } else {
+                        const int x = __float_as_int(here.scale);
+                        const float scale[4] = {__int_as_float(__builtin_amdgcn_update_dpp(0, x, 0x00, 0xF, 0xF, false)),
+                                                __int_as_float(__builtin_amdgcn_update_dpp(0, x, 0x55, 0xF, 0xF, false)),
+                                                __int_as_float(__builtin_amdgcn_update_dpp(0, x, 0xAA, 0xF, 0xF, false)),
+                                                __int_as_float(__builtin_amdgcn_update_dpp(0, x, 0xFF, 0xF, 0xF, false))};
+#pragma unroll
+                        for (uint32_t i = 0; i < 4u; i++)
+                            if ((i & (each - 1u)) == row && block + i < count) to[block + i] = counted(v[i], scale[i]), off = fmaxf(off, wide * scale[i]);
+                    }
+                    if (next >= most_blocks) break;
+                    base = next;
+                }
+                if (own < n) atomicMax(&s.off[own], __float_as_uint(off));
+            }
+        }
+        for (uint32_t y = 0; y < n; y++) {
+            const Request q = nth_of(y);
+            const Choice x = choice_of(a, q);
+            int32_t *const to = a.blocks + ((int64_t)(t0 + y) * a.c.heads + head) * a.n_select;
+            if (x.seen <= a.n_select) {
+                for (uint32_t i = tid; i < a.n_select; i += N) to[i] = i < x.seen ? (int32_t)i : -1;
+                continue;
+            }
+            for (uint32_t i = tid; i < a.n_first; i += N) to[i] = (int32_t)i;
+            for (uint32_t i = tid; i < a.n_recent; i += N) to[a.n_first + want + i] = (int32_t)(x.hi + i);
+            if (!want) continue;
+            __syncthreads();
+            for (uint32_t i = tid; i < kPickBins; i += N) s.hist[i] = 0;
+            if (tid < 3u) s.count[tid] = 0;
+            float *const own = scores + y * a.stride;
+            float least = INFINITY, most = -INFINITY;
+            for (uint32_t i = tid; i < x.hi - x.lo; i += N) {
+                const float v = own[i];
+                most = fmaxf(most, v), least = fminf(least, v == -INFINITY ? INFINITY : v);
+            }
+            choose<T, N>(s, a, q, t0 + y, head, x, own, true, __uint_as_float(s.off[y]), most, least);
+        }
+        t0 += n;
+    }
+}
+
+template <typename T, int DP> static hipError_t select(SelectArgs a, hipStream_t s)
 {
     constexpr uint32_t kMany = DP <= 128 ? 1024 : 512;
     const uint64_t items = (uint64_t)a.b.total_new * a.c.heads, per = (a.stride + kBlocksAtOnce - 1u) / kBlocksAtOnce;
@@ -501,7 +627,23 @@ template <typename T, int DP> static hipError_t select(const SelectArgs &a, hipS
     // 128, 2000 29 / 31, 256, 2000 34 / 47, 512, 2000 73 / 95, 8, 7000 72 / 23, 128, 7000 98 / 81.
     const bool fused = a.stride <= kMostInLds && (a.stride <= 1024u || items >= a.stride / 16u);
     if (!launchable(items + 8u * a.c.heads, kMany) || !launchable(items * per, kScoreThreads)) return hipErrorInvalidConfiguration;
+    // Many tokens of few requests: two or four of a request at a time, while there are four workgroups for every compute unit and their scores take no
+    // more LDS than leaves two (heads of 64: three) of them resident.  Measured (us, one at a time / so; requests x tokens x heads, query heads each,
+    // blocks): heads of 128, 1 x 512 x 8, 4, 1875 252 / 158, 4 x 256 x 8, 4, 500 111 / 93, 1 x 2048 x 8, 8, 625 393 / 336, 4 x 190 x 16, 1, 3125
+    // 1214 / 673; of 64, 4 x 190 x 16, 4, 3200 776 / 490, 16 x 64 x 8, 1, 250 85 / 61; of 256, 16 x 64 x 8, 2, 250 222 / 135.  Of 2048 tokens and heads
+    // 28 / 34, with 250 blocks 35 / 40: one at a time.  Eight at a time took 140 where four take 111 (16 x 64 x 8, 1, 1000) and 54 where they take 61.
+    a.several = 1u;
+    if (fused && a.b.starts && a.group <= 8u && a.stride > a.n_select && items >= (DP <= 128 ? 4096u : 2048u)) {
+        uint32_t several = a.group <= 4u ? 4u : 2u;
+        while (several > 1u && (several * a.stride * 4u > (DP <= 64 ? 32768u : 53248u) || (uint64_t)several * a.b.n_reqs > a.b.total_new || items / several < 1024u)) several /= 2u;
+        a.several = several;
+    }
     const uint32_t lds = a.stride > a.n_select && a.stride <= kMostInLds ? a.stride * 4u : 0u;
+    if (a.several > 1u) {
+        const uint32_t groups = (a.b.total_new + a.several - 1u) / a.several * a.c.heads;
+        pick_several_kernel<T, DP, 256><<<groups, 256, a.several * a.stride * 4u, s>>>(a);
+        return hipGetLastError();
+    }
     if (fused) {
         // Workgroups of eight wavefronts while all of them are resident, of four beyond (us, four / eight: 256, 500 18 / 16, 512, 500 22 / 22, 1024 of
         // up to 512 27 / 32).

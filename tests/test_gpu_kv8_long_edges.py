@@ -164,3 +164,47 @@ def test_many_rows_in_front_of_long_rests_of_unequal_length(B, dtype, heads, gro
     """More rows than a tile a head, contexts behind the prefixes (and those of requests without one) in splits that not every request reaches."""
     s = Shared(B, 93, [(shared, [(12, n + 12) for n in lens]), (48, [(1, 60), (9, 700)])], heads, dim, 16, alone=(1, 1))
     _check_shared(B, s, dtype, group)
+
+
+def _several(B, seed, heads, dim, block=16, **more):        # noqa: F811
+    """Requests with enough tokens for one pass over the bounds to serve several of them; chunks of tokens that end inside of a request, hold
+    several of them, and a context of a single block."""
+    n = 4300 // heads
+    return Setup(B, seed, [(1, 12 * block), (n // 2, n // 2 + 11 * block), (0, 5), (3, 9 * block + 1), (1, 1), (n - n // 2, n - n // 2 + 6 * block)],
+                 heads, dim, block, bad=[(1, 4), (5, 3)], **more)
+
+
+@pytest.mark.parametrize("dtype,heads,group,dim", [(BF16, 32, 1, 64), (FP16, 32, 3, 80), (BF16, 16, 2, 256), (FP16, 32, 8, 16), (BF16, 24, 5, 128)])
+def test_selections_of_many_tokens(B, dtype, heads, group, dim):        # noqa: F811
+    s = _several(B, 94, heads, dim, seqs=9)
+    _check_select(B, s, dtype, group, 7, 1, 2)
+    bounds = np.full((s.k.shape[0], heads, 2, dim), 0x38, dtype=np.uint8)
+    bounds[s.rng.integers(0, len(bounds), 9)] = 0x40
+    bounds[s.rng.integers(0, len(bounds), 4)] = 0x7F
+    _check_select(B, s, dtype, group, 6, 0, 1, bounds=bounds)           # (equal ones, and no numbers)
+    _check_select(B, s, dtype, group, 4, 2, 2, bounds=bounds)           # (none by score)
+
+
+def test_selections_of_many_tokens_whose_scores_lie_close(B):        # noqa: F811
+    """Few nearer to each other than fp32 tells apart, and more than there is room for, one token's behind another's."""
+    s = Setup(B, 95, [(131, 300), (3, 16 * 301), (2, 16 * 290)], 32, 64, 16)
+    s.k_scale.fill_(0.25)
+    s.cache = B.KV8(s.k, s.v, s.k_scale, s.v_scale, s.table)
+    bounds = np.full((s.k.shape[0], 32, 2, 64), 0x7E, dtype=np.uint8)
+    bounds[:, :, :, -1] = s.rng.integers(0, 4, size=bounds.shape[:3])
+    q = torch.ones((s.total, 32, 64), dtype=BF16, device=DEV)
+    q[..., -1] = 2.0 ** -12
+    for _ in range(2):
+        _check_select(B, s, BF16, 1, 20, 1, 1, bounds=np.sort(bounds, axis=2), q=(q, q.double().cpu().numpy()))
+        bounds[s.rng.random(len(bounds)) < 0.97, :, :, 0] = 0x70
+
+
+def test_selections_of_many_tokens_of_any_size_and_rows_of_no_request(B):        # noqa: F811
+    """Queries far apart, infinite or no number in one pass; rows behind max_new in the middle of a pass are left."""
+    s = _several(B, 96, 32, 64)
+    most = max(new for _, _, new, _ in s.spans) - 5
+    s.batch = B.KV8Batch(s.lens, starts=s.starts_dev, rows=s.rows_dev, total_new=s.total, max_new=most, max_len=s.max_len)
+    s.spans = [(row, start, min(new, most), length) for row, start, new, length in s.spans]
+    q = torch.from_numpy(s.rng.normal(size=(s.total, 64, 64)) * 2.0 ** s.rng.integers(-125, 110, (s.total, 1, 1))).to(BF16)
+    q[5, 3, 2], q[6, 9, 1], q[9, 0] = math.inf, math.nan, 0.0
+    _check_select(B, s, BF16, 2, 5, 1, 1, q=(q.to(DEV), q.double().numpy()))
