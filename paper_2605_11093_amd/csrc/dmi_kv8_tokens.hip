@@ -849,9 +849,8 @@ template <typename T> static hipError_t tokens(const AttendArgs &a, const Tokens
 }
 
 // A workgroup (or p.splits of them) for each request or new token and head: the rest of contexts behind a prefix, or a prefix and one of its
-// group's row tiles, whose parts another kernel joins, or listed blocks.  Listed blocks of 128 tokens x 8 heads, 64 of 16 tokens each: 269 MB in 57
-// us, 4.7 TB/s in pieces of 128 bytes from all over (the same codes in order 5.8), 6 us of it before the first.  Workgroups of three or six
-// wavefronts, which leave no compute unit to a second round, took 58.
+// group's row tiles, whose parts another kernel joins, or listed blocks.  Listed blocks of 128 tokens x 8 heads, 64 of 16 tokens each: 269 MB in 49
+// us, 5.5 TB/s in pieces of 128 bytes from all over (the same codes in order 5.8), by a wavefront each; by four 57, three or six 58.
 template <typename T, Kind KIND> static hipError_t tokens_apart(const AttendArgs &a, const TokensPlan &p, hipStream_t s)
 {
     const uint32_t units = KIND == kListed ? a.b.total_new : KIND == kPrefix ? a.n_groups : a.b.n_reqs;
