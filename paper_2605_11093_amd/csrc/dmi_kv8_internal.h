@@ -126,7 +126,7 @@ struct TokensPlan {
     bool whole;                                 // a workgroup takes a request and head, or one of its equal splits: no ranges
     uint32_t splits;
     uint32_t ranges;                            // equal parts of all contexts
-    uint32_t waves;                             // of a workgroup, not kWhole: 4 or 8, kListed also 1
+    uint32_t waves;                             // of a workgroup, not kWhole: 4 or 8, kListed and kRest also 1
     bool by_xcd;                                // kPrefix: what reads the same codes on one XCD
     uint32_t tile_rows, row_tiles;              // query rows of a wavefront; wavefronts for the rows that share a head
     uint32_t join_blocks;                       // workgroups of the second launch that join parts, 0 if there can be none

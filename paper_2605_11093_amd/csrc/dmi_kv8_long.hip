@@ -62,6 +62,19 @@ uint32_t splits_of(uint64_t units, uint64_t tokens, uint32_t rows, uint32_t dim)
 // other on one XCD took 57.8 and 56.0 us where these calls take 56.7 and 53.8.
 uint32_t waves_of(uint64_t pairs, uint32_t splits) { return pairs * splits > 256u ? 4u : 8u; }
 
+// Whether many lists, or contexts and heads, have a wavefront each: where rounds of one on each of 1024 SIMDs end sooner so than of four, the start of
+// one counted as six of its tiles of 32 tokens.  Measured (us, four wavefronts / one): lists x their tokens, heads of 128, one token a request, 1024 x 256
+// 22.3 / 18.2, x 1024 56.7 / 49.7, x 4096 237 / 231, 768 x 512 25.8 / 25.0, x 1536 61.7 / 66.7; many tokens a request 13176 x 320 213 / 177, 2048 x 1536
+// 108 / 103, of 256 elements 2048 x 512 110 / 80, of 64 one request's 160 tokens x 16 heads with all it has 86 / 105.  (Two took 55, 184 and 90 where one
+// takes 50, 177 and 80.)  The whole call behind prefixes of 2000: 1000 requests x 8 heads of up to 100 tokens 160 / 116, 256 x 8 of 200 63 / 52, of 1000
+// 115 / 113, 128 x 8 of 1000 67.6 / 68.7.
+bool alone(uint64_t pairs, uint64_t tokens)
+{
+    const uint64_t tiles = (tokens + 31u) / 32u;
+    auto cost = [&](uint64_t waves) { return (pairs * waves + 1023u) / 1024u * (6u + (tiles + waves - 1u) / waves); };
+    return cost(1u) < cost(4u);
+}
+
 }  // namespace
 
 extern "C" dmi_status_t dmi_kv8_append_rotated(const dmi_kv8_t *cache, const dmi_kv8_batch_t *batch, const dmi_kv8_heads_t *key,
@@ -193,14 +206,7 @@ BlocksPlan plan_blocks(uint32_t heads, uint32_t dim, uint32_t block_size, const 
     // (the launch that joins parts has a token in each of its rows)
     t.splits = b.total_new > 65535u ? 1u : splits_of((uint64_t)b.total_new * heads, blocks * block_size, group, dim);
     t.waves = waves_of((uint64_t)b.total_new * heads, t.splits);
-    // Many lists: a wavefront for each, where rounds of one on each of 1024 SIMDs end sooner so, a list's start counted as six of its tiles of 32
-    // tokens.  Measured (us, four wavefronts / one; lists x their tokens): heads of 128, one token a request, 1024 x 256 22.3 / 18.2, x 1024
-    // 56.7 / 49.7, x 4096 237 / 231, 768 x 512 25.8 / 25.0, x 1536 61.7 / 66.7; many tokens a request 13176 x 320 213 / 177, 2048 x 1536 108 / 103, of
-    // 256 elements 2048 x 512 110 / 80, of 64 one request's 160 tokens x 16 heads with all it has 86 / 105.  (Two took 55, 184 and 90 where one takes 50,
-    // 177 and 80.)
-    const uint64_t lists = (uint64_t)b.total_new * heads * t.splits, tiles = (blocks * block_size / t.splits + 31u) / 32u;
-    auto cost = [&](uint64_t waves) { return (lists * waves + 1023u) / 1024u * (6u + (tiles + waves - 1u) / waves); };
-    if (lists >= 768u && cost(1u) < cost(4u)) t.waves = 1u;
+    if ((uint64_t)b.total_new * heads * t.splits >= 768u && alone((uint64_t)b.total_new * heads * t.splits, blocks * block_size / t.splits)) t.waves = 1u;
     t.join_blocks = t.splits > 1u ? (q_heads + 3u) / 4u : 0u;
     const uint64_t parts = t.splits > 1u ? (uint64_t)b.total_new * q_heads * t.splits : 0u;
     p.parts = pad64(parts * 8u);
@@ -305,6 +311,7 @@ SharedSizes plan_shared(uint32_t heads, uint32_t dim, uint32_t block_size, const
         t.row_tiles = 1u;
         t.splits = p.splits = splits_of((uint64_t)b.n_reqs * heads, behind, (uint32_t)shared, dim);
         t.waves = waves_of((uint64_t)b.n_reqs * heads, t.splits);
+        if (t.splits == 1u && (uint64_t)b.n_reqs * heads > 1024u && alone((uint64_t)b.n_reqs * heads, behind)) t.waves = 1u;
     } else {
         PartsPlan &m = p.many;
         m.row_tiles = (uint32_t)((shared + rows_each - 1u) / rows_each);

@@ -864,7 +864,7 @@ template <typename T, Kind KIND> static hipError_t tokens_apart(const AttendArgs
             tokens_kernel<T, DP, NT, true, KIND, NW><<<(uint32_t)groups, 64 * NW, 0, s>>>(a, p);
             return hipGetLastError();
         };
-        if constexpr (KIND == kListed)
+        if constexpr (KIND == kListed || KIND == kRest)
             if (p.waves == 1u) return with(Int<1>{});
         return p.waves == 4u || many == 4 ? with(Int<4>{}) : with(Int<many>{});
     };

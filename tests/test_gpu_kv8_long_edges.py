@@ -208,3 +208,19 @@ def test_selections_of_many_tokens_of_any_size_and_rows_of_no_request(B):       
     q = torch.from_numpy(s.rng.normal(size=(s.total, 64, 64)) * 2.0 ** s.rng.integers(-125, 110, (s.total, 1, 1))).to(BF16)
     q[5, 3, 2], q[6, 9, 1], q[9, 0] = math.inf, math.nan, 0.0
     _check_select(B, s, BF16, 2, 5, 1, 1, q=(q.to(DEV), q.double().numpy()))
+
+
+@pytest.mark.parametrize("dtype,heads,group,dim,new,kind", [
+    (BF16, 16, 4, 128, 1, "spread"), (FP16, 16, 16, 64, 2, "far"), (BF16, 16, 8, 80, 1, "odd"), (FP16, 16, 1, 256, 3, "tiny")])
+@pytest.mark.parametrize("groups", [1, 5])
+def test_rests_of_a_wavefront_each(B, dtype, heads, group, dim, new, kind, groups):        # noqa: F811
+    """Many requests with few rows and short contexts behind their prefixes, each gone through by one wavefront; some that share nothing."""
+    s = Shared(B, 97, [(32 * g + 32, [(new, 32 * g + 32 + new + (i * 7) % 40) for i in range(60 // groups)]) for g in range(groups)], heads, dim, 16, alone=(3, 6))
+    assert len(s.spans) * heads > 1024
+    s.v_scale.copy_(_scales(s, kind, s.rng))
+    qd, qn = s.values(heads * group, dtype, 1.3)
+    out, lse = torch.empty_like(qd), torch.empty(qd.shape[:2], device=DEV)
+    B.kv8_attend_shared(s.cache, s.batch, s.prefix, qd, out, lse=lse, stream=_stream())
+    (o, l, _), (do, dl, _) = _bounds(s, qn, dim ** -0.5, group, dtype)
+    K.near(lse.cpu().numpy(), l, dl, "lse")
+    K.near(out.float().cpu().numpy(), o, do, "out")
