@@ -143,6 +143,7 @@ struct TokensPlan {
 struct PartsPlan {
     uint32_t row_tiles;                         // workgroups for the rows that share a head
     bool counted;                               // requests' rows differ much: see parts_kernel
+    bool spread;                                // not kWhole, and counted: row tiles go to the XCDs in turn
     uint32_t splits, chunk;                     // parts of the longest context, their tokens
     f32x2 *sums;                                // [row of out][split]: maximum, sum of 2^(score - maximum); one split: unused
     float *parts;                               // [row of out][split][dim]

@@ -68,6 +68,7 @@ void parts_kernel(AttendArgs a, PartsPlan p)
     // The row tiles of a request and head on one XCD, those that see most first: workgroups go to the eight XCDs in turn, and every eighth
     // pair of request and head belongs to each.
     const uint32_t xcd = blockIdx.x & 7u, item = (blockIdx.x >> 3) / p.splits, split = (blockIdx.x >> 3) - item * p.splits;
+    const bool spread = KIND != kWhole && p.spread;             // (row tiles in turn)
     Request q{0, 0, 0, 0};
     uint32_t head = 0;
     [[maybe_unused]] int unit_at = 0;           // the request, or group
@@ -81,8 +82,8 @@ void parts_kernel(AttendArgs a, PartsPlan p)
             Request own{0, 0, 0, 0};
             if (r < units) own = PREFIX ? group_rows(a, (int)r) : request_of(a.b, a.c, (int)r);
             const int row_tiles = (own.fresh * (int)a.group + 32 * NW - 1) / (32 * NW);
-            const uint32_t pairs = ((r + 1u) * a.c.heads + 7u - xcd) / 8u - (r * a.c.heads + 7u - xcd) / 8u;
-            const int upto = lanes_scan(row_tiles * (int)pairs), place = (int)(item - before);
+            const uint32_t pairs = spread ? a.c.heads : ((r + 1u) * a.c.heads + 7u - xcd) / 8u - (r * a.c.heads + 7u - xcd) / 8u;
+            const int upto = lanes_scan(row_tiles * (int)pairs), place = (int)((spread ? 8u * item + xcd : item) - before);
             const uint64_t behind = __ballot(upto > place);
             if (!behind) {
                 before += (uint32_t)__builtin_amdgcn_readlane(upto, 63);
@@ -93,7 +94,7 @@ void parts_kernel(AttendArgs a, PartsPlan p)
             const uint32_t first = (n0 + (uint32_t)in) * a.c.heads;
             q = request_in(own, in);
             unit_at = (int)n0 + in;
-            head = ((xcd - first) & 7u) + 8u * (uint32_t)which;
+            head = spread ? (uint32_t)which : ((xcd - first) & 7u) + 8u * (uint32_t)which;
             row0 = (of - 1 - (nth - which * of)) * 32 * NW;
             break;
         }
@@ -802,8 +803,15 @@ template <typename T, int DP, int NW, Kind KIND> static hipError_t parts(const A
     const uint64_t units = KIND == kPrefix || KIND == kLast ? a.n_groups : a.b.n_reqs;
     const uint64_t by_pairs = (units * a.c.heads + 7u) / 8u * p.row_tiles;
     const uint64_t by_rows = ((uint64_t)a.b.total_new * a.group / (32u * NW) + units) * ((a.c.heads + 7u) / 8u);
-    p.counted = by_pairs > by_rows;
-    const uint64_t groups = (p.counted ? by_rows : by_pairs) * p.splits * 8u;
+    // Few pairs, of a group and a head or of a request, that eight do not divide: XCDs without any, or with one more than others; their row tiles
+    // go to the XCDs in turn.  (Us, by pairs / so; requests x tokens,
+    // heads, query heads each, prefixes: 59 x 370, 1 x 256, 1, one of 7000 2057 / 359; 85 x 174, 1 x 128, 2, three of 8000 460 / 151; 32 x 300, 4 x 128, 4, one
+    // of 4000 844 / 491; 64 x 32, 12 x 128, 4, one of 4000 376 / 304; 32 x 100, 10 x 128, 4, six 461 / 458.)
+    const uint64_t pairs = units * a.c.heads;
+    p.spread = KIND != kWhole && pairs % 8u && pairs < 64u;
+    p.counted = p.spread || by_pairs > by_rows;
+    const uint64_t all = std::min(((uint64_t)a.b.total_new * a.group / (32u * NW) + units) * a.c.heads, pairs * p.row_tiles);
+    const uint64_t groups = (p.spread ? (all + 7u) / 8u : p.counted ? by_rows : by_pairs) * p.splits * 8u;
     const uint64_t weight_groups = a.w.data ? (a.b.max_len + 255ull) / 256u * a.c.heads : 0u;
     if (!launchable(groups, 64u * NW) || !launchable(weight_groups, 256)) return hipErrorInvalidConfiguration;
     parts_kernel<T, DP, NW, KIND><<<(uint32_t)groups, 64 * NW, 0, s>>>(a, p);

@@ -224,3 +224,14 @@ def test_rests_of_a_wavefront_each(B, dtype, heads, group, dim, new, kind, group
     (o, l, _), (do, dl, _) = _bounds(s, qn, dim ** -0.5, group, dtype)
     K.near(lse.cpu().numpy(), l, dl, "lse")
     K.near(out.float().cpu().numpy(), o, do, "out")
+
+
+@pytest.mark.parametrize("dtype,heads,group,dim", [(BF16, 1, 2, 128), (BF16, 8, 2, 128), (FP16, 3, 3, 64), (FP16, 8, 3, 64), (BF16, 5, 1, 256), (BF16, 8, 1, 256)])
+@pytest.mark.parametrize("groups", [
+    [(96, [(300, 400), (2, 150), (70, 240)])],                                  # unsplit, rows that differ much
+    [(600, [(90, 700)] * 7)],                                                   # alike, split or not
+    [(64, [(150, 220), (3, 90)]), (0, [(40, 60)]), (200, [(33, 240), (1, 201), (260, 470)]), (16, [(9, 30)])]])
+def test_row_tiles_by_pairs_and_in_turn(B, dtype, heads, group, dim, groups):        # noqa: F811
+    """Eight heads, whose pairs the XCDs have one by one, and other counts, whose row tiles go to them in turn."""
+    s = Shared(B, 98, groups, heads, dim, 16, alone=(1, 0))
+    _check_shared(B, s, dtype, group)
