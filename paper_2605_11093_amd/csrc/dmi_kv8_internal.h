@@ -127,6 +127,7 @@ struct TokensPlan {
     uint32_t splits;
     uint32_t ranges;                            // equal parts of all contexts
     uint32_t waves;                             // of a workgroup, not kWhole: 4 or 8, kListed and kRest also 1
+    bool through;                               // kRest: prefixes too, through the first request's row
     bool by_xcd;                                // kPrefix: what reads the same codes on one XCD
     uint32_t tile_rows, row_tiles;              // query rows of a wavefront; wavefronts for the rows that share a head
     uint32_t join_blocks;                       // workgroups of the second launch that join parts, 0 if there can be none
@@ -155,6 +156,7 @@ struct SharedPlan {
     PartsPlan prefix;                           // splits 0: there is none
     bool few_rows;                              // few rows for it: by tokens_kernel, whose splits are all there
     TokensPlan prefix_few;
+    bool through;                               // not read once: few and short, each request reads it
     bool last;                                  // the prefix goes on from the rests' sums: nothing is split
     bool tokens;                                // few rows a head behind it: by tokens_kernel
     TokensPlan few;
@@ -250,7 +252,7 @@ __device__ __forceinline__ int group_tokens(const AttendArgs &a, int g, int &row
 }
 // How many of them a request takes: all, where it has as many in front of its new tokens, or none.  All lanes of a wavefront look for its
 // group, the last one that begins at or in front of it, 64 places at a time.
-__device__ __forceinline__ int shared_tokens(const AttendArgs &a, int r, const Request &q)
+__device__ __forceinline__ int shared_tokens(const AttendArgs &a, int r, const Request &q, int &row)
 {
     int g = 0, n = (int)a.n_groups;
     if (!n) return 0;
@@ -261,9 +263,13 @@ __device__ __forceinline__ int shared_tokens(const AttendArgs &a, int r, const R
         n = min(step, n - (k - 1) * step);
     }
     if (r < a.group_starts[g] || r >= a.group_starts[g + 1]) return 0;
-    int row;
     const int tokens = group_tokens(a, g, row);
     return q.len - q.fresh >= tokens ? tokens : 0;
+}
+__device__ __forceinline__ int shared_tokens(const AttendArgs &a, int r, const Request &q)
+{
+    int row;
+    return shared_tokens(a, r, q, row);
 }
 
 // Sums over the lanes up to each one

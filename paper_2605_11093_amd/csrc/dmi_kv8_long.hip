@@ -311,7 +311,13 @@ SharedSizes plan_shared(uint32_t heads, uint32_t dim, uint32_t block_size, const
         t.row_tiles = 1u;
         t.splits = p.splits = splits_of((uint64_t)b.n_reqs * heads, behind, (uint32_t)shared, dim);
         t.waves = waves_of((uint64_t)b.n_reqs * heads, t.splits);
-        if (t.splits == 1u && (uint64_t)b.n_reqs * heads > 1024u && alone((uint64_t)b.n_reqs * heads, behind)) t.waves = 1u;
+        // Short prefixes of few requests: each reads its group's by itself (out of the caches), in one launch.  Measured (us, read once / so; requests x
+        // tokens, one prefix): 8 heads x 128, 8 x 1, 1024 21.1 / 15.0, 64 x 1, 512 22.8 / 15.6, 1024 23.4 / 20.3, 128 x 1, 512 29.5 / 27.5, 1024 32.5 / 37.1,
+        // 512 x 1, 64 42.7 / 30.0, 256 44.7 / 48.2; 4 x 64, 512 x 3, 512 36.9 / 30.3, 1024 42.6 / 45.3; 8 x 256, 128 x 1, 256 45.8 / 43.1, 512 46.9 / 53.1.
+        const uint64_t pairs = (uint64_t)b.n_reqs * heads;
+        p.through = p.prefix.splits && pairs * prefix * dim <= 1ull << 26 && splits_of(pairs, b.max_len, (uint32_t)shared, dim) == 1u;
+        if (p.through) t.through = true, t.splits = p.splits = 1u, t.waves = waves_of((uint64_t)b.n_reqs * heads, 1u);
+        if (t.splits == 1u && (uint64_t)b.n_reqs * heads > 1024u && alone((uint64_t)b.n_reqs * heads, p.through ? b.max_len : behind)) t.waves = 1u;
     } else {
         PartsPlan &m = p.many;
         m.row_tiles = (uint32_t)((shared + rows_each - 1u) / rows_each);
@@ -334,11 +340,11 @@ SharedSizes plan_shared(uint32_t heads, uint32_t dim, uint32_t block_size, const
     }
     // Nothing split: the sums of what is behind the prefix are where the prefix begins, and its end writes outputs (32 prompts behind 4000
     // tokens 753 us; 810 with a part of every row more to write, and two to read).
-    p.last = !p.few_rows && p.prefix.splits == 1u && p.splits == 1u;
+    p.last = !p.few_rows && p.prefix.splits == 1u && p.splits == 1u && !p.through;
     // Few rows behind it that nothing splits: their workgroups read its parts and write outputs (64 tokens behind 8192: 55.6 us with a
     // launch that joins, 53.4 without; 24 x 3 in four groups 23.9 and 20.9).
     p.few.before = p.tokens && p.splits == 1u && !p.last;
-    const uint64_t parts = p.last ? 0u : rows * p.prefix.splits;
+    const uint64_t parts = p.last || p.through ? 0u : rows * p.prefix.splits;
     z.prefix_parts = pad64(parts * 8u);
     z.sums = z.prefix_parts + pad64(parts * dim * 4u);
     z.parts = z.sums + pad64(rows * p.splits * 8u);

@@ -898,7 +898,7 @@ __global__ __launch_bounds__(256) void join_shared_kernel(AttendArgs a, SharedPl
 hipError_t launch_shared(const AttendArgs &a, const SharedPlan &p, uint32_t dtype, hipStream_t s)
 {
     hipError_t e = hipSuccess;
-    if (a.n_groups && !p.last) {
+    if (a.n_groups && !p.last && !p.through) {
         e = p.few_rows ? launch_tokens_apart(a, p.prefix_few, kPrefix, dtype, s) : launch_parts_apart(a, p.prefix, kPrefix, dtype, s);
         if (e != hipSuccess) return e;
     }

@@ -84,6 +84,8 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
     int r = 0, seg0 = 0, range = 0, first, last;        // seg0: the request's first tile; first, last: the range's tiles
     Request held{0, 0, 0, 0};                           // of this lane, where there are no more than lanes
     [[maybe_unused]] uint32_t skipped = 0;              // kRest: blocks in front
+    [[maybe_unused]] uint32_t front = 0;                // kRest: or blocks that are read through front_row
+    [[maybe_unused]] int front_row = 0;
     if constexpr (WHOLE) {
         uint32_t pair = blockIdx.x / p.splits;
         range = (int)(blockIdx.x - pair * p.splits);
@@ -101,9 +103,10 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
         Request q = KIND == kListed ? token_of(a.b, a.c, r) : KIND == kPrefix ? group_rows(a, r) : request_of(a.b, a.c, r);
         if constexpr (KIND == kPrefix) q.len = group_tokens(a, r, q.row);
         if constexpr (KIND == kRest) {
-            const int shared = shared_tokens(a, r, q);
-            q.len -= shared;
-            skipped = block_of(a.c, (uint32_t)shared >> 4);
+            const int shared = shared_tokens(a, r, q, front_row);
+            const uint32_t blocks = block_of(a.c, (uint32_t)shared >> 4);
+            if (p.through) front = blocks;
+            else q.len -= shared, skipped = blocks;
         }
         if (KIND == kPrefix && (int)row_tile * 16 * NT >= q.fresh * (int)a.group) return;
         const int tiles = KIND == kListed ? (listed_tokens(a, q) + 31) >> 5 : KIND == kPrefix ? (q.len + 31) >> 5 : q.fresh > 0 ? tiles_of(q) : a.w.data ? (q.len + 31) >> 5 : 0;
@@ -188,7 +191,7 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
                     if (l.left <= 0) block = a.c.max_blocks;
                 }
                 if constexpr (KIND == kRest) block += skipped;
-                l.entry = entry_of(a.c, q.row, block);
+                l.entry = entry_of(a.c, KIND == kRest && block < front ? front_row : q.row, block);
                 if (l.entry >= 0) {
                     l.ks = *scale_at(a.c, 0, l.entry, head) * a.scale_log2;
                     l.vs = *scale_at(a.c, 1, l.entry, head);

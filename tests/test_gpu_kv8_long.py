@@ -326,7 +326,10 @@ def test_listed_blocks_are_what_all_blocks_are(B):        # noqa: F811
 
 # ------------------------------------------------------------------ shared prefixes
 class Shared(Setup):
-    """Requests whose rows of the table begin with the blocks of their group's first."""
+    """Requests whose rows of the table begin with the blocks of their group's first.  READ_ONCE: the host's bounds are so high that no request
+    reads a prefix by itself."""
+
+    READ_ONCE = False
 
     def __init__(self, B, seed, groups, heads, dim, block, *, alone=(0, 0), **more):        # noqa: F811
         """groups: (shared tokens, [(new tokens, length), ...]); alone: requests in front of the groups and behind them that share nothing."""
@@ -341,7 +344,14 @@ class Shared(Setup):
         self.table.copy_(torch.from_numpy(table))
         self.group_starts = torch.tensor(starts, dtype=torch.int32, device=DEV)
         self.shared = torch.tensor([shared for shared, _ in groups], dtype=torch.int32, device=DEV)
-        self.prefix = B.KV8Prefix(self.group_starts, self.shared, max_prefix=max([1] + [shared for shared, _ in groups]))
+        longest = max([1] + [shared for shared, _ in groups])
+        if self.READ_ONCE:                      # (the table has to be as wide)
+            longest = self.max_len = max(self.max_len, (1 << 26) // (self.n * heads * dim) + 2 * block)
+            self.batch = B.KV8Batch(self.lens, starts=self.starts_dev, rows=self.rows_dev, total_new=self.total, max_new=max(new for new, _ in spans),
+                                    max_len=longest)
+            self.table = torch.nn.functional.pad(self.table, (0, -(-longest // block) - self.per), value=-1)
+            self.cache = B.KV8(self.k, self.v, self.k_scale, self.v_scale, self.table)
+        self.prefix = B.KV8Prefix(self.group_starts, self.shared, max_prefix=longest)
 
 
 def _check_shared(B, s, dtype, group, *, scale=None, spread=1.3, prefix=None, in_place=False):        # noqa: F811

@@ -10,6 +10,7 @@ import _kv8 as K
 import _kv8_long as L
 from test_gpu_kv8 import B, BF16, DEV, FP16, FP32, Setup, _stream        # noqa: F401
 from test_gpu_kv8_edges import _bounds, _scales
+import test_gpu_kv8_long as shared
 from test_gpu_kv8_long import Shared, _check_blocks, _check_rotated, _check_select, _check_shared, _lists
 
 pytestmark = pytest.mark.gpu
@@ -235,3 +236,34 @@ def test_row_tiles_by_pairs_and_in_turn(B, dtype, heads, group, dim, groups):   
     """Eight heads, whose pairs the XCDs have one by one, and other counts, whose row tiles go to them in turn."""
     s = Shared(B, 98, groups, heads, dim, 16, alone=(1, 0))
     _check_shared(B, s, dtype, group)
+
+
+@pytest.mark.parametrize("call", [
+    *(lambda B, d=d, x=x: shared.test_shared_by_single_tokens(B, d, *x)
+      for d, x in ((BF16, (2, 4, 64, 16)), (FP16, (1, 7, 80, 32)), (BF16, (2, 1, 256, 16)), (FP16, (2, 8, 128, 16)), (BF16, (1, 32, 96, 48)))),
+    lambda B: shared.test_shared_in_splits(B), lambda B: shared.test_shared_by_none(B), lambda B: shared.test_shared_in_place(B),
+    lambda B: shared.test_shared_by_requests_that_are_not_there(B), lambda B: shared.test_shared_with_what_is_no_number(B),
+    lambda B: shared.test_shared_and_never_split(B, BF16, 128, 4), lambda B: shared.test_shared_and_never_split(B, FP16, 128, 8),
+    lambda B: shared.test_shared_by_many_requests_and_groups(B), lambda B: shared.test_shared_by_groups_that_are_none(B, [-5, 2, 1 << 30]),
+    *(lambda B, d=d, k=k, x=x: test_scales_of_v_behind_prefixes(B, [(x[0], [(1, x[0] + 9 + 7 * i) for i in range(x[1])])], x[2], x[3], d, k)
+      for d, k in ((FP16, "spread"), (FP16, "far"), (FP16, "odd"), (BF16, "tiny")) for x in ((300, 5, 4, 64), (400, 30, 4, 128), (100, 3, 4, 256))),
+    *(lambda B, bad=bad: test_queries_that_are_no_numbers_spoil_no_others(B, bad, True) for bad in (math.nan, math.inf))])
+def test_prefixes_read_once_for_few_requests(B, monkeypatch, call):        # noqa: F811
+    """What short prefixes of few requests are checked for, with bounds that make a launch of their own of them."""
+    monkeypatch.setattr(Shared, "READ_ONCE", True)
+    call(B)
+
+
+@pytest.mark.parametrize("once", [False, True])
+def test_prefixes_that_the_others_rows_do_not_list(B, monkeypatch, once):        # noqa: F811
+    """They are read through the first request's."""
+    monkeypatch.setattr(Shared, "READ_ONCE", once)
+    s = Shared(B, 99, [(100, [(1, 140), (3, 120), (1, 99 + 16)]), (48, [(1, 50), (1, 90)])], 2, 64, 16, alone=(1, 0))
+    q, qn = s.values(8, BF16)
+    (o, l, _), (do, dl, _) = K.attend(s.cpu(), s.spans, qn, 64 ** -0.5, 4, BF16)
+    for r, n in ((2, 6), (3, 6), (5, 3)):
+        s.table[s.rows[r], :n] = -1
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:2], device=DEV)
+    B.kv8_attend_shared(s.cache, s.batch, s.prefix, q, out, lse=lse, stream=_stream())
+    K.near(lse.cpu().numpy(), l, dl, "lse")
+    K.near(out.float().cpu().numpy(), o, do, "out")
