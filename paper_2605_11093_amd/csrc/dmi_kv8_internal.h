@@ -239,31 +239,45 @@ __device__ __forceinline__ Request group_rows(const AttendArgs &a, int g)
     const int end = a.b.starts ? min(max(a.b.starts[last], start), (int)a.b.total_new) : last;
     return {first, 0, start, first < last ? end - start : 0};
 }
-// Tokens that are read once for group g: whole blocks of its prefix, in front of its first request's new tokens.  `row`: that one's in the table.
-__device__ __forceinline__ int group_tokens(const AttendArgs &a, int g, int &row)
+// Tokens that are read once for the group of requests `start` to `end`: whole blocks of its prefix, in front of its first request's new tokens.
+// `row`: that one's in the table.
+__device__ __forceinline__ int tokens_of(const AttendArgs &a, int start, int end, int prefix, int &row)
 {
-    const int first = min(max(a.group_starts[g], 0), (int)a.b.n_reqs);
+    const int first = min(max(start, 0), (int)a.b.n_reqs);
     row = 0;
-    if (first >= min(a.group_starts[g + 1], (int)a.b.n_reqs)) return 0;
+    if (first >= min(end, (int)a.b.n_reqs)) return 0;
     const Request q = request_of(a.b, a.c, first);
     row = q.row;
-    const int tokens = min(min(max(a.prefix[g], 0), (int)a.max_prefix), max(q.len - q.fresh, 0));
+    const int tokens = min(min(max(prefix, 0), (int)a.max_prefix), max(q.len - q.fresh, 0));
     return (int)(((uint32_t)(((uint64_t)((uint32_t)tokens >> 4) * a.c.per_block) >> 31)) * a.c.bs);
 }
+__device__ __forceinline__ int group_tokens(const AttendArgs &a, int g, int &row)
+{
+    return tokens_of(a, a.group_starts[g], a.group_starts[g + 1], a.prefix[g], row);
+}
 // How many of them a request takes: all, where it has as many in front of its new tokens, or none.  All lanes of a wavefront look for its
-// group, the last one that begins at or in front of it, 64 places at a time.
+// group, the last one that begins at or in front of it, 64 places at a time; up to 64 groups in one trip to memory.
 __device__ __forceinline__ int shared_tokens(const AttendArgs &a, int r, const Request &q, int &row)
 {
-    int g = 0, n = (int)a.n_groups;
+    int n = (int)a.n_groups, start, end, prefix;
     if (!n) return 0;
-    while (n > 1) {
-        const int step = (n + 63) >> 6, at = (int)(threadIdx.x & 63u) * step;
-        const int k = max(1, __popcll(__ballot(at < n && a.group_starts[g + min(at, n - 1)] <= r)));
-        g += (k - 1) * step;
-        n = min(step, n - (k - 1) * step);
+    const int lane = (int)(threadIdx.x & 63u);
+    if (n <= 64) {
+        const int i = min(lane, n - 1), from = a.group_starts[i], to = a.group_starts[i + 1], tokens = a.prefix[i];
+        const int g = max(1, __popcll(__ballot(lane < n && from <= r))) - 1;
+        start = __builtin_amdgcn_readlane(from, g), end = __builtin_amdgcn_readlane(to, g), prefix = __builtin_amdgcn_readlane(tokens, g);
+    } else {
+        int g = 0;
+        while (n > 1) {
+            const int step = (n + 63) >> 6, at = lane * step;
+            const int k = max(1, __popcll(__ballot(at < n && a.group_starts[g + min(at, n - 1)] <= r)));
+            g += (k - 1) * step;
+            n = min(step, n - (k - 1) * step);
+        }
+        start = a.group_starts[g], end = a.group_starts[g + 1], prefix = a.prefix[g];
     }
-    if (r < a.group_starts[g] || r >= a.group_starts[g + 1]) return 0;
-    const int tokens = group_tokens(a, g, row);
+    if (r < start || r >= end) return 0;
+    const int tokens = tokens_of(a, start, end, prefix, row);
     return q.len - q.fresh >= tokens ? tokens : 0;
 }
 __device__ __forceinline__ int shared_tokens(const AttendArgs &a, int r, const Request &q)

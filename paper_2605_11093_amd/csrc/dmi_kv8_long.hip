@@ -343,12 +343,13 @@ SharedSizes plan_shared(uint32_t heads, uint32_t dim, uint32_t block_size, const
     p.last = !p.few_rows && p.prefix.splits == 1u && p.splits == 1u && !p.through;
     // Few rows behind it that nothing splits: their workgroups read its parts and write outputs (64 tokens behind 8192: 55.6 us with a
     // launch that joins, 53.4 without; 24 x 3 in four groups 23.9 and 20.9).
-    p.few.before = p.tokens && p.splits == 1u && !p.last;
+    p.few.before = p.tokens && p.splits == 1u && !p.last && !p.through;
     const uint64_t parts = p.last || p.through ? 0u : rows * p.prefix.splits;
     z.prefix_parts = pad64(parts * 8u);
     z.sums = z.prefix_parts + pad64(parts * dim * 4u);
-    z.parts = z.sums + pad64(rows * p.splits * 8u);
-    z.bytes = rows && b.n_reqs ? z.parts + pad64(rows * p.splits * dim * 4u) : 0u;
+    const uint64_t behind_parts = p.through || p.few.before ? 0u : rows * p.splits;
+    z.parts = z.sums + pad64(behind_parts * 8u);
+    z.bytes = rows && b.n_reqs ? z.parts + pad64(behind_parts * dim * 4u) : 0u;
     return z;
 }
 

@@ -904,7 +904,7 @@ hipError_t launch_shared(const AttendArgs &a, const SharedPlan &p, uint32_t dtyp
     }
     e = p.tokens ? launch_tokens_apart(a, p.few, kRest, dtype, s) : launch_parts_apart(a, p.many, kRest, dtype, s);
     if (e != hipSuccess) return e;
-    if (p.tokens && p.few.before) return hipSuccess;
+    if (p.through || (p.tokens && p.few.before)) return hipSuccess;
     if (p.last) {
         PartsPlan prefix = p.prefix;
         prefix.sums = p.sums, prefix.parts = p.parts;

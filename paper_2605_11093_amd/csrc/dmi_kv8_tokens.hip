@@ -580,7 +580,7 @@ void tokens_kernel(AttendArgs a, TokensPlan p)
                 float l_all;
                 const float total = total_of(nth, l_all), f = total == -INFINITY && l_all == 0.0f ? 0.0f : 1.0f / l_all;
                 const QueryRow w = query_row(a, head, (uint32_t)row);
-                if (KIND == kRest || KIND == kPrefix || p.splits > 1u) {
+                if (KIND == kRest ? !p.through : KIND == kPrefix || p.splits > 1u) {
                     const int64_t part = ((int64_t)(q.start + w.token) * a.q_heads + w.head) * p.splits + range;
                     if (g == 0 && j == 0) p.sums[part] = f32x2{top_of(nth), l_all};
                     float *dst = p.parts + part * a.c.dim;
