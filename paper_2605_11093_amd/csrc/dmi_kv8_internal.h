@@ -103,14 +103,14 @@ struct AttendArgs {
     uint32_t group, q_heads;
     const int32_t *blocks;                      // kListed: those attended to, [new token][head][n_select]
     uint32_t n_select;
-    uint32_t n_groups, max_prefix;              // kPrefix, kLast, kRest: see dmi_kv8_prefix_t
+    uint32_t n_groups, max_prefix;              // kPrefix, kLast, kRest, kThrough: see dmi_kv8_prefix_t
     const int32_t *group_starts, *prefix;
 };
 
 // What the attention kernels do: a whole context; the rest of one behind a shared prefix, whose sums are left as parts whatever their
 // number; such a prefix, for all rows of a group of requests, whose sums are left as parts, or which goes on from the rests' sums to outputs;
-// listed blocks, for each new token by itself.
-enum Kind { kWhole, kRest, kPrefix, kLast, kListed };
+// listed blocks, for each new token by itself; a whole context whose prefix is read through its group's first request's row.
+enum Kind { kWhole, kRest, kPrefix, kLast, kListed, kThrough };
 
 constexpr uint32_t kFewRows = 32;               // query rows that share a head: up to here by tokens_kernel
 
@@ -156,7 +156,7 @@ struct SharedPlan {
     PartsPlan prefix;                           // splits 0: there is none
     bool few_rows;                              // few rows for it: by tokens_kernel, whose splits are all there
     TokensPlan prefix_few;
-    bool through;                               // not read once: few and short, each request reads it
+    bool through;                               // not read once: each request reads it, in one launch
     bool last;                                  // the prefix goes on from the rests' sums: nothing is split
     bool tokens;                                // few rows a head behind it: by tokens_kernel
     TokensPlan few;

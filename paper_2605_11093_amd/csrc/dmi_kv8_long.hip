@@ -267,6 +267,7 @@ SharedSizes plan_shared(uint32_t heads, uint32_t dim, uint32_t block_size, const
     const uint32_t group = q_heads / heads, rows_each = dim <= 128u ? 256u : 128u, max_new = std::min(b.max_new, b.total_new);
     const uint64_t rows = (uint64_t)b.total_new * q_heads, shared = (uint64_t)max_new * group;
     const uint32_t prefix = std::min(x.max_prefix, b.max_len) / block_size * block_size;
+    double once = INFINITY;                     // us that prefixes read once take
     if (x.n_groups && prefix) {
         const uint64_t all = (uint64_t)b.total_new * group;
         auto tiles_of = [&](uint32_t rows) { return std::max<uint64_t>(x.n_groups, (all + (uint64_t)x.n_groups * rows / 2u) / rows); };
@@ -286,16 +287,16 @@ SharedSizes plan_shared(uint32_t heads, uint32_t dim, uint32_t block_size, const
             t.waves = 4u;
             t.by_xcd = x.n_groups * heads >= 8u;
             t.splits = p.prefix.splits = (uint32_t)std::max<uint64_t>(1u, std::min<uint64_t>(256u / few, prefix / 256u));
+            once = 8.0 + 1.5 * ((prefix / 32u + t.splits * 4u - 1u) / (t.splits * 4u));
         } else {
             PartsPlan &m = p.prefix;
             m.row_tiles = (uint32_t)((all + rows_each - 1u) / rows_each);
             // As many splits as make the sum of two least: rounds of 256 workgroups, with three tiles of 64 tokens for each one's start and
             // end, 2.5 us a tile; and a part of every row written and read again, at 4 TB/s.
             const uint64_t groups = tiles_of(rows_each) * heads, tiles = (prefix + 63u) / 64u;
-            double best = INFINITY;
             for (uint32_t s = 1; s <= 64u && (s == 1u || s * 128u <= prefix); s++) {
                 const double cost = (double)((groups * s + 255u) / 256u) * (double)((tiles + s - 1u) / s + 3u) * 2.5 + (double)rows * s * dim * 8.0 / 4e6;
-                if (cost < best) best = cost, m.splits = s;
+                if (cost < once) once = cost, m.splits = s;
             }
             m.chunk = std::max(64u, ((prefix + m.splits - 1u) / m.splits + 63u) & ~63u);
             m.splits = (prefix + m.chunk - 1u) / m.chunk;
@@ -325,7 +326,8 @@ SharedSizes plan_shared(uint32_t heads, uint32_t dim, uint32_t block_size, const
         // is counted for here, and more splits of the same length.)  Measured (us, the whole call,
         // unsplit / so; 8 heads x 128, 32 query heads): 8 requests of 16 new tokens, 4000 behind prefixes of 2000, 116 / 58, 8000 behind 175 / 78; two of 64 and
         // 8000 257 / 57; one of 40 and 20000, 2 heads, 566 / 66; one head of 256 and 7 query heads, 4 x 6 and 1400 99 / 34; 4 x 256 and 2000 168 / 172.
-        const uint64_t groups = std::min((uint64_t)b.n_reqs * m.row_tiles, (uint64_t)b.total_new * group / rows_each + b.n_reqs / 2u + 1u) * heads;
+        const uint64_t likely = m.row_tiles > 1u ? (uint64_t)b.total_new * group / rows_each + b.n_reqs / 2u + 1u : b.n_reqs;
+        const uint64_t groups = std::min((uint64_t)b.n_reqs * m.row_tiles, likely) * heads;
         const uint64_t tiles = (behind + 63u) / 64u;
         const bool last = !p.few_rows && p.prefix.splits == 1u;
         double best = INFINITY;
@@ -334,6 +336,12 @@ SharedSizes plan_shared(uint32_t heads, uint32_t dim, uint32_t block_size, const
             const double cost = (double)((groups * s + 255u) / 256u) * (double)((tiles + s - 1u) / s + 3u) * 2.5 + parts;
             if (cost < best) best = cost, m.splits = s;
         }
+        // Or each request reads its group's prefix by itself, in one launch: what prompts do with codes takes longer than reading them.  Measured (us,
+        // read once / so; 8 heads x 128, 32 query heads, three groups of 32 in all): 12 tokens behind 500 44.2 / 25.7, behind 2000 52.0 / 65.4; 64 behind
+        // 2000 132 / 84, behind 6000 277 / 216; 32-512 behind 500 258 / 174, behind 6000 1168 / 1022; one of 8 such, behind 6000 358 / 409.
+        const double alone_cost = (double)((groups + 255u) / 256u) * (double)((b.max_len + 63u) / 64u + 3u) * 2.5;
+        p.through = p.prefix.splits && alone_cost <= once + best + 6.0;
+        if (p.through) m.splits = 1u;
         const uint32_t length = m.splits > 1u ? std::max((behind + m.splits - 1u) / m.splits, b.max_len / 16u) : b.max_len;
         m.chunk = std::max(64u, (length + 63u) & ~63u);
         m.splits = p.splits = std::max(1u, (b.max_len + m.chunk - 1u) / m.chunk);

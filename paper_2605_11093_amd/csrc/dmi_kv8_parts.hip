@@ -73,6 +73,8 @@ void parts_kernel(AttendArgs a, PartsPlan p)
     uint32_t head = 0;
     [[maybe_unused]] int unit_at = 0;           // the request, or group
     [[maybe_unused]] uint32_t skipped = 0;      // kRest: blocks in front
+    [[maybe_unused]] uint32_t front = 0;        // kThrough: blocks that are read through front_row
+    [[maybe_unused]] int front_row = 0;
     int row0 = -1;
     const uint32_t units = PREFIX ? a.n_groups : a.b.n_reqs;
     if (p.counted) {
@@ -116,6 +118,7 @@ void parts_kernel(AttendArgs a, PartsPlan p)
         q.len -= shared;
         skipped = block_of(a.c, (uint32_t)shared >> 4);
     }
+    if constexpr (KIND == kThrough) front = block_of(a.c, (uint32_t)shared_tokens(a, unit_at, q, front_row) >> 4);
     const int older = PREFIX ? q.len - 1 : q.len - q.fresh, last_row = min(row0 + 32 * NW, rows) - 1;
     // tokens that the workgroup's last row sees (of a prefix all rows see all)
     const int seen = PREFIX ? q.len : older + last_row / (int)a.group + 1;
@@ -184,7 +187,7 @@ void parts_kernel(AttendArgs a, PartsPlan p)
         const int t = begin + 1024 * batch + 16 * lane;
         const uint32_t block = block_of(a.c, (uint32_t)t >> 4);
         const uint32_t column = KIND == kRest ? block + skipped : block;
-        const int raw = a.c.table[(int64_t)q.row * a.c.table_stride + min(column, a.c.max_blocks - 1u)];
+        const int raw = a.c.table[(int64_t)(KIND == kThrough && block < front ? front_row : q.row) * a.c.table_stride + min(column, a.c.max_blocks - 1u)];
         const bool there = t < end && column < a.c.max_blocks && (uint32_t)raw < a.c.n_blocks;
         const int entry = there ? raw : 0;
         const int64_t at = (int64_t)entry * a.c.block_stride + (int64_t)((uint32_t)t - block * a.c.bs) * a.c.slot_stride + (int64_t)head * a.c.head_stride;
@@ -498,7 +501,7 @@ void parts_kernel(AttendArgs a, PartsPlan p)
     l += __shfl_xor(l, 32);
     const int64_t at = (int64_t)(q.start + w.token) * a.q_heads + w.head;
     const bool empty = m == -INFINITY && l == 0.0f;
-    if (KIND == kLast || (KIND == kWhole && p.splits == 1)) {
+    if (KIND == kLast || KIND == kThrough || (KIND == kWhole && p.splits == 1)) {
         // Rows are put together in LDS, so that a store writes whole ones: as the lanes hold them it would write 16 bytes here and there.
         const float f = __builtin_ldexpf(empty ? 0.0f : 1.0f / l, ref);
         const int64_t dst = (int64_t)(q.start + w.token) * a.out.row_stride + (int64_t)w.head * a.out.head_stride;
@@ -842,6 +845,7 @@ hipError_t launch_parts(const AttendArgs &a, const PartsPlan &p, uint32_t dtype,
 hipError_t launch_parts_apart(const AttendArgs &a, const PartsPlan &p, Kind kind, uint32_t dtype, hipStream_t s)
 {
     if (kind == kLast) return dtype == DMI_DTYPE_BF16 ? parts_of<Bf16, kLast>(a, p, s) : parts_of<Fp16, kLast>(a, p, s);
+    if (kind == kThrough) return dtype == DMI_DTYPE_BF16 ? parts_of<Bf16, kThrough>(a, p, s) : parts_of<Fp16, kThrough>(a, p, s);
     if (kind == kPrefix) return dtype == DMI_DTYPE_BF16 ? parts_of<Bf16, kPrefix>(a, p, s) : parts_of<Fp16, kPrefix>(a, p, s);
     return dtype == DMI_DTYPE_BF16 ? parts_of<Bf16, kRest>(a, p, s) : parts_of<Fp16, kRest>(a, p, s);
 }
@@ -902,7 +906,7 @@ hipError_t launch_shared(const AttendArgs &a, const SharedPlan &p, uint32_t dtyp
         e = p.few_rows ? launch_tokens_apart(a, p.prefix_few, kPrefix, dtype, s) : launch_parts_apart(a, p.prefix, kPrefix, dtype, s);
         if (e != hipSuccess) return e;
     }
-    e = p.tokens ? launch_tokens_apart(a, p.few, kRest, dtype, s) : launch_parts_apart(a, p.many, kRest, dtype, s);
+    e = p.tokens ? launch_tokens_apart(a, p.few, kRest, dtype, s) : launch_parts_apart(a, p.many, p.through ? kThrough : kRest, dtype, s);
     if (e != hipSuccess) return e;
     if (p.through || (p.tokens && p.few.before)) return hipSuccess;
     if (p.last) {

@@ -267,3 +267,28 @@ def test_prefixes_that_the_others_rows_do_not_list(B, monkeypatch, once):       
     B.kv8_attend_shared(s.cache, s.batch, s.prefix, q, out, lse=lse, stream=_stream())
     K.near(lse.cpu().numpy(), l, dl, "lse")
     K.near(out.float().cpu().numpy(), o, do, "out")
+
+
+@pytest.mark.parametrize("dtype,heads,group,dim,requests,new", [(BF16, 16, 4, 256, 80, 1), (FP16, 32, 1, 128, 90, 1), (BF16, 32, 4, 64, 150, 1), (BF16, 8, 4, 128, 200, 10)])
+def test_unsplit_prefixes_that_many_requests_read_once(B, dtype, heads, group, dim, requests, new):        # noqa: F811
+    """They go on from the sums of what is behind them; some requests share nothing."""
+    s = Shared(B, 100, [(245, [(new, 246 + new + i % 9) for i in range(requests)] + [(1, 30), (0, 250)])], heads, dim, 16, alone=(2, 1))
+    _check_shared(B, s, dtype, group)
+
+
+@pytest.mark.parametrize("dtype,heads,group,dim", [(BF16, 1, 4, 128), (FP16, 2, 7, 64), (BF16, 3, 4, 256), (FP16, 8, 4, 96)])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_short_prefixes_of_prompts(B, dtype, heads, group, dim, in_place):        # noqa: F811
+    """Each prompt reads them by itself, through the first request's row: prefixes of a block, of none, that end inside of a tile, that a request is
+    too short for, and what is no number in one."""
+    s = Shared(B, 101, [(16, [(20, 40), (90, 106)]), (200, [(40, 240), (130, 330), (33, 190), (0, 210), (1, 201)]), (0, [(50, 50)])], heads, dim, 16, alone=(1, 2))
+    s.v[s.table[s.rows[3], 11].item(), 3, 0, 9] = 0x7F
+    cpu = s.cpu()
+    q, qn = s.values(heads * group, dtype, 1.3)
+    for r, n in ((2, 1), (4, 12), (7, 12)):
+        s.table[s.rows[r], :n] = -1
+    out, lse = q if in_place else torch.empty_like(q), torch.empty(q.shape[:2], device=DEV)
+    B.kv8_attend_shared(s.cache, s.batch, s.prefix, q, out, lse=lse, stream=_stream())
+    (o, l, _), (do, dl, _) = K.attend(cpu, s.spans, qn, dim ** -0.5, group, dtype)
+    K.near(lse.cpu().numpy(), l, dl, "lse")
+    K.near(out.float().cpu().numpy(), o, do, "out")
