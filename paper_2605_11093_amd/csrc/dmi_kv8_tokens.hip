@@ -68,8 +68,10 @@ template <bool WHOLE> __device__ __forceinline__ int64_t part_at(const AttendArg
 // instead of 238 at that time).
 constexpr int waves_of(int dp, int nt, bool whole) { return !whole || dp * nt > 128 ? 4 : 8; }
 
+// Two wavefronts a SIMD where there is a start and an end for little in between (us, one / two: behind 2000 shared tokens, 128 requests of 5 tokens with up
+// to 1000 of their own, two tiles of rows x 128, 120 / 92, of one, 256 elements, 115 / 105; 32480 listed 112 tokens x 256 410 / 335).
 template <typename T, int DP, int NT, bool WHOLE, Kind KIND = kWhole, int NW = waves_of(DP, NT, WHOLE)>
-__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DP * NT <= 128 ? 2 : 1)))
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DP * NT <= 128 || KIND != kWhole ? 2 : 1)))
 void tokens_kernel(AttendArgs a, TokensPlan p)
 {
     constexpr int KL = DP / 64;                 // 16-byte loads of K a lane and sixteen
