@@ -627,16 +627,19 @@ template <typename T, int DP> static hipError_t select(SelectArgs a, hipStream_t
     // 128, 2000 29 / 31, 256, 2000 34 / 47, 512, 2000 73 / 95, 8, 7000 72 / 23, 128, 7000 98 / 81.
     const bool fused = a.stride <= kMostInLds && (a.stride <= 1024u || items >= a.stride / 16u);
     if (!launchable(items + 8u * a.c.heads, kMany) || !launchable(items * per, kScoreThreads)) return hipErrorInvalidConfiguration;
-    // Many tokens of few requests: two or four of a request at a time, while there are four workgroups for every compute unit and their scores take no
-    // more LDS than leaves two (heads of 64: three) of them resident.  Measured (us, one at a time / so; requests x tokens x heads, query heads each,
-    // blocks): heads of 128, 1 x 512 x 8, 4, 1875 252 / 158, 4 x 256 x 8, 4, 500 111 / 93, 1 x 2048 x 8, 8, 625 393 / 336, 4 x 190 x 16, 1, 3125
-    // 1214 / 673; of 64, 4 x 190 x 16, 4, 3200 776 / 490, 16 x 64 x 8, 1, 250 85 / 61; of 256, 16 x 64 x 8, 2, 250 222 / 135.  Of 2048 tokens and heads
-    // 28 / 34, with 250 blocks 35 / 40: one at a time.  Eight at a time took 140 where four take 111 (16 x 64 x 8, 1, 1000) and 54 where they take 61.
+    // Many tokens of few requests: four of a request at a time (two, where eight query heads leave room for no more), while there are four workgroups for
+    // every compute unit (two over many blocks, one of 256 elements) and their scores take no more LDS than leaves two (heads of 64: three) resident.
+    // Measured (us, one at a time / so; requests x tokens x heads, query heads each, blocks): heads of 128, 1 x 512 x 8, 4, 1875 252 / 158, 4 x 256 x 8, 4,
+    // 500 111 / 93, 1 x 2048 x 8, 8, 625 393 / 336, 4 x 190 x 16, 1, 3125 1214 / 673, 4 x 64 x 8, 4, 312 38 / 35, 1375 105 / 64, 6250 423 / 306; of 64, 4 x 190 x
+    // 16, 4, 3200 776 / 490, 16 x 64 x 8, 1, 250 85 / 61, 4 x 40 x 8, 1, 1375 60 / 48; of 256, 16 x 64 x 8, 2, 250 222 / 135, 4 x 58 x 8, 4, 206 59 / 44, 3125
+    // 422 / 221.  Fewer blocks, two at a time: 5 x 154 x 4, 7, 102 22 / 29, 4 x 172 x 8, 7, 283 75 / 79.  Fewer tokens: 2048 and heads of 128 with 62 blocks 28 / 34, 1600, two at a time, with 312 34 / 41, with 1625 110 / 105: one at a time.  Eight
+    // took 140 where four take 111 (16 x 64 x 8, 1, 1000) and 54 where they take 61.
     a.several = 1u;
-    if (fused && a.b.starts && a.group <= 8u && a.stride > a.n_select && items >= (DP <= 128 ? 4096u : 2048u)) {
+    if (fused && a.b.starts && a.group <= 8u && a.stride > a.n_select) {
+        const uint64_t least = DP > 128 ? 256u : a.stride >= 300u ? 512u : 1024u;
         uint32_t several = a.group <= 4u ? 4u : 2u;
-        while (several > 1u && (several * a.stride * 4u > (DP <= 64 ? 32768u : 53248u) || (uint64_t)several * a.b.n_reqs > a.b.total_new || items / several < 1024u)) several /= 2u;
-        a.several = several;
+        while (several > 1u && (several * a.stride * 4u > (DP <= 64 ? 32768u : 53248u) || (uint64_t)several * a.b.n_reqs > a.b.total_new)) several /= 2u;
+        if (items / several >= least && a.stride >= (several == 4u ? 48u : DP <= 128 ? 400u : 128u)) a.several = several;
     }
     const uint32_t lds = a.stride > a.n_select && a.stride <= kMostInLds ? a.stride * 4u : 0u;
     if (a.several > 1u) {

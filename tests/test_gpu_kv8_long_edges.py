@@ -167,17 +167,17 @@ def test_many_rows_in_front_of_long_rests_of_unequal_length(B, dtype, heads, gro
     _check_shared(B, s, dtype, group)
 
 
-def _several(B, seed, heads, dim, block=16, **more):        # noqa: F811
+def _several(B, seed, heads, dim, blocks, block=16, **more):        # noqa: F811
     """Requests with enough tokens for one pass over the bounds to serve several of them; chunks of tokens that end inside of a request, hold
-    several of them, and a context of a single block."""
+    several of them, a context of a single block and one of many."""
     n = 4300 // heads
-    return Setup(B, seed, [(1, 12 * block), (n // 2, n // 2 + 11 * block), (0, 5), (3, 9 * block + 1), (1, 1), (n - n // 2, n - n // 2 + 6 * block)],
+    return Setup(B, seed, [(1, 12 * block), (n // 2, n // 2 + 11 * block), (0, 5), (3, blocks * block - 1), (1, 1), (n - n // 2, n - n // 2 + 6 * block)],
                  heads, dim, block, bad=[(1, 4), (5, 3)], **more)
 
 
 @pytest.mark.parametrize("dtype,heads,group,dim", [(BF16, 32, 1, 64), (FP16, 32, 3, 80), (BF16, 16, 2, 256), (FP16, 32, 8, 16), (BF16, 24, 5, 128)])
 def test_selections_of_many_tokens(B, dtype, heads, group, dim):        # noqa: F811
-    s = _several(B, 94, heads, dim, seqs=9)
+    s = _several(B, 94, heads, dim, 60 if group < 5 else 410, seqs=9)
     _check_select(B, s, dtype, group, 7, 1, 2)
     bounds = np.full((s.k.shape[0], heads, 2, dim), 0x38, dtype=np.uint8)
     bounds[s.rng.integers(0, len(bounds), 9)] = 0x40
@@ -202,7 +202,7 @@ def test_selections_of_many_tokens_whose_scores_lie_close(B):        # noqa: F81
 
 def test_selections_of_many_tokens_of_any_size_and_rows_of_no_request(B):        # noqa: F811
     """Queries far apart, infinite or no number in one pass; rows behind max_new in the middle of a pass are left."""
-    s = _several(B, 96, 32, 64)
+    s = _several(B, 96, 32, 64, 60)
     most = max(new for _, _, new, _ in s.spans) - 5
     s.batch = B.KV8Batch(s.lens, starts=s.starts_dev, rows=s.rows_dev, total_new=s.total, max_new=most, max_len=s.max_len)
     s.spans = [(row, start, min(new, most), length) for row, start, new, length in s.spans]
