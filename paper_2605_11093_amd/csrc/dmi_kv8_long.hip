@@ -347,10 +347,10 @@ SharedSizes plan_shared(uint32_t heads, uint32_t dim, uint32_t block_size, const
         m.splits = p.splits = std::max(1u, (b.max_len + m.chunk - 1u) / m.chunk);
     }
     // Nothing split: the sums of what is behind the prefix are where the prefix begins, and its end writes outputs (32 prompts behind 4000
-    // tokens 753 us; 810 with a part of every row more to write, and two to read).
+    // tokens, read once, 753 us; 810 with a part of every row more to write, and two to read).
     p.last = !p.few_rows && p.prefix.splits == 1u && p.splits == 1u && !p.through;
     // Few rows behind it that nothing splits: their workgroups read its parts and write outputs (64 tokens behind 8192: 55.6 us with a
-    // launch that joins, 53.4 without; 24 x 3 in four groups 23.9 and 20.9).
+    // launch that joins, 53.4 without).
     p.few.before = p.tokens && p.splits == 1u && !p.last && !p.through;
     const uint64_t parts = p.last || p.through ? 0u : rows * p.prefix.splits;
     z.prefix_parts = pad64(parts * 8u);

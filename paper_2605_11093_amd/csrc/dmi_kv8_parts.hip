@@ -851,9 +851,9 @@ hipError_t launch_parts_apart(const AttendArgs &a, const PartsPlan &p, Kind kind
 }
 
 // ---------------------------------------------------------------- contexts behind shared prefixes
-// Prefixes that groups share: 32 prompts, 8700 tokens of 32 query heads behind one prefix of 4000, 545 GFLOP in 700 us by parts_kernel (kLast, 780
-// TFLOP/s), their own tokens 88; 64 single tokens behind 8192, 256 rows a head in 26 splits 24 us: 5 until the first tile, 2.4 each of five, 7 to
-// write 27 MB of parts.
+// Prefixes that groups share: 32 prompts, 8700 tokens of 32 query heads behind one of 4000, 545 GFLOP, read by each (kThrough) 670 to 770 us by card;
+// read once 700 (kLast), and 88 for their own tokens in front.  64 single tokens behind 8192, 256 rows a head in 26 splits 22 us: 5 until the first
+// tile, 2.4 each of five, 7 to write 27 MB of parts.
 //
 // Outputs out of the parts of prefixes and of what is behind them (p.last: of requests that share nothing, the others' are written already):
 // see join_parts_kernel.
