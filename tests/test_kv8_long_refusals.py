@@ -131,8 +131,9 @@ def test_sizes_that_are_refused_have_no_workspace():
     assert B.kv8_attend_blocks_workspace(c, _batch(), 2 * 33, 8) == 0
     p = B.KV8Prefix(torch.zeros(2, dtype=I32), torch.zeros(1, dtype=I32), max_prefix=1 << 25)
     assert B.kv8_attend_shared_workspace(c, _batch(), p, 4) == 0
-    p = B.KV8Prefix(torch.zeros(2, dtype=I32), torch.zeros(1, dtype=I32), max_prefix=32)
-    assert B.kv8_attend_shared_workspace(c, _batch(), p, 3) == 0 and B.kv8_attend_shared_workspace(c, _batch(), p, 80) > 0
+    p = B.KV8Prefix(torch.zeros(2, dtype=I32), torch.zeros(1, dtype=I32), max_prefix=1 << 20)
+    c, b = _cache(per=1 << 16), _batch(max_len=1 << 20)
+    assert B.kv8_attend_shared_workspace(c, b, p, 3) == 0 and B.kv8_attend_shared_workspace(c, b, p, 4) > 0
 
 
 def test_attention_over_listed_blocks():
@@ -153,8 +154,8 @@ def test_attention_over_listed_blocks():
 
 def test_attention_behind_shared_prefixes():
     c, b = _cache(), _batch()
-    p = B.KV8Prefix(torch.zeros(2, dtype=I32), torch.zeros(1, dtype=I32), max_prefix=32)
-    _refused("workspace", B.kv8_attend_shared, c, b, p, _x(80), _x(80), workspace=torch.zeros(8, dtype=torch.uint8))
+    p = B.KV8Prefix(torch.zeros(2, dtype=I32), torch.zeros(1, dtype=I32), max_prefix=1 << 20)
+    _refused("workspace", B.kv8_attend_shared, _cache(per=1 << 16), _batch(max_len=1 << 20), p, _x(4), _x(4), workspace=torch.zeros(8, dtype=torch.uint8))
     p._raw = B._PACK_KV8_PREFIX(1, 32, 0, 0)
     _refused("group_starts_dev", B.kv8_attend_shared, c, b, p, _x(4), _x(4), workspace=torch.zeros(1 << 20, dtype=torch.uint8))
     p._raw = B._PACK_KV8_PREFIX(1 << 17, 32, 8, 8)
