@@ -107,7 +107,7 @@ typedef struct {
  * dmi_kv8_attend (without weights) for such groups.  The whole blocks of a prefix that lie in front of the first request's new tokens are
  * read once for the group, through that request's row of the block table (the others' rows need not list them), by every request that has as
  * many tokens in front of its new ones.  All other tokens, and all tokens of a request that has not, are read through its own row.
- * (Where that takes less time, short prefixes of few requests, each reads them by itself, through that row too.)
+ * (Where that takes less time, each request reads them by itself, through that row too.)
  */
 uint64_t dmi_kv8_attend_shared_workspace(const dmi_kv8_t *cache /*[host]*/, const dmi_kv8_batch_t *batch /*[host]*/,
                                          const dmi_kv8_prefix_t *prefix /*[host]*/, uint32_t n_q_heads);
