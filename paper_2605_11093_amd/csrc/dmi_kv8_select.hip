@@ -155,6 +155,13 @@ __device__ __forceinline__ float counted(float best, float scale)
     const float v = best * scale;
     return scale != 0.0f && fabsf(v) < INFINITY ? v + 0.0f : -INFINITY;
 }
+// How far that may be off, `wide` before K's scale.  A scale that takes a number out of fp32's range says nothing about it: it is looked at in 64
+// bits, and as long as scores are not exact there is an error, however small (one that fp32 has no number for counted as none).
+__device__ __forceinline__ float off_of(float wide, float best, float scale)
+{
+    if (fabsf(best) < INFINITY && fabsf(best * scale) == INFINITY) return INFINITY;
+    return scale != 0.0f && wide > 0.0f ? fmaxf(wide * scale, 0x1p-126f) : 0.0f;
+}
 
 // A score in 64 bits, as an unsigned number in their order: a wavefront's work, 16 lanes a query row.
 template <typename T> __device__ __forceinline__ uint64_t exact_order(const SelectArgs &a, const Request &q, uint32_t token, uint32_t head, uint32_t block)
@@ -320,7 +327,7 @@ template <typename T, int DP> __global__ __launch_bounds__(kScoreThreads) __attr
 #pragma unroll
     for (uint32_t y = 0; y < 2u; y++) {
         const uint32_t block = block0 + 16u * y + 4u * (uint32_t)scorer.g + (uint32_t)scorer.col;
-        if (scorer.col < 4 && block < x.hi) a.scores[(int64_t)item * a.stride + block] = f32x2{counted(s[y], tile[y].scale), scorer.off * tile[y].scale};
+        if (scorer.col < 4 && block < x.hi) a.scores[(int64_t)item * a.stride + block] = f32x2{counted(s[y], tile[y].scale), off_of(scorer.off, s[y], tile[y].scale)};
     }
 }
 
@@ -494,11 +501,10 @@ __global__ __launch_bounds__(N) __attribute__((amdgpu_waves_per_eu(DP <= 128 ? 4
                 const uint32_t next = base + N / 4u;
                 if (next < count) tile = scorer.fetch(entries(next));
                 float v = scorer.of(here);
-                off = fmaxf(off, scorer.off * here.scale);      // (no number where there is no block and no bound: left out)
                 const uint32_t i = base + 4u * (uint32_t)scorer.g + (uint32_t)scorer.col;
                 if (scorer.col < 4 && i < count) {
                     if (row0) v = fmaxf(v, own[i]);
-                    if (row0 + 16u >= a.group) v = counted(v, here.scale), look(v);
+                    if (row0 + 16u >= a.group) off = fmaxf(off, off_of(scorer.off, v, here.scale)), v = counted(v, here.scale), look(v);
                     own[i] = v;
                 }
                 if (next >= count) break;
@@ -575,7 +581,7 @@ __global__ __launch_bounds__(N) __attribute__((amdgpu_waves_per_eu(DP <= 64 ? 4 
                     const uint32_t block = base + 4u * (uint32_t)scorer.g;
                     if (each >= 4u) {           // one of four lanes' blocks
                         const float w = row & 2u ? row & 1u ? v[3] : v[2] : row & 1u ? v[1] : v[0];
-                        if (row < 4u && block + row < count) to[block + row] = counted(w, here.scale), off = fmaxf(off, wide * here.scale);
+                        if (row < 4u && block + row < count) to[block + row] = counted(w, here.scale), off = fmaxf(off, off_of(wide, w, here.scale));
                     } else {
                         const int x = __float_as_int(here.scale);
                         const float scale[4] = {__int_as_float(__builtin_amdgcn_update_dpp(0, x, 0x00, 0xF, 0xF, false)),
@@ -584,7 +590,7 @@ __global__ __launch_bounds__(N) __attribute__((amdgpu_waves_per_eu(DP <= 64 ? 4 
                                                 __int_as_float(__builtin_amdgcn_update_dpp(0, x, 0xFF, 0xF, 0xF, false))};
 #pragma unroll
                         for (uint32_t i = 0; i < 4u; i++)
-                            if ((i & (each - 1u)) == row && block + i < count) to[block + i] = counted(v[i], scale[i]), off = fmaxf(off, wide * scale[i]);
+                            if ((i & (each - 1u)) == row && block + i < count) to[block + i] = counted(v[i], scale[i]), off = fmaxf(off, off_of(wide, v[i], scale[i]));
                     }
                     if (next >= most_blocks) break;
                     base = next;

@@ -292,3 +292,22 @@ def test_short_prefixes_of_prompts(B, dtype, heads, group, dim, in_place):      
     (o, l, _), (do, dl, _) = K.attend(cpu, s.spans, qn, dim ** -0.5, group, dtype)
     K.near(lse.cpu().numpy(), l, dl, "lse")
     K.near(out.float().cpu().numpy(), o, do, "out")
+
+
+@pytest.mark.parametrize("path", ["one launch", "two", "several tokens", "more rows than a tile"])
+@pytest.mark.parametrize("dtype,size,least,most", [(BF16, 2.0, 104, 121), (FP16, 2.0, 104, 121), (BF16, 2.0 ** 60, 50, 70), (BF16, 2.0 ** -60, -115, -85), (BF16, 2.0 ** -60, -126, -100),
+                                                   (FP16, 2.0 ** -10, -126, -110), (BF16, 2.0 ** -45, -126, 120)])
+def test_selections_of_scores_past_the_range_of_fp32(B, path, dtype, size, least, most):        # noqa: F811
+    """Queries and scales of any size, which 64 bits have room for and fp32 has not; largest scores that are above it among others that are not,
+    and nothing but such as are nothing in it.  (Below zero too: those above fp32's range are then the least.)"""
+    if path == "several tokens":
+        s, group = _several(B, 102, 32, 64, 60), 2
+    else:
+        s, group = Setup(B, 103, [(1, 16 * (1500 if path == "two" else 90)), (1, 16 * 40)], 1, 64, 16), 20 if path == "more rows than a tile" else 3
+    s.k_scale.copy_(torch.from_numpy((2.0 ** s.rng.integers(least, most, s.k_scale.shape)).astype(np.float32)))
+    bounds = K.nearest_code(np.sort(s.rng.normal(size=(s.k.shape[0], s.heads, 2, 64)) * 60 + 20, axis=2))
+    bounds[s.rng.random(len(bounds)) < 0.1, :, :, 7] = 0x7F
+    for sign in (1.0, -1.0):
+        q = (torch.from_numpy(np.abs(s.rng.normal(size=(s.total, s.heads * group, 64)))) * (sign * size)).to(dtype)
+        for n_select in (7, 36):
+            _check_select(B, s, dtype, group, n_select, 1, 1, bounds=bounds, q=(q.to(DEV), q.double().numpy()))
