@@ -632,7 +632,6 @@ template <typename T, int DP> static hipError_t select(SelectArgs a, hipStream_t
     // over more workgroups otherwise.  Measured (us, one launch / two; tokens x heads, blocks): 8, 500 15 / 19, 128, 500 15 / 20, 8, 2000 27 / 20,
     // 128, 2000 29 / 31, 256, 2000 34 / 47, 512, 2000 73 / 95, 8, 7000 72 / 23, 128, 7000 98 / 81.
     const bool fused = a.stride <= kMostInLds && (a.stride <= 1024u || items >= a.stride / 16u);
-    if (!launchable(items + 8u * a.c.heads, kMany) || !launchable(items * per, kScoreThreads)) return hipErrorInvalidConfiguration;
     // Many tokens of few requests: four of a request at a time (two, where eight query heads leave room for no more), while there are four workgroups for
     // every compute unit (two over many blocks, one of 256 elements) and their scores take no more LDS than leaves two (heads of 64: three) resident.
     // Measured (us, one at a time / so; requests x tokens x heads, query heads each, blocks): heads of 128, 1 x 512 x 8, 4, 1875 252 / 158, 4 x 256 x 8, 4,
@@ -649,18 +648,21 @@ template <typename T, int DP> static hipError_t select(SelectArgs a, hipStream_t
     }
     const uint32_t lds = a.stride > a.n_select && a.stride <= kMostInLds ? a.stride * 4u : 0u;
     if (a.several > 1u) {
-        const uint32_t groups = (a.b.total_new + a.several - 1u) / a.several * a.c.heads;
-        pick_several_kernel<T, DP, 256><<<groups, 256, a.several * a.stride * 4u, s>>>(a);
+        const uint64_t groups = ((uint64_t)a.b.total_new + a.several - 1u) / a.several * a.c.heads;
+        if (!launchable(groups, 256)) return hipErrorInvalidConfiguration;
+        pick_several_kernel<T, DP, 256><<<(uint32_t)groups, 256, a.several * a.stride * 4u, s>>>(a);
         return hipGetLastError();
     }
     if (fused) {
         // Workgroups of eight wavefronts while all of them are resident, of four beyond (us, four / eight: 256, 500 18 / 16, 512, 500 22 / 22, 1024 of
         // up to 512 27 / 32).
-        const uint32_t groups = (a.b.total_new + 7u) / 8u * 8u * a.c.heads;
-        if (items <= 512u) pick_kernel<T, DP, true, 512><<<groups, 512, lds, s>>>(a);
-        else pick_kernel<T, DP, true, 256><<<groups, 256, lds, s>>>(a);
+        const uint64_t groups = ((uint64_t)a.b.total_new + 7u) / 8u * 8u * a.c.heads;
+        if (!launchable(groups, items <= 512u ? 512 : 256)) return hipErrorInvalidConfiguration;
+        if (items <= 512u) pick_kernel<T, DP, true, 512><<<(uint32_t)groups, 512, lds, s>>>(a);
+        else pick_kernel<T, DP, true, 256><<<(uint32_t)groups, 256, lds, s>>>(a);
         return hipGetLastError();
     }
+    if (!launchable(items, kMany) || (a.stride > a.n_select && !launchable(items * per, kScoreThreads))) return hipErrorInvalidConfiguration;
     if (a.stride > a.n_select) {
         score_kernel<T, DP><<<(uint32_t)(items * per), kScoreThreads, 0, s>>>(a);
         const hipError_t e = hipGetLastError();

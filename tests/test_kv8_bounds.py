@@ -164,3 +164,32 @@ def test_new_lengths_inside_the_lengths():
         with pytest.raises(B.DmiError, match="lens_dev") as e:
             B.kv8_evict(c, B.KV8Batch(lens, max_len=64), w[0], to, w[1], keep=16, recent=4, positions=positions, lens=new)
         assert e.value.code == B.ERR_INVALID_ARG
+
+
+def _select(reqs, total, length, *, heads=8, group=4, n_select=64, call=True):
+    """dmi_kv8_select's status (or its workspace) for `total` new tokens over up to `length`, by addresses that nothing looks at."""
+    at = _pointer()
+    cache = B._PACK_KV8(at, at, at, at, 16 * heads * 128, heads * 128, 128, heads, 1, 16, heads, 128, 1, reqs, length // 16, at, length // 16)
+    batch = B._PACK_KV8_BATCH(reqs, total, total, length, at, at, 0)
+    if not call:
+        return B.lib().dmi_kv8_select_workspace(cache, batch, n_select)
+    q = B._PACK_KV8_HEADS(at, B.DT_BF16, heads * group * 128, 128)
+    return B.lib().dmi_kv8_select(cache, batch, B._PACK_KV8_BOUNDS(at, heads * 256, 256), q, heads * group, n_select, 1, 2, at, 256, 1 << 62, None)
+
+
+NO_DEVICE = pytest.mark.skipif(torch.cuda.is_available(), reason="launches by addresses that are none")
+
+
+@NO_DEVICE
+@pytest.mark.parametrize("reqs,total,length,group", [
+    (1, 32768, 131072, 4),              # a part of a long prompt, one launch
+    (1, 1 << 19, 131072, 4), (64, 1 << 20, 16 * 3000, 4), (4, 1 << 21, 16 * 3000, 2), (1, 4000000, 16 * 1000, 8)])
+def test_select_of_no_more_workgroups_than_a_launch_has(reqs, total, length, group):
+    """What a path launches is what it is refused for, not what another one would: only a device is missing."""
+    assert _select(reqs, total, length, call=False) > 0
+    assert _select(reqs, total, length, group=group) == B.ERR_HIP, B.lib().dmi_last_error()
+
+
+@pytest.mark.parametrize("reqs,total,length", [(1, 1 << 24, 131072), (4, 1 << 23, 16 * 3000), (1, 1 << 17, 16 * 400000)], ids=["one launch", "several", "two"])
+def test_select_past_the_workgroups_of_a_launch(reqs, total, length):
+    assert _select(reqs, total, length) == B.ERR_INVALID_ARG and b"launch" in B.lib().dmi_last_error()
