@@ -87,7 +87,7 @@ struct SelectArgs {
     int64_t bounds_block_stride, bounds_head_stride;
     uint32_t group, n_select, n_first, n_recent;
     uint32_t stride;                            // blocks of the longest request
-    f32x2 *scores;                              // [new token][head][stride]: a score, how far it may be off
+    f32x2 *scores;                              // [new token][head][stride]: a score, how far it may be off; one launch: unused
     uint64_t *keys;                             // the same places: scores in 64 bits, as unsigned numbers in their order
     int32_t *blocks;
     uint32_t several;                           // tokens that a pass over the bounds is for
@@ -165,6 +165,13 @@ struct SharedPlan {
     f32x2 *sums;                                // [row of out][split]
     float *parts;
 };
+
+// Whether a selection, of `items` new tokens and heads over up to `blocks` blocks each, takes one launch, with scores in LDS: where a
+// workgroup goes through a head's blocks in the time that a second launch takes, or there are workgroups enough; scores over more workgroups, and
+// in memory, otherwise.  Measured (us, one launch / two; tokens x heads, blocks): 8, 500 15 / 19, 128, 500 15 / 20, 8, 2000 27 / 20, 128, 2000 29 / 31,
+// 256, 2000 34 / 47, 512, 2000 73 / 95, 8, 7000 72 / 23, 128, 7000 98 / 81.
+constexpr uint32_t kMostInLds = 8192;           // blocks whose scores a workgroup keeps
+inline bool selects_in_one(uint64_t items, uint32_t blocks) { return blocks <= kMostInLds && (blocks <= 1024u || items >= blocks / 16u); }
 
 // What a launch may have in its first dimension: threads are counted in 32 bits.  A call whose launches need more is refused before
 // the first of them (hipErrorInvalidConfiguration).

@@ -144,10 +144,16 @@ dmi_status_t check_select(const dmi_kv8_t &cache, const dmi_kv8_batch_t &b, uint
     return DMI_OK;
 }
 
-uint64_t select_bytes(const dmi_kv8_t &cache, const dmi_kv8_batch_t &b, uint32_t n_select)
+// (scores first, of two launches; then the words that they are ranked by)
+struct SelectBytes {
+    uint64_t scores, all;
+};
+SelectBytes select_bytes(const dmi_kv8_t &cache, const dmi_kv8_batch_t &b, uint32_t n_select)
 {
     const uint32_t stride = score_stride(cache, b);
-    return stride > n_select ? 2u * pad64((uint64_t)b.total_new * cache.n_heads * stride * 8u) : 0u;
+    const uint64_t items = (uint64_t)b.total_new * cache.n_heads, each = stride > n_select ? pad64(items * stride * 8u) : 0u;
+    const uint64_t scores = selects_in_one(items, stride) ? 0u : each;
+    return {scores, scores + each};
 }
 
 }  // namespace
@@ -157,7 +163,7 @@ extern "C" uint64_t dmi_kv8_select_workspace(const dmi_kv8_t *cache, const dmi_k
     if (!cache || !batch || check_shape(cache, "cache") != DMI_OK || check_counts(batch, true) != DMI_OK ||
         check_select(*cache, *batch, n_select) != DMI_OK)
         return 0;
-    return select_bytes(*cache, *batch, n_select);
+    return select_bytes(*cache, *batch, n_select).all;
 }
 
 extern "C" dmi_status_t dmi_kv8_select(const dmi_kv8_t *cache, const dmi_kv8_batch_t *batch, const dmi_kv8_bounds_t *bounds,
@@ -174,7 +180,8 @@ extern "C" dmi_status_t dmi_kv8_select(const dmi_kv8_t *cache, const dmi_kv8_bat
     if (!n_recent || n_first > n_select || n_recent > n_select - n_first)
         return fail(DMI_ERR_INVALID_ARG, "n_recent %u must be positive, and n_first %u and it no more than n_select %u", n_recent, n_first, n_select);
     if ((!blocks_dev && a.b.total_new) || (uintptr_t)blocks_dev % 4u) return fail(DMI_ERR_INVALID_ARG, "blocks_dev is NULL or not 4-byte aligned");
-    if ((st = check_workspace(select_bytes(*cache, *batch, n_select), workspace, workspace_bytes)) != DMI_OK) return st;
+    const SelectBytes bytes = select_bytes(*cache, *batch, n_select);
+    if ((st = check_workspace(bytes.all, workspace, workspace_bytes)) != DMI_OK) return st;
     if (!a.b.n_reqs || !a.b.total_new || !a.b.max_new) return DMI_OK;
     a.bounds = bounds->data;
     a.bounds_block_stride = bounds->block_stride;
@@ -183,7 +190,7 @@ extern "C" dmi_status_t dmi_kv8_select(const dmi_kv8_t *cache, const dmi_kv8_bat
     a.n_select = n_select, a.n_first = n_first, a.n_recent = n_recent;
     a.stride = score_stride(*cache, *batch);
     a.scores = static_cast<f32x2 *>(workspace);
-    a.keys = reinterpret_cast<uint64_t *>(static_cast<char *>(workspace) + select_bytes(*cache, *batch, n_select) / 2u);
+    a.keys = reinterpret_cast<uint64_t *>(static_cast<char *>(workspace) + bytes.scores);
     a.blocks = blocks_dev;
     return launched(launch_select(a, q->dtype, (hipStream_t)hip_stream));
 }

@@ -212,7 +212,6 @@ template <typename T> __device__ __forceinline__ uint64_t exact_order(const Sele
 
 // ---------------------------------------------------------------- which blocks
 constexpr uint32_t kScoreThreads = 256, kBlocksAtOnce = kScoreThreads / 2;      // blocks of a workgroup
-constexpr uint32_t kMostInLds = 8192;                           // blocks whose scores a workgroup keeps
 constexpr uint32_t kPickBins = 2048;
 constexpr uint32_t kClose = 256;                                // blocks near the border that are ranked in LDS
 
@@ -628,10 +627,7 @@ template <typename T, int DP> static hipError_t select(SelectArgs a, hipStream_t
 {
     constexpr uint32_t kMany = DP <= 128 ? 1024 : 512;
     const uint64_t items = (uint64_t)a.b.total_new * a.c.heads, per = (a.stride + kBlocksAtOnce - 1u) / kBlocksAtOnce;
-    // One launch where a workgroup goes through a head's blocks in the time that a second one takes, or there are workgroups enough; scores
-    // over more workgroups otherwise.  Measured (us, one launch / two; tokens x heads, blocks): 8, 500 15 / 19, 128, 500 15 / 20, 8, 2000 27 / 20,
-    // 128, 2000 29 / 31, 256, 2000 34 / 47, 512, 2000 73 / 95, 8, 7000 72 / 23, 128, 7000 98 / 81.
-    const bool fused = a.stride <= kMostInLds && (a.stride <= 1024u || items >= a.stride / 16u);
+    const bool fused = selects_in_one(items, a.stride);
     // Many tokens of few requests: four of a request at a time (two, where eight query heads leave room for no more), while there are four workgroups for
     // every compute unit (two over many blocks, one of 256 elements) and their scores take no more LDS than leaves two (heads of 64: three) resident.
     // Measured (us, one at a time / so; requests x tokens x heads, query heads each, blocks): heads of 128, 1 x 512 x 8, 4, 1875 252 / 158, 4 x 256 x 8, 4,

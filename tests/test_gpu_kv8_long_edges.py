@@ -311,3 +311,25 @@ def test_selections_of_scores_past_the_range_of_fp32(B, path, dtype, size, least
         q = (torch.from_numpy(np.abs(s.rng.normal(size=(s.total, s.heads * group, 64)))) * (sign * size)).to(dtype)
         for n_select in (7, 36):
             _check_select(B, s, dtype, group, n_select, 1, 1, bounds=bounds, q=(q.to(DEV), q.double().numpy()))
+
+
+@pytest.mark.parametrize("path", ["one launch", "two", "several tokens"])
+def test_selections_write_nothing_behind_their_workspace(B, path):        # noqa: F811
+    """Scores of which more lie close to each other than a workgroup has room for go through all of it."""
+    if path == "several tokens":
+        s = Setup(B, 104, [(131, 300), (3, 16 * 301), (2, 16 * 290)], 32, 64, 16)
+    else:
+        s = Setup(B, 105, [(1, 16 * (1500 if path == "two" else 400)), (1, 16 * 333)], 2, 64, 16)
+    s.k_scale.fill_(0.25)
+    bounds = np.full((s.k.shape[0], s.heads, 2, 64), 0x7E, dtype=np.uint8)
+    bounds[:, :, :, -1] = np.sort(s.rng.integers(0, 4, size=bounds.shape[:3]), axis=2)
+    q = torch.ones((s.total, s.heads, 64), dtype=BF16, device=DEV)
+    q[..., -1] = 2.0 ** -12
+    need = B.kv8_select_workspace(s.cache, s.batch, 20)
+    room = torch.full((need + 8192,), 0x5A, dtype=torch.uint8, device=DEV)
+    got = torch.full((s.total, s.heads, 20), 77, dtype=torch.int32, device=DEV)
+    want = got.cpu().numpy().copy()
+    B.kv8_select(s.cache, s.batch, torch.from_numpy(bounds).to(DEV), q, got, first=1, recent=1, workspace=room[4096:4096 + need], stream=_stream())
+    L.select(s.cpu(), s.spans, bounds, q.double().cpu().numpy(), 1, 20, 1, 1, want)
+    np.testing.assert_array_equal(got.cpu().numpy(), want)
+    assert (room[:4096] == 0x5A).all() and (room[4096 + need:] == 0x5A).all()

@@ -193,3 +193,15 @@ def test_select_of_no_more_workgroups_than_a_launch_has(reqs, total, length, gro
 @pytest.mark.parametrize("reqs,total,length", [(1, 1 << 24, 131072), (4, 1 << 23, 16 * 3000), (1, 1 << 17, 16 * 400000)], ids=["one launch", "several", "two"])
 def test_select_past_the_workgroups_of_a_launch(reqs, total, length):
     assert _select(reqs, total, length) == B.ERR_INVALID_ARG and b"launch" in B.lib().dmi_last_error()
+
+
+@pytest.mark.parametrize("total,length", [(128, 8192), (3, 16 * 900), (32768, 131072), (760, 50000)])
+def test_workspace_of_a_selection_in_one_launch(total, length):
+    """Its scores lie in LDS: what it keeps in memory is a word of 8 bytes for each, and no more."""
+    assert total * 8 * (length // 16) * 8 <= _select(1, total, length, call=False) <= total * 8 * (length // 16) * 8 + 256
+
+
+@pytest.mark.parametrize("total,length", [(4, 16 * 7500), (3, 16 * 9000)])
+def test_workspace_of_a_selection_in_two_launches(total, length):
+    """Scores with what they may be off, and a word for each."""
+    assert _select(1, total, length, call=False) >= total * 8 * (length // 16) * 16
