@@ -861,11 +861,11 @@ template <typename T, Kind KIND> static hipError_t tokens_apart(const AttendArgs
     const uint32_t units = KIND == kListed ? a.b.total_new : KIND == kPrefix ? a.n_groups : a.b.n_reqs;
     const uint64_t pairs = (uint64_t)units * a.c.heads;
     const uint64_t groups = (KIND != kPrefix ? pairs : (p.by_xcd ? (pairs + 7u) / 8u * 8u : pairs) * p.row_tiles) * p.splits;
-    if (!launchable(groups, 512) || pairs > UINT32_MAX) return hipErrorInvalidConfiguration;
     auto launch = [&](auto dp_, auto nt_) {
         constexpr int DP = decltype(dp_)::value, NT = decltype(nt_)::value, many = waves_of(DP, NT, true);
         auto with = [&](auto waves) {
             constexpr int NW = decltype(waves)::value;
+            if (!launchable(groups, 64 * NW)) return hipErrorInvalidConfiguration;
             tokens_kernel<T, DP, NT, true, KIND, NW><<<(uint32_t)groups, 64 * NW, 0, s>>>(a, p);
             return hipGetLastError();
         };

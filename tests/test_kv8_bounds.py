@@ -205,3 +205,26 @@ def test_workspace_of_a_selection_in_one_launch(total, length):
 def test_workspace_of_a_selection_in_two_launches(total, length):
     """Scores with what they may be off, and a word for each."""
     assert _select(1, total, length, call=False) >= total * 8 * (length // 16) * 16
+
+
+def _attend(call, reqs, heads, total, new, length, *more, dim=64, starts=True):
+    """The status of an attention for long contexts, by addresses that nothing looks at."""
+    at = _pointer()
+    cache = B._PACK_KV8(at, at, at, at, 16 * heads * dim, heads * dim, dim, heads, 1, 16, heads, dim, 1, reqs, -(-length // 16), at, -(-length // 16))
+    batch = B._PACK_KV8_BATCH(reqs, total, new, length, at, at if starts else 0, 0)
+    q, out = (B._PACK_KV8_HEADS(at + x, B.DT_BF16, heads * dim, dim) for x in (0, 1 << 40))
+    if call == "blocks":
+        return B.lib().dmi_kv8_attend_blocks(cache, batch, at, more[0], q, heads, 1.0, out, None, 256, 1 << 62, None)
+    prefix = B._PACK_KV8_PREFIX(1, more[0], at, at)
+    return B.lib().dmi_kv8_attend_shared(cache, batch, prefix, q, heads, 1.0, out, None, 256, 1 << 62, None)
+
+
+@NO_DEVICE
+@pytest.mark.parametrize("total,heads,n_select", [(1 << 20, 8, 8), (1 << 20, 16, 64), (1 << 22, 8, 8)])
+def test_attend_blocks_of_no_more_workgroups_than_a_launch_has(total, heads, n_select):
+    """A wavefront for each of many lists is a workgroup of 64 threads: only a device is missing."""
+    assert _attend("blocks", 32, heads, total, total, 65536, n_select) == B.ERR_HIP, B.lib().dmi_last_error()
+
+
+def test_attend_blocks_past_the_workgroups_of_a_launch():
+    assert _attend("blocks", 32, 64, 1 << 21, 1 << 21, 65536, 8) == B.ERR_INVALID_ARG and b"launch" in B.lib().dmi_last_error()
