@@ -184,6 +184,7 @@ hipError_t launch_select(const SelectArgs &a, uint32_t dtype, hipStream_t s);
 hipError_t launch_evict(const EvictArgs &a, hipStream_t s);
 hipError_t launch_parts(const AttendArgs &a, const PartsPlan &p, uint32_t dtype, hipStream_t s);
 hipError_t launch_parts_apart(const AttendArgs &a, const PartsPlan &p, Kind kind, uint32_t dtype, hipStream_t s);
+bool tokens_apart_fit(const AttendArgs &a, const TokensPlan &p, Kind kind);        // whether a launch has workgroups enough
 hipError_t launch_shared(const AttendArgs &a, const SharedPlan &p, uint32_t dtype, hipStream_t s);
 hipError_t launch_tokens_apart(const AttendArgs &a, const TokensPlan &p, Kind kind, uint32_t dtype, hipStream_t s);
 hipError_t launch_tokens(const AttendArgs &a, const TokensPlan &p, uint32_t dtype, hipStream_t s);

@@ -797,24 +797,32 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 128 ?
     }
 }
 
-template <typename T, int DP, int NW, Kind KIND> static hipError_t parts(const AttendArgs &a, PartsPlan p, hipStream_t s)
+// Workgroups of a launch, of `waves` wavefronts each, and how they find their rows (p.counted, p.spread)
+static uint64_t groups_of(const AttendArgs &a, PartsPlan &p, Kind kind, uint32_t waves)
 {
     // Row tiles of an XCD at most: as many as the longest request makes, for each pair; as many as all rows make, and one for each request.
     // Where the second is less the kernel counts for itself: a workgroup that finds nothing to do has waited for a compute unit of its own.
     // Measured (us, first / second): one prompt of 8192 tokens among 63 single ones 2163 / 1387, one of 512 among 255 1031 / 284, 32 ragged
     // prompts 609 / 603; where all requests are alike counting costs some 0.7 us for every 64 of them, and is not done.
-    const uint64_t units = KIND == kPrefix || KIND == kLast ? a.n_groups : a.b.n_reqs;
+    const uint64_t units = kind == kPrefix || kind == kLast ? a.n_groups : a.b.n_reqs;
     const uint64_t by_pairs = (units * a.c.heads + 7u) / 8u * p.row_tiles;
-    const uint64_t by_rows = ((uint64_t)a.b.total_new * a.group / (32u * NW) + units) * ((a.c.heads + 7u) / 8u);
+    const uint64_t by_rows = ((uint64_t)a.b.total_new * a.group / (32u * waves) + units) * ((a.c.heads + 7u) / 8u);
     // Few pairs, of a group and a head or of a request, that eight do not divide: XCDs without any, or with one more than others; their row tiles
     // go to the XCDs in turn.  (Us, by pairs / so; requests x tokens,
     // heads, query heads each, prefixes: 59 x 370, 1 x 256, 1, one of 7000 2057 / 359; 85 x 174, 1 x 128, 2, three of 8000 460 / 151; 32 x 300, 4 x 128, 4, one
     // of 4000 844 / 491; 64 x 32, 12 x 128, 4, one of 4000 376 / 304; 32 x 100, 10 x 128, 4, six 461 / 458.)
     const uint64_t pairs = units * a.c.heads;
-    p.spread = KIND != kWhole && pairs % 8u && pairs < 64u;
+    p.spread = kind != kWhole && pairs % 8u && pairs < 64u;
     p.counted = p.spread || by_pairs > by_rows;
-    const uint64_t all = std::min(((uint64_t)a.b.total_new * a.group / (32u * NW) + units) * a.c.heads, pairs * p.row_tiles);
-    const uint64_t groups = (p.spread ? (all + 7u) / 8u : p.counted ? by_rows : by_pairs) * p.splits * 8u;
+    const uint64_t all = std::min(((uint64_t)a.b.total_new * a.group / (32u * waves) + units) * a.c.heads, pairs * p.row_tiles);
+    return (p.spread ? (all + 7u) / 8u : p.counted ? by_rows : by_pairs) * p.splits * 8u;
+}
+static uint32_t parts_waves(const AttendArgs &a) { return a.c.dim <= 128u ? 8u : 4u; }
+static bool parts_fit(const AttendArgs &a, PartsPlan p, Kind kind) { return launchable(groups_of(a, p, kind, parts_waves(a)), 64u * parts_waves(a)); }
+
+template <typename T, int DP, int NW, Kind KIND> static hipError_t parts(const AttendArgs &a, PartsPlan p, hipStream_t s)
+{
+    const uint64_t groups = groups_of(a, p, KIND, NW);
     const uint64_t weight_groups = a.w.data ? (a.b.max_len + 255ull) / 256u * a.c.heads : 0u;
     if (!launchable(groups, 64u * NW) || !launchable(weight_groups, 256)) return hipErrorInvalidConfiguration;
     parts_kernel<T, DP, NW, KIND><<<(uint32_t)groups, 64 * NW, 0, s>>>(a, p);
@@ -901,12 +909,17 @@ __global__ __launch_bounds__(256) void join_shared_kernel(AttendArgs a, SharedPl
 
 hipError_t launch_shared(const AttendArgs &a, const SharedPlan &p, uint32_t dtype, hipStream_t s)
 {
+    const Kind rest = p.tokens || !p.through ? kRest : kThrough;
+    const bool first = a.n_groups && !p.last && !p.through;
+    if ((first && !(p.few_rows ? tokens_apart_fit(a, p.prefix_few, kPrefix) : parts_fit(a, p.prefix, kPrefix))) ||
+        !(p.tokens ? tokens_apart_fit(a, p.few, kRest) : parts_fit(a, p.many, rest)) || (p.last && !parts_fit(a, p.prefix, kLast)))
+        return hipErrorInvalidConfiguration;
     hipError_t e = hipSuccess;
-    if (a.n_groups && !p.last && !p.through) {
+    if (first) {
         e = p.few_rows ? launch_tokens_apart(a, p.prefix_few, kPrefix, dtype, s) : launch_parts_apart(a, p.prefix, kPrefix, dtype, s);
         if (e != hipSuccess) return e;
     }
-    e = p.tokens ? launch_tokens_apart(a, p.few, kRest, dtype, s) : launch_parts_apart(a, p.many, p.through ? kThrough : kRest, dtype, s);
+    e = p.tokens ? launch_tokens_apart(a, p.few, kRest, dtype, s) : launch_parts_apart(a, p.many, rest, dtype, s);
     if (e != hipSuccess) return e;
     if (p.through || (p.tokens && p.few.before)) return hipSuccess;
     if (p.last) {

@@ -853,32 +853,43 @@ template <typename T> static hipError_t tokens(const AttendArgs &a, const Tokens
     return hipGetLastError();
 }
 
+// Workgroups of such a launch, and the wavefronts of one
+static uint64_t groups_apart(const AttendArgs &a, const TokensPlan &p, Kind kind)
+{
+    const uint64_t pairs = (uint64_t)(kind == kListed ? a.b.total_new : kind == kPrefix ? a.n_groups : a.b.n_reqs) * a.c.heads;
+    return (kind != kPrefix ? pairs : (p.by_xcd ? (pairs + 7u) / 8u * 8u : pairs) * p.row_tiles) * p.splits;
+}
+static uint32_t waves_apart(const AttendArgs &a, const TokensPlan &p)
+{
+    return p.waves == 1u ? 1u : p.waves == 4u ? 4u : (uint32_t)waves_of(a.c.dim <= 64u ? 64 : a.c.dim <= 128u ? 128 : 256, p.tile_rows == 16u ? 1 : 2, true);
+}
+bool tokens_apart_fit(const AttendArgs &a, const TokensPlan &p, Kind kind) { return launchable(groups_apart(a, p, kind), 64u * waves_apart(a, p)); }
+
 // A workgroup (or p.splits of them) for each request or new token and head: the rest of contexts behind a prefix, or a prefix and one of its
 // group's row tiles, whose parts another kernel joins, or listed blocks.  Listed blocks of 128 tokens x 8 heads, 64 of 16 tokens each: 269 MB in 49
 // us, 5.5 TB/s in pieces of 128 bytes from all over (the same codes in order 5.8), by a wavefront each; by four 57, three or six 58.
 template <typename T, Kind KIND> static hipError_t tokens_apart(const AttendArgs &a, const TokensPlan &p, hipStream_t s)
 {
-    const uint32_t units = KIND == kListed ? a.b.total_new : KIND == kPrefix ? a.n_groups : a.b.n_reqs;
-    const uint64_t pairs = (uint64_t)units * a.c.heads;
-    const uint64_t groups = (KIND != kPrefix ? pairs : (p.by_xcd ? (pairs + 7u) / 8u * 8u : pairs) * p.row_tiles) * p.splits;
+    const uint64_t groups = groups_apart(a, p, KIND);
+    if (!tokens_apart_fit(a, p, KIND)) return hipErrorInvalidConfiguration;
     auto launch = [&](auto dp_, auto nt_) {
         constexpr int DP = decltype(dp_)::value, NT = decltype(nt_)::value, many = waves_of(DP, NT, true);
-        auto with = [&](auto waves) {
-            constexpr int NW = decltype(waves)::value;
-            if (!launchable(groups, 64 * NW)) return hipErrorInvalidConfiguration;
+        const uint32_t waves = waves_apart(a, p);
+        auto with = [&](auto nw) {
+            constexpr int NW = decltype(nw)::value;
             tokens_kernel<T, DP, NT, true, KIND, NW><<<(uint32_t)groups, 64 * NW, 0, s>>>(a, p);
             return hipGetLastError();
         };
         if constexpr (KIND == kListed || KIND == kRest)
-            if (p.waves == 1u) return with(Int<1>{});
-        return p.waves == 4u || many == 4 ? with(Int<4>{}) : with(Int<many>{});
+            if (waves == 1u) return with(Int<1>{});
+        return waves == 4u ? with(Int<4>{}) : with(Int<many>{});
     };
     const int dp = a.c.dim <= 64 ? 64 : a.c.dim <= 128 ? 128 : 256;
     hipError_t e;
     if (p.tile_rows == 16) e = dp == 64 ? launch(Int<64>{}, Int<1>{}) : dp == 128 ? launch(Int<128>{}, Int<1>{}) : launch(Int<256>{}, Int<1>{});
     else e = dp == 64 ? launch(Int<64>{}, Int<2>{}) : launch(Int<128>{}, Int<2>{});
     if (KIND != kListed || e != hipSuccess || p.splits == 1u) return e;
-    finish_kernel<T, true, KIND><<<dim3(p.join_blocks, units), 256, 0, s>>>(a, p);
+    finish_kernel<T, true, KIND><<<dim3(p.join_blocks, a.b.total_new), 256, 0, s>>>(a, p);
     return hipGetLastError();
 }
 

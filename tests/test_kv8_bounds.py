@@ -219,6 +219,13 @@ def _attend(call, reqs, heads, total, new, length, *more, dim=64, starts=True):
     return B.lib().dmi_kv8_attend_shared(cache, batch, prefix, q, heads, 1.0, out, None, 256, 1 << 62, None)
 
 
+@pytest.mark.parametrize("reqs,heads,total,new,length", [(4096, 64, 4096, 1, 500000), (65535, 256, 65535, 1, 20000), (40000, 256, 1 << 22, 256, 20000)],
+                         ids=["single tokens", "more of them", "prompts"])
+def test_attend_shared_past_the_workgroups_of_a_launch(reqs, heads, total, new, length):
+    """What is behind prefixes takes more workgroups than a launch has, prefixes do not: found before the prefixes' launch."""
+    assert _attend("shared", reqs, heads, total, new, length, 64, starts=new > 1) == B.ERR_INVALID_ARG and b"launch" in B.lib().dmi_last_error()
+
+
 @NO_DEVICE
 @pytest.mark.parametrize("total,heads,n_select", [(1 << 20, 8, 8), (1 << 20, 16, 64), (1 << 22, 8, 8)])
 def test_attend_blocks_of_no_more_workgroups_than_a_launch_has(total, heads, n_select):
