@@ -36,7 +36,8 @@ typedef struct {
 
 /*
  * Writes the new tokens' K, rotated, and V into their places as dmi_kv8_append does (a rotated element is rounded to fp32, and from
- * there on is dmi_kv8_append's x).  With q, the new tokens' queries are rotated into q_out, rounded once to their type.
+ * there on is dmi_kv8_append's x).  With q, the new tokens' queries are rotated into q_out: those
+ * of FP32 in 64 bits and rounded once, those of 16 bits in fp32 (at most three roundings: two products and their sum) and then rounded to their type.
  *   q, q_out  [host, optional, both or neither] total_new rows of n_q_heads heads, of key's dtype.  q_out may be q, or share no element
  *             with q, key or value.  Rows of tokens that no request has, or whose place lies below 0, are left as they were.  n_q_heads need
  *             not be a multiple of n_heads.
@@ -85,7 +86,7 @@ dmi_status_t dmi_kv8_select(const dmi_kv8_t *cache /*[host]*/, const dmi_kv8_bat
  * a row of blocks_dev as many entries are looked at as the token sees blocks; those below 0, and those behind the token's own block, stand for
  * nothing, and a block that is listed twice counts twice.
  *   blocks_dev  [device] int32 [total_new][n_heads][n_select], as dmi_kv8_select writes it
- *   n_q_heads   up to 32 query heads read a head of the cache
+ *   n_q_heads   up to 32 query heads read a head of the cache, up to 16 of more than 128 elements
  */
 uint64_t dmi_kv8_attend_blocks_workspace(const dmi_kv8_t *cache /*[host]*/, const dmi_kv8_batch_t *batch /*[host]*/,
                                          uint32_t n_q_heads, uint32_t n_select);

@@ -859,7 +859,7 @@ hipError_t launch_parts_apart(const AttendArgs &a, const PartsPlan &p, Kind kind
 }
 
 // ---------------------------------------------------------------- contexts behind shared prefixes
-// Prefixes that groups share: 32 prompts, 8700 tokens of 32 query heads behind one of 4000, 545 GFLOP, read by each (kThrough) 670 to 770 us by card;
+// Prefixes that groups share: 32 prompts, 8516 tokens of 32 query heads behind one of 4000, 581 GFLOP, read by each (kThrough) 670 to 770 us by card;
 // read once 700 (kLast), and 88 for their own tokens in front.  64 single tokens behind 8192, 256 rows a head in 26 splits 22 us: 5 until the first
 // tile, 2.4 each of five, 7 to write 27 MB of parts.
 //

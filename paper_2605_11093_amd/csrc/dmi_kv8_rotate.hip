@@ -117,14 +117,16 @@ template <> __device__ __forceinline__ void store8<float>(float *p, const float 
 }
 
 template <typename T> constexpr uint32_t kAheadOf = sizeof(T) == 4 ? 2 : 4;     // sixteens of queries that are asked for before the first is used
-constexpr uint32_t kTableBytes = 32768;         // cosines and sines in LDS: as many tokens as they are room for
+constexpr uint32_t kTableBytes = 32768;         // cosines and sines in LDS: as many tokens as there is room for
 
 // A workgroup per block that new tokens reach and a.each of its items: K of a head, V of a head, queries of a.q_each tokens (which lie in one
-// piece).  Cosines and sines of the block's tokens are computed once into LDS, in 64 bits (angles of far positions have no others), and every
-// item takes them from there; a wavefront has an item at a time, a lane the same sixteen of every few rows.  As in append_kernel the scale of K
+// piece).  Cosines and sines of the block's tokens are computed into LDS, in 64 bits (angles of far positions have no others), and every
+// item takes them from there: once where those of all tokens fit in kTableBytes, else a part of the tokens at a time, again for every four items and
+// each of their two passes (16 prompts of 1024 tokens, 369 MB: 4 heads x 256, blocks of 32 108 us, of 64 157; 8 x 128, of 64 106, of 128 155, of 1024 448).
+// A wavefront has an item at a time, a lane the same sixteen of every few rows.  As in append_kernel the scale of K
 // and V wants the largest of all the block's new elements first; what a lane can hold of them it does.
 //
-// Bound by memory where there is much: 32 prompts, 38600 tokens, K and V of 8 heads x 128 and queries of 32 in bf16, 857 MB in 180 us (4.8 TB/s;
+// Bound by memory where there is much: 32 prompts, 38014 tokens, K and V of 8 heads x 128 and queries of 32 in bf16, 857 MB in 180 us (4.8 TB/s;
 // a copy reaches 5.2); single tokens by the chain of lengths, table, cosines, rows: 7.3 us.  Measured and not better for the prompts: one
 // sixteen of queries under way at a time 268, four wavefronts a SIMD (spills) 362, three sixteens of K or V held 205, queries by head 186.
 template <typename T, bool NEIGHBOURS>
@@ -370,7 +372,7 @@ struct Extremes {
 
 // A wavefront per block that new tokens reach and 64 places of its heads' rows, a lane 16 elements of every token (of every few, where the
 // heads have fewer places): what the wavefront reads of a token lies in one piece where heads follow each other, and no extreme has to cross
-// lanes.  Bound by memory where there is much: 32 prompts, 2400 blocks of 16 x 8 x 128, 40 MB in 10.5 us (3.8 TB/s; 21 us with a wavefront a
+// lanes.  Bound by memory where there is much: 32 prompts, 2200 blocks of 16 x 8 x 128, 40 MB in 10.5 us (3.8 TB/s; 21 us with a wavefront a
 // head, whose lanes shared a token's elements: vector instructions); single tokens of 128 requests 4.2 us, loads that wait for each other.
 __global__ __launch_bounds__(256) void bound_kernel(BoundArgs a)
 {
